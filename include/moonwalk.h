@@ -310,6 +310,117 @@ mw_status mw_gemm_split_bf16_static(const float* A, int32_t a_mn, const float* B
                                     float* D, int32_t M, int32_t N, int32_t K, int32_t terms,
                                     void* stream);
 
+/* ---- layers in front of a net, and the optimiser's step (extensions: the paper has no counterpart) --
+ *
+ * A stack of sequence-mixing blocks (projection -> gated recurrence -> gated, normed residual sum) can
+ * stand in front of a net: mw_input_cotangent's g0 = dL/dx_0 is then the cotangent of the stack's output,
+ * and the backward calls below carry it on.  Like the net itself they keep few activations: the
+ * recurrence keeps its state at every MW_SCAN_STATE_EVERY-th step, the residual sum two numbers a row.
+ * dtype: 1 = float, 2 = bf16 (the tensors named per call); arithmetic, states, norms, statistics and the
+ * gradients of per-channel weights are float.  Results do not depend on scheduling: repeated calls give
+ * the same bits.  Sizes of zero (batch, length, rows) are legal: nothing is computed, sums are zero. */
+
+/* Gated linear recurrence over time, per channel:
+ *   a_t = sigmoid(f_t),   u_t = 1 - a_t (MW_SCAN_COMPLEMENT) or sqrt(1 - a_t^2) (MW_SCAN_ENERGY)
+ *   h_t = r_t a_t h_{t-1} + u_t v_t,   y_t = h_t,   r_t = 0 where reset[b][t] != 0, else 1
+ * for t < lengths[b]; from there on the state is held, y_t = 0, and nothing of v, f, dy is read. */
+typedef enum { MW_SCAN_COMPLEMENT = 0, MW_SCAN_ENERGY = 1 } mw_scan_gate;
+#define MW_SCAN_STATE_EVERY 16
+typedef struct {
+  int32_t batch, length, channels;
+  int32_t dtype;              /* of v, f, y, dy, dv, df */
+  int32_t input_gate;         /* mw_scan_gate */
+  int32_t reserved;           /* 0 */
+  /* elements between sequences and between steps (channels are contiguous): windows of wider rows,
+   * time-major arrays.  A pair of zeros means [batch][length][channels]. */
+  int64_t v_batch, v_time, f_batch, f_time;
+  int64_t y_batch, y_time;    /* y, and dy in the backward call */
+  int64_t dv_batch, dv_time, df_batch, df_time;
+} mw_gated_scan_desc;
+
+/* Bytes of the `states` array: float [batch][ceil(length / MW_SCAN_STATE_EVERY)][channels]; entry i is
+ * the state before step i * MW_SCAN_STATE_EVERY. */
+mw_status mw_gated_scan_states_bytes(const mw_gated_scan_desc* desc, size_t* bytes);
+/* reset: uint8 [batch][length] or NULL; lengths: int32 [batch] (values are clamped to 0..length) or
+ * NULL; h0: float [batch][channels] or NULL (zero); h_last: float [batch][channels] or NULL, may be h0
+ * itself; states: see above, or NULL (no backward call follows).  length = 1 is the serving step. */
+mw_status mw_gated_scan_forward(const mw_gated_scan_desc* desc, const void* v, const void* f,
+                                const uint8_t* reset, const int32_t* lengths, const float* h0, void* y,
+                                float* h_last, float* states, void* stream);
+/* From dy (or NULL: zero) and dh_last (or NULL: zero): dv, df (zero from lengths[b] on) and dh0 (or
+ * NULL).  Inputs as in the forward call; states as it left them. */
+mw_status mw_gated_scan_backward(const mw_gated_scan_desc* desc, const void* v, const void* f,
+                                 const uint8_t* reset, const int32_t* lengths, const float* states,
+                                 const void* dy, const float* dh_last, void* dv, void* df, float* dh0,
+                                 void* stream);
+
+/* Residual sum of a block with the norms around it, per row of `cols` channels:
+ *   p  = w_post * b / sqrt(mean(b^2) + eps)         (w_post NULL: p = b)
+ *   x' = x + scale * z sigmoid(z) * p               (z NULL: no gate; scale NULL: 1; b NULL: x' = x)
+ *   n  = w_pre * x' / sqrt(mean(x'^2) + eps)        (w_pre NULL: no n)
+ * x' is stored as x_out; n is formed from it before that rounding. */
+typedef struct {
+  int64_t rows;
+  int32_t cols;               /* 1..32768 */
+  int32_t dtype;              /* of x, b, z, x_out, n and their cotangents */
+  double eps;                 /* > 0 */
+  int64_t ld_x, ld_b, ld_z;   /* elements between rows of x, b, z (0 = cols); x_out, n and all */
+} mw_residual_norm_desc;      /* cotangents are dense [rows][cols]                              */
+
+/* x_out (may be x itself where ld_x = cols, or NULL), n (NULL exactly where w_pre is NULL), weights
+ * float[cols]; inv_rms: float [2][rows] = 1/sqrt(mean(b^2)+eps), 1/sqrt(mean(x'^2)+eps) for the
+ * backward call, or NULL. */
+mw_status mw_residual_norm_forward(const mw_residual_norm_desc* desc, const void* x, const void* b,
+                                   const void* z, const float* w_post, const float* scale,
+                                   const float* w_pre, void* x_out, void* n, float* inv_rms, void* stream);
+mw_status mw_residual_norm_scratch_bytes(const mw_residual_norm_desc* desc, size_t* bytes);
+/* From dx_out and dn (either may be NULL: zero): dx (may be dx_out itself), db, dz, and the sums over
+ * rows dw_post, dscale, dw_pre (float[cols]); any output may be NULL.  x, b, z, weights as in the
+ * forward call, inv_rms as it left them.  scratch: 256-byte aligned device memory. */
+mw_status mw_residual_norm_backward(const mw_residual_norm_desc* desc, const void* x, const void* b,
+                                    const void* z, const float* w_post, const float* scale,
+                                    const float* w_pre, const float* inv_rms, const void* dx_out,
+                                    const void* dn, void* dx, void* db, void* dz, float* dw_post,
+                                    float* dscale, float* dw_pre, void* scratch, size_t scratch_bytes,
+                                    void* stream);
+
+/* Orthogonalised update of `count` weight matrices [rows][cols] of one shape:
+ *   M' = beta M + G,   U = G + beta M' (nesterov) or M',   X_0 = U / ||U||_F  (0 where U = 0)
+ *   `steps` times, with S the shorter side's Gram matrix X X^T (or X^T X):  X <- (c0 + c1 S + c2 S^2) X
+ *   W' = (1 - lr * weight_decay) W - lr * scale * X
+ * The polynomial drives every singular value of U that is not tiny towards 1, so a step moves all
+ * directions of W alike; weights that started near a multiple of an orthogonal matrix stay in the
+ * domain of the Newton-Schulz inverse far longer than under a plain gradient step.  A non-finite entry
+ * of U makes its own matrix's result NaN and no other's. */
+typedef struct {
+  int32_t rows, cols, count;
+  int32_t prec;               /* MW_F32: W float; MW_BF16_F32ACC: W bf16.  G and M are float in both */
+  int32_t steps;              /* 0 = 5; at most 16 */
+  int32_t nesterov;           /* 1: U = G + beta M';  0: U = M' */
+  int32_t terms;              /* operand terms of the products: 1 (about 1e-3 of X), 2 (fp32-accurate),
+                                 0 = 2 for MW_F32, 1 for MW_BF16_F32ACC */
+  int32_t reserved;           /* 0 */
+  double coef[3];             /* c0, c1, c2; all zero = 3.4445, -4.7750, 2.0315 */
+} mw_orth_desc;
+typedef struct mw_orth mw_orth; /* opaque, host side; owns no device memory */
+mw_status mw_orth_create(const mw_orth_desc* desc, mw_orth** out);
+void mw_orth_destroy(mw_orth* plan);
+mw_status mw_orth_workspace_bytes(const mw_orth* plan, size_t* bytes);
+/* Host arrays of `count` DEVICE pointers, matrices dense and row-major: grads, momentum, momentum_out
+ * float; params, params_out storage type of `prec`.  momentum_out[i] may be momentum[i], params_out[i]
+ * may be params[i].  workspace: device, 256-byte aligned.  A bounded wait that runs out inside the
+ * launch is recorded in the workspace (mw_orth_status). */
+mw_status mw_orth_step(mw_orth* plan, const void* const* params, const void* const* grads,
+                       const void* const* momentum, void* const* params_out, void* const* momentum_out,
+                       double lr, double beta, double weight_decay, double scale, void* workspace,
+                       size_t workspace_bytes, void* stream);
+/* The projection alone: out[i] = X of U = in[i], both in the storage type of `prec`; out[i] may be in[i]. */
+mw_status mw_orth_project(mw_orth* plan, const void* const* in, void* const* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+/* Synchronise `stream`, return the first device-side error recorded in the workspace by the last call
+ * (MW_OK if none). */
+mw_status mw_orth_status(const mw_orth* plan, const void* workspace, void* stream);
+
 /* ---- whole step from host buffers, and measurement hooks --------------------------------- */
 
 /* One Moonwalk gradient step (Algorithm 1 with Phases I-II in front) whose per-step inputs

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -45,6 +45,22 @@ class NetOpts(C.Structure):
                 ("conv_vijp_iters", C.c_int32), ("backend", C.c_int32),
                 ("inverse_iters", C.c_int32), ("resident_inverse", C.c_int32),
                 ("warm_inverse", C.c_int32), ("frag_block", C.c_int32), ("lu_param", C.c_int32)]
+
+
+class GatedScanDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "length", "channels", "dtype", "input_gate", "reserved")] + \
+               [(n, C.c_int64) for n in ("v_batch", "v_time", "f_batch", "f_time", "y_batch", "y_time",
+                                         "dv_batch", "dv_time", "df_batch", "df_time")]
+
+
+class ResidualNormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_double),
+                ("ld_x", C.c_int64), ("ld_b", C.c_int64), ("ld_z", C.c_int64)]
+
+
+class OrthDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "cols", "count", "prec", "steps", "nesterov", "terms",
+                                         "reserved")] + [("coef", C.c_double * 3)]
 
 
 _lib = None
@@ -95,6 +111,20 @@ def lib() -> C.CDLL:
         L.mw_set_cooperative_launch.restype = i32
         L.mw_set_merge_orders.argtypes = [i32]
         L.mw_set_merge_orders.restype = i32
+        scan, norm, orth = C.POINTER(GatedScanDesc), C.POINTER(ResidualNormDesc), C.POINTER(OrthDesc)
+        L.mw_gated_scan_states_bytes.argtypes = [scan, C.POINTER(sz)]
+        L.mw_gated_scan_forward.argtypes = [scan] + [vp] * 9
+        L.mw_gated_scan_backward.argtypes = [scan] + [vp] * 11
+        L.mw_residual_norm_forward.argtypes = [norm] + [vp] * 10
+        L.mw_residual_norm_scratch_bytes.argtypes = [norm, C.POINTER(sz)]
+        L.mw_residual_norm_backward.argtypes = [norm] + [vp] * 16 + [sz, vp]
+        L.mw_orth_create.argtypes = [orth, C.POINTER(vp)]
+        L.mw_orth_destroy.argtypes = [vp]
+        L.mw_orth_destroy.restype = None
+        L.mw_orth_workspace_bytes.argtypes = [vp, C.POINTER(sz)]
+        L.mw_orth_step.argtypes = [vp] + [C.POINTER(vp)] * 5 + [C.c_double] * 4 + [vp, sz, vp]
+        L.mw_orth_project.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), vp, sz, vp]
+        L.mw_orth_status.argtypes = [vp, vp, vp]
         L.mw_profile_begin.argtypes = []
         L.mw_profile_begin.restype = None
         L.mw_profile_end.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64),
@@ -443,6 +473,253 @@ def gemm_split_bf16_static(A, B, a_mn: bool, b_mn: bool, terms: int, stream=None
                                            int(terms), _stream_handle(stream)),
            "mw_gemm_split_bf16_static")
     return D
+
+
+# ---- layers in front of a net, and the optimiser's step --------------------------------------
+INPUT_GATE = {"complement": 0, "energy": 1}
+SCAN_STATE_EVERY = 16
+
+
+def _operand_dtype(t, where: str) -> int:
+    import torch
+    codes = {torch.float32: 1, torch.bfloat16: 2}
+    if t.dtype not in codes:
+        raise TypeError(f"{where}: float32 or bfloat16 tensors, got {t.dtype}")
+    return codes[t.dtype]
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _same_device(ref, named, where: str):
+    for name, t in named.items():
+        if t is not None:
+            _need(t.device == ref.device, f"{where}: {name} is on {t.device}, not on {ref.device}")
+
+
+def _check_float(t, shape, name, device):
+    """Optional float32 contiguous tensor of a given shape."""
+    import torch
+    if t is not None:
+        _need(t.dtype == torch.float32 and tuple(t.shape) == tuple(shape) and t.is_contiguous() and
+              t.device == device, f"{name}: a contiguous float32 tensor of shape {tuple(shape)} on {device}")
+
+
+def _scan_call(v, f, reset, lengths, input_gate, named):
+    """Checks of the tensors every scan call shares; `named` {name: [B, T, D] tensor like v or None}."""
+    import torch
+    _need(v.dim() == 3, "gated_scan: v is [batch, length, channels]")
+    if input_gate not in INPUT_GATE:
+        raise ValueError(f"gated_scan: input_gate is one of {sorted(INPUT_GATE)}")
+    B, T, D = v.shape
+    d = GatedScanDesc(B, T, D, _operand_dtype(v, "gated_scan"), INPUT_GATE[input_gate], 0)
+    # (a tensor without elements, or of one step or sequence, has strides that mean nothing)
+    for name, field, t in [("v", "v", v), ("f", "f", f)] + named:
+        if t is None:
+            continue
+        _need(t.dtype == v.dtype and tuple(t.shape) == (B, T, D), f"gated_scan: {name} has the type and shape of v")
+        _need(D <= 1 or t.stride(2) == 1 or t.numel() == 0, f"gated_scan: {name}'s channels are contiguous")
+        if t.numel():
+            setattr(d, field + "_batch", t.stride(0) if B > 1 else T * D)
+            setattr(d, field + "_time", t.stride(1) if T > 1 else D)
+    if reset is not None:
+        _need(reset.dtype in (torch.uint8, torch.bool) and tuple(reset.shape) == (B, T) and reset.is_contiguous(),
+              "gated_scan: reset is a contiguous uint8 or bool [batch, length]")
+    if lengths is not None:
+        _need(lengths.dtype == torch.int32 and tuple(lengths.shape) == (B,) and lengths.is_contiguous(),
+              "gated_scan: lengths is a contiguous int32 [batch]")
+    _same_device(v, dict({n: t for n, _, t in named}, f=f, reset=reset, lengths=lengths), "gated_scan")
+    return d
+
+
+def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "complement", keep_states=False,
+               y=None, h_last=None, stream=None):
+    """Gated linear recurrence h_t = r_t sigmoid(f_t) h_{t-1} + u_t v_t over dim 1 of [batch, length,
+    channels] tensors (float32 or bfloat16; rows may be windows of wider ones).  Returns (y, h_last),
+    with keep_states=True (y, h_last, states) for gated_scan_backward.  One step (length 1) with
+    h0 = h_last = the cached state is the serving form."""
+    import torch
+    if y is None:
+        y = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    d = _scan_call(v, f, reset, lengths, input_gate, [("y", "y", y)])
+    B, T, D = v.shape
+    if h_last is None:
+        h_last = torch.empty((B, D), dtype=torch.float32, device=v.device)
+    _check_float(h0, (B, D), "gated_scan: h0", v.device)
+    _check_float(h_last, (B, D), "gated_scan: h_last", v.device)
+    states = None
+    if keep_states:
+        states = torch.empty((B, -(-T // SCAN_STATE_EVERY), D), dtype=torch.float32, device=v.device)
+    _check(lib().mw_gated_scan_forward(C.byref(d), _ptr(v), _ptr(f), _ptr(reset), _ptr(lengths), _ptr(h0), _ptr(y),
+                                       _ptr(h_last), _ptr(states), _stream_handle(stream)), "mw_gated_scan_forward")
+    return (y, h_last, states) if keep_states else (y, h_last)
+
+
+def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_last=None,
+                        input_gate: str = "complement", dv=None, df=None, stream=None):
+    """(dv, df, dh0) of gated_scan from the cotangents of y and h_last (either may be None) and the
+    states that the forward call kept (they include h0, which is accepted for symmetry)."""
+    import torch
+    if dv is None:
+        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    if df is None:
+        df = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    d = _scan_call(v, f, reset, lengths, input_gate, [("dy", "y", dy), ("dv", "dv", dv), ("df", "df", df)])
+    B, T, D = v.shape
+    _check_float(dh_last, (B, D), "gated_scan_backward: dh_last", v.device)
+    _need(states is not None, "gated_scan_backward: states come from gated_scan(..., keep_states=True)")
+    _check_float(states, (B, -(-T // SCAN_STATE_EVERY), D), "gated_scan_backward: states", v.device)
+    dh0 = torch.empty((B, D), dtype=torch.float32, device=v.device)
+    _check(lib().mw_gated_scan_backward(C.byref(d), _ptr(v), _ptr(f), _ptr(reset), _ptr(lengths), _ptr(states),
+                                        _ptr(dy), _ptr(dh_last), _ptr(dv), _ptr(df), _ptr(dh0),
+                                        _stream_handle(stream)), "mw_gated_scan_backward")
+    return dv, df, dh0
+
+
+def _norm_call(x, b, z, w_post, scale, w_pre, eps, dense):
+    _need(x.dim() == 2, "residual_norm: x is [rows, cols]")
+    R, D = x.shape
+    d = ResidualNormDesc(R, D, _operand_dtype(x, "residual_norm"), float(eps), 0, 0, 0)
+    for name, t in (("x", x), ("b", b), ("z", z)):
+        if t is None:
+            continue
+        _need(t.dtype == x.dtype and tuple(t.shape) == (R, D), f"residual_norm: {name} has the type and shape of x")
+        _need(D <= 1 or t.stride(1) == 1 or t.numel() == 0, f"residual_norm: {name}'s columns are contiguous")
+        setattr(d, "ld_" + name, t.stride(0) if R > 1 and t.numel() else D)
+    for name, t in dense.items():
+        if t is not None:
+            _need(t.dtype == x.dtype and tuple(t.shape) == (R, D) and t.is_contiguous(),
+                  f"residual_norm: {name} is contiguous, of x's type and shape")
+    for name, t in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
+        _check_float(t, (D,), "residual_norm: " + name, x.device)
+    _same_device(x, dict(dense, b=b, z=z), "residual_norm")
+    return d
+
+
+def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: float = 1e-6, keep_rms=False,
+                  x_out=None, n=None, stream=None):
+    """x' = x + scale silu(z) rmsnorm(b; w_post) and n = rmsnorm(x'; w_pre) on [rows, cols] tensors; what
+    is None is left out.  Returns (x', n), with keep_rms=True (x', n, inv_rms) for the backward call."""
+    import torch
+    if x_out is None:
+        x_out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if n is None and w_pre is not None:
+        n = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    d = _norm_call(x, b, z, w_post, scale, w_pre, eps, {"x_out": x_out, "n": n})
+    rms = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device) if keep_rms else None
+    _check(lib().mw_residual_norm_forward(C.byref(d), _ptr(x), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale),
+                                          _ptr(w_pre), _ptr(x_out), _ptr(n), _ptr(rms), _stream_handle(stream)),
+           "mw_residual_norm_forward")
+    return (x_out, n, rms) if keep_rms else (x_out, n)
+
+
+class ResidualNormGrads(NamedTuple):
+    dx: object
+    db: object
+    dz: object
+    dw_post: object
+    dscale: object
+    dw_pre: object
+
+
+def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre=None, eps: float = 1e-6,
+                           dx_out=None, dn=None, stream=None) -> ResidualNormGrads:
+    """Gradients of residual_norm from the cotangents of x' and n (either may be None); the gradients of
+    what was left out are None."""
+    import torch
+
+    def like(t):
+        return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+    d = _norm_call(x, b, z, w_post, scale, w_pre, eps, {"dx_out": dx_out, "dn": dn})
+    _check_float(inv_rms, (2, x.shape[0]), "residual_norm_backward: inv_rms", x.device)
+    g = ResidualNormGrads(*(like(t) for t in (x, b, z, w_post, scale, w_pre)))
+    need = C.c_size_t()
+    _check(lib().mw_residual_norm_scratch_bytes(C.byref(d), C.byref(need)), "mw_residual_norm_scratch_bytes")
+    scratch = torch.empty(int(need.value), dtype=torch.uint8, device=x.device)
+    _check(lib().mw_residual_norm_backward(
+        C.byref(d), _ptr(x), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre), _ptr(inv_rms), _ptr(dx_out),
+        _ptr(dn), _ptr(g.dx), _ptr(g.db), _ptr(g.dz), _ptr(g.dw_post), _ptr(g.dscale), _ptr(g.dw_pre), _ptr(scratch),
+        scratch.numel(), _stream_handle(stream)), "mw_residual_norm_backward")
+    return g
+
+
+class Orth:
+    """Host-side handle of the orthogonalised update (mw_orth) of `count` weights of one shape.  Owns no
+    device memory."""
+
+    def __init__(self, rows: int, cols: int, count: int = 1, prec: str = "f32", steps: int = 0,
+                 nesterov: bool = True, terms: int = 0, coef=(0.0, 0.0, 0.0)):
+        self._h = C.c_void_p()
+        self.shape, self.count, self.prec = (int(rows), int(cols)), int(count), prec
+        d = OrthDesc(int(rows), int(cols), int(count), PREC[prec], int(steps), int(bool(nesterov)), int(terms), 0,
+                     (C.c_double * 3)(*coef))
+        _check(lib().mw_orth_create(C.byref(d), C.byref(self._h)), "mw_orth_create")
+
+    def close(self):
+        if self._h:
+            lib().mw_orth_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def storage_dtype(self):
+        import torch
+        return {"f32": torch.float32, "bf16_f32acc": torch.bfloat16}[self.prec]
+
+    def workspace_bytes(self) -> int:
+        n = C.c_size_t()
+        _check(lib().mw_orth_workspace_bytes(self._h, C.byref(n)), "mw_orth_workspace_bytes")
+        return int(n.value)
+
+    def alloc_workspace(self, device="cuda"):
+        import torch
+        return torch.empty(self.workspace_bytes() + 256, dtype=torch.uint8, device=device)
+
+    def _list(self, tensors, dtype, name):
+        tensors = list(tensors)
+        _need(len(tensors) == self.count, f"Orth: {name} has {self.count} tensors")
+        for t in tensors:
+            _need(t.dtype == dtype and tuple(t.shape) == self.shape and t.is_contiguous(),
+                  f"Orth: {name} are contiguous {dtype} tensors of shape {self.shape}")
+        return _ptr_array(tensors)
+
+    def step(self, params, grads, momentum, workspace, lr: float, beta: float = 0.95, weight_decay: float = 0.0,
+             scale: float = 1.0, params_out=None, momentum_out=None, stream=None):
+        """M <- beta M + G, W <- (1 - lr weight_decay) W - lr scale X; in place unless outputs are given."""
+        import torch
+        params_out = params if params_out is None else params_out
+        momentum_out = momentum if momentum_out is None else momentum_out
+        st, f32 = self.storage_dtype(), torch.float32
+        wp, wb = Net._ws(workspace)
+        _check(lib().mw_orth_step(
+            self._h, self._list(params, st, "params"), self._list(grads, f32, "grads"),
+            self._list(momentum, f32, "momentum"), self._list(params_out, st, "params_out"),
+            self._list(momentum_out, f32, "momentum_out"), float(lr), float(beta), float(weight_decay), float(scale),
+            wp, wb, _stream_handle(stream)), "mw_orth_step")
+        return params_out
+
+    def project(self, mats, workspace, out=None, stream=None):
+        """The orthogonalised factor X of every matrix, in the storage type."""
+        import torch
+        st = self.storage_dtype()
+        if out is None:
+            out = [torch.empty_like(t) for t in mats]
+        wp, wb = Net._ws(workspace)
+        _check(lib().mw_orth_project(self._h, self._list(mats, st, "mats"), self._list(out, st, "out"), wp, wb,
+                                     _stream_handle(stream)), "mw_orth_project")
+        return out
+
+    def status(self, workspace, stream=None) -> int:
+        """Waits for the stream; the first device-side error of the last call on this workspace (0: none)."""
+        wp, _ = Net._ws(workspace)
+        return int(lib().mw_orth_status(self._h, wp, _stream_handle(stream)))
 
 
 # ---- moving a synthetic problem onto the device -------------------------------------------
