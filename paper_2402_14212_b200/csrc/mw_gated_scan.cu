@@ -28,12 +28,14 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
 // a = sigmoid(f) and w = 1 - a, each to full relative accuracy at either end (one exponential, one
-// reciprocal: 1 - a formed by subtraction would lose the slow channels, where a is close to 1)
+// reciprocal: 1 - a formed by subtraction would lose the slow channels, where a is close to 1).
+// f below -80 counts as -80 (a = 2e-35), which keeps the exponential finite; NaN stays NaN.
 __device__ __forceinline__ void gate_of(float f, float& a, float& w) {
-  const float e = __expf(-fabsf(f)), big = __fdividef(1.f, 1.f + e), small = e * big;
-  a = f >= 0.f ? big : small;
-  w = f >= 0.f ? small : big;
-  if (isnan(f)) a = w = f;
+  float g;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(g) : "f"(f), "f"(-80.f));
+  const float e = __expf(-g);
+  a = __fdividef(1.f, 1.f + e);
+  w = e * a;
 }
 template <int GATE>
 __device__ __forceinline__ float input_of(float a, float w) {
@@ -127,12 +129,334 @@ scan_walk_back_kernel(const ScanArgs p) {
   if (p.dh0) p.dh0[bc] = g;
 }
 
+// ---------------------------------------------------------------------------------------------
+// Long sequences.  A step is the affine map h -> a h + b, and maps compose associatively, so time is
+// cut three ways: a thread walks kEvery steps of its channel(s) held in registers, the W warps of a
+// block cover W * kEvery consecutive steps, and the C blocks of a cluster cover C such pieces in a
+// row.  Each level hands its composed map (P, H) to the next one through shared memory (its own, then
+// that of the cluster's blocks), takes the state it starts from, and walks its steps again with it:
+// every tensor crosses HBM once however the time axis is cut, and no block waits for another outside
+// its cluster.  The cluster then moves on to the next C * W * kEvery steps, with the loads of those
+// already under way.
+// ---------------------------------------------------------------------------------------------
+constexpr int kScanWarps = 8;
+constexpr int kMaxCluster = 16;
+
+// what one lane of a row holds: VEC channels of type T
+template <typename T, int VEC>
+struct Lane;
+template <>
+struct Lane<float, 1> {
+  using Raw = float;
+  static __device__ __forceinline__ Raw zero() { return 0.f; }
+  static __device__ __forceinline__ void get(Raw r, float (&v)[1]) { v[0] = r; }
+  static __device__ __forceinline__ Raw put(const float (&v)[1]) { return v[0]; }
+};
+template <>
+struct Lane<__nv_bfloat16, 1> {
+  using Raw = unsigned short;
+  static __device__ __forceinline__ Raw zero() { return 0; }
+  static __device__ __forceinline__ void get(Raw r, float (&v)[1]) { v[0] = __uint_as_float((uint32_t)r << 16); }
+  static __device__ __forceinline__ Raw put(const float (&v)[1]) { return __bfloat16_as_ushort(__float2bfloat16_rn(v[0])); }
+};
+template <>
+struct Lane<__nv_bfloat16, 2> {
+  using Raw = uint32_t;
+  static __device__ __forceinline__ Raw zero() { return 0u; }
+  static __device__ __forceinline__ void get(Raw r, float (&v)[2]) {
+    v[0] = __uint_as_float(r << 16);
+    v[1] = __uint_as_float(r & 0xffff0000u);
+  }
+  static __device__ __forceinline__ Raw put(const float (&v)[2]) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// 8 bytes into the shared memory of block `rank` of the cluster, at this block's address `p`
+__device__ __forceinline__ void store_to_rank(float2* p, int rank, float2 v) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(r), "f"(v.x), "f"(v.y) : "memory");
+}
+
+// no block's shared memory is written by another before that block runs
+__device__ __forceinline__ void cluster_start(int C) {
+  if (C > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+}
+
+// h -> P h + H.  With CUT a zero P drops h whatever it is: infinities and NaN of what came before a
+// reset do not reach the steps after it.
+template <bool CUT>
+__device__ __forceinline__ float affine(float P, float h, float H) {
+  return CUT && P == 0.f ? H : fmaf(P, h, H);
+}
+
+// Composes the maps of the block's warps and of the cluster's blocks.  In: this thread's map (P, H).
+// Out: the state its steps start from, given the state `carry` the cluster's piece starts from;
+// `carry` becomes the state after the piece.  REVERSE: the pieces follow one another from the last
+// warp of the last block to the first (the cotangent's direction).
+template <int VEC, bool CUT, bool REVERSE>
+struct Exchange {
+  float2 warp_map[2][kScanWarps][VEC][32];
+  float2 block_map[2][kMaxCluster][VEC][32];
+
+  __device__ __forceinline__ void run(const float (&P)[VEC], const float (&H)[VEC], float (&carry)[VEC],
+                                      float (&start)[VEC], int flip, int rank, int C) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) warp_map[flip][warp][i][lane] = make_float2(P[i], H[i]);
+    __syncthreads();
+    float pe[VEC], he[VEC], pt[VEC], ht[VEC];     // before this warp, and of the whole block
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      pt[i] = 1.f;
+      ht[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kScanWarps; ++k) {
+        const int w = REVERSE ? kScanWarps - 1 - k : k;
+        if (w == warp) { pe[i] = pt[i]; he[i] = ht[i]; }
+        const float2 m = warp_map[flip][w][i][lane];
+        ht[i] = affine<CUT>(m.x, ht[i], m.y);
+        pt[i] *= m.x;
+      }
+    }
+    if (C > 1) {
+      for (int r = warp; r < C; r += kScanWarps)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) store_to_rank(&block_map[flip][rank][i][lane], r, make_float2(pt[i], ht[i]));
+      cluster_arrive();
+      cluster_wait();
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float h = carry[i];
+        for (int k = 0; k < C; ++k) {
+          const int r = REVERSE ? C - 1 - k : k;
+          if (r == rank) start[i] = h;
+          const float2 m = block_map[flip][r][i][lane];
+          h = affine<CUT>(m.x, h, m.y);
+        }
+        carry[i] = h;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        start[i] = carry[i];
+        carry[i] = affine<CUT>(pt[i], carry[i], ht[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) start[i] = affine<CUT>(pe[i], start[i], he[i]);
+  }
+};
+
+// grid (C, channel blocks, batch), clusters of C blocks along x
+template <typename T, int VEC, int GATE, bool CUT>
+__global__ void __launch_bounds__(32 * kScanWarps, 2)
+scan_chunk_kernel(const ScanArgs p) {
+  using L = Lane<T, VEC>;
+  using Raw = typename L::Raw;
+  __shared__ Exchange<VEC, CUT, false> ex;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
+  const int c = (blockIdx.y * 32 + lane) * VEC;
+  const bool live = c < p.D;
+  const int n = length_of(p, b);
+  const int piece = C * kScanWarps * kEvery;
+  const T* vb = static_cast<const T*>(p.v) + b * p.v_b + c;
+  const T* fb = static_cast<const T*>(p.f) + b * p.f_b + c;
+  const int64_t nst = (p.T + kEvery - 1) / kEvery;
+  Raw rv[kEvery], rf[kEvery];
+  // (steps are the same for all lanes: the tests on t are warp-uniform)
+  auto load = [&](int t0) {
+    const T* v = vb + t0 * p.v_t;
+    const T* f = fb + t0 * p.f_t;
+#pragma unroll
+    for (int j = 0; j < kEvery; ++j) {
+      rv[j] = rf[j] = L::zero();
+      if (live && t0 + j < n) {
+        rv[j] = __ldcs(reinterpret_cast<const Raw*>(v));
+        rf[j] = __ldcs(reinterpret_cast<const Raw*>(f));
+      }
+      v += p.v_t;
+      f += p.f_t;
+    }
+  };
+  int t0 = (rank * kScanWarps + warp) * kEvery;
+  load(t0);
+  cluster_start(C);
+  float carry[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) carry[i] = p.h0 && live ? p.h0[(int64_t)b * p.D + c + i] : 0.f;
+  int flip = 0;
+  for (int base = 0; base < p.T; base += piece, t0 += piece, flip ^= 1) {
+    float a[kEvery][VEC], in[kEvery][VEC], P[VEC], H[VEC], h[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) { P[i] = 1.f; H[i] = 0.f; }
+#pragma unroll
+    for (int j = 0; j < kEvery; ++j) {
+      float v[VEC], f[VEC];
+      L::get(rv[j], v);
+      L::get(rf[j], f);
+      const bool on = t0 + j < n;
+      const bool cut = CUT && on && p.reset[(int64_t)b * p.T + t0 + j] != 0;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float w;
+        gate_of(f[i], a[j][i], w);
+        in[j][i] = input_of<GATE>(a[j][i], w) * v[i];
+        if (CUT && cut) a[j][i] = 0.f;
+        if (!on) { a[j][i] = 1.f; in[j][i] = 0.f; }
+        H[i] = affine<CUT>(a[j][i], H[i], in[j][i]);
+        P[i] *= a[j][i];
+      }
+    }
+    if (base + piece < p.T) load(t0 + piece);
+    ex.run(P, H, carry, h, flip, rank, C);
+    if (live && t0 < p.T) {
+      if (p.states) {
+        float* st = p.states + (b * nst + t0 / kEvery) * p.D + c;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) st[i] = h[i];
+      }
+      T* y = static_cast<T*>(p.y) + b * p.y_b + c + t0 * p.y_t;
+#pragma unroll
+      for (int j = 0; j < kEvery; ++j) {
+        float o[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          h[i] = affine<CUT>(a[j][i], h[i], in[j][i]);
+          o[i] = t0 + j < n ? h[i] : 0.f;
+        }
+        if (t0 + j < p.T) __stcs(reinterpret_cast<Raw*>(y), L::put(o));
+        y += p.y_t;
+      }
+    }
+  }
+  if (p.h_last && live && rank == 0 && warp == 0)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) p.h_last[(int64_t)b * p.D + c + i] = carry[i];
+}
+
+// The cotangent runs from the end: a step maps G (the cotangent of the state after it) to
+// r a (G + dy), the cotangent of the state before it.  The states before each thread's steps were
+// kept by the forward pass, so h needs no exchange.
+template <typename T, int VEC, int GATE, bool CUT>
+__global__ void __launch_bounds__(32 * kScanWarps)
+scan_chunk_back_kernel(const ScanArgs p) {
+  using L = Lane<T, VEC>;
+  using Raw = typename L::Raw;
+  __shared__ Exchange<VEC, CUT, true> ex;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
+  const int c = (blockIdx.y * 32 + lane) * VEC;
+  const bool live = c < p.D;
+  const int n = length_of(p, b);
+  const int piece = C * kScanWarps * kEvery;
+  const int64_t nst = (p.T + kEvery - 1) / kEvery;
+  const int pieces = (p.T + piece - 1) / piece;
+  cluster_start(C);
+  float carry[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) carry[i] = p.dh_last && live ? p.dh_last[(int64_t)b * p.D + c + i] : 0.f;
+  int flip = 0;
+  for (int it = pieces - 1; it >= 0; --it, flip ^= 1) {
+    const int t0 = it * piece + (rank * kScanWarps + warp) * kEvery;
+    Raw rv[kEvery], rf[kEvery], rd[kEvery];
+    {
+      const T* v = static_cast<const T*>(p.v) + b * p.v_b + c + t0 * p.v_t;
+      const T* f = static_cast<const T*>(p.f) + b * p.f_b + c + t0 * p.f_t;
+      const T* d = p.dy ? static_cast<const T*>(p.dy) + b * p.y_b + c + t0 * p.y_t : nullptr;
+#pragma unroll
+      for (int j = 0; j < kEvery; ++j) {
+        rv[j] = rf[j] = rd[j] = L::zero();
+        if (live && t0 + j < n) {
+          rv[j] = __ldcs(reinterpret_cast<const Raw*>(v));
+          rf[j] = __ldcs(reinterpret_cast<const Raw*>(f));
+          if (d) rd[j] = __ldcs(reinterpret_cast<const Raw*>(d));
+        }
+        v += p.v_t;
+        f += p.f_t;
+        if (d) d += p.y_t;
+      }
+    }
+    float h[VEC], P[VEC], E[VEC], G[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      h[i] = live && t0 < p.T ? p.states_in[(b * nst + t0 / kEvery) * p.D + c + i] : 0.f;
+      P[i] = 1.f;
+      E[i] = 0.f;
+    }
+    float a[kEvery][VEC], u[kEvery][VEC], k[kEvery][VEC];       // r a, u, a (1 - a) (r h_before + u' v)
+#pragma unroll
+    for (int j = 0; j < kEvery; ++j) {
+      float v[VEC], f[VEC];
+      L::get(rv[j], v);
+      L::get(rf[j], f);
+      const bool on = t0 + j < n;
+      const bool cut = CUT && on && p.reset[(int64_t)b * p.T + t0 + j] != 0;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float s, w;
+        gate_of(f[i], s, w);
+        const float before = CUT && cut ? 0.f : h[i];
+        u[j][i] = input_of<GATE>(s, w);
+        k[j][i] = fmaf(s * w, before, input_slope<GATE>(s, w) * v[i]);
+        if (on) h[i] = fmaf(s, before, u[j][i] * v[i]);
+        a[j][i] = !on ? 1.f : (CUT && cut ? 0.f : s);
+      }
+    }
+#pragma unroll
+    for (int j = kEvery - 1; j >= 0; --j) {
+      float d[VEC];
+      L::get(rd[j], d);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        E[i] = CUT && a[j][i] == 0.f ? 0.f : a[j][i] * (E[i] + d[i]);
+        P[i] *= a[j][i];
+      }
+    }
+    ex.run(P, E, carry, G, flip, rank, C);
+    if (live && t0 < p.T) {
+      T* dv = static_cast<T*>(p.dv) + b * p.dv_b + c + (t0 + kEvery - 1) * p.dv_t;
+      T* df = static_cast<T*>(p.df) + b * p.df_b + c + (t0 + kEvery - 1) * p.df_t;
+#pragma unroll
+      for (int j = kEvery - 1; j >= 0; --j) {
+        float d[VEC], ov[VEC], of[VEC];
+        L::get(rd[j], d);
+        const bool on = t0 + j < n;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float g = G[i] + d[i];
+          ov[i] = on ? u[j][i] * g : 0.f;
+          of[i] = on ? k[j][i] * g : 0.f;
+          G[i] = CUT && a[j][i] == 0.f ? 0.f : a[j][i] * g;
+        }
+        if (t0 + j < p.T) {
+          __stcs(reinterpret_cast<Raw*>(dv), L::put(ov));
+          __stcs(reinterpret_cast<Raw*>(df), L::put(of));
+        }
+        dv -= p.dv_t;
+        df -= p.df_t;
+      }
+    }
+  }
+  if (p.dh0 && live && rank == 0 && warp == 0)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) p.dh0[(int64_t)b * p.D + c + i] = carry[i];
+}
+
 mw_status check_desc(const mw_gated_scan_desc* d) {
   if (!d || d->batch < 0 || d->length < 0 || d->channels < 1 || d->reserved != 0) return MW_ERR_INVALID_ARG;
   if (d->input_gate != MW_SCAN_COMPLEMENT && d->input_gate != MW_SCAN_ENERGY) return MW_ERR_INVALID_ARG;
   if (d->dtype == 0) return MW_ERR_UNSUPPORTED;
   if (d->dtype != 1 && d->dtype != 2) return MW_ERR_INVALID_ARG;
-  if (d->batch > 65535) return MW_ERR_UNSUPPORTED;
+  if (d->batch > 65535 || d->length > (1 << 30) || d->channels > (1 << 20)) return MW_ERR_UNSUPPORTED;
   return MW_OK;
 }
 
@@ -160,20 +484,54 @@ mw_status fill_scan(const mw_gated_scan_desc* d, ScanArgs& p) {
   return MW_OK;
 }
 
-template <typename T, int GATE>
+template <typename T, int VEC, int GATE, bool CUT>
+mw_status launch_chunks(const ScanArgs& p, bool backward, cudaStream_t s) {
+  const int columns = ceil_div(p.D, 32 * VEC);
+  const int pieces = ceil_div(p.T, kScanWarps * kEvery);
+  // blocks along time until there are two for every SM, as far as there are pieces for them
+  int C = 1;
+  while (C < kMaxCluster && C < pieces && (int64_t)columns * p.B * C < 2 * 148) C *= 2;
+  void (*kernel)(const ScanArgs) = backward ? scan_chunk_back_kernel<T, VEC, GATE, CUT> : scan_chunk_kernel<T, VEC, GATE, CUT>;
+  if (C > 8) MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)C, (unsigned)columns, (unsigned)p.B);
+  cfg.blockDim = dim3(32 * kScanWarps);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)C;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  ++g_launch_count;
+  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
+}
+
+template <typename T, int VEC, int GATE>
 mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
-  const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
-  if (backward) scan_walk_back_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
-  else scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
-  return launch_ok();
+  // up to kEvery steps there is nothing to cut: a thread a channel
+  if (p.T <= kEvery) {
+    const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
+    if (backward) scan_walk_back_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
+    else scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
+    return launch_ok();
+  }
+  return p.reset ? launch_chunks<T, VEC, GATE, true>(p, backward, s) : launch_chunks<T, VEC, GATE, false>(p, backward, s);
+}
+
+template <typename T, int VEC>
+mw_status gate_scan(const mw_gated_scan_desc* d, const ScanArgs& p, bool backward, cudaStream_t s) {
+  return d->input_gate == MW_SCAN_COMPLEMENT ? run_scan<T, VEC, MW_SCAN_COMPLEMENT>(p, backward, s)
+                                             : run_scan<T, VEC, MW_SCAN_ENERGY>(p, backward, s);
 }
 
 mw_status dispatch_scan(const mw_gated_scan_desc* d, const ScanArgs& p, bool backward, cudaStream_t s) {
-  if (d->dtype == 1)
-    return d->input_gate == MW_SCAN_COMPLEMENT ? run_scan<float, MW_SCAN_COMPLEMENT>(p, backward, s)
-                                               : run_scan<float, MW_SCAN_ENERGY>(p, backward, s);
-  return d->input_gate == MW_SCAN_COMPLEMENT ? run_scan<__nv_bfloat16, MW_SCAN_COMPLEMENT>(p, backward, s)
-                                             : run_scan<__nv_bfloat16, MW_SCAN_ENERGY>(p, backward, s);
+  if (d->dtype == 1) return gate_scan<float, 1>(d, p, backward, s);
+  // two bf16 channels a lane where every row of every tensor starts on a 4-byte boundary
+  const int64_t odd = p.D | p.v_b | p.v_t | p.f_b | p.f_t | p.y_b | p.y_t | p.dv_b | p.dv_t | p.df_b | p.df_t;
+  const uintptr_t at = (uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df;
+  return (odd & 1) == 0 && (at & 3) == 0 ? gate_scan<__nv_bfloat16, 2>(d, p, backward, s)
+                                         : gate_scan<__nv_bfloat16, 1>(d, p, backward, s);
 }
 
 }  // namespace

@@ -178,6 +178,30 @@ def test_nan_stays_in_its_channel_and_after_its_step():
     assert torch.equal(y[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("T", [12, 400])
+def test_a_reset_keeps_out_what_came_before(T):
+    # NaN and infinities before a reset do not reach the steps after it, nor cotangents the steps before
+    import torch
+    v, f, dy, h0, _, _, _ = make(1, T, 64, "f32", 12)
+    at = T // 2
+    reset = torch.zeros((1, T), dtype=torch.uint8, device="cuda")
+    reset[0, at] = 1
+    y0, h_last0, st0 = mwb.gated_scan(v, f, reset=reset, h0=h0, keep_states=True)
+    g0 = mwb.gated_scan_backward(v, f, dy, st0, reset=reset)
+    bad = v.clone()
+    bad[0, at - 3, :32] = float("nan")
+    bad[0, at - 2, 32:] = float("inf")
+    y, h_last, st = mwb.gated_scan(bad, f, reset=reset, h0=h0, keep_states=True)
+    assert torch.equal(y[:, at:], y0[:, at:]) and torch.equal(h_last, h_last0)
+    g = mwb.gated_scan_backward(bad, f, dy, st, reset=reset)
+    assert torch.equal(g[0][:, at:], g0[0][:, at:]) and torch.equal(g[1][:, at:], g0[1][:, at:])
+    worse = dy.clone()
+    worse[0, at + 2] = float("nan")
+    g = mwb.gated_scan_backward(v, f, worse, st0, reset=reset)
+    assert torch.equal(g[0][:, :at], g0[0][:, :at]) and torch.equal(g[1][:, :at], g0[1][:, :at])
+    assert torch.equal(g[2], g0[2])
+
+
 def test_no_cotangents_and_empty_sizes():
     import torch
     v, f, _, h0, dh, _, _ = make(2, 30, 64, "f32", 4)
