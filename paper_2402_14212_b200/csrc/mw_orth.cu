@@ -54,12 +54,16 @@ constexpr int kPtrGroup = 64;         // matrices of one launch of the small ker
 constexpr int kTile = 256;            // rows and columns of a pair's tile
 constexpr int kHalf = 128;            // ... of one CTA's share
 constexpr int kBK = 64;
-constexpr int kOrthThreads = 192;     // producer warp, issuing warp, four epilogue warps
-constexpr int kOrthEpi = 4;
+constexpr int kOrthThreads = 320;     // producer warp, issuing warp, eight epilogue warps
+constexpr int kOrthEpi = 8;
+// K blocks that one accumulator takes of a two-term product.  The tensor core truncates its accumulator at
+// every instruction, which over the 3 x 4 instructions of each block adds up to a bias of about 4e-7 a block
+// on sums of like signs (the diagonals of X X^T and A^2); the epilogue adds the pieces rounding to nearest.
+constexpr int kPieceBlocks = 4;
 constexpr int kOrthStagesMax = 6;
 constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;      // one operand plane of one stage and CTA
 constexpr uint32_t kSlot = 2048;                       // one 32 x 32 block of fp16
-constexpr int kSlots = 4;                              // per epilogue warp
+constexpr int kSlots = 2;                              // per epilogue warp
 constexpr int kSetColumns = 256;
 constexpr int kTmemColumns = 512;
 constexpr int kMaxSide = 32768;
@@ -81,6 +85,7 @@ struct alignas(64) OrthParams {
   CUtensorMap map[10];
   int count, tm, tn, steps, tri, per_step, total;
   int kb_m, kb_n;                // K blocks of a sum over m and over n
+  int piece_blocks;              // K blocks of one accumulator (0: all)
   int m, n, mp, np, tall, bf16_out, stages;
   uint32_t stage_bytes;
   float a_scale, b_acc, x_acc, out_scale, keep, step;
@@ -92,7 +97,7 @@ struct alignas(64) OrthParams {
   uint64_t wait_ns;
 };
 
-struct OrthUnit { int step, phase, mat, ti, tj, bn, nkb; };
+struct OrthUnit { int step, phase, mat, ti, tj, bn, nkb, pieces; };
 
 // place t of a triangle of tiles (i, j >= i): row by row, or column by column
 __device__ __forceinline__ void triangle_rows(int t, int tm, int& i, int& j) {
@@ -132,6 +137,7 @@ __device__ __forceinline__ OrthUnit orth_unit(const OrthParams& p, int u) {
     w.nkb = p.kb_m;
     if ((w.tj + 1) * kTile > p.np) w.bn = kHalf;
   }
+  w.pieces = p.piece_blocks ? (w.nkb + p.piece_blocks - 1) / p.piece_blocks : 1;
   return w;
 }
 
@@ -296,12 +302,8 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
       int j = 0;
       bool ok = true;
-      for (int u = pair; u < p.total && ok; u += pairs, ++j) {
+      for (int u = pair; u < p.total && ok; u += pairs) {
         const OrthUnit w = orth_unit(p, u);
-        const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
-        if (!mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u)) break;
-        tc_fence_after();
-        const uint32_t d = tmem_base + set * (uint32_t)kSetColumns;
         const bool mn = w.phase == 2;
         // fp32 accumulator, fp16 operands, B's major-ness, N / 8, M / 16
         const uint32_t idesc = (1u << 4) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(w.bn >> 3) << 17) |
@@ -309,39 +311,48 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         const uint32_t a_base = 1u << 16, b_base = (mn ? (8192u >> 4) : 1u) << 16;
         const uint32_t b_adv = mn ? (2048u >> 4) : (32u >> 4);
         const uint32_t b_off = TERMS * kPlaneBytes, b_plane = (uint32_t)(w.bn >> 1) * (kBK * 2);
-        bool ready = mbar_try_wait<true>(full0 + 8u * stage, phase);
-        for (int kb = 0; kb < w.nkb; ++kb) {
-          if (!ready && !mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u)) { ok = false; break; }
+        const int piece = p.piece_blocks ? p.piece_blocks : w.nkb;
+        for (int kb0 = 0; kb0 < w.nkb && ok; kb0 += piece, ++j) {
+          const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
+          if (!mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t sb = tiles + stage * p.stage_bytes;
-          const uint32_t a0 = (sb >> 4) | a_base, b0 = ((sb + b_off) >> 4) | b_base;
-          umma_f16(d, a0, b0, idesc, kb > 0);
-          if (TERMS == 2) {
-            umma_f16(d, a0, b0 + (b_plane >> 4), idesc, 1u);
-            umma_f16(d, a0 + (kPlaneBytes >> 4), b0, idesc, 1u);
-          }
-          const uint32_t freed = empty0 + 8u * stage;
-          if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-          ready = kb + 1 < w.nkb && mbar_try_wait<true>(full0 + 8u * stage, phase);
-#pragma unroll
-          for (int k = 1; k < kBK / 16; ++k) {
-            const uint32_t a = a0 + (uint32_t)k * (32u >> 4), b = b0 + (uint32_t)k * b_adv;
-            umma_f16(d, a, b, idesc, 1u);
+          const uint32_t d = tmem_base + set * (uint32_t)kSetColumns;
+          const int kb1 = kb0 + piece < w.nkb ? kb0 + piece : w.nkb;
+          bool ready = mbar_try_wait<true>(full0 + 8u * stage, phase);
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!ready && !mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sb = tiles + stage * p.stage_bytes;
+            const uint32_t a0 = (sb >> 4) | a_base, b0 = ((sb + b_off) >> 4) | b_base;
+            umma_f16(d, a0, b0, idesc, kb > kb0);
             if (TERMS == 2) {
-              umma_f16(d, a, b + (b_plane >> 4), idesc, 1u);
-              umma_f16(d, a + (kPlaneBytes >> 4), b, idesc, 1u);
+              umma_f16(d, a0, b0 + (b_plane >> 4), idesc, 1u);
+              umma_f16(d, a0 + (kPlaneBytes >> 4), b0, idesc, 1u);
             }
+            // the next stage's barrier is polled while the first products run
+            const uint32_t freed = empty0 + 8u * stage;
+            if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+            ready = kb + 1 < kb1 && mbar_try_wait<true>(full0 + 8u * stage, phase);
+#pragma unroll
+            for (int k = 1; k < kBK / 16; ++k) {
+              const uint32_t a = a0 + (uint32_t)k * (32u >> 4), b = b0 + (uint32_t)k * b_adv;
+              umma_f16(d, a, b, idesc, 1u);
+              if (TERMS == 2) {
+                umma_f16(d, a, b + (b_plane >> 4), idesc, 1u);
+                umma_f16(d, a + (kPlaneBytes >> 4), b, idesc, 1u);
+              }
+            }
+            umma_commit<true>(freed);
           }
-          umma_commit<true>(freed);
+          if (ok) umma_commit<true>(smem_u32(&acc_full[set]));
         }
-        if (!ok) break;
-        umma_commit<true>(smem_u32(&acc_full[set]));
       }
     }
   } else {
     // ---------------- epilogue ----------------
-    const int quarter = warp & 3;
-    const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)quarter * (kSlots * kSlot);
+    // a tensor-memory lane quarter and one half of the tile's columns each
+    const int quarter = warp & 3, side = (warp - 2) >> 2;
+    const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)(warp - 2) * (kSlots * kSlot);
     uint32_t slot = 0;
     int j = 0;
     // the next free staging block: the copy engine has read what it held (lane 0 owns the copies)
@@ -391,10 +402,10 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         }
       }
     };
-    for (int u = pair; u < p.total; u += pairs, ++j) {
+    for (int u = pair; u < p.total; u += pairs) {
       const OrthUnit w = orth_unit(p, u);
-      const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
-      const int row0 = w.ti * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane, n0 = w.tj * kTile;
+      const int row0 = w.ti * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+      const int cols = w.bn >> 1, n0 = w.tj * kTile + side * cols;      // this warp's columns
       const bool last = w.phase == 2 && w.step == p.steps - 1;
       // addends are read with plain loads: this warp sees their rows complete for itself
       bool ok = true;
@@ -403,10 +414,36 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         else if (w.phase == 2 && w.step > 0) ok = wait_done(row_counter(p, w.step - 1, 2, w.mat, w.ti), x_rows, wc);
       }
       ok = __all_sync(0xffffffffu, ok);
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
+      // the pieces of the sum meet in registers, and the accumulator goes straight back
+      float acc[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[c][i] = 0.f;
+      for (int s = 0; s < w.pieces && ok; ++s, ++j) {
+        const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
+        ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kSetColumns + (uint32_t)(side * cols);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (c * 32 < cols) {
+            uint32_t r[32];
+            tmem_ld32_issue(t0 + (uint32_t)(c * 32), r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[c][i] += __uint_as_float(r[i]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (rank != 0) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty[set]), 0u));
+          else mbar_arrive(smem_u32(&acc_empty[set]));
+        }
+      }
       if (!ok) break;
-      tc_fence_after();
-      const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kSetColumns;
       const int addends = w.phase == 0 ? 0 : (w.phase == 1 ? TERMS : 2);
       const int ld = w.phase == 1 ? p.mp : p.np;
       const __half* src = w.phase == 1 ? p.a : p.x[w.step & 1];
@@ -414,56 +451,45 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       if (addends) src += (int64_t)w.mat * addends * plane + (int64_t)row * ld + n0;
       OrthTarget target = {nullptr, nullptr};
       if (last) target = p.target[w.mat];
-#pragma unroll 1
-      for (int c = 0; c < w.bn; c += 32) {
-        uint32_t r[32];
-        tmem_ld32_issue(t0 + (uint32_t)c, r);
-        uint4 q[2][4];
+      const float alpha = w.phase == 0 ? p.a_scale : (w.phase == 1 ? p.b_acc : p.x_acc);
+      const float scale = w.phase == 1 ? p.b_add[w.step] : p.x_add[w.step];
+      const float diag = w.phase == 0 ? p.a_diag[w.step] : p.b_diag[w.step];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (t < addends) {
-            const uint4* a4 = reinterpret_cast<const uint4*>(src + t * plane + c);
+      for (int c = 0; c < 4; ++c) {
+        if (c * 32 < cols) {
+          float (&v)[32] = acc[c];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[t][i] = __ldcg(a4 + i);
+          for (int i = 0; i < 32; ++i) v[i] *= alpha;
+          for (int t = 0; t < addends; ++t) {
+            const uint4* a4 = reinterpret_cast<const uint4*>(src + t * plane + c * 32);
+            uint4 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = __ldcg(a4 + i);
+            add_plane(v, q, scale);
           }
-        tmem_ld_wait();
-        const float alpha = w.phase == 0 ? p.a_scale : (w.phase == 1 ? p.b_acc : p.x_acc);
-        float v[32];
+          const int col = n0 + c * 32;
+          if (w.phase < 2) {
+            if (w.ti == w.tj) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = alpha * __uint_as_float(r[i]);
-        if (addends) {
-          const float scale = w.phase == 1 ? p.b_add[w.step] : p.x_add[w.step];
-          add_plane(v, q[0], scale);
-          if (addends == 2) add_plane(v, q[1], scale);
-        }
-        if (w.phase < 2) {
-          const float diag = w.phase == 0 ? p.a_diag[w.step] : p.b_diag[w.step];
-          if (w.ti == w.tj) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (n0 + c + i == row) v[i] += diag;
+              for (int i = 0; i < 32; ++i)
+                if (col + i == row) v[i] += diag;
+            }
+            store_block(v, TERMS, &p.map[w.phase == 0 ? MAP_AO : MAP_BO], w.mat * TERMS, row0, col, w.ti != w.tj);
+          } else if (!last) {
+            store_block(v, 2, &p.map[MAP_XO + ((w.step + 1) & 1)], w.mat * 2, row0, col, false);
+          } else if (p.bf16_out) {
+            orth_store<__nv_bfloat16>(p, target, v, row, col);
+          } else {
+            orth_store<float>(p, target, v, row, col);
           }
-          store_block(v, TERMS, &p.map[w.phase == 0 ? MAP_AO : MAP_BO], w.mat * TERMS, row0, n0 + c, w.ti != w.tj);
-        } else if (!last) {
-          store_block(v, 2, &p.map[MAP_XO + ((w.step + 1) & 1)], w.mat * 2, row0, n0 + c, false);
-        } else if (p.bf16_out) {
-          orth_store<__nv_bfloat16>(p, target, v, row, n0 + c);
-        } else {
-          orth_store<float>(p, target, v, row, n0 + c);
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (rank != 0) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty[set]), 0u));
-        else mbar_arrive(smem_u32(&acc_empty[set]));
-        if (!last) {
-          bulk_wait_all();               // written, not just read from the staging blocks
-          __threadfence();
-          unsigned* cnt = const_cast<unsigned*>(row_counter(p, w.step, w.phase, w.mat, 0));
-          atomicAdd(cnt + w.ti, 1u);
-          if (w.phase < 2 && w.ti != w.tj) atomicAdd(cnt + w.tj, 1u);
-        }
+      if (lane == 0 && !last) {
+        bulk_wait_all();               // written, not just read from the staging blocks
+        __threadfence();
+        unsigned* cnt = const_cast<unsigned*>(row_counter(p, w.step, w.phase, w.mat, 0));
+        atomicAdd(cnt + w.ti, 1u);
+        if (w.phase < 2 && w.ti != w.tj) atomicAdd(cnt + w.tj, 1u);
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -728,6 +754,7 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.total = q.per_step * p->steps;
   q.kb_m = ceil_div(m, kBK);
   q.kb_n = ceil_div(n, kBK);
+  q.piece_blocks = p->terms == 2 ? kPieceBlocks : 0;
   q.m = m; q.n = n; q.mp = p->mp; q.np = p->np; q.tall = p->tall;
   q.bf16_out = p->d.prec == MW_BF16_F32ACC;
   // Sa: the entries of B are at most |c1| s + |c2| s^2 with s <= 2 the largest eigenvalue of A
