@@ -26,6 +26,7 @@
 
 #include <new>
 
+#include "mw_tc_gemm.cuh"
 #include "mw_tc_ptx.cuh"
 
 namespace mw {
@@ -43,55 +44,55 @@ struct mw_orth {
   int mp, np;          // padded sides: multiples of 256 and 128
   // tensor maps of a workspace, encoded when the workspace first comes along
   const void* mapped = nullptr;
-  CUtensorMap maps[10];
+  CUtensorMap maps[12];
 };
 
 namespace mw {
 namespace {
 
-constexpr int kNormBlocks = 64;       // partial sums of ||U||^2 per matrix
+constexpr int kNormBlocks = 592;      // most partial sums of ||U||^2 per matrix
 constexpr int kPtrGroup = 64;         // matrices of one launch of the small kernels
 constexpr int kTile = 256;            // rows and columns of a pair's tile
 constexpr int kHalf = 128;            // ... of one CTA's share
 constexpr int kBK = 64;
-constexpr int kOrthThreads = 320;     // producer warp, issuing warp, eight epilogue warps
+constexpr int kOrthThreads = 384;     // producer warp, issuing warp, two idle ones; eight epilogue warps
+constexpr int kOrthFirstEpi = 4;
 constexpr int kOrthEpi = 8;
+// registers a thread: the launch gives 384 x 168 = 64512, handed over as 128 x 104 + 256 x 200 = 64512
+constexpr int kFewRegisters = 104, kManyRegisters = 200;
 // K blocks that one accumulator takes of a two-term product.  The tensor core truncates its accumulator at
 // every instruction, which over the 3 x 4 instructions of each block adds up to a bias of about 4e-7 a block
 // on sums of like signs (the diagonals of X X^T and A^2); the epilogue adds the pieces rounding to nearest.
 constexpr int kPieceBlocks = 4;
-constexpr int kOrthStagesMax = 6;
+constexpr int kOrthStagesMax = 5;
 constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;      // one operand plane of one stage and CTA
-constexpr uint32_t kSlot = 2048;                       // one 32 x 32 block of fp16
-constexpr int kSlots = 2;                              // per epilogue warp
+__host__ __device__ constexpr uint32_t kStagingBytes(int terms) { return terms == 1 ? 8192u : 4096u; }   // per epilogue warp
 constexpr int kSetColumns = 256;
 constexpr int kTmemColumns = 512;
 constexpr int kMaxSide = 32768;
 constexpr uint64_t kOrthWaitNs = 2000000000ull;
 
-enum { MAP_XK = 0, MAP_XMN = 2, MAP_XO = 4, MAP_A = 6, MAP_AO = 7, MAP_B = 8, MAP_BO = 9 };
-
-struct OrthTarget { const void* w; void* out; };       // params (null: store X itself), output
+// operands: K-major rows, MN-major rows; blocks that an epilogue warp reads and writes; transposed blocks
+enum { MAP_XK = 0, MAP_XMN = 2, MAP_XO = 4, MAP_A = 6, MAP_B, MAP_AO, MAP_BO, MAP_AT, MAP_BT, MAP_COUNT };
 
 struct OrthPtrs {
   const void* u[kPtrGroup];
   const float* g[kPtrGroup];
   const float* m[kPtrGroup];
   float* mo[kPtrGroup];
-  OrthTarget t[kPtrGroup];
+  const void* w[kPtrGroup];      // params (null: X itself is stored) and outputs
+  void* out[kPtrGroup];
 };
 
 struct alignas(64) OrthParams {
-  CUtensorMap map[10];
+  CUtensorMap map[MAP_COUNT];
   int count, tm, tn, steps, tri, per_step, total;
   int kb_m, kb_n;                // K blocks of a sum over m and over n
   int piece_blocks;              // K blocks of one accumulator (0: all)
-  int m, n, mp, np, tall, bf16_out, stages;
+  int mp, np, stages;
   uint32_t stage_bytes;
-  float a_scale, b_acc, x_acc, out_scale, keep, step;
+  float a_scale, b_acc, x_acc;
   float a_diag[kOrthMaxSteps], b_add[kOrthMaxSteps], b_diag[kOrthMaxSteps], x_add[kOrthMaxSteps];
-  const __half *x[2], *a;        // planes for the epilogue's addends
-  const OrthTarget* target;
   unsigned* done;                // [step][phase][matrix][row of tiles]
   DeviceStatus* st;
   uint64_t wait_ns;
@@ -157,18 +158,11 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t v) {
   return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
 
-// 32 consecutive fp16 values of this lane's row, added as `scale` times themselves
-__device__ __forceinline__ void add_plane(float (&v)[32], const uint4 (&r)[4], float scale) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint32_t w[4] = {r[q].x, r[q].y, r[q].z, r[q].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = unpack_half2(w[i]);
-      v[8 * q + 2 * i] = fmaf(scale, f.x, v[8 * q + 2 * i]);
-      v[8 * q + 2 * i + 1] = fmaf(scale, f.y, v[8 * q + 2 * i + 1]);
-    }
-  }
+// byte offset of 16-byte piece c of row r in a block of rows of 2 * COLS bytes under the tensor map's swizzle
+// (128-byte rows: c ^ (r & 7); 64-byte rows: c ^ ((r >> 1) & 3)); lanes of a warp then meet distinct banks
+template <int COLS>
+__device__ __forceinline__ uint32_t piece_at(uint32_t r, uint32_t c) {
+  return COLS == 64 ? r * 128u + ((c ^ (r & 7u)) << 4) : r * 64u + ((c ^ ((r >> 1) & 3u)) << 4);
 }
 
 template <typename T>
@@ -178,25 +172,6 @@ __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// the last step's 32 values of X: W' = keep W - step X, or X itself; element (row, col) of X lies at
-// (col, row) of a tall matrix (then a warp's lanes write consecutive elements)
-template <typename T>
-__device__ __forceinline__ void orth_store(const OrthParams& p, const OrthTarget& t, float (&v)[32], int row, int col) {
-  if (row >= p.m || col >= p.n) return;
-  const T* w = static_cast<const T*>(t.w);
-  T* out = static_cast<T*>(t.out);
-  const int64_t stride = p.tall ? p.m : 1;
-  const int64_t at = p.tall ? (int64_t)col * p.m + row : (int64_t)row * p.n + col;
-  const int cnt = p.n - col < 32 ? p.n - col : 32;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    if (i < cnt) {
-      const float x = v[i] * p.out_scale;
-      out[at + i * stride] = narrow<T>(w ? fmaf(-p.step, x, p.keep * to_f32(w[at + i * stride])) : x);
-    }
-  }
-}
-
 template <int TERMS>
 __global__ void __launch_bounds__(kOrthThreads, 1)
 orth_products_kernel(const __grid_constant__ OrthParams p) {
@@ -205,6 +180,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   __shared__ __align__(8) uint64_t empty_bar[kOrthStagesMax];
   __shared__ __align__(8) uint64_t acc_full[2];
   __shared__ __align__(8) uint64_t acc_empty[2];
+  __shared__ __align__(8) uint64_t add_full[kOrthEpi];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
@@ -222,6 +198,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       mbar_init(smem_u32(&acc_full[s]), 1);
       mbar_init(smem_u32(&acc_empty[s]), kOrthEpi * 2);
     }
+    for (int s = 0; s < kOrthEpi; ++s) mbar_init(smem_u32(&add_full[s]), 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -242,6 +219,9 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   wc.abort_flag = &abort_flag;
   wc.limit_ns = p.wait_ns;
   const unsigned sym_rows = (unsigned)p.tm * kOrthEpi * 2, x_rows = (unsigned)p.tn * kOrthEpi * 2;
+
+  if (warp < kOrthFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
 
   if (warp == 0) {
     // ---------------- TMA producer ----------------
@@ -348,143 +328,206 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         }
       }
     }
-  } else {
+  } else if (warp >= kOrthFirstEpi) {
     // ---------------- epilogue ----------------
-    // a tensor-memory lane quarter and one half of the tile's columns each
-    const int quarter = warp & 3, side = (warp - 2) >> 2;
-    const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)(warp - 2) * (kSlots * kSlot);
-    uint32_t slot = 0;
+    // a tensor-memory lane quarter and one half of the tile's columns each, taken kPass columns at a time:
+    // the copy engine brings the block's addend (both planes of X, or A) into the warp's staging buffer,
+    // each lane replaces its row by the result, and the engine takes it away again
+    constexpr int kPass = TERMS == 1 ? 64 : 32;
+    constexpr uint32_t kPlane = 32 * kPass * 2;
+    const int ew = warp - kOrthFirstEpi, quarter = warp & 3, side = ew >> 2;
+    const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)ew * kStagingBytes(TERMS);
+    const uint32_t add_bar = smem_u32(&add_full[ew]);
+    uint32_t add_phase = 0;
     int j = 0;
-    // the next free staging block: the copy engine has read what it held (lane 0 owns the copies)
-    auto next_slot = [&]() {
-      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kSlots - 1) : "memory");
-      __syncwarp();
-      const uint32_t s = sbuf + slot * kSlot;
-      slot = (slot + 1) % kSlots;
-      return s;
+    // lane 0: start the addend's copy once the engine has read what the buffer held
+    auto fetch = [&](const CUtensorMap* map, int col, int row, int plane, int planes) {
+      bulk_wait_read_all();
+      mbar_expect_tx(add_bar, (uint32_t)planes * kPlane);
+      tma_load_3d<false>(sbuf, map, add_bar, col, row, plane);
     };
     auto hand_over = [&](const CUtensorMap* map, uint32_t src, int col, int row, int plane) {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) bulk_store_3d(map, src, col, row, plane);
     };
-    // `planes` fp16 terms of a 32 x 32 block (one row a lane), and of its transpose for a mirrored tile
-    auto store_block = [&](float (&v)[32], int planes, const CUtensorMap* map, int plane0, int row0, int col0,
-                           bool mirror) {
-      for (int t = 0; t < planes; ++t) {
-        uint32_t pk[16];
+    // eight elements of this lane's row, first .. first + 7, into rows of the transposed block: element i goes
+    // to row i, column `lane`, so the two-byte stores of a warp fill one 64-byte row
+    auto store_turned = [&](uint32_t base, uint32_t first, const uint32_t (&pk)[4]) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          pk[i] = pack_half2(v[2 * i], v[2 * i + 1]);
-          const float2 f = unpack_half2(pk[i]);
-          v[2 * i] -= f.x;
-          v[2 * i + 1] -= f.y;
-        }
-        // rows of 64 bytes in the map's 64-byte swizzle: piece c of row r sits at c ^ ((r >> 1) & 3)
-        const uint32_t s0 = next_slot();
-        const uint32_t rowp = s0 + (uint32_t)lane * 64u, sw = ((uint32_t)lane >> 1) & 3u;
-#pragma unroll
-        for (uint32_t c = 0; c < 4; ++c)
-          st_shared_v4(rowp + ((c ^ sw) << 4), pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
-        hand_over(map, s0, col0, row0, plane0 + t);
-        if (mirror) {
-          const uint32_t s1 = next_slot();
-          const uint32_t piece = (uint32_t)lane >> 3, inside = ((uint32_t)lane & 7u) * 2u;
-#pragma unroll
-          for (uint32_t i = 0; i < 16; ++i) {
-            const uint32_t r0 = 2u * i, r1 = 2u * i + 1u;
-            const uint32_t q0 = s1 + r0 * 64u + ((piece ^ ((r0 >> 1) & 3u)) << 4) + inside;
-            const uint32_t q1 = s1 + r1 * 64u + ((piece ^ ((r1 >> 1) & 3u)) << 4) + inside;
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(q0), "h"((unsigned short)(pk[i] & 0xffffu)) : "memory");
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(q1), "h"((unsigned short)(pk[i] >> 16)) : "memory");
-          }
-          hand_over(map, s1, row0, col0, plane0 + t);
-        }
+      for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t at = base + piece_at<32>(first + i, (uint32_t)lane >> 3) + ((uint32_t)lane & 7u) * 2u;
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)(i & 1 ? pk[i / 2] >> 16 : pk[i / 2] & 0xffffu)) : "memory");
       }
     };
     for (int u = pair; u < p.total; u += pairs) {
       const OrthUnit w = orth_unit(p, u);
       const int row0 = w.ti * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
       const int cols = w.bn >> 1, n0 = w.tj * kTile + side * cols;      // this warp's columns
-      const bool last = w.phase == 2 && w.step == p.steps - 1;
-      // addends are read with plain loads: this warp sees their rows complete for itself
+      const int addends = w.phase == 0 ? 0 : (w.phase == 1 ? TERMS : 2);
+      const CUtensorMap* from = w.phase == 1 ? &p.map[MAP_AO] : &p.map[MAP_XO + (w.step & 1)];
+      const CUtensorMap* to = w.phase == 0 ? &p.map[MAP_AO] : (w.phase == 1 ? &p.map[MAP_BO] : &p.map[MAP_XO + ((w.step + 1) & 1)]);
+      const int plane0 = w.mat * (w.phase == 2 ? 2 : TERMS);
+      // the addend's rows are complete before its first block is fetched, ahead of the sum
       bool ok = true;
       if (lane == 0) {
         if (w.phase == 1) ok = wait_done(row_counter(p, w.step, 0, w.mat, w.ti), sym_rows, wc);
         else if (w.phase == 2 && w.step > 0) ok = wait_done(row_counter(p, w.step - 1, 2, w.mat, w.ti), x_rows, wc);
+        if (ok && addends) {
+          asm volatile("fence.proxy.async;" ::: "memory");
+          fetch(from, n0, row0, plane0, addends);
+        }
       }
       ok = __all_sync(0xffffffffu, ok);
-      // the pieces of the sum meet in registers, and the accumulator goes straight back
-      float acc[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 32; ++i) acc[c][i] = 0.f;
-      for (int s = 0; s < w.pieces && ok; ++s, ++j) {
-        const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
+      // Two terms: the pieces of the sum meet in registers, and each accumulator goes straight back.
+      // One term: a pass reads its columns from the one accumulator, which goes back after the last.
+      float acc[TERMS == 2 ? 4 : 1][32];
+      uint32_t t0 = 0, set = 0;
+      auto await_sum = [&]() {
+        set = (uint32_t)j & 1u;
+        const uint32_t aphase = ((uint32_t)j >> 1) & 1u;
+        ++j;
         ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
-        if (!ok) break;
         tc_fence_after();
-        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kSetColumns + (uint32_t)(side * cols);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if (c * 32 < cols) {
-            uint32_t r[32];
-            tmem_ld32_issue(t0 + (uint32_t)(c * 32), r);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[c][i] += __uint_as_float(r[i]);
-          }
-        }
+        t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kSetColumns + (uint32_t)(side * cols);
+      };
+      auto give_back = [&]() {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
           if (rank != 0) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty[set]), 0u));
           else mbar_arrive(smem_u32(&acc_empty[set]));
         }
+      };
+      if (TERMS == 1) {
+        if (ok) await_sum();
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[TERMS == 2 ? c : 0][i] = 0.f;
+#pragma unroll 1
+        for (int s = 0; s < w.pieces && ok; ++s) {
+          await_sum();
+          if (!ok) break;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            if (c * 16 < cols) {
+              uint32_t r[16];
+              tmem_ld16_issue(t0 + (uint32_t)(c * 16), r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[TERMS == 2 ? c / 2 : 0][c % 2 * 16 + i] += __uint_as_float(r[i]);
+            }
+          }
+          give_back();
+        }
       }
       if (!ok) break;
-      const int addends = w.phase == 0 ? 0 : (w.phase == 1 ? TERMS : 2);
-      const int ld = w.phase == 1 ? p.mp : p.np;
-      const __half* src = w.phase == 1 ? p.a : p.x[w.step & 1];
-      const int64_t plane = (int64_t)p.mp * ld;
-      if (addends) src += (int64_t)w.mat * addends * plane + (int64_t)row * ld + n0;
-      OrthTarget target = {nullptr, nullptr};
-      if (last) target = p.target[w.mat];
       const float alpha = w.phase == 0 ? p.a_scale : (w.phase == 1 ? p.b_acc : p.x_acc);
       const float scale = w.phase == 1 ? p.b_add[w.step] : p.x_add[w.step];
       const float diag = w.phase == 0 ? p.a_diag[w.step] : p.b_diag[w.step];
+      const int planes = w.phase == 2 ? 2 : TERMS;
+      const bool mirror = w.phase < 2 && w.ti != w.tj;
+      // (unrolled for two terms, whose sums sit in registers)
+#pragma unroll(TERMS == 2 ? 4 : 1)
+      for (int c0 = 0; c0 < 128; c0 += kPass) {
+        if (c0 < cols && ok) {
+          const int col = n0 + c0;
+          float v[kPass];
+          if (TERMS == 1) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        if (c * 32 < cols) {
-          float (&v)[32] = acc[c];
+            for (int h = 0; h < kPass; h += 32) {
+              uint32_t r[32];
+              tmem_ld32_issue(t0 + (uint32_t)(c0 + h), r);
+              tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] *= alpha;
-          for (int t = 0; t < addends; ++t) {
-            const uint4* a4 = reinterpret_cast<const uint4*>(src + t * plane + c * 32);
-            uint4 q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = __ldcg(a4 + i);
-            add_plane(v, q, scale);
-          }
-          const int col = n0 + c * 32;
-          if (w.phase < 2) {
-            if (w.ti == w.tj) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col + i == row) v[i] += diag;
+              for (int i = 0; i < 32; ++i) v[h + i] = alpha * __uint_as_float(r[i]);
             }
-            store_block(v, TERMS, &p.map[w.phase == 0 ? MAP_AO : MAP_BO], w.mat * TERMS, row0, col, w.ti != w.tj);
-          } else if (!last) {
-            store_block(v, 2, &p.map[MAP_XO + ((w.step + 1) & 1)], w.mat * 2, row0, col, false);
-          } else if (p.bf16_out) {
-            orth_store<__nv_bfloat16>(p, target, v, row, col);
+            if (c0 + kPass >= cols) give_back();
           } else {
-            orth_store<float>(p, target, v, row, col);
+#pragma unroll
+            for (int i = 0; i < kPass; ++i) v[i] = alpha * acc[TERMS == 2 ? c0 / 32 : 0][i];
+          }
+          if (addends) {
+            if (lane == 0 && c0 > 0) fetch(from, col, row0, plane0, addends);
+            ok = __all_sync(0xffffffffu, mbar_wait<false>(add_bar, add_phase, wc, 6u));
+            add_phase ^= 1u;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (t < addends) {
+#pragma unroll
+                for (uint32_t q = 0; q < kPass / 8; ++q) {
+                  uint32_t r[4];
+                  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                               : "r"(sbuf + (uint32_t)t * kPlane + piece_at<kPass>((uint32_t)lane, q)));
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const float2 f = unpack_half2(r[i]);
+                    v[8 * q + 2 * i] = fmaf(scale, f.x, v[8 * q + 2 * i]);
+                    v[8 * q + 2 * i + 1] = fmaf(scale, f.y, v[8 * q + 2 * i + 1]);
+                  }
+                }
+              }
+            }
+          } else {
+            if (lane == 0) bulk_wait_read_all();
+            __syncwarp();
+          }
+          if (w.phase < 2 && w.ti == w.tj) {
+#pragma unroll
+            for (int i = 0; i < kPass; ++i)
+              if (col + i == row) v[i] += diag;
+          }
+          // the result's terms, 16 bytes of a row at a time
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (t < planes) {
+#pragma unroll
+              for (uint32_t q = 0; q < kPass / 8; ++q) {
+                uint32_t pk[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  pk[i] = pack_half2(v[8 * q + 2 * i], v[8 * q + 2 * i + 1]);
+                  const float2 f = unpack_half2(pk[i]);
+                  v[8 * q + 2 * i] -= f.x;
+                  v[8 * q + 2 * i + 1] -= f.y;
+                }
+                st_shared_v4(sbuf + (uint32_t)t * kPlane + piece_at<kPass>((uint32_t)lane, q), pk[0], pk[1], pk[2], pk[3]);
+                if (TERMS == 1 && mirror) store_turned(sbuf + kPlane, 8u * q, pk);     // the other half of the buffer
+              }
+            }
+          }
+          hand_over(to, sbuf, col, row0, plane0);
+          if (mirror) {
+            if (TERMS == 2) {
+              // two terms fill the buffer: the rows are read back, and turned once the engine has them
+              uint32_t pk[2][kPass / 2];
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (uint32_t q = 0; q < kPass / 8; ++q)
+                  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                               : "=r"(pk[t][4 * q]), "=r"(pk[t][4 * q + 1]), "=r"(pk[t][4 * q + 2]), "=r"(pk[t][4 * q + 3])
+                               : "r"(sbuf + (uint32_t)t * kPlane + piece_at<kPass>((uint32_t)lane, q))
+                               : "memory");
+              if (lane == 0) bulk_wait_read_all();
+              __syncwarp();
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (uint32_t q = 0; q < kPass / 8; ++q) {
+                  const uint32_t four[4] = {pk[t][4 * q], pk[t][4 * q + 1], pk[t][4 * q + 2], pk[t][4 * q + 3]};
+                  store_turned(sbuf + (uint32_t)t * kPlane, 8u * q, four);
+                }
+            }
+            hand_over(w.phase == 0 ? &p.map[MAP_AT] : &p.map[MAP_BT], TERMS == 1 ? sbuf + kPlane : sbuf, row0, col, plane0);
           }
         }
       }
-      if (lane == 0 && !last) {
+      if (!ok) break;
+      if (lane == 0) {
         bulk_wait_all();               // written, not just read from the staging blocks
         __threadfence();
         unsigned* cnt = const_cast<unsigned*>(row_counter(p, w.step, w.phase, w.mat, 0));
@@ -508,10 +551,63 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
                  : "memory");
 }
 
+// Blocks of 32 rows by 64 columns of X, eight consecutive columns a thread.  A tall matrix holds X's columns
+// as rows: its block is turned in shared memory.
+// eight values of a row that starts at `at` and ends `left` values later (WIDE: all eight, 16-byte aligned)
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load8(const T* at, int left, float (&v)[8]) {
+  if (WIDE && left >= 8) {
+    if (sizeof(T) == 4) {
+      const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 a = *reinterpret_cast<const uint4*>(at);
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < left ? to_f32(at[j]) : 0.f;
+  }
+}
+template <typename T, bool WIDE>
+__device__ __forceinline__ void store8(T* at, int left, const float (&v)[8]) {
+  if (WIDE && left >= 8) {
+    if (sizeof(T) == 4) {
+      reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) at[j] = narrow<T>(v[j]);
+  }
+}
+// position of this thread's eight values: in the matrix (rows of `width` values) and in the block
+struct Eight { int row, col, left; };
+__device__ __forceinline__ Eight eight_of(int tall, int height, int width, int row0, int col0) {
+  Eight e;
+  e.row = tall ? col0 + (int)(threadIdx.x >> 2) : row0 + (int)(threadIdx.x >> 3);
+  e.col = tall ? row0 + (int)(threadIdx.x & 3) * 8 : col0 + (int)(threadIdx.x & 7) * 8;
+  e.left = e.row < height ? width - e.col : 0;
+  return e;
+}
+
 // ---------------------------------------------------------------------------------------------
 // M' = beta M + G (or U given) and partial sums of ||U||^2, one per block, in double: a fixed order,
-// and no overflow whatever the gradients' scale.  Also leaves the output pointers where the products'
-// last step finds them.
+// and no overflow whatever the gradients' scale.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ float update_of(float g, float m2, float beta, int nesterov) {
   return nesterov ? fmaf(beta, m2, g) : m2;
@@ -520,37 +616,28 @@ __device__ __forceinline__ float update_of(float g, float m2, float beta, int ne
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 orth_momentum_kernel(const __grid_constant__ OrthPtrs ptr, int64_t n, float beta, int nesterov,
-                     double* __restrict__ partials, OrthTarget* __restrict__ table) {
+                     double* __restrict__ partials) {
   __shared__ double buf[8];
   const int i = blockIdx.y;
-  constexpr int V = WIDE ? 4 : 1;
   double s = 0.0;
-  for (int64_t k = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; k < n; k += (int64_t)gridDim.x * 256 * V) {
-    float u[V];
+  for (int64_t k = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; k < n; k += (int64_t)gridDim.x * 2048) {
+    const int left = n - k < 8 ? (int)(n - k) : 8;
+    float u[8];
     if (ptr.u[i]) {
-      const T* in = static_cast<const T*>(ptr.u[i]) + k;
-#pragma unroll
-      for (int j = 0; j < V; ++j) u[j] = to_f32(in[j]);
+      load8<T, WIDE>(static_cast<const T*>(ptr.u[i]) + k, left, u);
     } else {
-      float g[V], m[V];
-      if (WIDE) {
-        const float4 a = *reinterpret_cast<const float4*>(ptr.g[i] + k), b = *reinterpret_cast<const float4*>(ptr.m[i] + k);
-        g[0] = a.x; g[V > 1] = a.y; g[V > 2 ? 2 : 0] = a.z; g[V > 3 ? 3 : 0] = a.w;
-        m[0] = b.x; m[V > 1] = b.y; m[V > 2 ? 2 : 0] = b.z; m[V > 3 ? 3 : 0] = b.w;
-      } else {
-        g[0] = ptr.g[i][k];
-        m[0] = ptr.m[i][k];
-      }
+      float g[8], m[8];
+      load8<float, WIDE>(ptr.g[i] + k, left, g);
+      load8<float, WIDE>(ptr.m[i] + k, left, m);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
+      for (int j = 0; j < 8; ++j) {
         m[j] = fmaf(beta, m[j], g[j]);
         u[j] = update_of(g[j], m[j], beta, nesterov);
       }
-      if (WIDE) *reinterpret_cast<float4*>(ptr.mo[i] + k) = make_float4(m[0], m[V > 1], m[V > 2 ? 2 : 0], m[V > 3 ? 3 : 0]);
-      else ptr.mo[i][k] = m[0];
+      store8<float, WIDE>(ptr.mo[i] + k, left, m);
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) s += (double)u[j] * (double)u[j];
+    for (int j = 0; j < 8; ++j) s += (double)u[j] * (double)u[j];
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -560,57 +647,110 @@ orth_momentum_kernel(const __grid_constant__ OrthPtrs ptr, int64_t n, float beta
     double t = 0.0;
     for (int w = 0; w < 8; ++w) t += buf[w];
     partials[(int64_t)i * gridDim.x + blockIdx.x] = t;
-    if (blockIdx.x == 0) table[i] = ptr.t[i];
   }
 }
 
-// X_0 = Sx U / ||U||_F as fp16 leading term and remainder, padded with zeros, transposed for a tall U.
-// A block forms 32 rows by 64 columns of X.
-template <typename T>
+// X_0 = Sx U / ||U||_F as fp16 leading term and remainder, padded with zeros
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 orth_start_kernel(const __grid_constant__ OrthPtrs ptr, int m, int n, int mp, int np, int tall, float beta, int nesterov,
                   const double* __restrict__ partials, int parts, double sx, __half* __restrict__ x) {
   __shared__ float tile[64][33];
-  const int i = blockIdx.z;
+  __shared__ double buf[9];
+  const int i = blockIdx.z, row0 = blockIdx.y * 32, col0 = blockIdx.x * 64;
   double t = 0.0;
-  for (int k = 0; k < parts; ++k) t += partials[(int64_t)i * parts + k];
-  const double r = t > 0.0 ? sx / sqrt(t) : (t == 0.0 ? 0.0 : t);      // NaN stays NaN
-  const int row0 = blockIdx.y * 32, col0 = blockIdx.x * 64;
-  auto value = [&](int64_t k) {
-    if (ptr.u[i]) return to_f32(static_cast<const T*>(ptr.u[i])[k]);
-    return update_of(ptr.g[i][k], ptr.mo[i][k], beta, nesterov);
-  };
-  if (tall) {      // rows of U are columns of X
-    for (int e = threadIdx.x; e < 32 * 64; e += 256) {
-      const int a = e & 31, b = e >> 5;
-      tile[b][a] = row0 + a < m && col0 + b < n ? value((int64_t)(col0 + b) * m + row0 + a) : 0.f;
-    }
-    __syncthreads();
-  }
-  __half* hi = x + (int64_t)i * 2 * mp * np;
-  __half* lo = hi + (int64_t)mp * np;
-  for (int e = threadIdx.x; e < 32 * 32; e += 256) {
-    const int a = e >> 5, b = (e & 31) * 2, row = row0 + a, col = col0 + b;
-    float v[2];
+  for (int k = threadIdx.x; k < parts; k += 256) t += partials[(int64_t)i * parts + k];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (tall) v[j] = tile[b + j][a];
-      else v[j] = row < m && col + j < n ? value((int64_t)row * n + col + j) : 0.f;
-      v[j] = row < m && col + j < n ? (float)((double)v[j] * r) : 0.f;
-    }
-    const uint32_t h = pack_half2(v[0], v[1]);
-    const float2 f = unpack_half2(h);
-    const int64_t at = (int64_t)row * np + col;
-    *reinterpret_cast<uint32_t*>(hi + at) = h;
-    *reinterpret_cast<uint32_t*>(lo + at) = pack_half2(v[0] - f.x, v[1] - f.y);
+  for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = t;
+  const Eight e = eight_of(tall, tall ? n : m, tall ? m : n, row0, col0);
+  const int64_t at = (int64_t)e.row * (tall ? m : n) + e.col;
+  float v[8];
+  if (e.left <= 0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+  } else if (ptr.u[i]) {
+    load8<T, WIDE>(static_cast<const T*>(ptr.u[i]) + at, e.left, v);
+  } else {
+    float g[8], m2[8];
+    load8<float, WIDE>(ptr.g[i] + at, e.left, g);
+    load8<float, WIDE>(ptr.mo[i] + at, e.left, m2);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = update_of(g[j], m2[j], beta, nesterov);
   }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int w = 0; w < 8; ++w) s += buf[w];
+    buf[8] = s > 0.0 ? sx / sqrt(s) : (s == 0.0 ? 0.0 : s);      // NaN stays NaN
+  }
+  const int a = threadIdx.x >> 3, b = (threadIdx.x & 7) * 8;
+  if (tall)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[threadIdx.x >> 2][(threadIdx.x & 3) * 8 + j] = v[j];
+  __syncthreads();
+  if (tall)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = tile[b + j][a];
+  const double r = buf[8];
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool in0 = row0 + a < m && col0 + b + 2 * j < n, in1 = row0 + a < m && col0 + b + 2 * j + 1 < n;
+    const float x0 = in0 ? (float)((double)v[2 * j] * r) : 0.f, x1 = in1 ? (float)((double)v[2 * j + 1] * r) : 0.f;
+    hi[j] = pack_half2(x0, x1);
+    const float2 f = unpack_half2(hi[j]);
+    lo[j] = pack_half2(x0 - f.x, x1 - f.y);
+  }
+  __half* to = x + (int64_t)i * 2 * mp * np + (int64_t)(row0 + a) * np + col0 + b;
+  *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  *reinterpret_cast<uint4*>(to + (int64_t)mp * np) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+// W' = keep W - step X, or X itself, from the two planes of the last X
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256)
+orth_apply_kernel(const __grid_constant__ OrthPtrs ptr, int m, int n, int mp, int np, int tall, const __half* __restrict__ x,
+                  float out_scale, float keep, float step) {
+  __shared__ float tile[64][33];
+  const int i = blockIdx.z, row0 = blockIdx.y * 32, col0 = blockIdx.x * 64;
+  const int a = threadIdx.x >> 3, b = (threadIdx.x & 7) * 8;
+  const __half* from = x + (int64_t)i * 2 * mp * np + (int64_t)(row0 + a) * np + col0 + b;
+  const uint4 hi = *reinterpret_cast<const uint4*>(from), lo = *reinterpret_cast<const uint4*>(from + (int64_t)mp * np);
+  const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 p = unpack_half2(h[j]), q = unpack_half2(l[j]);
+    v[2 * j] = p.x + q.x;
+    v[2 * j + 1] = p.y + q.y;
+  }
+  if (tall) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[b + j][a] = v[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = tile[threadIdx.x >> 2][(threadIdx.x & 3) * 8 + j];
+  }
+  const Eight e = eight_of(tall, tall ? n : m, tall ? m : n, row0, col0);
+  if (e.left <= 0) return;
+  const int64_t at = (int64_t)e.row * (tall ? m : n) + e.col;
+  if (ptr.w[i]) {
+    float w[8];
+    load8<T, WIDE>(static_cast<const T*>(ptr.w[i]) + at, e.left, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = fmaf(-step, v[j] * out_scale, keep * w[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= out_scale;
+  }
+  store8<T, WIDE>(static_cast<T*>(ptr.out[i]) + at, e.left, v);
 }
 
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
 struct OrthWs {
-  OrthTarget* table;
   double* partials;
   unsigned* done;
   size_t done_bytes;
@@ -629,7 +769,6 @@ size_t orth_layout(const mw_orth* p, char* base, OrthWs* w) {
   OrthWs l;
   l.done_bytes = (size_t)p->steps * 3 * c * (p->mp / kTile) * sizeof(unsigned);
   l.done = reinterpret_cast<unsigned*>(take(l.done_bytes));
-  l.table = reinterpret_cast<OrthTarget*>(take(c * sizeof(OrthTarget)));
   l.partials = reinterpret_cast<double*>(take(c * kNormBlocks * sizeof(double)));
   for (auto& x : l.x) x = reinterpret_cast<__half*>(take(c * 2 * mn * 2));
   l.a = reinterpret_cast<__half*>(take(c * p->terms * mm * 2));
@@ -658,15 +797,17 @@ mw_status orth_maps(mw_orth* p, const OrthWs& l, const void* ws) {
   const int64_t c = p->d.count;
   const int t = p->terms;
   const auto S128 = CU_TENSOR_MAP_SWIZZLE_128B, S64 = CU_TENSOR_MAP_SWIZZLE_64B;
+  const int pass = t == 1 ? 64 : 32;
+  const auto SP = t == 1 ? S128 : S64;
   for (int b = 0; b < 2; ++b) {
     MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, kBK, kHalf, t, S128, &p->maps[MAP_XK + b]));
     MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, 64, kBK, 1, S128, &p->maps[MAP_XMN + b]));
-    MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, 32, 32, 1, S64, &p->maps[MAP_XO + b]));
+    MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, pass, 32, 2, SP, &p->maps[MAP_XO + b]));
+    const __half* s = b ? l.b : l.a;
+    MW_TRY(half_map(s, p->mp, p->mp, t * c, kBK, kHalf, t, S128, &p->maps[MAP_A + b]));
+    MW_TRY(half_map(s, p->mp, p->mp, t * c, pass, 32, t, SP, &p->maps[MAP_AO + b]));
+    MW_TRY(half_map(s, p->mp, p->mp, t * c, 32, pass, t, S64, &p->maps[MAP_AT + b]));
   }
-  MW_TRY(half_map(l.a, p->mp, p->mp, t * c, kBK, kHalf, t, S128, &p->maps[MAP_A]));
-  MW_TRY(half_map(l.a, p->mp, p->mp, t * c, 32, 32, 1, S64, &p->maps[MAP_AO]));
-  MW_TRY(half_map(l.b, p->mp, p->mp, t * c, kBK, kHalf, t, S128, &p->maps[MAP_B]));
-  MW_TRY(half_map(l.b, p->mp, p->mp, t * c, 32, 32, 1, S64, &p->maps[MAP_BO]));
   p->mapped = ws;
   return MW_OK;
 }
@@ -685,7 +826,7 @@ mw_status orth_launch(const OrthParams& prm, size_t smem, cudaStream_t s) {
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeCooperative;      // tiles wait for one another: all pairs are resident
-  attr[1].val.cooperative = 1;
+  attr[1].val.cooperative = tc_cooperative();
   cfg.attrs = attr;
   if (pairs[dev] == 0) {
     MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
@@ -714,35 +855,37 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   MW_TRY(orth_maps(p, l, ws));
   MW_CUDA_OK(cudaMemsetAsync(ws, 0, 1024 + l.done_bytes, s));     // status and counters
   const int m = p->m, n = p->n, count = p->d.count;
-  const int64_t mn = (int64_t)m * n;
+  const int64_t mn = (int64_t)m * n, rowlen = p->tall ? m : n;
   double sx = 64.0 * exp2(ceil(log2(sqrt((double)n))));
   if (sx > 16384.0) sx = 16384.0;
-  const int64_t want = (mn + 2047) / 2048;
-  const int parts = (int)(want < kNormBlocks ? want : kNormBlocks);
+  // blocks of the momentum pass: about eight an SM over all matrices
+  const int64_t want = (mn + 2047) / 2048, share = ceil_div(8 * 148, count < kPtrGroup ? count : kPtrGroup);
+  int parts = (int)(want < kNormBlocks ? want : kNormBlocks);
+  if (parts > share) parts = (int)share;
   for (int first = 0; first < count; first += kPtrGroup) {
     const int c = count - first < kPtrGroup ? count - first : kPtrGroup;
     static thread_local OrthPtrs ptr;
-    bool wide = mn % 4 == 0;
+    // 16-byte accesses where every row of every matrix starts on such a boundary
+    bool wide = (rowlen * (int64_t)sizeof(T)) % 16 == 0;
     for (int i = 0; i < c; ++i) {
       const int k = first + i;
       ptr.u[i] = project_in ? project_in[k] : nullptr;
       ptr.g[i] = grads ? static_cast<const float*>(grads[k]) : nullptr;
       ptr.m[i] = momentum ? static_cast<const float*>(momentum[k]) : nullptr;
       ptr.mo[i] = momentum_out ? static_cast<float*>(momentum_out[k]) : nullptr;
-      ptr.t[i].w = params ? params[k] : nullptr;
-      ptr.t[i].out = out[k];
-      wide = wide && (((uintptr_t)ptr.g[i] | (uintptr_t)ptr.m[i] | (uintptr_t)ptr.mo[i]) & 15) == 0;
+      wide = wide && (((uintptr_t)ptr.u[i] | (uintptr_t)ptr.g[i] | (uintptr_t)ptr.m[i] | (uintptr_t)ptr.mo[i]) & 15) == 0;
     }
     double* part = l.partials + (size_t)first * parts;
     auto k1 = wide ? orth_momentum_kernel<T, true> : orth_momentum_kernel<T, false>;
-    k1<<<dim3((unsigned)parts, (unsigned)c), 256, 0, s>>>(ptr, mn, (float)beta, p->d.nesterov, part, l.table + first);
-    orth_start_kernel<T><<<dim3((unsigned)(p->np / 64), (unsigned)(p->mp / 32), (unsigned)c), 256, 0, s>>>(
+    auto k2 = wide ? orth_start_kernel<T, true> : orth_start_kernel<T, false>;
+    k1<<<dim3((unsigned)parts, (unsigned)c), 256, 0, s>>>(ptr, mn, (float)beta, p->d.nesterov, part);
+    k2<<<dim3((unsigned)(p->np / 64), (unsigned)(p->mp / 32), (unsigned)c), 256, 0, s>>>(
         ptr, m, n, p->mp, p->np, p->tall, (float)beta, p->d.nesterov, part, parts, sx,
         l.x[0] + (size_t)first * 2 * p->mp * p->np);
     MW_TRY(launch_ok(2));
   }
   static thread_local OrthParams q;
-  for (int i = 0; i < 10; ++i) q.map[i] = p->maps[i];
+  for (int i = 0; i < MAP_COUNT; ++i) q.map[i] = p->maps[i];
   q.count = count;
   q.tm = p->mp / kTile;
   q.tn = ceil_div(p->np, kTile);
@@ -755,8 +898,7 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.kb_m = ceil_div(m, kBK);
   q.kb_n = ceil_div(n, kBK);
   q.piece_blocks = p->terms == 2 ? kPieceBlocks : 0;
-  q.m = m; q.n = n; q.mp = p->mp; q.np = p->np; q.tall = p->tall;
-  q.bf16_out = p->d.prec == MW_BF16_F32ACC;
+  q.mp = p->mp; q.np = p->np;
   // Sa: the entries of B are at most |c1| s + |c2| s^2 with s <= 2 the largest eigenvalue of A
   double sa = 1024.0;
   const double most = 2.0 * fabs(p->c[1]) + 4.0 * fabs(p->c[2]);
@@ -764,9 +906,6 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.a_scale = (float)(sa / (sx * sx));
   q.b_acc = (float)(p->c[2] / sa);
   q.x_acc = (float)(1.0 / sa);
-  q.out_scale = (float)(1.0 / sx);
-  q.keep = (float)(1.0 - lr * wd);
-  q.step = (float)(lr * scale);
   const bool shifts = p->d.coef[0] == 0.0 && p->d.coef[1] == 0.0 && p->d.coef[2] == 0.0;
   for (int k = 0; k < p->steps; ++k) {
     // (the shifts are identities; these values lie in the middle of the spectra that the default
@@ -779,15 +918,29 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
     q.b_diag[k] = (float)(sa * (p->c[1] * al + p->c[2] * al * al + be));
     q.x_add[k] = (float)(p->c[0] - be);
   }
-  q.x[0] = l.x[0]; q.x[1] = l.x[1]; q.a = l.a;
-  q.target = l.table;
   q.done = l.done;
   q.st = reinterpret_cast<DeviceStatus*>(ws);
   q.wait_ns = kOrthWaitNs;
   q.stage_bytes = 2u * (uint32_t)p->terms * kPlaneBytes;
-  q.stages = p->terms == 1 ? 6 : 3;
-  const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * kSlots * kSlot;
-  return p->terms == 1 ? orth_launch<1>(q, smem, s) : orth_launch<2>(q, smem, s);
+  q.stages = p->terms == 1 ? 5 : 3;
+  const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * kStagingBytes(p->terms);
+  MW_TRY(p->terms == 1 ? orth_launch<1>(q, smem, s) : orth_launch<2>(q, smem, s));
+  for (int first = 0; first < count; first += kPtrGroup) {
+    const int c = count - first < kPtrGroup ? count - first : kPtrGroup;
+    static thread_local OrthPtrs ptr;
+    bool wide = (rowlen * (int64_t)sizeof(T)) % 16 == 0;
+    for (int i = 0; i < c; ++i) {
+      ptr.w[i] = params ? params[first + i] : nullptr;
+      ptr.out[i] = out[first + i];
+      wide = wide && (((uintptr_t)ptr.w[i] | (uintptr_t)ptr.out[i]) & 15) == 0;
+    }
+    auto k3 = wide ? orth_apply_kernel<T, true> : orth_apply_kernel<T, false>;
+    k3<<<dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 32), (unsigned)c), 256, 0, s>>>(
+        ptr, m, n, p->mp, p->np, p->tall, l.x[p->steps & 1] + (size_t)first * 2 * p->mp * p->np, (float)(1.0 / sx),
+        (float)(1.0 - lr * wd), (float)(lr * scale));
+    MW_TRY(launch_ok());
+  }
+  return MW_OK;
 }
 
 bool all_set(const void* const* p, int n) {

@@ -1885,6 +1885,7 @@ int tc_set_bulk_epilogue(int mode) {
   g_bulk_epilogue = mode != 0;
   return old;
 }
+int tc_cooperative() { return g_cooperative; }
 int tc_set_cooperative(int mode) {
   const int old = g_cooperative;
   g_cooperative = mode != 0;

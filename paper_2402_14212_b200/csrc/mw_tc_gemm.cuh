@@ -214,6 +214,7 @@ int tc_set_merge_orders(int mode);
 int tc_set_bulk_epilogue(int mode);
 // program launches with (1, default) or without (0) the cooperative-launch attribute
 int tc_set_cooperative(int mode);
+int tc_cooperative();                     // the present setting
 
 // Per-launch timing of the product kernel (CUDA events around every launch while enabled).
 void tc_profile_begin();
