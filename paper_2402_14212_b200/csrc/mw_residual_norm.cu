@@ -23,7 +23,7 @@ struct NormArgs {
   const float* rms_in;
   const void *dx_out, *dn;
   void *dx, *db, *dz;
-  float* partials;      // [grid][3][cols]
+  float* partials;      // [grid * rows a block][2][cols]
 };
 
 // VEC consecutive elements of a row as floats
@@ -89,13 +89,11 @@ __device__ __forceinline__ void load_weight(const float* w, int col, float (&v)[
   }
 }
 
-__device__ __forceinline__ float sigmoid_f(float z) {
-  const float e = __expf(-fabsf(z)), big = __frcp_rn(1.f + e);
-  return z >= 0.f ? big : e * big;
-}
+// (the exponential of a z far below zero is infinite, and the quotient zero)
+__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 
-// sums over the G threads that share a row (G a power of two, 32..1024, aligned inside the block);
-// `buf` double-buffers by call so that one barrier a reduction is enough
+// sums over the G threads that share a row (G a power of two, 32..1024, aligned inside the block); the
+// caller alternates between two buffers, so that one barrier a reduction is enough
 template <int G, int N>
 __device__ __forceinline__ void row_sum(float (&s)[N], float* buf) {
 #pragma unroll
@@ -107,112 +105,138 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* buf) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp / W * W;
     if (lane == 0)
 #pragma unroll
-      for (int i = 0; i < N; ++i) buf[warp * N + i] = s[i];
+      for (int i = 0; i < N; ++i) buf[i * 32 + warp] = s[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = 0.f;
+    for (int i = 0; i < N; ++i) s[i] = buf[i * 32 + first + (lane & (W - 1))];
 #pragma unroll
-    for (int w = 0; w < W; ++w)
+    for (int o = W / 2; o; o >>= 1)
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[i] += buf[(first + w) * N + i];
+      for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
   }
 }
 
+// per-column constants of a thread: scale times post-norm weight, pre-norm weight
+template <int VEC, int G, int K>
+__device__ __forceinline__ void column_constants(const NormArgs& a, int t, float (&ks)[K][VEC], float (&wn)[K][VEC]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * G + t) * VEC;
+    if (c < a.cols) {
+      float wp[VEC], sc[VEC];
+      load_weight<VEC>(a.w_post, c, wp);
+      load_weight<VEC>(a.scale, c, sc);
+      load_weight<VEC>(a.w_pre, c, wn[k]);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) ks[k][i] = wp[i] * sc[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) ks[k][i] = wn[k][i] = 0.f;
+    }
+  }
+}
+
+// The grid is persistent in both directions: a thread meets the same columns in every row, keeps their
+// weights in registers, and has the next row's loads under way while it works on the present one.
 template <typename T, int VEC, int G, int K>
-__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads)
+__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 2)
 norm_forward_kernel(const NormArgs a) {
   using P = Pack<T, VEC>;
   using Raw = typename P::Raw;
   constexpr int kRows = (G > kNormThreads ? G : kNormThreads) / G;
   __shared__ float buf[2][32];
-  const int t = threadIdx.x % G;
-  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
-  const bool live = row < a.rows;
-  if (!live) row = a.rows - 1;                // takes part in the barriers, stores nothing
+  const int t = threadIdx.x % G, sub = threadIdx.x / G;
   const int D = a.cols;
-  const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  const T* b = static_cast<const T*>(a.b);
-  const T* z = static_cast<const T*>(a.z);
-  if (b) b += row * a.ld_b;
-  if (z) z += row * a.ld_z;
+  const float inv_d = 1.f / (float)D;
+  const bool has_b = a.b != nullptr, has_z = a.z != nullptr;
   Raw rx[K], rb[K], rz[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = (k * G + t) * VEC;
-    rx[k] = rb[k] = rz[k] = P::zero();
-    if (c < D) {
-      rx[k] = *reinterpret_cast<const Raw*>(x + c);
-      if (b) rb[k] = *reinterpret_cast<const Raw*>(b + c);
-      if (z) rz[k] = *reinterpret_cast<const Raw*>(z + c);
-    }
-  }
-  float inv_b = 1.f;
-  if (b && a.w_post) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float v[VEC];
-      P::get(rb[k], v);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) s[0] = fmaf(v[i], v[i], s[0]);
-    }
-    row_sum<G, 1>(s, buf[0]);
-    inv_b = rsqrtf(s[0] / (float)D + a.eps);
-  }
-  float y[K][VEC];
-  float s[1] = {0.f};
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = (k * G + t) * VEC;
-    P::get(rx[k], y[k]);
-    if (b && c < D) {
-      float vb[VEC], vz[VEC], wp[VEC], sc[VEC];
-      P::get(rb[k], vb);
-      load_weight<VEC>(a.w_post, c, wp);
-      load_weight<VEC>(a.scale, c, sc);
-      P::get(rz[k], vz);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float gate = z ? vz[i] * sigmoid_f(vz[i]) : 1.f;
-        y[k][i] = fmaf(sc[i] * gate, vb[i] * inv_b * wp[i], y[k][i]);
-      }
-    }
-    if (live && a.x_out && c < D)
-      *reinterpret_cast<Raw*>(static_cast<T*>(a.x_out) + row * D + c) = P::put(y[k]);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) s[0] = fmaf(y[k][i], y[k][i], s[0]);
-  }
-  float inv_x = 1.f;
-  if (a.w_pre) {
-    row_sum<G, 1>(s, buf[1]);
-    inv_x = rsqrtf(s[0] / (float)D + a.eps);
+  auto load = [&](int64_t row) {
+    if (row >= a.rows) row = a.rows - 1;        // takes part in the barriers, stores nothing
+    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+    const T* b = static_cast<const T*>(a.b) + row * a.ld_b;
+    const T* z = static_cast<const T*>(a.z) + row * a.ld_z;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * G + t) * VEC;
-      if (live && c < D) {
-        float w[VEC], o[VEC];
-        load_weight<VEC>(a.w_pre, c, w);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) o[i] = y[k][i] * inv_x * w[i];
-        *reinterpret_cast<Raw*>(static_cast<T*>(a.n) + row * D + c) = P::put(o);
+      rx[k] = rb[k] = rz[k] = P::zero();
+      if (c < D) {
+        rx[k] = __ldcs(reinterpret_cast<const Raw*>(x + c));
+        if (has_b) rb[k] = __ldcs(reinterpret_cast<const Raw*>(b + c));
+        if (has_z) rz[k] = __ldcs(reinterpret_cast<const Raw*>(z + c));
       }
     }
-  }
-  if (live && a.inv_rms && t == 0) {
-    a.inv_rms[row] = inv_b;
-    a.inv_rms[a.rows + row] = inv_x;
+  };
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  load((int64_t)blockIdx.x * kRows + sub);
+  float ks[K][VEC], wn[K][VEC];
+  column_constants<VEC, G, K>(a, t, ks, wn);
+  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += stride) {
+    const int64_t row = base + sub;
+    const bool live = row < a.rows;
+    float y[K][VEC], tau[K][VEC];
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float vb[VEC], vz[VEC];
+      P::get(rx[k], y[k]);
+      P::get(rb[k], vb);
+      P::get(rz[k], vz);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        s[0] = fmaf(vb[i], vb[i], s[0]);
+        tau[k][i] = ks[k][i] * vb[i] * (has_z ? vz[i] * sigmoid_f(vz[i]) : 1.f);
+      }
+    }
+    if (base + stride < a.rows) load(row + stride);
+    float inv_b = 1.f;
+    if (a.w_post) {
+      row_sum<G, 1>(s, buf[0]);
+      inv_b = rsqrtf(fmaf(s[0], inv_d, a.eps));
+    }
+    s[0] = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * G + t) * VEC;
+      if (has_b)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[k][i] = fmaf(tau[k][i], inv_b, y[k][i]);
+      if (live && a.x_out && c < D) __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.x_out) + row * D + c), P::put(y[k]));
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s[0] = fmaf(y[k][i], y[k][i], s[0]);
+    }
+    float inv_x = 1.f;
+    if (a.w_pre) {
+      row_sum<G, 1>(s, buf[1]);
+      inv_x = rsqrtf(fmaf(s[0], inv_d, a.eps));
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int c = (k * G + t) * VEC;
+        if (live && c < D) {
+          float o[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) o[i] = y[k][i] * inv_x * wn[k][i];
+          __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.n) + row * D + c), P::put(o));
+        }
+      }
+    }
+    if (live && a.inv_rms && t == 0) {
+      a.inv_rms[row] = inv_b;
+      a.inv_rms[a.rows + row] = inv_x;
+    }
+    // (each buffer is written again only after the other's barrier, or this row's, has been passed by all)
+    if (G > 32 && !(a.w_post && a.w_pre)) __syncthreads();
   }
 }
 
-// Backward of a row, with xh = x' / rms, bh = b / rms, q = dn w_pre, tau = scale silu(z) w_post bh:
-//   dx  = dx_out + (q - xh m1) / rms(x'),             m1 = mean(q xh)
-//   dp  = dx scale silu(z);  db = (dp w_post - bh m2) / rms(b),  m2 = mean(dp w_post bh) = mean(dx tau)
+// Backward of a row, with xh = x' / rms, bh = b / rms, q = dn w_pre, ks = scale w_post, tau = ks silu(z) bh:
+//   dx = dx_out + (q - xh m1) / rms(x'),                m1 = mean(q xh)
+//   db = (dx ks silu(z) - bh m2) / rms(b),              m2 = mean(dx tau)
+//   dz = dx ks bh silu'(z);   dw_pre = sum dn xh;   dw_post = scale S, dscale = w_post S,  S = sum dx silu(z) bh
 // m2 needs dx, which needs m1; written out, mean(dx tau) = mean((dx_out + q/rms) tau) - m1 mean(xh tau)/rms,
-// so the three sums go through ONE reduction a row.
-// The grid is persistent; a thread meets the same columns in every row and keeps its share of the
-// weight gradients in registers, partials meet in fixed order in norm_reduce_kernel.
+// so the three sums go through ONE reduction a row.  A thread keeps its columns' two sums over rows in
+// registers; the blocks' partials meet in fixed order in norm_reduce_kernel.
 template <typename T, int VEC, int G, int K>
-__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads)
+__global__ void __launch_bounds__(G > kNormThreads ? G : kNormThreads, G > kNormThreads ? 1 : 2)
 norm_backward_kernel(const NormArgs a) {
   using P = Pack<T, VEC>;
   using Raw = typename P::Raw;
@@ -221,145 +245,142 @@ norm_backward_kernel(const NormArgs a) {
   __shared__ float buf[2][96];
   const int t = threadIdx.x % G, sub = threadIdx.x / G;
   const int D = a.cols;
-  const bool has_b = a.b != nullptr, has_z = a.z != nullptr;
-  float acc_wp[K][VEC], acc_sc[K][VEC], acc_wn[K][VEC];
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) acc_wp[k][i] = acc_sc[k][i] = acc_wn[k][i] = 0.f;
-  int flip = 0;
-  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += (int64_t)gridDim.x * kRows) {
-    int64_t row = base + sub;
-    const bool live = row < a.rows;
-    if (!live) row = a.rows - 1;
+  const float inv_d = 1.f / (float)D;
+  const bool has_b = a.b != nullptr, has_z = a.z != nullptr, normed = a.w_post != nullptr;
+  Raw rx[K], rb[K], rz[K], ro[K], rn[K];
+  float next_b = 0.f, next_x = 0.f;
+  auto load = [&](int64_t row) {
+    if (row >= a.rows) row = a.rows - 1;        // takes part in the barriers, counts for nothing
     const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-    const T* b = has_b ? static_cast<const T*>(a.b) + row * a.ld_b : nullptr;
-    const T* z = has_z ? static_cast<const T*>(a.z) + row * a.ld_z : nullptr;
-    const T* go = a.dx_out ? static_cast<const T*>(a.dx_out) + row * D : nullptr;
-    const T* gn = a.dn ? static_cast<const T*>(a.dn) + row * D : nullptr;
-    Raw rx[K], rb[K], rz[K], ro[K], rn[K];
+    const T* b = static_cast<const T*>(a.b) + row * a.ld_b;
+    const T* z = static_cast<const T*>(a.z) + row * a.ld_z;
+    const T* go = static_cast<const T*>(a.dx_out) + row * D;
+    const T* gn = static_cast<const T*>(a.dn) + row * D;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * G + t) * VEC;
       rx[k] = rb[k] = rz[k] = ro[k] = rn[k] = P::zero();
       if (c < D) {
-        rx[k] = *reinterpret_cast<const Raw*>(x + c);
-        if (b) rb[k] = *reinterpret_cast<const Raw*>(b + c);
-        if (z) rz[k] = *reinterpret_cast<const Raw*>(z + c);
-        if (go) ro[k] = *reinterpret_cast<const Raw*>(go + c);
-        if (gn) rn[k] = *reinterpret_cast<const Raw*>(gn + c);
+        rx[k] = __ldcs(reinterpret_cast<const Raw*>(x + c));
+        if (has_b) rb[k] = __ldcs(reinterpret_cast<const Raw*>(b + c));
+        if (has_z) rz[k] = __ldcs(reinterpret_cast<const Raw*>(z + c));
+        if (a.dx_out) ro[k] = __ldcs(reinterpret_cast<const Raw*>(go + c));
+        if (a.dn) rn[k] = __ldcs(reinterpret_cast<const Raw*>(gn + c));
       }
     }
-    const float inv_b = a.rms_in[row], inv_x = a.rms_in[a.rows + row];
-    const float inv_d = 1.f / (float)D;
+    next_b = a.rms_in[row];
+    next_x = a.rms_in[a.rows + row];
+  };
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  load((int64_t)blockIdx.x * kRows + sub);
+  float ks[K][VEC], wn[K][VEC], acc_s[K][VEC], acc_n[K][VEC];
+  column_constants<VEC, G, K>(a, t, ks, wn);
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc_s[k][i] = acc_n[k][i] = 0.f;
+  int flip = 0;
+  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += stride) {
+    const int64_t row = base + sub;
+    const bool live = row < a.rows;
+    const float inv_b = next_b, inv_x = a.w_pre ? next_x : 0.f, xs = next_x;
+    // kept over the reduction: dx_out + q / rms(x'), xh, silu(z), silu'(z), b
+    float A[K][VEC], xh[K][VEC], gate[K][VEC], slope[K][VEC];
+    Raw cb[K];
     float s[3] = {0.f, 0.f, 0.f};
-    // one element's quantities, formed again after the reduction (cheaper than keeping them)
-    struct El { float xh, bh, gate, dgate, q, go; };
-    auto element = [&](float vx, float vb, float vz, float vo, float vn, float wp, float sc, float wn) {
-      El e;
-      float sig = 1.f;
-      e.gate = 1.f;
-      e.dgate = 0.f;
-      if (has_z) {
-        sig = sigmoid_f(vz);
-        e.gate = vz * sig;
-        e.dgate = sig * fmaf(vz, 1.f - sig, 1.f);
-      }
-      e.bh = vb * inv_b;
-      e.xh = (has_b ? fmaf(sc * e.gate, e.bh * wp, vx) : vx) * inv_x;
-      e.q = vn * wn;
-      e.go = vo;
-      return e;
-    };
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = (k * G + t) * VEC;
-      if (c >= D) continue;
-      float vx[VEC], vb[VEC], vz[VEC], vo[VEC], vn[VEC], wp[VEC], sc[VEC], wn[VEC];
+      float vx[VEC], vb[VEC], vz[VEC], vo[VEC], vn[VEC];
       P::get(rx[k], vx); P::get(rb[k], vb); P::get(rz[k], vz); P::get(ro[k], vo); P::get(rn[k], vn);
-      load_weight<VEC>(a.w_post, c, wp); load_weight<VEC>(a.scale, c, sc); load_weight<VEC>(a.w_pre, c, wn);
+      cb[k] = rb[k];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const El e = element(vx[i], vb[i], vz[i], vo[i], vn[i], wp[i], sc[i], wn[i]);
-        const float tau = sc[i] * e.gate * wp[i] * e.bh;
-        s[0] = fmaf(e.q, e.xh, s[0]);
-        s[1] = fmaf(fmaf(e.q, inv_x, e.go), tau, s[1]);
-        s[2] = fmaf(e.xh, tau, s[2]);
+        gate[k][i] = 1.f;
+        slope[k][i] = 0.f;
+        if (has_z) {
+          const float sig = sigmoid_f(vz[i]);
+          gate[k][i] = vz[i] * sig;
+          slope[k][i] = sig * fmaf(vz[i], 1.f - sig, 1.f);
+        }
+        const float tau = ks[k][i] * (vb[i] * inv_b) * gate[k][i];
+        xh[k][i] = (has_b ? vx[i] + tau : vx[i]) * xs;
+        const float q = vn[i] * wn[k][i];
+        A[k][i] = fmaf(q, inv_x, vo[i]);
+        s[0] = fmaf(q, xh[k][i], s[0]);
+        s[1] = fmaf(A[k][i], tau, s[1]);
+        s[2] = fmaf(xh[k][i], tau, s[2]);
+        if (live) acc_n[k][i] = fmaf(vn[i], xh[k][i], acc_n[k][i]);
       }
     }
+    if (base + stride < a.rows) load(row + stride);
     row_sum<G, 3>(s, buf[flip]);
     flip ^= 1;
-    const float m1 = a.w_pre ? s[0] * inv_d : 0.f;
-    const float m2 = (s[1] - m1 * inv_x * s[2]) * inv_d;
+    const float m1 = s[0] * inv_d * inv_x;
+    const float m2 = normed ? fmaf(-m1, s[2], s[1]) * inv_d * inv_b : 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * G + t) * VEC;
       if (c >= D || !live) continue;
-      float vx[VEC], vb[VEC], vz[VEC], vo[VEC], vn[VEC], wp[VEC], sc[VEC], wn[VEC];
-      P::get(rx[k], vx); P::get(rb[k], vb); P::get(rz[k], vz); P::get(ro[k], vo); P::get(rn[k], vn);
-      load_weight<VEC>(a.w_post, c, wp); load_weight<VEC>(a.scale, c, sc); load_weight<VEC>(a.w_pre, c, wn);
-      float ox[VEC], ob[VEC], oz[VEC];
+      float vb[VEC], ox[VEC], ob[VEC], oz[VEC];
+      P::get(cb[k], vb);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const El e = element(vx[i], vb[i], vz[i], vo[i], vn[i], wp[i], sc[i], wn[i]);
-        const float dx = a.w_pre ? fmaf(inv_x, e.q - e.xh * m1, e.go) : e.go;
+        const float dx = fmaf(-xh[k][i], m1, A[k][i]), bh = vb[i] * inv_b, dk = dx * ks[k][i], dg = dx * gate[k][i];
         ox[i] = dx;
-        if (has_b) {
-          const float p = e.bh * wp[i], dxg = dx * e.gate, dp = dxg * sc[i];
-          ob[i] = a.w_post ? inv_b * (dp * wp[i] - e.bh * m2) : dp;
-          oz[i] = dx * sc[i] * p * e.dgate;
-          acc_wp[k][i] = fmaf(dp, e.bh, acc_wp[k][i]);
-          acc_sc[k][i] = fmaf(dxg, p, acc_sc[k][i]);
-        }
-        acc_wn[k][i] = fmaf(vn[i], e.xh, acc_wn[k][i]);
+        ob[i] = fmaf(dk * gate[k][i], inv_b, -bh * m2);
+        oz[i] = dk * bh * slope[k][i];
+        acc_s[k][i] = fmaf(dg, bh, acc_s[k][i]);
       }
-      if (a.dx) *reinterpret_cast<Raw*>(static_cast<T*>(a.dx) + row * D + c) = P::put(ox);
-      if (a.db) *reinterpret_cast<Raw*>(static_cast<T*>(a.db) + row * D + c) = P::put(ob);
-      if (a.dz) *reinterpret_cast<Raw*>(static_cast<T*>(a.dz) + row * D + c) = P::put(oz);
+      if (a.dx) __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.dx) + row * D + c), P::put(ox));
+      if (a.db) __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.db) + row * D + c), P::put(ob));
+      if (a.dz) __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.dz) + row * D + c), P::put(oz));
     }
   }
   if (a.partials == nullptr) return;
-  // rows that share a block meet here; block partials meet in norm_reduce_kernel
-  float* out = a.partials + ((int64_t)blockIdx.x * kRows + sub) * 3 * D;
+  float* out = a.partials + ((int64_t)blockIdx.x * kRows + sub) * 2 * D;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = (k * G + t) * VEC;
     if (c >= D) continue;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      out[c + i] = acc_wp[k][i];
-      out[D + c + i] = acc_sc[k][i];
-      out[2 * D + c + i] = acc_wn[k][i];
+      out[c + i] = acc_s[k][i];
+      out[D + c + i] = acc_n[k][i];
     }
   }
 }
 
-// sums of `parts` rows of [3][D], in fixed order: a block owns 32 columns, its 8 warps the parts w, w+8, ...
-__global__ void __launch_bounds__(256)
-norm_reduce_kernel(const float* __restrict__ partials, int parts, int D, float* __restrict__ dw_post,
-                   float* __restrict__ dscale, float* __restrict__ dw_pre) {
-  __shared__ float buf[8][33];
+// sums of `parts` rows of [2][D], in fixed order: a block owns 32 columns, its 32 warps the parts w, w + 32, ...
+__global__ void __launch_bounds__(1024)
+norm_reduce_kernel(const float* __restrict__ partials, int parts, int D, const float* __restrict__ w_post,
+                   const float* __restrict__ scale, float* dw_post, float* dscale, float* dw_pre) {
+  __shared__ float buf[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane, which = blockIdx.y;
-  float* out = which == 0 ? dw_post : (which == 1 ? dscale : dw_pre);
-  if (out == nullptr) return;
+  if (which == 0 ? !dw_post && !dscale : !dw_pre) return;
   float s = 0.f;
   if (c < D)
-    for (int p = warp; p < parts; p += 8) s += partials[((int64_t)p * 3 + which) * D + c];
+    for (int p = warp; p < parts; p += 32) s += partials[((int64_t)p * 2 + which) * D + c];
   buf[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < D) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) v += buf[w][lane];
-    out[c] = v;
+    for (int w = 0; w < 32; ++w) v += buf[w][lane];
+    if (which == 1) {
+      dw_pre[c] = v;
+    } else {
+      if (dw_post) dw_post[c] = v * (scale ? scale[c] : 1.f);
+      if (dscale) dscale[c] = v * (w_post ? w_post[c] : 1.f);
+    }
   }
 }
 
-// threads that share a row of `cols`: as few as keep 16 values a thread (32 beyond 16384 columns)
-int group_of(int cols) {
+// Threads that share a row of `cols`: the forward pass keeps 16 values a thread, the backward pass, whose
+// threads also carry three sums a column and the next row's five tensors, 8 (more beyond 512 threads' worth).
+int group_of(int cols, bool backward) {
   int g = 32;
-  while (g < 1024 && g * 16 < cols) g <<= 1;
+  while (g < (backward ? 512 : 1024) && g * (backward ? 8 : 16) < cols) g <<= 1;
   return g;
 }
 int rows_per_block(int g) { return g > kNormThreads ? 1 : kNormThreads / g; }
@@ -373,38 +394,52 @@ int norm_sms() {
   }
   return n;
 }
-// blocks of the backward pass: two blocks of 256 threads (or one larger) an SM
+// blocks of the backward pass: two of 256 threads (or one of 512) an SM
 int64_t backward_blocks(int64_t rows, int cols) {
-  const int g = group_of(cols), r = rows_per_block(g);
-  const int64_t need = (rows + r - 1) / r, most = (int64_t)norm_sms() * (g > 512 ? 1 : 2);
+  const int g = group_of(cols, true), r = rows_per_block(g);
+  const int64_t need = (rows + r - 1) / r, most = (int64_t)norm_sms() * (g > 256 ? 1 : 2);
   return need < most ? need : most;
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
-template <typename T, int VEC, int G, int K>
-mw_status launch_norm(const NormArgs& a, bool backward, cudaStream_t s) {
-  const int threads = G > kNormThreads ? G : kNormThreads, r = threads / G;
-  const int64_t need = (a.rows + r - 1) / r;
-  if (backward)
-    norm_backward_kernel<T, VEC, G, K><<<(unsigned)backward_blocks(a.rows, a.cols), threads, 0, s>>>(a);
-  else
-    norm_forward_kernel<T, VEC, G, K><<<(unsigned)need, threads, 0, s>>>(a);
+template <typename T, int VEC, int G, int VALUES>
+mw_status launch_forward(const NormArgs& a, cudaStream_t s) {
+  constexpr int threads = G > kNormThreads ? G : kNormThreads, r = threads / G;
+  const int64_t need = (a.rows + r - 1) / r, most = (int64_t)norm_sms() * (G > kNormThreads ? 1 : 2);
+  norm_forward_kernel<T, VEC, G, VALUES / VEC><<<(unsigned)(need < most ? need : most), threads, 0, s>>>(a);
+  return launch_ok();
+}
+template <typename T, int VEC, int G, int VALUES>
+mw_status launch_backward(const NormArgs& a, cudaStream_t s) {
+  constexpr int threads = G > kNormThreads ? G : kNormThreads;
+  norm_backward_kernel<T, VEC, G, VALUES / VEC><<<(unsigned)backward_blocks(a.rows, a.cols), threads, 0, s>>>(a);
   return launch_ok();
 }
 
 template <typename T, int VEC>
 mw_status dispatch_norm(const NormArgs& a, bool backward, cudaStream_t s) {
-  constexpr int K = 16 / VEC;
-  switch (group_of(a.cols)) {
-    case 32: return launch_norm<T, VEC, 32, K>(a, backward, s);
-    case 64: return launch_norm<T, VEC, 64, K>(a, backward, s);
-    case 128: return launch_norm<T, VEC, 128, K>(a, backward, s);
-    case 256: return launch_norm<T, VEC, 256, K>(a, backward, s);
-    case 512: return launch_norm<T, VEC, 512, K>(a, backward, s);
+  if (backward) {
+    switch (group_of(a.cols, true)) {
+      case 32: return launch_backward<T, VEC, 32, 8>(a, s);
+      case 64: return launch_backward<T, VEC, 64, 8>(a, s);
+      case 128: return launch_backward<T, VEC, 128, 8>(a, s);
+      case 256: return launch_backward<T, VEC, 256, 8>(a, s);
+      default:
+        if (a.cols <= 4096) return launch_backward<T, VEC, 512, 8>(a, s);
+        if (a.cols <= 8192) return launch_backward<T, VEC, 512, 16>(a, s);
+        if (a.cols <= 16384) return launch_backward<T, VEC, 512, 32>(a, s);
+        return launch_backward<T, VEC, 512, 64>(a, s);
+    }
+  }
+  switch (group_of(a.cols, false)) {
+    case 32: return launch_forward<T, VEC, 32, 16>(a, s);
+    case 64: return launch_forward<T, VEC, 64, 16>(a, s);
+    case 128: return launch_forward<T, VEC, 128, 16>(a, s);
+    case 256: return launch_forward<T, VEC, 256, 16>(a, s);
+    case 512: return launch_forward<T, VEC, 512, 16>(a, s);
     default:
-      return a.cols <= 16384 ? launch_norm<T, VEC, 1024, K>(a, backward, s)
-                             : launch_norm<T, VEC, 1024, 2 * K>(a, backward, s);
+      return a.cols <= 16384 ? launch_forward<T, VEC, 1024, 16>(a, s) : launch_forward<T, VEC, 1024, 32>(a, s);
   }
 }
 
@@ -456,7 +491,7 @@ extern "C" mw_status mw_residual_norm_scratch_bytes(const mw_residual_norm_desc*
   using namespace mw;
   if (!desc || !bytes || desc->rows < 0 || desc->cols < 1) return MW_ERR_INVALID_ARG;
   if (desc->cols > kMaxCols) return MW_ERR_UNSUPPORTED;
-  *bytes = (size_t)backward_blocks(desc->rows, desc->cols) * rows_per_block(group_of(desc->cols)) * 3 *
+  *bytes = (size_t)backward_blocks(desc->rows, desc->cols) * rows_per_block(group_of(desc->cols, true)) * 2 *
            (size_t)desc->cols * sizeof(float);
   return MW_OK;
 }
@@ -491,8 +526,8 @@ extern "C" mw_status mw_residual_norm_backward(const mw_residual_norm_desc* desc
   }
   MW_TRY(desc->dtype == 1 ? (run_norm<float, 4>(a, true, s)) : (run_norm<__nv_bfloat16, 8>(a, true, s)));
   if (!sums) return MW_OK;
-  const int parts = (int)backward_blocks(a.rows, a.cols) * rows_per_block(group_of(a.cols));
-  norm_reduce_kernel<<<dim3((unsigned)((a.cols + 31) / 32), 3), 256, 0, s>>>(a.partials, parts, a.cols, dw_post, dscale,
-                                                                             dw_pre);
+  const int parts = (int)backward_blocks(a.rows, a.cols) * rows_per_block(group_of(a.cols, true));
+  norm_reduce_kernel<<<dim3((unsigned)((a.cols + 31) / 32), 2), 1024, 0, s>>>(a.partials, parts, a.cols, w_post, scale,
+                                                                              dw_post, dscale, dw_pre);
   return launch_ok();
 }
