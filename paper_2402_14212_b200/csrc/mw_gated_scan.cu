@@ -28,23 +28,28 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
 // a = sigmoid(f) and w = 1 - a, each to full relative accuracy at either end (one exponential, one
-// reciprocal: 1 - a formed by subtraction would lose the slow channels, where a is close to 1).
-// f below -80 counts as -80 (a = 2e-35), which keeps the exponential finite; NaN stays NaN.
+// reciprocal: 1 - a formed by subtraction would lose the slow channels, where a is close to 1).  The
+// exponent is held below 116, where a is 1e-35 and w exactly 1: the exponential stays finite.  NaN stays NaN.
 __device__ __forceinline__ void gate_of(float f, float& a, float& w) {
-  float g;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(g) : "f"(f), "f"(-80.f));
-  const float e = __expf(-g);
-  a = __fdividef(1.f, 1.f + e);
+  float x, e;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(f * -1.4426950408889634f), "f"(116.f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.f + e));
   w = e * a;
+}
+__device__ __forceinline__ float sqrt_of(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 template <int GATE>
 __device__ __forceinline__ float input_of(float a, float w) {
-  return GATE == MW_SCAN_COMPLEMENT ? w : sqrtf(w * (1.f + a));
+  return GATE == MW_SCAN_COMPLEMENT ? w : sqrt_of(fmaf(w, a, w));
 }
 // a (1 - a) u'(a): -a w, or -a^2 w / u = -a^2 sqrt(w / (1 + a)) (finite where u is zero)
 template <int GATE>
 __device__ __forceinline__ float input_slope(float a, float w) {
-  return GATE == MW_SCAN_COMPLEMENT ? -a * w : -a * a * sqrtf(__fdividef(w, 1.f + a));
+  return GATE == MW_SCAN_COMPLEMENT ? -a * w : -a * a * sqrt_of(__fdividef(w, 1.f + a));
 }
 
 __device__ __forceinline__ int length_of(const ScanArgs& p, int b) {
@@ -212,42 +217,61 @@ struct Exchange {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) warp_map[flip][warp][i][lane] = make_float2(P[i], H[i]);
     __syncthreads();
-    float pe[VEC], he[VEC], pt[VEC], ht[VEC];     // before this warp, and of the whole block
+    if (C > 1) {
+      // warp w sends the block's whole map to ranks w, w + W, ...
+      if (warp < C) {
+        float2 whole[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      pt[i] = 1.f;
-      ht[i] = 0.f;
+        for (int i = 0; i < VEC; ++i) {
+          whole[i] = make_float2(1.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < kScanWarps; ++k) {
-        const int w = REVERSE ? kScanWarps - 1 - k : k;
-        if (w == warp) { pe[i] = pt[i]; he[i] = ht[i]; }
-        const float2 m = warp_map[flip][w][i][lane];
-        ht[i] = affine<CUT>(m.x, ht[i], m.y);
-        pt[i] *= m.x;
+          for (int k = 0; k < kScanWarps; ++k) {
+            const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][i][lane];
+            whole[i].y = affine<CUT>(m.x, whole[i].y, m.y);
+            whole[i].x *= m.x;
+          }
+        }
+        for (int r = warp; r < C; r += kScanWarps)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) store_to_rank(&block_map[flip][rank][i][lane], r, whole[i]);
+      }
+      cluster_arrive();
+    }
+    // while the others' maps arrive: the maps of this block's warps before this one
+    const int before = REVERSE ? kScanWarps - 1 - warp : warp;
+    float pe[VEC], he[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) { pe[i] = 1.f; he[i] = 0.f; }
+    for (int k = 0; k < before; ++k) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][i][lane];
+        he[i] = affine<CUT>(m.x, he[i], m.y);
+        pe[i] *= m.x;
       }
     }
     if (C > 1) {
-      for (int r = warp; r < C; r += kScanWarps)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) store_to_rank(&block_map[flip][rank][i][lane], r, make_float2(pt[i], ht[i]));
-      cluster_arrive();
       cluster_wait();
+      const int first = REVERSE ? C - 1 - rank : rank;      // blocks before this one
+      for (int k = 0; k < C; ++k) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        float h = carry[i];
-        for (int k = 0; k < C; ++k) {
-          const int r = REVERSE ? C - 1 - k : k;
-          if (r == rank) start[i] = h;
-          const float2 m = block_map[flip][r][i][lane];
-          h = affine<CUT>(m.x, h, m.y);
+        for (int i = 0; i < VEC; ++i) {
+          if (k == first) start[i] = carry[i];
+          const float2 m = block_map[flip][REVERSE ? C - 1 - k : k][i][lane];
+          carry[i] = affine<CUT>(m.x, carry[i], m.y);
         }
-        carry[i] = h;
       }
     } else {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         start[i] = carry[i];
-        carry[i] = affine<CUT>(pt[i], carry[i], ht[i]);
+        float p = pe[i], h = he[i];
+        for (int k = before; k < kScanWarps; ++k) {
+          const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][i][lane];
+          h = affine<CUT>(m.x, h, m.y);
+          p *= m.x;
+        }
+        carry[i] = affine<CUT>(p, carry[i], h);
       }
     }
 #pragma unroll
@@ -255,7 +279,20 @@ struct Exchange {
   }
 };
 
-// grid (C, channel blocks, batch), clusters of C blocks along x
+// a step's rows lie 32-bit byte offsets apart inside a thread's kEvery steps (checked by the host)
+template <typename Raw>
+__device__ __forceinline__ Raw load_row(const void* base, int offset) {
+  return __ldcs(reinterpret_cast<const Raw*>(static_cast<const char*>(base) + offset));
+}
+template <typename Raw>
+__device__ __forceinline__ void store_row(void* base, int offset, Raw v) {
+  __stcs(reinterpret_cast<Raw*>(static_cast<char*>(base) + offset), v);
+}
+template <bool V>
+struct Flag { static constexpr bool value = V; };
+
+// grid (C, channel blocks, batch), clusters of C blocks along x.  Pieces that lie wholly inside the sequence
+// take a path without a test a step; the tests of the other path are warp-uniform.
 template <typename T, int VEC, int GATE, bool CUT>
 __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_chunk_kernel(const ScanArgs p) {
@@ -268,23 +305,28 @@ scan_chunk_kernel(const ScanArgs p) {
   const bool live = c < p.D;
   const int n = length_of(p, b);
   const int piece = C * kScanWarps * kEvery;
-  const T* vb = static_cast<const T*>(p.v) + b * p.v_b + c;
-  const T* fb = static_cast<const T*>(p.f) + b * p.f_b + c;
   const int64_t nst = (p.T + kEvery - 1) / kEvery;
+  const int v_row = (int)(p.v_t * sizeof(T)), f_row = (int)(p.f_t * sizeof(T)), y_row = (int)(p.y_t * sizeof(T));
+  const int cc = live ? c : 0;       // lanes past the last channel read the first, and store nothing
   Raw rv[kEvery], rf[kEvery];
-  // (steps are the same for all lanes: the tests on t are warp-uniform)
   auto load = [&](int t0) {
-    const T* v = vb + t0 * p.v_t;
-    const T* f = fb + t0 * p.f_t;
+    const T* v = static_cast<const T*>(p.v) + b * p.v_b + cc + t0 * p.v_t;
+    const T* f = static_cast<const T*>(p.f) + b * p.f_b + cc + t0 * p.f_t;
+    if (t0 + kEvery <= n) {
 #pragma unroll
-    for (int j = 0; j < kEvery; ++j) {
-      rv[j] = rf[j] = L::zero();
-      if (live && t0 + j < n) {
-        rv[j] = __ldcs(reinterpret_cast<const Raw*>(v));
-        rf[j] = __ldcs(reinterpret_cast<const Raw*>(f));
+      for (int j = 0; j < kEvery; ++j) {
+        rv[j] = load_row<Raw>(v, j * v_row);
+        rf[j] = load_row<Raw>(f, j * f_row);
       }
-      v += p.v_t;
-      f += p.f_t;
+    } else {
+#pragma unroll
+      for (int j = 0; j < kEvery; ++j) {
+        rv[j] = rf[j] = L::zero();
+        if (t0 + j < n) {
+          rv[j] = load_row<Raw>(v, j * v_row);
+          rf[j] = load_row<Raw>(f, j * f_row);
+        }
+      }
     }
   };
   int t0 = (rank * kScanWarps + warp) * kEvery;
@@ -292,30 +334,32 @@ scan_chunk_kernel(const ScanArgs p) {
   cluster_start(C);
   float carry[VEC];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) carry[i] = p.h0 && live ? p.h0[(int64_t)b * p.D + c + i] : 0.f;
+  for (int i = 0; i < VEC; ++i) carry[i] = p.h0 ? p.h0[(int64_t)b * p.D + cc + i] : 0.f;
   int flip = 0;
   for (int base = 0; base < p.T; base += piece, t0 += piece, flip ^= 1) {
     float a[kEvery][VEC], in[kEvery][VEC], P[VEC], H[VEC], h[VEC];
+    const bool whole = t0 + kEvery <= n;
+    auto compose = [&](auto full) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) { P[i] = 1.f; H[i] = 0.f; }
+      for (int j = 0; j < kEvery; ++j) {
+        float v[VEC], f[VEC];
+        L::get(rv[j], v);
+        L::get(rf[j], f);
+        const bool on = decltype(full)::value || t0 + j < n;
+        const bool cut = CUT && on && p.reset[(int64_t)b * p.T + t0 + j] != 0;
 #pragma unroll
-    for (int j = 0; j < kEvery; ++j) {
-      float v[VEC], f[VEC];
-      L::get(rv[j], v);
-      L::get(rf[j], f);
-      const bool on = t0 + j < n;
-      const bool cut = CUT && on && p.reset[(int64_t)b * p.T + t0 + j] != 0;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        float w;
-        gate_of(f[i], a[j][i], w);
-        in[j][i] = input_of<GATE>(a[j][i], w) * v[i];
-        if (CUT && cut) a[j][i] = 0.f;
-        if (!on) { a[j][i] = 1.f; in[j][i] = 0.f; }
-        H[i] = affine<CUT>(a[j][i], H[i], in[j][i]);
-        P[i] *= a[j][i];
+        for (int i = 0; i < VEC; ++i) {
+          float w;
+          gate_of(f[i], a[j][i], w);
+          in[j][i] = input_of<GATE>(a[j][i], w) * v[i];
+          if (CUT && cut) a[j][i] = 0.f;
+          if (!on) { a[j][i] = 1.f; in[j][i] = 0.f; }
+          P[i] = j ? P[i] * a[j][i] : a[j][i];
+          H[i] = j ? affine<CUT>(a[j][i], H[i], in[j][i]) : in[j][i];
+        }
       }
-    }
+    };
+    if (whole) compose(Flag<true>()); else compose(Flag<false>());
     if (base + piece < p.T) load(t0 + piece);
     ex.run(P, H, carry, h, flip, rank, C);
     if (live && t0 < p.T) {
@@ -325,17 +369,19 @@ scan_chunk_kernel(const ScanArgs p) {
         for (int i = 0; i < VEC; ++i) st[i] = h[i];
       }
       T* y = static_cast<T*>(p.y) + b * p.y_b + c + t0 * p.y_t;
+      auto emit = [&](auto full) {
 #pragma unroll
-      for (int j = 0; j < kEvery; ++j) {
-        float o[VEC];
+        for (int j = 0; j < kEvery; ++j) {
+          float o[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          h[i] = affine<CUT>(a[j][i], h[i], in[j][i]);
-          o[i] = t0 + j < n ? h[i] : 0.f;
+          for (int i = 0; i < VEC; ++i) {
+            h[i] = affine<CUT>(a[j][i], h[i], in[j][i]);
+            o[i] = decltype(full)::value || t0 + j < n ? h[i] : 0.f;
+          }
+          if (decltype(full)::value || t0 + j < p.T) store_row<Raw>(y, j * y_row, L::put(o));
         }
-        if (t0 + j < p.T) __stcs(reinterpret_cast<Raw*>(y), L::put(o));
-        y += p.y_t;
-      }
+      };
+      if (whole) emit(Flag<true>()); else emit(Flag<false>());
     }
   }
   if (p.h_last && live && rank == 0 && warp == 0)
@@ -345,9 +391,10 @@ scan_chunk_kernel(const ScanArgs p) {
 
 // The cotangent runs from the end: a step maps G (the cotangent of the state after it) to
 // r a (G + dy), the cotangent of the state before it.  The states before each thread's steps were
-// kept by the forward pass, so h needs no exchange.
+// kept by the forward pass, so h needs no exchange.  Over the exchange a thread keeps, per step, 1 - a
+// (from which a and u follow), dy and the factor of g in df; resets are a bit mask, the same in all lanes.
 template <typename T, int VEC, int GATE, bool CUT>
-__global__ void __launch_bounds__(32 * kScanWarps)
+__global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_chunk_back_kernel(const ScanArgs p) {
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
@@ -356,94 +403,110 @@ scan_chunk_back_kernel(const ScanArgs p) {
   const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
   const int c = (blockIdx.y * 32 + lane) * VEC;
   const bool live = c < p.D;
+  const int cc = live ? c : 0;
   const int n = length_of(p, b);
   const int piece = C * kScanWarps * kEvery;
   const int64_t nst = (p.T + kEvery - 1) / kEvery;
   const int pieces = (p.T + piece - 1) / piece;
+  const int v_row = (int)(p.v_t * sizeof(T)), f_row = (int)(p.f_t * sizeof(T)), y_row = (int)(p.y_t * sizeof(T));
+  const int dv_row = (int)(p.dv_t * sizeof(T)), df_row = (int)(p.df_t * sizeof(T));
   cluster_start(C);
   float carry[VEC];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) carry[i] = p.dh_last && live ? p.dh_last[(int64_t)b * p.D + c + i] : 0.f;
+  for (int i = 0; i < VEC; ++i) carry[i] = p.dh_last ? p.dh_last[(int64_t)b * p.D + cc + i] : 0.f;
   int flip = 0;
   for (int it = pieces - 1; it >= 0; --it, flip ^= 1) {
     const int t0 = it * piece + (rank * kScanWarps + warp) * kEvery;
+    const bool whole = t0 + kEvery <= n;
     Raw rv[kEvery], rf[kEvery], rd[kEvery];
     {
-      const T* v = static_cast<const T*>(p.v) + b * p.v_b + c + t0 * p.v_t;
-      const T* f = static_cast<const T*>(p.f) + b * p.f_b + c + t0 * p.f_t;
-      const T* d = p.dy ? static_cast<const T*>(p.dy) + b * p.y_b + c + t0 * p.y_t : nullptr;
+      const T* v = static_cast<const T*>(p.v) + b * p.v_b + cc + t0 * p.v_t;
+      const T* f = static_cast<const T*>(p.f) + b * p.f_b + cc + t0 * p.f_t;
+      const T* d = static_cast<const T*>(p.dy) + b * p.y_b + cc + t0 * p.y_t;
+      if (whole && p.dy) {
 #pragma unroll
-      for (int j = 0; j < kEvery; ++j) {
-        rv[j] = rf[j] = rd[j] = L::zero();
-        if (live && t0 + j < n) {
-          rv[j] = __ldcs(reinterpret_cast<const Raw*>(v));
-          rf[j] = __ldcs(reinterpret_cast<const Raw*>(f));
-          if (d) rd[j] = __ldcs(reinterpret_cast<const Raw*>(d));
+        for (int j = 0; j < kEvery; ++j) {
+          rv[j] = load_row<Raw>(v, j * v_row);
+          rf[j] = load_row<Raw>(f, j * f_row);
+          rd[j] = load_row<Raw>(d, j * y_row);
         }
-        v += p.v_t;
-        f += p.f_t;
-        if (d) d += p.y_t;
+      } else {
+#pragma unroll
+        for (int j = 0; j < kEvery; ++j) {
+          rv[j] = rf[j] = rd[j] = L::zero();
+          if (t0 + j < n) {
+            rv[j] = load_row<Raw>(v, j * v_row);
+            rf[j] = load_row<Raw>(f, j * f_row);
+            if (p.dy) rd[j] = load_row<Raw>(d, j * y_row);
+          }
+        }
       }
     }
     float h[VEC], P[VEC], E[VEC], G[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      h[i] = live && t0 < p.T ? p.states_in[(b * nst + t0 / kEvery) * p.D + c + i] : 0.f;
-      P[i] = 1.f;
-      E[i] = 0.f;
-    }
-    float a[kEvery][VEC], u[kEvery][VEC], k[kEvery][VEC];       // r a, u, a (1 - a) (r h_before + u' v)
+    for (int i = 0; i < VEC; ++i) h[i] = t0 < p.T ? p.states_in[(b * nst + t0 / kEvery) * p.D + cc + i] : 0.f;
+    unsigned cuts = 0;
+    if (CUT)
 #pragma unroll
-    for (int j = 0; j < kEvery; ++j) {
-      float v[VEC], f[VEC];
-      L::get(rv[j], v);
-      L::get(rf[j], f);
-      const bool on = t0 + j < n;
-      const bool cut = CUT && on && p.reset[(int64_t)b * p.T + t0 + j] != 0;
+      for (int j = 0; j < kEvery; ++j)
+        if (t0 + j < n && p.reset[(int64_t)b * p.T + t0 + j] != 0) cuts |= 1u << j;
+    float w[kEvery][VEC], k[kEvery][VEC];
+    auto compose = [&](auto full) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        float s, w;
-        gate_of(f[i], s, w);
-        const float before = CUT && cut ? 0.f : h[i];
-        u[j][i] = input_of<GATE>(s, w);
-        k[j][i] = fmaf(s * w, before, input_slope<GATE>(s, w) * v[i]);
-        if (on) h[i] = fmaf(s, before, u[j][i] * v[i]);
-        a[j][i] = !on ? 1.f : (CUT && cut ? 0.f : s);
-      }
-    }
-#pragma unroll
-    for (int j = kEvery - 1; j >= 0; --j) {
-      float d[VEC];
-      L::get(rd[j], d);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        E[i] = CUT && a[j][i] == 0.f ? 0.f : a[j][i] * (E[i] + d[i]);
-        P[i] *= a[j][i];
-      }
-    }
-    ex.run(P, E, carry, G, flip, rank, C);
-    if (live && t0 < p.T) {
-      T* dv = static_cast<T*>(p.dv) + b * p.dv_b + c + (t0 + kEvery - 1) * p.dv_t;
-      T* df = static_cast<T*>(p.df) + b * p.df_b + c + (t0 + kEvery - 1) * p.df_t;
-#pragma unroll
-      for (int j = kEvery - 1; j >= 0; --j) {
-        float d[VEC], ov[VEC], of[VEC];
-        L::get(rd[j], d);
-        const bool on = t0 + j < n;
+      for (int j = 0; j < kEvery; ++j) {
+        float v[VEC], f[VEC];
+        L::get(rv[j], v);
+        L::get(rf[j], f);
+        const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const float g = G[i] + d[i];
-          ov[i] = on ? u[j][i] * g : 0.f;
-          of[i] = on ? k[j][i] * g : 0.f;
-          G[i] = CUT && a[j][i] == 0.f ? 0.f : a[j][i] * g;
+          float s;
+          gate_of(f[i], s, w[j][i]);
+          const float before = cut ? 0.f : h[i], in = input_of<GATE>(s, w[j][i]) * v[i];
+          k[j][i] = fmaf(s * w[j][i], before, input_slope<GATE>(s, w[j][i]) * v[i]);
+          if (on) h[i] = fmaf(s, before, in);
+          if (!on) w[j][i] = 0.f;                     // a = 1: the cotangent passes
         }
-        if (t0 + j < p.T) {
-          __stcs(reinterpret_cast<Raw*>(dv), L::put(ov));
-          __stcs(reinterpret_cast<Raw*>(df), L::put(of));
-        }
-        dv -= p.dv_t;
-        df -= p.df_t;
       }
+#pragma unroll
+      for (int j = kEvery - 1; j >= 0; --j) {
+        float d[VEC];
+        L::get(rd[j], d);
+        const bool cut = CUT && ((cuts >> j) & 1u);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float a = 1.f - w[j][i];
+          P[i] = j == kEvery - 1 ? a : P[i] * a;
+          E[i] = j == kEvery - 1 ? a * d[i] : a * (E[i] + d[i]);
+          if (cut) P[i] = E[i] = 0.f;
+        }
+      }
+    };
+    if (whole) compose(Flag<true>()); else compose(Flag<false>());
+    ex.run(P, E, carry, G, flip, rank, C);
+    if (live && t0 < p.T) {
+      T* dv = static_cast<T*>(p.dv) + b * p.dv_b + c + t0 * p.dv_t;
+      T* df = static_cast<T*>(p.df) + b * p.df_b + c + t0 * p.df_t;
+      auto emit = [&](auto full) {
+#pragma unroll
+        for (int j = kEvery - 1; j >= 0; --j) {
+          float d[VEC], ov[VEC], of[VEC];
+          L::get(rd[j], d);
+          const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float a = 1.f - w[j][i], g = G[i] + d[i];
+            ov[i] = on ? input_of<GATE>(a, w[j][i]) * g : 0.f;
+            of[i] = on ? k[j][i] * g : 0.f;
+            G[i] = cut ? 0.f : a * g;
+          }
+          if (decltype(full)::value || t0 + j < p.T) {
+            store_row<Raw>(dv, j * dv_row, L::put(ov));
+            store_row<Raw>(df, j * df_row, L::put(of));
+          }
+        }
+      };
+      if (whole) emit(Flag<true>()); else emit(Flag<false>());
     }
   }
   if (p.dh0 && live && rank == 0 && warp == 0)
@@ -509,8 +572,12 @@ mw_status launch_chunks(const ScanArgs& p, bool backward, cudaStream_t s) {
 
 template <typename T, int VEC, int GATE>
 mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
-  // up to kEvery steps there is nothing to cut: a thread a channel
-  if (p.T <= kEvery) {
+  // up to kEvery steps there is nothing to cut: a thread a channel (the chunks' kernels also hold the offsets
+  // of kEvery rows in 32 bits, which only rows more than 2^26 bytes apart do not fit)
+  const int64_t most = (int64_t)1 << 26;
+  const bool near = p.v_t * (int64_t)sizeof(T) < most && p.f_t * (int64_t)sizeof(T) < most && p.y_t * (int64_t)sizeof(T) < most &&
+                    p.dv_t * (int64_t)sizeof(T) < most && p.df_t * (int64_t)sizeof(T) < most;
+  if (p.T <= kEvery || !near) {
     const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
     if (backward) scan_walk_back_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
     else scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);

@@ -386,13 +386,18 @@ int group_of(int cols, bool backward) {
 int rows_per_block(int g) { return g > kNormThreads ? 1 : kNormThreads / g; }
 
 int norm_sms() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    n = 148;
+  static int cached[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
+  if (cached[dev] == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      n = 148;
+    }
+    cached[dev] = n;
   }
-  return n;
+  return cached[dev];
 }
 // blocks of the backward pass: two of 256 threads (or one of 512) an SM
 int64_t backward_blocks(int64_t rows, int cols) {
