@@ -145,7 +145,7 @@ scan_walk_back_kernel(const ScanArgs p) {
 // already under way.
 // ---------------------------------------------------------------------------------------------
 constexpr int kScanWarps = 8;
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;
 
 // what one lane of a row holds: VEC channels of type T
 template <typename T, int VEC>
@@ -178,20 +178,37 @@ struct Lane<__nv_bfloat16, 2> {
   }
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// 8 bytes into the shared memory of block `rank` of the cluster, at this block's address `p`
-__device__ __forceinline__ void store_to_rank(float2* p, int rank, float2 v) {
-  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(r), "f"(v.x), "f"(v.y) : "memory");
+// all threads of all blocks of the cluster
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-
-// no block's shared memory is written by another before that block runs
-__device__ __forceinline__ void cluster_start(int C) {
-  if (C > 1) {
-    cluster_arrive();
-    cluster_wait();
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t in_rank(uint32_t address, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
+  return r;
+}
+// Waits for one phase of a barrier of this block.  The senders are blocks of the same cluster, which run at
+// the same time; should a phase not complete in two seconds all the same, the wait ends and says so.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 0;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((i & 255u) == 255u) {
+      uint64_t now;
+      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > 2000000000ull) return false;
+    }
   }
 }
 
@@ -202,42 +219,59 @@ __device__ __forceinline__ float affine(float P, float h, float H) {
   return CUT && P == 0.f ? H : fmaf(P, h, H);
 }
 
-// Composes the maps of the block's warps and of the cluster's blocks.  In: this thread's map (P, H).
-// Out: the state its steps start from, given the state `carry` the cluster's piece starts from;
-// `carry` becomes the state after the piece.  REVERSE: the pieces follow one another from the last
-// warp of the last block to the first (the cotangent's direction).
+// Composes the maps of the block's warps and of the cluster's blocks.  `state` holds what the cluster's next
+// piece starts from, the same in all its blocks.  REVERSE: the pieces follow one another from the last warp
+// of the last block to the first (the cotangent's direction).
+//   - every warp leaves its map; after a barrier each composes those of the warps before it;
+//   - the last warp in order then has the block's map and hands it to the copy engine, one copy to each block
+//     of the cluster, counted on a barrier there (a cluster-wide barrier instead would also wait for every
+//     block's stores to global memory, and measured two to four times slower a piece);
+//   - one warp folds the blocks' maps into the state this block starts from and the next piece's.
+// Everything is double-buffered by piece.  A buffer is written again two pieces on, by a block that has every
+// map of the piece between, which no block sends before all its warps are done with this one.
 template <int VEC, bool CUT, bool REVERSE>
 struct Exchange {
-  float2 warp_map[2][kScanWarps][VEC][32];
-  float2 block_map[2][kMaxCluster][VEC][32];
+  float2 warp_map[2][kScanWarps][32][VEC];
+  float2 block_map[2][kMaxCluster][32][VEC];
+  float2 outgoing[2][32][VEC];
+  float block_start[2][32][VEC];
+  float state[2][32][VEC];
+  unsigned long long arrived[2];
 
-  __device__ __forceinline__ void run(const float (&P)[VEC], const float (&H)[VEC], float (&carry)[VEC],
-                                      float (&start)[VEC], int flip, int rank, int C) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // before the first piece
+  __device__ __forceinline__ void begin(const float (&first)[VEC], int C) {
+    if (threadIdx.x < 32)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) warp_map[flip][warp][i][lane] = make_float2(P[i], H[i]);
-    __syncthreads();
+      for (int i = 0; i < VEC; ++i) state[0][threadIdx.x][i] = first[i];
     if (C > 1) {
-      // warp w sends the block's whole map to ranks w, w + W, ...
-      if (warp < C) {
-        float2 whole[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          whole[i] = make_float2(1.f, 0.f);
-#pragma unroll
-          for (int k = 0; k < kScanWarps; ++k) {
-            const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][i][lane];
-            whole[i].y = affine<CUT>(m.x, whole[i].y, m.y);
-            whole[i].x *= m.x;
-          }
-        }
-        for (int r = warp; r < C; r += kScanWarps)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) store_to_rank(&block_map[flip][rank][i][lane], r, whole[i]);
+      if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i)
+          asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&arrived[i])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       }
-      cluster_arrive();
+      cluster_sync();
+    } else {
+      __syncthreads();
     }
-    // while the others' maps arrive: the maps of this block's warps before this one
+  }
+  // after the last: no block leaves while its maps are still being read, or sent to it
+  __device__ __forceinline__ void end(int C) {
+    if (C > 1) cluster_sync();
+    else __syncthreads();
+  }
+
+  // in: this thread's map (P, H) of piece `index`; out: the state its steps start from
+  __device__ __forceinline__ void run(const float (&P)[VEC], const float (&H)[VEC], float (&start)[VEC], int index,
+                                      int rank, int C) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, flip = index & 1;
+    constexpr uint32_t kBytes = 32 * VEC * sizeof(float2);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) warp_map[flip][warp][lane][i] = make_float2(P[i], H[i]);
+    if (C > 1 && threadIdx.x == 0)
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(&arrived[flip])),
+                   "r"(kBytes * (uint32_t)C)
+                   : "memory");
+    __syncthreads();
     const int before = REVERSE ? kScanWarps - 1 - warp : warp;
     float pe[VEC], he[VEC];
 #pragma unroll
@@ -245,37 +279,50 @@ struct Exchange {
     for (int k = 0; k < before; ++k) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][i][lane];
+        const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][lane][i];
         he[i] = affine<CUT>(m.x, he[i], m.y);
         pe[i] *= m.x;
       }
     }
-    if (C > 1) {
-      cluster_wait();
-      const int first = REVERSE ? C - 1 - rank : rank;      // blocks before this one
-      for (int k = 0; k < C; ++k) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          if (k == first) start[i] = carry[i];
-          const float2 m = block_map[flip][REVERSE ? C - 1 - k : k][i][lane];
-          carry[i] = affine<CUT>(m.x, carry[i], m.y);
-        }
-      }
-    } else {
+    const bool last = before == kScanWarps - 1;
+    if (C == 1) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        start[i] = carry[i];
-        float p = pe[i], h = he[i];
-        for (int k = before; k < kScanWarps; ++k) {
-          const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][i][lane];
-          h = affine<CUT>(m.x, h, m.y);
-          p *= m.x;
+        const float s = state[flip][lane][i];
+        start[i] = affine<CUT>(pe[i], s, he[i]);
+        if (last) state[flip ^ 1][lane][i] = affine<CUT>(P[i], start[i], H[i]);
+      }
+      return;
+    }
+    if (last) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) outgoing[flip][lane][i] = make_float2(P[i] * pe[i], affine<CUT>(P[i], he[i], H[i]));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane < C)
+        asm volatile(
+            "cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                in_rank(shared_address(&block_map[flip][rank][0][0]), lane)),
+            "r"(shared_address(&outgoing[flip][0][0])), "r"(kBytes), "r"(in_rank(shared_address(&arrived[flip]), lane))
+            : "memory");
+    }
+    if (warp == 0) {
+      const bool ok = wait_phase(shared_address(&arrived[flip]), (uint32_t)(index >> 1) & 1u);
+      const int first = REVERSE ? C - 1 - rank : rank;      // blocks before this one
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float s = ok ? state[flip][lane][i] : __int_as_float(0x7fffffff);      // (maps that never came: NaN)
+        for (int k = 0; k < C; ++k) {
+          if (k == first) block_start[flip][lane][i] = s;
+          const float2 m = block_map[flip][REVERSE ? C - 1 - k : k][lane][i];
+          s = affine<CUT>(m.x, s, m.y);
         }
-        carry[i] = affine<CUT>(p, carry[i], h);
+        state[flip ^ 1][lane][i] = s;
       }
     }
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) start[i] = affine<CUT>(pe[i], start[i], he[i]);
+    for (int i = 0; i < VEC; ++i) start[i] = affine<CUT>(pe[i], block_start[flip][lane][i], he[i]);
   }
 };
 
@@ -298,7 +345,7 @@ __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_chunk_kernel(const ScanArgs p) {
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
-  __shared__ Exchange<VEC, CUT, false> ex;
+  __shared__ __align__(16) Exchange<VEC, CUT, false> ex;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
   const int c = (blockIdx.y * 32 + lane) * VEC;
@@ -331,12 +378,12 @@ scan_chunk_kernel(const ScanArgs p) {
   };
   int t0 = (rank * kScanWarps + warp) * kEvery;
   load(t0);
-  cluster_start(C);
   float carry[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) carry[i] = p.h0 ? p.h0[(int64_t)b * p.D + cc + i] : 0.f;
-  int flip = 0;
-  for (int base = 0; base < p.T; base += piece, t0 += piece, flip ^= 1) {
+  ex.begin(carry, C);
+  int index = 0;
+  for (int base = 0; base < p.T; base += piece, t0 += piece, ++index) {
     float a[kEvery][VEC], in[kEvery][VEC], P[VEC], H[VEC], h[VEC];
     const bool whole = t0 + kEvery <= n;
     auto compose = [&](auto full) {
@@ -361,7 +408,7 @@ scan_chunk_kernel(const ScanArgs p) {
     };
     if (whole) compose(Flag<true>()); else compose(Flag<false>());
     if (base + piece < p.T) load(t0 + piece);
-    ex.run(P, H, carry, h, flip, rank, C);
+    ex.run(P, H, h, index, rank, C);
     if (live && t0 < p.T) {
       if (p.states) {
         float* st = p.states + (b * nst + t0 / kEvery) * p.D + c;
@@ -384,9 +431,10 @@ scan_chunk_kernel(const ScanArgs p) {
       if (whole) emit(Flag<true>()); else emit(Flag<false>());
     }
   }
+  ex.end(C);
   if (p.h_last && live && rank == 0 && warp == 0)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) p.h_last[(int64_t)b * p.D + c + i] = carry[i];
+    for (int i = 0; i < VEC; ++i) p.h_last[(int64_t)b * p.D + c + i] = ex.state[index & 1][lane][i];
 }
 
 // The cotangent runs from the end: a step maps G (the cotangent of the state after it) to
@@ -398,7 +446,7 @@ __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_chunk_back_kernel(const ScanArgs p) {
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
-  __shared__ Exchange<VEC, CUT, true> ex;
+  __shared__ __align__(16) Exchange<VEC, CUT, true> ex;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
   const int c = (blockIdx.y * 32 + lane) * VEC;
@@ -410,12 +458,12 @@ scan_chunk_back_kernel(const ScanArgs p) {
   const int pieces = (p.T + piece - 1) / piece;
   const int v_row = (int)(p.v_t * sizeof(T)), f_row = (int)(p.f_t * sizeof(T)), y_row = (int)(p.y_t * sizeof(T));
   const int dv_row = (int)(p.dv_t * sizeof(T)), df_row = (int)(p.df_t * sizeof(T));
-  cluster_start(C);
   float carry[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) carry[i] = p.dh_last ? p.dh_last[(int64_t)b * p.D + cc + i] : 0.f;
-  int flip = 0;
-  for (int it = pieces - 1; it >= 0; --it, flip ^= 1) {
+  ex.begin(carry, C);
+  int index = 0;
+  for (int it = pieces - 1; it >= 0; --it, ++index) {
     const int t0 = it * piece + (rank * kScanWarps + warp) * kEvery;
     const bool whole = t0 + kEvery <= n;
     Raw rv[kEvery], rf[kEvery], rd[kEvery];
@@ -483,7 +531,7 @@ scan_chunk_back_kernel(const ScanArgs p) {
       }
     };
     if (whole) compose(Flag<true>()); else compose(Flag<false>());
-    ex.run(P, E, carry, G, flip, rank, C);
+    ex.run(P, E, G, index, rank, C);
     if (live && t0 < p.T) {
       T* dv = static_cast<T*>(p.dv) + b * p.dv_b + c + t0 * p.dv_t;
       T* df = static_cast<T*>(p.df) + b * p.df_b + c + t0 * p.df_t;
@@ -509,9 +557,286 @@ scan_chunk_back_kernel(const ScanArgs p) {
       if (whole) emit(Flag<true>()); else emit(Flag<false>());
     }
   }
+  ex.end(C);
   if (p.dh0 && live && rank == 0 && warp == 0)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) p.dh0[(int64_t)b * p.D + c + i] = carry[i];
+    for (int i = 0; i < VEC; ++i) p.dh0[(int64_t)b * p.D + c + i] = ex.state[index & 1][lane][i];
+}
+
+// ---------------------------------------------------------------------------------------------
+// The same two kernels for rows that start on 16-byte boundaries.  They are bound by the issue of
+// instructions, and a third of those of the kernels above are loads, stores and their addresses, a row
+// of 128 bytes at a time.  Here a warp brings its kEvery rows of each tensor into shared memory by
+// asynchronous copies of 16 bytes a lane (four rows an instruction), one piece ahead of its work, reads
+// them there at constant offsets, leaves its results in their place and stores those 16 bytes a lane.
+// ---------------------------------------------------------------------------------------------
+constexpr int kRowBytes = 128;                          // 64 bf16 or 32 fp32 channels
+constexpr int kBlockBytes = kEvery * kRowBytes;         // one warp's rows of one tensor
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_started() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// where a lane copies: piece lane & 7 of rows lane >> 3, + 4, + 8, + 12
+template <typename T>
+struct Rows {
+  const char* base;
+  int64_t row;
+  __device__ __forceinline__ Rows(const void* p, int64_t batch, int64_t step, int b, int channel)
+      : base(static_cast<const char*>(p) + (b * batch + channel) * (int64_t)sizeof(T)), row(step * (int64_t)sizeof(T)) {}
+  // rows t0 .. t0 + kEvery - 1, zeros from row `end` on and where this lane has no channels
+  __device__ __forceinline__ void fetch(uint32_t to, int t0, int end, bool live) const {
+    const int lane = threadIdx.x & 31, first = lane >> 3;
+    const char* from = base + (int64_t)(t0 + first) * row;
+    to += (uint32_t)(first * kRowBytes + (lane & 7) * 16);
+#pragma unroll
+    for (int r = 0; r < kEvery / 4; ++r) {
+      const bool on = live && t0 + first + 4 * r < end;
+      copy16(to + (uint32_t)(r * 4 * kRowBytes), on ? from : base, on);
+      from += 4 * row;
+    }
+  }
+  __device__ __forceinline__ void store(const unsigned char* from, int t0, int end, bool live) const {
+    const int lane = threadIdx.x & 31, first = lane >> 3;
+    char* to = const_cast<char*>(base) + (int64_t)(t0 + first) * row;
+    from += first * kRowBytes + (lane & 7) * 16;
+#pragma unroll
+    for (int r = 0; r < kEvery / 4; ++r) {
+      const uint4 v = *reinterpret_cast<const uint4*>(from + r * 4 * kRowBytes);
+      if (live && t0 + first + 4 * r < end) __stcs(reinterpret_cast<uint4*>(to), v);
+      to += 4 * row;
+    }
+  }
+};
+
+template <typename T, int GATE, bool CUT>
+__global__ void __launch_bounds__(32 * kScanWarps, 2)
+scan_wide_kernel(const ScanArgs p) {
+  constexpr int VEC = 4 / sizeof(T);
+  using L = Lane<T, VEC>;
+  using Raw = typename L::Raw;
+  __shared__ __align__(16) Exchange<VEC, CUT, false> ex;
+  extern __shared__ __align__(128) unsigned char ring[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
+  const int c0 = blockIdx.y * 32 * VEC, c = c0 + lane * VEC;
+  const bool live = c < p.D;
+  const int cc = live ? c : 0;
+  const int n = length_of(p, b);
+  const int piece = C * kScanWarps * kEvery;
+  const int64_t nst = (p.T + kEvery - 1) / kEvery;
+  // this warp's two stages of (v, f)
+  unsigned char* mine = ring + warp * 4 * kBlockBytes;
+  const uint32_t mine_at = shared_address(mine);
+  const int cl = c0 + (lane & 7) * (16 / (int)sizeof(T));       // the channels this lane copies
+  const bool copies = cl < p.D;
+  const Rows<T> v_rows(p.v, p.v_b, p.v_t, b, copies ? cl : 0), f_rows(p.f, p.f_b, p.f_t, b, copies ? cl : 0),
+      y_rows(p.y, p.y_b, p.y_t, b, copies ? cl : 0);
+  int t0 = (rank * kScanWarps + warp) * kEvery;
+  auto fetch = [&](int stage, int t) {
+    v_rows.fetch(mine_at + (uint32_t)(stage * 2 * kBlockBytes), t, n, copies);
+    f_rows.fetch(mine_at + (uint32_t)(stage * 2 * kBlockBytes + kBlockBytes), t, n, copies);
+    copies_started();
+  };
+  fetch(0, t0);
+  float carry[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) carry[i] = p.h0 ? p.h0[(int64_t)b * p.D + cc + i] : 0.f;
+  ex.begin(carry, C);
+  int index = 0;
+  for (int base = 0; base < p.T; base += piece, t0 += piece, ++index) {
+    const int stage = index & 1;
+    __syncwarp();                      // every lane is done with the other stage
+    if (base + piece < p.T) {
+      fetch(stage ^ 1, t0 + piece);
+      copies_done<1>();
+    } else {
+      copies_done<0>();
+    }
+    __syncwarp();
+    unsigned char* at = mine + stage * 2 * kBlockBytes;
+    unsigned char* word = at + lane * 4;
+    float a[kEvery][VEC], in[kEvery][VEC], P[VEC], H[VEC], h[VEC];
+    const bool whole = t0 + kEvery <= n;
+    auto compose = [&](auto full) {
+#pragma unroll
+      for (int j = 0; j < kEvery; ++j) {
+        float v[VEC], f[VEC];
+        L::get(*reinterpret_cast<const Raw*>(word + j * kRowBytes), v);
+        L::get(*reinterpret_cast<const Raw*>(word + kBlockBytes + j * kRowBytes), f);
+        const bool on = decltype(full)::value || t0 + j < n;
+        const bool cut = CUT && on && p.reset[(int64_t)b * p.T + t0 + j] != 0;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          float w;
+          gate_of(f[i], a[j][i], w);
+          in[j][i] = input_of<GATE>(a[j][i], w) * v[i];
+          if (CUT && cut) a[j][i] = 0.f;
+          if (!on) { a[j][i] = 1.f; in[j][i] = 0.f; }
+          P[i] = j ? P[i] * a[j][i] : a[j][i];
+          H[i] = j ? affine<CUT>(a[j][i], H[i], in[j][i]) : in[j][i];
+        }
+      }
+    };
+    if (whole) compose(Flag<true>()); else compose(Flag<false>());
+    ex.run(P, H, h, index, rank, C);
+    if (t0 < p.T) {
+      if (p.states && live) {
+        float* st = p.states + (b * nst + t0 / kEvery) * p.D + c;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) st[i] = h[i];
+      }
+      auto emit = [&](auto full) {
+#pragma unroll
+        for (int j = 0; j < kEvery; ++j) {
+          float o[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            h[i] = affine<CUT>(a[j][i], h[i], in[j][i]);
+            o[i] = decltype(full)::value || t0 + j < n ? h[i] : 0.f;
+          }
+          *reinterpret_cast<Raw*>(word + j * kRowBytes) = L::put(o);
+        }
+      };
+      if (whole) emit(Flag<true>()); else emit(Flag<false>());
+      __syncwarp();
+      y_rows.store(at, t0, p.T, copies);
+    }
+  }
+  ex.end(C);
+  if (p.h_last && live && rank == 0 && warp == 0)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) p.h_last[(int64_t)b * p.D + c + i] = ex.state[index & 1][lane][i];
+}
+
+template <typename T, int GATE, bool CUT>
+__global__ void __launch_bounds__(32 * kScanWarps, 2)
+scan_wide_back_kernel(const ScanArgs p) {
+  constexpr int VEC = 4 / sizeof(T);
+  using L = Lane<T, VEC>;
+  using Raw = typename L::Raw;
+  __shared__ __align__(16) Exchange<VEC, CUT, true> ex;
+  extern __shared__ __align__(128) unsigned char ring[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x, C = gridDim.x, b = blockIdx.z;
+  const int c0 = blockIdx.y * 32 * VEC, c = c0 + lane * VEC;
+  const bool live = c < p.D;
+  const int cc = live ? c : 0;
+  const int n = length_of(p, b);
+  const int piece = C * kScanWarps * kEvery;
+  const int64_t nst = (p.T + kEvery - 1) / kEvery;
+  const int pieces = (p.T + piece - 1) / piece;
+  // this warp's two stages of (v, f, dy)
+  unsigned char* mine = ring + warp * 6 * kBlockBytes;
+  const uint32_t mine_at = shared_address(mine);
+  const int cl = c0 + (lane & 7) * (16 / (int)sizeof(T));
+  const bool copies = cl < p.D;
+  const int cs = copies ? cl : 0;
+  const Rows<T> v_rows(p.v, p.v_b, p.v_t, b, cs), f_rows(p.f, p.f_b, p.f_t, b, cs), d_rows(p.dy ? p.dy : p.v, p.y_b, p.y_t, b, cs),
+      dv_rows(p.dv, p.dv_b, p.dv_t, b, cs), df_rows(p.df, p.df_b, p.df_t, b, cs);
+  float next[VEC];                     // the state before this thread's steps of the next piece
+  auto fetch = [&](int stage, int t) {
+    const uint32_t to = mine_at + (uint32_t)(stage * 3 * kBlockBytes);
+    v_rows.fetch(to, t, n, copies);
+    f_rows.fetch(to + kBlockBytes, t, n, copies);
+    d_rows.fetch(to + 2 * kBlockBytes, t, p.dy ? n : 0, copies);
+    copies_started();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) next[i] = t < p.T ? p.states_in[(b * nst + t / kEvery) * p.D + cc + i] : 0.f;
+  };
+  int t0 = (pieces - 1) * piece + (rank * kScanWarps + warp) * kEvery;
+  fetch(0, t0);
+  float carry[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) carry[i] = p.dh_last ? p.dh_last[(int64_t)b * p.D + cc + i] : 0.f;
+  ex.begin(carry, C);
+  int index = 0;
+  for (int it = pieces - 1; it >= 0; --it, ++index, t0 -= piece) {
+    const int stage = index & 1;
+    float h[VEC], P[VEC], E[VEC], G[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) h[i] = next[i];
+    __syncwarp();                      // every lane is done with the other stage
+    if (it > 0) {
+      fetch(stage ^ 1, t0 - piece);
+      copies_done<1>();
+    } else {
+      copies_done<0>();
+    }
+    __syncwarp();
+    const bool whole = t0 + kEvery <= n;
+    unsigned char* at = mine + stage * 3 * kBlockBytes;
+    unsigned char* word = at + lane * 4;
+    unsigned cuts = 0;
+    if (CUT)
+#pragma unroll
+      for (int j = 0; j < kEvery; ++j)
+        if (t0 + j < n && p.reset[(int64_t)b * p.T + t0 + j] != 0) cuts |= 1u << j;
+    float w[kEvery][VEC], k[kEvery][VEC];
+    auto compose = [&](auto full) {
+#pragma unroll
+      for (int j = 0; j < kEvery; ++j) {
+        float v[VEC], f[VEC];
+        L::get(*reinterpret_cast<const Raw*>(word + j * kRowBytes), v);
+        L::get(*reinterpret_cast<const Raw*>(word + kBlockBytes + j * kRowBytes), f);
+        const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          float s;
+          gate_of(f[i], s, w[j][i]);
+          const float before = cut ? 0.f : h[i], in = input_of<GATE>(s, w[j][i]) * v[i];
+          k[j][i] = fmaf(s * w[j][i], before, input_slope<GATE>(s, w[j][i]) * v[i]);
+          if (on) h[i] = fmaf(s, before, in);
+          if (!on) w[j][i] = 0.f;                     // a = 1: the cotangent passes
+        }
+      }
+#pragma unroll
+      for (int j = kEvery - 1; j >= 0; --j) {
+        float d[VEC];
+        L::get(*reinterpret_cast<const Raw*>(word + 2 * kBlockBytes + j * kRowBytes), d);
+        const bool cut = CUT && ((cuts >> j) & 1u);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float a = 1.f - w[j][i];
+          P[i] = j == kEvery - 1 ? a : P[i] * a;
+          E[i] = j == kEvery - 1 ? a * d[i] : a * (E[i] + d[i]);
+          if (cut) P[i] = E[i] = 0.f;
+        }
+      }
+    };
+    if (whole) compose(Flag<true>()); else compose(Flag<false>());
+    ex.run(P, E, G, index, rank, C);
+    if (t0 < p.T) {
+      auto emit = [&](auto full) {
+#pragma unroll
+        for (int j = kEvery - 1; j >= 0; --j) {
+          float d[VEC], ov[VEC], of[VEC];
+          L::get(*reinterpret_cast<const Raw*>(word + 2 * kBlockBytes + j * kRowBytes), d);
+          const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float a = 1.f - w[j][i], g = G[i] + d[i];
+            ov[i] = on ? input_of<GATE>(a, w[j][i]) * g : 0.f;
+            of[i] = on ? k[j][i] * g : 0.f;
+            G[i] = cut ? 0.f : a * g;
+          }
+          *reinterpret_cast<Raw*>(word + j * kRowBytes) = L::put(ov);
+          *reinterpret_cast<Raw*>(word + kBlockBytes + j * kRowBytes) = L::put(of);
+        }
+      };
+      if (whole) emit(Flag<true>()); else emit(Flag<false>());
+      __syncwarp();
+      dv_rows.store(at, t0, p.T, copies);
+      df_rows.store(at + kBlockBytes, t0, p.T, copies);
+    }
+  }
+  ex.end(C);
+  if (p.dh0 && live && rank == 0 && warp == 0)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) p.dh0[(int64_t)b * p.D + c + i] = ex.state[index & 1][lane][i];
 }
 
 mw_status check_desc(const mw_gated_scan_desc* d) {
@@ -547,18 +872,35 @@ mw_status fill_scan(const mw_gated_scan_desc* d, ScanArgs& p) {
   return MW_OK;
 }
 
-template <typename T, int VEC, int GATE, bool CUT>
-mw_status launch_chunks(const ScanArgs& p, bool backward, cudaStream_t s) {
-  const int columns = ceil_div(p.D, 32 * VEC);
-  const int pieces = ceil_div(p.T, kScanWarps * kEvery);
-  // blocks along time until there are two for every SM, as far as there are pieces for them
+// Blocks along time, doubled while the grid would fill less than two thirds of the SMs (all of them for the
+// kernels without copies, which have more latency for a second block an SM to hide), as far as there are
+// pieces for them.  Each doubling costs an exchange a piece: 8x2048x2048 bf16 (256 columns) takes 42 us with
+// one block along time and 53 us with two; 1x65536x1024 (16 columns) 868, 592, 318, 210, 237 us with 1 to 16.
+int blocks_along_time(int64_t columns, int pieces, bool wide) {
+  const int64_t enough = wide ? 96 : 148;
   int C = 1;
-  while (C < kMaxCluster && C < pieces && (int64_t)columns * p.B * C < 2 * 148) C *= 2;
+  while (C < kMaxCluster && C < pieces && columns * C < enough) C *= 2;
+  return C;
+}
+int scan_pieces(const ScanArgs& p) { return ceil_div(p.T, kScanWarps * kEvery); }
+
+// `wide`: every row of every tensor starts on a 16-byte boundary
+template <typename T, int VEC, int GATE, bool CUT>
+mw_status launch_chunks(const ScanArgs& p, bool backward, bool wide, cudaStream_t s) {
+  const int columns = ceil_div(p.D, 32 * VEC);
+  const int C = blocks_along_time((int64_t)columns * p.B, scan_pieces(p), wide);
   void (*kernel)(const ScanArgs) = backward ? scan_chunk_back_kernel<T, VEC, GATE, CUT> : scan_chunk_kernel<T, VEC, GATE, CUT>;
-  if (C > 8) MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  size_t ring = 0;
+  if (wide) {
+    kernel = backward ? scan_wide_back_kernel<T, GATE, CUT> : scan_wide_kernel<T, GATE, CUT>;
+    ring = (size_t)kScanWarps * (backward ? 6 : 4) * kBlockBytes;
+    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
+  }
+  static_assert(kMaxCluster <= 8, "larger clusters are not portable");
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)C, (unsigned)columns, (unsigned)p.B);
   cfg.blockDim = dim3(32 * kScanWarps);
+  cfg.dynamicSmemBytes = ring;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -572,18 +914,24 @@ mw_status launch_chunks(const ScanArgs& p, bool backward, cudaStream_t s) {
 
 template <typename T, int VEC, int GATE>
 mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
-  // up to kEvery steps there is nothing to cut: a thread a channel (the chunks' kernels also hold the offsets
+  // what every row's place is a multiple of, in bytes
+  const int64_t e = sizeof(T), d = p.D * e;
+  const int64_t steps = p.v_t | p.f_t | p.y_t | p.dv_t | p.df_t;
+  const int64_t places = (p.v_b | p.f_b | p.y_b | p.dv_b | p.df_b | steps) * e | d |
+                         (int64_t)((uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df);
+  // up to kEvery steps there is nothing to cut: a thread a channel (the chunk kernels also hold the offsets
   // of kEvery rows in 32 bits, which only rows more than 2^26 bytes apart do not fit)
   const int64_t most = (int64_t)1 << 26;
-  const bool near = p.v_t * (int64_t)sizeof(T) < most && p.f_t * (int64_t)sizeof(T) < most && p.y_t * (int64_t)sizeof(T) < most &&
-                    p.dv_t * (int64_t)sizeof(T) < most && p.df_t * (int64_t)sizeof(T) < most;
+  const bool near = p.v_t * e < most && p.f_t * e < most && p.y_t * e < most && p.dv_t * e < most && p.df_t * e < most;
   if (p.T <= kEvery || !near) {
     const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
     if (backward) scan_walk_back_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
     else scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
     return launch_ok();
   }
-  return p.reset ? launch_chunks<T, VEC, GATE, true>(p, backward, s) : launch_chunks<T, VEC, GATE, false>(p, backward, s);
+  const bool wide = VEC * e == 4 && (places & 15) == 0;
+  return p.reset ? launch_chunks<T, VEC, GATE, true>(p, backward, wide, s)
+                 : launch_chunks<T, VEC, GATE, false>(p, backward, wide, s);
 }
 
 template <typename T, int VEC>
@@ -594,10 +942,13 @@ mw_status gate_scan(const mw_gated_scan_desc* d, const ScanArgs& p, bool backwar
 
 mw_status dispatch_scan(const mw_gated_scan_desc* d, const ScanArgs& p, bool backward, cudaStream_t s) {
   if (d->dtype == 1) return gate_scan<float, 1>(d, p, backward, s);
-  // two bf16 channels a lane where every row of every tensor starts on a 4-byte boundary
+  // two bf16 channels a lane where every row of every tensor starts on a 4-byte boundary; one all the same
+  // where there are so few columns that even four blocks along time leave SMs idle (1x65536x1024: 210 us with
+  // two channels a lane, 162 us with one, whose twice as many blocks hide each other's exchanges)
   const int64_t odd = p.D | p.v_b | p.v_t | p.f_b | p.f_t | p.y_b | p.y_t | p.dv_b | p.dv_t | p.df_b | p.df_t;
   const uintptr_t at = (uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df;
-  return (odd & 1) == 0 && (at & 3) == 0 ? gate_scan<__nv_bfloat16, 2>(d, p, backward, s)
+  const bool few = blocks_along_time((int64_t)ceil_div(p.D, 64) * p.B, scan_pieces(p), true) >= 4;
+  return (odd & 1) == 0 && (at & 3) == 0 && !few ? gate_scan<__nv_bfloat16, 2>(d, p, backward, s)
                                          : gate_scan<__nv_bfloat16, 1>(d, p, backward, s);
 }
 
