@@ -42,6 +42,7 @@ struct mw_orth {
   int steps, terms;
   double c[3];
   int mp, np;          // padded sides: multiples of 256 and 128
+  bool small;          // one CTA a matrix, everything in shared memory
   // tensor maps of a workspace, encoded when the workspace first comes along
   const void* mapped = nullptr;
   CUtensorMap maps[12];
@@ -84,6 +85,12 @@ struct OrthPtrs {
   void* out[kPtrGroup];
 };
 
+// factors of the three products' epilogues (see the top of the file)
+struct OrthFactors {
+  float a_scale, b_acc, x_acc, out_scale;
+  float a_diag[kOrthMaxSteps], b_add[kOrthMaxSteps], b_diag[kOrthMaxSteps], x_add[kOrthMaxSteps];
+};
+
 struct alignas(64) OrthParams {
   CUtensorMap map[MAP_COUNT];
   int count, tm, tn, steps, tri, per_step, total;
@@ -91,8 +98,7 @@ struct alignas(64) OrthParams {
   int piece_blocks;              // K blocks of one accumulator (0: all)
   int mp, np, stages;
   uint32_t stage_bytes;
-  float a_scale, b_acc, x_acc;
-  float a_diag[kOrthMaxSteps], b_add[kOrthMaxSteps], b_diag[kOrthMaxSteps], x_add[kOrthMaxSteps];
+  OrthFactors f;
   unsigned* done;                // [step][phase][matrix][row of tiles]
   DeviceStatus* st;
   uint64_t wait_ns;
@@ -424,9 +430,9 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         }
       }
       if (!ok) break;
-      const float alpha = w.phase == 0 ? p.a_scale : (w.phase == 1 ? p.b_acc : p.x_acc);
-      const float scale = w.phase == 1 ? p.b_add[w.step] : p.x_add[w.step];
-      const float diag = w.phase == 0 ? p.a_diag[w.step] : p.b_diag[w.step];
+      const float alpha = w.phase == 0 ? p.f.a_scale : (w.phase == 1 ? p.f.b_acc : p.f.x_acc);
+      const float scale = w.phase == 1 ? p.f.b_add[w.step] : p.f.x_add[w.step];
+      const float diag = w.phase == 0 ? p.f.a_diag[w.step] : p.f.b_diag[w.step];
       const int planes = w.phase == 2 ? 2 : TERMS;
       const bool mirror = w.phase < 2 && w.ti != w.tj;
       // (unrolled for two terms, whose sums sit in registers)
@@ -748,6 +754,210 @@ orth_apply_kernel(const __grid_constant__ OrthPtrs ptr, int m, int n, int mp, in
 }
 
 // ---------------------------------------------------------------------------------------------
+// Small matrices (up to 128 x 256, X and A within one SM's shared memory): one CTA a matrix does everything in one
+// launch -- momentum, norm, all steps, update.  A phase of the kernel above costs a trip through L2, 9 to
+// 16 us whatever the tile; here X, A and B stay in shared memory and each phase is a product, a read of the
+// accumulator and a rewrite in place.  X is laid out in groups of 64 columns, [128 rows][128 bytes] each under
+// the 128-byte swizzle: row by row that is a K-major operand of X X^T, and column by column an MN-major
+// operand of B X, so one copy serves both products.
+// ---------------------------------------------------------------------------------------------
+struct OrthSmall {
+  OrthFactors f;
+  int m, n, tall, steps, nesterov;
+  float beta, keep, step;
+  double sx;
+  DeviceStatus* st;
+  uint64_t wait_ns;
+};
+constexpr uint32_t kGroupBytes = 128 * 128;
+
+__host__ __device__ constexpr uint32_t small_bytes(int m, int n, int terms) {
+  return (uint32_t)(2 * ((n + 63) / 64) + terms * ((m + 63) / 64)) * kGroupBytes;
+}
+// byte offset of the 16 bytes that hold columns c .. c + 7 (c a multiple of 8) of row r
+__device__ __forceinline__ uint32_t small_at(int r, int c) {
+  return (uint32_t)(c >> 6) * kGroupBytes + (uint32_t)r * 128u + (uint32_t)((((c & 63) >> 3) ^ (r & 7)) << 4);
+}
+
+template <typename T, int TERMS>
+__global__ void __launch_bounds__(256)
+orth_small_kernel(const __grid_constant__ OrthPtrs ptr, const __grid_constant__ OrthSmall p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  __shared__ double buf[9];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = blockIdx.x;
+  const int m = p.m, n = p.n, width = p.tall ? m : n;
+  const int mg = (m + 63) / 64, ng = (n + 63) / 64;
+  uint8_t* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint8_t* x_hi = base;
+  uint8_t* x_lo = x_hi + ng * kGroupBytes;
+  uint8_t* a_hi = x_lo + ng * kGroupBytes;
+  uint8_t* a_lo = a_hi + mg * kGroupBytes;                 // (two terms only)
+  // accumulator columns of X X^T and A^2, then of B X
+  const uint32_t columns = mg * 64 + ng * 64 <= 128 ? 128u : (mg * 64 + ng * 64 <= 256 ? 256u : 512u);
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bar), 1);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // M', U and ||U||; X starts as zeros in its padding
+  const T* u_in = static_cast<const T*>(ptr.u[i]);
+  const float *g = ptr.g[i], *mom = ptr.m[i];
+  float* mom_out = ptr.mo[i];
+  double s = 0.0;
+  for (int k = threadIdx.x; k < m * n; k += 256) {
+    float u;
+    if (u_in) {
+      u = to_f32(u_in[k]);
+    } else {
+      const float m2 = fmaf(p.beta, mom[k], g[k]);
+      mom_out[k] = m2;
+      u = update_of(g[k], m2, p.beta, p.nesterov);
+    }
+    s += (double)u * (double)u;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) buf[warp] = s;
+  for (uint32_t k = threadIdx.x; k < 2u * ng * kGroupBytes / 16; k += 256)
+    reinterpret_cast<uint4*>(x_hi)[k] = make_uint4(0u, 0u, 0u, 0u);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (threadIdx.x == 0) {
+    double t = 0.0;
+    for (int w = 0; w < 8; ++w) t += buf[w];
+    buf[8] = t > 0.0 ? p.sx / sqrt(t) : (t == 0.0 ? 0.0 : t);      // NaN stays NaN
+  }
+  __syncthreads();
+  const double r = buf[8];
+  const uint32_t tmem = tmem_slot;
+  for (int k = threadIdx.x; k < m * n; k += 256) {
+    const int a = k / width, b = k - a * width, row = p.tall ? b : a, col = p.tall ? a : b;
+    const float u = u_in ? to_f32(u_in[k]) : update_of(g[k], mom_out[k], p.beta, p.nesterov);
+    const float x = (float)((double)u * r);
+    const __half h = __float2half_rn(x);
+    const uint32_t at = small_at(row, col & ~7) + (uint32_t)(col & 7) * 2u;
+    *reinterpret_cast<__half*>(x_hi + at) = h;
+    *reinterpret_cast<__half*>(x_lo + at) = __float2half_rn(x - __half2float(h));
+  }
+  WaitCtx wc;
+  wc.st = p.st;
+  wc.abort_flag = &abort_flag;
+  wc.limit_ns = p.wait_ns;
+  const int quarter = warp & 3, side = warp >> 2, row = quarter * 32 + lane;
+  const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+  const uint32_t xh = smem_u32(x_hi) >> 4, xl = smem_u32(x_lo) >> 4, ah = smem_u32(a_hi) >> 4, al = smem_u32(a_lo) >> 4;
+  uint32_t phase = 0;
+  bool ok = true;
+  for (int step = 0; step < p.steps && ok; ++step) {
+#pragma unroll 1
+    for (int ph = 0; ph < 3 && ok; ++ph) {
+      // the operands are written by all threads: make them visible to the tensor core
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      tc_fence_before();
+      __syncthreads();
+      const uint32_t d = tmem + (ph == 2 ? (uint32_t)(mg * 64) : 0u);
+      if (threadIdx.x == 0) {
+        tc_fence_after();
+        const int N = ph == 2 ? ng * 64 : mg * 64, ks = ph == 0 ? ng * 4 : (m + 15) / 16;
+        const uint32_t idesc = (1u << 4) | ((ph == 2 ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+        for (int k = 0; k < ks; ++k) {
+          // K-major: 16 columns are 32 bytes of a group; MN-major: 16 rows are 2048 bytes
+          const uint32_t kk = (uint32_t)(k >> 2) * (kGroupBytes >> 4) + (uint32_t)(k & 3) * 2u | (1u << 16);
+          const uint32_t kn = (uint32_t)k * (2048u >> 4) | ((kGroupBytes >> 4) << 16);
+          const uint32_t a0 = (ph == 0 ? xh : ah) + kk, b0 = ph == 2 ? xh + kn : (ph == 0 ? xh : ah) + kk;
+          umma_bf16<false>(d, a0, b0, idesc, k > 0);
+          if (TERMS == 2) {
+            const uint32_t a1 = (ph == 0 ? xl : al) + kk, b1 = ph == 2 ? xl + kn : (ph == 0 ? xl : al) + kk;
+            umma_bf16<false>(d, a0, b1, idesc, 1u);
+            umma_bf16<false>(d, a1, b0, idesc, 1u);
+          }
+        }
+        umma_commit<false>(smem_u32(&bar));
+      }
+      ok = __syncthreads_and(mbar_wait<false>(smem_u32(&bar), phase, wc, 7u));
+      phase ^= 1u;
+      if (!ok) break;
+      tc_fence_after();
+      const int cols = ph == 2 ? ng * 64 : mg * 64;
+      uint8_t* hi = ph == 2 ? x_hi : a_hi;
+      uint8_t* lo = ph == 2 ? x_lo : a_lo;
+      const int planes = ph == 2 ? 2 : TERMS;
+      const float alpha = ph == 0 ? p.f.a_scale : (ph == 1 ? p.f.b_acc : p.f.x_acc);
+      const float scale = ph == 1 ? p.f.b_add[step] : p.f.x_add[step];
+      const float diag = ph == 0 ? p.f.a_diag[step] : (ph == 1 ? p.f.b_diag[step] : 0.f);
+      for (int c = side * 32; c < cols; c += 64) {
+        uint32_t q[32];
+        tmem_ld32_issue(d + lanes + (uint32_t)c, q);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t at = small_at(row, c + 8 * e);
+          float v[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) v[t] = alpha * __uint_as_float(q[8 * e + t]);
+          if (ph) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (t < planes) {
+                const uint4 w = *reinterpret_cast<const uint4*>((t ? lo : hi) + at);
+                const uint32_t four[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                  const float2 f = unpack_half2(four[z]);
+                  v[2 * z] = fmaf(scale, f.x, v[2 * z]);
+                  v[2 * z + 1] = fmaf(scale, f.y, v[2 * z + 1]);
+                }
+              }
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+            if (c + 8 * e + t == row) v[t] += diag;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (t < planes) {
+              uint32_t four[4];
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                four[z] = pack_half2(v[2 * z], v[2 * z + 1]);
+                const float2 f = unpack_half2(four[z]);
+                v[2 * z] -= f.x;
+                v[2 * z + 1] -= f.y;
+              }
+              *reinterpret_cast<uint4*>((t ? lo : hi) + at) = make_uint4(four[0], four[1], four[2], four[3]);
+            }
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+  const T* w = static_cast<const T*>(ptr.w[i]);
+  T* out = static_cast<T*>(ptr.out[i]);
+  for (int k = threadIdx.x; k < m * n; k += 256) {
+    const int a = k / width, b = k - a * width, rr = p.tall ? b : a, cc = p.tall ? a : b;
+    const uint32_t at = small_at(rr, cc & ~7) + (uint32_t)(cc & 7) * 2u;
+    const float x = (__half2float(*reinterpret_cast<const __half*>(x_hi + at)) +
+                     __half2float(*reinterpret_cast<const __half*>(x_lo + at))) * p.f.out_scale;
+    out[k] = narrow<T>(w ? fmaf(-p.step, x, p.keep * to_f32(w[k])) : x);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
 struct OrthWs {
@@ -758,13 +968,13 @@ struct OrthWs {
 };
 
 size_t orth_layout(const mw_orth* p, char* base, OrthWs* w) {
-  size_t off = 256;                       // device status
+  if (p->small) return 1024;              // device status alone
+  size_t off = 1024;
   auto take = [&](size_t bytes) {
     char* q = base ? base + off : nullptr;
     off += align_up(bytes, 1024);
     return q;
   };
-  off = 1024;
   const size_t c = (size_t)p->d.count, mn = (size_t)p->mp * p->np, mm = (size_t)p->mp * p->mp;
   OrthWs l;
   l.done_bytes = (size_t)p->steps * 3 * c * (p->mp / kTile) * sizeof(unsigned);
@@ -846,18 +1056,78 @@ mw_status orth_launch(const OrthParams& prm, size_t smem, cudaStream_t s) {
 
 double pow2_floor(double v) { return exp2(floor(log2(v))); }
 
+// Sx: rows of X have norm about one, so sqrt(n) brings their entries to about one; 64 more leaves the remainders
+// of small entries in fp16's range
+double orth_sx(int n) {
+  const double sx = 64.0 * exp2(ceil(log2(sqrt((double)n))));
+  return sx < 16384.0 ? sx : 16384.0;
+}
+
+OrthFactors orth_factors(const mw_orth* p, double sx) {
+  OrthFactors f;
+  // Sa: the entries of B are at most |c1| s + |c2| s^2 with s <= 2 the largest eigenvalue of A
+  double sa = 1024.0;
+  const double most = 2.0 * fabs(p->c[1]) + 4.0 * fabs(p->c[2]);
+  if (most * sa > 32768.0) sa = pow2_floor(32768.0 / most);
+  f.a_scale = (float)(sa / (sx * sx));
+  f.b_acc = (float)(p->c[2] / sa);
+  f.x_acc = (float)(1.0 / sa);
+  f.out_scale = (float)(1.0 / sx);
+  const bool shifts = p->d.coef[0] == 0.0 && p->d.coef[1] == 0.0 && p->d.coef[2] == 0.0;
+  for (int k = 0; k < p->steps; ++k) {
+    // (the shifts are identities; these values lie in the middle of the spectra that the default
+    // polynomial has produced by then: of 5 sets tried on 20 matrices, the smallest largest error)
+    double al = 0.0, be = 0.0;
+    if (shifts && p->steps >= 5 && k == p->steps - 1) { al = 0.7; be = 2.0; }
+    else if (shifts && p->steps >= 5 && k == p->steps - 2) { al = 0.3; be = 1.0; }
+    f.a_diag[k] = (float)(-al * sa);
+    f.b_add[k] = (float)(p->c[1] + 2.0 * p->c[2] * al);
+    f.b_diag[k] = (float)(sa * (p->c[1] * al + p->c[2] * al * al + be));
+    f.x_add[k] = (float)(p->c[0] - be);
+  }
+  return f;
+}
+
 template <typename T>
 mw_status orth_run(mw_orth* p, const void* const* params, const void* const* grads, const void* const* momentum,
                    void* const* out, void* const* momentum_out, const void* const* project_in, double lr, double beta,
                    double wd, double scale, char* ws, cudaStream_t s) {
+  const int m = p->m, n = p->n, count = p->d.count;
+  if (p->small) {
+    MW_CUDA_OK(cudaMemsetAsync(ws, 0, 256, s));       // status
+    auto kernel = p->terms == 1 ? orth_small_kernel<T, 1> : orth_small_kernel<T, 2>;
+    const size_t smem = 1024 + small_bytes(m, n, p->terms);
+    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    static thread_local OrthSmall q;
+    q.sx = orth_sx(n);
+    q.f = orth_factors(p, q.sx);
+    q.m = m; q.n = n; q.tall = p->tall; q.steps = p->steps; q.nesterov = p->d.nesterov;
+    q.beta = (float)beta; q.keep = (float)(1.0 - lr * wd); q.step = (float)(lr * scale);
+    q.st = reinterpret_cast<DeviceStatus*>(ws);
+    q.wait_ns = kOrthWaitNs;
+    for (int first = 0; first < count; first += kPtrGroup) {
+      const int c = count - first < kPtrGroup ? count - first : kPtrGroup;
+      static thread_local OrthPtrs ptr;
+      for (int i = 0; i < c; ++i) {
+        const int k = first + i;
+        ptr.u[i] = project_in ? project_in[k] : nullptr;
+        ptr.g[i] = grads ? static_cast<const float*>(grads[k]) : nullptr;
+        ptr.m[i] = momentum ? static_cast<const float*>(momentum[k]) : nullptr;
+        ptr.mo[i] = momentum_out ? static_cast<float*>(momentum_out[k]) : nullptr;
+        ptr.w[i] = params ? params[k] : nullptr;
+        ptr.out[i] = out[k];
+      }
+      kernel<<<(unsigned)c, 256, smem, s>>>(ptr, q);
+      MW_TRY(launch_ok());
+    }
+    return MW_OK;
+  }
   OrthWs l;
   orth_layout(p, ws, &l);
   MW_TRY(orth_maps(p, l, ws));
   MW_CUDA_OK(cudaMemsetAsync(ws, 0, 1024 + l.done_bytes, s));     // status and counters
-  const int m = p->m, n = p->n, count = p->d.count;
   const int64_t mn = (int64_t)m * n, rowlen = p->tall ? m : n;
-  double sx = 64.0 * exp2(ceil(log2(sqrt((double)n))));
-  if (sx > 16384.0) sx = 16384.0;
+  const double sx = orth_sx(n);
   // blocks of the momentum pass: about eight an SM over all matrices
   const int64_t want = (mn + 2047) / 2048, share = ceil_div(8 * 148, count < kPtrGroup ? count : kPtrGroup);
   int parts = (int)(want < kNormBlocks ? want : kNormBlocks);
@@ -899,25 +1169,7 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.kb_n = ceil_div(n, kBK);
   q.piece_blocks = p->terms == 2 ? kPieceBlocks : 0;
   q.mp = p->mp; q.np = p->np;
-  // Sa: the entries of B are at most |c1| s + |c2| s^2 with s <= 2 the largest eigenvalue of A
-  double sa = 1024.0;
-  const double most = 2.0 * fabs(p->c[1]) + 4.0 * fabs(p->c[2]);
-  if (most * sa > 32768.0) sa = pow2_floor(32768.0 / most);
-  q.a_scale = (float)(sa / (sx * sx));
-  q.b_acc = (float)(p->c[2] / sa);
-  q.x_acc = (float)(1.0 / sa);
-  const bool shifts = p->d.coef[0] == 0.0 && p->d.coef[1] == 0.0 && p->d.coef[2] == 0.0;
-  for (int k = 0; k < p->steps; ++k) {
-    // (the shifts are identities; these values lie in the middle of the spectra that the default
-    // polynomial has produced by then: of 5 sets tried on 20 matrices, the smallest largest error)
-    double al = 0.0, be = 0.0;
-    if (shifts && p->steps >= 5 && k == p->steps - 1) { al = 0.7; be = 2.0; }
-    else if (shifts && p->steps >= 5 && k == p->steps - 2) { al = 0.3; be = 1.0; }
-    q.a_diag[k] = (float)(-al * sa);
-    q.b_add[k] = (float)(p->c[1] + 2.0 * p->c[2] * al);
-    q.b_diag[k] = (float)(sa * (p->c[1] * al + p->c[2] * al * al + be));
-    q.x_add[k] = (float)(p->c[0] - be);
-  }
+  q.f = orth_factors(p, sx);
   q.done = l.done;
   q.st = reinterpret_cast<DeviceStatus*>(ws);
   q.wait_ns = kOrthWaitNs;
@@ -936,7 +1188,7 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
     }
     auto k3 = wide ? orth_apply_kernel<T, true> : orth_apply_kernel<T, false>;
     k3<<<dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 32), (unsigned)c), 256, 0, s>>>(
-        ptr, m, n, p->mp, p->np, p->tall, l.x[p->steps & 1] + (size_t)first * 2 * p->mp * p->np, (float)(1.0 / sx),
+        ptr, m, n, p->mp, p->np, p->tall, l.x[p->steps & 1] + (size_t)first * 2 * p->mp * p->np, q.f.out_scale,
         (float)(1.0 - lr * wd), (float)(lr * scale));
     MW_TRY(launch_ok());
   }
@@ -978,6 +1230,7 @@ extern "C" mw_status mw_orth_create(const mw_orth_desc* desc, mw_orth** out) {
   p->n = p->tall ? d.rows : d.cols;
   p->steps = d.steps ? d.steps : 5;
   p->terms = d.terms ? d.terms : (d.prec == MW_F32 ? 2 : 1);
+  p->small = p->m <= 128 && p->n <= 256 && small_bytes(p->m, p->n, p->terms) <= 200u * 1024u;
   p->mp = (int)align_up((size_t)p->m, kTile);
   p->np = (int)align_up((size_t)p->n, kHalf);
   const bool given = d.coef[0] != 0.0 || d.coef[1] != 0.0 || d.coef[2] != 0.0;
