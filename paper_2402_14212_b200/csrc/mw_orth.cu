@@ -45,7 +45,7 @@ struct mw_orth {
   bool small;          // one CTA a matrix, everything in shared memory
   // tensor maps of a workspace, encoded when the workspace first comes along
   const void* mapped = nullptr;
-  CUtensorMap maps[12];
+  CUtensorMap maps[10];
 };
 
 namespace mw {
@@ -65,16 +65,19 @@ constexpr int kFewRegisters = 104, kManyRegisters = 200;
 // every instruction, which over the 3 x 4 instructions of each block adds up to a bias of about 4e-7 a block
 // on sums of like signs (the diagonals of X X^T and A^2); the epilogue adds the pieces rounding to nearest.
 constexpr int kPieceBlocks = 4;
-constexpr int kOrthStagesMax = 5;
+constexpr int kOrthStagesMax = 4;
 constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;      // one operand plane of one stage and CTA
-__host__ __device__ constexpr uint32_t kStagingBytes(int terms) { return terms == 1 ? 8192u : 4096u; }   // per epilogue warp
+constexpr int kPass = 32;                              // columns an epilogue warp takes at a time
+constexpr uint32_t kPassPlane = 32 * kPass * 2;        // one fp16 plane of such a block
+constexpr uint32_t kBuffer = 2 * kPassPlane;
+constexpr int kBuffers = 3;                            // per epilogue warp
 constexpr int kSetColumns = 256;
 constexpr int kTmemColumns = 512;
 constexpr int kMaxSide = 32768;
 constexpr uint64_t kOrthWaitNs = 2000000000ull;
 
-// operands: K-major rows, MN-major rows; blocks that an epilogue warp reads and writes; transposed blocks
-enum { MAP_XK = 0, MAP_XMN = 2, MAP_XO = 4, MAP_A = 6, MAP_B, MAP_AO, MAP_BO, MAP_AT, MAP_BT, MAP_COUNT };
+// operands: K-major rows, MN-major rows; blocks that an epilogue warp reads and writes
+enum { MAP_XK = 0, MAP_XMN = 2, MAP_XO = 4, MAP_A = 6, MAP_B, MAP_AO, MAP_BO, MAP_COUNT };
 
 struct OrthPtrs {
   const void* u[kPtrGroup];
@@ -164,11 +167,21 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t v) {
   return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
 
-// byte offset of 16-byte piece c of row r in a block of rows of 2 * COLS bytes under the tensor map's swizzle
-// (128-byte rows: c ^ (r & 7); 64-byte rows: c ^ ((r >> 1) & 3)); lanes of a warp then meet distinct banks
-template <int COLS>
-__device__ __forceinline__ uint32_t piece_at(uint32_t r, uint32_t c) {
-  return COLS == 64 ? r * 128u + ((c ^ (r & 7u)) << 4) : r * 64u + ((c ^ ((r >> 1) & 3u)) << 4);
+// byte offset of 16-byte piece c of row r in a block of 64-byte rows under the tensor map's 64-byte swizzle: the
+// lanes of a warp, a row each, then meet distinct banks
+__device__ __forceinline__ uint32_t piece_at(uint32_t r, uint32_t c) { return r * 64u + ((c ^ ((r >> 1) & 3u)) << 4); }
+// wait_done without pauses at first: a tile's rows are often about to be complete
+__device__ __forceinline__ bool wait_rows(const unsigned* counter, unsigned target, const WaitCtx& wc) {
+  for (int i = 0; i < 64; ++i) {
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+    if (v >= target) return true;
+  }
+  return wait_done(counter, target, wc);
+}
+// counts after everything this thread has written (or knows written) is visible to the device
+__device__ __forceinline__ void count_up(unsigned* counter) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
 }
 
 template <typename T>
@@ -186,7 +199,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   __shared__ __align__(8) uint64_t empty_bar[kOrthStagesMax];
   __shared__ __align__(8) uint64_t acc_full[2];
   __shared__ __align__(8) uint64_t acc_empty[2];
-  __shared__ __align__(8) uint64_t add_full[kOrthEpi];
+  __shared__ __align__(8) uint64_t add_full[kOrthEpi * kBuffers];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
@@ -204,7 +217,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       mbar_init(smem_u32(&acc_full[s]), 1);
       mbar_init(smem_u32(&acc_empty[s]), kOrthEpi * 2);
     }
-    for (int s = 0; s < kOrthEpi; ++s) mbar_init(smem_u32(&add_full[s]), 1);
+    for (int s = 0; s < kOrthEpi * kBuffers; ++s) mbar_init(smem_u32(&add_full[s]), 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -240,13 +253,13 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       // the rows this tile reads, each polled by a lane of its own
       if (w.phase == 0) {
         if (w.step > 0 && lane < 2)
-          ok = wait_done(row_counter(p, w.step - 1, 2, w.mat, lane ? w.tj : w.ti), x_rows, wc);
+          ok = wait_rows(row_counter(p, w.step - 1, 2, w.mat, lane ? w.tj : w.ti), x_rows, wc);
       } else if (w.phase == 1) {
-        if (lane < 2) ok = wait_done(row_counter(p, w.step, 0, w.mat, lane ? w.tj : w.ti), sym_rows, wc);
+        if (lane < 2) ok = wait_rows(row_counter(p, w.step, 0, w.mat, lane ? w.tj : w.ti), sym_rows, wc);
       } else {
-        if (lane == 0) ok = wait_done(row_counter(p, w.step, 1, w.mat, w.ti), sym_rows, wc);
+        if (lane == 0) ok = wait_rows(row_counter(p, w.step, 1, w.mat, w.ti), sym_rows, wc);
         if (w.step > 0)
-          for (int r = lane; r < p.tm && ok; r += 32) ok = wait_done(row_counter(p, w.step - 1, 2, w.mat, r), x_rows, wc);
+          for (int r = lane; r < p.tm && ok; r += 32) ok = wait_rows(row_counter(p, w.step - 1, 2, w.mat, r), x_rows, wc);
       }
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -336,21 +349,20 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
     }
   } else if (warp >= kOrthFirstEpi) {
     // ---------------- epilogue ----------------
-    // a tensor-memory lane quarter and one half of the tile's columns each, taken kPass columns at a time:
-    // the copy engine brings the block's addend (both planes of X, or A) into the warp's staging buffer,
-    // each lane replaces its row by the result, and the engine takes it away again
-    constexpr int kPass = TERMS == 1 ? 64 : 32;
-    constexpr uint32_t kPlane = 32 * kPass * 2;
+    // A tensor-memory lane quarter and one half of the tile's columns each, taken kPass columns at a time.  The
+    // copy engine brings a block's addend (both planes of X, or A) into one of the warp's three buffers, each
+    // lane replaces its row by the result, and the engine takes it away again.  Addends are fetched ahead: of
+    // X's four passes three before the sum is there and the fourth once the first's result has been read; of
+    // A's two, then one pass ahead (the third buffer is for transposed blocks).
     const int ew = warp - kOrthFirstEpi, quarter = warp & 3, side = ew >> 2;
-    const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)ew * kStagingBytes(TERMS);
-    const uint32_t add_bar = smem_u32(&add_full[ew]);
-    uint32_t add_phase = 0;
+    const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)ew * (kBuffers * kBuffer);
+    const uint32_t add_bar = smem_u32(&add_full[ew * kBuffers]);
+    uint32_t add_phase = 0;              // a bit per buffer
     int j = 0;
-    // lane 0: start the addend's copy once the engine has read what the buffer held
-    auto fetch = [&](const CUtensorMap* map, int col, int row, int plane, int planes) {
-      bulk_wait_read_all();
-      mbar_expect_tx(add_bar, (uint32_t)planes * kPlane);
-      tma_load_3d<false>(sbuf, map, add_bar, col, row, plane);
+    // lane 0: start an addend's copy into a buffer whose last result the engine has read
+    auto fetch = [&](const CUtensorMap* map, uint32_t buffer, int col, int row, int plane, int planes) {
+      mbar_expect_tx(add_bar + 8u * buffer, (uint32_t)planes * kPassPlane);
+      tma_load_3d<false>(sbuf + buffer * kBuffer, map, add_bar + 8u * buffer, col, row, plane);
     };
     auto hand_over = [&](const CUtensorMap* map, uint32_t src, int col, int row, int plane) {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -362,7 +374,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
     auto store_turned = [&](uint32_t base, uint32_t first, const uint32_t (&pk)[4]) {
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t at = base + piece_at<32>(first + i, (uint32_t)lane >> 3) + ((uint32_t)lane & 7u) * 2u;
+        const uint32_t at = base + piece_at(first + i, (uint32_t)lane >> 3) + ((uint32_t)lane & 7u) * 2u;
         asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)(i & 1 ? pk[i / 2] >> 16 : pk[i / 2] & 0xffffu)) : "memory");
       }
     };
@@ -377,11 +389,12 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       // the addend's rows are complete before its first block is fetched, ahead of the sum
       bool ok = true;
       if (lane == 0) {
-        if (w.phase == 1) ok = wait_done(row_counter(p, w.step, 0, w.mat, w.ti), sym_rows, wc);
-        else if (w.phase == 2 && w.step > 0) ok = wait_done(row_counter(p, w.step - 1, 2, w.mat, w.ti), x_rows, wc);
+        if (w.phase == 1) ok = wait_rows(row_counter(p, w.step, 0, w.mat, w.ti), sym_rows, wc);
+        else if (w.phase == 2 && w.step > 0) ok = wait_rows(row_counter(p, w.step - 1, 2, w.mat, w.ti), x_rows, wc);
         if (ok && addends) {
           asm volatile("fence.proxy.async;" ::: "memory");
-          fetch(from, n0, row0, plane0, addends);
+          const int ahead = w.phase == 2 ? 3 : 2;
+          for (int k = 0; k < ahead && k * kPass < cols; ++k) fetch(from, (uint32_t)k, n0 + k * kPass, row0, plane0, addends);
         }
       }
       ok = __all_sync(0xffffffffu, ok);
@@ -437,28 +450,34 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       const bool mirror = w.phase < 2 && w.ti != w.tj;
       // (unrolled for two terms, whose sums sit in registers)
 #pragma unroll(TERMS == 2 ? 4 : 1)
-      for (int c0 = 0; c0 < 128; c0 += kPass) {
+      for (int k = 0; k < 4; ++k) {
+        const int c0 = k * kPass;
         if (c0 < cols && ok) {
           const int col = n0 + c0;
+          const uint32_t buffer = w.phase == 2 ? (uint32_t)k % 3u : (uint32_t)k & 1u, at = sbuf + buffer * kBuffer;
+          if (k > 0 && (w.phase < 2 || k == 1)) {
+            if (lane == 0) {
+              bulk_wait_read_all();
+              if (w.phase == 2 && 3 * kPass < cols) fetch(from, 0u, n0 + 3 * kPass, row0, plane0, addends);
+              if (w.phase == 1 && k < 3 && c0 + kPass < cols) fetch(from, (uint32_t)(k + 1) & 1u, col + kPass, row0, plane0, addends);
+            }
+            __syncwarp();
+          }
           float v[kPass];
           if (TERMS == 1) {
+            uint32_t r[32];
+            tmem_ld32_issue(t0 + (uint32_t)c0, r);
+            tmem_ld_wait();
 #pragma unroll
-            for (int h = 0; h < kPass; h += 32) {
-              uint32_t r[32];
-              tmem_ld32_issue(t0 + (uint32_t)(c0 + h), r);
-              tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[h + i] = alpha * __uint_as_float(r[i]);
-            }
+            for (int i = 0; i < 32; ++i) v[i] = alpha * __uint_as_float(r[i]);
             if (c0 + kPass >= cols) give_back();
           } else {
 #pragma unroll
-            for (int i = 0; i < kPass; ++i) v[i] = alpha * acc[TERMS == 2 ? c0 / 32 : 0][i];
+            for (int i = 0; i < kPass; ++i) v[i] = alpha * acc[TERMS == 2 ? k : 0][i];
           }
           if (addends) {
-            if (lane == 0 && c0 > 0) fetch(from, col, row0, plane0, addends);
-            ok = __all_sync(0xffffffffu, mbar_wait<false>(add_bar, add_phase, wc, 6u));
-            add_phase ^= 1u;
+            ok = __all_sync(0xffffffffu, mbar_wait<false>(add_bar + 8u * buffer, (add_phase >> buffer) & 1u, wc, 6u));
+            add_phase ^= 1u << buffer;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
               if (t < addends) {
@@ -467,7 +486,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
                   uint32_t r[4];
                   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                               : "r"(sbuf + (uint32_t)t * kPlane + piece_at<kPass>((uint32_t)lane, q)));
+                               : "r"(at + (uint32_t)t * kPassPlane + piece_at((uint32_t)lane, q)));
 #pragma unroll
                   for (int i = 0; i < 4; ++i) {
                     const float2 f = unpack_half2(r[i]);
@@ -477,9 +496,6 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
                 }
               }
             }
-          } else {
-            if (lane == 0) bulk_wait_read_all();
-            __syncwarp();
           }
           if (w.phase < 2 && w.ti == w.tj) {
 #pragma unroll
@@ -500,45 +516,21 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
                   v[8 * q + 2 * i] -= f.x;
                   v[8 * q + 2 * i + 1] -= f.y;
                 }
-                st_shared_v4(sbuf + (uint32_t)t * kPlane + piece_at<kPass>((uint32_t)lane, q), pk[0], pk[1], pk[2], pk[3]);
-                if (TERMS == 1 && mirror) store_turned(sbuf + kPlane, 8u * q, pk);     // the other half of the buffer
+                st_shared_v4(at + (uint32_t)t * kPassPlane + piece_at((uint32_t)lane, q), pk[0], pk[1], pk[2], pk[3]);
+                if (mirror) store_turned(sbuf + 2u * kBuffer + (uint32_t)t * kPassPlane, 8u * q, pk);
               }
             }
           }
-          hand_over(to, sbuf, col, row0, plane0);
-          if (mirror) {
-            if (TERMS == 2) {
-              // two terms fill the buffer: the rows are read back, and turned once the engine has them
-              uint32_t pk[2][kPass / 2];
-#pragma unroll
-              for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (uint32_t q = 0; q < kPass / 8; ++q)
-                  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                               : "=r"(pk[t][4 * q]), "=r"(pk[t][4 * q + 1]), "=r"(pk[t][4 * q + 2]), "=r"(pk[t][4 * q + 3])
-                               : "r"(sbuf + (uint32_t)t * kPlane + piece_at<kPass>((uint32_t)lane, q))
-                               : "memory");
-              if (lane == 0) bulk_wait_read_all();
-              __syncwarp();
-#pragma unroll
-              for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (uint32_t q = 0; q < kPass / 8; ++q) {
-                  const uint32_t four[4] = {pk[t][4 * q], pk[t][4 * q + 1], pk[t][4 * q + 2], pk[t][4 * q + 3]};
-                  store_turned(sbuf + (uint32_t)t * kPlane, 8u * q, four);
-                }
-            }
-            hand_over(w.phase == 0 ? &p.map[MAP_AT] : &p.map[MAP_BT], TERMS == 1 ? sbuf + kPlane : sbuf, row0, col, plane0);
-          }
+          hand_over(to, at, col, row0, plane0);
+          if (mirror) hand_over(to, sbuf + 2u * kBuffer, row0, col, plane0);
         }
       }
       if (!ok) break;
       if (lane == 0) {
         bulk_wait_all();               // written, not just read from the staging blocks
-        __threadfence();
         unsigned* cnt = const_cast<unsigned*>(row_counter(p, w.step, w.phase, w.mat, 0));
-        atomicAdd(cnt + w.ti, 1u);
-        if (w.phase < 2 && w.ti != w.tj) atomicAdd(cnt + w.tj, 1u);
+        count_up(cnt + w.ti);
+        if (mirror) count_up(cnt + w.tj);
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -1007,16 +999,13 @@ mw_status orth_maps(mw_orth* p, const OrthWs& l, const void* ws) {
   const int64_t c = p->d.count;
   const int t = p->terms;
   const auto S128 = CU_TENSOR_MAP_SWIZZLE_128B, S64 = CU_TENSOR_MAP_SWIZZLE_64B;
-  const int pass = t == 1 ? 64 : 32;
-  const auto SP = t == 1 ? S128 : S64;
   for (int b = 0; b < 2; ++b) {
     MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, kBK, kHalf, t, S128, &p->maps[MAP_XK + b]));
     MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, 64, kBK, 1, S128, &p->maps[MAP_XMN + b]));
-    MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, pass, 32, 2, SP, &p->maps[MAP_XO + b]));
+    MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, kPass, 32, 2, S64, &p->maps[MAP_XO + b]));
     const __half* s = b ? l.b : l.a;
     MW_TRY(half_map(s, p->mp, p->mp, t * c, kBK, kHalf, t, S128, &p->maps[MAP_A + b]));
-    MW_TRY(half_map(s, p->mp, p->mp, t * c, pass, 32, t, SP, &p->maps[MAP_AO + b]));
-    MW_TRY(half_map(s, p->mp, p->mp, t * c, 32, pass, t, S64, &p->maps[MAP_AT + b]));
+    MW_TRY(half_map(s, p->mp, p->mp, t * c, kPass, 32, t, S64, &p->maps[MAP_AO + b]));
   }
   p->mapped = ws;
   return MW_OK;
@@ -1174,8 +1163,8 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.st = reinterpret_cast<DeviceStatus*>(ws);
   q.wait_ns = kOrthWaitNs;
   q.stage_bytes = 2u * (uint32_t)p->terms * kPlaneBytes;
-  q.stages = p->terms == 1 ? 5 : 3;
-  const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * kStagingBytes(p->terms);
+  q.stages = p->terms == 1 ? 4 : 2;
+  const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * kBuffers * kBuffer;
   MW_TRY(p->terms == 1 ? orth_launch<1>(q, smem, s) : orth_launch<2>(q, smem, s));
   for (int first = 0; first < count; first += kPtrGroup) {
     const int c = count - first < kPtrGroup ? count - first : kPtrGroup;
