@@ -179,6 +179,20 @@ __device__ __forceinline__ bool wait_rows(const unsigned* counter, unsigned targ
   }
   return wait_done(counter, target, wc);
 }
+// barriers of the epilogue warps alone; the first tells all of them whether any gave up
+__device__ __forceinline__ bool epilogue_any(bool failed) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.aligned.pred q, 1, %2, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)failed), "n"(kOrthEpi * 32)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void epilogue_sync() { asm volatile("barrier.cta.sync.aligned 2, %0;" ::"n"(kOrthEpi * 32) : "memory"); }
 // counts after everything this thread has written (or knows written) is visible to the device
 __device__ __forceinline__ void count_up(unsigned* counter) {
   asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
@@ -237,7 +251,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   wc.st = p.st;
   wc.abort_flag = &abort_flag;
   wc.limit_ns = p.wait_ns;
-  const unsigned sym_rows = (unsigned)p.tm * kOrthEpi * 2, x_rows = (unsigned)p.tn * kOrthEpi * 2;
+  const unsigned sym_rows = (unsigned)p.tm * 2, x_rows = (unsigned)p.tn * 2;      // one count a CTA and tile
 
   if (warp < kOrthFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
@@ -359,6 +373,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
     const uint32_t add_bar = smem_u32(&add_full[ew * kBuffers]);
     uint32_t add_phase = 0;              // a bit per buffer
     int j = 0;
+    bool failed = false;                 // a wait ran out: all epilogue warps leave together
     // lane 0: start an addend's copy into a buffer whose last result the engine has read
     auto fetch = [&](const CUtensorMap* map, uint32_t buffer, int col, int row, int plane, int planes) {
       mbar_expect_tx(add_bar + 8u * buffer, (uint32_t)planes * kPassPlane);
@@ -388,16 +403,17 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       const int plane0 = w.mat * (w.phase == 2 ? 2 : TERMS);
       // the addend's rows are complete before its first block is fetched, ahead of the sum
       bool ok = true;
-      if (lane == 0) {
+      if (ew == 0 && lane == 0) {
         if (w.phase == 1) ok = wait_rows(row_counter(p, w.step, 0, w.mat, w.ti), sym_rows, wc);
         else if (w.phase == 2 && w.step > 0) ok = wait_rows(row_counter(p, w.step - 1, 2, w.mat, w.ti), x_rows, wc);
-        if (ok && addends) {
-          asm volatile("fence.proxy.async;" ::: "memory");
-          const int ahead = w.phase == 2 ? 3 : 2;
-          for (int k = 0; k < ahead && k * kPass < cols; ++k) fetch(from, (uint32_t)k, n0 + k * kPass, row0, plane0, addends);
-        }
       }
-      ok = __all_sync(0xffffffffu, ok);
+      __syncwarp();
+      if (epilogue_any(!ok || failed)) break;
+      if (lane == 0 && addends) {
+        asm volatile("fence.proxy.async;" ::: "memory");
+        const int ahead = w.phase == 2 ? 3 : 2;
+        for (int k = 0; k < ahead && k * kPass < cols; ++k) fetch(from, (uint32_t)k, n0 + k * kPass, row0, plane0, addends);
+      }
       // Two terms: the pieces of the sum meet in registers, and each accumulator goes straight back.
       // One term: a pass reads its columns from the one accumulator, which goes back after the last.
       float acc[TERMS == 2 ? 4 : 1][32];
@@ -442,7 +458,6 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
           give_back();
         }
       }
-      if (!ok) break;
       const float alpha = w.phase == 0 ? p.f.a_scale : (w.phase == 1 ? p.f.b_acc : p.f.x_acc);
       const float scale = w.phase == 1 ? p.f.b_add[w.step] : p.f.x_add[w.step];
       const float diag = w.phase == 0 ? p.f.a_diag[w.step] : p.f.b_diag[w.step];
@@ -525,9 +540,13 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
           if (mirror) hand_over(to, sbuf + 2u * kBuffer, row0, col, plane0);
         }
       }
-      if (!ok) break;
-      if (lane == 0) {
-        bulk_wait_all();               // written, not just read from the staging blocks
+      // one count for the whole CTA, once all its stores have been written (a release a warp would be eight
+      // fences on end)
+      if (lane == 0) bulk_wait_all();
+      __syncwarp();
+      failed = !ok;
+      epilogue_sync();
+      if (ew == 0 && lane == 0) {
         unsigned* cnt = const_cast<unsigned*>(row_counter(p, w.step, w.phase, w.mat, 0));
         count_up(cnt + w.ti);
         if (mirror) count_up(cnt + w.tj);
