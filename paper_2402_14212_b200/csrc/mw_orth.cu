@@ -45,7 +45,7 @@ struct mw_orth {
   bool small;          // one CTA a matrix, everything in shared memory
   // tensor maps of a workspace, encoded when the workspace first comes along
   const void* mapped = nullptr;
-  CUtensorMap maps[10];
+  CUtensorMap maps[13];
 };
 
 namespace mw {
@@ -77,7 +77,8 @@ constexpr int kMaxSide = 32768;
 constexpr uint64_t kOrthWaitNs = 2000000000ull;
 
 // operands: K-major rows, MN-major rows; blocks that an epilogue warp reads and writes
-enum { MAP_XK = 0, MAP_XMN = 2, MAP_XO = 4, MAP_A = 6, MAP_B, MAP_AO, MAP_BO, MAP_COUNT };
+// (MAP_XK64, MAP_A64: 64 rows for the second operand of a tile of 128 columns)
+enum { MAP_XK = 0, MAP_XMN = 2, MAP_XO = 4, MAP_A = 6, MAP_B, MAP_AO, MAP_BO, MAP_XK64, MAP_A64 = 12, MAP_COUNT };
 
 struct OrthPtrs {
   const void* u[kPtrGroup];
@@ -96,7 +97,8 @@ struct OrthFactors {
 
 struct alignas(64) OrthParams {
   CUtensorMap map[MAP_COUNT];
-  int count, tm, tn, steps, tri, per_step, total;
+  int count, tm, tn, steps, per_step, total;
+  int bn_sym, bn_x, sym_tiles;   // tile widths; tiles of a symmetric product (tn counts those of B X)
   int kb_m, kb_n;                // K blocks of a sum over m and over n
   int piece_blocks;              // K blocks of one accumulator (0: all)
   int mp, np, stages;
@@ -107,7 +109,7 @@ struct alignas(64) OrthParams {
   uint64_t wait_ns;
 };
 
-struct OrthUnit { int step, phase, mat, ti, tj, bn, nkb, pieces; };
+struct OrthUnit { int step, phase, mat, ti, tj, n0, bn, nkb, pieces; };      // tj: the row of tiles that column n0 mirrors to
 
 // place t of a triangle of tiles (i, j >= i): row by row, or column by column
 __device__ __forceinline__ void triangle_rows(int t, int tm, int& i, int& j) {
@@ -125,16 +127,19 @@ __device__ __forceinline__ OrthUnit orth_unit(const OrthParams& p, int u) {
   OrthUnit w;
   w.step = u / p.per_step;
   int r = u - w.step * p.per_step;
-  const int sym = p.count * p.tri;
-  w.bn = kTile;
+  const int sym = p.count * p.sym_tiles;
   if (r < 2 * sym) {
     w.phase = r >= sym;
     r -= w.phase * sym;
-    w.mat = r / p.tri;
-    r -= w.mat * p.tri;
+    w.mat = r / p.sym_tiles;
+    r -= w.mat * p.sym_tiles;
+    w.bn = p.bn_sym;
+    int half = 0;
+    if (w.bn < kTile) { half = r & 1; r >>= 1; }
     // A's rows are completed early for B; B waits for them in the order they come
     if (w.phase == 0) triangle_rows(r, p.tm, w.ti, w.tj);
     else triangle_columns(r, w.ti, w.tj);
+    w.n0 = w.tj * kTile + half * w.bn;
     w.nkb = w.phase == 0 ? p.kb_n : p.kb_m;
   } else {
     r -= 2 * sym;
@@ -143,9 +148,10 @@ __device__ __forceinline__ OrthUnit orth_unit(const OrthParams& p, int u) {
     w.mat = r / per;
     r -= w.mat * per;
     w.ti = r / p.tn;
-    w.tj = r - w.ti * p.tn;
+    w.n0 = (r - w.ti * p.tn) * p.bn_x;
+    w.tj = 0;
     w.nkb = p.kb_m;
-    if ((w.tj + 1) * kTile > p.np) w.bn = kHalf;
+    w.bn = p.np - w.n0 < p.bn_x ? kHalf : p.bn_x;
   }
   w.pieces = p.piece_blocks ? (w.nkb + p.piece_blocks - 1) / p.piece_blocks : 1;
   return w;
@@ -251,7 +257,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   wc.st = p.st;
   wc.abort_flag = &abort_flag;
   wc.limit_ns = p.wait_ns;
-  const unsigned sym_rows = (unsigned)p.tm * 2, x_rows = (unsigned)p.tn * 2;      // one count a CTA and tile
+  const unsigned sym_rows = (unsigned)(p.tm * (kTile / p.bn_sym)) * 2, x_rows = (unsigned)p.tn * 2;      // one count a CTA and tile
 
   if (warp < kOrthFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
@@ -282,10 +288,11 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         const int buf = w.step & 1;
         const CUtensorMap* ta = w.phase == 0 ? &p.map[MAP_XK + buf] : (w.phase == 1 ? &p.map[MAP_A] : &p.map[MAP_B]);
         const int plane_a = w.mat * (w.phase == 0 ? 2 : TERMS);
-        const CUtensorMap* tb = w.phase == 2 ? &p.map[MAP_XMN + buf] : ta;
+        const CUtensorMap* tb = w.phase == 2 ? &p.map[MAP_XMN + buf]
+                                             : (w.bn == kTile ? ta : (w.phase == 0 ? &p.map[MAP_XK64 + buf] : &p.map[MAP_A64]));
         const int am0 = w.ti * kTile + (int)rank * kHalf;
         const int half = w.bn >> 1;
-        const int bn0 = w.tj * kTile + (int)rank * half;
+        const int bn0 = w.n0 + (int)rank * half;
         const uint32_t b_off = TERMS * kPlaneBytes, b_plane = (uint32_t)half * (kBK * 2);
         const uint32_t tx = 2u * TERMS * (kPlaneBytes + b_plane);
         for (int kb = 0; kb < w.nkb; ++kb) {
@@ -396,7 +403,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
     for (int u = pair; u < p.total; u += pairs) {
       const OrthUnit w = orth_unit(p, u);
       const int row0 = w.ti * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
-      const int cols = w.bn >> 1, n0 = w.tj * kTile + side * cols;      // this warp's columns
+      const int cols = w.bn >> 1, n0 = w.n0 + side * cols;      // this warp's columns
       const int addends = w.phase == 0 ? 0 : (w.phase == 1 ? TERMS : 2);
       const CUtensorMap* from = w.phase == 1 ? &p.map[MAP_AO] : &p.map[MAP_XO + (w.step & 1)];
       const CUtensorMap* to = w.phase == 0 ? &p.map[MAP_AO] : (w.phase == 1 ? &p.map[MAP_BO] : &p.map[MAP_XO + ((w.step + 1) & 1)]);
@@ -1026,16 +1033,59 @@ mw_status orth_maps(mw_orth* p, const OrthWs& l, const void* ws) {
     MW_TRY(half_map(s, p->mp, p->mp, t * c, kBK, kHalf, t, S128, &p->maps[MAP_A + b]));
     MW_TRY(half_map(s, p->mp, p->mp, t * c, kPass, 32, t, S64, &p->maps[MAP_AO + b]));
   }
+  for (int b = 0; b < 2; ++b) MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, kBK, 64, t, S128, &p->maps[MAP_XK64 + b]));
+  MW_TRY(half_map(l.a, p->mp, p->mp, t * c, kBK, 64, t, S128, &p->maps[MAP_A64]));
   p->mapped = ws;
   return MW_OK;
 }
 
+// CTA pairs that the device holds at once (cached per device)
 template <int TERMS>
-mw_status orth_launch(const OrthParams& prm, size_t smem, cudaStream_t s) {
+mw_status orth_pairs(size_t smem, int* out) {
   static int pairs[kMaxDevices] = {};
   const int dev = current_device();
-  auto kernel = orth_products_kernel<TERMS>;
+  if (pairs[dev] == 0) {
+    auto kernel = orth_products_kernel<TERMS>;
+    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (unsigned)sm_count());
+    cfg.blockDim = dim3(kOrthThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int c = 0;
+    MW_CUDA_OK(cudaOccupancyMaxActiveClusters(&c, kernel, &cfg));
+    if (c < 1) return MW_ERR_CUDA;
+    pairs[dev] = c < sm_count() / 2 ? c : sm_count() / 2;
+  }
+  *out = pairs[dev];
+  return MW_OK;
+}
+
+template <int TERMS>
+mw_status orth_launch(OrthParams& prm, size_t smem, cudaStream_t s) {
+  int pairs = 0;
+  MW_TRY(orth_pairs<TERMS>(smem, &pairs));
+  // Tiles of 256 columns, whose products run at the full rate; of 128 where all of a product's fit the device
+  // at once, so that a phase, which then lasts as long as one tile, is shorter (one 1024 x 1024 in bf16: SYM_US us
+  // with 128 columns, 257 us with 256; 16 of them, whose tiles do not fit: 487 us with 256)
+  const int tri = prm.tm * (prm.tm + 1) / 2;
+  const int64_t sym = (int64_t)prm.count * tri, x128 = (int64_t)prm.count * prm.tm * ceil_div(prm.np, kHalf);
+  prm.bn_sym = 2 * sym <= pairs ? kHalf : kTile;
+  prm.bn_x = x128 <= pairs ? kHalf : kTile;
+  prm.sym_tiles = tri * (kTile / prm.bn_sym);
+  prm.tn = ceil_div(prm.np, prm.bn_x);
+  const int64_t per = (int64_t)prm.count * (2 * (int64_t)prm.sym_tiles + (int64_t)prm.tm * prm.tn);
+  if (per * prm.steps > (1 << 30)) return MW_ERR_UNSUPPORTED;
+  prm.per_step = (int)per;
+  prm.total = prm.per_step * prm.steps;
+  const int64_t widest = (int64_t)prm.count * (prm.tm * prm.tn > prm.sym_tiles ? prm.tm * prm.tn : prm.sym_tiles);
   cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (unsigned)(widest < pairs ? widest : pairs));
   cfg.blockDim = dim3(kOrthThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -1046,20 +1096,9 @@ mw_status orth_launch(const OrthParams& prm, size_t smem, cudaStream_t s) {
   attr[1].id = cudaLaunchAttributeCooperative;      // tiles wait for one another: all pairs are resident
   attr[1].val.cooperative = tc_cooperative();
   cfg.attrs = attr;
-  if (pairs[dev] == 0) {
-    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    cfg.gridDim = dim3(2 * (unsigned)sm_count());
-    cfg.numAttrs = 1;
-    int c = 0;
-    MW_CUDA_OK(cudaOccupancyMaxActiveClusters(&c, kernel, &cfg));
-    if (c < 1) return MW_ERR_CUDA;
-    pairs[dev] = c < sm_count() / 2 ? c : sm_count() / 2;
-  }
-  const int widest = prm.count * (prm.tm * prm.tn > prm.tri ? prm.tm * prm.tn : prm.tri);
-  cfg.gridDim = dim3(2 * (unsigned)(widest < pairs[dev] ? widest : pairs[dev]));
   cfg.numAttrs = 2;
   ++g_launch_count;
-  return cudaLaunchKernelEx(&cfg, kernel, prm) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, orth_products_kernel<TERMS>, prm) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
 }
 
 double pow2_floor(double v) { return exp2(floor(log2(v))); }
@@ -1166,13 +1205,7 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   for (int i = 0; i < MAP_COUNT; ++i) q.map[i] = p->maps[i];
   q.count = count;
   q.tm = p->mp / kTile;
-  q.tn = ceil_div(p->np, kTile);
   q.steps = p->steps;
-  q.tri = q.tm * (q.tm + 1) / 2;
-  const int64_t per = (int64_t)count * (2 * (int64_t)q.tri + (int64_t)q.tm * q.tn);
-  if (per * p->steps > (1 << 30)) return MW_ERR_UNSUPPORTED;
-  q.per_step = (int)per;
-  q.total = q.per_step * p->steps;
   q.kb_m = ceil_div(m, kBK);
   q.kb_n = ceil_div(n, kBK);
   q.piece_blocks = p->terms == 2 ? kPieceBlocks : 0;

@@ -42,7 +42,7 @@ def rel(a, b):
     return float(np.linalg.norm(a - b) / max(np.linalg.norm(b), 1e-300))
 
 
-SHAPES = [(1, 1, 2), (1, 9, 1), (7, 3, 2), (33, 65, 3), (64, 64, 2), (128, 128, 1), (70, 130, 2), (200, 96, 3), (128, 256, 3), (250, 128, 2), (128, 300, 1), (129, 200, 1),
+SHAPES = [(1, 1, 2), (1, 9, 1), (7, 3, 2), (33, 65, 3), (64, 64, 2), (128, 128, 1), (70, 130, 2), (200, 96, 3), (128, 256, 3), (250, 128, 2), (128, 300, 1), (129, 200, 1), (513, 520, 14),
           (256, 256, 2), (257, 300, 2), (512, 192, 1), (640, 640, 2), (1000, 260, 1)]
 
 
