@@ -228,6 +228,12 @@ norm_forward_kernel(const NormArgs a) {
   }
 }
 
+// rows whose copies (80 bytes for each 16-byte piece of a row) fit beside each other: four up to 40 KB a row, two up
+// to 80 KB; longer rows are held in registers
+__host__ __device__ constexpr int backward_stages(int pieces) {
+  return pieces <= 512 ? 4 : (pieces <= 1024 ? 2 : 0);
+}
+
 // Backward of a row, with xh = x' / rms, bh = b / rms, q = dn w_pre, ks = scale w_post, tau = ks silu(z) bh:
 //   dx = dx_out + (q - xh m1) / rms(x'),                m1 = mean(q xh)
 //   db = (dx ks silu(z) - bh m2) / rms(b),              m2 = mean(dx tau)
@@ -247,42 +253,96 @@ norm_backward_kernel(const NormArgs a) {
   const int D = a.cols;
   const float inv_d = 1.f / (float)D;
   const bool has_b = a.b != nullptr, has_z = a.z != nullptr, normed = a.w_post != nullptr;
+  // A thread's 16 bytes of each tensor come by asynchronous copies into shared memory of its own, kStages - 1 rows
+  // ahead: at 40 bytes an element in and out, one row ahead leaves HBM idle while a row is reduced.  (Rows
+  // that are read element by element, whose copies could not be that small, are held in registers, one
+  // row ahead.)
+  constexpr bool kStaged = sizeof(Raw) == 16 && backward_stages(kThreads * K) > 0;
+  constexpr int kStages = kStaged ? backward_stages(kThreads * K) : 1;
+  extern __shared__ __align__(16) unsigned char ring[];
+  unsigned char* mine = ring + threadIdx.x * 16;
+  constexpr uint32_t kTensor = kThreads * 16, kPart = 5 * kTensor, kStage = K * kPart;
   Raw rx[K], rb[K], rz[K], ro[K], rn[K];
   float next_b = 0.f, next_x = 0.f;
+  auto place = [&](int64_t row, const T* (&at)[5]) {
+    at[0] = static_cast<const T*>(a.x) + row * a.ld_x;
+    at[1] = static_cast<const T*>(a.b) + row * a.ld_b;
+    at[2] = static_cast<const T*>(a.z) + row * a.ld_z;
+    at[3] = static_cast<const T*>(a.dx_out) + row * D;
+    at[4] = static_cast<const T*>(a.dn) + row * D;
+  };
+  const bool has[5] = {true, has_b, has_z, a.dx_out != nullptr, a.dn != nullptr};
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  // start the copies of the row `ahead` iterations from `row` (one group each, empty past the end)
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < a.rows) {
+      const T* at[5];
+      place(row, at);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int c = (k * G + t) * VEC;
+#pragma unroll
+        for (int j = 0; j < 5; ++j) {
+          const bool on = has[j] && c < D;
+          const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine + stage * kStage + k * kPart + j * kTensor);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(on ? (const void*)(at[j] + c) : a.x),
+                       "r"(on ? 16 : 0)
+                       : "memory");
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // the present row's values; the rows' two factors come one row ahead in registers either way
   auto load = [&](int64_t row) {
     if (row >= a.rows) row = a.rows - 1;        // takes part in the barriers, counts for nothing
-    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-    const T* b = static_cast<const T*>(a.b) + row * a.ld_b;
-    const T* z = static_cast<const T*>(a.z) + row * a.ld_z;
-    const T* go = static_cast<const T*>(a.dx_out) + row * D;
-    const T* gn = static_cast<const T*>(a.dn) + row * D;
+    if (!kStaged) {
+      const T* at[5];
+      place(row, at);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = (k * G + t) * VEC;
-      rx[k] = rb[k] = rz[k] = ro[k] = rn[k] = P::zero();
-      if (c < D) {
-        rx[k] = __ldcs(reinterpret_cast<const Raw*>(x + c));
-        if (has_b) rb[k] = __ldcs(reinterpret_cast<const Raw*>(b + c));
-        if (has_z) rz[k] = __ldcs(reinterpret_cast<const Raw*>(z + c));
-        if (a.dx_out) ro[k] = __ldcs(reinterpret_cast<const Raw*>(go + c));
-        if (a.dn) rn[k] = __ldcs(reinterpret_cast<const Raw*>(gn + c));
+      for (int k = 0; k < K; ++k) {
+        const int c = (k * G + t) * VEC;
+        rx[k] = rb[k] = rz[k] = ro[k] = rn[k] = P::zero();
+        if (c < D) {
+          rx[k] = __ldcs(reinterpret_cast<const Raw*>(at[0] + c));
+          if (has[1]) rb[k] = __ldcs(reinterpret_cast<const Raw*>(at[1] + c));
+          if (has[2]) rz[k] = __ldcs(reinterpret_cast<const Raw*>(at[2] + c));
+          if (has[3]) ro[k] = __ldcs(reinterpret_cast<const Raw*>(at[3] + c));
+          if (has[4]) rn[k] = __ldcs(reinterpret_cast<const Raw*>(at[4] + c));
+        }
       }
     }
     next_b = a.rms_in[row];
     next_x = a.rms_in[a.rows + row];
   };
-  const int64_t stride = (int64_t)gridDim.x * kRows;
-  load((int64_t)blockIdx.x * kRows + sub);
+  const int64_t row0 = (int64_t)blockIdx.x * kRows + sub;
+  if (kStaged)
+    for (int i = 0; i < kStages - 1; ++i) fetch(row0 + i * stride, i);
+  load(row0);
   float ks[K][VEC], wn[K][VEC], acc_s[K][VEC], acc_n[K][VEC];
   column_constants<VEC, G, K>(a, t, ks, wn);
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc_s[k][i] = acc_n[k][i] = 0.f;
-  int flip = 0;
+  int flip = 0, stage = 0;
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += stride) {
     const int64_t row = base + sub;
     const bool live = row < a.rows;
+    if (kStaged) {
+      fetch(row + (kStages - 1) * stride, (stage + kStages - 1) % kStages);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      const unsigned char* at = mine + stage * kStage;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        rx[k] = *reinterpret_cast<const Raw*>(at + k * kPart);
+        rb[k] = *reinterpret_cast<const Raw*>(at + k * kPart + kTensor);
+        rz[k] = *reinterpret_cast<const Raw*>(at + k * kPart + 2 * kTensor);
+        ro[k] = *reinterpret_cast<const Raw*>(at + k * kPart + 3 * kTensor);
+        rn[k] = *reinterpret_cast<const Raw*>(at + k * kPart + 4 * kTensor);
+      }
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
     const float inv_b = next_b, inv_x = a.w_pre ? next_x : 0.f, xs = next_x;
     // kept over the reduction: dx_out + q / rms(x'), xh, silu(z), silu'(z), b
     float A[K][VEC], xh[K][VEC], gate[K][VEC], slope[K][VEC];
@@ -417,8 +477,11 @@ mw_status launch_forward(const NormArgs& a, cudaStream_t s) {
 }
 template <typename T, int VEC, int G, int VALUES>
 mw_status launch_backward(const NormArgs& a, cudaStream_t s) {
-  constexpr int threads = G > kNormThreads ? G : kNormThreads;
-  norm_backward_kernel<T, VEC, G, VALUES / VEC><<<(unsigned)backward_blocks(a.rows, a.cols), threads, 0, s>>>(a);
+  constexpr int threads = G > kNormThreads ? G : kNormThreads, K = VALUES / VEC;
+  const size_t ring = VEC * sizeof(T) == 16 ? (size_t)backward_stages(threads * K) * threads * K * 80 : 0;
+  auto kernel = norm_backward_kernel<T, VEC, G, K>;
+  MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
+  kernel<<<(unsigned)backward_blocks(a.rows, a.cols), threads, ring, s>>>(a);
   return launch_ok();
 }
 
