@@ -531,6 +531,15 @@ def _raw_stream(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _used_on(stream, *tensors):
+    """Tensors made here on the current stream, used on `stream`: the allocator must not hand their memory
+    out again before the work there is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _dense_like(t):
     """A new dense tensor of t's shape and type."""
     import torch
@@ -540,6 +549,7 @@ def _dense_like(t):
 def _scan_call(v, f, reset, lengths, input_gate, named):
     """Checks of the tensors every scan call shares; `named` {name: [B, T, D] tensor like v or None}."""
     import torch
+    _need(v.is_cuda, "gated_scan: CUDA tensors")
     _need(v.dim() == 3, "gated_scan: v is [batch, length, channels]")
     if input_gate not in INPUT_GATE:
         raise ValueError(f"gated_scan: input_gate is one of {sorted(INPUT_GATE)}")
@@ -592,6 +602,7 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
     _check(lib().mw_gated_scan_forward(d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), _ptr(h0),
                                        y.data_ptr(), h_last.data_ptr(), _ptr(states), _raw_stream(stream, v.device)),
            "mw_gated_scan_forward")
+    _used_on(stream, y, h_last, states)
     return (y, h_last, states) if keep_states else (y, h_last)
 
 
@@ -619,10 +630,12 @@ def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_
     _check(lib().mw_gated_scan_backward(d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), states.data_ptr(),
                                         _ptr(dy), _ptr(dh_last), dv.data_ptr(), df.data_ptr(), dh0.data_ptr(),
                                         _raw_stream(stream, v.device)), "mw_gated_scan_backward")
+    _used_on(stream, dv, df, dh0)
     return dv, df, dh0
 
 
 def _norm_call(x, b, z, w_post, scale, w_pre, eps, dense):
+    _need(x.is_cuda, "residual_norm: CUDA tensors")
     _need(x.dim() == 2, "residual_norm: x is [rows, cols]")
     R, D = x.shape
     d = ResidualNormDesc(R, D, _operand_dtype(x, "residual_norm"), float(eps), 0, 0, 0)
@@ -661,6 +674,7 @@ def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: f
     _check(lib().mw_residual_norm_forward(d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre),
                                           x_out.data_ptr(), _ptr(n), _ptr(rms), _raw_stream(stream, x.device)),
            "mw_residual_norm_forward")
+    _used_on(stream, x_out, n, rms)
     return (x_out, n, rms) if keep_rms else (x_out, n)
 
 
@@ -695,6 +709,7 @@ def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre
         d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre), inv_rms.data_ptr(), _ptr(dx_out),
         _ptr(dn), g.dx.data_ptr(), _ptr(g.db), _ptr(g.dz), _ptr(g.dw_post), _ptr(g.dscale), _ptr(g.dw_pre),
         scratch.data_ptr(), need, _raw_stream(stream, x.device)), "mw_residual_norm_backward")
+    _used_on(stream, scratch, *g)
     return g
 
 
@@ -734,13 +749,14 @@ class Orth:
         import torch
         return torch.empty(self.workspace_bytes() + 256, dtype=torch.uint8, device=device)
 
-    def _list(self, tensors, dtype, name):
+    def _list(self, tensors, dtype, name, workspace):
         tensors = list(tensors)
-        ok = len(tensors) == self.count
+        ok = len(tensors) == self.count and workspace.is_cuda
         for t in tensors:
-            ok = ok and t.dtype == dtype and t.shape == self.shape and t.is_contiguous()
+            ok = ok and t.dtype == dtype and t.shape == self.shape and t.is_contiguous() and t.device == workspace.device
         if not ok:
-            raise ValueError(f"Orth: {name} are {self.count} contiguous {dtype} tensors of shape {self.shape}")
+            raise ValueError(f"Orth: {name} are {self.count} contiguous {dtype} tensors of shape {self.shape} on the "
+                             "workspace's CUDA device")
         return (C.c_void_p * self.count)(*[t.data_ptr() for t in tensors])
 
     def step(self, params, grads, momentum, workspace, lr: float, beta: float = 0.95, weight_decay: float = 0.0,
@@ -752,9 +768,9 @@ class Orth:
         st, f32 = self.storage_dtype(), torch.float32
         wp, wb = Net._ws(workspace)
         _check(lib().mw_orth_step(
-            self._h, self._list(params, st, "params"), self._list(grads, f32, "grads"),
-            self._list(momentum, f32, "momentum"), self._list(params_out, st, "params_out"),
-            self._list(momentum_out, f32, "momentum_out"), float(lr), float(beta), float(weight_decay), float(scale),
+            self._h, self._list(params, st, "params", workspace), self._list(grads, f32, "grads", workspace),
+            self._list(momentum, f32, "momentum", workspace), self._list(params_out, st, "params_out", workspace),
+            self._list(momentum_out, f32, "momentum_out", workspace), float(lr), float(beta), float(weight_decay), float(scale),
             wp, wb, _raw_stream(stream, workspace.device)), "mw_orth_step")
         return params_out
 
@@ -764,8 +780,9 @@ class Orth:
         st = self.storage_dtype()
         if out is None:
             out = [torch.empty_like(t) for t in mats]
+            _used_on(stream, *out)
         wp, wb = Net._ws(workspace)
-        _check(lib().mw_orth_project(self._h, self._list(mats, st, "mats"), self._list(out, st, "out"), wp, wb,
+        _check(lib().mw_orth_project(self._h, self._list(mats, st, "mats", workspace), self._list(out, st, "out", workspace), wp, wb,
                                      _raw_stream(stream, workspace.device)), "mw_orth_project")
         return out
 

@@ -566,13 +566,10 @@ scan_chunk_back_kernel(const ScanArgs p) {
 // ---------------------------------------------------------------------------------------------
 // The same two kernels for rows that start on 16-byte boundaries.  They are bound by the issue of
 // instructions, and a third of those of the kernels above are loads, stores and their addresses, a row
-// of 128 bytes at a time.  Here a warp brings its kEvery rows of each tensor into shared memory by
-// asynchronous copies of 16 bytes a lane (four rows an instruction), one piece ahead of its work, reads
-// them there at constant offsets, leaves its results in their place and stores those 16 bytes a lane.
+// of 64 or 128 bytes at a time.  Here a warp brings its kEvery rows of each tensor into shared memory by
+// asynchronous copies of 16 bytes a lane (four or eight rows an instruction), one piece ahead of its work,
+// reads them there at constant offsets, leaves its results in their place and stores those 16 bytes a lane.
 // ---------------------------------------------------------------------------------------------
-constexpr int kRowBytes = 128;                          // 64 bf16 or 32 fp32 channels
-constexpr int kBlockBytes = kEvery * kRowBytes;         // one warp's rows of one tensor
-
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
 }
@@ -580,42 +577,50 @@ __device__ __forceinline__ void copies_started() { asm volatile("cp.async.commit
 template <int LEFT>
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// where a lane copies: piece lane & 7 of rows lane >> 3, + 4, + 8, + 12
-template <typename T>
+// a warp's rows of one tensor: 32 lanes of VEC channels each
+template <typename T, int VEC>
 struct Rows {
+  static constexpr int kBytes = 32 * VEC * (int)sizeof(T);   // of a row
+  static constexpr int kPieces = kBytes / 16;                // lanes that copy one row
+  static constexpr int kAtOnce = 32 / kPieces;               // rows of one instruction
+  static constexpr int kBlock = kEvery * kBytes;
+  static constexpr int kEach = 16 / (int)sizeof(T);          // channels of one copy
   const char* base;
   int64_t row;
   __device__ __forceinline__ Rows(const void* p, int64_t batch, int64_t step, int b, int channel)
       : base(static_cast<const char*>(p) + (b * batch + channel) * (int64_t)sizeof(T)), row(step * (int64_t)sizeof(T)) {}
+  // first channel, from the warp's, that this lane copies
+  static __device__ __forceinline__ int channel() { return (int)(threadIdx.x % kPieces) * kEach; }
   // rows t0 .. t0 + kEvery - 1, zeros from row `end` on and where this lane has no channels
   __device__ __forceinline__ void fetch(uint32_t to, int t0, int end, bool live) const {
-    const int lane = threadIdx.x & 31, first = lane >> 3;
+    const int lane = threadIdx.x & 31, first = lane / kPieces;
     const char* from = base + (int64_t)(t0 + first) * row;
-    to += (uint32_t)(first * kRowBytes + (lane & 7) * 16);
+    to += (uint32_t)(first * kBytes + (lane % kPieces) * 16);
 #pragma unroll
-    for (int r = 0; r < kEvery / 4; ++r) {
-      const bool on = live && t0 + first + 4 * r < end;
-      copy16(to + (uint32_t)(r * 4 * kRowBytes), on ? from : base, on);
-      from += 4 * row;
+    for (int r = 0; r < kEvery / kAtOnce; ++r) {
+      const bool on = live && t0 + first + kAtOnce * r < end;
+      copy16(to + (uint32_t)(r * kAtOnce * kBytes), on ? from : base, on);
+      from += kAtOnce * row;
     }
   }
   __device__ __forceinline__ void store(const unsigned char* from, int t0, int end, bool live) const {
-    const int lane = threadIdx.x & 31, first = lane >> 3;
+    const int lane = threadIdx.x & 31, first = lane / kPieces;
     char* to = const_cast<char*>(base) + (int64_t)(t0 + first) * row;
-    from += first * kRowBytes + (lane & 7) * 16;
+    from += first * kBytes + (lane % kPieces) * 16;
 #pragma unroll
-    for (int r = 0; r < kEvery / 4; ++r) {
-      const uint4 v = *reinterpret_cast<const uint4*>(from + r * 4 * kRowBytes);
-      if (live && t0 + first + 4 * r < end) __stcs(reinterpret_cast<uint4*>(to), v);
-      to += 4 * row;
+    for (int r = 0; r < kEvery / kAtOnce; ++r) {
+      const uint4 v = *reinterpret_cast<const uint4*>(from + r * kAtOnce * kBytes);
+      if (live && t0 + first + kAtOnce * r < end) __stcs(reinterpret_cast<uint4*>(to), v);
+      to += kAtOnce * row;
     }
   }
 };
 
-template <typename T, int GATE, bool CUT>
+template <typename T, int VEC, int GATE, bool CUT>
 __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_wide_kernel(const ScanArgs p) {
-  constexpr int VEC = 4 / sizeof(T);
+  using R = Rows<T, VEC>;
+  constexpr int kBlockBytes = R::kBlock, kRowBytes = R::kBytes;
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
   __shared__ __align__(16) Exchange<VEC, CUT, false> ex;
@@ -631,9 +636,9 @@ scan_wide_kernel(const ScanArgs p) {
   // this warp's two stages of (v, f)
   unsigned char* mine = ring + warp * 4 * kBlockBytes;
   const uint32_t mine_at = shared_address(mine);
-  const int cl = c0 + (lane & 7) * (16 / (int)sizeof(T));       // the channels this lane copies
+  const int cl = c0 + R::channel();       // the channels this lane copies
   const bool copies = cl < p.D;
-  const Rows<T> v_rows(p.v, p.v_b, p.v_t, b, copies ? cl : 0), f_rows(p.f, p.f_b, p.f_t, b, copies ? cl : 0),
+  const R v_rows(p.v, p.v_b, p.v_t, b, copies ? cl : 0), f_rows(p.f, p.f_b, p.f_t, b, copies ? cl : 0),
       y_rows(p.y, p.y_b, p.y_t, b, copies ? cl : 0);
   int t0 = (rank * kScanWarps + warp) * kEvery;
   auto fetch = [&](int stage, int t) {
@@ -658,7 +663,7 @@ scan_wide_kernel(const ScanArgs p) {
     }
     __syncwarp();
     unsigned char* at = mine + stage * 2 * kBlockBytes;
-    unsigned char* word = at + lane * 4;
+    unsigned char* word = at + lane * (int)sizeof(Raw);
     float a[kEvery][VEC], in[kEvery][VEC], P[VEC], H[VEC], h[VEC];
     const bool whole = t0 + kEvery <= n;
     auto compose = [&](auto full) {
@@ -712,10 +717,11 @@ scan_wide_kernel(const ScanArgs p) {
     for (int i = 0; i < VEC; ++i) p.h_last[(int64_t)b * p.D + c + i] = ex.state[index & 1][lane][i];
 }
 
-template <typename T, int GATE, bool CUT>
+template <typename T, int VEC, int GATE, bool CUT>
 __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_wide_back_kernel(const ScanArgs p) {
-  constexpr int VEC = 4 / sizeof(T);
+  using R = Rows<T, VEC>;
+  constexpr int kBlockBytes = R::kBlock, kRowBytes = R::kBytes;
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
   __shared__ __align__(16) Exchange<VEC, CUT, true> ex;
@@ -732,10 +738,10 @@ scan_wide_back_kernel(const ScanArgs p) {
   // this warp's two stages of (v, f, dy)
   unsigned char* mine = ring + warp * 6 * kBlockBytes;
   const uint32_t mine_at = shared_address(mine);
-  const int cl = c0 + (lane & 7) * (16 / (int)sizeof(T));
+  const int cl = c0 + R::channel();
   const bool copies = cl < p.D;
   const int cs = copies ? cl : 0;
-  const Rows<T> v_rows(p.v, p.v_b, p.v_t, b, cs), f_rows(p.f, p.f_b, p.f_t, b, cs), d_rows(p.dy ? p.dy : p.v, p.y_b, p.y_t, b, cs),
+  const R v_rows(p.v, p.v_b, p.v_t, b, cs), f_rows(p.f, p.f_b, p.f_t, b, cs), d_rows(p.dy ? p.dy : p.v, p.y_b, p.y_t, b, cs),
       dv_rows(p.dv, p.dv_b, p.dv_t, b, cs), df_rows(p.df, p.df_b, p.df_t, b, cs);
   float next[VEC];                     // the state before this thread's steps of the next piece
   auto fetch = [&](int stage, int t) {
@@ -769,7 +775,7 @@ scan_wide_back_kernel(const ScanArgs p) {
     __syncwarp();
     const bool whole = t0 + kEvery <= n;
     unsigned char* at = mine + stage * 3 * kBlockBytes;
-    unsigned char* word = at + lane * 4;
+    unsigned char* word = at + lane * (int)sizeof(Raw);
     unsigned cuts = 0;
     if (CUT)
 #pragma unroll
@@ -888,12 +894,12 @@ int scan_pieces(const ScanArgs& p) { return ceil_div(p.T, kScanWarps * kEvery); 
 template <typename T, int VEC, int GATE, bool CUT>
 mw_status launch_chunks(const ScanArgs& p, bool backward, bool wide, cudaStream_t s) {
   const int columns = ceil_div(p.D, 32 * VEC);
-  const int C = blocks_along_time((int64_t)columns * p.B, scan_pieces(p), wide);
+  const int C = blocks_along_time((int64_t)columns * p.B, scan_pieces(p), wide && VEC * sizeof(T) == 4);
   void (*kernel)(const ScanArgs) = backward ? scan_chunk_back_kernel<T, VEC, GATE, CUT> : scan_chunk_kernel<T, VEC, GATE, CUT>;
   size_t ring = 0;
   if (wide) {
-    kernel = backward ? scan_wide_back_kernel<T, GATE, CUT> : scan_wide_kernel<T, GATE, CUT>;
-    ring = (size_t)kScanWarps * (backward ? 6 : 4) * kBlockBytes;
+    kernel = backward ? scan_wide_back_kernel<T, VEC, GATE, CUT> : scan_wide_kernel<T, VEC, GATE, CUT>;
+    ring = (size_t)kScanWarps * (backward ? 6 : 4) * Rows<T, VEC>::kBlock;
     MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
   }
   static_assert(kMaxCluster <= 8, "larger clusters are not portable");
@@ -929,7 +935,7 @@ mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
     else scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
     return launch_ok();
   }
-  const bool wide = VEC * e == 4 && (places & 15) == 0;
+  const bool wide = (places & 15) == 0;
   return p.reset ? launch_chunks<T, VEC, GATE, true>(p, backward, wide, s)
                  : launch_chunks<T, VEC, GATE, false>(p, backward, wide, s);
 }

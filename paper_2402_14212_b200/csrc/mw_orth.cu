@@ -1079,9 +1079,7 @@ mw_status orth_launch(OrthParams& prm, size_t smem, cudaStream_t s) {
   prm.bn_x = x128 <= pairs ? kHalf : kTile;
   prm.sym_tiles = tri * (kTile / prm.bn_sym);
   prm.tn = ceil_div(prm.np, prm.bn_x);
-  const int64_t per = (int64_t)prm.count * (2 * (int64_t)prm.sym_tiles + (int64_t)prm.tm * prm.tn);
-  if (per * prm.steps > (1 << 30)) return MW_ERR_UNSUPPORTED;
-  prm.per_step = (int)per;
+  prm.per_step = prm.count * (2 * prm.sym_tiles + prm.tm * prm.tn);       // (mw_orth_create bounds the total)
   prm.total = prm.per_step * prm.steps;
   const int64_t widest = (int64_t)prm.count * (prm.tm * prm.tn > prm.sym_tiles ? prm.tm * prm.tn : prm.sym_tiles);
   cudaLaunchConfig_t cfg = {};
@@ -1263,6 +1261,12 @@ extern "C" mw_status mw_orth_create(const mw_orth_desc* desc, mw_orth** out) {
   if (d.prec != MW_F32 && d.prec != MW_BF16_F32ACC) return MW_ERR_INVALID_ARG;
   for (double c : d.coef)
     if (!isfinite(c)) return MW_ERR_INVALID_ARG;
+  {
+    // tiles of all steps are counted in 32 bits
+    const int64_t m = d.rows < d.cols ? d.rows : d.cols, n = d.rows < d.cols ? d.cols : d.rows;
+    const int64_t tm = (m + kTile - 1) / kTile, tn = (n + kTile - 1) / kTile;
+    if (d.count * (tm * (tm + 1) + tm * tn) * (d.steps ? d.steps : 5) > (1 << 30)) return MW_ERR_UNSUPPORTED;
+  }
   mw_orth* p = new (std::nothrow) mw_orth();
   if (!p) return MW_ERR_CUDA;
   p->d = d;

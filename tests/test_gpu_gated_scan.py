@@ -231,8 +231,9 @@ def test_repeated_calls_and_other_streams_give_the_same_bits():
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
         b = once()
+    c = once(s)                       # tensors of one stream, work on another
     s.synchronize()
-    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert all(torch.equal(p, q) for p, q in zip(a, b)) and all(torch.equal(p, q) for p, q in zip(a, c))
 
 
 @pytest.mark.parametrize("gate", ["complement", "energy"])
@@ -270,7 +271,7 @@ def test_refusals():
                 lambda: mwb.gated_scan(v, v, h0=torch.zeros((2, 8), device="cuda")),
                 lambda: mwb.gated_scan(v, v, lengths=torch.zeros(2, device="cuda")),
                 lambda: mwb.gated_scan(v, v, reset=torch.zeros((2, 7), dtype=torch.uint8, device="cuda")),
-                lambda: mwb.gated_scan(v, v, h0=torch.zeros((2, 16))),
+                lambda: mwb.gated_scan(v, v, h0=torch.zeros((2, 16))), lambda: mwb.gated_scan(v.cpu(), v.cpu()),
                 lambda: mwb.gated_scan_backward(v, v, v, None)):
         with pytest.raises((TypeError, ValueError, mwb.MwError)):
             bad()

@@ -172,7 +172,7 @@ def test_refusals():
     ws = plan.alloc_workspace()
     t = [torch.zeros((8, 8), device="cuda") for _ in range(2)]
     for bad in (lambda: plan.project(t[:1], ws), lambda: plan.project([t[0], t[1].bfloat16()], ws),
-                lambda: plan.project([t[0], t[1][:4]], ws), lambda: plan.project(t, ws[:512]),
+                lambda: plan.project([t[0], t[1][:4]], ws), lambda: plan.project([t[0], t[1].cpu()], ws), lambda: plan.project(t, ws[:512]),
                 lambda: plan.step(t, t, t, ws, lr=float("inf"))):
         with pytest.raises((ValueError, mwb.MwError)):
             bad()

@@ -193,17 +193,18 @@ def test_repeated_calls_and_other_streams_give_the_same_bits():
     x, b, z, wp, sc, wn, dxo, dn = make(1500, 320, "bf16", 5)
     kw = dict(z=z, w_post=wp, scale=sc, w_pre=wn)
 
-    def once():
-        xo, n, rms = mwb.residual_norm(x, b, keep_rms=True, **kw)
-        return (xo, n) + tuple(mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, **kw))
+    def once(stream=None):
+        xo, n, rms = mwb.residual_norm(x, b, keep_rms=True, stream=stream, **kw)
+        return (xo, n) + tuple(mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, stream=stream, **kw))
 
     a = once()
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
         c = once()
+    d = once(s)                       # tensors of one stream, work on another
     s.synchronize()
-    assert all(torch.equal(p, q) for p, q in zip(a, c))
+    assert all(torch.equal(p, q) for p, q in zip(a, c)) and all(torch.equal(p, q) for p, q in zip(a, d))
 
 
 def test_gradients_match_differences():
@@ -239,7 +240,7 @@ def test_refusals():
                 lambda: mwb.residual_norm(x, w_post=w), lambda: mwb.residual_norm(x, x, w_post=w[:3]),
                 lambda: mwb.residual_norm(x, x, w_post=w, eps=0.0), lambda: mwb.residual_norm(x[:, ::2], None, w_pre=w),
                 lambda: mwb.residual_norm(torch.zeros((1, 32769), device="cuda")),
-                lambda: mwb.residual_norm(x, x, w_post=w.cpu()),
+                lambda: mwb.residual_norm(x, x, w_post=w.cpu()), lambda: mwb.residual_norm(x.cpu(), x.cpu()),
                 lambda: mwb.residual_norm_backward(x, x, torch.ones((2, 4), device="cuda"), dn=x)):
         with pytest.raises((TypeError, ValueError, mwb.MwError)):
             bad()
