@@ -53,6 +53,7 @@ namespace {
 
 constexpr int kNormBlocks = 592;      // most partial sums of ||U||^2 per matrix
 constexpr int kPtrGroup = 64;         // matrices of one launch of the small kernels
+constexpr int kTmemColumns = 512;
 constexpr int kTile = 256;            // rows and columns of a pair's tile
 constexpr int kHalf = 128;            // ... of one CTA's share
 constexpr int kBK = 64;
@@ -62,17 +63,21 @@ constexpr int kOrthEpi = 8;
 // registers a thread: the launch gives 384 x 168 = 64512, handed over as 128 x 104 + 256 x 200 = 64512
 constexpr int kFewRegisters = 104, kManyRegisters = 200;
 // K blocks that one accumulator takes of a two-term product.  The tensor core truncates its accumulator at
-// every instruction, which over the 3 x 4 instructions of each block adds up to a bias of about 4e-7 a block
-// on sums of like signs (the diagonals of X X^T and A^2); the epilogue adds the pieces rounding to nearest.
+// every instruction; over 64 K blocks of fp32-accurate products that came to errors of 1e-5 to 1e-4 of X, in
+// pieces of 4 blocks that the epilogue adds, rounding to nearest, to 2e-6 (an accumulator of their own for the
+// cross products changed nothing).  Pieces want accumulators to run ahead into while the epilogue stores a tile:
+// two-term tiles are 128 columns wide, which makes four of them (64 matrices of 1024 x 1024: 6.2 ms; 6.5 ms with two
+// of 256 columns, where the products wait for the epilogue)
 constexpr int kPieceBlocks = 4;
+__host__ __device__ constexpr int set_columns(int terms) { return terms == 1 ? 256 : 128; }
+__host__ __device__ constexpr int set_count(int terms) { return kTmemColumns / set_columns(terms); }
 constexpr int kOrthStagesMax = 4;
 constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;      // one operand plane of one stage and CTA
 constexpr int kPass = 32;                              // columns an epilogue warp takes at a time
 constexpr uint32_t kPassPlane = 32 * kPass * 2;        // one fp16 plane of such a block
 constexpr uint32_t kBuffer = 2 * kPassPlane;
-constexpr int kBuffers = 3;                            // per epilogue warp
-constexpr int kSetColumns = 256;
-constexpr int kTmemColumns = 512;
+// buffers of an epilogue warp: two-term products need the room for their stages more, and have the time
+__host__ __device__ constexpr int staging_buffers(int terms) { return terms == 1 ? 3 : 1; }
 constexpr int kMaxSide = 32768;
 constexpr uint64_t kOrthWaitNs = 2000000000ull;
 
@@ -217,9 +222,10 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[kOrthStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kOrthStagesMax];
-  __shared__ __align__(8) uint64_t acc_full[2];
-  __shared__ __align__(8) uint64_t acc_empty[2];
-  __shared__ __align__(8) uint64_t add_full[kOrthEpi * kBuffers];
+  constexpr int kSets = set_count(TERMS), kSetColumns = set_columns(TERMS);
+  __shared__ __align__(8) uint64_t acc_full[kSets];
+  __shared__ __align__(8) uint64_t acc_empty[kSets];
+  __shared__ __align__(8) uint64_t add_full[kOrthEpi * staging_buffers(TERMS)];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
@@ -233,11 +239,11 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       mbar_init(smem_u32(&full_bar[s]), 1);
       mbar_init(smem_u32(&empty_bar[s]), 1);
     }
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kSets; ++s) {
       mbar_init(smem_u32(&acc_full[s]), 1);
       mbar_init(smem_u32(&acc_empty[s]), kOrthEpi * 2);
     }
-    for (int s = 0; s < kOrthEpi * kBuffers; ++s) mbar_init(smem_u32(&add_full[s]), 1);
+    for (int s = 0; s < kOrthEpi * staging_buffers(TERMS); ++s) mbar_init(smem_u32(&add_full[s]), 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -333,7 +339,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         const uint32_t b_off = TERMS * kPlaneBytes, b_plane = (uint32_t)(w.bn >> 1) * (kBK * 2);
         const int piece = p.piece_blocks ? p.piece_blocks : w.nkb;
         for (int kb0 = 0; kb0 < w.nkb && ok; kb0 += piece, ++j) {
-          const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
+          const uint32_t set = (uint32_t)j % kSets, aphase = ((uint32_t)j / kSets) & 1u;
           if (!mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d = tmem_base + set * (uint32_t)kSetColumns;
@@ -370,12 +376,14 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
     }
   } else if (warp >= kOrthFirstEpi) {
     // ---------------- epilogue ----------------
-    // A tensor-memory lane quarter and one half of the tile's columns each, taken kPass columns at a time.  The
-    // copy engine brings a block's addend (both planes of X, or A) into one of the warp's three buffers, each
-    // lane replaces its row by the result, and the engine takes it away again.  Addends are fetched ahead: of
-    // X's four passes three before the sum is there and the fourth once the first's result has been read; of
-    // A's two, then one pass ahead (the third buffer is for transposed blocks).
+    // A tensor-memory lane quarter and one half of the tile's columns each, taken kPass columns at a time (sixteen
+    // warps with a quarter each measured a fifth slower).  The
+    // copy engine brings a block's addend (both planes of X, or A) into one of the warp's buffers, each lane
+    // replaces its row by the result, and the engine takes it away again.  With three buffers (one term) addends
+    // are fetched ahead: of X's four passes three before the sum is there and the fourth once the first's
+    // result has been read; of A's two, then one pass ahead, the third buffer being for transposed blocks.
     const int ew = warp - kOrthFirstEpi, quarter = warp & 3, side = ew >> 2;
+    constexpr int kBuffers = staging_buffers(TERMS);
     const uint32_t sbuf = tiles + (uint32_t)p.stages * p.stage_bytes + (uint32_t)ew * (kBuffers * kBuffer);
     const uint32_t add_bar = smem_u32(&add_full[ew * kBuffers]);
     uint32_t add_phase = 0;              // a bit per buffer
@@ -418,16 +426,16 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       if (epilogue_any(!ok || failed)) break;
       if (lane == 0 && addends) {
         asm volatile("fence.proxy.async;" ::: "memory");
-        const int ahead = w.phase == 2 ? 3 : 2;
+        const int ahead = TERMS == 2 ? 1 : (w.phase == 2 ? 3 : 2);
         for (int k = 0; k < ahead && k * kPass < cols; ++k) fetch(from, (uint32_t)k, n0 + k * kPass, row0, plane0, addends);
       }
       // Two terms: the pieces of the sum meet in registers, and each accumulator goes straight back.
       // One term: a pass reads its columns from the one accumulator, which goes back after the last.
-      float acc[TERMS == 2 ? 4 : 1][32];
+      float acc[TERMS == 2 ? 2 : 1][32];
       uint32_t t0 = 0, set = 0;
       auto await_sum = [&]() {
-        set = (uint32_t)j & 1u;
-        const uint32_t aphase = ((uint32_t)j >> 1) & 1u;
+        set = (uint32_t)j % kSets;
+        const uint32_t aphase = ((uint32_t)j / kSets) & 1u;
         ++j;
         ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
         tc_fence_after();
@@ -445,7 +453,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
         if (ok) await_sum();
       } else {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
           for (int i = 0; i < 32; ++i) acc[TERMS == 2 ? c : 0][i] = 0.f;
 #pragma unroll 1
@@ -453,14 +461,12 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
           await_sum();
           if (!ok) break;
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            if (c * 16 < cols) {
-              uint32_t r[16];
-              tmem_ld16_issue(t0 + (uint32_t)(c * 16), r);
-              tmem_ld_wait();
+          for (int c = 0; c < 2; ++c) {
+            uint32_t r[32];
+            tmem_ld32_issue(t0 + (uint32_t)(c * 32), r);
+            tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) acc[TERMS == 2 ? c / 2 : 0][c % 2 * 16 + i] += __uint_as_float(r[i]);
-            }
+            for (int i = 0; i < 32; ++i) acc[TERMS == 2 ? c : 0][i] += __uint_as_float(r[i]);
           }
           give_back();
         }
@@ -471,13 +477,20 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
       const int planes = w.phase == 2 ? 2 : TERMS;
       const bool mirror = w.phase < 2 && w.ti != w.tj;
       // (unrolled for two terms, whose sums sit in registers)
-#pragma unroll(TERMS == 2 ? 4 : 1)
-      for (int k = 0; k < 4; ++k) {
+#pragma unroll(TERMS == 2 ? 2 : 1)
+      for (int k = 0; k < (TERMS == 2 ? 2 : 4); ++k) {
         const int c0 = k * kPass;
         if (c0 < cols && ok) {
           const int col = n0 + c0;
-          const uint32_t buffer = w.phase == 2 ? (uint32_t)k % 3u : (uint32_t)k & 1u, at = sbuf + buffer * kBuffer;
-          if (k > 0 && (w.phase < 2 || k == 1)) {
+          const uint32_t buffer = TERMS == 2 ? 0u : (w.phase == 2 ? (uint32_t)k % 3u : (uint32_t)k & 1u);
+          const uint32_t at = sbuf + buffer * kBuffer;
+          if (TERMS == 2) {
+            if (lane == 0 && k > 0) {
+              bulk_wait_read_all();
+              if (addends) fetch(from, 0u, col, row0, plane0, addends);
+            }
+            __syncwarp();
+          } else if (k > 0 && (w.phase < 2 || k == 1)) {
             if (lane == 0) {
               bulk_wait_read_all();
               if (w.phase == 2 && 3 * kPass < cols) fetch(from, 0u, n0 + 3 * kPass, row0, plane0, addends);
@@ -539,12 +552,33 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
                   v[8 * q + 2 * i + 1] -= f.y;
                 }
                 st_shared_v4(at + (uint32_t)t * kPassPlane + piece_at((uint32_t)lane, q), pk[0], pk[1], pk[2], pk[3]);
-                if (mirror) store_turned(sbuf + 2u * kBuffer + (uint32_t)t * kPassPlane, 8u * q, pk);
+                if (TERMS == 1 && mirror) store_turned(sbuf + 2u * kBuffer, 8u * q, pk);
               }
             }
           }
           hand_over(to, at, col, row0, plane0);
-          if (mirror) hand_over(to, sbuf + 2u * kBuffer, row0, col, plane0);
+          if (TERMS == 2 && mirror) {
+            // the rows are read back, and turned in their place once the engine has them
+            uint32_t pk[2][kPass / 2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (uint32_t q = 0; q < kPass / 8; ++q)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(pk[t][4 * q]), "=r"(pk[t][4 * q + 1]), "=r"(pk[t][4 * q + 2]), "=r"(pk[t][4 * q + 3])
+                             : "r"(at + (uint32_t)t * kPassPlane + piece_at((uint32_t)lane, q))
+                             : "memory");
+            if (lane == 0) bulk_wait_read_all();
+            __syncwarp();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (uint32_t q = 0; q < kPass / 8; ++q) {
+                const uint32_t four[4] = {pk[t][4 * q], pk[t][4 * q + 1], pk[t][4 * q + 2], pk[t][4 * q + 3]};
+                store_turned(at + (uint32_t)t * kPassPlane, 8u * q, four);
+              }
+          }
+          if (mirror) hand_over(to, TERMS == 2 ? at : sbuf + 2u * kBuffer, row0, col, plane0);
         }
       }
       // one count for the whole CTA, once all its stores have been written (a release a warp would be eight
@@ -1075,8 +1109,8 @@ mw_status orth_launch(OrthParams& prm, size_t smem, cudaStream_t s) {
   // with 128 columns, 257 us with 256; 16 of them, whose tiles do not fit: 487 us with 256)
   const int tri = prm.tm * (prm.tm + 1) / 2;
   const int64_t sym = (int64_t)prm.count * tri, x128 = (int64_t)prm.count * prm.tm * ceil_div(prm.np, kHalf);
-  prm.bn_sym = 2 * sym <= pairs ? kHalf : kTile;
-  prm.bn_x = x128 <= pairs ? kHalf : kTile;
+  prm.bn_sym = TERMS == 2 || 2 * sym <= pairs ? kHalf : kTile;
+  prm.bn_x = TERMS == 2 || x128 <= pairs ? kHalf : kTile;
   prm.sym_tiles = tri * (kTile / prm.bn_sym);
   prm.tn = ceil_div(prm.np, prm.bn_x);
   prm.per_step = prm.count * (2 * prm.sym_tiles + prm.tm * prm.tn);       // (mw_orth_create bounds the total)
@@ -1212,9 +1246,9 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.done = l.done;
   q.st = reinterpret_cast<DeviceStatus*>(ws);
   q.wait_ns = kOrthWaitNs;
-  q.stage_bytes = 2u * (uint32_t)p->terms * kPlaneBytes;
-  q.stages = p->terms == 1 ? 4 : 2;
-  const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * kBuffers * kBuffer;
+  q.stage_bytes = (uint32_t)p->terms * (kPlaneBytes + (uint32_t)set_columns(p->terms) / 2u * kBK * 2u);
+  q.stages = 4;
+  const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * staging_buffers(p->terms) * kBuffer;
   MW_TRY(p->terms == 1 ? orth_launch<1>(q, smem, s) : orth_launch<2>(q, smem, s));
   for (int first = 0; first < count; first += kPtrGroup) {
     const int c = count - first < kPtrGroup ? count - first : kPtrGroup;
