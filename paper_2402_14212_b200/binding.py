@@ -531,13 +531,18 @@ def _raw_stream(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
-def _used_on(stream, *tensors):
-    """Tensors made here on the current stream, used on `stream`: the allocator must not hand their memory
-    out again before the work there is done."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _on_stream(stream, like, call, *args):
+    """call(*args) on `stream`.  What it allocates comes from that stream's memory, whose earlier uses lie
+    before the call there, and what it hands back is kept until the caller's stream is done with it too."""
+    import torch
+    _need(stream.device == like.device, f"{call.__name__}: a stream of {like.device}, not of {stream.device}")
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    here = torch.cuda.current_stream(like.device)
+    for t in out:
+        if t is not None:
+            t.record_stream(here)
+    return out
 
 
 def _dense_like(t):
@@ -581,6 +586,8 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
     with keep_states=True (y, h_last, states) for gated_scan_backward.  One step (length 1) with
     h0 = h_last = the cached state is the serving form."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, v, gated_scan, v, f, reset, lengths, h0, input_gate, keep_states, y, h_last)
     key = ("scan", input_gate, keep_states, _layout(v), _layout(f), _layout(y), _layout(reset), _layout(lengths),
            _layout(h0), _layout(h_last))
     d = _passed.get(key)
@@ -600,9 +607,8 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
     if keep_states:
         states = torch.empty((B, -(-T // SCAN_STATE_EVERY), D), dtype=torch.float32, device=v.device)
     _check(lib().mw_gated_scan_forward(d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), _ptr(h0),
-                                       y.data_ptr(), h_last.data_ptr(), _ptr(states), _raw_stream(stream, v.device)),
+                                       y.data_ptr(), h_last.data_ptr(), _ptr(states), _raw_stream(None, v.device)),
            "mw_gated_scan_forward")
-    _used_on(stream, y, h_last, states)
     return (y, h_last, states) if keep_states else (y, h_last)
 
 
@@ -611,6 +617,8 @@ def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_
     """(dv, df, dh0) of gated_scan from the cotangents of y and h_last (either may be None) and the
     states that the forward call kept (they include h0, which is accepted for symmetry)."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, v, gated_scan_backward, v, f, dy, states, reset, lengths, h0, dh_last, input_gate, dv, df)
     key = ("scan backward", input_gate, _layout(v), _layout(f), _layout(dy), _layout(states), _layout(reset),
            _layout(lengths), _layout(dh_last), _layout(dv), _layout(df))
     d = _passed.get(key)
@@ -629,8 +637,7 @@ def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_
     dh0 = torch.empty_like(dh_last) if dh_last is not None else torch.empty((B, D), dtype=torch.float32, device=v.device)
     _check(lib().mw_gated_scan_backward(d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), states.data_ptr(),
                                         _ptr(dy), _ptr(dh_last), dv.data_ptr(), df.data_ptr(), dh0.data_ptr(),
-                                        _raw_stream(stream, v.device)), "mw_gated_scan_backward")
-    _used_on(stream, dv, df, dh0)
+                                        _raw_stream(None, v.device)), "mw_gated_scan_backward")
     return dv, df, dh0
 
 
@@ -660,6 +667,8 @@ def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: f
     """x' = x + scale silu(z) rmsnorm(b; w_post) and n = rmsnorm(x'; w_pre) on [rows, cols] tensors; what
     is None is left out.  Returns (x', n), with keep_rms=True (x', n, inv_rms) for the backward call."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, x, residual_norm, x, b, z, w_post, scale, w_pre, eps, keep_rms, x_out, n)
     key = ("norm", eps, _layout(x), _layout(b), _layout(z), _layout(w_post), _layout(scale), _layout(w_pre),
            _layout(x_out), _layout(n))
     d = _passed.get(key)
@@ -672,9 +681,8 @@ def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: f
         d = _remember(key, _norm_call(x, b, z, w_post, scale, w_pre, eps, {"x_out": x_out, "n": n}))
     rms = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device) if keep_rms else None
     _check(lib().mw_residual_norm_forward(d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre),
-                                          x_out.data_ptr(), _ptr(n), _ptr(rms), _raw_stream(stream, x.device)),
+                                          x_out.data_ptr(), _ptr(n), _ptr(rms), _raw_stream(None, x.device)),
            "mw_residual_norm_forward")
-    _used_on(stream, x_out, n, rms)
     return (x_out, n, rms) if keep_rms else (x_out, n)
 
 
@@ -692,6 +700,8 @@ def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre
     """Gradients of residual_norm from the cotangents of x' and n (either may be None); the gradients of
     what was left out are None."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, x, residual_norm_backward, x, b, inv_rms, z, w_post, scale, w_pre, eps, dx_out, dn)
     key = ("norm backward", eps, _layout(x), _layout(b), _layout(inv_rms), _layout(z), _layout(w_post),
            _layout(scale), _layout(w_pre), _layout(dx_out), _layout(dn))
     known = _passed.get(key)
@@ -708,8 +718,7 @@ def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre
     _check(lib().mw_residual_norm_backward(
         d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre), inv_rms.data_ptr(), _ptr(dx_out),
         _ptr(dn), g.dx.data_ptr(), _ptr(g.db), _ptr(g.dz), _ptr(g.dw_post), _ptr(g.dscale), _ptr(g.dw_pre),
-        scratch.data_ptr(), need, _raw_stream(stream, x.device)), "mw_residual_norm_backward")
-    _used_on(stream, scratch, *g)
+        scratch.data_ptr(), need, _raw_stream(None, x.device)), "mw_residual_norm_backward")
     return g
 
 
@@ -777,10 +786,11 @@ class Orth:
     def project(self, mats, workspace, out=None, stream=None):
         """The orthogonalised factor X of every matrix, in the storage type."""
         import torch
+        if stream is not None and out is None:
+            return _on_stream(stream, workspace, self.project, mats, workspace)
         st = self.storage_dtype()
         if out is None:
             out = [torch.empty_like(t) for t in mats]
-            _used_on(stream, *out)
         wp, wb = Net._ws(workspace)
         _check(lib().mw_orth_project(self._h, self._list(mats, st, "mats", workspace), self._list(out, st, "out", workspace), wp, wb,
                                      _raw_stream(stream, workspace.device)), "mw_orth_project")

@@ -58,7 +58,12 @@ __device__ __forceinline__ int length_of(const ScanArgs& p, int b) {
   return n < 0 ? 0 : (n < p.T ? n : p.T);
 }
 
-// one thread per channel walks the whole sequence
+// One thread per channel walks the whole sequence: the single steps of serving, short sequences, and rows so far
+// apart that the kernels below cannot address them.  Bound by latency: the rows of kAhead steps are asked for before
+// the first is used (eight wanted more registers than the waits were worth).
+// One step of 64x2048 bf16 takes 2 us, 256x16x2048 12 us forward and 26 backward (50 and 75 MB).
+constexpr int kAhead = 4;
+
 template <typename T, int GATE>
 __global__ void __launch_bounds__(128)
 scan_walk_kernel(const ScanArgs p) {
@@ -71,23 +76,39 @@ scan_walk_kernel(const ScanArgs p) {
   const int64_t bc = (int64_t)b * p.D + c;
   float h = p.h0 ? p.h0[bc] : 0.f;
   const int64_t nst = (p.T + kEvery - 1) / kEvery;
-  for (int t = 0; t < p.T; ++t) {
-    if (p.states && t % kEvery == 0) p.states[(b * nst + t / kEvery) * p.D + c] = h;
-    float out = 0.f;
-    if (t < n) {
-      float a, w;
-      gate_of(to_f32(f[t * p.f_t]), a, w);
-      const float u = input_of<GATE>(a, w);
-      const bool cut = p.reset && p.reset[(int64_t)b * p.T + t];
-      h = cut ? u * to_f32(v[t * p.v_t]) : fmaf(a, h, u * to_f32(v[t * p.v_t]));
-      out = h;
+  auto step = [&](int t, float vt, float ft, bool cut) {
+    float a, w;
+    gate_of(ft, a, w);
+    const float in = input_of<GATE>(a, w) * vt;
+    h = cut ? in : fmaf(a, h, in);
+    y[t * p.y_t] = from_f32<T>(h);
+  };
+  static_assert(kEvery % kAhead == 0, "a kept state stands at the start of a stretch");
+  int t = 0;
+  for (; t + kAhead <= n; t += kAhead) {
+    float vs[kAhead], fs[kAhead];
+    bool cut[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      fs[j] = to_f32(f[(t + j) * p.f_t]);
+      vs[j] = to_f32(v[(t + j) * p.v_t]);
+      cut[j] = p.reset && p.reset[(int64_t)b * p.T + t + j];
     }
-    y[t * p.y_t] = from_f32<T>(out);
+    if (p.states && t % kEvery == 0) p.states[(b * nst + t / kEvery) * p.D + c] = h;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) step(t + j, vs[j], fs[j], cut[j]);
+  }
+#pragma unroll 1
+  for (; t < p.T; ++t) {
+    if (p.states && t % kEvery == 0) p.states[(b * nst + t / kEvery) * p.D + c] = h;
+    if (t < n) step(t, to_f32(v[t * p.v_t]), to_f32(f[t * p.f_t]), p.reset && p.reset[(int64_t)b * p.T + t]);
+    else y[t * p.y_t] = from_f32<T>(0.f);
   }
   if (p.h_last) p.h_last[bc] = h;
 }
 
-template <typename T, int GATE>
+// WHOLE: some stretches between kept states are whole (without them the kernel needs half the registers)
+template <typename T, int GATE, bool WHOLE>
 __global__ void __launch_bounds__(128)
 scan_walk_back_kernel(const ScanArgs p) {
   const int c = blockIdx.x * 128 + threadIdx.x, b = blockIdx.y;
@@ -103,8 +124,47 @@ scan_walk_back_kernel(const ScanArgs p) {
   float g = p.dh_last ? p.dh_last[bc] : 0.f;       // cotangent of the state after the current step
   for (int i = (int)nst - 1; i >= 0; --i) {
     const int t0 = i * kEvery, len = min(kEvery, p.T - t0);
-    float before[kEvery];
     float h = p.states_in[(b * nst + i) * p.D + c];
+    if (WHOLE && t0 + kEvery <= n) {
+      float w[kEvery], k[kEvery];                   // 1 - a and df / g of each step
+      unsigned cuts = 0;
+#pragma unroll
+      for (int q = 0; q < kEvery; q += kAhead) {
+        float vs[kAhead], fs[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int t = t0 + q + j;
+          fs[j] = to_f32(f[t * p.f_t]);
+          vs[j] = to_f32(v[t * p.v_t]);
+          if (p.reset && p.reset[(int64_t)b * p.T + t]) cuts |= 1u << (q + j);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          float a;
+          gate_of(fs[j], a, w[q + j]);
+          const float before = (cuts >> (q + j)) & 1u ? 0.f : h;
+          k[q + j] = fmaf(a * w[q + j], before, input_slope<GATE>(a, w[q + j]) * vs[j]);
+          h = fmaf(a, before, input_of<GATE>(a, w[q + j]) * vs[j]);
+        }
+      }
+#pragma unroll
+      for (int q = kEvery - kAhead; q >= 0; q -= kAhead) {
+        float ds[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) ds[j] = dy ? to_f32(dy[(t0 + q + j) * p.y_t]) : 0.f;
+#pragma unroll
+        for (int j = kAhead - 1; j >= 0; --j) {
+          const int t = t0 + q + j;
+          const float a = 1.f - w[q + j];
+          g += ds[j];
+          dv[t * p.dv_t] = from_f32<T>(input_of<GATE>(a, w[q + j]) * g);
+          df[t * p.df_t] = from_f32<T>(k[q + j] * g);
+          g = (cuts >> (q + j)) & 1u ? 0.f : a * g;
+        }
+      }
+      continue;
+    }
+    float before[kEvery];
     for (int j = 0; j < len; ++j) {
       const int t = t0 + j;
       const bool cut = p.reset && p.reset[(int64_t)b * p.T + t];
@@ -146,6 +206,7 @@ scan_walk_back_kernel(const ScanArgs p) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kScanWarps = 8;
 constexpr int kMaxCluster = 8;
+constexpr int64_t kFewBlocks = 148;      // one block an SM
 
 // what one lane of a row holds: VEC channels of type T
 template <typename T, int VEC>
@@ -578,12 +639,12 @@ template <int LEFT>
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // a warp's rows of one tensor: 32 lanes of VEC channels each
-template <typename T, int VEC>
+template <typename T, int VEC, int STEPS>
 struct Rows {
   static constexpr int kBytes = 32 * VEC * (int)sizeof(T);   // of a row
   static constexpr int kPieces = kBytes / 16;                // lanes that copy one row
   static constexpr int kAtOnce = 32 / kPieces;               // rows of one instruction
-  static constexpr int kBlock = kEvery * kBytes;
+  static constexpr int kBlock = STEPS * kBytes;
   static constexpr int kEach = 16 / (int)sizeof(T);          // channels of one copy
   const char* base;
   int64_t row;
@@ -597,7 +658,7 @@ struct Rows {
     const char* from = base + (int64_t)(t0 + first) * row;
     to += (uint32_t)(first * kBytes + (lane % kPieces) * 16);
 #pragma unroll
-    for (int r = 0; r < kEvery / kAtOnce; ++r) {
+    for (int r = 0; r < STEPS / kAtOnce; ++r) {
       const bool on = live && t0 + first + kAtOnce * r < end;
       copy16(to + (uint32_t)(r * kAtOnce * kBytes), on ? from : base, on);
       from += kAtOnce * row;
@@ -608,7 +669,7 @@ struct Rows {
     char* to = const_cast<char*>(base) + (int64_t)(t0 + first) * row;
     from += first * kBytes + (lane % kPieces) * 16;
 #pragma unroll
-    for (int r = 0; r < kEvery / kAtOnce; ++r) {
+    for (int r = 0; r < STEPS / kAtOnce; ++r) {
       const uint4 v = *reinterpret_cast<const uint4*>(from + r * kAtOnce * kBytes);
       if (live && t0 + first + kAtOnce * r < end) __stcs(reinterpret_cast<uint4*>(to), v);
       to += kAtOnce * row;
@@ -616,10 +677,10 @@ struct Rows {
   }
 };
 
-template <typename T, int VEC, int GATE, bool CUT>
+template <typename T, int VEC, int GATE, bool CUT, int STEPS>
 __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_wide_kernel(const ScanArgs p) {
-  using R = Rows<T, VEC>;
+  using R = Rows<T, VEC, STEPS>;
   constexpr int kBlockBytes = R::kBlock, kRowBytes = R::kBytes;
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
@@ -631,7 +692,7 @@ scan_wide_kernel(const ScanArgs p) {
   const bool live = c < p.D;
   const int cc = live ? c : 0;
   const int n = length_of(p, b);
-  const int piece = C * kScanWarps * kEvery;
+  const int piece = C * kScanWarps * STEPS;
   const int64_t nst = (p.T + kEvery - 1) / kEvery;
   // this warp's two stages of (v, f)
   unsigned char* mine = ring + warp * 4 * kBlockBytes;
@@ -640,7 +701,7 @@ scan_wide_kernel(const ScanArgs p) {
   const bool copies = cl < p.D;
   const R v_rows(p.v, p.v_b, p.v_t, b, copies ? cl : 0), f_rows(p.f, p.f_b, p.f_t, b, copies ? cl : 0),
       y_rows(p.y, p.y_b, p.y_t, b, copies ? cl : 0);
-  int t0 = (rank * kScanWarps + warp) * kEvery;
+  int t0 = (rank * kScanWarps + warp) * STEPS;
   auto fetch = [&](int stage, int t) {
     v_rows.fetch(mine_at + (uint32_t)(stage * 2 * kBlockBytes), t, n, copies);
     f_rows.fetch(mine_at + (uint32_t)(stage * 2 * kBlockBytes + kBlockBytes), t, n, copies);
@@ -664,11 +725,11 @@ scan_wide_kernel(const ScanArgs p) {
     __syncwarp();
     unsigned char* at = mine + stage * 2 * kBlockBytes;
     unsigned char* word = at + lane * (int)sizeof(Raw);
-    float a[kEvery][VEC], in[kEvery][VEC], P[VEC], H[VEC], h[VEC];
-    const bool whole = t0 + kEvery <= n;
+    float a[STEPS][VEC], in[STEPS][VEC], P[VEC], H[VEC], h[VEC];
+    const bool whole = t0 + STEPS <= n;
     auto compose = [&](auto full) {
 #pragma unroll
-      for (int j = 0; j < kEvery; ++j) {
+      for (int j = 0; j < STEPS; ++j) {
         float v[VEC], f[VEC];
         L::get(*reinterpret_cast<const Raw*>(word + j * kRowBytes), v);
         L::get(*reinterpret_cast<const Raw*>(word + kBlockBytes + j * kRowBytes), f);
@@ -689,15 +750,15 @@ scan_wide_kernel(const ScanArgs p) {
     if (whole) compose(Flag<true>()); else compose(Flag<false>());
     ex.run(P, H, h, index, rank, C);
     if (t0 < p.T) {
-      if (p.states && live) {
-        float* st = p.states + (b * nst + t0 / kEvery) * p.D + c;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) st[i] = h[i];
-      }
       auto emit = [&](auto full) {
 #pragma unroll
-        for (int j = 0; j < kEvery; ++j) {
+        for (int j = 0; j < STEPS; ++j) {
           float o[VEC];
+          if (j % kEvery == 0 && p.states && live && t0 + j < p.T) {
+            float* st = p.states + (b * nst + (t0 + j) / kEvery) * p.D + c;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) st[i] = h[i];
+          }
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             h[i] = affine<CUT>(a[j][i], h[i], in[j][i]);
@@ -717,10 +778,11 @@ scan_wide_kernel(const ScanArgs p) {
     for (int i = 0; i < VEC; ++i) p.h_last[(int64_t)b * p.D + c + i] = ex.state[index & 1][lane][i];
 }
 
-template <typename T, int VEC, int GATE, bool CUT>
+template <typename T, int GATE, bool CUT, int STEPS>
 __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_wide_back_kernel(const ScanArgs p) {
-  using R = Rows<T, VEC>;
+  constexpr int VEC = 1;               // (two channels' w and k would leave 16 steps between exchanges)
+  using R = Rows<T, VEC, STEPS>;
   constexpr int kBlockBytes = R::kBlock, kRowBytes = R::kBytes;
   using L = Lane<T, VEC>;
   using Raw = typename L::Raw;
@@ -732,7 +794,7 @@ scan_wide_back_kernel(const ScanArgs p) {
   const bool live = c < p.D;
   const int cc = live ? c : 0;
   const int n = length_of(p, b);
-  const int piece = C * kScanWarps * kEvery;
+  const int piece = C * kScanWarps * STEPS;
   const int64_t nst = (p.T + kEvery - 1) / kEvery;
   const int pieces = (p.T + piece - 1) / piece;
   // this warp's two stages of (v, f, dy)
@@ -753,7 +815,7 @@ scan_wide_back_kernel(const ScanArgs p) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) next[i] = t < p.T ? p.states_in[(b * nst + t / kEvery) * p.D + cc + i] : 0.f;
   };
-  int t0 = (pieces - 1) * piece + (rank * kScanWarps + warp) * kEvery;
+  int t0 = (pieces - 1) * piece + (rank * kScanWarps + warp) * STEPS;
   fetch(0, t0);
   float carry[VEC];
 #pragma unroll
@@ -773,18 +835,18 @@ scan_wide_back_kernel(const ScanArgs p) {
       copies_done<0>();
     }
     __syncwarp();
-    const bool whole = t0 + kEvery <= n;
+    const bool whole = t0 + STEPS <= n;
     unsigned char* at = mine + stage * 3 * kBlockBytes;
     unsigned char* word = at + lane * (int)sizeof(Raw);
     unsigned cuts = 0;
     if (CUT)
 #pragma unroll
-      for (int j = 0; j < kEvery; ++j)
+      for (int j = 0; j < STEPS; ++j)
         if (t0 + j < n && p.reset[(int64_t)b * p.T + t0 + j] != 0) cuts |= 1u << j;
-    float w[kEvery][VEC], k[kEvery][VEC];
+    float w[STEPS][VEC], k[STEPS][VEC];
     auto compose = [&](auto full) {
 #pragma unroll
-      for (int j = 0; j < kEvery; ++j) {
+      for (int j = 0; j < STEPS; ++j) {
         float v[VEC], f[VEC];
         L::get(*reinterpret_cast<const Raw*>(word + j * kRowBytes), v);
         L::get(*reinterpret_cast<const Raw*>(word + kBlockBytes + j * kRowBytes), f);
@@ -800,15 +862,15 @@ scan_wide_back_kernel(const ScanArgs p) {
         }
       }
 #pragma unroll
-      for (int j = kEvery - 1; j >= 0; --j) {
+      for (int j = STEPS - 1; j >= 0; --j) {
         float d[VEC];
         L::get(*reinterpret_cast<const Raw*>(word + 2 * kBlockBytes + j * kRowBytes), d);
         const bool cut = CUT && ((cuts >> j) & 1u);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
           const float a = 1.f - w[j][i];
-          P[i] = j == kEvery - 1 ? a : P[i] * a;
-          E[i] = j == kEvery - 1 ? a * d[i] : a * (E[i] + d[i]);
+          P[i] = j == STEPS - 1 ? a : P[i] * a;
+          E[i] = j == STEPS - 1 ? a * d[i] : a * (E[i] + d[i]);
           if (cut) P[i] = E[i] = 0.f;
         }
       }
@@ -818,7 +880,7 @@ scan_wide_back_kernel(const ScanArgs p) {
     if (t0 < p.T) {
       auto emit = [&](auto full) {
 #pragma unroll
-        for (int j = kEvery - 1; j >= 0; --j) {
+        for (int j = STEPS - 1; j >= 0; --j) {
           float d[VEC], ov[VEC], of[VEC];
           L::get(*reinterpret_cast<const Raw*>(word + 2 * kBlockBytes + j * kRowBytes), d);
           const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
@@ -878,39 +940,27 @@ mw_status fill_scan(const mw_gated_scan_desc* d, ScanArgs& p) {
   return MW_OK;
 }
 
-// Blocks along time, doubled while the grid would fill less than two thirds of the SMs (all of them for the
-// kernels without copies, which have more latency for a second block an SM to hide), as far as there are
-// pieces for them.  Each doubling costs an exchange a piece: 8x2048x2048 bf16 (256 columns) takes 42 us with
-// one block along time and 53 us with two; 1x65536x1024 (16 columns) 868, 592, 318, 210, 237 us with 1 to 16.
-int blocks_along_time(int64_t columns, int pieces, bool wide) {
-  const int64_t enough = wide ? 96 : 148;
+// Blocks along time: doubled while the grid leaves SMs without one, as far as there are pieces of the sequence
+// for them.  Each doubling costs an exchange a piece: 8x2048x2048 bf16 (256 columns of blocks) takes 41 us with one
+// block along time and 51 us with two, 1x65536x1024 (32 of them) 484, 295, 156, 121 us with 1, 2, 4, 8.
+int blocks_along_time(int64_t columns, int pieces) {
   int C = 1;
-  while (C < kMaxCluster && C < pieces && columns * C < enough) C *= 2;
+  while (C < kMaxCluster && C < pieces && columns * C < kFewBlocks) C *= 2;
   return C;
 }
-int scan_pieces(const ScanArgs& p) { return ceil_div(p.T, kScanWarps * kEvery); }
 
-// `wide`: every row of every tensor starts on a 16-byte boundary
-template <typename T, int VEC, int GATE, bool CUT>
-mw_status launch_chunks(const ScanArgs& p, bool backward, bool wide, cudaStream_t s) {
-  const int columns = ceil_div(p.D, 32 * VEC);
-  const int C = blocks_along_time((int64_t)columns * p.B, scan_pieces(p), wide && VEC * sizeof(T) == 4);
-  void (*kernel)(const ScanArgs) = backward ? scan_chunk_back_kernel<T, VEC, GATE, CUT> : scan_chunk_kernel<T, VEC, GATE, CUT>;
-  size_t ring = 0;
-  if (wide) {
-    kernel = backward ? scan_wide_back_kernel<T, VEC, GATE, CUT> : scan_wide_kernel<T, VEC, GATE, CUT>;
-    ring = (size_t)kScanWarps * (backward ? 6 : 4) * Rows<T, VEC>::kBlock;
-    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
-  }
+template <int STEPS>
+mw_status launch_clusters(void (*kernel)(const ScanArgs), const ScanArgs& p, int columns, size_t ring, cudaStream_t s) {
   static_assert(kMaxCluster <= 8, "larger clusters are not portable");
+  if (ring) MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)C, (unsigned)columns, (unsigned)p.B);
+  cfg.gridDim = dim3((unsigned)blocks_along_time((int64_t)columns * p.B, ceil_div(p.T, kScanWarps * STEPS)), (unsigned)columns, (unsigned)p.B);
   cfg.blockDim = dim3(32 * kScanWarps);
   cfg.dynamicSmemBytes = ring;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)C;
+  attr[0].val.clusterDim.x = cfg.gridDim.x;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
@@ -918,44 +968,84 @@ mw_status launch_chunks(const ScanArgs& p, bool backward, bool wide, cudaStream_
   return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
 }
 
-template <typename T, int VEC, int GATE>
-mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
-  // what every row's place is a multiple of, in bytes
-  const int64_t e = sizeof(T), d = p.D * e;
-  const int64_t steps = p.v_t | p.f_t | p.y_t | p.dv_t | p.df_t;
-  const int64_t places = (p.v_b | p.f_b | p.y_b | p.dv_b | p.df_b | steps) * e | d |
-                         (int64_t)((uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df);
-  // up to kEvery steps there is nothing to cut: a thread a channel (the chunk kernels also hold the offsets
-  // of kEvery rows in 32 bits, which only rows more than 2^26 bytes apart do not fit)
-  const int64_t most = (int64_t)1 << 26;
-  const bool near = p.v_t * e < most && p.f_t * e < most && p.y_t * e < most && p.dv_t * e < most && p.df_t * e < most;
-  if (p.T <= kEvery || !near) {
-    const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
-    if (backward) scan_walk_back_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
-    else scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
-    return launch_ok();
-  }
-  const bool wide = (places & 15) == 0;
-  return p.reset ? launch_chunks<T, VEC, GATE, true>(p, backward, wide, s)
-                 : launch_chunks<T, VEC, GATE, false>(p, backward, wide, s);
+template <typename T, int VEC, int GATE, bool CUT>
+mw_status launch_chunks(const ScanArgs& p, bool backward, cudaStream_t s) {
+  return launch_clusters<kEvery>(backward ? scan_chunk_back_kernel<T, VEC, GATE, CUT> : scan_chunk_kernel<T, VEC, GATE, CUT>,
+                                 p, ceil_div(p.D, 32 * VEC), 0, s);
+}
+template <typename T, int VEC, int GATE, bool CUT, int STEPS>
+mw_status launch_wide(const ScanArgs& p, cudaStream_t s) {
+  return launch_clusters<STEPS>(scan_wide_kernel<T, VEC, GATE, CUT, STEPS>, p, ceil_div(p.D, 32 * VEC),
+                                (size_t)kScanWarps * 4 * Rows<T, VEC, STEPS>::kBlock, s);
+}
+template <typename T, int GATE, bool CUT, int STEPS>
+mw_status launch_wide_back(const ScanArgs& p, cudaStream_t s) {
+  return launch_clusters<STEPS>(scan_wide_back_kernel<T, GATE, CUT, STEPS>, p, ceil_div(p.D, 32),
+                                (size_t)kScanWarps * 6 * Rows<T, 1, STEPS>::kBlock, s);
 }
 
-template <typename T, int VEC>
+// `wide`: every row of every tensor starts on a 16-byte boundary; `pairs`: on a 4-byte one.
+//   - Where one exchange covers the sequence there is nothing to copy ahead of, and copies only add their latency:
+//     direct loads (64x128x2048 bf16, forward and backward: 25 and 37 us; 26 and 55 with copies).  Two bf16 channels a
+//     lane if that still gives every SM a block (25 us; one channel 36; but 1x512x1024 5.0 us, one channel 4.4).
+//   - Longer ones copy ahead (2x8192x1024 f32 backward 61 us, direct loads 71; forward 40 and 38).
+//   - bf16 then takes one channel a lane and uses the registers for twice the steps between two exchanges (1x65536x1024
+//     forward 111 us; 136 with 16 steps, 200 with two channels; backward 194, 206, above 300) ...
+//   - ... except forward with more columns than the device holds blocks at once, which gains more from half the
+//     instructions (8x2048x2048 42 us with two channels, 46 with one; 4x4096x2048, with half the columns, 51 and 46;
+//     backward 80 and 79).
+template <typename T, int GATE, bool CUT>
+mw_status cut_scan(const ScanArgs& p, bool backward, bool wide, bool pairs, cudaStream_t s) {
+  constexpr bool kNarrow = sizeof(T) == 2;       // bf16: two channels a lane are possible
+  const int pieces = ceil_div(p.T, kScanWarps * kEvery);
+  const int64_t columns = (int64_t)ceil_div(p.D, kNarrow ? 64 : 32) * p.B;
+  const int C = blocks_along_time(columns, pieces);
+  if (!wide || pieces <= C) {
+    if constexpr (kNarrow)
+      if (pairs && columns * C >= kFewBlocks) return launch_chunks<T, 2, GATE, CUT>(p, backward, s);
+    return launch_chunks<T, 1, GATE, CUT>(p, backward, s);
+  }
+  if constexpr (kNarrow) {
+    if (backward) return launch_wide_back<T, GATE, CUT, 2 * kEvery>(p, s);
+    return columns < kFewBlocks * 3 / 2 ? launch_wide<T, 1, GATE, CUT, 2 * kEvery>(p, s) : launch_wide<T, 2, GATE, CUT, kEvery>(p, s);
+  } else {
+    return backward ? launch_wide_back<T, GATE, CUT, kEvery>(p, s) : launch_wide<T, 1, GATE, CUT, kEvery>(p, s);
+  }
+}
+
+template <typename T, int GATE>
+mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
+  // what every row's place is a multiple of, in bytes
+  const int64_t e = sizeof(T);
+  const int64_t places = (p.D | p.v_b | p.v_t | p.f_b | p.f_t | p.y_b | p.y_t | p.dv_b | p.dv_t | p.df_b | p.df_t) * e |
+                         (int64_t)((uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df);
+  // A thread a channel where there is nothing to cut, up to kEvery steps, and up to four times as many where the
+  // channels alone give every SM four blocks (64x64x2048 bf16 forward 15 us, backward 26, 20 and 27 in chunks;
+  // 256x32x2048 25 and 49, 72 and 106; but 8x64x2048 13 and 11, 4 and 5 in chunks).
+  // The chunk kernels also hold the offsets of kEvery rows in 32 bits, which only rows more than 2^26 bytes
+  // apart do not fit.
+  const int64_t most = (int64_t)1 << 26;
+  const bool near = p.v_t * e < most && p.f_t * e < most && p.y_t * e < most && p.dv_t * e < most && p.df_t * e < most;
+  const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
+  const int shortest = (int64_t)grid.x * grid.y >= 4 * kFewBlocks ? 4 * kEvery : kEvery;
+  if (p.T <= shortest || !near) {
+    if (!backward) scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
+    else if (p.T >= kEvery) scan_walk_back_kernel<T, GATE, true><<<grid, 128, 0, s>>>(p);
+    else scan_walk_back_kernel<T, GATE, false><<<grid, 128, 0, s>>>(p);
+    return launch_ok();
+  }
+  const bool wide = (places & 15) == 0, pairs = (places & 3) == 0;
+  return p.reset ? cut_scan<T, GATE, true>(p, backward, wide, pairs, s) : cut_scan<T, GATE, false>(p, backward, wide, pairs, s);
+}
+
+template <typename T>
 mw_status gate_scan(const mw_gated_scan_desc* d, const ScanArgs& p, bool backward, cudaStream_t s) {
-  return d->input_gate == MW_SCAN_COMPLEMENT ? run_scan<T, VEC, MW_SCAN_COMPLEMENT>(p, backward, s)
-                                             : run_scan<T, VEC, MW_SCAN_ENERGY>(p, backward, s);
+  return d->input_gate == MW_SCAN_COMPLEMENT ? run_scan<T, MW_SCAN_COMPLEMENT>(p, backward, s)
+                                             : run_scan<T, MW_SCAN_ENERGY>(p, backward, s);
 }
 
 mw_status dispatch_scan(const mw_gated_scan_desc* d, const ScanArgs& p, bool backward, cudaStream_t s) {
-  if (d->dtype == 1) return gate_scan<float, 1>(d, p, backward, s);
-  // two bf16 channels a lane where every row of every tensor starts on a 4-byte boundary; one all the same
-  // where there are so few columns that even four blocks along time leave SMs idle (1x65536x1024: 210 us with
-  // two channels a lane, 162 us with one, whose twice as many blocks hide each other's exchanges)
-  const int64_t odd = p.D | p.v_b | p.v_t | p.f_b | p.f_t | p.y_b | p.y_t | p.dv_b | p.dv_t | p.df_b | p.df_t;
-  const uintptr_t at = (uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df;
-  const bool few = blocks_along_time((int64_t)ceil_div(p.D, 64) * p.B, scan_pieces(p), true) >= 4;
-  return (odd & 1) == 0 && (at & 3) == 0 && !few ? gate_scan<__nv_bfloat16, 2>(d, p, backward, s)
-                                         : gate_scan<__nv_bfloat16, 1>(d, p, backward, s);
+  return d->dtype == 1 ? gate_scan<float>(d, p, backward, s) : gate_scan<__nv_bfloat16>(d, p, backward, s);
 }
 
 }  // namespace

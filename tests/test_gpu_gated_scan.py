@@ -119,6 +119,17 @@ def test_forward_and_backward_match_the_recurrence(size, dtype, gate, ragged):
     check(got, ref, V, dtype)
 
 
+# more sequences than SMs, a length of several rounds for one block of 128 (16 steps a thread) or 256; 66 columns
+# leave rows off the 16-byte boundaries
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(230, 150, 64), (230, 300, 8), (230, 140, 66), (80, 520, 64), (40, 700, 40)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("gate,ragged", [("complement", True), ("energy", False)])
+def test_many_sequences(size, dtype, gate, ragged):
+    got, ref, V = run_both(*size, dtype, gate, ragged, seed=sum(size))
+    check(got, ref, V, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [1, 2, 8])
 def test_windows_of_wider_rows(dtype, pad):
@@ -178,11 +189,12 @@ def test_nan_stays_in_its_channel_and_after_its_step():
     assert torch.equal(y[~bad], clean[~bad])
 
 
-@pytest.mark.parametrize("T", [12, 400])
-def test_a_reset_keeps_out_what_came_before(T):
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [12, 400, 3000])
+def test_a_reset_keeps_out_what_came_before(T, dtype):
     # NaN and infinities before a reset do not reach the steps after it, nor cotangents the steps before
     import torch
-    v, f, dy, h0, _, _, _ = make(1, T, 64, "f32", 12)
+    v, f, dy, h0, _, _, _ = make(1, T, 64, dtype, 12)
     at = T // 2
     reset = torch.zeros((1, T), dtype=torch.uint8, device="cuda")
     reset[0, at] = 1
@@ -234,6 +246,28 @@ def test_repeated_calls_and_other_streams_give_the_same_bits():
     c = once(s)                       # tensors of one stream, work on another
     s.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(a, b)) and all(torch.equal(p, q) for p, q in zip(a, c))
+
+
+def test_work_on_another_stream_does_not_meet_freed_memory():
+    # a tensor freed while the current stream still has to write it: its memory must not become the output of a
+    # call on another stream, which does not wait for that write
+    import torch
+    v, f, dy, h0, dh, reset, lengths = make(2, 700, 192, "bf16", 6, ragged=True)
+    kw = dict(reset=reset, lengths=lengths, h0=h0)
+    y, hl, st = mwb.gated_scan(v, f, keep_states=True, **kw)
+    dv, df, dh0 = mwb.gated_scan_backward(v, f, dy, st, dh_last=dh, reset=reset, lengths=lengths)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    old = [torch.empty_like(t) for t in (y, hl, st, dv, df)]
+    torch.cuda._sleep(20_000_000)
+    for t in old:
+        t.fill_(7.0)
+    del old, t
+    y2, hl2, st2 = mwb.gated_scan(v, f, keep_states=True, stream=s, **kw)
+    grads = mwb.gated_scan_backward(v, f, dy, st2, dh_last=dh, reset=reset, lengths=lengths, stream=s)
+    torch.cuda.synchronize()
+    for a, b in zip((y, hl, st, dv, df, dh0), (y2, hl2, st2) + grads):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("gate", ["complement", "energy"])

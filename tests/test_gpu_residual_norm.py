@@ -207,6 +207,28 @@ def test_repeated_calls_and_other_streams_give_the_same_bits():
     assert all(torch.equal(p, q) for p, q in zip(a, c)) and all(torch.equal(p, q) for p, q in zip(a, d))
 
 
+def test_work_on_another_stream_does_not_meet_freed_memory():
+    # a tensor freed while the current stream still has to write it: its memory must not become the output of a
+    # call on another stream, which does not wait for that write
+    import torch
+    x, b, z, wp, sc, wn, dxo, dn = make(1500, 320, "bf16", 5)
+    kw = dict(z=z, w_post=wp, scale=sc, w_pre=wn)
+    xo, n, rms = mwb.residual_norm(x, b, keep_rms=True, **kw)
+    g = mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, **kw)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    old = [torch.empty_like(t) for t in (xo, n, rms) + tuple(g)]
+    torch.cuda._sleep(20_000_000)
+    for t in old:
+        t.fill_(7.0)
+    del old, t
+    xo2, n2, rms2 = mwb.residual_norm(x, b, keep_rms=True, stream=s, **kw)
+    g2 = mwb.residual_norm_backward(x, b, rms2, dx_out=dxo, dn=dn, stream=s, **kw)
+    torch.cuda.synchronize()
+    for p, q in zip((xo, n, rms) + tuple(g), (xo2, n2, rms2) + tuple(g2)):
+        assert torch.equal(p, q)
+
+
 def test_gradients_match_differences():
     # directional derivatives of sum(dx_out x') + sum(dn n) in 64 bits; central differences of step 1e-4 are
     # good to 1e-6 of the terms they sum, the fp32 gradients to 2e-5 of them
