@@ -2,6 +2,7 @@
 //   a = sigmoid(f),  u = 1 - a or sqrt(1 - a^2),  h_t = r_t a_t h_{t-1} + u_t v_t
 // backward, with g_t the whole cotangent of h_t:
 //   g_t = dy_t + r_{t+1} a_{t+1} g_{t+1},  dv = u g,  df = a (1 - a) g (r h_{t-1} + u'(a) v)
+#include "mw_cluster.cuh"
 #include "mw_common.cuh"
 
 namespace mw {
@@ -238,40 +239,6 @@ struct Lane<__nv_bfloat16, 2> {
     return *reinterpret_cast<const uint32_t*>(&h);
   }
 };
-
-// all threads of all blocks of the cluster
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint32_t in_rank(uint32_t address, int rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
-  return r;
-}
-// Waits for one phase of a barrier of this block.  The senders are blocks of the same cluster, which run at
-// the same time; should a phase not complete in two seconds all the same, the wait ends and says so.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity) {
-  uint64_t t0 = 0;
-  for (uint32_t i = 0;; ++i) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    if (ok) return true;
-    if ((i & 255u) == 255u) {
-      uint64_t now;
-      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-      if (t0 == 0) t0 = now;
-      else if (now - t0 > 2000000000ull) return false;
-    }
-  }
-}
 
 // h -> P h + H.  With CUT a zero P drops h whatever it is: infinities and NaN of what came before a
 // reset do not reach the steps after it.

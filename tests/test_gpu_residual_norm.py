@@ -128,7 +128,8 @@ def run_and_check(R, D, dtype, have="bzpsn", pad=0, seed=0, eps=1e-6):
 
 
 SIZES = [(1, 1), (1, 8), (3, 2), (2, 33), (5, 64), (7, 100), (4, 512), (3, 513), (9, 1000), (300, 1024), (2, 1111),
-         (33, 2048), (5, 4096), (3, 5000), (700, 264), (2, 8192), (2, 16384), (1, 20001), (2, 32768)]
+         (33, 2048), (5, 4096), (3, 5000), (700, 264), (2, 8192), (2, 16384), (1, 20001), (2, 32768),
+         (3000, 16), (1500, 72), (400, 96), (200, 8200), (170, 5003), (60, 16392), (40, 32760)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
