@@ -6,6 +6,7 @@
   python -m paper_2402_14212_b200.profile_cases conv --images 512 --op 1 --terms 2
   python -m paper_2402_14212_b200.profile_cases sconv --images 16 --op 0 --terms 3
   python -m paper_2402_14212_b200.profile_cases step --workload sweep_mlp --depth 4 --no-coop
+  python -m paper_2402_14212_b200.profile_cases sequence --no-coop --reps 1
 
 Each case allocates its seeded inputs, runs the kernel `--reps` times and exits.
 """
@@ -20,7 +21,7 @@ def main():
     import torch
     from . import binding as mwb
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "pack", "fragments", "vijp", "conv", "sconv", "step"])
+    ap.add_argument("case", choices=["gemm", "pack", "fragments", "vijp", "conv", "sconv", "step", "sequence"])
     ap.add_argument("--workload", default="sweep_mlp", help="step: a workload of paper_2402_14212_b200.synth")
     ap.add_argument("--depth", type=int, default=4)
     ap.add_argument("--no-coop", action="store_true",
@@ -41,6 +42,27 @@ def main():
     g = torch.Generator(device="cuda").manual_seed(0)
     if a.no_pair:
         mwb.set_pair_mode(False)
+    if a.case == "sequence":
+        # the recurrence, the residual norm and the orthogonalised update at sizes above L2
+        if a.no_coop:
+            mwb.set_cooperative_launch(False)
+        rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda")
+        v, f, dy = (rand(8, 2048, 2048).bfloat16() for _ in range(3))
+        x, b, z, dxo, dn = (rand(16384, 4096).bfloat16() for _ in range(5))
+        w = torch.ones(4096, device="cuda")
+        plans = [(mwb.Orth(n, n, c, p), c, n) for n, c, p in ((64, 4, "f32"), (1024, 8, "f32"), (2048, 4, "bf16_f32acc"))]
+        mats = [[rand(n, n).to(p.storage_dtype()) for _ in range(c)] for p, c, n in plans]
+        wss = [p.alloc_workspace() for p, _, _ in plans]
+        for _ in range(a.reps):
+            _, _, st = mwb.gated_scan(v, f, keep_states=True)
+            mwb.gated_scan_backward(v, f, dy, st)
+            kw = dict(z=z, w_post=w, scale=w, w_pre=w)
+            _, _, rms = mwb.residual_norm(x, b, keep_rms=True, **kw)
+            mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, **kw)
+            for (p, _, _), m, ws in zip(plans, mats, wss):
+                p.project(m, ws)
+        torch.cuda.synchronize()
+        return
     if a.case == "step":
         # warm steps, then `reps` whole Moonwalk steps of a synthetic workload (launch lists)
         from . import synth as S
