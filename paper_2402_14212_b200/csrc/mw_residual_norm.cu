@@ -751,9 +751,9 @@ extern "C" mw_status mw_residual_norm_scratch_bytes(const mw_residual_norm_desc*
   using namespace mw;
   if (!desc || !bytes || desc->rows < 0 || desc->cols < 1) return MW_ERR_INVALID_ARG;
   if (desc->cols > kMaxCols) return MW_ERR_UNSUPPORTED;
-  // (rows that can be taken 16 bytes at a time leave as many partial sums as others, or not: room for either)
-  const int narrow = backward_parts(desc->rows, desc->cols, 1), wide = backward_parts(desc->rows, desc->cols, desc->dtype == 1 ? 4 : 8);
-  *bytes = (size_t)(narrow > wide ? narrow : wide) * 2 * (size_t)desc->cols * sizeof(float);
+  // a partial sum a block: at most one a row, and two blocks an SM
+  const int64_t most = 2 * (int64_t)norm_sms();
+  *bytes = (size_t)(desc->rows < most ? desc->rows : most) * 2 * (size_t)desc->cols * sizeof(float);
   return MW_OK;
 }
 
