@@ -551,6 +551,17 @@ def _dense_like(t):
     return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
+def _repeats(t) -> bool:
+    """Whether elements of t share memory by a stride of zero, as expanded tensors' do."""
+    return t is not None and any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape))
+
+
+def _own_memory(*tensors):
+    """Each tensor, or a dense copy where it repeats elements: the library wants rows apart, and reads a stride of
+    zero as the dense one."""
+    return tuple(t.contiguous() if _repeats(t) else t for t in tensors)
+
+
 def _scan_call(v, f, reset, lengths, input_gate, named):
     """Checks of the tensors every scan call shares; `named` {name: [B, T, D] tensor like v or None}."""
     import torch
@@ -566,6 +577,7 @@ def _scan_call(v, f, reset, lengths, input_gate, named):
             continue
         _need(t.dtype == v.dtype and tuple(t.shape) == (B, T, D), f"gated_scan: {name} has the type and shape of v")
         _need(D <= 1 or t.stride(2) == 1 or t.numel() == 0, f"gated_scan: {name}'s channels are contiguous")
+        _need(not _repeats(t), f"gated_scan: {name} is written, and repeats elements")      # (inputs are copied before)
         if t.numel():
             setattr(d, field + "_batch", t.stride(0) if B > 1 else T * D)
             setattr(d, field + "_time", t.stride(1) if T > 1 else D)
@@ -582,9 +594,9 @@ def _scan_call(v, f, reset, lengths, input_gate, named):
 def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "complement", keep_states=False,
                y=None, h_last=None, stream=None):
     """Gated linear recurrence h_t = r_t sigmoid(f_t) h_{t-1} + u_t v_t over dim 1 of [batch, length,
-    channels] tensors (float32 or bfloat16; rows may be windows of wider ones).  Returns (y, h_last),
-    with keep_states=True (y, h_last, states) for gated_scan_backward.  One step (length 1) with
-    h0 = h_last = the cached state is the serving form."""
+    channels] tensors (float32 or bfloat16; rows may be windows of wider ones; expanded ones are copied first).
+    Returns (y, h_last), with keep_states=True (y, h_last, states) for gated_scan_backward.  One step
+    (length 1) with h0 = h_last = the cached state is the serving form."""
     import torch
     if stream is not None:
         return _on_stream(stream, v, gated_scan, v, f, reset, lengths, h0, input_gate, keep_states, y, h_last)
@@ -592,6 +604,8 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
            _layout(h0), _layout(h_last))
     d = _passed.get(key)
     fresh = d is None
+    if fresh and (_repeats(v) or _repeats(f)):
+        return gated_scan(*_own_memory(v, f), reset, lengths, h0, input_gate, keep_states, y, h_last)
     if y is None:
         y = _dense_like(v)
     if fresh:
@@ -615,7 +629,8 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
 def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_last=None,
                         input_gate: str = "complement", dv=None, df=None, stream=None):
     """(dv, df, dh0) of gated_scan from the cotangents of y and h_last (either may be None) and the
-    states that the forward call kept (they include h0, which is accepted for symmetry)."""
+    states that the forward call kept (they include h0, which is accepted for symmetry).  Gradients of expanded
+    inputs come element by element, as if the inputs had been dense."""
     import torch
     if stream is not None:
         return _on_stream(stream, v, gated_scan_backward, v, f, dy, states, reset, lengths, h0, dh_last, input_gate, dv, df)
@@ -623,6 +638,8 @@ def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_
            _layout(lengths), _layout(dh_last), _layout(dv), _layout(df))
     d = _passed.get(key)
     fresh = d is None
+    if fresh and (_repeats(v) or _repeats(f) or _repeats(dy)):
+        return gated_scan_backward(*_own_memory(v, f, dy), states, reset, lengths, h0, dh_last, input_gate, dv, df)
     if dv is None:
         dv = _dense_like(v)
     if df is None:
@@ -651,6 +668,7 @@ def _norm_call(x, b, z, w_post, scale, w_pre, eps, dense):
             continue
         _need(t.dtype == x.dtype and tuple(t.shape) == (R, D), f"residual_norm: {name} has the type and shape of x")
         _need(D <= 1 or t.stride(1) == 1 or t.numel() == 0, f"residual_norm: {name}'s columns are contiguous")
+        _need(not _repeats(t), f"residual_norm: {name} repeats elements")       # (copied before)
         setattr(d, "ld_" + name, t.stride(0) if R > 1 and t.numel() else D)
     for name, t in dense.items():
         if t is not None:
@@ -665,7 +683,8 @@ def _norm_call(x, b, z, w_post, scale, w_pre, eps, dense):
 def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: float = 1e-6, keep_rms=False,
                   x_out=None, n=None, stream=None):
     """x' = x + scale silu(z) rmsnorm(b; w_post) and n = rmsnorm(x'; w_pre) on [rows, cols] tensors; what
-    is None is left out.  Returns (x', n), with keep_rms=True (x', n, inv_rms) for the backward call."""
+    is None is left out (expanded x, b, z are copied first).  Returns (x', n), with keep_rms=True (x', n, inv_rms)
+    for the backward call."""
     import torch
     if stream is not None:
         return _on_stream(stream, x, residual_norm, x, b, z, w_post, scale, w_pre, eps, keep_rms, x_out, n)
@@ -673,6 +692,9 @@ def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: f
            _layout(x_out), _layout(n))
     d = _passed.get(key)
     fresh = d is None
+    if fresh and (_repeats(x) or _repeats(b) or _repeats(z)):
+        x, b, z = _own_memory(x, b, z)
+        return residual_norm(x, b, z, w_post, scale, w_pre, eps, keep_rms, x_out, n)
     if x_out is None:
         x_out = _dense_like(x)
     if n is None and w_pre is not None:
@@ -698,13 +720,16 @@ class ResidualNormGrads(NamedTuple):
 def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre=None, eps: float = 1e-6,
                            dx_out=None, dn=None, stream=None) -> ResidualNormGrads:
     """Gradients of residual_norm from the cotangents of x' and n (either may be None); the gradients of
-    what was left out are None."""
+    what was left out are None, those of expanded inputs as if they had been dense."""
     import torch
     if stream is not None:
         return _on_stream(stream, x, residual_norm_backward, x, b, inv_rms, z, w_post, scale, w_pre, eps, dx_out, dn)
     key = ("norm backward", eps, _layout(x), _layout(b), _layout(inv_rms), _layout(z), _layout(w_post),
            _layout(scale), _layout(w_pre), _layout(dx_out), _layout(dn))
     known = _passed.get(key)
+    if known is None and (_repeats(x) or _repeats(b) or _repeats(z)):
+        x, b, z = _own_memory(x, b, z)
+        return residual_norm_backward(x, b, inv_rms, z, w_post, scale, w_pre, eps, dx_out, dn)
     if known is None:
         d = _norm_call(x, b, z, w_post, scale, w_pre, eps, {"dx_out": dx_out, "dn": dn})
         _need(inv_rms is not None, "residual_norm_backward: inv_rms comes from residual_norm(..., keep_rms=True)")

@@ -1,0 +1,133 @@
+"""What the sequence-block bindings hand to the library, seen without a GPU: CPU tensors stand in for CUDA ones,
+and a recorder stands in for the library."""
+import pytest
+import torch
+
+from paper_2402_14212_b200 import binding as mwb
+
+
+class OnDevice(torch.Tensor):
+    """A CPU tensor that calls itself a CUDA one."""
+    is_cuda = True
+
+
+def on_device(t):
+    return t.as_subclass(OnDevice)
+
+
+class Recorder:
+    """Takes the place of the loaded library: every call succeeds and is remembered."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return mwb.MW_OK
+        return call
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    rec = Recorder()
+    monkeypatch.setattr(mwb, "lib", lambda: rec)
+    monkeypatch.setattr(mwb, "_raw_stream", lambda stream, device: 0)
+    monkeypatch.setattr(mwb, "_passed", {})
+    # bytes from the address of a tensor that was asked for it to the end of its memory
+    rec.room = {}
+    plain = torch.Tensor.data_ptr
+
+    def data_ptr(t):
+        p = plain(t)
+        if t.numel():
+            s = t.untyped_storage()
+            rec.room[p] = s.data_ptr() + s.nbytes() - p
+        return p
+
+    monkeypatch.setattr(torch.Tensor, "data_ptr", data_ptr)
+    return rec
+
+
+def scan_reach(d, which):
+    """Bytes from a tensor's first element to the end of the last that the library touches."""
+    b, t = getattr(d, which + "_batch"), getattr(d, which + "_time")
+    if b == 0 and t == 0:              # the library's sign for dense
+        t = d.channels
+        b = t * d.length
+    return ((d.batch - 1) * b + (d.length - 1) * t + d.channels) * (4 if d.dtype == 1 else 2)
+
+
+def norm_reach(d, which):
+    ld = getattr(d, "ld_" + which) or d.cols
+    return ((d.rows - 1) * ld + d.cols) * (4 if d.dtype == 1 else 2)
+
+
+B, T, D, R = 3, 40, 16, 24
+EXPANDED = {"all": lambda: torch.randn(1, 1, D).expand(B, T, D), "time": lambda: torch.randn(B, 1, D).expand(B, T, D),
+            "batch": lambda: torch.randn(1, T, D).expand(B, T, D), "scalar": lambda: torch.randn(()).expand(B, T, D)}
+
+
+@pytest.mark.parametrize("how", sorted(EXPANDED))
+@pytest.mark.parametrize("which", ["v", "f", "dy"])
+def test_scan_reads_expanded_inputs_inside_their_memory(recorder, which, how):
+    dense = {k: on_device(torch.randn(B, T, D)) for k in ("v", "f", "dy")}
+    dense[which] = on_device(EXPANDED[how]())
+    want = dense[which].clone()
+    v, f, dy = dense["v"], dense["f"], dense["dy"]
+    y, _, states = mwb.gated_scan(v, f, keep_states=True)
+    mwb.gated_scan_backward(v, f, dy, states)
+    for name, args in recorder.calls:
+        d = args[0]
+        places = {"v": args[1], "f": args[2]}
+        if name.endswith("backward"):
+            places["y"], places["dv"], places["df"] = args[6], args[8], args[9]
+        else:
+            places["y"] = args[6]
+        for field, at in places.items():
+            assert scan_reach(d, field) <= recorder.room[at], (name, field)
+    assert y.shape == (B, T, D) and torch.equal(dense[which], want)
+
+
+def test_scan_reads_the_cotangent_of_a_sum(recorder):
+    # the cotangent that y.sum() hands back, of one channel too
+    for shape in ((B, T, D), (B, T, 1)):
+        recorder.calls.clear()
+        v = on_device(torch.randn(shape))
+        dy = on_device(torch.ones(()).expand(shape))
+        _, _, states = mwb.gated_scan(v, v, keep_states=True)
+        mwb.gated_scan_backward(v, v, dy, states)
+        name, args = recorder.calls[-1]
+        assert name == "mw_gated_scan_backward" and scan_reach(args[0], "y") <= recorder.room[args[6]]
+
+
+def test_scan_refuses_outputs_that_repeat_elements(recorder):
+    v = on_device(torch.randn(B, T, D))
+    _, _, states = mwb.gated_scan(v, v, keep_states=True)
+    n = len(recorder.calls)
+    for how in EXPANDED.values():
+        out = on_device(how())
+        with pytest.raises(ValueError):
+            mwb.gated_scan(v, v, y=out)
+        with pytest.raises(ValueError):
+            mwb.gated_scan_backward(v, v, v, states, dv=out)
+        with pytest.raises(ValueError):
+            mwb.gated_scan_backward(v, v, v, states, df=out)
+    assert len(recorder.calls) == n
+
+
+@pytest.mark.parametrize("which", ["x", "b", "z"])
+def test_norm_reads_expanded_inputs_inside_their_memory(recorder, which):
+    t = {k: on_device(torch.randn(R, D)) for k in ("x", "b", "z")}
+    t[which] = on_device(torch.randn(1, D).expand(R, D))
+    w = on_device(torch.ones(D))
+    _, _, rms = mwb.residual_norm(t["x"], t["b"], z=t["z"], w_post=w, w_pre=w, keep_rms=True)
+    g = on_device(torch.randn(R, D))
+    mwb.residual_norm_backward(t["x"], t["b"], rms, z=t["z"], w_post=w, w_pre=w, dx_out=g, dn=g)
+    checked = 0
+    for name, args in recorder.calls:
+        if name.endswith(("forward", "backward")):
+            for field, at in zip("xbz", args[1:4]):
+                assert norm_reach(args[0], field) <= recorder.room[at], (name, field)
+                checked += 1
+    assert checked == 6
