@@ -531,6 +531,18 @@ def _raw_stream(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _call(name, device, *args, stream=None) -> int:
+    """A library call with `device` current, on `stream` or the device's current stream: the library launches, and
+    asks for the number of SMs, on the current device.  Returns its status."""
+    import torch
+    _need(stream is None or stream.device == device, f"{name}: a stream of {device}")
+    handle = _raw_stream(stream, device)
+    if torch.cuda.current_device() == device.index:
+        return getattr(lib(), name)(*args, handle)
+    with torch.cuda.device(device):
+        return getattr(lib(), name)(*args, handle)
+
+
 def _on_stream(stream, like, call, *args):
     """call(*args) on `stream`.  What it allocates comes from that stream's memory, whose earlier uses lie
     before the call there, and what it hands back is kept until the caller's stream is done with it too."""
@@ -620,9 +632,8 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
     states = None
     if keep_states:
         states = torch.empty((B, -(-T // SCAN_STATE_EVERY), D), dtype=torch.float32, device=v.device)
-    _check(lib().mw_gated_scan_forward(d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), _ptr(h0),
-                                       y.data_ptr(), h_last.data_ptr(), _ptr(states), _raw_stream(None, v.device)),
-           "mw_gated_scan_forward")
+    _check(_call("mw_gated_scan_forward", v.device, d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), _ptr(h0),
+                 y.data_ptr(), h_last.data_ptr(), _ptr(states)), "mw_gated_scan_forward")
     return (y, h_last, states) if keep_states else (y, h_last)
 
 
@@ -652,9 +663,9 @@ def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_
         _check_float(states, (B, -(-T // SCAN_STATE_EVERY), D), "gated_scan_backward: states", v.device)
         _remember(key, d)
     dh0 = torch.empty_like(dh_last) if dh_last is not None else torch.empty((B, D), dtype=torch.float32, device=v.device)
-    _check(lib().mw_gated_scan_backward(d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths), states.data_ptr(),
-                                        _ptr(dy), _ptr(dh_last), dv.data_ptr(), df.data_ptr(), dh0.data_ptr(),
-                                        _raw_stream(None, v.device)), "mw_gated_scan_backward")
+    _check(_call("mw_gated_scan_backward", v.device, d, v.data_ptr(), f.data_ptr(), _ptr(reset), _ptr(lengths),
+                 states.data_ptr(), _ptr(dy), _ptr(dh_last), dv.data_ptr(), df.data_ptr(), dh0.data_ptr()),
+           "mw_gated_scan_backward")
     return dv, df, dh0
 
 
@@ -702,9 +713,8 @@ def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: f
     if fresh:
         d = _remember(key, _norm_call(x, b, z, w_post, scale, w_pre, eps, {"x_out": x_out, "n": n}))
     rms = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device) if keep_rms else None
-    _check(lib().mw_residual_norm_forward(d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre),
-                                          x_out.data_ptr(), _ptr(n), _ptr(rms), _raw_stream(None, x.device)),
-           "mw_residual_norm_forward")
+    _check(_call("mw_residual_norm_forward", x.device, d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale),
+                 _ptr(w_pre), x_out.data_ptr(), _ptr(n), _ptr(rms)), "mw_residual_norm_forward")
     return (x_out, n, rms) if keep_rms else (x_out, n)
 
 
@@ -735,15 +745,16 @@ def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre
         _need(inv_rms is not None, "residual_norm_backward: inv_rms comes from residual_norm(..., keep_rms=True)")
         _check_float(inv_rms, (2, x.shape[0]), "residual_norm_backward: inv_rms", x.device)
         need = C.c_size_t()
-        _check(lib().mw_residual_norm_scratch_bytes(d, need), "mw_residual_norm_scratch_bytes")
+        with torch.cuda.device(x.device):          # (a partial sum a block, and blocks go by the device's SMs)
+            _check(lib().mw_residual_norm_scratch_bytes(d, need), "mw_residual_norm_scratch_bytes")
         known = _remember(key, (d, int(need.value)))
     d, need = known
     g = ResidualNormGrads(*(None if t is None else _dense_like(t) for t in (x, b, z, w_post, scale, w_pre)))
     scratch = torch.empty(need, dtype=torch.uint8, device=x.device)
-    _check(lib().mw_residual_norm_backward(
-        d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre), inv_rms.data_ptr(), _ptr(dx_out),
-        _ptr(dn), g.dx.data_ptr(), _ptr(g.db), _ptr(g.dz), _ptr(g.dw_post), _ptr(g.dscale), _ptr(g.dw_pre),
-        scratch.data_ptr(), need, _raw_stream(None, x.device)), "mw_residual_norm_backward")
+    _check(_call(
+        "mw_residual_norm_backward", x.device, d, x.data_ptr(), _ptr(b), _ptr(z), _ptr(w_post), _ptr(scale), _ptr(w_pre),
+        inv_rms.data_ptr(), _ptr(dx_out), _ptr(dn), g.dx.data_ptr(), _ptr(g.db), _ptr(g.dz), _ptr(g.dw_post),
+        _ptr(g.dscale), _ptr(g.dw_pre), scratch.data_ptr(), need), "mw_residual_norm_backward")
     return g
 
 
@@ -801,11 +812,12 @@ class Orth:
         momentum_out = momentum if momentum_out is None else momentum_out
         st, f32 = self.storage_dtype(), torch.float32
         wp, wb = Net._ws(workspace)
-        _check(lib().mw_orth_step(
-            self._h, self._list(params, st, "params", workspace), self._list(grads, f32, "grads", workspace),
+        _check(_call(
+            "mw_orth_step", workspace.device, self._h, self._list(params, st, "params", workspace),
+            self._list(grads, f32, "grads", workspace),
             self._list(momentum, f32, "momentum", workspace), self._list(params_out, st, "params_out", workspace),
             self._list(momentum_out, f32, "momentum_out", workspace), float(lr), float(beta), float(weight_decay), float(scale),
-            wp, wb, _raw_stream(stream, workspace.device)), "mw_orth_step")
+            wp, wb, stream=stream), "mw_orth_step")
         return params_out
 
     def project(self, mats, workspace, out=None, stream=None):
@@ -817,14 +829,14 @@ class Orth:
         if out is None:
             out = [torch.empty_like(t) for t in mats]
         wp, wb = Net._ws(workspace)
-        _check(lib().mw_orth_project(self._h, self._list(mats, st, "mats", workspace), self._list(out, st, "out", workspace), wp, wb,
-                                     _raw_stream(stream, workspace.device)), "mw_orth_project")
+        _check(_call("mw_orth_project", workspace.device, self._h, self._list(mats, st, "mats", workspace),
+                     self._list(out, st, "out", workspace), wp, wb, stream=stream), "mw_orth_project")
         return out
 
     def status(self, workspace, stream=None) -> int:
         """Waits for the stream; the first device-side error of the last call on this workspace (0: none)."""
         wp, _ = Net._ws(workspace)
-        return int(lib().mw_orth_status(self._h, wp, _stream_handle(stream)))
+        return int(_call("mw_orth_status", workspace.device, self._h, wp, stream=stream))
 
 
 # ---- moving a synthetic problem onto the device -------------------------------------------

@@ -1,5 +1,7 @@
 """What the sequence-block bindings hand to the library, seen without a GPU: CPU tensors stand in for CUDA ones,
 and a recorder stands in for the library."""
+import contextlib
+
 import pytest
 import torch
 
@@ -34,6 +36,8 @@ def recorder(monkeypatch):
     monkeypatch.setattr(mwb, "lib", lambda: rec)
     monkeypatch.setattr(mwb, "_raw_stream", lambda stream, device: 0)
     monkeypatch.setattr(mwb, "_passed", {})
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: torch.device("cpu").index)
+    monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
     # bytes from the address of a tensor that was asked for it to the end of its memory
     rec.room = {}
     plain = torch.Tensor.data_ptr
@@ -47,6 +51,48 @@ def recorder(monkeypatch):
 
     monkeypatch.setattr(torch.Tensor, "data_ptr", data_ptr)
     return rec
+
+
+class OnSecond(OnDevice):
+    device = torch.device("cuda", 1)
+
+
+@pytest.fixture
+def devices(monkeypatch, recorder):
+    """The device that is current, as the bindings see and set it; every recorded call notes it."""
+    current = [0]
+
+    class Device:
+        def __init__(self, device):
+            self.index = torch.device(device).index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    recorder.at = []
+    plain = Recorder.__getattr__
+
+    def noted(self, name):
+        call = plain(self, name)
+
+        def both(*args):
+            recorder.at.append((name, current[0]))
+            return call(*args)
+        return both
+
+    monkeypatch.setattr(Recorder, "__getattr__", noted)
+    return current
+
+
+class Stream:
+    def __init__(self, index):
+        self.device = torch.device("cuda", index)
+        self.cuda_stream = 64 + index
 
 
 def scan_reach(d, which):
@@ -131,3 +177,51 @@ def test_norm_reads_expanded_inputs_inside_their_memory(recorder, which):
                 assert norm_reach(args[0], field) <= recorder.room[at], (name, field)
                 checked += 1
     assert checked == 6
+
+
+def second(*shape, dtype=torch.float32):
+    return torch.randn(*shape).to(dtype).as_subclass(OnSecond)
+
+
+def orth_lists(count=2):
+    return [[second(8, 8) for _ in range(count)] for _ in range(3)]
+
+
+def test_calls_run_with_the_tensors_device_current(devices, recorder):
+    v, h = second(B, T, D), second(B, D)
+    st = second(B, -(-T // mwb.SCAN_STATE_EVERY), D)
+    x, w = second(R, D), second(D)
+    plan = mwb.Orth(8, 8, 2, "f32")
+    ws = torch.empty(1 << 16, dtype=torch.uint8).as_subclass(OnSecond)
+    W, G, M = orth_lists()
+    recorder.at.clear()
+    for _ in range(2):                 # the first call of a layout and a remembered one
+        mwb.gated_scan(v, v, h0=h, y=second(B, T, D), h_last=h)
+        mwb.gated_scan_backward(v, v, v, st, dh_last=h, dv=second(B, T, D), df=second(B, T, D))
+        mwb.residual_norm(x, x, w_pre=w, x_out=second(R, D), n=second(R, D))
+        plan.step(W, G, M, ws, lr=0.1)
+        plan.project(W, ws, out=M)
+        plan.status(ws)
+    assert len(recorder.at) == 12 and all(at == 1 for _, at in recorder.at), recorder.at
+    assert devices[0] == 0
+
+
+def test_backward_of_the_norm_runs_with_the_tensors_device_current(devices, recorder, monkeypatch):
+    # (the call allocates its scratch: on the CPU here)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw))
+    x, w, rms = second(R, D), second(D), second(2, R)
+    mwb.residual_norm_backward(x, x, rms, w_pre=w, dx_out=x, dn=x)
+    assert recorder.at == [("mw_residual_norm_scratch_bytes", 1), ("mw_residual_norm_backward", 1)] and devices[0] == 0
+
+
+def test_orth_refuses_a_stream_of_another_device(devices, recorder):
+    plan = mwb.Orth(8, 8, 2, "f32")
+    ws = torch.empty(1 << 16, dtype=torch.uint8).as_subclass(OnSecond)
+    W, G, M = orth_lists()
+    n = len(recorder.calls)
+    for bad in (lambda: plan.step(W, G, M, ws, lr=0.1, stream=Stream(0)), lambda: plan.project(W, ws, out=M, stream=Stream(0)),
+                lambda: plan.status(ws, stream=Stream(0))):
+        with pytest.raises(ValueError):
+            bad()
+    assert len(recorder.calls) == n
