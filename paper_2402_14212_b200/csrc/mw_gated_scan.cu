@@ -28,16 +28,21 @@ __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// a = sigmoid(f) and w = 1 - a, each to full relative accuracy at either end (one exponential, one
-// reciprocal: 1 - a formed by subtraction would lose the slow channels, where a is close to 1).  The
-// exponent is held below 116, where a is 1e-35 and w exactly 1: the exponential stays finite.  NaN stays NaN.
-__device__ __forceinline__ void gate_of(float f, float& a, float& w) {
+// exp(-f).  The exponent is held below 116, where a is 1e-35 and 1 - a exactly 1: the exponential stays finite.
+// NaN stays NaN.
+__device__ __forceinline__ float decay_of(float f) {
   float x, e;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(f * -1.4426950408889634f), "f"(116.f));
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  return e;
+}
+// a = sigmoid(f) and w = 1 - a from exp(-f): one reciprocal gives both ends to their own relative accuracy.  Formed
+// by a subtraction, 1 - a would lose the slow channels, where a is close to 1, and a the fast ones.
+__device__ __forceinline__ void gate_from(float e, float& a, float& w) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.f + e));
   w = e * a;
 }
+__device__ __forceinline__ void gate_of(float f, float& a, float& w) { gate_from(decay_of(f), a, w); }
 __device__ __forceinline__ float sqrt_of(float x) {
   float r;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -127,7 +132,7 @@ scan_walk_back_kernel(const ScanArgs p) {
     const int t0 = i * kEvery, len = min(kEvery, p.T - t0);
     float h = p.states_in[(b * nst + i) * p.D + c];
     if (WHOLE && t0 + kEvery <= n) {
-      float w[kEvery], k[kEvery];                   // 1 - a and df / g of each step
+      float e[kEvery], k[kEvery];                   // exp(-f) and df / g of each step
       unsigned cuts = 0;
 #pragma unroll
       for (int q = 0; q < kEvery; q += kAhead) {
@@ -141,11 +146,12 @@ scan_walk_back_kernel(const ScanArgs p) {
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          float a;
-          gate_of(fs[j], a, w[q + j]);
+          float a, w;
+          e[q + j] = decay_of(fs[j]);
+          gate_from(e[q + j], a, w);
           const float before = (cuts >> (q + j)) & 1u ? 0.f : h;
-          k[q + j] = fmaf(a * w[q + j], before, input_slope<GATE>(a, w[q + j]) * vs[j]);
-          h = fmaf(a, before, input_of<GATE>(a, w[q + j]) * vs[j]);
+          k[q + j] = fmaf(a * w, before, input_slope<GATE>(a, w) * vs[j]);
+          h = fmaf(a, before, input_of<GATE>(a, w) * vs[j]);
         }
       }
 #pragma unroll
@@ -156,9 +162,10 @@ scan_walk_back_kernel(const ScanArgs p) {
 #pragma unroll
         for (int j = kAhead - 1; j >= 0; --j) {
           const int t = t0 + q + j;
-          const float a = 1.f - w[q + j];
+          float a, w;
+          gate_from(e[q + j], a, w);
           g += ds[j];
-          dv[t * p.dv_t] = from_f32<T>(input_of<GATE>(a, w[q + j]) * g);
+          dv[t * p.dv_t] = from_f32<T>(input_of<GATE>(a, w) * g);
           df[t * p.df_t] = from_f32<T>(k[q + j] * g);
           g = (cuts >> (q + j)) & 1u ? 0.f : a * g;
         }
@@ -526,35 +533,29 @@ scan_chunk_back_kernel(const ScanArgs p) {
 #pragma unroll
       for (int j = 0; j < kEvery; ++j)
         if (t0 + j < n && p.reset[(int64_t)b * p.T + t0 + j] != 0) cuts |= 1u << j;
-    float w[kEvery][VEC], k[kEvery][VEC];
+    float e[kEvery][VEC], k[kEvery][VEC];         // exp(-f) and df / g of each step
     auto compose = [&](auto full) {
 #pragma unroll
       for (int j = 0; j < kEvery; ++j) {
-        float v[VEC], f[VEC];
+        float v[VEC], f[VEC], d[VEC];
         L::get(rv[j], v);
         L::get(rf[j], f);
+        L::get(rd[j], d);
         const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          float s;
-          gate_of(f[i], s, w[j][i]);
-          const float before = cut ? 0.f : h[i], in = input_of<GATE>(s, w[j][i]) * v[i];
-          k[j][i] = fmaf(s * w[j][i], before, input_slope<GATE>(s, w[j][i]) * v[i]);
-          if (on) h[i] = fmaf(s, before, in);
-          if (!on) w[j][i] = 0.f;                     // a = 1: the cotangent passes
-        }
-      }
-#pragma unroll
-      for (int j = kEvery - 1; j >= 0; --j) {
-        float d[VEC];
-        L::get(rd[j], d);
-        const bool cut = CUT && ((cuts >> j) & 1u);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float a = 1.f - w[j][i];
-          P[i] = j == kEvery - 1 ? a : P[i] * a;
-          E[i] = j == kEvery - 1 ? a * d[i] : a * (E[i] + d[i]);
-          if (cut) P[i] = E[i] = 0.f;
+          float a, w;
+          e[j][i] = decay_of(f[i]);
+          gate_from(e[j][i], a, w);
+          const float before = cut ? 0.f : h[i], in = input_of<GATE>(a, w) * v[i];
+          k[j][i] = fmaf(a * w, before, input_slope<GATE>(a, w) * v[i]);
+          if (on) h[i] = fmaf(a, before, in);
+          if (!on) { a = 1.f; e[j][i] = 0.f; }        // the cotangent passes
+          // d reaches the state before the first step through all gates up to its own
+          if (CUT && cut) a = 0.f;
+          P[i] = j ? P[i] * a : a;
+          if (!j) E[i] = 0.f;
+          if (!CUT || P[i] != 0.f) E[i] = fmaf(P[i], d[i], E[i]);
         }
       }
     };
@@ -571,8 +572,10 @@ scan_chunk_back_kernel(const ScanArgs p) {
           const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            const float a = 1.f - w[j][i], g = G[i] + d[i];
-            ov[i] = on ? input_of<GATE>(a, w[j][i]) * g : 0.f;
+            float a, w;
+            gate_from(e[j][i], a, w);
+            const float g = G[i] + d[i];
+            ov[i] = on ? input_of<GATE>(a, w) * g : 0.f;
             of[i] = on ? k[j][i] * g : 0.f;
             G[i] = cut ? 0.f : a * g;
           }
@@ -748,7 +751,7 @@ scan_wide_kernel(const ScanArgs p) {
 template <typename T, int GATE, bool CUT, int STEPS>
 __global__ void __launch_bounds__(32 * kScanWarps, 2)
 scan_wide_back_kernel(const ScanArgs p) {
-  constexpr int VEC = 1;               // (two channels' w and k would leave 16 steps between exchanges)
+  constexpr int VEC = 1;               // (two channels' e and k would leave 16 steps between exchanges)
   using R = Rows<T, VEC, STEPS>;
   constexpr int kBlockBytes = R::kBlock, kRowBytes = R::kBytes;
   using L = Lane<T, VEC>;
@@ -810,35 +813,29 @@ scan_wide_back_kernel(const ScanArgs p) {
 #pragma unroll
       for (int j = 0; j < STEPS; ++j)
         if (t0 + j < n && p.reset[(int64_t)b * p.T + t0 + j] != 0) cuts |= 1u << j;
-    float w[STEPS][VEC], k[STEPS][VEC];
+    float e[STEPS][VEC], k[STEPS][VEC];         // exp(-f) and df / g of each step
     auto compose = [&](auto full) {
 #pragma unroll
       for (int j = 0; j < STEPS; ++j) {
-        float v[VEC], f[VEC];
+        float v[VEC], f[VEC], d[VEC];
         L::get(*reinterpret_cast<const Raw*>(word + j * kRowBytes), v);
         L::get(*reinterpret_cast<const Raw*>(word + kBlockBytes + j * kRowBytes), f);
+        L::get(*reinterpret_cast<const Raw*>(word + 2 * kBlockBytes + j * kRowBytes), d);
         const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          float s;
-          gate_of(f[i], s, w[j][i]);
-          const float before = cut ? 0.f : h[i], in = input_of<GATE>(s, w[j][i]) * v[i];
-          k[j][i] = fmaf(s * w[j][i], before, input_slope<GATE>(s, w[j][i]) * v[i]);
-          if (on) h[i] = fmaf(s, before, in);
-          if (!on) w[j][i] = 0.f;                     // a = 1: the cotangent passes
-        }
-      }
-#pragma unroll
-      for (int j = STEPS - 1; j >= 0; --j) {
-        float d[VEC];
-        L::get(*reinterpret_cast<const Raw*>(word + 2 * kBlockBytes + j * kRowBytes), d);
-        const bool cut = CUT && ((cuts >> j) & 1u);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float a = 1.f - w[j][i];
-          P[i] = j == STEPS - 1 ? a : P[i] * a;
-          E[i] = j == STEPS - 1 ? a * d[i] : a * (E[i] + d[i]);
-          if (cut) P[i] = E[i] = 0.f;
+          float a, w;
+          e[j][i] = decay_of(f[i]);
+          gate_from(e[j][i], a, w);
+          const float before = cut ? 0.f : h[i], in = input_of<GATE>(a, w) * v[i];
+          k[j][i] = fmaf(a * w, before, input_slope<GATE>(a, w) * v[i]);
+          if (on) h[i] = fmaf(a, before, in);
+          if (!on) { a = 1.f; e[j][i] = 0.f; }        // the cotangent passes
+          // d reaches the state before the first step through all gates up to its own
+          if (CUT && cut) a = 0.f;
+          P[i] = j ? P[i] * a : a;
+          if (!j) E[i] = 0.f;
+          if (!CUT || P[i] != 0.f) E[i] = fmaf(P[i], d[i], E[i]);
         }
       }
     };
@@ -853,8 +850,10 @@ scan_wide_back_kernel(const ScanArgs p) {
           const bool on = decltype(full)::value || t0 + j < n, cut = CUT && ((cuts >> j) & 1u);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            const float a = 1.f - w[j][i], g = G[i] + d[i];
-            ov[i] = on ? input_of<GATE>(a, w[j][i]) * g : 0.f;
+            float a, w;
+            gate_from(e[j][i], a, w);
+            const float g = G[i] + d[i];
+            ov[i] = on ? input_of<GATE>(a, w) * g : 0.f;
             of[i] = on ? k[j][i] * g : 0.f;
             G[i] = cut ? 0.f : a * g;
           }

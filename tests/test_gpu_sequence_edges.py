@@ -45,3 +45,53 @@ def test_expanded_norm_operands_equal_dense_ones(dtype):
                 xo, n, rms = mwb.residual_norm(x, b, keep_rms=True, **kw)
                 results.append((xo, n) + tuple(mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, **kw)))
             assert all(torch.equal(p, q) for p, q in zip(*results))
+
+
+def far_gates(T, D, B, gate, dtype, seed):
+    """Gates that forget almost all, and the backward recurrence from dh_last alone in 64 bits."""
+    import torch
+    rng = np.random.default_rng(seed)
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    v = torch.from_numpy(rng.standard_normal((B, T, D))).to(dt).cuda()
+    f = torch.from_numpy(np.linspace(-20, -6, D) + 0.5 * rng.standard_normal((B, T, D))).to(dt).cuda()
+    h0, dh = (torch.from_numpy(rng.standard_normal((B, D))).float().cuda() for _ in range(2))
+    V, F, H, g = (t.double().cpu().numpy() for t in (v, f, h0, dh))
+    a, w = 1 / (1 + np.exp(-F)), 1 / (1 + np.exp(F))
+    u = w if gate == "complement" else np.sqrt(w * (1 + a))
+    slope = -a * w if gate == "complement" else -a * a * np.sqrt(w / (1 + a))
+    before = np.zeros((B, T, D))
+    for t in range(T):
+        before[:, t] = H
+        H = a[:, t] * H + u[:, t] * V[:, t]
+    dv, df, size = np.zeros((B, T, D)), np.zeros((B, T, D)), np.zeros((B, T, D))
+    for t in range(T - 1, -1, -1):
+        dv[:, t] = u[:, t] * g
+        df[:, t] = g * (a[:, t] * w[:, t] * before[:, t] + slope[:, t] * V[:, t])
+        size[:, t] = np.abs(g) * (a[:, t] * w[:, t] * np.abs(before[:, t]) + np.abs(slope[:, t] * V[:, t]))
+        g = a[:, t] * g
+    return v, f, h0, dh, dv, df, size, g
+
+
+# Each gate carries a relative error of (|f| + 4) 2^-24 (the rounding of f log2(e), then an exponential and a reciprocal
+# of one or two units), so after k steps a cotangent is off by k (|f| + 4) 2^-24 of itself: |f| < 23 here.  bf16
+# results add 2^-8 of their value.  Values below 1e-30 (products of a few gates) are left out: what they are multiplied
+# from is near the smallest normal number.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", ["complement", "energy"])
+@pytest.mark.parametrize("shape", [(2, 1, 64), (2, 15, 64), (2, 16, 64), (2, 17, 66), (2, 17, 64), (1, 400, 64), (1, 400, 66),
+                                   (3, 2100, 64), (230, 40, 264)], ids=lambda s: "x".join(map(str, s)))
+def test_cotangents_through_gates_that_forget(shape, gate, dtype):
+    import torch
+    B, T, D = shape
+    v, f, h0, dh, dv, df, size, dh0 = far_gates(T, D, B, gate, dtype, sum(shape))
+    _, _, st = mwb.gated_scan(v, f, h0=h0, input_gate=gate, keep_states=True)
+    none = torch.zeros((B, T), dtype=torch.uint8, device="cuda")
+    back = np.arange(T, 0, -1)[None, :, None]
+    ulp = 2.0 ** -8 if dtype == "bf16" else 0.0
+    for reset in (None, none):
+        got = [t.double().cpu().numpy() for t in mwb.gated_scan_backward(v, f, None, st, reset=reset, dh_last=dh, input_gate=gate)]
+        for g, want, scale, steps, r in ((got[0], dv, np.abs(dv), back + 1, ulp), (got[1], df, size, back + 1, ulp),
+                                         (got[2], dh0, np.abs(dh0), T + 1, 0.0)):
+            err = np.abs(g - want) - r * np.abs(want) - scale * steps * 27 * 2.0 ** -24
+            assert (err[scale > 1e-30] <= 0).all()
+            assert np.isfinite(g).all()
