@@ -247,11 +247,19 @@ struct Lane<__nv_bfloat16, 2> {
   }
 };
 
-// h -> P h + H.  With CUT a zero P drops h whatever it is: infinities and NaN of what came before a
-// reset do not reach the steps after it.
+// h -> P h + H.  A map over a reset has P = -0, which no product of gates is (they are positive, and what underflows
+// is +0): it drops h whatever it is, so infinities and NaN of what came before a reset do not reach the steps
+// after it, while those of a state that has merely decayed do.
+constexpr float kCutFactor = -0.f;
+__device__ __forceinline__ bool is_cut(float P) { return __float_as_uint(P) == 0x80000000u; }
 template <bool CUT>
 __device__ __forceinline__ float affine(float P, float h, float H) {
-  return CUT && P == 0.f ? H : fmaf(P, h, H);
+  return CUT && is_cut(P) ? H : fmaf(P, h, H);
+}
+// the factor of a map P after one of factor Q (a NaN before a reset is dropped with the rest)
+template <bool CUT>
+__device__ __forceinline__ float chained(float P, float Q) {
+  return CUT && is_cut(P) ? P : P * Q;
 }
 
 // Composes the maps of the block's warps and of the cluster's blocks.  `state` holds what the cluster's next
@@ -316,7 +324,7 @@ struct Exchange {
       for (int i = 0; i < VEC; ++i) {
         const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][lane][i];
         he[i] = affine<CUT>(m.x, he[i], m.y);
-        pe[i] *= m.x;
+        pe[i] = chained<CUT>(m.x, pe[i]);
       }
     }
     const bool last = before == kScanWarps - 1;
@@ -331,7 +339,7 @@ struct Exchange {
     }
     if (last) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) outgoing[flip][lane][i] = make_float2(P[i] * pe[i], affine<CUT>(P[i], he[i], H[i]));
+      for (int i = 0; i < VEC; ++i) outgoing[flip][lane][i] = make_float2(chained<CUT>(P[i], pe[i]), affine<CUT>(P[i], he[i], H[i]));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane < C)
@@ -434,9 +442,9 @@ scan_chunk_kernel(const ScanArgs p) {
           float w;
           gate_of(f[i], a[j][i], w);
           in[j][i] = input_of<GATE>(a[j][i], w) * v[i];
-          if (CUT && cut) a[j][i] = 0.f;
+          if (CUT && cut) a[j][i] = kCutFactor;
           if (!on) { a[j][i] = 1.f; in[j][i] = 0.f; }
-          P[i] = j ? P[i] * a[j][i] : a[j][i];
+          P[i] = j ? chained<CUT>(a[j][i], P[i]) : a[j][i];
           H[i] = j ? affine<CUT>(a[j][i], H[i], in[j][i]) : in[j][i];
         }
       }
@@ -552,10 +560,10 @@ scan_chunk_back_kernel(const ScanArgs p) {
           if (on) h[i] = fmaf(a, before, in);
           if (!on) { a = 1.f; e[j][i] = 0.f; }        // the cotangent passes
           // d reaches the state before the first step through all gates up to its own
-          if (CUT && cut) a = 0.f;
-          P[i] = j ? P[i] * a : a;
+          if (CUT && cut) a = kCutFactor;
+          P[i] = j ? chained<CUT>(P[i], a) : a;
           if (!j) E[i] = 0.f;
-          if (!CUT || P[i] != 0.f) E[i] = fmaf(P[i], d[i], E[i]);
+          if (!CUT || !is_cut(P[i])) E[i] = fmaf(P[i], d[i], E[i]);
         }
       }
     };
@@ -710,9 +718,9 @@ scan_wide_kernel(const ScanArgs p) {
           float w;
           gate_of(f[i], a[j][i], w);
           in[j][i] = input_of<GATE>(a[j][i], w) * v[i];
-          if (CUT && cut) a[j][i] = 0.f;
+          if (CUT && cut) a[j][i] = kCutFactor;
           if (!on) { a[j][i] = 1.f; in[j][i] = 0.f; }
-          P[i] = j ? P[i] * a[j][i] : a[j][i];
+          P[i] = j ? chained<CUT>(a[j][i], P[i]) : a[j][i];
           H[i] = j ? affine<CUT>(a[j][i], H[i], in[j][i]) : in[j][i];
         }
       }
@@ -832,10 +840,10 @@ scan_wide_back_kernel(const ScanArgs p) {
           if (on) h[i] = fmaf(a, before, in);
           if (!on) { a = 1.f; e[j][i] = 0.f; }        // the cotangent passes
           // d reaches the state before the first step through all gates up to its own
-          if (CUT && cut) a = 0.f;
-          P[i] = j ? P[i] * a : a;
+          if (CUT && cut) a = kCutFactor;
+          P[i] = j ? chained<CUT>(P[i], a) : a;
           if (!j) E[i] = 0.f;
-          if (!CUT || P[i] != 0.f) E[i] = fmaf(P[i], d[i], E[i]);
+          if (!CUT || !is_cut(P[i])) E[i] = fmaf(P[i], d[i], E[i]);
         }
       }
     };

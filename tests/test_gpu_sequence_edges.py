@@ -95,3 +95,64 @@ def test_cotangents_through_gates_that_forget(shape, gate, dtype):
             err = np.abs(g - want) - r * np.abs(want) - scale * steps * 27 * 2.0 ** -24
             assert (err[scale > 1e-30] <= 0).all()
             assert np.isfinite(g).all()
+
+
+def scan_inputs(B, T, D, dtype, seed, logit=1.0):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    v, f, dy = (torch.randn(B, T, D, generator=g, device="cuda") for _ in range(3))
+    h0 = torch.randn(B, D, generator=g, device="cuda")
+    return v.to(dt), (f + logit).to(dt), dy.to(dt), h0
+
+
+# 12 steps are walked, 400 are one piece of a few blocks, 3000 several
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 66])
+@pytest.mark.parametrize("T", [12, 400, 3000])
+def test_a_reset_keeps_out_a_gate_that_is_not_a_number(T, D, dtype):
+    import torch
+    v, f, dy, h0 = scan_inputs(1, T, D, dtype, 12)
+    at = T // 2
+    reset = torch.zeros((1, T), dtype=torch.uint8, device="cuda")
+    reset[0, at] = 1
+    y0, h_last0, st0 = mwb.gated_scan(v, f, reset=reset, h0=h0, keep_states=True)
+    g0 = mwb.gated_scan_backward(v, f, dy, st0, reset=reset)
+    before, after = f.clone(), f.clone()
+    before[0, at - 3] = float("nan")
+    after[0, at + 2] = float("nan")
+    y, h_last, st = mwb.gated_scan(v, before, reset=reset, h0=h0, keep_states=True)
+    assert torch.equal(y[:, at:], y0[:, at:]) and torch.equal(h_last, h_last0)
+    assert bool(torch.isnan(y[:, at - 3:at]).all())
+    g = mwb.gated_scan_backward(v, before, dy, st, reset=reset)
+    assert torch.equal(g[0][:, at:], g0[0][:, at:]) and torch.equal(g[1][:, at:], g0[1][:, at:])
+    _, _, st = mwb.gated_scan(v, after, reset=reset, h0=h0, keep_states=True)
+    g = mwb.gated_scan_backward(v, after, dy, st, reset=reset)
+    assert torch.equal(g[0][:, :at], g0[0][:, :at]) and torch.equal(g[1][:, :at], g0[1][:, :at])
+    assert torch.equal(g[2], g0[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 66])
+@pytest.mark.parametrize("T", [600, 3000])
+def test_without_a_reset_a_nan_stays_however_strong_the_decay(T, D, dtype):
+    # the product of the gates underflows on the way; the reset array is there, but empty
+    import torch
+    v, f, dy, h0 = scan_inputs(2, T, D, dtype, 3, logit=-1.0)
+    reset = torch.zeros((2, T), dtype=torch.uint8, device="cuda")
+    bad = v.clone()
+    bad[1, 100, 5] = float("nan")
+    for r in (reset, None):
+        y, h_last, _ = mwb.gated_scan(bad, f, reset=r, h0=h0, keep_states=True)
+        nan = torch.isnan(y)
+        assert bool(nan[1, 100:, 5].all()) and int(nan.sum()) == T - 100
+        assert bool(torch.isnan(h_last[1, 5])) and int(torch.isnan(h_last).sum()) == 1
+    _, _, st = mwb.gated_scan(v, f, reset=reset, h0=h0, keep_states=True)
+    worse = dy.clone()
+    worse[1, T - 50, 7] = float("nan")
+    for r in (reset, None):
+        dv, df, dh0 = mwb.gated_scan_backward(v, f, worse, st, reset=r)
+        for t in (dv, df):
+            nan = torch.isnan(t)
+            assert bool(nan[1, :T - 49, 7].all()) and int(nan.sum()) == T - 49
+        assert bool(torch.isnan(dh0[1, 7])) and int(torch.isnan(dh0).sum()) == 1
