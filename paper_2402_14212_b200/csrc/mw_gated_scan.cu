@@ -262,6 +262,10 @@ __device__ __forceinline__ float chained(float P, float Q) {
   return CUT && is_cut(P) ? P : P * Q;
 }
 
+// A product of gates that has underflowed, as the least positive number: an infinite h then stays infinite, as it
+// does step by step (0 would make it NaN), and a finite one counts for 5e-7 at the very most.
+__device__ __forceinline__ float held(float P) { return __uint_as_float(max(__float_as_uint(P), 1u)); }
+
 // Composes the maps of the block's warps and of the cluster's blocks.  `state` holds what the cluster's next
 // piece starts from, the same in all its blocks.  REVERSE: the pieces follow one another from the last warp
 // of the last block to the first (the cotangent's direction).
@@ -304,10 +308,12 @@ struct Exchange {
   }
 
   // in: this thread's map (P, H) of piece `index`; out: the state its steps start from
-  __device__ __forceinline__ void run(const float (&P)[VEC], const float (&H)[VEC], float (&start)[VEC], int index,
+  __device__ __forceinline__ void run(float (&P)[VEC], const float (&H)[VEC], float (&start)[VEC], int index,
                                       int rank, int C) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, flip = index & 1;
     constexpr uint32_t kBytes = 32 * VEC * sizeof(float2);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) P[i] = held(P[i]);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) warp_map[flip][warp][lane][i] = make_float2(P[i], H[i]);
     if (C > 1 && threadIdx.x == 0)
@@ -324,7 +330,7 @@ struct Exchange {
       for (int i = 0; i < VEC; ++i) {
         const float2 m = warp_map[flip][REVERSE ? kScanWarps - 1 - k : k][lane][i];
         he[i] = affine<CUT>(m.x, he[i], m.y);
-        pe[i] = chained<CUT>(m.x, pe[i]);
+        pe[i] = held(chained<CUT>(m.x, pe[i]));
       }
     }
     const bool last = before == kScanWarps - 1;
@@ -339,7 +345,7 @@ struct Exchange {
     }
     if (last) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) outgoing[flip][lane][i] = make_float2(chained<CUT>(P[i], pe[i]), affine<CUT>(P[i], he[i], H[i]));
+      for (int i = 0; i < VEC; ++i) outgoing[flip][lane][i] = make_float2(held(chained<CUT>(P[i], pe[i])), affine<CUT>(P[i], he[i], H[i]));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane < C)
@@ -561,7 +567,7 @@ scan_chunk_back_kernel(const ScanArgs p) {
           if (!on) { a = 1.f; e[j][i] = 0.f; }        // the cotangent passes
           // d reaches the state before the first step through all gates up to its own
           if (CUT && cut) a = kCutFactor;
-          P[i] = j ? chained<CUT>(P[i], a) : a;
+          P[i] = j ? held(chained<CUT>(P[i], a)) : a;
           if (!j) E[i] = 0.f;
           if (!CUT || !is_cut(P[i])) E[i] = fmaf(P[i], d[i], E[i]);
         }
@@ -841,7 +847,7 @@ scan_wide_back_kernel(const ScanArgs p) {
           if (!on) { a = 1.f; e[j][i] = 0.f; }        // the cotangent passes
           // d reaches the state before the first step through all gates up to its own
           if (CUT && cut) a = kCutFactor;
-          P[i] = j ? chained<CUT>(P[i], a) : a;
+          P[i] = j ? held(chained<CUT>(P[i], a)) : a;
           if (!j) E[i] = 0.f;
           if (!CUT || !is_cut(P[i])) E[i] = fmaf(P[i], d[i], E[i]);
         }

@@ -156,3 +156,30 @@ def test_without_a_reset_a_nan_stays_however_strong_the_decay(T, D, dtype):
             nan = torch.isnan(t)
             assert bool(nan[1, :T - 49, 7].all()) and int(nan.sum()) == T - 49
         assert bool(torch.isnan(dh0[1, 7])) and int(torch.isnan(dh0).sum()) == 1
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 66])
+@pytest.mark.parametrize("T", [12, 600, 3000])
+def test_an_infinite_state_stays_infinite(T, D, dtype):
+    # the recurrence keeps it, however far the product of the gates after it has underflowed
+    import torch
+    v, f, dy, h0 = scan_inputs(2, T, D, dtype, 4, logit=-1.0)
+    none = torch.zeros((2, T), dtype=torch.uint8, device="cuda")
+    at = min(T // 3, 100)
+    bad, worse = v.clone(), dy.clone()
+    bad[0, at, 3], bad[1, at, 5] = float("inf"), -float("inf")
+    worse[0, T - at, 3], worse[1, T - at, 5] = float("inf"), -float("inf")
+    for reset in (None, none):
+        y0, _ = mwb.gated_scan(v, f, reset=reset, h0=h0)
+        y, h_last, st = mwb.gated_scan(bad, f, reset=reset, h0=h0, keep_states=True)
+        assert bool((y[0, at:, 3] == float("inf")).all()) and bool((y[1, at:, 5] == -float("inf")).all())
+        assert float(h_last[0, 3]) == float("inf") and float(h_last[1, 5]) == -float("inf")
+        rest = torch.ones_like(y, dtype=torch.bool)
+        rest[0, at:, 3] = rest[1, at:, 5] = False
+        assert torch.equal(y[rest], y0[rest])
+        _, _, st = mwb.gated_scan(v, f, reset=reset, h0=h0, keep_states=True)
+        dv, _, dh0 = mwb.gated_scan_backward(v, f, worse, st, reset=reset)
+        assert bool((dv[0, :T - at + 1, 3] == float("inf")).all()) and bool((dv[1, :T - at + 1, 5] == -float("inf")).all())
+        assert float(dh0[0, 3]) == float("inf") and float(dh0[1, 5]) == -float("inf")
+        assert int((~torch.isfinite(dv)).sum()) == 2 * (T - at + 1)
