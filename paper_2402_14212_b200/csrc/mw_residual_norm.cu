@@ -353,7 +353,8 @@ norm_backward_kernel(const NormArgs a, const NormPlan p) {
   const int C = CLUSTER ? p.cluster : 1;
   const int D = a.cols;
   const float inv_d = 1.f / (float)D;
-  const bool has_b = a.b != nullptr, has_z = a.z != nullptr, normed = a.w_post != nullptr;
+  // (without a cotangent of n nothing depends on x': what it holds, infinities too, stays out of the sums)
+  const bool has_b = a.b != nullptr, has_z = a.z != nullptr, has_n = a.dn != nullptr, normed = a.w_post != nullptr;
   // A thread's 16 bytes of each tensor come by asynchronous copies into shared memory of its own, kStages - 1 rows
   // ahead: at 40 bytes an element in and out, one row ahead leaves HBM idle while a row is reduced.  (Rows
   // that are read element by element, whose copies could not be that small, are held in registers, one
@@ -447,7 +448,7 @@ norm_backward_kernel(const NormArgs a, const NormPlan p) {
       }
       stage = stage + 1 == kStages ? 0 : stage + 1;
     }
-    const float inv_b = next_b, inv_x = a.w_pre ? next_x : 0.f, xs = next_x;
+    const float inv_b = next_b, inv_x = has_n ? next_x : 0.f, xs = next_x;
     // kept over the reduction: dx_out + q / rms(x'), xh, silu(z), silu'(z), b
     float A[K][VEC], xh[K][VEC], gate[K][VEC], slope[K][VEC];
     Raw cb[K];
@@ -467,7 +468,7 @@ norm_backward_kernel(const NormArgs a, const NormPlan p) {
           slope[k][i] = sig * fmaf(vz[i], 1.f - sig, 1.f);
         }
         const float tau = ks[k][i] * (vb[i] * inv_b) * gate[k][i];
-        xh[k][i] = (has_b ? vx[i] + tau : vx[i]) * xs;
+        xh[k][i] = has_n ? (has_b ? vx[i] + tau : vx[i]) * xs : 0.f;
         const float q = vn[i] * wn[k][i];
         A[k][i] = fmaf(q, inv_x, vo[i]);
         s[0] = fmaf(q, xh[k][i], s[0]);
@@ -479,8 +480,8 @@ norm_backward_kernel(const NormArgs a, const NormPlan p) {
     if (base + stride < a.rows) load(row + stride);
     meet.template sum<LANES, W, 3>(s, n, p, w.rank, ok);
     n = CLUSTER ? n + 1 : n ^ 1;
-    const float m1 = s[0] * inv_d * inv_x;
-    const float m2 = normed ? fmaf(-m1, s[2], s[1]) * inv_d * inv_b : 0.f;
+    const float m1 = has_n ? s[0] * inv_d * inv_x : 0.f;
+    const float m2 = normed ? (has_n ? fmaf(-m1, s[2], s[1]) : s[1]) * inv_d * inv_b : 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (w.piece + k * STEP) * VEC;

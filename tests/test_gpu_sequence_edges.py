@@ -183,3 +183,32 @@ def test_an_infinite_state_stays_infinite(T, D, dtype):
         assert bool((dv[0, :T - at + 1, 3] == float("inf")).all()) and bool((dv[1, :T - at + 1, 5] == -float("inf")).all())
         assert float(dh0[0, 3]) == float("inf") and float(dh0[1, 5]) == -float("inf")
         assert int((~torch.isfinite(dv)).sum()) == 2 * (T - at + 1)
+
+
+# rows of 8 and 16 lanes, one to sixteen warps, element by element, and a cluster
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [40, 96, 264, 1003, 2048, 4096, 9000])
+def test_what_does_not_depend_on_the_sum_is_not_spoilt_by_it(D, dtype):
+    # without a cotangent of n, dx is dx_out, and db and dz hold no x: an infinity, a NaN or a number whose square
+    # overflows in x leaves them as they are
+    import torch
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x, b, z, dxo = (torch.randn(5, D, generator=g, device="cuda").to(dt) for _ in range(4))
+    wp, sc, wn = (torch.rand(D, generator=g, device="cuda") + 0.5 for _ in range(3))
+    bad = x.clone()
+    bad[0, 3], bad[1, D - 1], bad[2, 7], bad[3, 5] = float("inf"), -float("inf"), float("nan"), 3e38
+    b[3, 5] = 1e30
+    for kw in (dict(w_post=wp, scale=sc, z=z), dict(w_post=wp), dict(scale=sc, z=z), dict(w_post=wp, scale=sc, z=z, w_pre=wn)):
+        out = []
+        for t in (x, bad):
+            _, _, rms = mwb.residual_norm(t, b, keep_rms=True, **kw)
+            out.append(mwb.residual_norm_backward(t, b, rms, dx_out=dxo, dn=None, **kw))
+        want, got = out
+        assert torch.equal(got.dx, dxo) and torch.equal(want.dx, dxo)
+        for name in ("db", "dz", "dw_post", "dscale"):
+            p, q = getattr(got, name), getattr(want, name)
+            if p is not None:
+                assert bool(torch.isfinite(p).all()) and torch.equal(p, q), name
+        if got.dw_pre is not None:
+            assert not got.dw_pre.any()
