@@ -543,17 +543,27 @@ def _call(name, device, *args, stream=None) -> int:
         return getattr(lib(), name)(*args, handle)
 
 
+def _keep_for(stream, *things):
+    """Marks tensors (and lists of them) as used on `stream`: their memory is not given out again, should the caller
+    drop them, before the work there is done."""
+    import torch
+    for t in things:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+        elif isinstance(t, (list, tuple)):
+            _keep_for(stream, *t)
+
+
 def _on_stream(stream, like, call, *args):
     """call(*args) on `stream`.  What it allocates comes from that stream's memory, whose earlier uses lie
-    before the call there, and what it hands back is kept until the caller's stream is done with it too."""
+    before the call there, and what it hands back is kept until the caller's stream is done with it too; what it is
+    given is kept until `stream` is.  `stream` does not wait for the caller's stream: that is the caller's to order."""
     import torch
     _need(stream.device == like.device, f"{call.__name__}: a stream of {like.device}, not of {stream.device}")
     with torch.cuda.stream(stream):
         out = call(*args)
-    here = torch.cuda.current_stream(like.device)
-    for t in out:
-        if t is not None:
-            t.record_stream(here)
+    _keep_for(stream, *args)
+    _keep_for(torch.cuda.current_stream(like.device), out)
     return out
 
 
@@ -608,7 +618,8 @@ def gated_scan(v, f, reset=None, lengths=None, h0=None, input_gate: str = "compl
     """Gated linear recurrence h_t = r_t sigmoid(f_t) h_{t-1} + u_t v_t over dim 1 of [batch, length,
     channels] tensors (float32 or bfloat16; rows may be windows of wider ones; expanded ones are copied first).
     Returns (y, h_last), with keep_states=True (y, h_last, states) for gated_scan_backward.  One step
-    (length 1) with h0 = h_last = the cached state is the serving form."""
+    (length 1) with h0 = h_last = the cached state is the serving form.  With `stream` the work runs there, after
+    what that stream was given before: it does not wait for the current one."""
     import torch
     if stream is not None:
         return _on_stream(stream, v, gated_scan, v, f, reset, lengths, h0, input_gate, keep_states, y, h_last)
@@ -641,7 +652,7 @@ def gated_scan_backward(v, f, dy, states, reset=None, lengths=None, h0=None, dh_
                         input_gate: str = "complement", dv=None, df=None, stream=None):
     """(dv, df, dh0) of gated_scan from the cotangents of y and h_last (either may be None) and the
     states that the forward call kept (they include h0, which is accepted for symmetry).  Gradients of expanded
-    inputs come element by element, as if the inputs had been dense."""
+    inputs come element by element, as if the inputs had been dense.  `stream` as in gated_scan."""
     import torch
     if stream is not None:
         return _on_stream(stream, v, gated_scan_backward, v, f, dy, states, reset, lengths, h0, dh_last, input_gate, dv, df)
@@ -695,7 +706,7 @@ def residual_norm(x, b=None, z=None, w_post=None, scale=None, w_pre=None, eps: f
                   x_out=None, n=None, stream=None):
     """x' = x + scale silu(z) rmsnorm(b; w_post) and n = rmsnorm(x'; w_pre) on [rows, cols] tensors; what
     is None is left out (expanded x, b, z are copied first).  Returns (x', n), with keep_rms=True (x', n, inv_rms)
-    for the backward call."""
+    for the backward call.  `stream` as in gated_scan."""
     import torch
     if stream is not None:
         return _on_stream(stream, x, residual_norm, x, b, z, w_post, scale, w_pre, eps, keep_rms, x_out, n)
@@ -730,7 +741,7 @@ class ResidualNormGrads(NamedTuple):
 def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre=None, eps: float = 1e-6,
                            dx_out=None, dn=None, stream=None) -> ResidualNormGrads:
     """Gradients of residual_norm from the cotangents of x' and n (either may be None); the gradients of
-    what was left out are None, those of expanded inputs as if they had been dense."""
+    what was left out are None, those of expanded inputs as if they had been dense.  `stream` as in gated_scan."""
     import torch
     if stream is not None:
         return _on_stream(stream, x, residual_norm_backward, x, b, inv_rms, z, w_post, scale, w_pre, eps, dx_out, dn)
@@ -806,7 +817,8 @@ class Orth:
 
     def step(self, params, grads, momentum, workspace, lr: float, beta: float = 0.95, weight_decay: float = 0.0,
              scale: float = 1.0, params_out=None, momentum_out=None, stream=None):
-        """M <- beta M + G, W <- (1 - lr weight_decay) W - lr scale X; in place unless outputs are given."""
+        """M <- beta M + G, W <- (1 - lr weight_decay) W - lr scale X; in place unless outputs are given.  With
+        `stream` the work runs there, after what that stream was given before."""
         import torch
         params_out = params if params_out is None else params_out
         momentum_out = momentum if momentum_out is None else momentum_out
@@ -818,19 +830,21 @@ class Orth:
             self._list(momentum, f32, "momentum", workspace), self._list(params_out, st, "params_out", workspace),
             self._list(momentum_out, f32, "momentum_out", workspace), float(lr), float(beta), float(weight_decay), float(scale),
             wp, wb, stream=stream), "mw_orth_step")
+        if stream is not None:
+            _keep_for(stream, params, grads, momentum, params_out, momentum_out, workspace)
         return params_out
 
     def project(self, mats, workspace, out=None, stream=None):
-        """The orthogonalised factor X of every matrix, in the storage type."""
+        """The orthogonalised factor X of every matrix, in the storage type; on `stream` as in step()."""
         import torch
-        if stream is not None and out is None:
-            return _on_stream(stream, workspace, self.project, mats, workspace)
+        if stream is not None:
+            return _on_stream(stream, workspace, self.project, list(mats), workspace, out)
         st = self.storage_dtype()
         if out is None:
             out = [torch.empty_like(t) for t in mats]
         wp, wb = Net._ws(workspace)
         _check(_call("mw_orth_project", workspace.device, self._h, self._list(mats, st, "mats", workspace),
-                     self._list(out, st, "out", workspace), wp, wb, stream=stream), "mw_orth_project")
+                     self._list(out, st, "out", workspace), wp, wb), "mw_orth_project")
         return out
 
     def status(self, workspace, stream=None) -> int:

@@ -212,3 +212,40 @@ def test_what_does_not_depend_on_the_sum_is_not_spoilt_by_it(D, dtype):
                 assert bool(torch.isfinite(p).all()) and torch.equal(p, q), name
         if got.dw_pre is not None:
             assert not got.dw_pre.any()
+
+
+def test_inputs_dropped_while_another_stream_still_reads_them():
+    # the stream is busy, the caller drops its only references and fills as much memory with something else
+    import torch
+    v, f, dy, h0 = scan_inputs(2, 700, 192, "bf16", 6)
+    x, b, dxo, dn = (torch.randn(1500, 320, device="cuda").bfloat16() for _ in range(4))
+    w = torch.rand(320, device="cuda") + 0.5
+    mats = [torch.randn(96, 160, device="cuda") for _ in range(3)]
+    plan = mwb.Orth(96, 160, 3, "f32")
+    y, hl, st = mwb.gated_scan(v, f, h0=h0, keep_states=True)
+    g = mwb.gated_scan_backward(v, f, dy, st)
+    xo, n, rms = mwb.residual_norm(x, b, w_post=w, w_pre=w, keep_rms=True)
+    gn = mwb.residual_norm_backward(x, b, rms, w_post=w, w_pre=w, dx_out=dxo, dn=dn)
+    X = plan.project(mats, plan.alloc_workspace())
+    s = torch.cuda.Stream()
+    calls = [((v, f, h0), lambda v, f, h0: mwb.gated_scan(v, f, h0=h0, stream=s), (y, hl)),
+             ((v, f, dy, st), lambda v, f, dy, st: mwb.gated_scan_backward(v, f, dy, st, stream=s), g),
+             ((x, b, w), lambda x, b, w: mwb.residual_norm(x, b, w_post=w, w_pre=w, stream=s), (xo, n)),
+             ((x, b, rms, w, dxo, dn),
+              lambda x, b, rms, w, dxo, dn: mwb.residual_norm_backward(x, b, rms, w_post=w, w_pre=w, dx_out=dxo, dn=dn, stream=s),
+              (gn.dx, gn.db, None, gn.dw_post, None, gn.dw_pre)),
+             (tuple(mats) + (plan.alloc_workspace(),),
+              lambda *t: plan.project(t[:3], t[3], out=[torch.empty_like(m) for m in t[:3]], stream=s), X)]
+    for inputs, call, want in calls:
+        copies = [t.clone() for t in inputs]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(20_000_000)
+        got = call(*copies)
+        del copies
+        other = [torch.full_like(t, 7) for t in inputs for _ in range(2)]
+        torch.cuda.synchronize()
+        assert len(got) == len(want)
+        for p, q in zip(got, want):
+            assert (p is None and q is None) or torch.equal(p, q)
+        del other

@@ -225,3 +225,51 @@ def test_orth_refuses_a_stream_of_another_device(devices, recorder):
         with pytest.raises(ValueError):
             bad()
     assert len(recorder.calls) == n
+
+
+@pytest.fixture
+def streams(monkeypatch, devices):
+    """Which tensors (by address) were marked as used on which stream, in the order of the calls."""
+    marks = []
+    here = Stream(1)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw).as_subclass(OnSecond))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: here)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: marks.append((t.data_ptr(), s)))
+    return marks
+
+
+def test_everything_a_call_on_another_stream_touches_is_marked_for_it(streams, recorder):
+    # memory of a tensor that the caller drops after the call is not given out before the work there is done
+    s = Stream(1)
+
+    def check(tensors, call):
+        streams.clear()
+        call()
+        for i, t in enumerate(tensors):
+            assert (t.data_ptr(), s) in streams, i
+
+    v, f, dy, y, dv, df = (second(B, T, D) for _ in range(6))
+    h0, hl, dh = (second(B, D) for _ in range(3))
+    reset = torch.zeros((B, T), dtype=torch.uint8).as_subclass(OnSecond)
+    lengths = torch.full((B,), T, dtype=torch.int32).as_subclass(OnSecond)
+    st = second(B, -(-T // mwb.SCAN_STATE_EVERY), D)
+    check([v, f, reset, lengths, h0, y, hl],
+          lambda: mwb.gated_scan(v, f, reset=reset, lengths=lengths, h0=h0, y=y, h_last=hl, stream=s))
+    check([v, f, dy, st, reset, lengths, dh, dv, df],
+          lambda: mwb.gated_scan_backward(v, f, dy, st, reset=reset, lengths=lengths, dh_last=dh, dv=dv, df=df, stream=s))
+    x, b, z, xo, n, dxo, dn = (second(R, D) for _ in range(7))
+    wp, sc, wn = (second(D) for _ in range(3))
+    rms = second(2, R)
+    kw = dict(z=z, w_post=wp, scale=sc, w_pre=wn, stream=s)
+    check([x, b, z, wp, sc, wn, xo, n], lambda: mwb.residual_norm(x, b, x_out=xo, n=n, **kw))
+    check([x, b, z, wp, sc, wn, rms, dxo, dn], lambda: mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, **kw))
+    plan = mwb.Orth(8, 8, 2, "f32")
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    W, G, M = orth_lists()
+    W2, M2, _ = orth_lists()
+    check(W + G + M + W2 + M2 + [ws],
+          lambda: plan.step(W, G, M, ws, lr=0.1, params_out=W2, momentum_out=M2, stream=s))
+    check(W + W2 + [ws], lambda: plan.project(W, ws, out=W2, stream=s))
+    check(W + [ws], lambda: plan.project(W, ws, stream=s))
