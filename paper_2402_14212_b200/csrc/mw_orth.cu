@@ -1203,8 +1203,9 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   }
   OrthWs l;
   orth_layout(p, ws, &l);
+  // status and counters (ahead of the maps: their encoder wants a context, which a thread's first runtime call makes)
+  MW_CUDA_OK(cudaMemsetAsync(ws, 0, 1024 + l.done_bytes, s));
   MW_TRY(orth_maps(p, l, ws));
-  MW_CUDA_OK(cudaMemsetAsync(ws, 0, 1024 + l.done_bytes, s));     // status and counters
   const int64_t mn = (int64_t)m * n, rowlen = p->tall ? m : n;
   const double sx = orth_sx(n);
   // blocks of the momentum pass: about eight an SM over all matrices

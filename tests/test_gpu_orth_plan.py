@@ -1,0 +1,29 @@
+"""Plans of the orthogonalised update and threads."""
+import threading
+
+import pytest
+
+from paper_2402_14212_b200 import binding as mwb
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_call_may_be_its_threads_first_touch_of_the_device():
+    import torch
+    plan = mwb.Orth(300, 260, 2, "bf16_f32acc")
+    mats = [torch.randn(300, 260, device="cuda").bfloat16() for _ in range(2)]
+    spaces, bad = [plan.alloc_workspace() for _ in range(2)], []
+    want = plan.project(mats, spaces[0])
+    out = [torch.empty_like(m) for m in mats]
+    torch.cuda.synchronize()
+
+    def work():
+        try:
+            plan.project(mats, spaces[1], out=out)
+        except Exception as e:          # noqa: BLE001 (reported below)
+            bad.append(e)
+
+    t = threading.Thread(target=work)
+    t.start()
+    t.join(120)
+    assert not bad and plan.status(spaces[1]) == 0 and all(torch.equal(p, q) for p, q in zip(out, want))
