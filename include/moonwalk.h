@@ -402,7 +402,8 @@ typedef struct {
   int32_t reserved;           /* 0 */
   double coef[3];             /* c0, c1, c2; all zero = 3.4445, -4.7750, 2.0315 */
 } mw_orth_desc;
-typedef struct mw_orth mw_orth; /* opaque, host side; owns no device memory */
+typedef struct mw_orth mw_orth; /* opaque, host side; owns no device memory.  Threads may share a plan, each
+                                   call with a workspace that no other call in flight uses */
 mw_status mw_orth_create(const mw_orth_desc* desc, mw_orth** out);
 void mw_orth_destroy(mw_orth* plan);
 mw_status mw_orth_workspace_bytes(const mw_orth* plan, size_t* bytes);

@@ -24,6 +24,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <mutex>
 #include <new>
 
 #include "mw_tc_gemm.cuh"
@@ -43,7 +44,9 @@ struct mw_orth {
   double c[3];
   int mp, np;          // padded sides: multiples of 256 and 128
   bool small;          // one CTA a matrix, everything in shared memory
-  // tensor maps of a workspace, encoded when the workspace first comes along
+  // tensor maps of a workspace, encoded when the workspace first comes along; calls on one plan may come from
+  // several threads, so they are read and written under the lock
+  std::mutex lock;
   const void* mapped = nullptr;
   CUtensorMap maps[13];
 };
@@ -1053,8 +1056,13 @@ mw_status half_map(const __half* base, int rows, int cols, int64_t planes, int b
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? MW_OK : MW_ERR_CUDA;
 }
 
-mw_status orth_maps(mw_orth* p, const OrthWs& l, const void* ws) {
-  if (p->mapped == ws) return MW_OK;
+// the maps of a workspace into `out`
+mw_status orth_maps(mw_orth* p, const OrthWs& l, const void* ws, CUtensorMap* out) {
+  std::lock_guard<std::mutex> held(p->lock);
+  if (p->mapped == ws) {
+    for (int i = 0; i < MAP_COUNT; ++i) out[i] = p->maps[i];
+    return MW_OK;
+  }
   p->mapped = nullptr;
   const int64_t c = p->d.count;
   const int t = p->terms;
@@ -1070,6 +1078,7 @@ mw_status orth_maps(mw_orth* p, const OrthWs& l, const void* ws) {
   for (int b = 0; b < 2; ++b) MW_TRY(half_map(l.x[b], p->mp, p->np, 2 * c, kBK, 64, t, S128, &p->maps[MAP_XK64 + b]));
   MW_TRY(half_map(l.a, p->mp, p->mp, t * c, kBK, 64, t, S128, &p->maps[MAP_A64]));
   p->mapped = ws;
+  for (int i = 0; i < MAP_COUNT; ++i) out[i] = p->maps[i];
   return MW_OK;
 }
 
@@ -1205,7 +1214,8 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   orth_layout(p, ws, &l);
   // status and counters (ahead of the maps: their encoder wants a context, which a thread's first runtime call makes)
   MW_CUDA_OK(cudaMemsetAsync(ws, 0, 1024 + l.done_bytes, s));
-  MW_TRY(orth_maps(p, l, ws));
+  static thread_local OrthParams q;
+  MW_TRY(orth_maps(p, l, ws, q.map));
   const int64_t mn = (int64_t)m * n, rowlen = p->tall ? m : n;
   const double sx = orth_sx(n);
   // blocks of the momentum pass: about eight an SM over all matrices
@@ -1234,8 +1244,6 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
         l.x[0] + (size_t)first * 2 * p->mp * p->np);
     MW_TRY(launch_ok(2));
   }
-  static thread_local OrthParams q;
-  for (int i = 0; i < MAP_COUNT; ++i) q.map[i] = p->maps[i];
   q.count = count;
   q.tm = p->mp / kTile;
   q.steps = p->steps;

@@ -27,3 +27,30 @@ def test_a_call_may_be_its_threads_first_touch_of_the_device():
     t.start()
     t.join(120)
     assert not bad and plan.status(spaces[1]) == 0 and all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+def test_threads_share_a_plan_with_a_workspace_each():
+    import torch
+    plan = mwb.Orth(300, 260, 2, "bf16_f32acc")
+    inputs = [[torch.randn(300, 260, device="cuda").bfloat16() for _ in range(2)] for _ in range(4)]
+    want = [plan.project(m, plan.alloc_workspace()) for m in inputs]
+    spaces = [plan.alloc_workspace() for _ in inputs]
+    bad, start = [], threading.Barrier(len(inputs))
+
+    def work(i):
+        try:
+            start.wait(20)
+            got = [plan.project(inputs[i], spaces[i]) for _ in range(40)]
+            torch.cuda.synchronize()
+            if not all(torch.equal(p, q) for g in got for p, q in zip(g, want[i])):
+                bad.append(i)
+        except Exception as e:          # noqa: BLE001 (reported below)
+            bad.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(inputs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(120)
+    assert not bad and not any(t.is_alive() for t in threads)
+    assert all(plan.status(ws) == 0 for ws in spaces)
