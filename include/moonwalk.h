@@ -410,7 +410,8 @@ mw_status mw_orth_workspace_bytes(const mw_orth* plan, size_t* bytes);
 /* Host arrays of `count` DEVICE pointers, matrices dense and row-major: grads, momentum, momentum_out
  * float; params, params_out storage type of `prec`.  momentum_out[i] may be momentum[i], params_out[i]
  * may be params[i].  workspace: device, 256-byte aligned.  A bounded wait that runs out inside the
- * launch is recorded in the workspace (mw_orth_status). */
+ * launch is recorded in the workspace (mw_orth_status); params_out then stays as it was (of small
+ * matrices, those that ran out), while momentum_out holds M'. */
 mw_status mw_orth_step(mw_orth* plan, const void* const* params, const void* const* grads,
                        const void* const* momentum, void* const* params_out, void* const* momentum_out,
                        double lr, double beta, double weight_decay, double scale, void* workspace,
@@ -421,6 +422,9 @@ mw_status mw_orth_project(mw_orth* plan, const void* const* in, void* const* out
 /* Synchronise `stream`, return the first device-side error recorded in the workspace by the last call
  * (MW_OK if none). */
 mw_status mw_orth_status(const mw_orth* plan, const void* workspace, void* stream);
+/* Self-test: the plan's next calls hold a wait that nothing meets and that runs out after limit_ms (1..1000), as
+ * a lost signal would; 0 ends it. */
+mw_status mw_orth_selftest_unmet_wait(mw_orth* plan, uint32_t limit_ms);
 
 /* ---- whole step from host buffers, and measurement hooks --------------------------------- */
 

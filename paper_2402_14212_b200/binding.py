@@ -125,6 +125,7 @@ def lib() -> C.CDLL:
         L.mw_orth_step.argtypes = [vp] + [C.POINTER(vp)] * 5 + [C.c_double] * 4 + [vp, sz, vp]
         L.mw_orth_project.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), vp, sz, vp]
         L.mw_orth_status.argtypes = [vp, vp, vp]
+        L.mw_orth_selftest_unmet_wait.argtypes = [vp, C.c_uint32]
         L.mw_profile_begin.argtypes = []
         L.mw_profile_begin.restype = None
         L.mw_profile_end.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64),
@@ -818,7 +819,8 @@ class Orth:
     def step(self, params, grads, momentum, workspace, lr: float, beta: float = 0.95, weight_decay: float = 0.0,
              scale: float = 1.0, params_out=None, momentum_out=None, stream=None):
         """M <- beta M + G, W <- (1 - lr weight_decay) W - lr scale X; in place unless outputs are given.  With
-        `stream` the work runs there, after what that stream was given before."""
+        `stream` the work runs there, after what that stream was given before.  Where status() then tells of a wait
+        that ran out, the weights are as they were."""
         import torch
         params_out = params if params_out is None else params_out
         momentum_out = momentum if momentum_out is None else momentum_out
@@ -846,6 +848,10 @@ class Orth:
         _check(_call("mw_orth_project", workspace.device, self._h, self._list(mats, st, "mats", workspace),
                      self._list(out, st, "out", workspace), wp, wb), "mw_orth_project")
         return out
+
+    def selftest_unmet_wait(self, limit_ms: int):
+        """The next calls hold a wait that nothing meets and that runs out after limit_ms (0 ends it)."""
+        _check(lib().mw_orth_selftest_unmet_wait(self._h, int(limit_ms)), "mw_orth_selftest_unmet_wait")
 
     def status(self, workspace, stream=None) -> int:
         """Waits for the stream; the first device-side error of the last call on this workspace (0: none)."""

@@ -44,6 +44,7 @@ struct mw_orth {
   double c[3];
   int mp, np;          // padded sides: multiples of 256 and 128
   bool small;          // one CTA a matrix, everything in shared memory
+  uint32_t unmet_ms = 0;     // self-test: a wait that nothing meets, and its limit (0: none)
   // tensor maps of a workspace, encoded when the workspace first comes along; calls on one plan may come from
   // several threads, so they are read and written under the lock
   std::mutex lock;
@@ -115,6 +116,7 @@ struct alignas(64) OrthParams {
   unsigned* done;                // [step][phase][matrix][row of tiles]
   DeviceStatus* st;
   uint64_t wait_ns;
+  unsigned unmet;                // self-test: counts that B's tiles wait for and nothing adds
 };
 
 struct OrthUnit { int step, phase, mat, ti, tj, n0, bn, nkb, pieces; };      // tj: the row of tiles that column n0 mirrors to
@@ -266,7 +268,7 @@ orth_products_kernel(const __grid_constant__ OrthParams p) {
   wc.st = p.st;
   wc.abort_flag = &abort_flag;
   wc.limit_ns = p.wait_ns;
-  const unsigned sym_rows = (unsigned)(p.tm * (kTile / p.bn_sym)) * 2, x_rows = (unsigned)p.tn * 2;      // one count a CTA and tile
+  const unsigned sym_rows = (unsigned)(p.tm * (kTile / p.bn_sym)) * 2 + p.unmet, x_rows = (unsigned)p.tn * 2;      // one count a CTA and tile
 
   if (warp < kOrthFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
@@ -768,12 +770,14 @@ orth_start_kernel(const __grid_constant__ OrthPtrs ptr, int m, int n, int mp, in
   *reinterpret_cast<uint4*>(to + (int64_t)mp * np) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
-// W' = keep W - step X, or X itself, from the two planes of the last X
+// W' = keep W - step X, or X itself, from the two planes of the last X.  Where a wait of the products ran out there is
+// no X, and the outputs, which may be the weights themselves, stay as they are.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 orth_apply_kernel(const __grid_constant__ OrthPtrs ptr, int m, int n, int mp, int np, int tall, const __half* __restrict__ x,
-                  float out_scale, float keep, float step) {
+                  float out_scale, float keep, float step, const DeviceStatus* __restrict__ st) {
   __shared__ float tile[64][33];
+  if (st->code != 0) return;
   const int i = blockIdx.z, row0 = blockIdx.y * 32, col0 = blockIdx.x * 64;
   const int a = threadIdx.x >> 3, b = (threadIdx.x & 7) * 8;
   const __half* from = x + (int64_t)i * 2 * mp * np + (int64_t)(row0 + a) * np + col0 + b;
@@ -823,6 +827,7 @@ struct OrthSmall {
   double sx;
   DeviceStatus* st;
   uint64_t wait_ns;
+  unsigned unmet;       // self-test: the first product is not started
 };
 constexpr uint32_t kGroupBytes = 128 * 128;
 
@@ -921,7 +926,7 @@ orth_small_kernel(const __grid_constant__ OrthPtrs ptr, const __grid_constant__ 
       tc_fence_before();
       __syncthreads();
       const uint32_t d = tmem + (ph == 2 ? (uint32_t)(mg * 64) : 0u);
-      if (threadIdx.x == 0) {
+      if (threadIdx.x == 0 && !p.unmet) {
         tc_fence_after();
         const int N = ph == 2 ? ng * 64 : mg * 64, ks = ph == 0 ? ng * 4 : (m + 15) / 16;
         const uint32_t idesc = (1u << 4) | ((ph == 2 ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
@@ -1001,6 +1006,7 @@ orth_small_kernel(const __grid_constant__ OrthPtrs ptr, const __grid_constant__ 
   tc_fence_after();
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+  if (!ok) return;                 // no X: the outputs stay as they are
   const T* w = static_cast<const T*>(ptr.w[i]);
   T* out = static_cast<T*>(ptr.out[i]);
   for (int k = threadIdx.x; k < m * n; k += 256) {
@@ -1192,7 +1198,8 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
     q.m = m; q.n = n; q.tall = p->tall; q.steps = p->steps; q.nesterov = p->d.nesterov;
     q.beta = (float)beta; q.keep = (float)(1.0 - lr * wd); q.step = (float)(lr * scale);
     q.st = reinterpret_cast<DeviceStatus*>(ws);
-    q.wait_ns = kOrthWaitNs;
+    q.wait_ns = p->unmet_ms ? p->unmet_ms * 1000000ull : kOrthWaitNs;
+    q.unmet = p->unmet_ms != 0;
     for (int first = 0; first < count; first += kPtrGroup) {
       const int c = count - first < kPtrGroup ? count - first : kPtrGroup;
       static thread_local OrthPtrs ptr;
@@ -1254,7 +1261,8 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
   q.f = orth_factors(p, sx);
   q.done = l.done;
   q.st = reinterpret_cast<DeviceStatus*>(ws);
-  q.wait_ns = kOrthWaitNs;
+  q.wait_ns = p->unmet_ms ? p->unmet_ms * 1000000ull : kOrthWaitNs;
+  q.unmet = p->unmet_ms != 0;
   q.stage_bytes = (uint32_t)p->terms * (kPlaneBytes + (uint32_t)set_columns(p->terms) / 2u * kBK * 2u);
   q.stages = 4;
   const size_t smem = 1024 + (size_t)q.stages * q.stage_bytes + kOrthEpi * staging_buffers(p->terms) * kBuffer;
@@ -1271,7 +1279,7 @@ mw_status orth_run(mw_orth* p, const void* const* params, const void* const* gra
     auto k3 = wide ? orth_apply_kernel<T, true> : orth_apply_kernel<T, false>;
     k3<<<dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 32), (unsigned)c), 256, 0, s>>>(
         ptr, m, n, p->mp, p->np, p->tall, l.x[p->steps & 1] + (size_t)first * 2 * p->mp * p->np, q.f.out_scale,
-        (float)(1.0 - lr * wd), (float)(lr * scale));
+        (float)(1.0 - lr * wd), (float)(lr * scale), q.st);
     MW_TRY(launch_ok());
   }
   return MW_OK;
@@ -1364,6 +1372,12 @@ extern "C" mw_status mw_orth_project(mw_orth* plan, const void* const* in, void*
   char* ws = static_cast<char*>(workspace);
   return plan->d.prec == MW_F32 ? orth_run<float>(plan, nullptr, nullptr, nullptr, out, nullptr, in, 0, 0, 0, 0, ws, s)
                                 : orth_run<__nv_bfloat16>(plan, nullptr, nullptr, nullptr, out, nullptr, in, 0, 0, 0, 0, ws, s);
+}
+
+extern "C" mw_status mw_orth_selftest_unmet_wait(mw_orth* plan, uint32_t limit_ms) {
+  if (!plan || limit_ms > 1000) return MW_ERR_INVALID_ARG;
+  plan->unmet_ms = limit_ms;
+  return MW_OK;
 }
 
 extern "C" mw_status mw_orth_status(const mw_orth* plan, const void* workspace, void* stream) {
