@@ -532,16 +532,22 @@ def _raw_stream(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _current_device() -> int:
+    import torch
+    return torch._C._cuda_getDevice()
+
+
 def _call(name, device, *args, stream=None) -> int:
     """A library call with `device` current, on `stream` or the device's current stream: the library launches, and
     asks for the number of SMs, on the current device.  Returns its status."""
+    if stream is not None:
+        _need(stream.device == device, f"{name}: a stream of {device}")
+    call, handle = getattr(lib(), name), _raw_stream(stream, device)
+    if _current_device() == device.index:
+        return call(*args, handle)
     import torch
-    _need(stream is None or stream.device == device, f"{name}: a stream of {device}")
-    handle = _raw_stream(stream, device)
-    if torch.cuda.current_device() == device.index:
-        return getattr(lib(), name)(*args, handle)
     with torch.cuda.device(device):
-        return getattr(lib(), name)(*args, handle)
+        return call(*args, handle)
 
 
 def _keep_for(stream, *things):

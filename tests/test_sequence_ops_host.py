@@ -36,7 +36,7 @@ def recorder(monkeypatch):
     monkeypatch.setattr(mwb, "lib", lambda: rec)
     monkeypatch.setattr(mwb, "_raw_stream", lambda stream, device: 0)
     monkeypatch.setattr(mwb, "_passed", {})
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: torch.device("cpu").index)
+    monkeypatch.setattr(mwb, "_current_device", lambda: torch.device("cpu").index)
     monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
     # bytes from the address of a tensor that was asked for it to the end of its memory
     rec.room = {}
@@ -72,7 +72,7 @@ def devices(monkeypatch, recorder):
         def __exit__(self, *_):
             current[0] = self.before
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(mwb, "_current_device", lambda: current[0])
     monkeypatch.setattr(torch.cuda, "device", Device)
     recorder.at = []
     plain = Recorder.__getattr__
