@@ -468,13 +468,13 @@ norm_backward_kernel(const NormArgs a, const NormPlan p) {
           slope[k][i] = sig * fmaf(vz[i], 1.f - sig, 1.f);
         }
         const float tau = ks[k][i] * (vb[i] * inv_b) * gate[k][i];
-        xh[k][i] = has_n ? (has_b ? vx[i] + tau : vx[i]) * xs : 0.f;
+        xh[k][i] = (has_b ? vx[i] + tau : vx[i]) * xs;
         const float q = vn[i] * wn[k][i];
         A[k][i] = fmaf(q, inv_x, vo[i]);
         s[0] = fmaf(q, xh[k][i], s[0]);
         s[1] = fmaf(A[k][i], tau, s[1]);
         s[2] = fmaf(xh[k][i], tau, s[2]);
-        if (live) acc_n[k][i] = fmaf(vn[i], xh[k][i], acc_n[k][i]);
+        if (live && has_n) acc_n[k][i] = fmaf(vn[i], xh[k][i], acc_n[k][i]);
       }
     }
     if (base + stride < a.rows) load(row + stride);
@@ -490,7 +490,9 @@ norm_backward_kernel(const NormArgs a, const NormPlan p) {
       P::get(cb[k], vb);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float dx = fmaf(-xh[k][i], m1, A[k][i]), bh = vb[i] * inv_b, dk = dx * ks[k][i], dg = dx * gate[k][i];
+        float dx = A[k][i];
+        if (has_n) dx = fmaf(-xh[k][i], m1, dx);
+        const float bh = vb[i] * inv_b, dk = dx * ks[k][i], dg = dx * gate[k][i];
         ox[i] = dx;
         ob[i] = fmaf(dk * gate[k][i], inv_b, -bh * m2);
         oz[i] = dk * bh * slope[k][i];
