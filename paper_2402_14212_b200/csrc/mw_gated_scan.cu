@@ -999,15 +999,16 @@ mw_status run_scan(const ScanArgs& p, bool backward, cudaStream_t s) {
   const int64_t e = sizeof(T);
   const int64_t places = (p.D | p.v_b | p.v_t | p.f_b | p.f_t | p.y_b | p.y_t | p.dv_b | p.dv_t | p.df_b | p.df_t) * e |
                          (int64_t)((uintptr_t)p.v | (uintptr_t)p.f | (uintptr_t)p.y | (uintptr_t)p.dy | (uintptr_t)p.dv | (uintptr_t)p.df);
-  // A thread a channel where there is nothing to cut, up to kEvery steps, and up to four times as many where the
-  // channels alone give every SM four blocks (64x64x2048 bf16 forward 15 us, backward 26, 20 and 27 in chunks;
-  // 256x32x2048 25 and 49, 72 and 106; but 8x64x2048 13 and 11, 4 and 5 in chunks).
+  // A thread a channel where there is nothing to cut, up to kEvery steps, and up to four times as many (twice in the
+  // backward pass) where the channels alone give every SM four blocks.  In us, walked and in chunks, bf16, inputs
+  // above L2: 256x32x2048 forward 25 and 81, backward 71 and 113; 64x64x2048 17 and 22, 45 and 29; backward at 48
+  // steps even (256x48x2048 104 and 113, 64x48x2048 35 and 29); with few channels 8x64x2048 6.1 and 4.1, 9.3 and 5.3.
   // The chunk kernels also hold the offsets of kEvery rows in 32 bits, which only rows more than 2^26 bytes
   // apart do not fit.
   const int64_t most = (int64_t)1 << 26;
   const bool near = p.v_t * e < most && p.f_t * e < most && p.y_t * e < most && p.dv_t * e < most && p.df_t * e < most;
   const dim3 grid((unsigned)ceil_div(p.D, 128), (unsigned)p.B);
-  const int shortest = (int64_t)grid.x * grid.y >= 4 * kFewBlocks ? 4 * kEvery : kEvery;
+  const int shortest = (int64_t)grid.x * grid.y < 4 * kFewBlocks ? kEvery : backward ? 2 * kEvery : 4 * kEvery;
   if (p.T <= shortest || !near) {
     if (!backward) scan_walk_kernel<T, GATE><<<grid, 128, 0, s>>>(p);
     else if (p.T >= kEvery) scan_walk_back_kernel<T, GATE, true><<<grid, 128, 0, s>>>(p);

@@ -104,3 +104,11 @@ def test_recurrence_over_rows_far_apart(T, apart, dtype):
     scan.check(got, ref, V, dtype)
     for i, t in enumerate((v, f, dy)):
         assert torch.equal(at(i), t)
+
+
+# sequences of 30 to 70 steps with channels for every SM, on both sides of where the walk ends in either pass
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [30, 32, 33, 48, 64, 65])
+def test_short_sequences_of_many_channels(T, dtype):
+    got, ref, V = scan.run_both(230, T, 264, dtype, "energy", T % 2 == 0, seed=T)
+    scan.check(got, ref, V, dtype)
