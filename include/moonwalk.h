@@ -391,7 +391,9 @@ mw_status mw_residual_norm_backward(const mw_residual_norm_desc* desc, const voi
  * The polynomial drives every singular value of U that is not tiny towards 1, so a step moves all
  * directions of W alike; weights that started near a multiple of an orthogonal matrix stay in the
  * domain of the Newton-Schulz inverse far longer than under a plain gradient step.  A non-finite entry
- * of U makes its own matrix's result NaN and no other's. */
+ * of U makes its own matrix's result NaN and no other's.  (The update and the default coefficients are those
+ * that K. Jordan et al. published as the Muon optimizer, 2024; the iteration is Newton and Schulz's for the
+ * polar factor, with a quintic polynomial.) */
 typedef struct {
   int32_t rows, cols, count;
   int32_t prec;               /* MW_F32: W float; MW_BF16_F32ACC: W bf16.  G and M are float in both */

@@ -37,7 +37,10 @@ __device__ __forceinline__ float decay_of(float f) {
   return e;
 }
 // a = sigmoid(f) and w = 1 - a from exp(-f): one reciprocal gives both ends to their own relative accuracy.  Formed
-// by a subtraction, 1 - a would lose the slow channels, where a is close to 1, and a the fast ones.
+// by a subtraction, 1 - a would lose the slow channels, where a is close to 1, and a the fast ones.  The product
+// f log2(e) is rounded before the exponential, which makes the smaller of the two off by up to (|f| + 4) 2^-24 of
+// itself (measured: 5.8e-7 at |f| = 10, 9.5e-7 at 20; 1.6e-7 with the library's exponential).  bf16 results hide it a
+// thousand times over; a second term of the product would be two more instructions a gate.
 __device__ __forceinline__ void gate_from(float e, float& a, float& w) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.f + e));
   w = e * a;
@@ -67,7 +70,7 @@ __device__ __forceinline__ int length_of(const ScanArgs& p, int b) {
 // One thread per channel walks the whole sequence: the single steps of serving, short sequences, and rows so far
 // apart that the kernels below cannot address them.  Bound by latency: the rows of kAhead steps are asked for before
 // the first is used (eight wanted more registers than the waits were worth).
-// One step of 64x2048 bf16 takes 2 us, 256x16x2048 12 us forward and 26 backward (50 and 75 MB).
+// One step of 64x2048 bf16 takes 2 us, 256x16x2048 14 us forward and 39 backward (50 and 86 MB).
 constexpr int kAhead = 4;
 
 template <typename T, int GATE>
@@ -609,9 +612,9 @@ scan_chunk_back_kernel(const ScanArgs p) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// The same two kernels for rows that start on 16-byte boundaries.  They are bound by the issue of
-// instructions, and a third of those of the kernels above are loads, stores and their addresses, a row
-// of 64 or 128 bytes at a time.  Here a warp brings its kEvery rows of each tensor into shared memory by
+// The same two kernels for rows that start on 16-byte boundaries.  They are bound by latency at 16 warps an SM
+// (122 to 128 registers a thread; 60 to 63% of issue slots used), so instructions count twice: a third of those of the
+// kernels above are loads, stores and their addresses, a row of 64 or 128 bytes at a time.  Here a warp brings its kEvery rows of each tensor into shared memory by
 // asynchronous copies of 16 bytes a lane (four or eight rows an instruction), one piece ahead of its work,
 // reads them there at constant offsets, leaves its results in their place and stores those 16 bytes a lane.
 // ---------------------------------------------------------------------------------------------
@@ -921,8 +924,8 @@ mw_status fill_scan(const mw_gated_scan_desc* d, ScanArgs& p) {
 }
 
 // Blocks along time: doubled while the grid leaves SMs without one, as far as there are pieces of the sequence
-// for them.  Each doubling costs an exchange a piece: 8x2048x2048 bf16 (256 columns of blocks) takes 41 us with one
-// block along time and 51 us with two, 1x65536x1024 (32 of them) 484, 295, 156, 121 us with 1, 2, 4, 8.
+// for them.  Each doubling costs an exchange a piece: 8x2048x2048 bf16 (256 columns of blocks) takes 39 us with one
+// block along time and 51 us with two, 1x65536x1024 (32 of them, energy gate) 465, 294, 155, 119 us with 1, 2, 4, 8.
 int blocks_along_time(int64_t columns, int pieces) {
   int C = 1;
   while (C < kMaxCluster && C < pieces && columns * C < kFewBlocks) C *= 2;
@@ -965,15 +968,15 @@ mw_status launch_wide_back(const ScanArgs& p, cudaStream_t s) {
 }
 
 // `wide`: every row of every tensor starts on a 16-byte boundary; `pairs`: on a 4-byte one.
+// (Inputs above L2, complement gate.)
 //   - Where one exchange covers the sequence there is nothing to copy ahead of, and copies only add their latency:
-//     direct loads (64x128x2048 bf16, forward and backward: 25 and 37 us; 26 and 55 with copies).  Two bf16 channels a
-//     lane if that still gives every SM a block (25 us; one channel 36; but 1x512x1024 5.0 us, one channel 4.4).
-//   - Longer ones copy ahead (2x8192x1024 f32 backward 61 us, direct loads 71; forward 40 and 38).
+//     direct loads (64x128x2048 bf16, forward and backward: 27 and 40 us; 28 and 72 with copies).  Two bf16 channels a
+//     lane if that still gives every SM a block (one channel 38 and 51 us; but 1x512x1024 4.9 us, one channel 4.4).
+//   - Longer ones copy ahead (2x8192x1024 f32 backward 61 us, direct loads 74; forward 37 and 39).
 //   - bf16 then takes one channel a lane and uses the registers for twice the steps between two exchanges (1x65536x1024
-//     forward 111 us; 136 with 16 steps, 200 with two channels; backward 194, 206, above 300) ...
+//     forward 108 us; 134 with 16 steps, 200 with two channels; backward 195 and 205 with 16 steps) ...
 //   - ... except forward with more columns than the device holds blocks at once, which gains more from half the
-//     instructions (8x2048x2048 42 us with two channels, 46 with one; 4x4096x2048, with half the columns, 51 and 46;
-//     backward 80 and 79).
+//     instructions (8x2048x2048 39 us with two channels, 45 with one; 4x4096x2048, with half the columns, 48 and 44).
 template <typename T, int GATE, bool CUT>
 mw_status cut_scan(const ScanArgs& p, bool backward, bool wide, bool pairs, cudaStream_t s) {
   constexpr bool kNarrow = sizeof(T) == 2;       // bf16: two channels a lane are possible

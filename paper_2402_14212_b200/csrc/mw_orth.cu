@@ -11,8 +11,10 @@
 // both, and only the product B X sees the leading term alone; in the last two steps, where the spectrum
 // has reached its plateau, A is stored as A - alpha I and B as B + beta I (with c0 - beta in front of X), so
 // that what is rounded is the small difference.  One-term operands then give X to about 1e-3 (2e-3 at
-// rank-deficient U), where bf16 operands gave 1e-2 to 6e-2 on the same matrices.  Two-term operands
-// (leading term and remainder, three products of four) give fp32 accuracy.
+// rank-deficient U), where bf16 operands gave 1e-2 to 6e-2 on the same matrices: less than the 2e-3 that
+// rounding X to bf16 costs, which is why bf16 weights take them by default, but more than 32-bit products would
+// leave.  Two-term operands (leading term and remainder, three products of four) give fp32 accuracy, at three
+// times the work: 2 of 4096 x 4096 with bf16 weights 2.9 ms with one term, 9.0 ms with two.
 //
 // A and B are symmetric: tiles on and above the diagonal are computed, the others stored as their
 // transposes, 3 m^2 n + m^3 flops a step instead of 4 m^2 n + 2 m^3.
@@ -70,8 +72,9 @@ constexpr int kFewRegisters = 104, kManyRegisters = 200;
 // every instruction; over 64 K blocks of fp32-accurate products that came to errors of 1e-5 to 1e-4 of X, in
 // pieces of 4 blocks that the epilogue adds, rounding to nearest, to 2e-6 (an accumulator of their own for the
 // cross products changed nothing).  Pieces want accumulators to run ahead into while the epilogue stores a tile:
-// two-term tiles are 128 columns wide, which makes four of them (64 matrices of 1024 x 1024: 6.2 ms; 6.5 ms with two
-// of 256 columns, where the products wait for the epilogue)
+// two-term tiles are 128 columns wide, which makes four of them (64 matrices of 1024 x 1024: 6.1 ms; 6.5 ms with two
+// of 256 columns, where the products wait for the epilogue).  The two-term epilogue spills: 268 bytes a thread
+// stored, 344 loaded, of sums and mirrored rows held at once.
 constexpr int kPieceBlocks = 4;
 __host__ __device__ constexpr int set_columns(int terms) { return terms == 1 ? 256 : 128; }
 __host__ __device__ constexpr int set_count(int terms) { return kTmemColumns / set_columns(terms); }
