@@ -10,7 +10,9 @@ Block (x: residual stream [batch * time, width], n: its normed copy):
 
 The net behind it sees every position as a sample.  Its `mw_input_cotangent` gives g0 = dL/dx_0, which is the
 cotangent of the stack's output: the blocks' backward calls carry it on from there, while the net's forward
-sweep forms its own gradients.  Everything runs in the library; torch holds the memory.
+sweep forms its own gradients.  Products, recurrence, norms, the net and the updates of its weights and of the projections
+run in the library; torch holds the memory, adds the fixed bias of f, puts dz beside dv and df, and takes the plain
+gradient steps of the per-channel weights.
 """
 from __future__ import annotations
 
