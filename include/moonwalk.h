@@ -399,8 +399,9 @@ typedef struct {
   int32_t prec;               /* MW_F32: W float; MW_BF16_F32ACC: W bf16.  G and M are float in both */
   int32_t steps;              /* 0 = 5; at most 16 */
   int32_t nesterov;           /* 1: U = G + beta M';  0: U = M' */
-  int32_t terms;              /* operand terms of the products: 1 (about 1e-3 of X), 2 (fp32-accurate),
-                                 0 = 2 for MW_F32, 1 for MW_BF16_F32ACC */
+  int32_t terms;              /* operand terms of the products: 1 (1e-3 of X; up to 9e-3 where the shorter
+                                 side is below 32), 2 (fp32-accurate), 0 = 2 for MW_F32 and for
+                                 MW_BF16_F32ACC up to 128 x 256 or with a side below 32, else 1 */
   int32_t reserved;           /* 0 */
   double coef[3];             /* c0, c1, c2; all zero = 3.4445, -4.7750, 2.0315 */
 } mw_orth_desc;

@@ -779,7 +779,8 @@ def residual_norm_backward(x, b, inv_rms, z=None, w_post=None, scale=None, w_pre
 class Orth:
     """Host-side handle of the orthogonalised update (mw_orth) of `count` weights of one shape.  Owns no
     device memory.  `prec` is the weights' storage; `terms` the accuracy of X: 1 (about 1e-3, the default for bf16
-    weights) or 2 (fp32 accuracy at three times the work, the default for float ones)."""
+    weights that are neither small nor of few rows) or 2 (fp32 accuracy at three times the work, the default
+    elsewhere)."""
 
     def __init__(self, rows: int, cols: int, count: int = 1, prec: str = "f32", steps: int = 0,
                  nesterov: bool = True, terms: int = 0, coef=(0.0, 0.0, 0.0)):

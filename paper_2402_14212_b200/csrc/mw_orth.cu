@@ -12,8 +12,8 @@
 // has reached its plateau, A is stored as A - alpha I and B as B + beta I (with c0 - beta in front of X), so
 // that what is rounded is the small difference.  One-term operands then give X to about 1e-3 (2e-3 at
 // rank-deficient U), where bf16 operands gave 1e-2 to 6e-2 on the same matrices: less than the 2e-3 that
-// rounding X to bf16 costs, which is why bf16 weights take them by default, but more than 32-bit products would
-// leave.  Two-term operands (leading term and remainder, three products of four) give fp32 accuracy, at three
+// rounding X to bf16 costs, which is why bf16 weights of 32 rows and more take them by default, but more than 32-bit
+// products would leave.  Two-term operands (leading term and remainder, three products of four) give fp32 accuracy, at three
 // times the work: 2 of 4096 x 4096 with bf16 weights 2.9 ms with one term, 9.0 ms with two.
 //
 // A and B are symmetric: tiles on and above the diagonal are computed, the others stored as their
@@ -837,6 +837,7 @@ constexpr uint32_t kGroupBytes = 128 * 128;
 __host__ __device__ constexpr uint32_t small_bytes(int m, int n, int terms) {
   return (uint32_t)(2 * ((n + 63) / 64) + terms * ((m + 63) / 64)) * kGroupBytes;
 }
+constexpr int kSmallRows = 128, kSmallColumns = 256;
 // byte offset of the 16 bytes that hold columns c .. c + 7 (c a multiple of 8) of row r
 __device__ __forceinline__ uint32_t small_at(int r, int c) {
   return (uint32_t)(c >> 6) * kGroupBytes + (uint32_t)r * 128u + (uint32_t)((((c & 63) >> 3) ^ (r & 7)) << 4);
@@ -1328,8 +1329,14 @@ extern "C" mw_status mw_orth_create(const mw_orth_desc* desc, mw_orth** out) {
   p->m = p->tall ? d.cols : d.rows;
   p->n = p->tall ? d.rows : d.cols;
   p->steps = d.steps ? d.steps : 5;
-  p->terms = d.terms ? d.terms : (d.prec == MW_F32 ? 2 : 1);
-  p->small = p->m <= 128 && p->n <= 256 && small_bytes(p->m, p->n, p->terms) <= 200u * 1024u;
+  // bf16 weights: one term where its error stays below the rounding to bf16 and a second one costs.  Rows share the
+  // error between them: 2.3e-3 of X at the most for 26 rows, 9e-3 for two (2e-6 with two terms, whatever the size); and in
+  // one CTA a matrix the second term is cheap (64 of 64 x 64 projected in 37 us, 33 with one; 16 of 31 x 1024, which
+  // is not, 197 and 139).
+  const bool few = p->m < 32, in_one = p->m <= kSmallRows && p->n <= kSmallColumns;
+  p->terms = d.terms ? d.terms : (d.prec == MW_F32 || few || in_one ? 2 : 1);
+  static_assert(small_bytes(kSmallRows, kSmallColumns, 2) <= 200u * 1024u, "X and A in one SM's shared memory");
+  p->small = in_one;
   p->mp = (int)align_up((size_t)p->m, kTile);
   p->np = (int)align_up((size_t)p->n, kHalf);
   const bool given = d.coef[0] != 0.0 || d.coef[1] != 0.0 || d.coef[2] != 0.0;

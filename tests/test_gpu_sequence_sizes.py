@@ -112,3 +112,35 @@ def test_recurrence_over_rows_far_apart(T, apart, dtype):
 def test_short_sequences_of_many_channels(T, dtype):
     got, ref, V = scan.run_both(230, T, 264, dtype, "energy", T % 2 == 0, seed=T)
     scan.check(got, ref, V, dtype)
+
+
+# bf16 weights of few rows, or small ones, take two-term products: the same bits as when two are asked for.  (One-term
+# products leave up to 9e-3 of X where only a few singular values share the error.)
+@pytest.mark.parametrize("shape", [(1, 1, 20), (1, 6, 70), (2, 13, 70), (13, 2, 70), (3, 207, 30), (26, 123, 30), (64, 64, 8),
+                                   (128, 256, 4), (3, 700, 20), (31, 1000, 4), (2000, 5, 6)], ids=lambda s: "x".join(map(str, s)))
+def test_bf16_matrices_that_are_small_or_of_few_rows_take_two_terms(shape):
+    import torch
+    rows, cols, count = shape
+    U = [torch.randn(rows, cols, device="cuda").bfloat16() for _ in range(count)]
+    got = []
+    for terms in (0, 2):
+        plan = mwb.Orth(rows, cols, count, "bf16_f32acc", terms=terms)
+        ws = plan.alloc_workspace()
+        got.append(plan.project(U, ws))
+        assert plan.status(ws) == 0
+    assert all(torch.equal(p, q) for p, q in zip(*got))
+
+
+# ... and two-term products are right there: fp32 weights, the tolerance of the other shapes
+@pytest.mark.parametrize("shape", [(1, 1, 20), (1, 6, 70), (2, 13, 70), (13, 2, 70), (3, 207, 30), (26, 123, 30), (3, 700, 20),
+                                   (31, 1000, 4), (2000, 5, 6)], ids=lambda s: "x".join(map(str, s)))
+def test_projection_of_matrices_of_few_rows(shape):
+    import torch
+    rows, cols, count = shape
+    plan = mwb.Orth(rows, cols, count, "f32")
+    U = torch.randn(count, rows, cols, device="cuda")
+    ws = plan.alloc_workspace()
+    X = torch.stack(plan.project(list(U), ws)).double()
+    want = project64(U)
+    err = torch.linalg.matrix_norm(X - want) / torch.linalg.matrix_norm(want)
+    assert plan.status(ws) == 0 and float(err.max()) <= 1e-4
