@@ -429,6 +429,76 @@ mw_status mw_orth_status(const mw_orth* plan, const void* workspace, void* strea
  * a lost signal would; 0 ends it. */
 mw_status mw_orth_selftest_unmet_wait(mw_orth* plan, uint32_t limit_ms);
 
+/* ---- the two ends of a token model, and the bound of its step (extensions) ------------------------
+ *
+ * Tokens enter a stack through rows of a table; a vocabulary's softmax cross entropy ends it and hands
+ * its cotangent back; the gradients of a step are bounded by their common norm.  dtype: 1 = float, 2 = bf16
+ * (grad_dtype 0 = dtype).  Sums are float or wider and in a fixed order: repeated calls give the same bits.
+ * Sizes of zero (tokens, rows, tensors) are legal. */
+
+/* Lookup with scaling, and its gradient:
+ *   out_i = scale * table[tokens_i]           (a row of zeros where tokens_i is not in 0..vocab-1)
+ *   dtable_v = scale * sum over {i: tokens_i = v} of dout_i, in the order of i */
+typedef struct {
+  int64_t tokens;             /* 0..2^30 */
+  int32_t vocab, dim;         /* >= 1 */
+  int32_t dtype;              /* of table, out, dout */
+  int32_t grad_dtype;         /* of dtable */
+  int32_t index_bytes;        /* tokens are int32 (4) or int64 (8) */
+  int32_t reserved;           /* 0 */
+  int64_t ld_table, ld_out, ld_dtable; /* elements between rows (0 = dim); ld_out: of out and of dout */
+  double scale;
+} mw_embedding_desc;
+mw_status mw_embedding_forward(const mw_embedding_desc* desc, const void* tokens, const void* table, void* out,
+                               void* stream);
+mw_status mw_embedding_scratch_bytes(const mw_embedding_desc* desc, size_t* bytes);
+/* accumulate = 0: dtable is written whole, rows that no token names with zeros.  1: the rows that tokens
+ * name are added to, the others left alone (a table that is also the vocabulary's weight takes both gradients).
+ * scratch: 256-byte aligned device memory. */
+mw_status mw_embedding_backward(const mw_embedding_desc* desc, const void* tokens, const void* dout, void* dtable,
+                                int32_t accumulate, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Softmax cross entropy over a vocabulary, of states h and a weight row per token:
+ *   z_ij = scale * h_i . weight_j,   loss_i = log sum_j exp z_ij - z_i,targets_i,   total = sum_i g_i loss_i
+ *   dh_i = scale * sum_j dz_ij weight_j,   dweight_j = scale * sum_i dz_ij h_i,
+ *   dz_ij = g_i (exp(z_ij) / sum_k exp(z_ik) - [j = targets_i])
+ * A row whose target is not in 0..vocab-1 (or whose g_i is zero) is left out: its loss and dh are zero, and
+ * nothing of its h is read into anything.  g_i = row_weight[i], or without row_weight 1 / (rows not left out).
+ * The logits are never held whole: the loss alone keeps two numbers for 128 of them, the gradient a piece of
+ * rows at a time, which is turned into dz in its place. */
+typedef struct {
+  int64_t rows;               /* 0..2^24 */
+  int32_t vocab, dim;         /* 1..2^24, 1..2^16 */
+  int32_t dtype;              /* of h, weight, dh */
+  int32_t grad_dtype;         /* of dweight */
+  int32_t index_bytes;        /* targets are int32 (4) or int64 (8) */
+  int32_t piece_rows;         /* rows of a piece of the gradient; 0 = as many as take 1 GiB, 1024 at least */
+  int64_t ld_h, ld_weight, ld_dh, ld_dweight; /* elements between rows (0 = dim) */
+  double scale;
+} mw_token_loss_desc;
+mw_status mw_token_loss_workspace_bytes(const mw_token_loss_desc* desc, int32_t gradient, size_t* bytes);
+/* loss: float [rows]; total: float [1] or NULL; row_weight: float [rows] or NULL.  workspace: 256-byte aligned
+ * device memory, which no other call in flight uses. */
+mw_status mw_token_loss_forward(const mw_token_loss_desc* desc, const void* h, const void* weight,
+                                const void* targets, const float* row_weight, float* loss, float* total,
+                                void* workspace, size_t workspace_bytes, void* stream);
+/* dh or dweight may be NULL (not wanted); dh may be h itself where ld_dh = ld_h. */
+mw_status mw_token_loss_gradient(const mw_token_loss_desc* desc, const void* h, const void* weight,
+                                 const void* targets, const float* row_weight, float* loss, float* total, void* dh,
+                                 void* dweight, void* workspace, size_t workspace_bytes, void* stream);
+/* Synchronise `stream`, return the first device-side error recorded in the workspace by the last call. */
+mw_status mw_token_loss_status(const void* workspace, void* stream);
+
+/* Clipping by the norm of all gradients together:
+ *   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)
+ * Where norm is not finite, out = g and norm says so.  Host arrays of `count`: device pointers (dense tensors;
+ * out[k] may be in[k]), element counts, dtypes.  norm: float [1], device.  max_norm > 0; infinity: the norm alone
+ * (out may then be NULL).  scratch: 256-byte aligned device memory. */
+mw_status mw_clip_scratch_bytes(int32_t count, size_t* bytes);
+mw_status mw_clip_gradients(int32_t count, const void* const* in, void* const* out, const int64_t* sizes,
+                            const int32_t* dtypes, double max_norm, float* norm, void* scratch,
+                            size_t scratch_bytes, void* stream);
+
 /* ---- whole step from host buffers, and measurement hooks --------------------------------- */
 
 /* One Moonwalk gradient step (Algorithm 1 with Phases I-II in front) whose per-step inputs

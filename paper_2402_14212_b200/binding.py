@@ -58,6 +58,19 @@ class ResidualNormDesc(C.Structure):
                 ("ld_x", C.c_int64), ("ld_b", C.c_int64), ("ld_z", C.c_int64)]
 
 
+class EmbeddingDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int32), ("dim", C.c_int32), ("dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("index_bytes", C.c_int32), ("reserved", C.c_int32),
+                ("ld_table", C.c_int64), ("ld_out", C.c_int64), ("ld_dtable", C.c_int64), ("scale", C.c_double)]
+
+
+class TokenLossDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int32), ("dim", C.c_int32), ("dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("index_bytes", C.c_int32), ("piece_rows", C.c_int32),
+                ("ld_h", C.c_int64), ("ld_weight", C.c_int64), ("ld_dh", C.c_int64), ("ld_dweight", C.c_int64),
+                ("scale", C.c_double)]
+
+
 class OrthDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("rows", "cols", "count", "prec", "steps", "nesterov", "terms",
                                          "reserved")] + [("coef", C.c_double * 3)]
@@ -126,6 +139,17 @@ def lib() -> C.CDLL:
         L.mw_orth_project.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), vp, sz, vp]
         L.mw_orth_status.argtypes = [vp, vp, vp]
         L.mw_orth_selftest_unmet_wait.argtypes = [vp, C.c_uint32]
+        embed, tloss = C.POINTER(EmbeddingDesc), C.POINTER(TokenLossDesc)
+        L.mw_embedding_forward.argtypes = [embed] + [vp] * 4
+        L.mw_embedding_scratch_bytes.argtypes = [embed, C.POINTER(sz)]
+        L.mw_embedding_backward.argtypes = [embed, vp, vp, vp, i32, vp, sz, vp]
+        L.mw_token_loss_workspace_bytes.argtypes = [tloss, i32, C.POINTER(sz)]
+        L.mw_token_loss_forward.argtypes = [tloss] + [vp] * 7 + [sz, vp]
+        L.mw_token_loss_gradient.argtypes = [tloss] + [vp] * 9 + [sz, vp]
+        L.mw_token_loss_status.argtypes = [vp, vp]
+        L.mw_clip_scratch_bytes.argtypes = [i32, C.POINTER(sz)]
+        L.mw_clip_gradients.argtypes = [i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(C.c_int64), C.POINTER(i32),
+                                        C.c_double, vp, vp, sz, vp]
         L.mw_profile_begin.argtypes = []
         L.mw_profile_begin.restype = None
         L.mw_profile_end.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64),
@@ -865,6 +889,214 @@ class Orth:
         """Waits for the stream; the first device-side error of the last call on this workspace (0: none)."""
         wp, _ = Net._ws(workspace)
         return int(_call("mw_orth_status", workspace.device, self._h, wp, stream=stream))
+
+
+# ---- the two ends of a token model, and the bound of its step ----------------------------------
+def _index_bytes(t, where: str) -> int:
+    import torch
+    if t.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"{where}: int32 or int64, got {t.dtype}")
+    return 4 if t.dtype == torch.int32 else 8
+
+
+def _grad_code(dtype, own, where: str):
+    """(torch type, code) of a weight gradient: `dtype`, or the weight's own type where None."""
+    import torch
+    dtype = own if dtype is None else dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{where}: a gradient in float32 or bfloat16, got {dtype}")
+    return dtype, 1 if dtype == torch.float32 else 2
+
+
+def _rows_apart(t, name):
+    """Elements between the rows of a [rows, columns] tensor whose columns are contiguous."""
+    _need(t.shape[1] <= 1 or t.stride(1) == 1 or t.numel() == 0, f"{name}: columns are contiguous")
+    return t.stride(0) if t.shape[0] > 1 and t.numel() else max(1, t.shape[1])
+
+
+def _table_rows(t, name):
+    _need(t.dim() == 2 and t.shape[0] >= 1 and t.shape[1] >= 1, f"{name}: [vocabulary, columns], neither zero")
+    return _rows_apart(t, name)
+
+
+def embedding(tokens, table, scale: float = 1.0, out=None, stream=None):
+    """out = scale * table[tokens]: tokens int32 or int64 of any shape, table [vocabulary, columns] float32 or
+    bfloat16 (rows may be windows of wider ones), out [*tokens.shape, columns].  A token that is no row of the
+    table gives zeros.  `stream` as in gated_scan."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, table, embedding, tokens, table, scale, out)
+    key = ("embedding", scale, _layout(tokens), _layout(table), _layout(out))
+    d = _passed.get(key)
+    fresh = d is None
+    if fresh and (_repeats(table) or not tokens.is_contiguous()):
+        return embedding(tokens.contiguous(), *_own_memory(table), scale, out)
+    if fresh:
+        _need(table.is_cuda, "embedding: CUDA tensors")
+        d = EmbeddingDesc(tokens.numel(), table.shape[0], table.shape[-1], _operand_dtype(table, "embedding"), 0,
+                          _index_bytes(tokens, "embedding: tokens"), 0, _table_rows(table, "embedding: table"), 0, 0, float(scale))
+        if out is not None:
+            _need(out.dtype == table.dtype and tuple(out.shape) == (*tokens.shape, table.shape[1]) and out.is_contiguous(),
+                  "embedding: out is contiguous, of the table's type and shape [*tokens.shape, columns]")
+        _same_device(table, dict(tokens=tokens, out=out), "embedding")
+    if out is None:
+        out = torch.empty((*tokens.shape, table.shape[1]), dtype=table.dtype, device=table.device)
+    _check(_call("mw_embedding_forward", table.device, d, tokens.data_ptr(), table.data_ptr(), out.data_ptr()),
+           "mw_embedding_forward")
+    if fresh:
+        _remember(key, d)
+    return out
+
+
+def embedding_backward(tokens, dout, vocab: int, scale: float = 1.0, dtable=None, accumulate: bool = False,
+                       grad_dtype=None, stream=None):
+    """Gradient [vocab, columns] of embedding's table from dout [*tokens.shape, columns], summed in float32 in the
+    order of the tokens; grad_dtype: float32 or bfloat16 (dout's where None).  With accumulate the rows that tokens
+    name are added to dtable, whose other rows stay as they are.  `stream` as in gated_scan."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, dout, embedding_backward, tokens, dout, vocab, scale, dtable, accumulate, grad_dtype)
+    key = ("embedding backward", vocab, scale, bool(accumulate), grad_dtype, _layout(tokens), _layout(dout), _layout(dtable))
+    known = _passed.get(key)
+    if known is None:
+        _need(dout.is_cuda, "embedding_backward: CUDA tensors")
+        _need(dout.dim() >= 1 and tuple(dout.shape[:-1]) == tuple(tokens.shape) and dout.shape[-1] >= 1,
+              "embedding_backward: dout is [*tokens.shape, columns]")
+        rows = dout if dout.dim() == 2 else None
+        if _repeats(dout) or not tokens.is_contiguous() or (rows is None and not dout.is_contiguous()):
+            return embedding_backward(tokens.contiguous(), dout.contiguous(), vocab, scale, dtable, accumulate, grad_dtype)
+        _need(not accumulate or dtable is not None, "embedding_backward: accumulate adds to a dtable")
+        kind, code = _grad_code(dtable.dtype if dtable is not None and grad_dtype is None else grad_dtype, dout.dtype,
+                                "embedding_backward")
+        d = EmbeddingDesc(tokens.numel(), int(vocab), dout.shape[-1], _operand_dtype(dout, "embedding_backward"), code,
+                          _index_bytes(tokens, "embedding_backward: tokens"), 0, 0,
+                          _rows_apart(rows, "embedding_backward: dout") if rows is not None else 0, 0, float(scale))
+        if dtable is not None:
+            _need(dtable.dtype == kind and tuple(dtable.shape) == (vocab, dout.shape[-1]) and not _repeats(dtable),
+                  f"embedding_backward: dtable is [{vocab}, {dout.shape[-1]}] of {kind}")
+            d.ld_dtable = _table_rows(dtable, "embedding_backward: dtable")
+        _same_device(dout, dict(tokens=tokens, dtable=dtable), "embedding_backward")
+        need = C.c_size_t()
+        _check(lib().mw_embedding_scratch_bytes(d, need), "mw_embedding_scratch_bytes")
+        known = (d, int(need.value), kind)
+        _remember(key, known)
+    d, need, kind = known
+    if dtable is None:
+        dtable = torch.empty((vocab, dout.shape[-1]), dtype=kind, device=dout.device)
+    scratch = torch.empty(need, dtype=torch.uint8, device=dout.device)
+    _check(_call("mw_embedding_backward", dout.device, d, tokens.data_ptr(), dout.data_ptr(), dtable.data_ptr(),
+                 int(bool(accumulate)), scratch.data_ptr(), need), "mw_embedding_backward")
+    return dtable
+
+
+class TokenLoss(NamedTuple):
+    loss: object          # float32 [rows]
+    total: object         # float32 []
+    dh: object = None
+    dweight: object = None
+
+
+def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want):
+    import torch
+    key = ("token loss", gradient, scale, piece_rows, grad_dtype, want, _layout(h), _layout(weight), _layout(targets),
+           _layout(row_weight), _layout(dh), _layout(dweight))
+    known = _passed.get(key)
+    if known is None:
+        _need(h.is_cuda, "token_loss: CUDA tensors")
+        _need(h.dim() == 2 and weight.dim() == 2 and h.shape[1] == weight.shape[1] and h.dtype == weight.dtype,
+              "token_loss: h is [rows, columns], weight [vocabulary, columns] of the same type")
+        _need(tuple(targets.shape) == (h.shape[0],) and targets.is_contiguous(), "token_loss: targets are contiguous, [rows]")
+        _check_float(row_weight, (h.shape[0],), "token_loss: row_weight", h.device)
+        kind, code = _grad_code(dweight.dtype if dweight is not None and grad_dtype is None else grad_dtype, weight.dtype,
+                                "token_loss")
+        d = TokenLossDesc(h.shape[0], weight.shape[0], h.shape[1], _operand_dtype(h, "token_loss"), code,
+                          _index_bytes(targets, "token_loss: targets"), int(piece_rows), 0,
+                          _table_rows(weight, "token_loss: weight"), 0, 0, float(scale))
+        d.ld_h = _rows_apart(h, "token_loss: h")
+        if dh is not None:
+            _need(dh.dtype == h.dtype and dh.shape == h.shape and not _repeats(dh), "token_loss: dh has the type and shape of h")
+            d.ld_dh = _rows_apart(dh, "token_loss: dh")
+        if dweight is not None:
+            _need(dweight.dtype == kind and dweight.shape == weight.shape and not _repeats(dweight),
+                  f"token_loss: dweight is {kind} of weight's shape")
+            d.ld_dweight = _table_rows(dweight, "token_loss: dweight")
+        _same_device(h, dict(weight=weight, targets=targets, dh=dh, dweight=dweight), "token_loss")
+        need = C.c_size_t()
+        _check(lib().mw_token_loss_workspace_bytes(d, int(gradient), need), "mw_token_loss_workspace_bytes")
+        known = _remember(key, (d, int(need.value), kind))
+    d, need, kind = known
+    R = h.shape[0]
+    # the total and the workspace are one allocation with the rows' losses behind the latter
+    loss = torch.empty(R + 1, dtype=torch.float32, device=h.device)
+    ws = torch.empty(need, dtype=torch.uint8, device=h.device)
+    if not gradient:
+        _check(_call("mw_token_loss_forward", h.device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
+                     _ptr(row_weight), loss.data_ptr(), loss.data_ptr() + 4 * R, ws.data_ptr(), need),
+               "mw_token_loss_forward")
+        return TokenLoss(loss[:R], loss[R])
+    if dh is None and want[0]:
+        dh = _dense_like(h)
+    if dweight is None and want[1]:
+        dweight = torch.empty(weight.shape, dtype=kind, device=h.device)
+    _check(_call("mw_token_loss_gradient", h.device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
+                 _ptr(row_weight), loss.data_ptr(), loss.data_ptr() + 4 * R, _ptr(dh), _ptr(dweight), ws.data_ptr(),
+                 need), "mw_token_loss_gradient")
+    return TokenLoss(loss[:R], loss[R], dh, dweight)
+
+
+def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=None) -> TokenLoss:
+    """Softmax cross entropy of z = scale * h weight^T over a vocabulary, the logits never held: h [rows, columns]
+    and weight [vocabulary, columns] float32 or bfloat16, targets int32 or int64 [rows].  Rows whose target is no row
+    of weight (a negative one, say), or whose row_weight is zero, are left out: their loss is zero and their h is
+    not read into anything.  total = sum of row_weight * loss, the mean over the rows that are left without
+    row_weight.  `stream` as in gated_scan."""
+    if stream is not None:
+        return _on_stream(stream, h, token_loss, h, weight, targets, scale, row_weight)
+    h, weight = _own_memory(h, weight)
+    return _token_loss(False, h, weight, targets, scale, row_weight, 0, None, None, None, (False, False))
+
+
+def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None, dh=None, dweight=None,
+                        grad_dtype=None, want=(True, True), piece_rows: int = 0, stream=None) -> TokenLoss:
+    """token_loss, and the gradients of its total: dh (zero in rows left out; may be h itself) and dweight
+    (float32 or bfloat16 by grad_dtype, weight's type where None).  want: which of the two.  piece_rows: rows whose
+    exponentials are held at a time (0: as many as take 1 GiB); fewer take less memory and more time.  `stream` as
+    in gated_scan."""
+    if stream is not None:
+        return _on_stream(stream, h, token_loss_gradient, h, weight, targets, scale, row_weight, dh, dweight, grad_dtype,
+                          want, piece_rows)
+    h, weight = _own_memory(h, weight)
+    return _token_loss(True, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight,
+                       (bool(want[0]), bool(want[1])))
+
+
+def clip_gradients(grads, max_norm: float, out=None, stream=None):
+    """Scales the tensors together so that their common norm is at most max_norm; in place unless `out` gives a
+    tensor for each.  Dense float32 or bfloat16 tensors of any shapes on one device.  Returns the norm before, a
+    float32 tensor of no dimensions; where it is not finite the gradients stay as they are.  max_norm infinite: the
+    norm alone.  `stream` as in gated_scan."""
+    import torch
+    grads = list(grads)
+    _need(len(grads) > 0, "clip_gradients: at least one tensor")
+    out = grads if out is None else list(out)
+    if stream is not None:
+        return _on_stream(stream, grads[0], clip_gradients, grads, max_norm, out)
+    n, device = len(grads), grads[0].device
+    _need(grads[0].is_cuda and len(out) == n, "clip_gradients: CUDA tensors, and as many outputs")
+    codes = {torch.float32: 1, torch.bfloat16: 2}
+    for g, o in zip(grads, out):
+        if not (g.dtype in codes and g.is_contiguous() and g.device == device and
+                (o is g or (o.dtype == g.dtype and o.shape == g.shape and o.is_contiguous() and o.device == device))):
+            raise ValueError("clip_gradients: contiguous float32 or bfloat16 tensors on one device, outputs like them")
+    need = C.c_size_t()
+    _check(lib().mw_clip_scratch_bytes(n, need), "mw_clip_scratch_bytes")
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    scratch = torch.empty(int(need.value), dtype=torch.uint8, device=device)
+    ptrs = C.c_void_p * n
+    _check(_call("mw_clip_gradients", device, n, ptrs(*[g.data_ptr() for g in grads]), ptrs(*[o.data_ptr() for o in out]),
+                 (C.c_int64 * n)(*[g.numel() for g in grads]), (C.c_int32 * n)(*[codes[g.dtype] for g in grads]),
+                 float(max_norm), norm.data_ptr(), scratch.data_ptr(), int(need.value)), "mw_clip_gradients")
+    return norm
 
 
 # ---- moving a synthetic problem onto the device -------------------------------------------
