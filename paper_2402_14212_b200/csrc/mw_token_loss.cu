@@ -1,9 +1,26 @@
 // Softmax cross entropy over a vocabulary, and its gradient (mw_token_loss_*):
 //   z = s h W^T,  loss_i = log sum_j exp z_ij - z_{i,t_i},  dz_ij = g_i (p_ij - [j = t_i]),  dh = s dz W,  dW = s dz^T h
+//
 // Rows that have a target are put together first, so that the others cost nothing and nothing of them is read.
+// The products run on the tensor cores (CTA pairs, 256 x 256 tiles) and bound the time: 2 N V D flops for the loss,
+// three times that with both gradients.
+//
+// Loss alone: a tile's epilogue leaves, for each row and 128 columns, a power of two k and the sum of 2^(z' - k)
+// (z' = z log2 e); a last kernel joins them.  Nothing else of the logits is written.
+//
+// Gradient: the logits are not computed twice.  A piece of rows at a time, the epilogue also writes 2^(z' - k) in
+// half precision (float for float operands); once the row's sum is known those become dz in their place, by
+// a factor per 128 columns, and two products take them in.  That costs 4 bytes of traffic an element, less than
+// the 2 D flops of computing it again from D of about 400 up, and the row's gradient is known without a second call.
+//
+// Numbers.  bf16 operands are taken as half-precision numbers times one power of two a tensor: their 8 bits
+// fit, 2^-29 of the largest is still a normal number, and dz keeps 11 bits where bf16 would leave 8.  Float
+// operands are split in two such terms (22 bits), three products of four.  Sums are float; the tensor core cuts its
+// accumulator off at every step, so a sum goes to registers, rounded to nearest, a piece of K at a time.
+#include <cuda_fp16.h>
 #include <math.h>
 
-#include "mw_common.cuh"
+#include "mw_tc_ptx.cuh"
 
 namespace mw {
 namespace {
@@ -11,21 +28,501 @@ namespace {
 constexpr int kIndexRows = 1024;          // rows of one block that looks for targets
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 
+// ---- tiles ------------------------------------------------------------------------------------
+constexpr int kTile = 256;                // rows and columns of a pair's tile
+constexpr int kHalf = 128;                // ... of one CTA's share of either operand
+constexpr int kBK = 64;
+constexpr int kSumColumns = 128;          // logits that share a power of two and a sum
+constexpr int kLossThreads = 384;         // producer warp, issuing warp, two idle ones; eight epilogue warps
+constexpr int kFirstEpi = 4, kEpi = 8;
+// registers a thread: the launch gives 384 x 168 = 64512, handed over as 128 x 104 + 256 x 200 = 64512
+constexpr int kFewRegisters = 104, kManyRegisters = 200;
+constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;       // one term of one operand of one stage and CTA
+constexpr uint32_t kBufferBytes = 32 * 128;             // 32 rows of 128 bytes of an epilogue warp
+constexpr uint64_t kLossWaitNs = 2000000000ull;
+__host__ __device__ constexpr int stage_count(int terms) { return terms == 1 ? 5 : 3; }
+__host__ __device__ constexpr int buffer_count(int terms) { return terms == 1 ? 2 : 1; }
+__host__ __device__ constexpr uint32_t stage_bytes(int terms) { return 2u * (uint32_t)terms * kPlaneBytes; }
+constexpr size_t loss_smem(int terms) {
+  return 1024 + (size_t)stage_count(terms) * stage_bytes(terms) + (size_t)kEpi * buffer_count(terms) * kBufferBytes;
+}
+// K blocks that one accumulator takes: 128 instructions of bf16 operands, 96 of two-term ones.  Each cuts the sum
+// off at its last place; what that leaves of a sum of one sign is 2^-17.
+__host__ __device__ constexpr int piece_blocks(int terms) { return terms == 1 ? 32 : 8; }
+
 // what the kernels of one call share, behind the status block
 struct LossInfo {
   DeviceStatus st;
   unsigned pad[59];
   int live;                 // rows that are not left out
-  unsigned pad2[63];
+  unsigned g_max;           // bits of the largest |g|
+  unsigned h_max, w_max;    // bits of the largest finite |h|, |W|
+  unsigned pad2[60];
 };
+
+// powers of two that bring the operands and dz into half precision's range: at most 2^14
+__device__ __forceinline__ int range_exponent(unsigned max_bits) {
+  const int e = (int)(max_bits >> 23) - 127;         // 2^e <= max < 2^(e + 1)
+  if (max_bits == 0 || e > 127) return 0;
+  const int x = 13 - e;
+  return x < -100 ? -100 : (x > 100 ? 100 : x);
+}
 
 struct LossArgs {
   int64_t rows;
   int vocab, dim;
   int64_t ld_h, ld_w, ld_dh, ld_dw;
   float scale;
+  int scaled;               // operands were multiplied by powers of two
 };
 
+enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
+
+struct alignas(64) ProductArgs {
+  CUtensorMap a, b, out, acc;
+  const LossInfo* info;
+  DeviceStatus* st;
+  int first, piece;         // rows of this piece begin at `first` of the live ones
+  int vocab, dim;
+  int tiles_m, tiles_n;     // of the whole piece (P_DW: of the vocabulary and the columns)
+  int blocks_k, splits, per_split;
+  int slab_rows;            // P_DH: rows of one split's sums
+  int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
+  uint32_t idesc;
+  float scale;
+  int scaled;
+  float2* sums;             // [row][sum_blocks]: power, sum
+  float* target_z;
+  const int* target;
+  // P_DW: the gradient itself where the copy engine cannot write it, and the sums over pieces
+  void* dw;
+  int64_t ld_dw;
+  int dw_bf16, dw_engine;
+  float* partial;
+  int64_t ld_partial;
+};
+
+struct Unit { int m0, n0, kb0, kb1, split; };
+
+template <int KIND>
+__device__ __forceinline__ int live_rows(const ProductArgs& p) {
+  const int n = p.info->live - p.first;
+  return n < 0 ? 0 : (n < p.piece ? n : p.piece);
+}
+template <int KIND>
+__device__ __forceinline__ int unit_count(const ProductArgs& p, int live) {
+  if (KIND == P_DW) return live > 0 || p.first == 0 ? p.tiles_m * p.tiles_n : 0;
+  return (live + kTile - 1) / kTile * p.tiles_n * p.splits;
+}
+// Tiles that run at the same time share operands in L2.  Logits: eight tiles of rows go through the vocabulary
+// together.  dh: all tiles of a share of K.  dW: a tile of the vocabulary with all its columns.
+template <int KIND>
+__device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live) {
+  Unit w;
+  w.split = 0;
+  if (KIND == P_SUMS || KIND == P_EXP) {
+    constexpr int kRows = 8;
+    const int tm = (live + kTile - 1) / kTile, per = kRows * p.tiles_n;
+    const int group = u / per, r = u - group * per;
+    const int left = tm - group * kRows, rows = left < kRows ? left : kRows;
+    w.m0 = (group * kRows + r % rows) * kTile;
+    w.n0 = r / rows * kTile;
+    w.kb0 = 0;
+    w.kb1 = p.blocks_k;
+  } else if (KIND == P_DH) {
+    const int tm = (live + kTile - 1) / kTile, per = tm * p.tiles_n;
+    w.split = u / per;
+    const int r = u - w.split * per;
+    w.m0 = r / p.tiles_n * kTile;
+    w.n0 = r % p.tiles_n * kTile;
+    w.kb0 = w.split * p.per_split;
+    w.kb1 = w.kb0 + p.per_split < p.blocks_k ? w.kb0 + p.per_split : p.blocks_k;
+  } else {
+    w.m0 = u / p.tiles_n * kTile;
+    w.n0 = u % p.tiles_n * kTile;
+    w.kb0 = 0;
+    w.kb1 = (live + kBK - 1) / kBK;
+  }
+  return w;
+}
+
+// byte offset of 16-byte piece c of row r in a block of 128-byte rows under the 128-byte swizzle
+__device__ __forceinline__ uint32_t piece_at(uint32_t r, uint32_t c) { return r * 128u + ((c ^ (r & 7u)) << 4); }
+__device__ __forceinline__ void bulk_store_2d(const CUtensorMap* tm, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(tm)),
+               "r"(src), "r"(c0), "r"(c1)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t bf162_bits(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int TERMS, int KIND>
+__global__ void __launch_bounds__(kLossThreads, 1)
+loss_products_kernel(const __grid_constant__ ProductArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  constexpr int kStages = stage_count(TERMS), kBuffers = buffer_count(TERMS), kPiece = piece_blocks(TERMS);
+  constexpr uint32_t kStage = stage_bytes(TERMS);
+  __shared__ __align__(8) uint64_t full_bar[kStages];
+  __shared__ __align__(8) uint64_t empty_bar[kStages];
+  __shared__ __align__(8) uint64_t acc_full[2];
+  __shared__ __align__(8) uint64_t acc_empty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_cta_rank();
+  const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(smem_u32(&full_bar[s]), 1);
+      mbar_init(smem_u32(&empty_bar[s]), 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&acc_full[s]), 1);
+      mbar_init(smem_u32(&acc_empty[s]), kEpi * 2);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  WaitCtx wc;
+  wc.st = p.st;
+  wc.abort_flag = &abort_flag;
+  wc.limit_ns = kLossWaitNs;
+  const int live = live_rows<KIND>(p), units = unit_count<KIND>(p, live);
+
+  constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
+  // (registers change hands inside the branches: where paths meet the compiler counts on the fewer)
+  if (warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+  if (warp == 0) {
+    // ---------------- copies ----------------
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+      const uint32_t full0_even = map_to_cta(full0, 0u);
+      bool ok = true;
+      for (int u = pair; u < units && ok; u += pairs) {
+        const Unit w = unit_at<KIND>(p, u, live);
+        const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * kHalf;
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          if (!mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u)) { ok = false; break; }
+          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, 2u * kStage);
+          const uint32_t fb = full0_even + 8u * stage;
+          const uint32_t base = tiles + stage * kStage;
+          if (KIND == P_SUMS || KIND == P_EXP) {
+            tma_load_3d<true>(base, &p.a, fb, kb * kBK, p.first + am, 0);
+            tma_load_3d<true>(base + TERMS * kPlaneBytes, &p.b, fb, kb * kBK, bn, 0);
+          } else if (KIND == P_DH) {
+            tma_load_4d<true>(base, &p.a, fb, 0, am, kb, 0);
+            tma_load_4d<true>(base + TERMS * kPlaneBytes, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
+          } else {
+            tma_load_4d<true>(base, &p.a, fb, 0, kb * kBK, am >> 6, 0);
+            tma_load_4d<true>(base + TERMS * kPlaneBytes, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
+          }
+          if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- products (even CTA, for both) ----------------
+    if (lane == 0 && rank == 0) {
+      uint32_t stage = 0, phase = 0;
+      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+      constexpr uint32_t a_base = (kTurnedA ? (8192u >> 4) : 1u) << 16, b_base = (kTurnedB ? (8192u >> 4) : 1u) << 16;
+      constexpr uint32_t a_adv = kTurnedA ? (2048u >> 4) : (32u >> 4), b_adv = kTurnedB ? (2048u >> 4) : (32u >> 4);
+      constexpr uint32_t term = kPlaneBytes >> 4;
+      int j = 0;
+      bool ok = true;
+      for (int u = pair; u < units && ok; u += pairs) {
+        const Unit w = unit_at<KIND>(p, u, live);
+        for (int kb0 = w.kb0; kb0 < w.kb1 && ok; kb0 += kPiece, ++j) {
+          const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
+          if (!mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t d = tmem_base + set * (uint32_t)kTile;
+          const int kb1 = kb0 + kPiece < w.kb1 ? kb0 + kPiece : w.kb1;
+          bool ready = mbar_try_wait<true>(full0 + 8u * stage, phase);
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!ready && !mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sb = tiles + stage * kStage;
+            const uint32_t a0 = (sb >> 4) | a_base, b0 = ((sb + TERMS * kPlaneBytes) >> 4) | b_base;
+            umma_bf16<true>(d, a0, b0, p.idesc, kb > kb0);
+            if (TERMS == 2) {
+              umma_bf16<true>(d, a0, b0 + term, p.idesc, 1u);
+              umma_bf16<true>(d, a0 + term, b0, p.idesc, 1u);
+            }
+            // the next stage's barrier is polled while the first products run
+            const uint32_t freed = empty0 + 8u * stage;
+            if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1u; }
+            ready = kb + 1 < kb1 && mbar_try_wait<true>(full0 + 8u * stage, phase);
+#pragma unroll
+            for (int k = 1; k < kBK / 16; ++k) {
+              const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
+              umma_bf16<true>(d, a, b, p.idesc, 1u);
+              if (TERMS == 2) {
+                umma_bf16<true>(d, a, b + term, p.idesc, 1u);
+                umma_bf16<true>(d, a + term, b, p.idesc, 1u);
+              }
+            }
+            umma_commit<true>(freed);
+          }
+          if (ok) umma_commit<true>(smem_u32(&acc_full[set]));
+        }
+      }
+    }
+  } else if (warp >= kFirstEpi) {
+    // ---------------- epilogue ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
+    // A lane has a row of 32 and a warp half the tile's columns, all of them in registers: an accumulator is handed
+    // back as soon as it has been read.
+    const int ew = warp - kFirstEpi, quarter = warp & 3, side = ew >> 2;
+    const uint32_t sbuf = tiles + kStages * kStage + (uint32_t)ew * (kBuffers * kBufferBytes);
+    uint32_t turn = 0;
+    int j = 0;
+    bool ok = true;
+    const int exps = p.scaled ? range_exponent(p.info->h_max) : 0, expw = p.scaled ? range_exponent(p.info->w_max) : 0;
+    const int expz = range_exponent(p.info->g_max);
+    const float factor = KIND == P_DH ? 1.f
+                         : KIND == P_DW ? (float)ldexp((double)p.scale, -(expz + exps))
+                                        : (float)ldexp((double)p.scale * 1.4426950408889634, -(exps + expw));
+    // a block of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the next buffer
+    auto next_buffer = [&]() -> uint32_t {
+      if (lane == 0) {
+        if (kBuffers == 2) bulk_wait_read_but_one();
+        else bulk_wait_read_all();
+      }
+      __syncwarp();
+      const uint32_t at = sbuf + (kBuffers == 2 ? turn * kBufferBytes : 0u);
+      turn ^= 1u;
+      return at;
+    };
+    auto hand_over = [&](const CUtensorMap* map, uint32_t at, int col, int row) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) bulk_store_2d(map, at, col, row);
+    };
+    for (int u = pair; u < units && ok; u += pairs) {
+      const Unit w = unit_at<KIND>(p, u, live);
+      const int row0 = w.m0 + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+      const int col0 = w.n0 + side * kSumColumns;
+      float acc[kSumColumns];
+#pragma unroll
+      for (int i = 0; i < kSumColumns; ++i) acc[i] = 0.f;
+#pragma unroll 1
+      for (int kb0 = w.kb0; kb0 < w.kb1; kb0 += kPiece) {
+        const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
+        ++j;
+        ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kTile + (uint32_t)(side * kSumColumns);
+#pragma unroll
+        for (int c = 0; c < kSumColumns; c += 16) {
+          uint32_t r[16];
+          tmem_ld16_issue(t0 + (uint32_t)c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(r[i]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (rank != 0) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty[set]), 0u));
+          else mbar_arrive(smem_u32(&acc_empty[set]));
+        }
+      }
+      if (!ok) break;
+      if (KIND == P_SUMS || KIND == P_EXP) {
+        const int valid = p.vocab - col0;          // columns of the vocabulary from col0 on
+        const bool on = row < live;
+        if (valid > 0) {
+          float m = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < kSumColumns; ++i) {
+            acc[i] *= factor;
+            m = fmaxf(m, valid >= kSumColumns || i < valid ? acc[i] : -INFINITY);
+          }
+          const int t = on ? p.target[p.first + row] - col0 : -1;
+          if (__any_sync(0xffffffffu, t >= 0 && t < kSumColumns)) {
+            float zt = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSumColumns; ++i) zt = i == t ? acc[i] : zt;
+            if (t >= 0 && t < kSumColumns) p.target_z[p.first + row] = zt;
+          }
+          // (a row of nothing but -inf here, or with an infinity, keeps its values as they are)
+          const float k = fabsf(m) < 1e30f ? ceilf(m) - 15.f : -15.f;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < kSumColumns; ++i) {
+            acc[i] = exp2_fast(acc[i] - k);
+            if (valid < kSumColumns && i >= valid) acc[i] = 0.f;
+            sum += acc[i];
+          }
+          if (on) p.sums[(size_t)row * p.sum_blocks + col0 / kSumColumns] = make_float2(k, sum);
+          if (KIND == P_EXP) {
+            constexpr int kCols = TERMS == 1 ? 64 : 32;
+#pragma unroll
+            for (int c = 0; c < kSumColumns; c += kCols) {
+              if (c >= (valid + kBK - 1) / kBK * kBK) continue;          // beyond the padded row
+              const uint32_t at = next_buffer();
+#pragma unroll
+              for (uint32_t q = 0; q < 8; ++q) {
+                if (TERMS == 1) {
+                  const int i = c + 8 * (int)q;
+                  st_shared_v4(at + piece_at((uint32_t)lane, q), half2_bits(acc[i % kSumColumns], acc[(i + 1) % kSumColumns]),
+                               half2_bits(acc[(i + 2) % kSumColumns], acc[(i + 3) % kSumColumns]),
+                               half2_bits(acc[(i + 4) % kSumColumns], acc[(i + 5) % kSumColumns]),
+                               half2_bits(acc[(i + 6) % kSumColumns], acc[(i + 7) % kSumColumns]));
+                } else {
+                  const int i = c + 4 * (int)q;
+                  st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
+                               __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
+                }
+              }
+              hand_over(&p.out, at, col0 + c, row0);
+            }
+          }
+        }
+      } else if (KIND == P_DH) {
+#pragma unroll
+        for (int c = 0; c < kSumColumns; c += 32) {
+          if (col0 + c < p.dim) {
+            const uint32_t at = next_buffer();
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q) {
+              const int i = c + 4 * (int)q;
+              st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
+                           __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
+            }
+            hand_over(&p.out, at, col0 + c, w.split * p.slab_rows + row0);
+          }
+        }
+      } else {
+        // sums over earlier pieces come from, and unless this is the last go back to, a float array of their own
+        const bool add = p.first > 0, last = p.first + p.piece >= p.info->live;
+#pragma unroll
+        for (int c = 0; c < kSumColumns; c += 32) {
+          if (col0 + c < p.dim) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[c + i] *= factor;
+            if (add && row < p.vocab) {
+              const float4* from = reinterpret_cast<const float4*>(p.partial + (size_t)row * p.ld_partial + col0 + c);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) {
+                const float4 v = from[q];
+                acc[c + 4 * q] += v.x; acc[c + 4 * q + 1] += v.y; acc[c + 4 * q + 2] += v.z; acc[c + 4 * q + 3] += v.w;
+              }
+            }
+          }
+        }
+        if (row0 >= p.vocab) continue;
+        if (last && p.dw_bf16) {
+#pragma unroll
+          for (int c = 0; c < kSumColumns; c += 64) {
+            if (col0 + c < p.dim) {
+              const uint32_t at = next_buffer();
+#pragma unroll
+              for (uint32_t q = 0; q < 8; ++q) {
+                const int i = c + 8 * (int)q;
+                st_shared_v4(at + piece_at((uint32_t)lane, q), bf162_bits(acc[i], acc[i + 1]), bf162_bits(acc[i + 2], acc[i + 3]),
+                             bf162_bits(acc[i + 4], acc[i + 5]), bf162_bits(acc[i + 6], acc[i + 7]));
+              }
+              if (p.dw_engine) {
+                hand_over(&p.out, at, col0 + c, row0);
+              } else {
+                __syncwarp();
+                for (int r = 0; r < 32 && row0 + r < p.vocab; ++r)
+#pragma unroll
+                  for (int x = 0; x < 2; ++x) {
+                    const int col = col0 + c + lane + 32 * x;
+                    const uint32_t e = (uint32_t)(lane + 32 * x);
+                    unsigned short v;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + piece_at((uint32_t)r, e >> 3) + (e & 7u) * 2u) : "memory");
+                    if (col < p.dim) static_cast<unsigned short*>(p.dw)[(size_t)(row0 + r) * p.ld_dw + col] = v;
+                  }
+                __syncwarp();
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < kSumColumns; c += 32) {
+            if (col0 + c < p.dim) {
+              const uint32_t at = next_buffer();
+#pragma unroll
+              for (uint32_t q = 0; q < 8; ++q) {
+                const int i = c + 4 * (int)q;
+                st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
+                             __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
+              }
+              if (!last) {
+                hand_over(&p.acc, at, col0 + c, row0);
+              } else if (p.dw_engine) {
+                hand_over(&p.out, at, col0 + c, row0);
+              } else {
+                __syncwarp();
+                for (int r = 0; r < 32 && row0 + r < p.vocab; ++r) {
+                  uint32_t v;
+                  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at + piece_at((uint32_t)r, (uint32_t)lane >> 2) + ((uint32_t)lane & 3u) * 4u) : "memory");
+                  if (col0 + c + lane < p.dim) static_cast<uint32_t*>(p.dw)[(size_t)(row0 + r) * p.ld_dw + col0 + c + lane] = v;
+                }
+                __syncwarp();
+              }
+            }
+          }
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0 && lane == 0 && abort_flag) {
+    // a wait ran out: copies still in flight get a bounded time to land before the CTA retires
+    for (int s = 0; s < kStages; ++s)
+      for (uint32_t i = 0; i < 4096u && !mbar_try_wait<true>(smem_u32(&full_bar[s]), 0u); ++i) __nanosleep(256);
+  }
+  cluster_sync_all();
+  tc_fence_after();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+}
+
+// ---- rows -------------------------------------------------------------------------------------
 template <typename I>
 __device__ __forceinline__ int target_of(const I* targets, const float* weight, int64_t i, int vocab) {
   const I t = targets[i];
@@ -65,93 +562,211 @@ index_live_kernel(const I* targets, const float* weight, int64_t rows, int vocab
   const int live = sums[0];
   int at = sums[1] + __popc(on & ((1u << lane) - 1u));
   for (int w = 0; w < warp; ++w) at += warp_sum[w];
-  if (blockIdx.x == 0 && threadIdx.x == 0) info->live = live;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    info->live = live;
+    if (!weight && live > 0) info->g_max = __float_as_uint(1.f / (float)live);
+  }
   if (i >= rows) return;
   if (t >= 0) {
     row[at] = (int)i;
     target[at] = t;
     g[at] = weight ? weight[i] : 1.f / (float)live;
+    if (weight) atomicMax(&info->g_max, __float_as_uint(fabsf(weight[i])));
   } else {
     row[rows - 1 - (i - at)] = (int)i;
     loss[i] = 0.f;
   }
 }
 
+
+// bits of a finite |v|, zero of another: the largest of them bounds the operands' range
+__device__ __forceinline__ unsigned finite_bits(float v) {
+  const unsigned b = __float_as_uint(fabsf(v));
+  return b < 0x7f800000u ? b : 0u;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256)
-stage_rows_kernel(LossArgs a, const T* h, const int* row, const LossInfo* info, float* staged, T* dh) {
-  const int live = info->live;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const T* from = h + (int64_t)row[r] * a.ld_h;
-    for (int c = threadIdx.x; c < a.dim; c += 256) {
-      staged[r * a.dim + c] = r < live ? to_f32(from[c]) : 0.f;
-      if (r >= live && dh) dh[(int64_t)row[r] * a.ld_dh + c] = from_f64<T>(0.0);
+largest_kernel(const T* x, const int* row, const int* count, int64_t rows, int dim, int64_t ld, unsigned* most) {
+  const int64_t n = count ? *count : rows;
+  unsigned m = 0;
+  for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    const T* from = x + (row ? (int64_t)row[r] : r) * ld;
+    for (int c = threadIdx.x; c < dim; c += 256) m = max(m, finite_bits(to_f32(from[c])));
+  }
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0 && m) atomicMax(most, m);
+}
+
+// the terms of v times a power of two; what neither an infinity nor a NaN leaves is zero
+__device__ __forceinline__ void split_half(float v, unsigned short& hi, unsigned short& lo) {
+  const __half h = __float2half_rn(v);
+  const float back = __half2float(h);
+  const __half l = __float2half_rn(isfinite(back) ? v - back : 0.f);
+  hi = __half_as_ushort(h);
+  lo = __half_as_ushort(l);
+}
+
+// Rows of h or W as operands: [terms][staged rows][padded columns], zero beyond a row's end and beyond the last row.
+// With an index, the rows it names, and zeros into the rows of dh that are left out.
+template <typename T, int TERMS, bool SCALED>
+__global__ void __launch_bounds__(256)
+stage_kernel(const T* x, int64_t ld, const int* row, const int* count, int64_t rows, int64_t staged_rows, int dim, int padded,
+             const unsigned* most, unsigned short* out, T* dead, int64_t ld_dead) {
+  const int64_t n = count ? *count : rows;
+  const int64_t upto = (n + kTile - 1) / kTile * kTile < staged_rows ? (n + kTile - 1) / kTile * kTile : staged_rows;
+  const int e = SCALED ? range_exponent(*most) : 0;
+  const float f = __uint_as_float((unsigned)(127 + e) << 23);
+  for (int64_t r = blockIdx.x; r < upto || r < rows; r += gridDim.x) {
+    const int64_t at = row && r < rows ? row[r] : r;
+    if (r < upto) {
+      for (int c = threadIdx.x; c < padded; c += 256) {
+        const bool in = r < n && c < dim;
+        unsigned short hi = 0, lo = 0;
+        if (SCALED) {
+          split_half(in ? to_f32(x[at * ld + c]) * f : 0.f, hi, lo);
+        } else if (in) {
+          hi = reinterpret_cast<const unsigned short*>(x)[at * ld + c];
+        }
+        out[r * padded + c] = hi;
+        if (TERMS == 2) out[(staged_rows + r) * padded + c] = lo;
+      }
     }
+    if (dead && r >= n && r < rows)
+      for (int c = threadIdx.x; c < dim; c += 256) dead[at * ld_dead + c] = from_f64<T>(0.0);
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) stage_weight_kernel(LossArgs a, const T* w, float* staged) {
-  for (int64_t v = blockIdx.x; v < a.vocab; v += gridDim.x)
-    for (int c = threadIdx.x; c < a.dim; c += 256) staged[v * a.dim + c] = to_f32(w[v * a.ld_w + c]);
+// joins the sums of a row's blocks: log2 of the whole sum
+struct RowSum { float k, sum; };
+__device__ __forceinline__ RowSum join(RowSum a, RowSum b) {
+  const float k = fmaxf(a.k, b.k);
+  return {k, a.sum * exp2_fast(a.k - k) + b.sum * exp2_fast(b.k - k)};
 }
-
-__device__ __forceinline__ float block_reduce(float v, bool max, float* warp_v) {
+__device__ __forceinline__ RowSum warp_join(RowSum v) {
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
-    const float o = __shfl_xor_sync(0xffffffffu, v, d);
-    v = max ? fmaxf(v, o) : v + o;
+    const RowSum o = {__shfl_xor_sync(0xffffffffu, v.k, d), __shfl_xor_sync(0xffffffffu, v.sum, d)};
+    // (both lanes of a pair join in the same order, so all lanes have the same bits)
+    v = (threadIdx.x & d) ? join(o, v) : join(v, o);
   }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) warp_v[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = warp_v[0];
-  for (int w = 1; w < 8; ++w) v = max ? fmaxf(v, warp_v[w]) : v + warp_v[w];
   return v;
 }
-
-__global__ void __launch_bounds__(256)
-softmax_kernel(LossArgs a, float* z, int first, const int* row, const int* target, const float* g, const LossInfo* info, float* loss,
-               double* part, bool gradient) {
-  __shared__ float warp_v[8];
-  const int r = blockIdx.x, i = first + r;
-  float* at = z + (size_t)r * a.vocab;
-  const bool on = i < info->live;
-  if (!on) {
-    if (gradient)
-      for (int j = threadIdx.x; j < a.vocab; j += 256) at[j] = 0.f;
-    if (threadIdx.x == 0) part[i] = 0.0;
-    return;
-  }
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < a.vocab; j += 256) m = fmaxf(m, at[j]);
-  m = block_reduce(m, true, warp_v);
-  float sum = 0.f;
-  for (int j = threadIdx.x; j < a.vocab; j += 256) sum += expf(at[j] - m);
-  sum = block_reduce(sum, false, warp_v);
-  const int t = target[i];
-  const float l = logf(sum) - (at[t] - m);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    loss[row[i]] = l;
-    part[i] = (double)g[i] * l;
-  }
-  if (gradient)
-    for (int j = threadIdx.x; j < a.vocab; j += 256) {
-      const float p = expf(at[j] - m) / sum;
-      at[j] = g[i] * (j == t ? expm1f(-l) : p);
-    }
+// k of a block whose row is empty so far: small, and its difference to any k is finite
+constexpr float kNoPower = -3e38f;
+__device__ __forceinline__ float loss_of(RowSum v, float zt) {
+  // (the sum holds the target's own term, so what rounding leaves below zero is zero; NaN stays)
+  const float l = 0.69314718055994531f * ((v.k - zt) + log2f(v.sum));
+  return l < 0.f ? 0.f : l;
 }
 
-__global__ void __launch_bounds__(256) total_kernel(const double* part, int64_t rows, float* total) {
-  __shared__ double sums[256];
+// losses of all live rows, a warp each
+__global__ void __launch_bounds__(256)
+loss_rows_kernel(const LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const int* row, const float* g,
+                 float* loss, double* part) {
+  const int lane = threadIdx.x & 31;
+  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < info->live; i += (int64_t)gridDim.x * 8) {
+    RowSum v = {kNoPower, 0.f};
+    for (int b = lane; b < sum_blocks; b += 32) {
+      const float2 s = sums[i * sum_blocks + b];
+      v = join(v, {s.x, s.y});
+    }
+    v = warp_join(v);
+    if (lane == 0) {
+      const float l = loss_of(v, target_z[i]);
+      loss[row[i]] = l;
+      part[i] = (double)g[i] * (double)l;
+    }
+  }
+}
+
+// a row's exponentials -> dz times a power of two, in their place: a block a row
+template <int TERMS>
+__global__ void __launch_bounds__(256)
+dz_kernel(const LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
+          const int* target, const float* g, float* loss, double* part, unsigned short* e, int vocab, int padded) {
+  __shared__ RowSum warp_v[8];
+  int live = info->live - first;
+  live = live < 0 ? 0 : (live < piece ? live : piece);
+  const int upto = (live + kBK - 1) / kBK * kBK;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float to_range = __uint_as_float((unsigned)(127 + range_exponent(info->g_max)) << 23);
+  for (int r = blockIdx.x; r < upto; r += gridDim.x) {
+    unsigned short* at = e + (size_t)r * padded * TERMS;
+    if (r >= live) {                                  // rows that fill up the last block of K
+      for (int c = threadIdx.x; c < padded * TERMS / 8; c += 256) reinterpret_cast<uint4*>(at)[c] = make_uint4(0u, 0u, 0u, 0u);
+      continue;
+    }
+    const float2* mine = sums + (size_t)r * sum_blocks;
+    RowSum v = {kNoPower, 0.f};
+    for (int b = threadIdx.x; b < sum_blocks; b += 256) v = join(v, {mine[b].x, mine[b].y});
+    v = warp_join(v);
+    __syncthreads();
+    if (lane == 0) warp_v[warp] = v;
+    __syncthreads();
+    v = warp_v[0];
+    for (int w = 1; w < 8; ++w) v = join(v, warp_v[w]);
+    const int i = first + r, t = target[i];
+    const float l = loss_of(v, target_z[i]);
+    if (threadIdx.x == 0) {
+      loss[row[i]] = l;
+      part[i] = (double)g[i] * (double)l;
+    }
+    const float gi = g[i] * to_range, at_target = gi * expm1f(-l), share = gi / v.sum;
+    if (TERMS == 1) {
+      for (int c = threadIdx.x * 8; c < padded; c += 256 * 8) {
+        const float f = share * exp2_fast(mine[c / kSumColumns].x - v.k);
+        const uint4 raw = *reinterpret_cast<const uint4*>(at + c);
+        const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
+        uint32_t out[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float2 x = __half22float2(*reinterpret_cast<const __half2*>(&in[q]));
+          x.x = c + 2 * q == t ? at_target : x.x * f;
+          x.y = c + 2 * q + 1 == t ? at_target : x.y * f;
+          out[q] = half2_bits(x.x, x.y);
+        }
+        *reinterpret_cast<uint4*>(at + c) = make_uint4(out[0], out[1], out[2], out[3]);
+      }
+    } else {
+      // a group of 64 floats becomes 64 leading terms and 64 remainders: sixteen lanes, four of them each
+      for (int c0 = warp * 128; c0 < padded; c0 += 8 * 128) {
+        const int c = c0 + lane * 4;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        if (c < padded) {
+          const float f = share * exp2_fast(mine[c / kSumColumns].x - v.k);
+          const float4 raw = *reinterpret_cast<const float4*>(at + 2 * c);
+          x[0] = raw.x * f; x[1] = raw.y * f; x[2] = raw.z * f; x[3] = raw.w * f;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[q] = c + q == t ? at_target : x[q];
+        }
+        __syncwarp();
+        if (c < padded) {
+          unsigned short hi[4], lo[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) split_half(x[q], hi[q], lo[q]);
+          unsigned short* to = at + 2 * (c & ~63) + (c & 63);
+          *reinterpret_cast<uint2*>(to) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
+          *reinterpret_cast<uint2*>(to + 64) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+        }
+        __syncwarp();
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(1024) total_kernel(const LossInfo* info, const double* part, float* total) {
+  __shared__ double sums[32];
+  const int n = info->live;
   double t = 0.0;
-  for (int64_t i = threadIdx.x; i < rows; i += 256) t += part[i];
-  sums[threadIdx.x] = t;
+  for (int i = threadIdx.x; i < n; i += 1024) t += part[i];
+#pragma unroll
+  for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = t;
   __syncthreads();
   if (threadIdx.x == 0) {
     t = 0.0;
-    for (int i = 0; i < 256; ++i) t += sums[i];
+    for (int i = 0; i < 32; ++i) t += sums[i];
     *total = (float)t;
   }
 }
@@ -159,54 +774,97 @@ __global__ void __launch_bounds__(256) total_kernel(const double* part, int64_t 
 __device__ __forceinline__ void put(float* at, float v) { *at = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2bfloat16_rn(v); }
 
+// dh of the piece's rows: the sums over the shares of K, in order, to the rows they belong to
 template <typename T>
 __global__ void __launch_bounds__(256)
-store_rows_kernel(LossArgs a, const float* from, int first, int rows, const int* row, const LossInfo* info, T* dh) {
-  const int live = info->live;
-  for (int r = blockIdx.x; r < rows && first + r < live; r += gridDim.x)
-    for (int c = threadIdx.x; c < a.dim; c += 256) put(dh + (int64_t)row[first + r] * a.ld_dh + c, from[(size_t)r * a.dim + c]);
-}
-template <typename G>
-__global__ void __launch_bounds__(256) store_weight_kernel(LossArgs a, const float* from, G* dw) {
-  for (int64_t v = blockIdx.x; v < a.vocab; v += gridDim.x)
-    for (int c = threadIdx.x; c < a.dim; c += 256) put(dw + v * a.ld_dw + c, from[v * a.dim + c]);
+dh_rows_kernel(LossArgs a, const float* slab, int splits, int slab_rows, int padded, int first, int piece, const int* row,
+               const LossInfo* info, T* dh) {
+  int live = info->live - first;
+  live = live < 0 ? 0 : (live < piece ? live : piece);
+  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? range_exponent(info->w_max) : 0)));
+  for (int r = blockIdx.x; r < live; r += gridDim.x) {
+    T* to = dh + (int64_t)row[first + r] * a.ld_dh;
+    for (int c = threadIdx.x; c < a.dim; c += 256) {
+      float v = 0.f;
+      for (int s = 0; s < splits; ++s) v += slab[((size_t)s * slab_rows + r) * padded + c];
+      put(to + c, f * v);
+    }
+  }
 }
 
+// ---- host -------------------------------------------------------------------------------------
 struct LossWs {
   LossInfo* info;
   int *counts, *row, *target;
-  float* g;
+  float *g, *target_z;
   double* part;
-  float *h, *w, *z, *dh, *dw;
-  int blocks, piece;
+  float2* sums;
+  unsigned short *h, *w, *e;
+  float *slab, *dw;
+  int blocks, piece, padded, vpadded, sum_blocks, staged_rows, piece_rows, splits;
+  bool in_place;          // W is read where it lies
 };
+
+// Shares of K of the dh product, so that its tiles fill the device evenly: the least of (waves of tiles) x (time of a
+// tile) + (the sums' way through memory), in cycles, with a K block's products at 512 a term product and 8 bytes a sum at
+// 4.6 KB a cycle
+int dh_splits(int64_t rows, int dim, int blocks_k, int terms) {
+  const int64_t tiles = (rows + kTile - 1) / kTile * ceil_div(dim, kTile);
+  const int64_t pairs = sm_count() / 2;
+  const double block = terms == 1 ? 512.0 : 1536.0;
+  int best = 1;
+  double least = 1e300;
+  for (int s = 1; s <= 32 && (s == 1 || blocks_k / s >= 16); ++s) {
+    const double t = (double)((tiles * s + pairs - 1) / pairs) * (ceil_div(blocks_k, s) * block + 3000.0) +
+                     (double)s * rows * dim * 8.0 / 4600.0;
+    if (t < least) { least = t; best = s; }
+  }
+  return best;
+}
+
 size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossWs* l) {
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* p = base + at;
-    at += align_up(bytes, 256);
+    at += align_up(bytes, 1024);
     return p;
   };
+  const int terms = d->dtype == MW_F32 ? 2 : 1;
   const size_t n = (size_t)d->rows, v = (size_t)d->vocab, dim = (size_t)d->dim;
+  const int64_t ld_w = d->ld_weight ? d->ld_weight : d->dim;
+  l->in_place = !gradient && terms == 1 && ld_w % 8 == 0;
   l->blocks = ceil_div(d->rows, kIndexRows);
-  int64_t piece = d->piece_rows;
-  if (!piece) {
-    piece = kPieceBytes / (4 * (int64_t)v);
-    if (piece < 1024) piece = 1024;
+  l->padded = (int)align_up(dim, kBK);
+  l->vpadded = (int)align_up(v, kBK);
+  l->sum_blocks = ceil_div(d->vocab, kSumColumns);
+  l->staged_rows = (int)align_up(n ? n : 1, kTile);
+  int64_t piece = d->rows ? d->rows : 1;
+  if (gradient) {
+    piece = d->piece_rows;
+    if (!piece) {
+      piece = kPieceBytes / (2 * terms * (int64_t)l->vpadded);
+      if (piece < 1024) piece = 1024;
+    }
+    if (piece < d->rows) piece = (int64_t)align_up((size_t)piece, kTile);
+    if (piece > d->rows) piece = d->rows ? d->rows : 1;
   }
-  l->piece = (int)(piece < d->rows ? piece : (d->rows ? d->rows : 1));
+  l->piece = (int)piece;
+  l->piece_rows = (int)align_up((size_t)piece, kTile);
+  l->splits = gradient ? dh_splits(piece, d->dim, l->vpadded / kBK, terms) : 0;
   l->info = (LossInfo*)take(sizeof(LossInfo));
   l->counts = (int*)take((size_t)l->blocks * 4);
   l->row = (int*)take(n * 4);
   l->target = (int*)take(n * 4);
   l->g = (float*)take(n * 4);
+  l->target_z = (float*)take(n * 4);
   l->part = (double*)take(n * 8);
-  l->h = (float*)take(n * dim * 4);
-  l->w = (float*)take(v * dim * 4);
-  l->z = (float*)take((size_t)l->piece * v * 4);
-  l->dh = (float*)take(gradient ? (size_t)l->piece * dim * 4 : 0);
-  l->dw = (float*)take(gradient ? v * dim * 4 : 0);
-  return at + 256;
+  l->sums = (float2*)take((size_t)l->piece * l->sum_blocks * 8);
+  l->h = (unsigned short*)take((size_t)l->staged_rows * l->padded * 2 * terms);
+  l->w = (unsigned short*)take(l->in_place ? 0 : v * l->padded * 2 * terms);
+  l->e = (unsigned short*)take(gradient ? (size_t)l->piece_rows * l->vpadded * 2 * terms : 0);
+  l->slab = (float*)take(gradient ? (size_t)l->splits * l->piece_rows * l->padded * 4 : 0);
+  l->dw = (float*)take(gradient && l->piece < d->rows ? v * l->padded * 4 : 0);
+  return at;
 }
 
 mw_status check_loss(const mw_token_loss_desc* d) {
@@ -220,9 +878,77 @@ mw_status check_loss(const mw_token_loss_desc* d) {
   return MW_OK;
 }
 
+// a tensor map of `rank` dimensions; strides in bytes, of all but the first
+mw_status make_map(CUtensorMap* out, CUtensorMapDataType type, int rank, const void* base, const int64_t* dims, const int64_t* strides,
+                   const int* box) {
+  auto fn = encode_fn();
+  if (!fn) return MW_ERR_CUDA;
+  cuuint64_t d[4], st[3];
+  cuuint32_t b[4], one[4] = {1u, 1u, 1u, 1u};
+  for (int i = 0; i < rank; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    b[i] = (cuuint32_t)box[i];
+    if (i) st[i - 1] = (cuuint64_t)strides[i - 1];
+  }
+  return fn(out, type, (cuuint32_t)rank, const_cast<void*>(base), d, st, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? MW_OK : MW_ERR_CUDA;
+}
+// operand rows with K along them: boxes of 64 columns, 128 rows and all terms
+mw_status row_map(CUtensorMap* out, bool bf16, const void* base, int64_t cols, int64_t rows, int64_t ld, int terms) {
+  const int64_t dims[3] = {cols, rows, terms}, strides[2] = {ld * 2, rows * ld * 2};
+  const int box[3] = {kBK, kHalf, terms};
+  return make_map(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dims, strides, box);
+}
+// operand rows in groups of 64 columns: boxes of `rows_box` rows and `groups` groups
+mw_status group_map(CUtensorMap* out, const void* base, int64_t cols, int64_t rows, int64_t row_bytes, int64_t group_bytes,
+                    int64_t term_bytes, int terms, int rows_box, int groups) {
+  const int64_t dims[4] = {64, rows, cols / 64, terms}, strides[3] = {row_bytes, group_bytes, term_bytes};
+  const int box[4] = {64, rows_box, groups, terms};
+  return make_map(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box);
+}
+// results: boxes of 32 rows of 128 bytes
+mw_status out_map(CUtensorMap* out, CUtensorMapDataType type, int size, const void* base, int64_t cols, int64_t rows, int64_t ld) {
+  const int64_t dims[2] = {cols, rows}, strides[1] = {ld * size};
+  const int box[2] = {128 / size, 32};
+  return make_map(out, type, 2, base, dims, strides, box);
+}
+
+template <int TERMS, int KIND>
+mw_status run_product(const ProductArgs& p, int64_t most_units, cudaStream_t s) {
+  static bool ready[kMaxDevices] = {};
+  const int dev = current_device();
+  auto kernel = loss_products_kernel<TERMS, KIND>;
+  if (!ready[dev]) {
+    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)loss_smem(TERMS)));
+    ready[dev] = true;
+  }
+  const int64_t pairs = sm_count() / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (unsigned)(most_units < pairs ? (most_units < 1 ? 1 : most_units) : pairs));
+  cfg.blockDim = dim3(kLossThreads);
+  cfg.dynamicSmemBytes = loss_smem(TERMS);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  ++g_launch_count;
+  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
+}
+
+// fp32 accumulator, the operands' type, K across the rows of A and of B, N / 8, M / 16
+uint32_t instruction(bool bf16, bool turned_a, bool turned_b) {
+  return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((turned_a ? 1u : 0u) << 15) | ((turned_b ? 1u : 0u) << 16) |
+         ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+}
+
 template <typename T, typename I>
 mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I* targets, const float* weight, float* loss, float* total,
                    T* dh, void* dw, bool gradient, char* ws, cudaStream_t s) {
+  constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
   LossArgs a;
   a.rows = d->rows; a.vocab = d->vocab; a.dim = d->dim;
   a.ld_h = d->ld_h ? d->ld_h : d->dim;
@@ -232,36 +958,95 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   a.scale = (float)d->scale;
   LossWs l;
   loss_layout(d, gradient, ws, &l);
+  // bf16 operands of the loss alone are taken as they are
+  const bool scaled = TERMS == 2 || gradient;
+  a.scaled = scaled;
   MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
   const unsigned wide = 148 * 8;
   if (a.rows > 0) {
     count_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, l.counts);
     index_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, l.counts, l.blocks, l.row, l.target, l.g, loss, l.info);
-    stage_rows_kernel<T><<<wide, 256, 0, s>>>(a, h, l.row, l.info, l.h, dh);
-    stage_weight_kernel<T><<<wide, 256, 0, s>>>(a, w, l.w);
-    MW_TRY(launch_ok(4));
-  }
-  if (dw && a.rows == 0) MW_CUDA_OK(cudaMemsetAsync(l.dw, 0, (size_t)a.vocab * a.dim * 4, s));
-  for (int64_t first = 0; first < a.rows; first += l.piece) {
-    const int rows = (int)(a.rows - first < l.piece ? a.rows - first : l.piece);
-    MW_TRY(gemm_simt<float>(0, 1, rows, a.vocab, a.dim, a.scale, l.h + first * a.dim, a.dim, l.w, a.dim, 0.0, l.z, a.vocab, s));
-    softmax_kernel<<<rows, 256, 0, s>>>(a, l.z, (int)first, l.row, l.target, l.g, l.info, loss, l.part, gradient);
-    MW_TRY(launch_ok());
-    if (dh) {
-      MW_TRY(gemm_simt<float>(0, 0, rows, a.dim, a.vocab, a.scale, l.z, a.vocab, l.w, a.dim, 0.0, l.dh, a.dim, s));
-      store_rows_kernel<T><<<wide, 256, 0, s>>>(a, l.dh, (int)first, rows, l.row, l.info, dh);
-      MW_TRY(launch_ok());
+    if (scaled) {
+      largest_kernel<T><<<wide, 256, 0, s>>>(h, l.row, &l.info->live, a.rows, a.dim, a.ld_h, &l.info->h_max);
+      largest_kernel<T><<<wide, 256, 0, s>>>(w, nullptr, nullptr, a.vocab, a.dim, a.ld_w, &l.info->w_max);
+      stage_kernel<T, TERMS, true><<<wide, 256, 0, s>>>(h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, a.dim, l.padded, &l.info->h_max, l.h, dh, a.ld_dh);
+      stage_kernel<T, TERMS, true><<<wide, 256, 0, s>>>(w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, a.dim, l.padded, &l.info->w_max, l.w, (T*)nullptr, 0);
+      MW_TRY(launch_ok(6));
+    } else {
+      stage_kernel<T, 1, false><<<wide, 256, 0, s>>>(h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, a.dim, l.padded, nullptr, l.h, (T*)nullptr, 0);
+      if (!l.in_place) stage_kernel<T, 1, false><<<wide, 256, 0, s>>>(w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, a.dim, l.padded, nullptr, l.w, (T*)nullptr, 0);
+      MW_TRY(launch_ok(l.in_place ? 3 : 4));
     }
-    if (dw) MW_TRY(gemm_simt<float>(1, 0, a.vocab, a.dim, rows, a.scale, l.z, a.vocab, l.h + first * a.dim, a.dim, first ? 1.0 : 0.0, l.dw, a.dim, s));
   }
-  if (dw) {
-    const int32_t g = d->grad_dtype ? d->grad_dtype : d->dtype;
-    if (g == MW_F32) store_weight_kernel<float><<<wide, 256, 0, s>>>(a, l.dw, (float*)dw);
-    else store_weight_kernel<__nv_bfloat16><<<wide, 256, 0, s>>>(a, l.dw, (__nv_bfloat16*)dw);
-    MW_TRY(launch_ok());
+  if (a.rows > 0 || dw) {
+    const bool bf16 = !scaled;
+    const int dw_bf16 = (d->grad_dtype ? d->grad_dtype : d->dtype) == MW_BF16_F32ACC;
+    const int dw_size = dw_bf16 ? 2 : 4;
+    ProductArgs p = {};
+    p.info = l.info;
+    p.st = &l.info->st;
+    p.vocab = a.vocab; p.dim = a.dim;
+    p.scale = a.scale; p.scaled = scaled;
+    p.piece = l.piece;
+    p.sum_blocks = l.sum_blocks;
+    p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
+    p.splits = 1;
+    ProductArgs logits = p, by_h = p, by_w = p;
+    logits.tiles_n = ceil_div(a.vocab, kTile);
+    logits.blocks_k = l.padded / kBK;
+    logits.idesc = instruction(bf16, false, false);
+    MW_TRY(row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS));
+    MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1) : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
+    if (gradient) {
+      const int64_t row_bytes = (int64_t)l.vpadded * 2 * TERMS, group_bytes = 128 * TERMS;
+      const int64_t hw_bytes = (int64_t)l.padded * 2;
+      MW_TRY(out_map(&logits.out, TERMS == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2 * TERMS, l.e, l.vpadded, l.piece_rows, l.vpadded));
+      // dh: K along the rows of dz and across those of W
+      by_h.tiles_n = ceil_div(a.dim, kTile);
+      by_h.blocks_k = l.vpadded / kBK;
+      by_h.splits = l.splits;
+      by_h.per_split = ceil_div(by_h.blocks_k, l.splits);
+      by_h.slab_rows = l.piece_rows;
+      by_h.idesc = instruction(false, false, true);
+      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, TERMS, kHalf, 1));
+      MW_TRY(group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, 2));
+      MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, (int64_t)l.splits * l.piece_rows, l.padded));
+      // dW: K across the rows of both
+      by_w.tiles_m = ceil_div(a.vocab, kTile);
+      by_w.tiles_n = ceil_div(a.dim, kTile);
+      by_w.idesc = instruction(false, true, true);
+      MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, TERMS, kBK, 2));
+      MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
+      by_w.dw = dw; by_w.ld_dw = a.ld_dw; by_w.dw_bf16 = dw_bf16;
+      by_w.dw_engine = ((uintptr_t)dw & 15) == 0 && (a.ld_dw * dw_size) % 16 == 0;
+      if (by_w.dw_engine && dw)
+        MW_TRY(out_map(&by_w.out, dw_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, dw_size, dw, a.dim, a.vocab, a.ld_dw));
+      by_w.partial = l.dw; by_w.ld_partial = l.padded;
+      if (l.piece < a.rows) MW_TRY(out_map(&by_w.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.dw, l.padded, a.vocab, l.padded));
+    }
+    const int64_t tm = ceil_div(l.piece, kTile);
+    for (int64_t first = 0; first < (a.rows > 0 ? a.rows : 1); first += l.piece) {
+      logits.first = by_h.first = by_w.first = (int)first;
+      if (a.rows > 0) {
+        if (gradient) {
+          MW_TRY((run_product<TERMS, P_EXP>(logits, tm * logits.tiles_n, s)));
+          dz_kernel<TERMS><<<wide, 256, 0, s>>>(l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part, l.e, a.vocab, l.vpadded);
+        } else {
+          MW_TRY((run_product<TERMS, P_SUMS>(logits, tm * logits.tiles_n, s)));
+          loss_rows_kernel<<<wide, 256, 0, s>>>(l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part);
+        }
+        MW_TRY(launch_ok());
+        if (dh) {
+          MW_TRY((run_product<TERMS, P_DH>(by_h, tm * by_h.tiles_n * l.splits, s)));
+          dh_rows_kernel<T><<<wide, 256, 0, s>>>(a, l.slab, l.splits, l.piece_rows, l.padded, (int)first, l.piece, l.row, l.info, dh);
+          MW_TRY(launch_ok());
+        }
+      }
+      if (dw) MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n, s)));
+    }
   }
   if (total) {
-    total_kernel<<<1, 256, 0, s>>>(l.part, a.rows, total);
+    total_kernel<<<1, 1024, 0, s>>>(l.info, l.part, total);
     MW_TRY(launch_ok());
   }
   return MW_OK;
@@ -273,6 +1058,9 @@ mw_status loss_call(const mw_token_loss_desc* d, const void* h, const void* w, c
   if (!w || (d->rows > 0 && (!h || !targets || !loss))) return MW_ERR_INVALID_ARG;
   const int64_t ld_h = d->ld_h ? d->ld_h : d->dim, ld_dh = d->ld_dh ? d->ld_dh : d->dim;
   if (dh == h && dh && ld_h != ld_dh) return MW_ERR_INVALID_ARG;
+  // rows that the copy engine reads start on 16-byte boundaries
+  const int64_t ld_w = d->ld_weight ? d->ld_weight : d->dim;
+  if (!gradient && d->dtype == MW_BF16_F32ACC && ld_w % 8 == 0 && ((uintptr_t)w & 15)) return MW_ERR_INVALID_ARG;
   LossWs l;
   if (!ws || ((uintptr_t)ws & 255u) || bytes < loss_layout(d, gradient, nullptr, &l)) return MW_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
