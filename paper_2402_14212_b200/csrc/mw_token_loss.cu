@@ -56,16 +56,28 @@ struct LossInfo {
   unsigned pad[59];
   int live;                 // rows that are not left out
   unsigned g_max;           // bits of the largest |g|
-  unsigned h_max, w_max;    // bits of the largest finite |h|, |W|
-  unsigned pad2[60];
+  unsigned h_max[2], w_max[2];    // bits of the largest finite |h|, |W|: of a sample of the rows, and of all
+  unsigned pad2[58];
 };
 
-// powers of two that bring the operands and dz into half precision's range: at most 2^14
+// the power of two that brings numbers of at most this size to 2^13 .. 2^14
 __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   const int e = (int)(max_bits >> 23) - 127;         // 2^e <= max < 2^(e + 1)
   if (max_bits == 0 || e > 127) return 0;
   const int x = 13 - e;
   return x < -100 ? -100 : (x > 100 ? 100 : x);
+}
+// ... of a large operand, whose size is known from a sample of its rows when it is written: room for numbers 16 times
+// as large as the sample's.  Where the largest of all turn out to lie elsewhere, too large or so small
+// that the lower terms would suffer, the operand is written again by what they are.
+constexpr int kSampleRoom = 4;
+__device__ __forceinline__ int sample_exponent(unsigned sample) { return range_exponent(sample) - (sample ? kSampleRoom : 0); }
+__device__ __forceinline__ bool sample_misses(const unsigned (&most)[2]) {
+  const int e = (int)(most[1] >> 23) - 127 + sample_exponent(most[0]);
+  return most[1] != 0 && (e > 14 || e < 13 - 2 * kSampleRoom);
+}
+__device__ __forceinline__ int operand_exponent(const unsigned (&most)[2], bool sampled) {
+  return !sampled ? range_exponent(most[0]) : (sample_misses(most) ? range_exponent(most[1]) : sample_exponent(most[0]));
 }
 
 struct LossArgs {
@@ -74,6 +86,7 @@ struct LossArgs {
   int64_t ld_h, ld_w, ld_dh, ld_dw;
   float scale;
   int scaled;               // operands were multiplied by powers of two
+  int sampled_h, sampled_w;
 };
 
 enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
@@ -90,7 +103,7 @@ struct alignas(64) ProductArgs {
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
   float scale;
-  int scaled;
+  int scaled, sampled_h, sampled_w;
   float2* sums;             // [row][sum_blocks]: power, sum
   float* target_z;
   const int* target;
@@ -314,7 +327,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     uint32_t turn = 0;
     int j = 0;
     bool ok = true;
-    const int exps = p.scaled ? range_exponent(p.info->h_max) : 0, expw = p.scaled ? range_exponent(p.info->w_max) : 0;
+    const int exps = p.scaled ? operand_exponent(p.info->h_max, p.sampled_h) : 0;
+    const int expw = p.scaled ? operand_exponent(p.info->w_max, p.sampled_w) : 0;
     const int expz = range_exponent(p.info->g_max);
     const float factor = KIND == P_DH ? 1.f
                          : KIND == P_DW ? (float)ldexp((double)p.scale, -(expz + exps))
@@ -585,20 +599,29 @@ __device__ __forceinline__ unsigned finite_bits(float v) {
   return b < 0x7f800000u ? b : 0u;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256)
-largest_kernel(const T* x, const int* row, const int* count, int64_t rows, int dim, int64_t ld, unsigned* most) {
-  const int64_t n = count ? *count : rows;
-  unsigned m = 0;
-  for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
-    const T* from = x + (row ? (int64_t)row[r] : r) * ld;
-    for (int c = threadIdx.x; c < dim; c += 256) m = max(m, finite_bits(to_f32(from[c])));
+// eight values of a row from column c on, zero from `dim` on (WIDE: rows and pieces lie on 16-byte boundaries)
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load8(const T* row, int c, int dim, float (&v)[8]) {
+  if (WIDE && sizeof(T) == 4) {
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 x = c < dim ? reinterpret_cast<const float4*>(row + c)[0] : zero;
+    const float4 y = c + 4 < dim ? reinterpret_cast<const float4*>(row + c)[1] : zero;
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+  } else if (WIDE) {
+    const uint4 x = c < dim ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < dim ? to_f32(row[c + i]) : 0.f;
   }
-  m = __reduce_max_sync(0xffffffffu, m);
-  if ((threadIdx.x & 31) == 0 && m) atomicMax(most, m);
 }
 
-// the terms of v times a power of two; what neither an infinity nor a NaN leaves is zero
+// The terms of v times a power of two; beside an infinity or a NaN the second is zero.
 __device__ __forceinline__ void split_half(float v, unsigned short& hi, unsigned short& lo) {
   const __half h = __float2half_rn(v);
   const float back = __half2float(h);
@@ -607,33 +630,106 @@ __device__ __forceinline__ void split_half(float v, unsigned short& hi, unsigned
   lo = __half_as_ushort(l);
 }
 
-// Rows of h or W as operands: [terms][staged rows][padded columns], zero beyond a row's end and beyond the last row.
-// With an index, the rows it names, and zeros into the rows of dh that are left out.
-template <typename T, int TERMS, bool SCALED>
-__global__ void __launch_bounds__(256)
-stage_kernel(const T* x, int64_t ld, const int* row, const int* count, int64_t rows, int64_t staged_rows, int dim, int padded,
-             const unsigned* most, unsigned short* out, T* dead, int64_t ld_dead) {
-  const int64_t n = count ? *count : rows;
-  const int64_t upto = (n + kTile - 1) / kTile * kTile < staged_rows ? (n + kTile - 1) / kTile * kTile : staged_rows;
-  const int e = SCALED ? range_exponent(*most) : 0;
+// h (rows with a target, by their index) or W as operands: [terms][staged rows][padded columns], zero beyond a row's
+// end and beyond the last row to a multiple of a tile
+template <typename T>
+struct Operand {
+  const T* x;
+  int64_t ld;
+  const int *row, *count;         // null: all rows
+  int64_t rows, staged_rows;
+  unsigned* most;                 // LossInfo::h_max or w_max
+  int sampled;                    // one row in kSampleRows was looked at
+  unsigned short* out;
+  T* dead;                        // rows of dh that get zeros
+  int64_t ld_dead;
+};
+constexpr int kSampleRows = 16;
+// operands of more than this are sampled: looking at all of a smaller one costs less than the launch that writes
+// an operand again
+constexpr int64_t kSampledBytes = (int64_t)32 << 20;
+
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) largest_kernel(Operand<T> w, Operand<T> h, int dim, int64_t w_blocks) {
+  const bool of_w = blockIdx.x < w_blocks;
+  const Operand<T>& o = of_w ? w : h;
+  const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
+  const int64_t n = o.count ? *o.count : o.rows;
+  const uint32_t per = (uint32_t)(dim + 7) / 8, step = o.sampled ? kSampleRows : 1;
+  const int64_t items = (n + step - 1) / step * per;
+  unsigned m = 0;
+  for (int64_t i = block * 256 + threadIdx.x; i < items; i += blocks * 256) {
+    const int64_t r = i / per * step;
+    float v[8];
+    load8<T, WIDE>(o.x + (o.row ? (int64_t)o.row[r] : r) * o.ld, (int)(i % per) * 8, dim, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = max(m, finite_bits(v[k]));
+  }
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0 && m) atomicMax(o.most, m);
+}
+
+// AGAIN: only what the sample misjudged.  SCALED false: bf16 as it is.
+template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
+__global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, int dim, int padded, int64_t w_blocks) {
+  const bool of_w = blockIdx.x < w_blocks;
+  const Operand<T>& o = of_w ? w : h;
+  const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
+  int e = 0;
+  if (SCALED) {
+    const unsigned most[2] = {o.most[0], AGAIN ? o.most[1] : 0u};
+    if (AGAIN && (!o.sampled || !sample_misses(most))) return;
+    e = AGAIN ? range_exponent(most[1]) : (o.sampled ? sample_exponent(most[0]) : range_exponent(most[0]));
+  }
   const float f = __uint_as_float((unsigned)(127 + e) << 23);
-  for (int64_t r = blockIdx.x; r < upto || r < rows; r += gridDim.x) {
-    const int64_t at = row && r < rows ? row[r] : r;
+  const int64_t n = o.count ? *o.count : o.rows;
+  const int64_t whole = (n + kTile - 1) / kTile * kTile, upto = whole < o.staged_rows ? whole : o.staged_rows;
+  const uint32_t per = (uint32_t)padded / 8;
+  const int64_t items = (o.dead && upto < o.rows ? o.rows : upto) * per;
+  unsigned m = 0;
+  for (int64_t i = block * 256 + threadIdx.x; i < items; i += blocks * 256) {
+    const int64_t r = i / per;
+    const int c = (int)(i % per) * 8;
+    const int64_t at = o.row && r < o.rows ? o.row[r] : r;
     if (r < upto) {
-      for (int c = threadIdx.x; c < padded; c += 256) {
-        const bool in = r < n && c < dim;
-        unsigned short hi = 0, lo = 0;
-        if (SCALED) {
-          split_half(in ? to_f32(x[at * ld + c]) * f : 0.f, hi, lo);
-        } else if (in) {
-          hi = reinterpret_cast<const unsigned short*>(x)[at * ld + c];
+      unsigned short hi[8], lo[8];
+      if (SCALED) {
+        float v[8];
+        if (r < n) {
+          load8<T, WIDE>(o.x + at * o.ld, c, dim, v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = 0.f;
         }
-        out[r * padded + c] = hi;
-        if (TERMS == 2) out[(staged_rows + r) * padded + c] = lo;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (!AGAIN) m = max(m, finite_bits(v[k]));
+          split_half(v[k] * f, hi[k], lo[k]);
+        }
+      } else {
+        const unsigned short* from = reinterpret_cast<const unsigned short*>(o.x) + at * o.ld;
+        if (WIDE) {
+          const uint4 x = r < n && c < dim ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0u, 0u, 0u, 0u);
+          const uint32_t b[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int k = 0; k < 8; ++k) hi[k] = (unsigned short)(b[k / 2] >> (k % 2 * 16));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) hi[k] = r < n && c + k < dim ? from[c + k] : (unsigned short)0;
+        }
       }
+      auto pack = [](const unsigned short (&x)[8]) {
+        return make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+      };
+      *reinterpret_cast<uint4*>(o.out + r * padded + c) = pack(hi);
+      if (TERMS == 2) *reinterpret_cast<uint4*>(o.out + (o.staged_rows + r) * padded + c) = pack(lo);
     }
-    if (dead && r >= n && r < rows)
-      for (int c = threadIdx.x; c < dim; c += 256) dead[at * ld_dead + c] = from_f64<T>(0.0);
+    if (!AGAIN && o.dead && r >= n && r < o.rows)
+      for (int k = 0; k < 8 && c + k < dim; ++k) o.dead[at * o.ld_dead + c + k] = from_f64<T>(0.0);
+  }
+  if (SCALED && !AGAIN && o.sampled) {
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((threadIdx.x & 31) == 0 && m) atomicMax(o.most + 1, m);
   }
 }
 
@@ -774,20 +870,34 @@ __global__ void __launch_bounds__(1024) total_kernel(const LossInfo* info, const
 __device__ __forceinline__ void put(float* at, float v) { *at = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2bfloat16_rn(v); }
 
-// dh of the piece's rows: the sums over the shares of K, in order, to the rows they belong to
-template <typename T>
+// dh of the piece's rows: the sums over the shares of K, in order, to the rows they belong to, four columns a thread
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 dh_rows_kernel(LossArgs a, const float* slab, int splits, int slab_rows, int padded, int first, int piece, const int* row,
                const LossInfo* info, T* dh) {
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
-  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? range_exponent(info->w_max) : 0)));
-  for (int r = blockIdx.x; r < live; r += gridDim.x) {
-    T* to = dh + (int64_t)row[first + r] * a.ld_dh;
-    for (int c = threadIdx.x; c < a.dim; c += 256) {
-      float v = 0.f;
-      for (int s = 0; s < splits; ++s) v += slab[((size_t)s * slab_rows + r) * padded + c];
-      put(to + c, f * v);
+  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, a.sampled_w)));
+  const uint32_t per = (uint32_t)(a.dim + 3) / 4;
+  const int64_t items = (int64_t)live * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per;
+    const int c = (int)(i % per) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < splits; ++s) {
+      const float4 x = *reinterpret_cast<const float4*>(slab + ((size_t)s * slab_rows + r) * padded + c);
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+    T* to = dh + (int64_t)row[first + r] * a.ld_dh + c;
+    if (WIDE) {
+      if (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = v;
+      else *reinterpret_cast<uint2*>(to) = make_uint2(bf162_bits(v.x, v.y), bf162_bits(v.z, v.w));
+    } else {
+      const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < a.dim) put(to + k, x[k]);
     }
   }
 }
@@ -961,21 +1071,44 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   // bf16 operands of the loss alone are taken as they are
   const bool scaled = TERMS == 2 || gradient;
   a.scaled = scaled;
+  a.sampled_h = scaled && a.rows * a.dim * (int64_t)sizeof(T) > kSampledBytes;
+  a.sampled_w = scaled && (int64_t)a.vocab * a.dim * (int64_t)sizeof(T) > kSampledBytes;
   MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
   const unsigned wide = 148 * 8;
   if (a.rows > 0) {
     count_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, l.counts);
     index_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, l.counts, l.blocks, l.row, l.target, l.g, loss, l.info);
+    Operand<T> oh = {h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, l.info->h_max, a.sampled_h, l.h, dh, a.ld_dh};
+    Operand<T> ow = {w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, l.info->w_max, a.sampled_w, l.w, nullptr, 0};
+    if (l.in_place) ow.rows = ow.staged_rows = 0;
+    auto aligned = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
+    const bool rows16 = aligned(h, a.ld_h) && aligned(w, a.ld_w) && a.dim * (int64_t)sizeof(T) % 16 == 0;
+    // blocks by the operands' shares of the work, eight a multiprocessor at the most
+    auto blocks_for = [&](int64_t rows) {
+      const int64_t want = (rows * (l.padded / 8) + 511) / 512;
+      return want < 8 * (int64_t)sm_count() ? want : 8 * (int64_t)sm_count();
+    };
+    const int64_t bw = blocks_for(ow.rows), bh = blocks_for(a.rows + kTile);
+    auto stage = [&](auto kernel) { kernel<<<(unsigned)(bw + bh), 256, 0, s>>>(ow, oh, a.dim, l.padded, bw); };
+    auto look = [&](auto kernel) { kernel<<<(unsigned)(bw + bh), 256, 0, s>>>(ow, oh, a.dim, bw); };
     if (scaled) {
-      largest_kernel<T><<<wide, 256, 0, s>>>(h, l.row, &l.info->live, a.rows, a.dim, a.ld_h, &l.info->h_max);
-      largest_kernel<T><<<wide, 256, 0, s>>>(w, nullptr, nullptr, a.vocab, a.dim, a.ld_w, &l.info->w_max);
-      stage_kernel<T, TERMS, true><<<wide, 256, 0, s>>>(h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, a.dim, l.padded, &l.info->h_max, l.h, dh, a.ld_dh);
-      stage_kernel<T, TERMS, true><<<wide, 256, 0, s>>>(w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, a.dim, l.padded, &l.info->w_max, l.w, (T*)nullptr, 0);
-      MW_TRY(launch_ok(6));
+      if (rows16) {
+        look(largest_kernel<T, true>);
+        stage(stage_kernel<T, TERMS, true, true, false>);
+      } else {
+        look(largest_kernel<T, false>);
+        stage(stage_kernel<T, TERMS, true, false, false>);
+      }
+      MW_TRY(launch_ok(4));
+      if (a.sampled_h || a.sampled_w) {
+        if (rows16) stage(stage_kernel<T, TERMS, true, true, true>);
+        else stage(stage_kernel<T, TERMS, true, false, true>);
+        MW_TRY(launch_ok());
+      }
     } else {
-      stage_kernel<T, 1, false><<<wide, 256, 0, s>>>(h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, a.dim, l.padded, nullptr, l.h, (T*)nullptr, 0);
-      if (!l.in_place) stage_kernel<T, 1, false><<<wide, 256, 0, s>>>(w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, a.dim, l.padded, nullptr, l.w, (T*)nullptr, 0);
-      MW_TRY(launch_ok(l.in_place ? 3 : 4));
+      if (rows16) stage(stage_kernel<T, 1, false, true, false>);
+      else stage(stage_kernel<T, 1, false, false, false>);
+      MW_TRY(launch_ok(3));
     }
   }
   if (a.rows > 0 || dw) {
@@ -986,7 +1119,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     p.info = l.info;
     p.st = &l.info->st;
     p.vocab = a.vocab; p.dim = a.dim;
-    p.scale = a.scale; p.scaled = scaled;
+    p.scale = a.scale; p.scaled = scaled; p.sampled_h = a.sampled_h; p.sampled_w = a.sampled_w;
     p.piece = l.piece;
     p.sum_blocks = l.sum_blocks;
     p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
@@ -1038,7 +1171,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
         MW_TRY(launch_ok());
         if (dh) {
           MW_TRY((run_product<TERMS, P_DH>(by_h, tm * by_h.tiles_n * l.splits, s)));
-          dh_rows_kernel<T><<<wide, 256, 0, s>>>(a, l.slab, l.splits, l.piece_rows, l.padded, (int)first, l.piece, l.row, l.info, dh);
+          auto rows_kernel = ((uintptr_t)dh & 15) == 0 && a.ld_dh % 4 == 0 && a.dim % 4 == 0 ? dh_rows_kernel<T, true> : dh_rows_kernel<T, false>;
+          rows_kernel<<<wide, 256, 0, s>>>(a, l.slab, l.splits, l.piece_rows, l.padded, (int)first, l.piece, l.row, l.info, dh);
           MW_TRY(launch_ok());
         }
       }
