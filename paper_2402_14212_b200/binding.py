@@ -7,7 +7,9 @@ device is absent, calls raise.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
+import operator
 import os
 from typing import List, NamedTuple, Optional, Sequence
 
@@ -1083,19 +1085,26 @@ def clip_gradients(grads, max_norm: float, out=None, stream=None):
         return _on_stream(stream, grads[0], clip_gradients, grads, max_norm, out)
     n, device = len(grads), grads[0].device
     _need(grads[0].is_cuda and len(out) == n, "clip_gradients: CUDA tensors, and as many outputs")
+    Tensor, in_place = torch.Tensor, all(map(operator.is_, grads, out))
+    # (whole lists at a time: a step has hundreds of tensors, and the loop over them is the call's time)
+    kinds, sizes = [g.dtype for g in grads], list(map(Tensor.numel, grads))
+    ok = all(map(Tensor.is_contiguous, grads)) and set(map(Tensor.get_device, grads)) == {device.index}
+    if not in_place:
+        ok = ok and all(map(Tensor.is_contiguous, out)) and set(map(Tensor.get_device, out)) == {device.index}
+        ok = ok and kinds == [o.dtype for o in out] and sizes == list(map(Tensor.numel, out))
     codes = {torch.float32: 1, torch.bfloat16: 2}
-    for g, o in zip(grads, out):
-        if not (g.dtype in codes and g.is_contiguous() and g.device == device and
-                (o is g or (o.dtype == g.dtype and o.shape == g.shape and o.is_contiguous() and o.device == device))):
-            raise ValueError("clip_gradients: contiguous float32 or bfloat16 tensors on one device, outputs like them")
+    if not ok or not codes.keys() >= set(kinds):
+        raise ValueError("clip_gradients: contiguous float32 or bfloat16 tensors on one device, outputs like them")
     need = C.c_size_t()
     _check(lib().mw_clip_scratch_bytes(n, need), "mw_clip_scratch_bytes")
     norm = torch.empty((), dtype=torch.float32, device=device)
-    scratch = torch.empty(int(need.value), dtype=torch.uint8, device=device)
-    ptrs = C.c_void_p * n
-    _check(_call("mw_clip_gradients", device, n, ptrs(*[g.data_ptr() for g in grads]), ptrs(*[o.data_ptr() for o in out]),
-                 (C.c_int64 * n)(*[g.numel() for g in grads]), (C.c_int32 * n)(*[codes[g.dtype] for g in grads]),
-                 float(max_norm), norm.data_ptr(), scratch.data_ptr(), int(need.value)), "mw_clip_gradients")
+    scratch = torch.empty(need.value, dtype=torch.uint8, device=device)
+    ptrs = (C.c_void_p * n).from_buffer
+    src = ptrs(array.array("Q", map(Tensor.data_ptr, grads)))
+    dst = src if in_place else ptrs(array.array("Q", map(Tensor.data_ptr, out)))
+    _check(_call("mw_clip_gradients", device, n, src, dst, (C.c_int64 * n).from_buffer(array.array("q", sizes)),
+                 (C.c_int32 * n).from_buffer(array.array("i", map(codes.__getitem__, kinds))),
+                 float(max_norm), norm.data_ptr(), scratch.data_ptr(), need.value), "mw_clip_gradients")
     return norm
 
 

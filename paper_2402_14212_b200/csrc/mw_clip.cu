@@ -10,9 +10,10 @@ namespace mw {
 namespace {
 
 constexpr int kGroup = 256;             // tensors of one launch
-constexpr int kChunk = 8192;            // elements
+constexpr int kChunkBytes = 32768;      // of a tensor, a block at a time
 constexpr int kClipThreads = 512;
-constexpr int kClipBlocks = 296;
+constexpr int kClipBlocks = 592;        // four a multiprocessor
+constexpr int kAccesses = kChunkBytes / 16 / kClipThreads;      // of 16 bytes, a thread, all under way at once
 
 struct ClipGroup {
   const void* in[kGroup];
@@ -42,23 +43,64 @@ __device__ __forceinline__ double block_sum(double v, double* warp_sum) {
   return t;
 }
 
+struct Share { int64_t first; int count; bool wide, bf16; const char* in; char* out; };
+__device__ __forceinline__ Share share_of(const ClipGroup& g, int64_t chunk) {
+  const int t = tensor_of(g, chunk);
+  Share c;
+  c.bf16 = g.bf16[t];
+  const int e = c.bf16 ? 2 : 4, per = kChunkBytes / e;
+  c.first = (chunk - g.first[t]) * per;
+  const int64_t left = g.size[t] - c.first;
+  c.count = (int)(left < per ? left : per);
+  c.in = static_cast<const char*>(g.in[t]) + c.first * e;
+  c.out = g.out[t] ? static_cast<char*>(g.out[t]) + c.first * e : nullptr;
+  c.wide = (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0;
+  return c;
+}
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ float element(const Share& c, int i) {
+  return c.bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(c.in)[i]) : reinterpret_cast<const float*>(c.in)[i];
+}
+__device__ __forceinline__ void add_square(double& sum, float v) { sum = fma((double)v, (double)v, sum); }
+
 __global__ void __launch_bounds__(kClipThreads) squares_kernel(const __grid_constant__ ClipGroup g, double* partial) {
   __shared__ double warp_sum[kClipThreads / 32];
   double sum = 0.0;
-  for (int64_t c = blockIdx.x; c < g.first[g.count]; c += gridDim.x) {
-    const int t = tensor_of(g, c);
-    const int64_t i0 = (c - g.first[t]) * kChunk;
-    const int n = (int)(g.size[t] - i0 < kChunk ? g.size[t] - i0 : kChunk);
-    for (int i = threadIdx.x; i < n; i += kClipThreads) {
-      const double v = g.bf16[t] ? (double)__bfloat162float(static_cast<const __nv_bfloat16*>(g.in[t])[i0 + i])
-                                 : (double)static_cast<const float*>(g.in[t])[i0 + i];
-      sum = fma(v, v, sum);
+  for (int64_t chunk = blockIdx.x; chunk < g.first[g.count]; chunk += gridDim.x) {
+    const Share c = share_of(g, chunk);
+    int done = 0;
+    if (c.wide) {
+      const int vecs = c.count * (c.bf16 ? 2 : 4) / 16;
+      uint4 x[kAccesses];
+#pragma unroll
+      for (int k = 0; k < kAccesses; ++k) {
+        const int i = k * kClipThreads + threadIdx.x;
+        x[k] = i < vecs ? reinterpret_cast<const uint4*>(c.in)[i] : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int k = 0; k < kAccesses; ++k) {
+        const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (c.bf16) {
+            add_square(sum, low(w[q]));
+            add_square(sum, high(w[q]));
+          } else {
+            add_square(sum, __uint_as_float(w[q]));
+          }
+        }
+      }
+      done = vecs * (c.bf16 ? 8 : 4);
     }
+#pragma unroll 8
+    for (int i = done + threadIdx.x; i < c.count; i += kClipThreads) add_square(sum, element(c, i));
   }
   sum = block_sum(sum, warp_sum);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
+// Chunks are taken from the last to the first: what the squares have just read is still in L2.
 __global__ void __launch_bounds__(kClipThreads)
 scale_kernel(const __grid_constant__ ClipGroup g, const double* __restrict__ partial, int partials, double max_norm, float* norm_out) {
   __shared__ double warp_sum[kClipThreads / 32];
@@ -67,17 +109,40 @@ scale_kernel(const __grid_constant__ ClipGroup g, const double* __restrict__ par
   const double norm = sqrt(block_sum(sum, warp_sum));
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const float k = norm > max_norm && isfinite(norm) ? (float)(max_norm / norm) : 1.f;
-  for (int64_t c = blockIdx.x; c < g.first[g.count]; c += gridDim.x) {
-    const int t = tensor_of(g, c);
-    if (!g.out[t] || (k == 1.f && g.in[t] == g.out[t])) continue;
-    const int64_t i0 = (c - g.first[t]) * kChunk;
-    const int n = (int)(g.size[t] - i0 < kChunk ? g.size[t] - i0 : kChunk);
-    for (int i = threadIdx.x; i < n; i += kClipThreads) {
-      if (g.bf16[t])
-        static_cast<__nv_bfloat16*>(g.out[t])[i0 + i] =
-            __float2bfloat16_rn(k * __bfloat162float(static_cast<const __nv_bfloat16*>(g.in[t])[i0 + i]));
-      else
-        static_cast<float*>(g.out[t])[i0 + i] = k * static_cast<const float*>(g.in[t])[i0 + i];
+  for (int64_t chunk = g.first[g.count] - 1 - blockIdx.x; chunk >= 0; chunk -= gridDim.x) {
+    const Share c = share_of(g, chunk);
+    if (!c.out || (k == 1.f && c.in == c.out)) continue;
+    int done = 0;
+    if (c.wide) {
+      const int vecs = c.count * (c.bf16 ? 2 : 4) / 16;
+      uint4 x[kAccesses];
+#pragma unroll
+      for (int j = 0; j < kAccesses; ++j) {
+        const int i = j * kClipThreads + threadIdx.x;
+        if (i < vecs) x[j] = reinterpret_cast<const uint4*>(c.in)[i];
+      }
+#pragma unroll
+      for (int j = 0; j < kAccesses; ++j) {
+        const int i = j * kClipThreads + threadIdx.x;
+        uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (c.bf16) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(k * low(w[q]), k * high(w[q]));
+            w[q] = *reinterpret_cast<const uint32_t*>(&h);
+          } else {
+            w[q] = __float_as_uint(k * __uint_as_float(w[q]));
+          }
+        }
+        if (i < vecs) reinterpret_cast<uint4*>(c.out)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      done = vecs * (c.bf16 ? 8 : 4);
+    }
+#pragma unroll 8
+    for (int i = done + threadIdx.x; i < c.count; i += kClipThreads) {
+      const float v = k * element(c, i);
+      if (c.bf16) reinterpret_cast<__nv_bfloat16*>(c.out)[i] = __float2bfloat16_rn(v);
+      else reinterpret_cast<float*>(c.out)[i] = v;
     }
   }
 }
@@ -119,7 +184,8 @@ extern "C" mw_status mw_clip_gradients(int32_t count, const void* const* in, voi
       g.size[k] = sizes[k0 + k];
       g.bf16[k] = dtypes[k0 + k] == MW_BF16_F32ACC;
       g.first[k] = chunks;
-      chunks += (sizes[k0 + k] + kChunk - 1) / kChunk;
+      const int64_t per = kChunkBytes / (g.bf16[k] ? 2 : 4);
+      chunks += (sizes[k0 + k] + per - 1) / per;
     }
     g.first[g.count] = chunks;
   };

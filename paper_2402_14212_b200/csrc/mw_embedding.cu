@@ -4,6 +4,11 @@
 // and V rows written).  The gradient sorts (token, position) by a stable radix sort, so that a token's positions
 // stand in a run, in order; runs are summed in float by warps that take 32 entries of the sorted list each,
 // whatever the runs' lengths, and what a run leaves in several warps' shares is joined in order afterwards.
+//
+// Up to 65536 tokens are sorted by one cluster of eight blocks, in their shared memory, while the other blocks of the
+// same launch fill the table's gradient with zeros: the sort's latency hides behind that.  More go through
+// three launches a digit.
+#include "mw_cluster.cuh"
 #include "mw_common.cuh"
 
 namespace mw {
@@ -21,7 +26,28 @@ struct EmbedArgs {
   float scale;
 };
 
-// VEC elements of a row as floats
+// VEC elements of a row: as they are, and as floats
+template <typename T, int VEC>
+struct RawOf { using type = uint4; };
+template <typename T>
+struct RawOf<T, 1> { using type = T; };
+template <typename T, int VEC>
+__device__ __forceinline__ void widen(const typename RawOf<T, VEC>::type& raw, float (&v)[VEC]) {
+  if constexpr (VEC == 1) {
+    v[0] = to_f32(raw);
+  } else {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (VEC == 4) {
+        v[i] = __uint_as_float(w[i]);
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+}
 template <typename T, int VEC>
 __device__ __forceinline__ void load_vec(const T* at, float (&v)[VEC]) {
   if (VEC == 1) {
@@ -200,111 +226,302 @@ radix_place_kernel(Entries<I> in, uint32_t n, int shift, const uint32_t* __restr
   }
 }
 
+// ---- the same sort by one cluster, beside blocks that write zeros ------------------------------
+constexpr int kSortBlocks = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortRounds = 8;
+constexpr int kSortBits = 9, kSortDigits = 1 << kSortBits;
+constexpr int kSortMost = kSortBlocks * kSortThreads * kSortRounds;        // tokens
+// shared memory: counts a warp, sums, first places; keys and positions of one pass
+constexpr size_t kSortFixed = (size_t)kSortWarps * kSortDigits * 2 + 2 * kSortDigits * 4;
+constexpr size_t sort_smem(int rounds) { return kSortFixed + (size_t)kSortThreads * rounds * 8; }
+
+// zeros into `count` elements from `to` on, by `threads` threads
+template <typename G>
+__device__ __forceinline__ void zero_row(G* to, int dim, int thread, int threads, bool wide) {
+  if (wide) {
+    for (int c = thread; c < dim * (int)sizeof(G) / 16; c += threads) reinterpret_cast<uint4*>(to)[c] = make_uint4(0u, 0u, 0u, 0u);
+  } else {
+    for (int c = thread; c < dim; c += threads) to[c] = from_f64<G>(0.0);
+  }
+}
+
+template <typename I, typename G>
+__global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(kSortThreads)
+sort_kernel(const I* __restrict__ tokens, uint32_t n, int vocab, int passes, int bits, int rounds, uint32_t* __restrict__ key_out,
+            uint32_t* __restrict__ pos_out, uint32_t* joins, G* dtable, int dim, int64_t ld, bool wide) {
+  extern __shared__ uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x >= kSortBlocks) {
+    // a warp a row
+    const int64_t warps = (int64_t)(gridDim.x - kSortBlocks) * kSortWarps;
+    for (int64_t r = (int64_t)(blockIdx.x - kSortBlocks) * kSortWarps + warp; r < vocab; r += warps)
+      zero_row(dtable + r * ld, dim, lane, 32, wide);
+    return;
+  }
+  uint16_t(*count)[kSortDigits] = reinterpret_cast<uint16_t(*)[kSortDigits]>(smem);
+  uint32_t* sum = reinterpret_cast<uint32_t*>(smem + (size_t)kSortWarps * kSortDigits * 2);
+  uint32_t* first = sum + kSortDigits;
+  uint2* entry = reinterpret_cast<uint2*>(smem + kSortFixed);        // (key, position) that the pass before sent here
+  __shared__ uint32_t warp_sum[kSortWarps];
+  const int rank = (int)blockIdx.x;
+  const uint32_t share = (uint32_t)kSortThreads * rounds, base = rank * share;
+  const int digits = 1 << bits;
+  if (rank == 0 && threadIdx.x == 0) *joins = 0;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * bits;
+    for (int d = lane; d < digits; d += 32) count[warp][d] = 0;
+    __syncwarp();
+    // a warp's keys are consecutive, 32 a round: a key's rank in its warp counts those of its digit before it
+    uint32_t key[kSortRounds], pos[kSortRounds], before[kSortRounds];
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+      const uint32_t i = (uint32_t)warp * 32 * rounds + k * 32 + lane;
+      key[k] = 0xffffffffu;
+      pos[k] = 0;
+      if (k < rounds && base + i < n) {
+        if (pass == 0) {
+          key[k] = (uint32_t)row_of(tokens[base + i], vocab);
+          pos[k] = base + i;
+        } else {
+          const uint2 e = entry[i];
+          key[k] = e.x;
+          pos[k] = e.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+      if (k >= rounds) break;
+      const bool on = key[k] != 0xffffffffu;
+      const uint32_t d = on ? (key[k] >> shift) & (digits - 1) : kSortDigits;
+      const uint32_t same = __match_any_sync(0xffffffffu, d);
+      const uint32_t had = on ? count[warp][d] : 0;
+      before[k] = had + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (on && (same >> lane) == 1u) count[warp][d] = (uint16_t)(had + __popc(same));      // the last lane of the digit
+      __syncwarp();
+    }
+    __syncthreads();
+    if (threadIdx.x < digits) {
+      uint32_t at = 0;
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = count[w][threadIdx.x];
+        count[w][threadIdx.x] = (uint16_t)at;
+        at += c;
+      }
+      sum[threadIdx.x] = at;
+    }
+    cluster_sync();
+    {
+      // first place of a digit: all smaller digits, and this one's in the blocks before
+      uint32_t all = 0, mine = 0;
+      if (threadIdx.x < digits) {
+        const uint32_t at = shared_address(sum + threadIdx.x);
+#pragma unroll
+        for (int r = 0; r < kSortBlocks; ++r) {
+          uint32_t c;
+          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(in_rank(at, r)) : "memory");
+          all += c;
+          if (r < rank) mine += c;
+        }
+      }
+      uint32_t x = all;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      if (lane == 31) warp_sum[warp] = x;
+      __syncthreads();
+      for (int w = 0; w < warp && w < kSortDigits / 32; ++w) mine += warp_sum[w];
+      if (threadIdx.x < digits) first[threadIdx.x] = mine + x - all;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+      if (k < rounds && key[k] != 0xffffffffu) {
+        const uint32_t d = (key[k] >> shift) & (digits - 1);
+        const uint32_t to = first[d] + count[warp][d] + before[k];
+        if (pass + 1 == passes) {
+          key_out[to] = key[k];
+          pos_out[to] = pos[k];
+        } else {
+          const uint32_t r = to / share;
+          asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(in_rank(shared_address(entry + (to - r * share)), (int)r)),
+                       "r"(key[k]), "r"(pos[k])
+                       : "memory");
+        }
+      }
+    }
+    cluster_sync();
+  }
+}
+
 // ---- sums of runs -----------------------------------------------------------------------------
 template <typename G>
-__global__ void __launch_bounds__(256) zero_rows_kernel(G* dtable, int64_t rows, int dim, int64_t ld) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int c = threadIdx.x; c < dim; c += 256) put(dtable + r * ld + c, 0.f);
+__global__ void __launch_bounds__(256) zero_rows_kernel(G* dtable, int64_t rows, int dim, int64_t ld, bool wide) {
+  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * 8)
+    zero_row(dtable + r * ld, dim, threadIdx.x & 31, 32, wide);
 }
 
-template <typename G, int VEC, bool ADD>
+// VEC columns of a row, GVEC of them an access (1 where the rows of the gradient do not lie on boundaries)
+template <typename G, int VEC, bool ADD, bool GWIDE>
 __device__ __forceinline__ void write_sum(G* at, float (&v)[VEC], float scale) {
-  float old[VEC];
+  if (ADD) {
+    float old[VEC];
+    if (GWIDE && VEC > 1 && VEC * sizeof(G) >= 16) {
+      constexpr int kPer = VEC > 1 ? 16 / (int)sizeof(G) : 1;
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) old[k] = ADD ? to_f32(at[k]) : 0.f;
+      for (int k = 0; k < VEC; k += kPer) {
+        float part[kPer];
+        load_vec<G, kPer>(at + k, part);
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) v[k] = ADD ? fmaf(scale, v[k], old[k]) : scale * v[k];
+        for (int i = 0; i < kPer; ++i) old[(k + i) % VEC] = part[i];
+      }
+    } else {
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) put(at + k, v[k]);
+      for (int k = 0; k < VEC; ++k) old[k] = to_f32(at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v[k] = fmaf(scale, v[k], old[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v[k] = scale * v[k];
+  }
+  if (GWIDE) {
+    store_vec<G, VEC>(at, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) put(at + k, v[k]);
+  }
 }
 
-// A warp sums one piece of the sorted list over 32 VEC columns.  A run that lies whole in the piece goes to its
-// row; what a piece holds of a run that came from the piece before goes to its first partial sum, of one
-// that starts here and goes on to its second.
-template <typename T, typename G, int VEC, bool ADD>
+// A warp sums one piece of the sorted list over 32 VEC columns, eight rows under way at a time.  A run that lies
+// whole in the piece goes to its row; what a piece holds of a run that came from the piece before goes to its
+// first partial sum, of one that starts here and goes on to its second, and the piece is listed for the join.
+template <typename T, typename G, int VEC, bool ADD, bool GWIDE>
 __global__ void __launch_bounds__(256)
 run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,
-                G* __restrict__ dtable, float* __restrict__ partial, int col_groups) {
+                G* __restrict__ dtable, float* __restrict__ partial, int col_groups, uint32_t* joins) {
+  constexpr int kAhead = 8;
   const int lane = threadIdx.x & 31;
   const uint32_t n = (uint32_t)a.n;
   const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const uint32_t p = (uint32_t)(w / col_groups), i0 = p * kPiece;
   if (i0 >= n) return;
-  const int c = ((int)(w - (int64_t)p * col_groups) * 32 + lane) * VEC;
+  const int group = (int)(w - (int64_t)p * col_groups);
+  const int c = (group * 32 + lane) * VEC;
   const bool on = c < a.dim;
-  const int count = (int)(n - i0 < kPiece ? n - i0 : kPiece);
+  int count = (int)(n - i0 < kPiece ? n - i0 : kPiece);
   const uint32_t my_key = lane < count ? key[i0 + lane] : 0xffffffffu;
   const uint32_t my_pos = lane < count ? pos[i0 + lane] : 0;
   const uint32_t before = i0 ? key[i0 - 1] : 0xffffffffu;
   const uint32_t after = i0 + kPiece < n ? key[i0 + kPiece] : 0xffffffffu;
+  // tokens that name no row come last
+  count = __popc(__ballot_sync(0xffffffffu, my_key < (uint32_t)a.vocab));
   float acc[VEC];
 #pragma unroll
   for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
   bool from_before = __shfl_sync(0xffffffffu, my_key, 0) == before;
-  for (int i = 0; i < count; ++i) {
-    const uint32_t v = __shfl_sync(0xffffffffu, my_key, i), r = __shfl_sync(0xffffffffu, my_pos, i);
-    const uint32_t next = __shfl_sync(0xffffffffu, my_key, i + 1 < count ? i + 1 : i);
-    if (v >= (uint32_t)a.vocab) break;            // tokens that name no row come last
-    if (on) {
-      float x[VEC];
-      load_vec<T, VEC>(dout + r * a.ld_out + c, x);
+  const int width = (a.dim + 3) / 4 * 4;
+  for (int b = 0; b < count; b += kAhead) {
+    using Raw = typename RawOf<T, VEC>::type;
+    Raw x[kAhead];
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) acc[k] += x[k];
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t r = __shfl_sync(0xffffffffu, my_pos, (b + k) & 31);
+      if (on && b + k < count) x[k] = *reinterpret_cast<const Raw*>(dout + r * a.ld_out + c);
     }
-    const bool last = i + 1 == count, goes_on = last && v == after;
-    if (!last && next == v) continue;
-    if (on) {
-      if (from_before || goes_on) {
-        float* to = partial + ((size_t)p * 2 + (from_before ? 0 : 1)) * a.dim + c;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) to[k] = acc[k];
-      } else {
-        write_sum<G, VEC, ADD>(dtable + v * a.ld_dtable + c, acc, a.scale);
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = b + k;
+      if (i < count) {
+        const uint32_t v = __shfl_sync(0xffffffffu, my_key, i & 31);
+        const uint32_t next = i == kPiece - 1 ? after : __shfl_sync(0xffffffffu, my_key, (i + 1) & 31);
+        if (on) {
+          float y[VEC];
+          widen<T, VEC>(x[k], y);
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) acc[q] += y[q];
+        }
+        if (next != v || i == kPiece - 1) {
+          const bool goes_on = next == v;
+          if (on) {
+            if (from_before || goes_on)
+              store_vec<float, VEC>(partial + ((size_t)p * 2 + (from_before ? 0 : 1)) * width + c, acc);
+            else
+              write_sum<G, VEC, ADD, GWIDE>(dtable + v * a.ld_dtable + c, acc, a.scale);
+          }
+          if (goes_on && !from_before && group == 0 && lane == 0) joins[1 + atomicAdd(joins, 1u)] = p;
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) acc[q] = 0.f;
+          from_before = false;
+        }
       }
     }
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
-    from_before = false;
   }
 }
 
-// A block joins the run that starts in its piece and goes on beyond it: the piece's second partial sum, then the
-// first ones of the pieces after, each warp every eighth of them, the warps' sums in order.
+// A block joins 256 columns of a run that starts in a listed piece and goes on beyond it: the piece's second partial
+// sum, then the first ones of the pieces after, each of eight rows of threads every eighth of them, the rows' sums in
+// order.  (The order of the list is that of the atomics; what is summed, and how, is not.)
+constexpr int kJoinRows = 8, kJoinColumns = 256, kJoinThreads = kJoinRows * kJoinColumns / 4;
 template <typename G, bool ADD>
-__global__ void __launch_bounds__(256)
-join_runs_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const float* __restrict__ partial, G* __restrict__ dtable) {
-  __shared__ float sums[8][32];
-  const uint32_t n = (uint32_t)a.n, p = blockIdx.x, i0 = p * kPiece;
-  const uint32_t end = i0 + kPiece;
-  if (end >= n) return;
-  const uint32_t v = key[end];
-  if (v >= (uint32_t)a.vocab || key[end - 1] != v || (key[i0] == v && i0 && key[i0 - 1] == v)) return;
-  // one past the run's last entry
-  uint32_t lo = end, hi = n;
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (key[mid] == v) lo = mid + 1; else hi = mid;
-  }
-  const uint32_t last_piece = (lo - 1) / kPiece;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int c0 = blockIdx.y * 32; c0 < a.dim; c0 += gridDim.y * 32) {
-    const int c = c0 + lane;
-    float acc = 0.f;
-    if (c < a.dim)
-      for (uint32_t q = p + 1 + warp; q <= last_piece; q += 8) acc += partial[(size_t)q * 2 * a.dim + c];
-    sums[warp][lane] = acc;
+__global__ void __launch_bounds__(kJoinThreads)
+join_runs_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const float* __restrict__ partial, G* __restrict__ dtable,
+                 const uint32_t* __restrict__ joins) {
+  __shared__ float4 sums[kJoinRows][kJoinColumns / 4];
+  const uint32_t n = (uint32_t)a.n;
+  const int across = threadIdx.x % (kJoinColumns / 4), down = threadIdx.x / (kJoinColumns / 4), lane = threadIdx.x & 31;
+  const uint32_t groups = (uint32_t)(a.dim + kJoinColumns - 1) / kJoinColumns;
+  const int width = (a.dim + 3) / 4 * 4;
+  const uint64_t items = (uint64_t)joins[0] * groups;
+  for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t p = joins[1 + item / groups];
+    const int c = (int)(item % groups) * kJoinColumns + across * 4;
+    const uint32_t v = key[p * kPiece + kPiece];
+    // the run's last entry, by 32 probes at a time
+    uint32_t lo = p * kPiece + kPiece, hi = n;
+    while (hi - lo > 1) {
+      const uint32_t step = (hi - lo + 31) / 32, at = lo + step * lane;
+      const uint32_t in = __ballot_sync(0xffffffffu, at < hi && key[at] == v);
+      const uint32_t last = lo + step * (31 - __clz(in));          // (lane 0's is of the run)
+      hi = hi < last + step ? hi : last + step;
+      lo = last;
+    }
+    const uint32_t last_piece = lo / kPiece;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < a.dim) {
+#pragma unroll 8
+      for (uint32_t q = p + 1 + down; q <= last_piece; q += kJoinRows) {
+        const float4 x = *reinterpret_cast<const float4*>(partial + (size_t)q * 2 * width + c);
+        acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+      }
+    }
+    sums[down][across] = acc;
     __syncthreads();
-    if (warp == 0 && c < a.dim) {
-      float t[1] = {partial[((size_t)p * 2 + 1) * a.dim + c]};
-      for (int w = 0; w < 8; ++w) t[0] += sums[w][lane];
-      write_sum<G, 1, ADD>(dtable + v * a.ld_dtable + c, t, a.scale);
+    if (down == 0 && c < a.dim) {
+      float4 t = *reinterpret_cast<const float4*>(partial + ((size_t)p * 2 + 1) * width + c);
+#pragma unroll
+      for (int w = 0; w < kJoinRows; ++w) {
+        const float4 x = sums[w][across];
+        t.x += x.x; t.y += x.y; t.z += x.z; t.w += x.w;
+      }
+      const float y[4] = {t.x, t.y, t.z, t.w};
+      G* to = dtable + v * a.ld_dtable + c;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (c + k < a.dim) {
+          float one[1] = {y[k]};
+          write_sum<G, 1, ADD, false>(to + k, one, a.scale);
+        }
+      }
     }
     __syncthreads();
   }
 }
 
 struct EmbedScratch {
-  uint32_t *key[2], *pos[2], *counts;
+  uint32_t *key[2], *pos[2], *counts, *joins;
   float* partial;
   uint32_t tiles, pieces;
 };
@@ -323,7 +540,8 @@ size_t embed_layout(const mw_embedding_desc* d, char* base, EmbedScratch* l) {
     l->pos[i] = (uint32_t*)take(n * 4);
   }
   l->counts = (uint32_t*)take((size_t)l->tiles * kRadixDigits * 4);
-  l->partial = (float*)take((size_t)l->pieces * 2 * d->dim * 4);
+  l->joins = (uint32_t*)take(((size_t)l->pieces + 1) * 4);
+  l->partial = (float*)take((size_t)l->pieces * 2 * align_up((size_t)d->dim, 4) * 4);
   return at + 256;
 }
 
@@ -366,15 +584,38 @@ mw_status lookup(const mw_embedding_desc* d, const void* tokens, const void* tab
   return launch_ok();
 }
 
-template <typename T, typename G, int VEC, bool ADD>
+// Clusters of the sort that the device holds at once (asked for once a device; at least two).  Allows its
+// shared memory, too.
+template <typename K>
+mw_status sort_clusters(K kernel, int* out) {
+  static int clusters[64] = {};
+  int dev = 0;
+  MW_CUDA_OK(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || clusters[dev] == 0) {
+    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(kSortRounds)));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSortBlocks * 18);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = sort_smem(kSortRounds);
+    int c = 0;
+    MW_CUDA_OK(cudaOccupancyMaxActiveClusters(&c, kernel, &cfg));
+    if (c < 2) c = 2;
+    if (dev < 0 || dev >= 64) { *out = c; return MW_OK; }
+    clusters[dev] = c;
+  }
+  *out = clusters[dev];
+  return MW_OK;
+}
+
+template <typename T, typename G, int VEC, bool ADD, bool GWIDE>
 mw_status sum_runs(const EmbedArgs& a, const EmbedScratch& l, const uint32_t* key, const uint32_t* pos, const T* dout, G* dtable,
                    cudaStream_t s) {
   const int groups = ceil_div(a.dim, 32 * VEC);
   const int64_t warps = (int64_t)l.pieces * groups;
   if (warps > ((int64_t)1 << 34)) return MW_ERR_UNSUPPORTED;
-  run_sums_kernel<T, G, VEC, ADD><<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a, key, pos, dout, dtable, l.partial, groups);
-  const int cols = ceil_div(a.dim, 32);
-  join_runs_kernel<G, ADD><<<dim3(l.pieces, (unsigned)(cols < 64 ? cols : 64)), 256, 0, s>>>(a, key, l.partial, dtable);
+  run_sums_kernel<T, G, VEC, ADD, GWIDE><<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a, key, pos, dout, dtable, l.partial, groups, l.joins);
+  const int64_t joins = (int64_t)l.pieces * ceil_div(a.dim, kJoinColumns);
+  join_runs_kernel<G, ADD><<<(unsigned)(joins < 148 * 4 ? joins : 148 * 4), kJoinThreads, 0, s>>>(a, key, l.partial, dtable, l.joins);
   return launch_ok(2);
 }
 
@@ -384,29 +625,57 @@ mw_status table_gradient(const mw_embedding_desc* d, const void* tokens, const v
   const EmbedArgs a = embed_args(d);
   EmbedScratch l;
   embed_layout(d, scratch, &l);
-  if (!add) {
-    zero_rows_kernel<G><<<(unsigned)(a.vocab < 148 * 16 ? a.vocab : 148 * 16), 256, 0, s>>>((G*)dtable, a.vocab, a.dim, a.ld_dtable);
+  const uint32_t n = (uint32_t)a.n;
+  G* g = (G*)dtable;
+  const bool gwide = wide_rows(dtable, a.ld_dtable, a.dim, sizeof(G));
+  if (!add && (n == 0 || n > (uint32_t)kSortMost)) {
+    zero_rows_kernel<G><<<(unsigned)(a.vocab < 148 * 64 ? ceil_div(a.vocab, 8) : 148 * 8), 256, 0, s>>>(g, a.vocab, a.dim, a.ld_dtable, gwide);
     MW_TRY(launch_ok());
   }
-  if (a.n == 0) return MW_OK;
-  const uint32_t n = (uint32_t)a.n;
-  Entries<I> in = {(const I*)tokens, nullptr, nullptr, a.vocab};
-  int to = 0;
-  // keys are 0..vocab
-  for (int shift = 0; shift < 32 && ((uint32_t)a.vocab >> shift) != 0; shift += kRadixBits) {
-    radix_count_kernel<I><<<l.tiles, kRadixThreads, 0, s>>>(in, n, shift, l.counts);
-    radix_scan_kernel<<<1, 1024, 0, s>>>(l.counts, l.tiles * kRadixDigits);
-    radix_place_kernel<I><<<l.tiles, kRadixThreads, 0, s>>>(in, n, shift, l.counts, l.key[to], l.pos[to]);
-    MW_TRY(launch_ok(3));
-    in = {nullptr, l.key[to], l.pos[to], a.vocab};
-    to ^= 1;
+  if (n == 0) return MW_OK;
+  int bits = 1;                                   // keys are 0..vocab
+  while ((uint32_t)a.vocab >> bits) ++bits;
+  const uint32_t *key = l.key[0], *pos = l.pos[0];
+  if (n <= (uint32_t)kSortMost) {
+    const int passes = ceil_div(bits, kSortBits), rounds = ceil_div(n, kSortBlocks * kSortThreads);
+    auto kernel = sort_kernel<I, G>;
+    // blocks that write zeros: the clusters that run beside the sort's (one more would begin when the others end), and
+    // not more than rows
+    int fill = 0;
+    if (!add) {
+      MW_TRY(sort_clusters(kernel, &fill));
+      fill = (fill - 1) * kSortBlocks;
+      const int rows = ceil_div(ceil_div(a.vocab, kSortWarps), kSortBlocks) * kSortBlocks;
+      if (fill > rows) fill = rows;
+    } else {
+      MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(kSortRounds)));
+    }
+    kernel<<<(unsigned)(kSortBlocks + fill), kSortThreads, sort_smem(rounds), s>>>(
+        (const I*)tokens, n, a.vocab, passes, ceil_div(bits, passes), rounds, l.key[0], l.pos[0], l.joins, g, a.dim, a.ld_dtable, gwide);
+    MW_TRY(launch_ok());
+  } else {
+    MW_CUDA_OK(cudaMemsetAsync(l.joins, 0, 4, s));
+    Entries<I> in = {(const I*)tokens, nullptr, nullptr, a.vocab};
+    int to = 0;
+    for (int shift = 0; shift < bits; shift += kRadixBits) {
+      radix_count_kernel<I><<<l.tiles, kRadixThreads, 0, s>>>(in, n, shift, l.counts);
+      radix_scan_kernel<<<1, 1024, 0, s>>>(l.counts, l.tiles * kRadixDigits);
+      radix_place_kernel<I><<<l.tiles, kRadixThreads, 0, s>>>(in, n, shift, l.counts, l.key[to], l.pos[to]);
+      MW_TRY(launch_ok(3));
+      in = {nullptr, l.key[to], l.pos[to], a.vocab};
+      to ^= 1;
+    }
+    key = in.key;
+    pos = in.pos;
   }
   const T* y = (const T*)dout;
-  G* g = (G*)dtable;
   constexpr int kVec = 16 / sizeof(T);
-  if (wide_rows(dout, a.ld_out, a.dim, sizeof(T)))
-    return add ? sum_runs<T, G, kVec, true>(a, l, in.key, in.pos, y, g, s) : sum_runs<T, G, kVec, false>(a, l, in.key, in.pos, y, g, s);
-  return add ? sum_runs<T, G, 1, true>(a, l, in.key, in.pos, y, g, s) : sum_runs<T, G, 1, false>(a, l, in.key, in.pos, y, g, s);
+  // (a row on 16-byte boundaries in dout's type and in the gradient's: eight or four columns an access in both)
+  if (wide_rows(dout, a.ld_out, a.dim, sizeof(T))) {
+    if (gwide) return add ? sum_runs<T, G, kVec, true, true>(a, l, key, pos, y, g, s) : sum_runs<T, G, kVec, false, true>(a, l, key, pos, y, g, s);
+    return add ? sum_runs<T, G, kVec, true, false>(a, l, key, pos, y, g, s) : sum_runs<T, G, kVec, false, false>(a, l, key, pos, y, g, s);
+  }
+  return add ? sum_runs<T, G, 1, true, false>(a, l, key, pos, y, g, s) : sum_runs<T, G, 1, false, false>(a, l, key, pos, y, g, s);
 }
 
 template <typename T, typename G>
