@@ -93,23 +93,37 @@ __device__ __forceinline__ void store_vec(T* at, const float (&v)[VEC]) {
 template <typename I>
 __device__ __forceinline__ int row_of(I t, int vocab) { return t >= 0 && t < (I)vocab ? (int)t : vocab; }
 
-// A block takes `rows` whole rows; a thread a piece of VEC columns at a time.
+// A block takes `rows` whole rows, a thread four pieces of VEC columns at a time, whose loads are all under way
+// before the first store.
+constexpr int kLookupPieces = 4;
 template <typename T, typename I, int VEC>
 __global__ void __launch_bounds__(256)
 lookup_kernel(EmbedArgs a, const I* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int rows) {
+  using Raw = typename RawOf<T, VEC>::type;
   const int per = a.dim / VEC;
   const int64_t r0 = (int64_t)blockIdx.x * rows;
   const int here = (int)(a.n - r0 < rows ? a.n - r0 : rows);
-  for (int i = threadIdx.x; i < here * per; i += 256) {
-    const int r = i / per, c = (i - r * per) * VEC;
-    const int v = row_of(tokens[r0 + r], a.vocab);
-    float x[VEC];
+  for (int i0 = threadIdx.x; i0 < here * per; i0 += 256 * kLookupPieces) {
+    Raw x[kLookupPieces];
+    bool in[kLookupPieces];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] = 0.f;
-    if (v < a.vocab) load_vec<T, VEC>(table + v * a.ld_table + c, x);
+    for (int k = 0; k < kLookupPieces; ++k) {
+      const int i = i0 + k * 256, r = i / per, c = (i - r * per) * VEC;
+      const int v = i < here * per ? row_of(tokens[r0 + r], a.vocab) : a.vocab;
+      in[k] = v < a.vocab;
+      if (in[k]) x[k] = *reinterpret_cast<const Raw*>(table + v * a.ld_table + c);
+    }
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] *= a.scale;
-    store_vec<T, VEC>(out + (r0 + r) * a.ld_out + c, x);
+    for (int k = 0; k < kLookupPieces; ++k) {
+      const int i = i0 + k * 256, r = i / per, c = (i - r * per) * VEC;
+      float y[VEC];
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) y[q] = 0.f;
+      if (in[k]) widen<T, VEC>(x[k], y);
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) y[q] *= a.scale;
+      if (i < here * per) store_vec<T, VEC>(out + (r0 + r) * a.ld_out + c, y);
+    }
   }
 }
 
@@ -577,7 +591,9 @@ mw_status lookup(const mw_embedding_desc* d, const void* tokens, const void* tab
   constexpr int kVec = 16 / sizeof(T);
   const bool wide = wide_rows(table, a.ld_table, a.dim, sizeof(T)) && wide_rows(out, a.ld_out, a.dim, sizeof(T));
   const int per = wide ? a.dim / kVec : a.dim;
-  const int rows = per >= 1024 ? 1 : 1024 / per;
+  // 1024 pieces a block; fewer while that leaves multiprocessors idle (one row of 256 pieces is the least)
+  int rows = per >= 1024 ? 1 : 1024 / per;
+  while (rows > 1 && rows * per > 256 && ceil_div(a.n, rows) < 148 * 4) rows = (rows + 1) / 2;
   const unsigned blocks = (unsigned)((a.n + rows - 1) / rows);
   if (wide) lookup_kernel<T, I, kVec><<<blocks, 256, 0, s>>>(a, (const I*)tokens, (const T*)table, (T*)out, rows);
   else lookup_kernel<T, I, 1><<<blocks, 256, 0, s>>>(a, (const I*)tokens, (const T*)table, (T*)out, rows);

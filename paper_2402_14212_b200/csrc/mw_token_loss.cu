@@ -57,7 +57,8 @@ struct LossInfo {
   int live;                 // rows that are not left out
   unsigned g_max;           // bits of the largest |g|
   unsigned h_max[2], w_max[2];    // bits of the largest finite |h|, |W|: of a sample of the rows, and of all
-  unsigned pad2[58];
+  unsigned done;            // blocks whose losses are in
+  unsigned pad2[57];
 };
 
 // the power of two that brings numbers of at most this size to 2^13 .. 2^14
@@ -102,6 +103,8 @@ struct alignas(64) ProductArgs {
   int slab_rows;            // P_DH: rows of one split's sums
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
+  uint32_t a_bytes;         // P_SUMS, P_EXP: what A's copies bring both CTAs in a stage
+  int a_even;               // ... they are the even CTA's alone: its rows hold all there are
   float scale;
   int scaled, sampled_h, sampled_w;
   float2* sums;             // [row][sum_blocks]: power, sum
@@ -252,11 +255,11 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * kHalf;
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           if (!mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u)) { ok = false; break; }
-          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, 2u * kStage);
+          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, KIND == P_SUMS || KIND == P_EXP ? p.a_bytes + kStage : 2u * kStage);
           const uint32_t fb = full0_even + 8u * stage;
           const uint32_t base = tiles + stage * kStage;
           if (KIND == P_SUMS || KIND == P_EXP) {
-            tma_load_3d<true>(base, &p.a, fb, kb * kBK, p.first + am, 0);
+            if (rank == 0 || !p.a_even) tma_load_3d<true>(base, &p.a, fb, kb * kBK, p.first + am, 0);
             tma_load_3d<true>(base + TERMS * kPlaneBytes, &p.b, fb, kb * kBK, bn, 0);
           } else if (KIND == P_DH) {
             tma_load_4d<true>(base, &p.a, fb, 0, am, kb, 0);
@@ -560,9 +563,12 @@ index_live_kernel(const I* targets, const float* weight, int64_t rows, int vocab
   __shared__ int sums[2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x < 2) sums[threadIdx.x] = 0;
+  // a block that is alone counts for itself and clears what the call's kernels share
+  const bool alone = counts == nullptr;
+  if (alone && threadIdx.x < sizeof(LossInfo) / 4) reinterpret_cast<unsigned*>(info)[threadIdx.x] = 0;
   __syncthreads();
   int mine[2] = {0, 0};
-  for (int b = threadIdx.x; b < blocks; b += kIndexRows) {
+  for (int b = threadIdx.x; !alone && b < blocks; b += kIndexRows) {
     mine[0] += counts[b];
     if (b < (int)blockIdx.x) mine[1] += counts[b];
   }
@@ -573,7 +579,9 @@ index_live_kernel(const I* targets, const float* weight, int64_t rows, int vocab
   const unsigned on = __ballot_sync(0xffffffffu, t >= 0);
   if (lane == 0) warp_sum[warp] = __popc(on);
   __syncthreads();
-  const int live = sums[0];
+  int live = sums[0];
+  if (alone)
+    for (int w = 0; w < 32; ++w) live += warp_sum[w];
   int at = sums[1] + __popc(on & ((1u << lane) - 1u));
   for (int w = 0; w < warp; ++w) at += warp_sum[w];
   if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -756,10 +764,38 @@ __device__ __forceinline__ float loss_of(RowSum v, float zt) {
   return l < 0.f ? 0.f : l;
 }
 
+// The last block of the launch that brings the last losses adds them up, in an order that the rows' number alone sets.
+__device__ __forceinline__ void total_by_last(LossInfo* info, const double* part, float* total) {
+  __shared__ double sums[8];
+  __shared__ bool last;
+  if (total == nullptr) return;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(&info->done, 1u) + 1u == gridDim.x;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!last) return;
+  const int n = info->live;
+  double t = 0.0;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < n; i += 256) t += __ldcg(part + i);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    t = 0.0;
+    for (int i = 0; i < 8; ++i) t += sums[i];
+    *total = (float)t;
+  }
+}
+
 // losses of all live rows, a warp each
 __global__ void __launch_bounds__(256)
-loss_rows_kernel(const LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const int* row, const float* g,
-                 float* loss, double* part) {
+loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const int* row, const float* g,
+                 float* loss, double* part, float* total) {
   const int lane = threadIdx.x & 31;
   for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < info->live; i += (int64_t)gridDim.x * 8) {
     RowSum v = {kNoPower, 0.f};
@@ -774,13 +810,14 @@ loss_rows_kernel(const LossInfo* info, const float2* sums, int sum_blocks, const
       part[i] = (double)g[i] * (double)l;
     }
   }
+  total_by_last(info, part, total);
 }
 
 // a row's exponentials -> dz times a power of two, in their place: a block a row
 template <int TERMS>
 __global__ void __launch_bounds__(256)
-dz_kernel(const LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
-          const int* target, const float* g, float* loss, double* part, unsigned short* e, int vocab, int padded) {
+dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
+          const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int vocab, int padded) {
   __shared__ RowSum warp_v[8];
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
@@ -849,22 +886,7 @@ dz_kernel(const LossInfo* info, int first, int piece, const float2* sums, int su
       }
     }
   }
-}
-
-__global__ void __launch_bounds__(1024) total_kernel(const LossInfo* info, const double* part, float* total) {
-  __shared__ double sums[32];
-  const int n = info->live;
-  double t = 0.0;
-  for (int i = threadIdx.x; i < n; i += 1024) t += part[i];
-#pragma unroll
-  for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = t;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    t = 0.0;
-    for (int i = 0; i < 32; ++i) t += sums[i];
-    *total = (float)t;
-  }
+  total_by_last(info, part, total);
 }
 
 __device__ __forceinline__ void put(float* at, float v) { *at = v; }
@@ -1005,9 +1027,9 @@ mw_status make_map(CUtensorMap* out, CUtensorMapDataType type, int rank, const v
              ? MW_OK : MW_ERR_CUDA;
 }
 // operand rows with K along them: boxes of 64 columns, 128 rows and all terms
-mw_status row_map(CUtensorMap* out, bool bf16, const void* base, int64_t cols, int64_t rows, int64_t ld, int terms) {
+mw_status row_map(CUtensorMap* out, bool bf16, const void* base, int64_t cols, int64_t rows, int64_t ld, int terms, int box_rows = kHalf) {
   const int64_t dims[3] = {cols, rows, terms}, strides[2] = {ld * 2, rows * ld * 2};
-  const int box[3] = {kBK, kHalf, terms};
+  const int box[3] = {kBK, box_rows, terms};
   return make_map(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dims, strides, box);
 }
 // operand rows in groups of 64 columns: boxes of `rows_box` rows and `groups` groups
@@ -1073,11 +1095,13 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   a.scaled = scaled;
   a.sampled_h = scaled && a.rows * a.dim * (int64_t)sizeof(T) > kSampledBytes;
   a.sampled_w = scaled && (int64_t)a.vocab * a.dim * (int64_t)sizeof(T) > kSampledBytes;
-  MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
   const unsigned wide = 148 * 8;
+  if (l.blocks != 1) MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
   if (a.rows > 0) {
-    count_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, l.counts);
-    index_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, l.counts, l.blocks, l.row, l.target, l.g, loss, l.info);
+    int* counts = l.blocks > 1 ? l.counts : nullptr;
+    if (counts) count_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, counts);
+    index_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, counts, l.blocks, l.row, l.target, l.g, loss, l.info);
+    MW_TRY(launch_ok(counts ? 2 : 1));
     Operand<T> oh = {h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, l.info->h_max, a.sampled_h, l.h, dh, a.ld_dh};
     Operand<T> ow = {w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, l.info->w_max, a.sampled_w, l.w, nullptr, 0};
     if (l.in_place) ow.rows = ow.staged_rows = 0;
@@ -1099,7 +1123,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
         look(largest_kernel<T, false>);
         stage(stage_kernel<T, TERMS, true, false, false>);
       }
-      MW_TRY(launch_ok(4));
+      MW_TRY(launch_ok(2));
       if (a.sampled_h || a.sampled_w) {
         if (rows16) stage(stage_kernel<T, TERMS, true, true, true>);
         else stage(stage_kernel<T, TERMS, true, false, true>);
@@ -1108,7 +1132,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     } else {
       if (rows16) stage(stage_kernel<T, 1, false, true, false>);
       else stage(stage_kernel<T, 1, false, false, false>);
-      MW_TRY(launch_ok(3));
+      MW_TRY(launch_ok());
     }
   }
   if (a.rows > 0 || dw) {
@@ -1128,7 +1152,13 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     logits.tiles_n = ceil_div(a.vocab, kTile);
     logits.blocks_k = l.padded / kBK;
     logits.idesc = instruction(bf16, false, false);
-    MW_TRY(row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS));
+    // Few rows: only theirs are copied, the others' products come out as whatever they are and are not read.  (One term
+    // alone: the planes of two lie a whole share apart.)  The path from L2 is the limit there: 16 rows of 32768x2048
+    // bf16 40 us with all 256 rows copied, half of it with 16.
+    logits.a_even = TERMS == 1 && a.rows <= kHalf;
+    const int box_rows = !logits.a_even ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
+    logits.a_bytes = (logits.a_even ? 1u : 2u) * TERMS * (uint32_t)box_rows * kBK * 2;
+    MW_TRY(row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, box_rows));
     MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1) : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
     if (gradient) {
       const int64_t row_bytes = (int64_t)l.vpadded * 2 * TERMS, group_bytes = 128 * TERMS;
@@ -1163,10 +1193,11 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       if (a.rows > 0) {
         if (gradient) {
           MW_TRY((run_product<TERMS, P_EXP>(logits, tm * logits.tiles_n, s)));
-          dz_kernel<TERMS><<<wide, 256, 0, s>>>(l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part, l.e, a.vocab, l.vpadded);
+          dz_kernel<TERMS><<<(unsigned)(l.piece_rows < (int)wide ? l.piece_rows : wide), 256, 0, s>>>(l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part, first + l.piece >= a.rows ? total : nullptr, l.e, a.vocab, l.vpadded);
         } else {
           MW_TRY((run_product<TERMS, P_SUMS>(logits, tm * logits.tiles_n, s)));
-          loss_rows_kernel<<<wide, 256, 0, s>>>(l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part);
+          // (a warp a row)
+          loss_rows_kernel<<<(unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide), 256, 0, s>>>(l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part, total);
         }
         MW_TRY(launch_ok());
         if (dh) {
@@ -1179,10 +1210,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       if (dw) MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n, s)));
     }
   }
-  if (total) {
-    total_kernel<<<1, 1024, 0, s>>>(l.info, l.part, total);
-    MW_TRY(launch_ok());
-  }
+  if (total && a.rows == 0) MW_CUDA_OK(cudaMemsetAsync(total, 0, 4, s));
   return MW_OK;
 }
 
