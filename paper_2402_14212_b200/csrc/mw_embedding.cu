@@ -485,7 +485,7 @@ join_runs_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const float* __r
                  const uint32_t* __restrict__ joins) {
   __shared__ float4 sums[kJoinRows][kJoinColumns / 4];
   const uint32_t n = (uint32_t)a.n;
-  const int across = threadIdx.x % (kJoinColumns / 4), down = threadIdx.x / (kJoinColumns / 4), lane = threadIdx.x & 31;
+  const int across = threadIdx.x % (kJoinColumns / 4), down = threadIdx.x / (kJoinColumns / 4);
   const uint32_t groups = (uint32_t)(a.dim + kJoinColumns - 1) / kJoinColumns;
   const int width = (a.dim + 3) / 4 * 4;
   const uint64_t items = (uint64_t)joins[0] * groups;
@@ -493,16 +493,14 @@ join_runs_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const float* __r
     const uint32_t p = joins[1 + item / groups];
     const int c = (int)(item % groups) * kJoinColumns + across * 4;
     const uint32_t v = key[p * kPiece + kPiece];
-    // the run's last entry, by 32 probes at a time
-    uint32_t lo = p * kPiece + kPiece, hi = n;
-    while (hi - lo > 1) {
-      const uint32_t step = (hi - lo + 31) / 32, at = lo + step * lane;
-      const uint32_t in = __ballot_sync(0xffffffffu, at < hi && key[at] == v);
-      const uint32_t last = lo + step * (31 - __clz(in));          // (lane 0's is of the run)
-      hi = hi < last + step ? hi : last + step;
-      lo = last;
+    // the run's last piece: as many pieces after this one begin with it as stand in a row
+    const uint32_t pieces = (n + kPiece - 1) / kPiece;
+    uint32_t last_piece = p + 1;
+    for (uint32_t q = p + 2; q < pieces; q += kJoinThreads) {
+      const int more = __syncthreads_count(q + threadIdx.x < pieces && key[(q + threadIdx.x) * kPiece] == v);
+      last_piece += (uint32_t)more;
+      if (more < kJoinThreads) break;
     }
-    const uint32_t last_piece = lo / kPiece;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < a.dim) {
 #pragma unroll 8
@@ -591,8 +589,10 @@ mw_status lookup(const mw_embedding_desc* d, const void* tokens, const void* tab
   constexpr int kVec = 16 / sizeof(T);
   const bool wide = wide_rows(table, a.ld_table, a.dim, sizeof(T)) && wide_rows(out, a.ld_out, a.dim, sizeof(T));
   const int per = wide ? a.dim / kVec : a.dim;
-  // 1024 pieces a block; fewer while that leaves multiprocessors idle (one row of 256 pieces is the least)
-  int rows = per >= 1024 ? 1 : 1024 / per;
+  // 1024 pieces a block (4096 where rows do not come out even); fewer while that leaves multiprocessors idle (one row
+  // of 256 pieces is the least)
+  const int most = 1024 % per == 0 ? 1024 : 4096;
+  int rows = per >= most ? 1 : most / per;
   while (rows > 1 && rows * per > 256 && ceil_div(a.n, rows) < 148 * 4) rows = (rows + 1) / 2;
   const unsigned blocks = (unsigned)((a.n + rows - 1) / rows);
   if (wide) lookup_kernel<T, I, kVec><<<blocks, 256, 0, s>>>(a, (const I*)tokens, (const T*)table, (T*)out, rows);

@@ -40,11 +40,16 @@ constexpr int kFewRegisters = 104, kManyRegisters = 200;
 constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;       // one term of one operand of one stage and CTA
 constexpr uint32_t kBufferBytes = 32 * 128;             // 32 rows of 128 bytes of an epilogue warp
 constexpr uint64_t kLossWaitNs = 2000000000ull;
-__host__ __device__ constexpr int stage_count(int terms) { return terms == 1 ? 5 : 3; }
-__host__ __device__ constexpr int buffer_count(int terms) { return terms == 1 ? 2 : 1; }
-__host__ __device__ constexpr uint32_t stage_bytes(int terms) { return 2u * (uint32_t)terms * kPlaneBytes; }
-constexpr size_t loss_smem(int terms) {
-  return 1024 + (size_t)stage_count(terms) * stage_bytes(terms) + (size_t)kEpi * buffer_count(terms) * kBufferBytes;
+enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
+// Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
+// few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
+__host__ __device__ constexpr int buffer_count(int terms, int kind) { return kind == P_SUMS ? 0 : (terms == 1 ? 2 : 1); }
+constexpr int kStagesMax = 12;
+constexpr size_t kSmemMost = 225 * 1024;
+constexpr int stages_for(int terms, int kind, uint32_t a_stage) {
+  const size_t room = kSmemMost - 1024 - (size_t)kEpi * buffer_count(terms, kind) * kBufferBytes;
+  const int n = (int)(room / (a_stage + (uint32_t)terms * kPlaneBytes));
+  return n < kStagesMax ? n : kStagesMax;
 }
 // K blocks that one accumulator takes: 128 instructions of bf16 operands, 96 of two-term ones.  Each cuts the sum
 // off at its last place; what that leaves of a sum of one sign is 2^-17.
@@ -90,8 +95,6 @@ struct LossArgs {
   int sampled_h, sampled_w;
 };
 
-enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
-
 struct alignas(64) ProductArgs {
   CUtensorMap a, b, out, acc;
   const LossInfo* info;
@@ -103,8 +106,9 @@ struct alignas(64) ProductArgs {
   int slab_rows;            // P_DH: rows of one split's sums
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
-  uint32_t a_bytes;         // P_SUMS, P_EXP: what A's copies bring both CTAs in a stage
-  int a_even;               // ... they are the even CTA's alone: its rows hold all there are
+  int stages;
+  uint32_t a_stage;         // bytes of A in a stage of a CTA
+  int a_even;               // A's copies are the even CTA's alone: its rows hold all there are
   float scale;
   int scaled, sampled_h, sampled_w;
   float2* sums;             // [row][sum_blocks]: power, sum
@@ -198,10 +202,10 @@ template <int TERMS, int KIND>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr int kStages = stage_count(TERMS), kBuffers = buffer_count(TERMS), kPiece = piece_blocks(TERMS);
-  constexpr uint32_t kStage = stage_bytes(TERMS);
-  __shared__ __align__(8) uint64_t full_bar[kStages];
-  __shared__ __align__(8) uint64_t empty_bar[kStages];
+  constexpr int kBuffers = buffer_count(TERMS, KIND), kPiece = piece_blocks(TERMS);
+  constexpr uint32_t b_stage = TERMS * kPlaneBytes;
+  __shared__ __align__(8) uint64_t full_bar[kStagesMax];
+  __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
   __shared__ __align__(8) uint64_t acc_full[2];
   __shared__ __align__(8) uint64_t acc_empty[2];
   __shared__ uint32_t tmem_slot;
@@ -209,11 +213,13 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_cta_rank();
-  const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int stages = p.stages;
+  const uint32_t a_stage = p.a_stage;
+  const uint32_t a_tiles = (smem_u32(smem_raw) + 1023u) & ~1023u, b_tiles = a_tiles + (uint32_t)stages * a_stage;
   const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(smem_u32(&full_bar[s]), 1);
       mbar_init(smem_u32(&empty_bar[s]), 1);
     }
@@ -255,20 +261,20 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * kHalf;
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           if (!mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u)) { ok = false; break; }
-          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, KIND == P_SUMS || KIND == P_EXP ? p.a_bytes + kStage : 2u * kStage);
+          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, (p.a_even ? 1u : 2u) * a_stage + 2u * b_stage);
           const uint32_t fb = full0_even + 8u * stage;
-          const uint32_t base = tiles + stage * kStage;
+          const uint32_t to_a = a_tiles + stage * a_stage, to_b = b_tiles + stage * b_stage;
           if (KIND == P_SUMS || KIND == P_EXP) {
-            if (rank == 0 || !p.a_even) tma_load_3d<true>(base, &p.a, fb, kb * kBK, p.first + am, 0);
-            tma_load_3d<true>(base + TERMS * kPlaneBytes, &p.b, fb, kb * kBK, bn, 0);
+            if (rank == 0 || !p.a_even) tma_load_3d<true>(to_a, &p.a, fb, kb * kBK, p.first + am, 0);
+            tma_load_3d<true>(to_b, &p.b, fb, kb * kBK, bn, 0);
           } else if (KIND == P_DH) {
-            tma_load_4d<true>(base, &p.a, fb, 0, am, kb, 0);
-            tma_load_4d<true>(base + TERMS * kPlaneBytes, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
+            tma_load_4d<true>(to_a, &p.a, fb, 0, am, kb, 0);
+            tma_load_4d<true>(to_b, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
           } else {
-            tma_load_4d<true>(base, &p.a, fb, 0, kb * kBK, am >> 6, 0);
-            tma_load_4d<true>(base + TERMS * kPlaneBytes, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
+            tma_load_4d<true>(to_a, &p.a, fb, 0, kb * kBK, am >> 6, 0);
+            tma_load_4d<true>(to_b, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
           }
-          if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1u; }
+          if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
         }
       }
     }
@@ -294,8 +300,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           for (int kb = kb0; kb < kb1; ++kb) {
             if (!ready && !mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t sb = tiles + stage * kStage;
-            const uint32_t a0 = (sb >> 4) | a_base, b0 = ((sb + TERMS * kPlaneBytes) >> 4) | b_base;
+            const uint32_t a0 = ((a_tiles + stage * a_stage) >> 4) | a_base, b0 = ((b_tiles + stage * b_stage) >> 4) | b_base;
             umma_bf16<true>(d, a0, b0, p.idesc, kb > kb0);
             if (TERMS == 2) {
               umma_bf16<true>(d, a0, b0 + term, p.idesc, 1u);
@@ -303,7 +308,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             }
             // the next stage's barrier is polled while the first products run
             const uint32_t freed = empty0 + 8u * stage;
-            if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1u; }
+            if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
             ready = kb + 1 < kb1 && mbar_try_wait<true>(full0 + 8u * stage, phase);
 #pragma unroll
             for (int k = 1; k < kBK / 16; ++k) {
@@ -326,7 +331,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     // A lane has a row of 32 and a warp half the tile's columns, all of them in registers: an accumulator is handed
     // back as soon as it has been read.
     const int ew = warp - kFirstEpi, quarter = warp & 3, side = ew >> 2;
-    const uint32_t sbuf = tiles + kStages * kStage + (uint32_t)ew * (kBuffers * kBufferBytes);
+    const uint32_t sbuf = b_tiles + (uint32_t)stages * b_stage + (uint32_t)ew * (kBuffers * kBufferBytes);
     uint32_t turn = 0;
     int j = 0;
     bool ok = true;
@@ -530,7 +535,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   __syncthreads();
   if (warp == 0 && lane == 0 && abort_flag) {
     // a wait ran out: copies still in flight get a bounded time to land before the CTA retires
-    for (int s = 0; s < kStages; ++s)
+    for (int s = 0; s < stages; ++s)
       for (uint32_t i = 0; i < 4096u && !mbar_try_wait<true>(smem_u32(&full_bar[s]), 0u); ++i) __nanosleep(256);
   }
   cluster_sync_all();
@@ -799,9 +804,12 @@ loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float
   const int lane = threadIdx.x & 31;
   for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < info->live; i += (int64_t)gridDim.x * 8) {
     RowSum v = {kNoPower, 0.f};
-    for (int b = lane; b < sum_blocks; b += 32) {
-      const float2 s = sums[i * sum_blocks + b];
-      v = join(v, {s.x, s.y});
+    for (int b0 = lane; b0 < sum_blocks; b0 += 32 * 8) {
+      float2 x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = b0 + 32 * q < sum_blocks ? sums[i * sum_blocks + b0 + 32 * q] : make_float2(kNoPower, 0.f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v = join(v, {x[q].x, x[q].y});
     }
     v = warp_join(v);
     if (lane == 0) {
@@ -1047,19 +1055,21 @@ mw_status out_map(CUtensorMap* out, CUtensorMapDataType type, int size, const vo
 }
 
 template <int TERMS, int KIND>
-mw_status run_product(const ProductArgs& p, int64_t most_units, cudaStream_t s) {
+mw_status run_product(ProductArgs& p, int64_t most_units, cudaStream_t s) {
+  if (KIND == P_DH || KIND == P_DW) p.a_stage = TERMS * kPlaneBytes;
+  p.stages = stages_for(TERMS, KIND, p.a_stage);
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
   auto kernel = loss_products_kernel<TERMS, KIND>;
   if (!ready[dev]) {
-    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)loss_smem(TERMS)));
+    MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost));
     ready[dev] = true;
   }
   const int64_t pairs = sm_count() / 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * (unsigned)(most_units < pairs ? (most_units < 1 ? 1 : most_units) : pairs));
   cfg.blockDim = dim3(kLossThreads);
-  cfg.dynamicSmemBytes = loss_smem(TERMS);
+  cfg.dynamicSmemBytes = kSmemMost;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1157,7 +1167,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     // bf16 40 us with all 256 rows copied, half of it with 16.
     logits.a_even = TERMS == 1 && a.rows <= kHalf;
     const int box_rows = !logits.a_even ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
-    logits.a_bytes = (logits.a_even ? 1u : 2u) * TERMS * (uint32_t)box_rows * kBK * 2;
+    logits.a_stage = TERMS * (uint32_t)box_rows * kBK * 2;
     MW_TRY(row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, box_rows));
     MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1) : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
     if (gradient) {
