@@ -4,7 +4,7 @@
 // chunks that the blocks take in turn, so one launch serves many tensors of any sizes; squares are summed in 64 bits.
 #include <math.h>
 
-#include "mw_common.cuh"
+#include "mw_launch.cuh"
 
 namespace mw {
 namespace {
@@ -65,6 +65,7 @@ __device__ __forceinline__ float element(const Share& c, int i) {
 __device__ __forceinline__ void add_square(double& sum, float v) { sum = fma((double)v, (double)v, sum); }
 
 __global__ void __launch_bounds__(kClipThreads) squares_kernel(const __grid_constant__ ClipGroup g, double* partial) {
+  after_previous();
   __shared__ double warp_sum[kClipThreads / 32];
   double sum = 0.0;
   for (int64_t chunk = blockIdx.x; chunk < g.first[g.count]; chunk += gridDim.x) {
@@ -103,6 +104,7 @@ __global__ void __launch_bounds__(kClipThreads) squares_kernel(const __grid_cons
 // Chunks are taken from the last to the first: what the squares have just read is still in L2.
 __global__ void __launch_bounds__(kClipThreads)
 scale_kernel(const __grid_constant__ ClipGroup g, const double* __restrict__ partial, int partials, double max_norm, float* norm_out) {
+  after_previous();
   __shared__ double warp_sum[kClipThreads / 32];
   double sum = 0.0;
   for (int i = threadIdx.x; i < partials; i += kClipThreads) sum += partial[i];
@@ -191,13 +193,11 @@ extern "C" mw_status mw_clip_gradients(int32_t count, const void* const* in, voi
   };
   for (int i = 0; i < groups; ++i) {
     fill(i);
-    squares_kernel<<<kClipBlocks, kClipThreads, 0, s>>>(g, partial + (size_t)i * kClipBlocks);
-    MW_TRY(launch_ok());
+    MW_TRY(launch_after(squares_kernel, kClipBlocks, kClipThreads, 0, s, g, partial + (size_t)i * kClipBlocks));
   }
   for (int i = 0; i < groups; ++i) {
     fill(i);
-    scale_kernel<<<kClipBlocks, kClipThreads, 0, s>>>(g, partial, groups * kClipBlocks, max_norm, i ? nullptr : norm);
-    MW_TRY(launch_ok());
+    MW_TRY(launch_after(scale_kernel, kClipBlocks, kClipThreads, 0, s, g, partial, groups * kClipBlocks, max_norm, i ? nullptr : norm));
   }
   return MW_OK;
 }

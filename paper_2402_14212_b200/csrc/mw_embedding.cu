@@ -9,7 +9,7 @@
 // same launch fill the table's gradient with zeros: the sort's latency hides behind that.  More go through
 // three launches a digit.
 #include "mw_cluster.cuh"
-#include "mw_common.cuh"
+#include "mw_launch.cuh"
 
 namespace mw {
 namespace {
@@ -99,6 +99,7 @@ constexpr int kLookupPieces = 4;
 template <typename T, typename I, int VEC>
 __global__ void __launch_bounds__(256)
 lookup_kernel(EmbedArgs a, const I* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int rows) {
+  after_previous();
   using Raw = typename RawOf<T, VEC>::type;
   const int per = a.dim / VEC;
   const int64_t r0 = (int64_t)blockIdx.x * rows;
@@ -262,6 +263,7 @@ template <typename I, typename G>
 __global__ void __cluster_dims__(kSortBlocks, 1, 1) __launch_bounds__(kSortThreads)
 sort_kernel(const I* __restrict__ tokens, uint32_t n, int vocab, int passes, int bits, int rounds, uint32_t* __restrict__ key_out,
             uint32_t* __restrict__ pos_out, uint32_t* joins, G* dtable, int dim, int64_t ld, bool wide) {
+  after_previous();
   extern __shared__ uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (blockIdx.x >= kSortBlocks) {
@@ -416,6 +418,7 @@ template <typename T, typename G, int VEC, bool ADD, bool GWIDE>
 __global__ void __launch_bounds__(256)
 run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,
                 G* __restrict__ dtable, float* __restrict__ partial, int col_groups, uint32_t* joins) {
+  after_previous();
   constexpr int kAhead = 8;
   const int lane = threadIdx.x & 31;
   const uint32_t n = (uint32_t)a.n;
@@ -483,6 +486,7 @@ template <typename G, bool ADD>
 __global__ void __launch_bounds__(kJoinThreads)
 join_runs_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const float* __restrict__ partial, G* __restrict__ dtable,
                  const uint32_t* __restrict__ joins) {
+  after_previous();
   __shared__ float4 sums[kJoinRows][kJoinColumns / 4];
   const uint32_t n = (uint32_t)a.n;
   const int across = threadIdx.x % (kJoinColumns / 4), down = threadIdx.x / (kJoinColumns / 4);
@@ -595,9 +599,7 @@ mw_status lookup(const mw_embedding_desc* d, const void* tokens, const void* tab
   int rows = per >= most ? 1 : most / per;
   while (rows > 1 && rows * per > 256 && ceil_div(a.n, rows) < 148 * 4) rows = (rows + 1) / 2;
   const unsigned blocks = (unsigned)((a.n + rows - 1) / rows);
-  if (wide) lookup_kernel<T, I, kVec><<<blocks, 256, 0, s>>>(a, (const I*)tokens, (const T*)table, (T*)out, rows);
-  else lookup_kernel<T, I, 1><<<blocks, 256, 0, s>>>(a, (const I*)tokens, (const T*)table, (T*)out, rows);
-  return launch_ok();
+  return launch_after(wide ? lookup_kernel<T, I, kVec> : lookup_kernel<T, I, 1>, blocks, 256, 0, s, a, (const I*)tokens, (const T*)table, (T*)out, rows);
 }
 
 // Clusters of the sort that the device holds at once (asked for once a device; at least two).  Allows its
@@ -629,10 +631,9 @@ mw_status sum_runs(const EmbedArgs& a, const EmbedScratch& l, const uint32_t* ke
   const int groups = ceil_div(a.dim, 32 * VEC);
   const int64_t warps = (int64_t)l.pieces * groups;
   if (warps > ((int64_t)1 << 34)) return MW_ERR_UNSUPPORTED;
-  run_sums_kernel<T, G, VEC, ADD, GWIDE><<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(a, key, pos, dout, dtable, l.partial, groups, l.joins);
+  MW_TRY(launch_after(run_sums_kernel<T, G, VEC, ADD, GWIDE>, (unsigned)((warps + 7) / 8), 256, 0, s, a, key, pos, dout, dtable, l.partial, groups, l.joins));
   const int64_t joins = (int64_t)l.pieces * ceil_div(a.dim, kJoinColumns);
-  join_runs_kernel<G, ADD><<<(unsigned)(joins < 148 * 4 ? joins : 148 * 4), kJoinThreads, 0, s>>>(a, key, l.partial, dtable, l.joins);
-  return launch_ok(2);
+  return launch_after(join_runs_kernel<G, ADD>, (unsigned)(joins < 148 * 4 ? joins : 148 * 4), kJoinThreads, 0, s, a, key, l.partial, dtable, l.joins);
 }
 
 template <typename T, typename G, typename I>
@@ -666,9 +667,8 @@ mw_status table_gradient(const mw_embedding_desc* d, const void* tokens, const v
     } else {
       MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(kSortRounds)));
     }
-    kernel<<<(unsigned)(kSortBlocks + fill), kSortThreads, sort_smem(rounds), s>>>(
-        (const I*)tokens, n, a.vocab, passes, ceil_div(bits, passes), rounds, l.key[0], l.pos[0], l.joins, g, a.dim, a.ld_dtable, gwide);
-    MW_TRY(launch_ok());
+    MW_TRY(launch_after(kernel, (unsigned)(kSortBlocks + fill), kSortThreads, sort_smem(rounds), s, (const I*)tokens, n, a.vocab, passes,
+                        ceil_div(bits, passes), rounds, l.key[0], l.pos[0], l.joins, g, a.dim, a.ld_dtable, gwide));
   } else {
     MW_CUDA_OK(cudaMemsetAsync(l.joins, 0, 4, s));
     Entries<I> in = {(const I*)tokens, nullptr, nullptr, a.vocab};

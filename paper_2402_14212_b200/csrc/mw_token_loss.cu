@@ -20,6 +20,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include "mw_launch.cuh"
 #include "mw_tc_ptx.cuh"
 
 namespace mw {
@@ -33,7 +34,7 @@ constexpr int kTile = 256;                // rows and columns of a pair's tile
 constexpr int kHalf = 128;                // ... of one CTA's share of either operand
 constexpr int kBK = 64;
 constexpr int kSumColumns = 128;          // logits that share a power of two and a sum
-constexpr int kLossThreads = 384;         // producer warp, issuing warp, two idle ones; eight epilogue warps
+constexpr int kLossThreads = 384;         // copies of A, products, copies of B, an idle warp; eight epilogue warps
 constexpr int kFirstEpi = 4, kEpi = 8;
 // registers a thread: the launch gives 384 x 168 = 64512, handed over as 128 x 104 + 256 x 200 = 64512
 constexpr int kFewRegisters = 104, kManyRegisters = 200;
@@ -107,6 +108,11 @@ struct alignas(64) ProductArgs {
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
   int stages;
+  int tile_n;               // columns of a tile: 256, fewer for few rows of the loss alone
+  int direct;               // few rows of the loss alone: h as it is, rows that are left out among the others
+  LossInfo* clear;          // ... and what the other kernels share is cleared here
+  const void* targets;
+  int index_bytes;
   uint32_t a_stage;         // bytes of A in a stage of a CTA
   int a_even;               // A's copies are the even CTA's alone: its rows hold all there are
   float scale;
@@ -126,6 +132,7 @@ struct Unit { int m0, n0, kb0, kb1, split; };
 
 template <int KIND>
 __device__ __forceinline__ int live_rows(const ProductArgs& p) {
+  if (KIND == P_SUMS && p.direct) return p.piece;
   const int n = p.info->live - p.first;
   return n < 0 ? 0 : (n < p.piece ? n : p.piece);
 }
@@ -146,7 +153,7 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live) {
     const int group = u / per, r = u - group * per;
     const int left = tm - group * kRows, rows = left < kRows ? left : kRows;
     w.m0 = (group * kRows + r % rows) * kTile;
-    w.n0 = r / rows * kTile;
+    w.n0 = r / rows * (KIND == P_SUMS ? p.tile_n : kTile);
     w.kb0 = 0;
     w.kb1 = p.blocks_k;
   } else if (KIND == P_DH) {
@@ -183,6 +190,18 @@ __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16
         "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+// whether a phase is complete, without waiting for it
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -244,35 +263,43 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   wc.st = p.st;
   wc.abort_flag = &abort_flag;
   wc.limit_ns = kLossWaitNs;
+  after_previous();
+  if (KIND == P_SUMS && p.direct && blockIdx.x == 0 && threadIdx.x < sizeof(LossInfo) / 4)
+    reinterpret_cast<unsigned*>(p.clear)[threadIdx.x] = 0;
   const int live = live_rows<KIND>(p), units = unit_count<KIND>(p, live);
 
   constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
   // (registers change hands inside the branches: where paths meet the compiler counts on the fewer)
   if (warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
-  if (warp == 0) {
-    // ---------------- copies ----------------
+  if (warp == 0 || warp == 2) {
+    // ---------------- copies: A's by one warp, B's by another ----------------
+    // (A copy takes the lane that issues it 120 to 190 cycles; two a K block by one lane, with its waits, took 0.34 us,
+    // whatever the copies brought.)
     if (lane == 0) {
+      const bool of_a = warp == 0;
       uint32_t stage = 0, phase = 0;
       const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
       const uint32_t full0_even = map_to_cta(full0, 0u);
+      const uint32_t tx = (p.a_even ? 1u : 2u) * a_stage + 2u * (KIND == P_SUMS ? b_stage / kHalf * (uint32_t)(p.tile_n / 2) : b_stage);
+      const bool idle = of_a && rank != 0 && p.a_even;
       bool ok = true;
-      for (int u = pair; u < units && ok; u += pairs) {
+      for (int u = pair; u < units && ok && !idle; u += pairs) {
         const Unit w = unit_at<KIND>(p, u, live);
-        const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * kHalf;
+        const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * (KIND == P_SUMS ? p.tile_n / 2 : kHalf);
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           if (!mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u)) { ok = false; break; }
-          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, (p.a_even ? 1u : 2u) * a_stage + 2u * b_stage);
+          if (of_a && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
           const uint32_t fb = full0_even + 8u * stage;
-          const uint32_t to_a = a_tiles + stage * a_stage, to_b = b_tiles + stage * b_stage;
+          const uint32_t to = of_a ? a_tiles + stage * a_stage : b_tiles + stage * b_stage;
           if (KIND == P_SUMS || KIND == P_EXP) {
-            if (rank == 0 || !p.a_even) tma_load_3d<true>(to_a, &p.a, fb, kb * kBK, p.first + am, 0);
-            tma_load_3d<true>(to_b, &p.b, fb, kb * kBK, bn, 0);
+            if (of_a) tma_load_3d<true>(to, &p.a, fb, kb * kBK, p.first + am, 0);
+            else tma_load_3d<true>(to, &p.b, fb, kb * kBK, bn, 0);
           } else if (KIND == P_DH) {
-            tma_load_4d<true>(to_a, &p.a, fb, 0, am, kb, 0);
-            tma_load_4d<true>(to_b, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
+            if (of_a) tma_load_4d<true>(to, &p.a, fb, 0, am, kb, 0);
+            else tma_load_4d<true>(to, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
           } else {
-            tma_load_4d<true>(to_a, &p.a, fb, 0, kb * kBK, am >> 6, 0);
-            tma_load_4d<true>(to_b, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
+            if (of_a) tma_load_4d<true>(to, &p.a, fb, 0, kb * kBK, am >> 6, 0);
+            else tma_load_4d<true>(to, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
           }
           if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
         }
@@ -296,31 +323,37 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           tc_fence_after();
           const uint32_t d = tmem_base + set * (uint32_t)kTile;
           const int kb1 = kb0 + kPiece < w.kb1 ? kb0 + kPiece : w.kb1;
-          bool ready = mbar_try_wait<true>(full0 + 8u * stage, phase);
+          // Between the last instruction of a K block and the first of the next the pipe holds one of them: there stand
+          // only a test and a branch.  What frees the block's stage follows the next block's first instruction, and the
+          // next stage's barrier and addresses come before the other three.
+          bool ready = false;
+          uint32_t freed = 0;
+          uint32_t a0 = (a_tiles + stage * a_stage) >> 4 | a_base, b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
           for (int kb = kb0; kb < kb1; ++kb) {
             if (!ready && !mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t a0 = ((a_tiles + stage * a_stage) >> 4) | a_base, b0 = ((b_tiles + stage * b_stage) >> 4) | b_base;
             umma_bf16<true>(d, a0, b0, p.idesc, kb > kb0);
             if (TERMS == 2) {
               umma_bf16<true>(d, a0, b0 + term, p.idesc, 1u);
               umma_bf16<true>(d, a0 + term, b0, p.idesc, 1u);
             }
-            // the next stage's barrier is polled while the first products run
-            const uint32_t freed = empty0 + 8u * stage;
+            if (freed) umma_commit<true>(freed);
+            freed = empty0 + 8u * stage;
             if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
-            ready = kb + 1 < kb1 && mbar_try_wait<true>(full0 + 8u * stage, phase);
+            ready = kb + 1 < kb1 && mbar_test(full0 + 8u * stage, phase);
+            const uint32_t a1 = a0, b1 = b0;
+            a0 = (a_tiles + stage * a_stage) >> 4 | a_base;
+            b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
 #pragma unroll
             for (int k = 1; k < kBK / 16; ++k) {
-              const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
+              const uint32_t a = a1 + (uint32_t)k * a_adv, b = b1 + (uint32_t)k * b_adv;
               umma_bf16<true>(d, a, b, p.idesc, 1u);
               if (TERMS == 2) {
                 umma_bf16<true>(d, a, b + term, p.idesc, 1u);
                 umma_bf16<true>(d, a + term, b, p.idesc, 1u);
               }
             }
-            umma_commit<true>(freed);
           }
+          if (ok) umma_commit<true>(freed);
           if (ok) umma_commit<true>(smem_u32(&acc_full[set]));
         }
       }
@@ -360,7 +393,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     for (int u = pair; u < units && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live);
       const int row0 = w.m0 + (int)rank * kHalf + quarter * 32, row = row0 + lane;
-      const int col0 = w.n0 + side * kSumColumns;
+      const int cols = KIND == P_SUMS ? p.tile_n / 2 : kSumColumns;          // of this warp
+      const int col0 = w.n0 + side * cols;
       float acc[kSumColumns];
 #pragma unroll
       for (int i = 0; i < kSumColumns; ++i) acc[i] = 0.f;
@@ -371,7 +405,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
         if (!ok) break;
         tc_fence_after();
-        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kTile + (uint32_t)(side * kSumColumns);
+        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kTile + (uint32_t)(side * cols);
 #pragma unroll
         for (int c = 0; c < kSumColumns; c += 16) {
           uint32_t r[16];
@@ -389,7 +423,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       }
       if (!ok) break;
       if (KIND == P_SUMS || KIND == P_EXP) {
-        const int valid = p.vocab - col0;          // columns of the vocabulary from col0 on
+        // columns of the vocabulary among them (the registers beyond hold another warp's, or nothing)
+        const int left = p.vocab - col0, valid = left < cols ? left : cols;
         const bool on = row < live;
         if (valid > 0) {
           float m = -INFINITY;
@@ -398,12 +433,20 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             acc[i] *= factor;
             m = fmaxf(m, valid >= kSumColumns || i < valid ? acc[i] : -INFINITY);
           }
-          const int t = on ? p.target[p.first + row] - col0 : -1;
-          if (__any_sync(0xffffffffu, t >= 0 && t < kSumColumns)) {
+          int t = -1;
+          if (on) {
+            if (KIND == P_SUMS && p.direct) {
+              const int64_t x = p.index_bytes == 4 ? (int64_t) static_cast<const int32_t*>(p.targets)[row] : static_cast<const int64_t*>(p.targets)[row];
+              t = x >= col0 && x < col0 + valid ? (int)(x - col0) : -1;
+            } else {
+              t = p.target[p.first + row] - col0;
+            }
+          }
+          if (__any_sync(0xffffffffu, t >= 0 && t < valid)) {
             float zt = 0.f;
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) zt = i == t ? acc[i] : zt;
-            if (t >= 0 && t < kSumColumns) p.target_z[p.first + row] = zt;
+            if (t >= 0 && t < valid) p.target_z[p.first + row] = zt;
           }
           // (a row of nothing but -inf here, or with an infinity, keeps its values as they are)
           const float k = fabsf(m) < 1e30f ? ceilf(m) - 15.f : -15.f;
@@ -414,7 +457,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             if (valid < kSumColumns && i >= valid) acc[i] = 0.f;
             sum += acc[i];
           }
-          if (on) p.sums[(size_t)row * p.sum_blocks + col0 / kSumColumns] = make_float2(k, sum);
+          if (on) p.sums[(size_t)row * p.sum_blocks + col0 / cols] = make_float2(k, sum);
           if (KIND == P_EXP) {
             constexpr int kCols = TERMS == 1 ? 64 : 32;
 #pragma unroll
@@ -554,6 +597,7 @@ __device__ __forceinline__ int target_of(const I* targets, const float* weight, 
 
 template <typename I>
 __global__ void __launch_bounds__(kIndexRows) count_live_kernel(const I* targets, const float* weight, int64_t rows, int vocab, int* counts) {
+  after_previous();
   const int64_t i = (int64_t)blockIdx.x * kIndexRows + threadIdx.x;
   const int n = __syncthreads_count(i < rows && target_of(targets, weight, i, vocab) >= 0);
   if (threadIdx.x == 0) counts[blockIdx.x] = n;
@@ -564,6 +608,7 @@ template <typename I>
 __global__ void __launch_bounds__(kIndexRows)
 index_live_kernel(const I* targets, const float* weight, int64_t rows, int vocab, const int* counts, int blocks, int* row, int* target,
                   float* g, float* loss, LossInfo* info) {
+  after_previous();
   __shared__ int warp_sum[32];
   __shared__ int sums[2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -664,6 +709,7 @@ constexpr int64_t kSampledBytes = (int64_t)32 << 20;
 
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) largest_kernel(Operand<T> w, Operand<T> h, int dim, int64_t w_blocks) {
+  after_previous();
   const bool of_w = blockIdx.x < w_blocks;
   const Operand<T>& o = of_w ? w : h;
   const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
@@ -685,6 +731,7 @@ __global__ void __launch_bounds__(256) largest_kernel(Operand<T> w, Operand<T> h
 // AGAIN: only what the sample misjudged.  SCALED false: bf16 as it is.
 template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
 __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, int dim, int padded, int64_t w_blocks) {
+  after_previous();
   const bool of_w = blockIdx.x < w_blocks;
   const Operand<T>& o = of_w ? w : h;
   const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
@@ -770,7 +817,7 @@ __device__ __forceinline__ float loss_of(RowSum v, float zt) {
 }
 
 // The last block of the launch that brings the last losses adds them up, in an order that the rows' number alone sets.
-__device__ __forceinline__ void total_by_last(LossInfo* info, const double* part, float* total) {
+__device__ __forceinline__ void total_by_last(LossInfo* info, int n, const double* part, float* total) {
   __shared__ double sums[8];
   __shared__ bool last;
   if (total == nullptr) return;
@@ -782,7 +829,6 @@ __device__ __forceinline__ void total_by_last(LossInfo* info, const double* part
   }
   __syncthreads();
   if (!last) return;
-  const int n = info->live;
   double t = 0.0;
 #pragma unroll 8
   for (int i = threadIdx.x; i < n; i += 256) t += __ldcg(part + i);
@@ -801,6 +847,7 @@ __device__ __forceinline__ void total_by_last(LossInfo* info, const double* part
 __global__ void __launch_bounds__(256)
 loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const int* row, const float* g,
                  float* loss, double* part, float* total) {
+  after_previous();
   const int lane = threadIdx.x & 31;
   for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < info->live; i += (int64_t)gridDim.x * 8) {
     RowSum v = {kNoPower, 0.f};
@@ -818,7 +865,36 @@ loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float
       part[i] = (double)g[i] * (double)l;
     }
   }
-  total_by_last(info, part, total);
+  total_by_last(info, info->live, part, total);
+}
+
+// The same of at most 256 rows that were taken as they are: those left out are found here.
+template <typename I>
+__global__ void __launch_bounds__(256)
+direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const I* targets, const float* weight, int rows,
+                   int vocab, float* loss, double* part, float* total) {
+  after_previous();
+  const int lane = threadIdx.x & 31, mine = threadIdx.x;
+  const int live = __syncthreads_count(mine < rows && target_of(targets, weight, mine, vocab) >= 0);
+  const int i = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (i < rows) {
+    const bool on = target_of(targets, weight, i, vocab) >= 0;
+    RowSum v = {kNoPower, 0.f};
+    for (int b0 = lane; b0 < sum_blocks && on; b0 += 32 * 8) {
+      float2 x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = b0 + 32 * q < sum_blocks ? sums[(size_t)i * sum_blocks + b0 + 32 * q] : make_float2(kNoPower, 0.f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v = join(v, {x[q].x, x[q].y});
+    }
+    v = warp_join(v);
+    if (lane == 0) {
+      const float l = on ? loss_of(v, target_z[i]) : 0.f;
+      loss[i] = l;
+      part[i] = on ? (double)(weight ? weight[i] : 1.f / (float)live) * (double)l : 0.0;
+    }
+  }
+  total_by_last(info, rows, part, total);
 }
 
 // a row's exponentials -> dz times a power of two, in their place: a block a row
@@ -826,6 +902,7 @@ template <int TERMS>
 __global__ void __launch_bounds__(256)
 dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
           const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int vocab, int padded) {
+  after_previous();
   __shared__ RowSum warp_v[8];
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
@@ -894,7 +971,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       }
     }
   }
-  total_by_last(info, part, total);
+  total_by_last(info, info->live, part, total);
 }
 
 __device__ __forceinline__ void put(float* at, float v) { *at = v; }
@@ -905,6 +982,7 @@ template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 dh_rows_kernel(LossArgs a, const float* slab, int splits, int slab_rows, int padded, int first, int piece, const int* row,
                const LossInfo* info, T* dh) {
+  after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
   const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, a.sampled_w)));
@@ -962,6 +1040,15 @@ int dh_splits(int64_t rows, int dim, int blocks_k, int terms) {
   return best;
 }
 
+// Columns of a tile of few rows, whose time is the vocabulary's way through memory: as even a share for every pair as
+// the instructions allow, 64 at least (16 rows of 32768x2048: 147 tiles of 224 columns on 74 pairs, 128 of 256 leave 20
+// pairs idle for half the time).
+int logits_tile(int vocab) {
+  const int pairs = sm_count() / 2, waves = ceil_div(ceil_div(vocab, kTile), pairs);
+  const int n = (int)align_up((size_t)ceil_div(vocab, waves * pairs), 32);
+  return n < 64 ? 64 : n;
+}
+
 size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossWs* l) {
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -998,7 +1085,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->g = (float*)take(n * 4);
   l->target_z = (float*)take(n * 4);
   l->part = (double*)take(n * 8);
-  l->sums = (float2*)take((size_t)l->piece * l->sum_blocks * 8);
+  // (few rows have blocks of 32 columns and more)
+  l->sums = (float2*)take((size_t)l->piece * (n <= kTile ? ceil_div(d->vocab, 32) : l->sum_blocks) * 8);
   l->h = (unsigned short*)take((size_t)l->staged_rows * l->padded * 2 * terms);
   l->w = (unsigned short*)take(l->in_place ? 0 : v * l->padded * 2 * terms);
   l->e = (unsigned short*)take(gradient ? (size_t)l->piece_rows * l->vpadded * 2 * terms : 0);
@@ -1071,20 +1159,22 @@ mw_status run_product(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   cfg.blockDim = dim3(kLossThreads);
   cfg.dynamicSmemBytes = kSmemMost;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   ++g_launch_count;
   return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
 }
 
 // fp32 accumulator, the operands' type, K across the rows of A and of B, N / 8, M / 16
-uint32_t instruction(bool bf16, bool turned_a, bool turned_b) {
+uint32_t instruction(bool bf16, bool turned_a, bool turned_b, int n = kTile) {
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((turned_a ? 1u : 0u) << 15) | ((turned_b ? 1u : 0u) << 16) |
-         ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+         ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 }
 
 template <typename T, typename I>
@@ -1106,12 +1196,13 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   a.sampled_h = scaled && a.rows * a.dim * (int64_t)sizeof(T) > kSampledBytes;
   a.sampled_w = scaled && (int64_t)a.vocab * a.dim * (int64_t)sizeof(T) > kSampledBytes;
   const unsigned wide = 148 * 8;
+  // few rows of the loss alone: no row is moved where the copy engine can read h as it lies
+  const bool direct = l.in_place && a.rows > 0 && a.rows <= kTile && a.ld_h % 8 == 0 && ((uintptr_t)h & 15) == 0;
   if (l.blocks != 1) MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
-  if (a.rows > 0) {
+  if (a.rows > 0 && !direct) {
     int* counts = l.blocks > 1 ? l.counts : nullptr;
-    if (counts) count_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, counts);
-    index_live_kernel<I><<<l.blocks, kIndexRows, 0, s>>>(targets, weight, a.rows, a.vocab, counts, l.blocks, l.row, l.target, l.g, loss, l.info);
-    MW_TRY(launch_ok(counts ? 2 : 1));
+    if (counts) MW_TRY(launch_after(count_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts));
+    MW_TRY(launch_after(index_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts, l.blocks, l.row, l.target, l.g, loss, l.info));
     Operand<T> oh = {h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, l.info->h_max, a.sampled_h, l.h, dh, a.ld_dh};
     Operand<T> ow = {w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, l.info->w_max, a.sampled_w, l.w, nullptr, 0};
     if (l.in_place) ow.rows = ow.staged_rows = 0;
@@ -1123,26 +1214,13 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       return want < 8 * (int64_t)sm_count() ? want : 8 * (int64_t)sm_count();
     };
     const int64_t bw = blocks_for(ow.rows), bh = blocks_for(a.rows + kTile);
-    auto stage = [&](auto kernel) { kernel<<<(unsigned)(bw + bh), 256, 0, s>>>(ow, oh, a.dim, l.padded, bw); };
-    auto look = [&](auto kernel) { kernel<<<(unsigned)(bw + bh), 256, 0, s>>>(ow, oh, a.dim, bw); };
+    auto stage = [&](auto kernel) { return launch_after(kernel, (unsigned)(bw + bh), 256, 0, s, ow, oh, a.dim, l.padded, bw); };
     if (scaled) {
-      if (rows16) {
-        look(largest_kernel<T, true>);
-        stage(stage_kernel<T, TERMS, true, true, false>);
-      } else {
-        look(largest_kernel<T, false>);
-        stage(stage_kernel<T, TERMS, true, false, false>);
-      }
-      MW_TRY(launch_ok(2));
-      if (a.sampled_h || a.sampled_w) {
-        if (rows16) stage(stage_kernel<T, TERMS, true, true, true>);
-        else stage(stage_kernel<T, TERMS, true, false, true>);
-        MW_TRY(launch_ok());
-      }
+      MW_TRY(launch_after(rows16 ? largest_kernel<T, true> : largest_kernel<T, false>, (unsigned)(bw + bh), 256, 0, s, ow, oh, a.dim, bw));
+      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, false> : stage_kernel<T, TERMS, true, false, false>));
+      if (a.sampled_h || a.sampled_w) MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>));
     } else {
-      if (rows16) stage(stage_kernel<T, 1, false, true, false>);
-      else stage(stage_kernel<T, 1, false, false, false>);
-      MW_TRY(launch_ok());
+      MW_TRY(stage(rows16 ? stage_kernel<T, 1, false, true, false> : stage_kernel<T, 1, false, false, false>));
     }
   }
   if (a.rows > 0 || dw) {
@@ -1158,18 +1236,26 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     p.sum_blocks = l.sum_blocks;
     p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
     p.splits = 1;
+    p.tile_n = kTile;
     ProductArgs logits = p, by_h = p, by_w = p;
-    logits.tiles_n = ceil_div(a.vocab, kTile);
+    logits.direct = direct;
+    logits.clear = l.info;
+    logits.targets = targets;
+    logits.index_bytes = (int)sizeof(I);
+    if (direct) logits.tile_n = logits_tile(a.vocab);
+    logits.tiles_n = ceil_div(a.vocab, logits.tile_n);
+    logits.sum_blocks = ceil_div(a.vocab, logits.tile_n / 2);
     logits.blocks_k = l.padded / kBK;
-    logits.idesc = instruction(bf16, false, false);
+    logits.idesc = instruction(bf16, false, false, logits.tile_n);
     // Few rows: only theirs are copied, the others' products come out as whatever they are and are not read.  (One term
     // alone: the planes of two lie a whole share apart.)  The path from L2 is the limit there: 16 rows of 32768x2048
     // bf16 40 us with all 256 rows copied, half of it with 16.
     logits.a_even = TERMS == 1 && a.rows <= kHalf;
     const int box_rows = !logits.a_even ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
     logits.a_stage = TERMS * (uint32_t)box_rows * kBK * 2;
-    MW_TRY(row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, box_rows));
-    MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1) : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
+    MW_TRY(direct ? row_map(&logits.a, bf16, h, a.dim, a.rows, a.ld_h, 1, box_rows) : row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, box_rows));
+    MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1, logits.tile_n / 2)
+                      : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
     if (gradient) {
       const int64_t row_bytes = (int64_t)l.vpadded * 2 * TERMS, group_bytes = 128 * TERMS;
       const int64_t hw_bytes = (int64_t)l.padded * 2;
@@ -1203,18 +1289,22 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       if (a.rows > 0) {
         if (gradient) {
           MW_TRY((run_product<TERMS, P_EXP>(logits, tm * logits.tiles_n, s)));
-          dz_kernel<TERMS><<<(unsigned)(l.piece_rows < (int)wide ? l.piece_rows : wide), 256, 0, s>>>(l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part, first + l.piece >= a.rows ? total : nullptr, l.e, a.vocab, l.vpadded);
+          MW_TRY(launch_after(dz_kernel<TERMS>, (unsigned)(l.piece_rows < (int)wide ? l.piece_rows : wide), 256, 0, s, l.info, (int)first, l.piece,
+                              l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part, first + l.piece >= a.rows ? total : nullptr, l.e,
+                              a.vocab, l.vpadded));
         } else {
           MW_TRY((run_product<TERMS, P_SUMS>(logits, tm * logits.tiles_n, s)));
-          // (a warp a row)
-          loss_rows_kernel<<<(unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide), 256, 0, s>>>(l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part, total);
+          const unsigned blocks = (unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide);          // (a warp a row)
+          if (direct)
+            MW_TRY(launch_after(direct_rows_kernel<I>, blocks, 256, 0, s, l.info, l.sums, logits.sum_blocks, l.target_z, targets, weight, (int)a.rows,
+                                a.vocab, loss, l.part, total));
+          else
+            MW_TRY(launch_after(loss_rows_kernel, blocks, 256, 0, s, l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part, total));
         }
-        MW_TRY(launch_ok());
         if (dh) {
           MW_TRY((run_product<TERMS, P_DH>(by_h, tm * by_h.tiles_n * l.splits, s)));
           auto rows_kernel = ((uintptr_t)dh & 15) == 0 && a.ld_dh % 4 == 0 && a.dim % 4 == 0 ? dh_rows_kernel<T, true> : dh_rows_kernel<T, false>;
-          rows_kernel<<<wide, 256, 0, s>>>(a, l.slab, l.splits, l.piece_rows, l.padded, (int)first, l.piece, l.row, l.info, dh);
-          MW_TRY(launch_ok());
+          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.splits, l.piece_rows, l.padded, (int)first, l.piece, l.row, l.info, dh));
         }
       }
       if (dw) MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n, s)));
