@@ -191,6 +191,18 @@ __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16
       : "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld32_floats(uint32_t taddr, float* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]),
+        "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]),
+        "=f"(r[30]), "=f"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
 // whether a phase is complete, without waiting for it
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -396,8 +408,6 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const int cols = KIND == P_SUMS ? p.tile_n / 2 : kSumColumns;          // of this warp
       const int col0 = w.n0 + side * cols;
       float acc[kSumColumns];
-#pragma unroll
-      for (int i = 0; i < kSumColumns; ++i) acc[i] = 0.f;
 #pragma unroll 1
       for (int kb0 = w.kb0; kb0 < w.kb1; kb0 += kPiece) {
         const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
@@ -406,13 +416,20 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         if (!ok) break;
         tc_fence_after();
         const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kTile + (uint32_t)(side * cols);
+        if (kb0 == w.kb0) {
+          // the first piece goes where the sum is to be
 #pragma unroll
-        for (int c = 0; c < kSumColumns; c += 16) {
-          uint32_t r[16];
-          tmem_ld16_issue(t0 + (uint32_t)c, r);
+          for (int c = 0; c < kSumColumns; c += 32) tmem_ld32_floats(t0 + (uint32_t)c, acc + c);
           tmem_ld_wait();
+        } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(r[i]);
+          for (int c = 0; c < kSumColumns; c += 16) {
+            uint32_t r[16];
+            tmem_ld16_issue(t0 + (uint32_t)c, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(r[i]);
+          }
         }
         tc_fence_before();
         __syncwarp();
@@ -422,16 +439,25 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         }
       }
       if (!ok) break;
+      if (w.kb0 >= w.kb1) {
+#pragma unroll
+        for (int i = 0; i < kSumColumns; ++i) acc[i] = 0.f;
+      }
       if (KIND == P_SUMS || KIND == P_EXP) {
         // columns of the vocabulary among them (the registers beyond hold another warp's, or nothing)
         const int left = p.vocab - col0, valid = left < cols ? left : cols;
         const bool on = row < live;
         if (valid > 0) {
+          // the largest logit: of a negative factor the least sum's
+          const bool whole = valid == kSumColumns;
           float m = -INFINITY;
+          if (whole && factor > 0.f) {
 #pragma unroll
-          for (int i = 0; i < kSumColumns; ++i) {
-            acc[i] *= factor;
-            m = fmaxf(m, valid >= kSumColumns || i < valid ? acc[i] : -INFINITY);
+            for (int i = 0; i < kSumColumns; ++i) m = fmaxf(m, acc[i]);
+            m *= factor;
+          } else {
+#pragma unroll
+            for (int i = 0; i < kSumColumns; ++i) m = fmaxf(m, i < valid ? acc[i] * factor : -INFINITY);
           }
           int t = -1;
           if (on) {
@@ -446,17 +472,19 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             float zt = 0.f;
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) zt = i == t ? acc[i] : zt;
-            if (t >= 0 && t < valid) p.target_z[p.first + row] = zt;
+            if (t >= 0 && t < valid) p.target_z[p.first + row] = zt * factor;
           }
           // (a row of nothing but -inf here, or with an infinity, keeps its values as they are)
           const float k = fabsf(m) < 1e30f ? ceilf(m) - 15.f : -15.f;
           float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < kSumColumns; ++i) {
-            acc[i] = exp2_fast(acc[i] - k);
-            if (valid < kSumColumns && i >= valid) acc[i] = 0.f;
-            sum += acc[i];
+          for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, -k));
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < kSumColumns; ++i) acc[i] = i < valid ? acc[i] : 0.f;
           }
+#pragma unroll
+          for (int i = 0; i < kSumColumns; ++i) sum += acc[i];
           if (on) p.sums[(size_t)row * p.sum_blocks + col0 / cols] = make_float2(k, sum);
           if (KIND == P_EXP) {
             constexpr int kCols = TERMS == 1 ? 64 : 32;
