@@ -1024,7 +1024,8 @@ def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, gra
             d.ld_dweight = _table_rows(dweight, "token_loss: dweight")
         _same_device(h, dict(weight=weight, targets=targets, dh=dh, dweight=dweight), "token_loss")
         need = C.c_size_t()
-        _check(lib().mw_token_loss_workspace_bytes(d, int(gradient), need), "mw_token_loss_workspace_bytes")
+        with torch.cuda.device(h.device):          # (some of it goes by the device's multiprocessors)
+            _check(lib().mw_token_loss_workspace_bytes(d, int(gradient), need), "mw_token_loss_workspace_bytes")
         known = _remember(key, (d, int(need.value), kind))
     d, need, kind = known
     R = h.shape[0]

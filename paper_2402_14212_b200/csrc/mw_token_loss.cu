@@ -44,7 +44,7 @@ constexpr uint64_t kLossWaitNs = 2000000000ull;
 enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
 // Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
 // few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
-__host__ __device__ constexpr int buffer_count(int terms, int kind) { return kind == P_SUMS ? 0 : (terms == 1 ? 2 : 1); }
+__host__ __device__ constexpr int buffer_count(int terms, int kind) { return kind == P_SUMS ? 0 : 1; }
 constexpr int kStagesMax = 12;
 constexpr size_t kSmemMost = 225 * 1024;
 constexpr int stages_for(int terms, int kind, uint32_t a_stage) {
@@ -103,8 +103,8 @@ struct alignas(64) ProductArgs {
   int first, piece;         // rows of this piece begin at `first` of the live ones
   int vocab, dim;
   int tiles_m, tiles_n;     // of the whole piece (P_DW: of the vocabulary and the columns)
-  int blocks_k, splits, per_split;
-  int slab_rows;            // P_DH: rows of one split's sums
+  int blocks_k;
+  int pairs;                // CTA pairs that the device holds
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
   int stages;
@@ -128,7 +128,28 @@ struct alignas(64) ProductArgs {
   int64_t ld_partial;
 };
 
-struct Unit { int m0, n0, kb0, kb1, split; };
+// How dh's tiles are laid over the pairs: waves of whole tiles, then the rest of them with K in shares, so that the last
+// wave is as short as the others leave it (4096 rows and 2048 columns are 128 tiles on 74 pairs: 1.75 waves with the last
+// 54 in four, 2 without).  The shares' sums, beyond the first, lie in blocks of their own and are added in order.
+struct DhPlan { int whole, rest, shares; };
+constexpr int kMostShares = 32;
+__host__ __device__ constexpr int share_blocks(int pairs) { return 4 * pairs; }      // most of them
+// (a warp calls it, a lane a number of shares)
+__device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, int pairs, int terms) {
+  const int tiles = (live + kTile - 1) / kTile * tiles_n;
+  DhPlan d;
+  d.whole = tiles / pairs * pairs;
+  d.rest = tiles - d.whole;
+  // cycles: a K block's products, what a tile costs beyond them, a sum's way through memory at 4.6 KB a cycle
+  const int s = (int)(threadIdx.x & 31) + 1, per = (blocks_k + s - 1) / s;
+  const bool can = s == 1 || (per >= 8 && d.rest * s <= share_blocks(pairs));
+  const unsigned cost = (unsigned)((d.rest * s + pairs - 1) / pairs) * (unsigned)(per * (terms == 1 ? 512 : 1536) + 3000) + (unsigned)(d.rest * s) * 114u;
+  const unsigned least = __reduce_min_sync(0xffffffffu, can ? cost : 0xffffffffu);
+  d.shares = __ffs(__ballot_sync(0xffffffffu, can && cost == least));
+  return d;
+}
+
+struct Unit { int m0, n0, kb0, kb1, share; };        // share: its block, -1 for the first
 
 template <int KIND>
 __device__ __forceinline__ int live_rows(const ProductArgs& p) {
@@ -137,16 +158,17 @@ __device__ __forceinline__ int live_rows(const ProductArgs& p) {
   return n < 0 ? 0 : (n < p.piece ? n : p.piece);
 }
 template <int KIND>
-__device__ __forceinline__ int unit_count(const ProductArgs& p, int live) {
+__device__ __forceinline__ int unit_count(const ProductArgs& p, int live, const DhPlan& plan) {
   if (KIND == P_DW) return live > 0 || p.first == 0 ? p.tiles_m * p.tiles_n : 0;
-  return (live + kTile - 1) / kTile * p.tiles_n * p.splits;
+  if (KIND == P_DH) return plan.whole + plan.rest * plan.shares;
+  return (live + kTile - 1) / kTile * p.tiles_n;
 }
 // Tiles that run at the same time share operands in L2.  Logits: eight tiles of rows go through the vocabulary
-// together.  dh: all tiles of a share of K.  dW: a tile of the vocabulary with all its columns.
+// together.  dh: tiles of the same rows of dz, or of the same share of K.  dW: a tile of the vocabulary with all its columns.
 template <int KIND>
-__device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live) {
+__device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live, const DhPlan& plan) {
   Unit w;
-  w.split = 0;
+  w.share = -1;
   if (KIND == P_SUMS || KIND == P_EXP) {
     constexpr int kRows = 8;
     const int tm = (live + kTile - 1) / kTile, per = kRows * p.tiles_n;
@@ -157,13 +179,17 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live) {
     w.kb0 = 0;
     w.kb1 = p.blocks_k;
   } else if (KIND == P_DH) {
-    const int tm = (live + kTile - 1) / kTile, per = tm * p.tiles_n;
-    w.split = u / per;
-    const int r = u - w.split * per;
-    w.m0 = r / p.tiles_n * kTile;
-    w.n0 = r % p.tiles_n * kTile;
-    w.kb0 = w.split * p.per_split;
-    w.kb1 = w.kb0 + p.per_split < p.blocks_k ? w.kb0 + p.per_split : p.blocks_k;
+    int tile = u, share = 0, per = p.blocks_k;
+    if (u >= plan.whole) {
+      share = (u - plan.whole) / plan.rest;
+      tile = u - share * plan.rest;
+      per = (p.blocks_k + plan.shares - 1) / plan.shares;
+      if (share) w.share = (tile - plan.whole) * (plan.shares - 1) + share - 1;
+    }
+    w.m0 = tile / p.tiles_n * kTile;
+    w.n0 = tile % p.tiles_n * kTile;
+    w.kb0 = share * per;
+    w.kb1 = w.kb0 + per < p.blocks_k ? w.kb0 + per : p.blocks_k;
   } else {
     w.m0 = u / p.tiles_n * kTile;
     w.n0 = u % p.tiles_n * kTile;
@@ -278,7 +304,10 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   after_previous();
   if (KIND == P_SUMS && p.direct && blockIdx.x == 0 && threadIdx.x < sizeof(LossInfo) / 4)
     reinterpret_cast<unsigned*>(p.clear)[threadIdx.x] = 0;
-  const int live = live_rows<KIND>(p), units = unit_count<KIND>(p, live);
+  const int live = live_rows<KIND>(p);
+  DhPlan plan = {0, 0, 1};
+  if (KIND == P_DH) plan = dh_plan(live, p.tiles_n, p.blocks_k, p.pairs, TERMS);
+  const int units = unit_count<KIND>(p, live, plan);
 
   constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
   // (registers change hands inside the branches: where paths meet the compiler counts on the fewer)
@@ -296,7 +325,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const bool idle = of_a && rank != 0 && p.a_even;
       bool ok = true;
       for (int u = pair; u < units && ok && !idle; u += pairs) {
-        const Unit w = unit_at<KIND>(p, u, live);
+        const Unit w = unit_at<KIND>(p, u, live, plan);
         const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * (KIND == P_SUMS ? p.tile_n / 2 : kHalf);
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           if (!mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u)) { ok = false; break; }
@@ -328,7 +357,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       int j = 0;
       bool ok = true;
       for (int u = pair; u < units && ok; u += pairs) {
-        const Unit w = unit_at<KIND>(p, u, live);
+        const Unit w = unit_at<KIND>(p, u, live, plan);
         for (int kb0 = w.kb0; kb0 < w.kb1 && ok; kb0 += kPiece, ++j) {
           const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
           if (!mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u)) { ok = false; break; }
@@ -403,7 +432,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       if (lane == 0) bulk_store_2d(map, at, col, row);
     };
     for (int u = pair; u < units && ok; u += pairs) {
-      const Unit w = unit_at<KIND>(p, u, live);
+      const Unit w = unit_at<KIND>(p, u, live, plan);
       const int row0 = w.m0 + (int)rank * kHalf + quarter * 32, row = row0 + lane;
       const int cols = KIND == P_SUMS ? p.tile_n / 2 : kSumColumns;          // of this warp
       const int col0 = w.n0 + side * cols;
@@ -521,7 +550,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
               st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
                            __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
             }
-            hand_over(&p.out, at, col0 + c, w.split * p.slab_rows + row0);
+            if (w.share < 0) hand_over(&p.out, at, col0 + c, row0);
+            else hand_over(&p.acc, at, col0 + c - w.n0, w.share * kTile + row0 - w.m0);
           }
         }
       } else {
@@ -1008,21 +1038,26 @@ __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2
 // dh of the piece's rows: the sums over the shares of K, in order, to the rows they belong to, four columns a thread
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
-dh_rows_kernel(LossArgs a, const float* slab, int splits, int slab_rows, int padded, int first, int piece, const int* row,
-               const LossInfo* info, T* dh) {
+dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, int tiles_n, int blocks_k, int pairs, int terms, int first,
+               int piece, const int* row, const LossInfo* info, T* dh) {
   after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
   const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, a.sampled_w)));
+  const DhPlan plan = dh_plan(live, tiles_n, blocks_k, pairs, terms);
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)live * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / per;
     const int c = (int)(i % per) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < splits; ++s) {
-      const float4 x = *reinterpret_cast<const float4*>(slab + ((size_t)s * slab_rows + r) * padded + c);
-      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    float4 v = *reinterpret_cast<const float4*>(slab + (size_t)r * padded + c);
+    const int tile = (int)(r / kTile) * tiles_n + c / kTile;
+    if (tile >= plan.whole) {
+      const float* from = shares + ((size_t)(tile - plan.whole) * (plan.shares - 1) * kTile + r % kTile) * kTile + c % kTile;
+      for (int s = 1; s < plan.shares; ++s, from += kTile * kTile) {
+        const float4 x = *reinterpret_cast<const float4*>(from);
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      }
     }
     v.x *= f; v.y *= f; v.z *= f; v.w *= f;
     T* to = dh + (int64_t)row[first + r] * a.ld_dh + c;
@@ -1046,27 +1081,10 @@ struct LossWs {
   double* part;
   float2* sums;
   unsigned short *h, *w, *e;
-  float *slab, *dw;
-  int blocks, piece, padded, vpadded, sum_blocks, staged_rows, piece_rows, splits;
+  float *slab, *shares, *dw;
+  int blocks, piece, padded, vpadded, sum_blocks, staged_rows, piece_rows;
   bool in_place;          // W is read where it lies
 };
-
-// Shares of K of the dh product, so that its tiles fill the device evenly: the least of (waves of tiles) x (time of a
-// tile) + (the sums' way through memory), in cycles, with a K block's products at 512 a term product and 8 bytes a sum at
-// 4.6 KB a cycle
-int dh_splits(int64_t rows, int dim, int blocks_k, int terms) {
-  const int64_t tiles = (rows + kTile - 1) / kTile * ceil_div(dim, kTile);
-  const int64_t pairs = sm_count() / 2;
-  const double block = terms == 1 ? 512.0 : 1536.0;
-  int best = 1;
-  double least = 1e300;
-  for (int s = 1; s <= 32 && (s == 1 || blocks_k / s >= 16); ++s) {
-    const double t = (double)((tiles * s + pairs - 1) / pairs) * (ceil_div(blocks_k, s) * block + 3000.0) +
-                     (double)s * rows * dim * 8.0 / 4600.0;
-    if (t < least) { least = t; best = s; }
-  }
-  return best;
-}
 
 // Columns of a tile of few rows, whose time is the vocabulary's way through memory: as even a share for every pair as
 // the instructions allow, 64 at least (16 rows of 32768x2048: 147 tiles of 224 columns on 74 pairs, 128 of 256 leave 20
@@ -1105,7 +1123,6 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   }
   l->piece = (int)piece;
   l->piece_rows = (int)align_up((size_t)piece, kTile);
-  l->splits = gradient ? dh_splits(piece, d->dim, l->vpadded / kBK, terms) : 0;
   l->info = (LossInfo*)take(sizeof(LossInfo));
   l->counts = (int*)take((size_t)l->blocks * 4);
   l->row = (int*)take(n * 4);
@@ -1118,7 +1135,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->h = (unsigned short*)take((size_t)l->staged_rows * l->padded * 2 * terms);
   l->w = (unsigned short*)take(l->in_place ? 0 : v * l->padded * 2 * terms);
   l->e = (unsigned short*)take(gradient ? (size_t)l->piece_rows * l->vpadded * 2 * terms : 0);
-  l->slab = (float*)take(gradient ? (size_t)l->splits * l->piece_rows * l->padded * 4 : 0);
+  l->slab = (float*)take(gradient ? (size_t)l->piece_rows * l->padded * 4 : 0);
+  l->shares = (float*)take(gradient ? (size_t)share_blocks(sm_count() / 2) * kTile * kTile * 4 : 0);
   l->dw = (float*)take(gradient && l->piece < d->rows ? v * l->padded * 4 : 0);
   return at;
 }
@@ -1263,7 +1281,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     p.piece = l.piece;
     p.sum_blocks = l.sum_blocks;
     p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
-    p.splits = 1;
+    p.pairs = sm_count() / 2;
     p.tile_n = kTile;
     ProductArgs logits = p, by_h = p, by_w = p;
     logits.direct = direct;
@@ -1291,13 +1309,11 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       // dh: K along the rows of dz and across those of W
       by_h.tiles_n = ceil_div(a.dim, kTile);
       by_h.blocks_k = l.vpadded / kBK;
-      by_h.splits = l.splits;
-      by_h.per_split = ceil_div(by_h.blocks_k, l.splits);
-      by_h.slab_rows = l.piece_rows;
       by_h.idesc = instruction(false, false, true);
       MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, TERMS, kHalf, 1));
       MW_TRY(group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, 2));
-      MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, (int64_t)l.splits * l.piece_rows, l.padded));
+      MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece_rows, l.padded));
+      MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)share_blocks(p.pairs) * kTile, kTile));
       // dW: K across the rows of both
       by_w.tiles_m = ceil_div(a.vocab, kTile);
       by_w.tiles_n = ceil_div(a.dim, kTile);
@@ -1330,9 +1346,10 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
             MW_TRY(launch_after(loss_rows_kernel, blocks, 256, 0, s, l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part, total));
         }
         if (dh) {
-          MW_TRY((run_product<TERMS, P_DH>(by_h, tm * by_h.tiles_n * l.splits, s)));
+          MW_TRY((run_product<TERMS, P_DH>(by_h, p.pairs, s)));
           auto rows_kernel = ((uintptr_t)dh & 15) == 0 && a.ld_dh % 4 == 0 && a.dim % 4 == 0 ? dh_rows_kernel<T, true> : dh_rows_kernel<T, false>;
-          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.splits, l.piece_rows, l.padded, (int)first, l.piece, l.row, l.info, dh));
+          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.shares, l.padded, by_h.tiles_n, by_h.blocks_k, p.pairs, TERMS, (int)first, l.piece,
+                              l.row, l.info, dh));
         }
       }
       if (dw) MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n, s)));
