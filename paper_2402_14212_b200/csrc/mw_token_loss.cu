@@ -52,9 +52,11 @@ constexpr int stages_for(int terms, int kind, uint32_t a_stage) {
   const int n = (int)(room / (a_stage + (uint32_t)terms * kPlaneBytes));
   return n < kStagesMax ? n : kStagesMax;
 }
-// K blocks that one accumulator takes: 128 instructions of bf16 operands, 96 of two-term ones.  Each cuts the sum
-// off at its last place; what that leaves of a sum of one sign is 2^-17.
-__host__ __device__ constexpr int piece_blocks(int terms) { return terms == 1 ? 32 : 8; }
+// K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place; of a sum of one sign 128
+// instructions (logits of bf16 operands), or 96 (two terms), take 2^-17.  dz of bf16 operands has 11 bits: its sums have
+// 512 instructions an accumulator, 2^-15, and are read out a quarter as often (3686 rows of 131072x4096: dh 3.05 ms with
+// 128 instructions).
+__host__ __device__ constexpr int piece_blocks(int terms, int kind) { return terms == 2 ? 8 : (kind == P_DH || kind == P_DW ? 128 : 32); }
 
 // what the kernels of one call share, behind the status block
 struct LossInfo {
@@ -259,7 +261,7 @@ template <int TERMS, int KIND>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr int kBuffers = buffer_count(TERMS, KIND), kPiece = piece_blocks(TERMS);
+  constexpr int kBuffers = buffer_count(TERMS, KIND), kPiece = piece_blocks(TERMS, KIND);
   constexpr uint32_t b_stage = TERMS * kPlaneBytes;
   __shared__ __align__(8) uint64_t full_bar[kStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
@@ -746,6 +748,18 @@ __device__ __forceinline__ void split_half(float v, unsigned short& hi, unsigned
   lo = __half_as_ushort(l);
 }
 
+// the largest of a block's values into *most
+__device__ __forceinline__ void block_largest(unsigned m, unsigned* most) {
+  __shared__ unsigned warp_m[8];
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0) warp_m[threadIdx.x >> 5] = m;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    m = __reduce_max_sync(0xffffffffu, threadIdx.x < 8 ? warp_m[threadIdx.x] : 0u);
+    if (threadIdx.x == 0 && m) atomicMax(most, m);
+  }
+}
+
 // h (rows with a target, by their index) or W as operands: [terms][staged rows][padded columns], zero beyond a row's
 // end and beyond the last row to a multiple of a tile
 template <typename T>
@@ -774,16 +788,17 @@ __global__ void __launch_bounds__(256) largest_kernel(Operand<T> w, Operand<T> h
   const int64_t n = o.count ? *o.count : o.rows;
   const uint32_t per = (uint32_t)(dim + 7) / 8, step = o.sampled ? kSampleRows : 1;
   const int64_t items = (n + step - 1) / step * per;
+  const bool small = items < 0x7fffffff;           // (divisions in 32 bits)
   unsigned m = 0;
+#pragma unroll 2
   for (int64_t i = block * 256 + threadIdx.x; i < items; i += blocks * 256) {
-    const int64_t r = i / per * step;
+    const int64_t row = small ? (uint32_t)i / per : i / per, r = row * step;
     float v[8];
-    load8<T, WIDE>(o.x + (o.row ? (int64_t)o.row[r] : r) * o.ld, (int)(i % per) * 8, dim, v);
+    load8<T, WIDE>(o.x + (o.row ? (int64_t)o.row[r] : r) * o.ld, (int)(i - row * per) * 8, dim, v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) m = max(m, finite_bits(v[k]));
   }
-  m = __reduce_max_sync(0xffffffffu, m);
-  if ((threadIdx.x & 31) == 0 && m) atomicMax(o.most, m);
+  block_largest(m, o.most);
 }
 
 // AGAIN: only what the sample misjudged.  SCALED false: bf16 as it is.
@@ -804,10 +819,12 @@ __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, 
   const int64_t whole = (n + kTile - 1) / kTile * kTile, upto = whole < o.staged_rows ? whole : o.staged_rows;
   const uint32_t per = (uint32_t)padded / 8;
   const int64_t items = (o.dead && upto < o.rows ? o.rows : upto) * per;
+  const bool small = items < 0x7fffffff;
   unsigned m = 0;
+#pragma unroll 2
   for (int64_t i = block * 256 + threadIdx.x; i < items; i += blocks * 256) {
-    const int64_t r = i / per;
-    const int c = (int)(i % per) * 8;
+    const int64_t r = small ? (uint32_t)i / per : i / per;
+    const int c = (int)(i - r * per) * 8;
     const int64_t at = o.row && r < o.rows ? o.row[r] : r;
     if (r < upto) {
       unsigned short hi[8], lo[8];
@@ -845,10 +862,7 @@ __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, 
     if (!AGAIN && o.dead && r >= n && r < o.rows)
       for (int k = 0; k < 8 && c + k < dim; ++k) o.dead[at * o.ld_dead + c + k] = from_f64<T>(0.0);
   }
-  if (SCALED && !AGAIN && o.sampled) {
-    m = __reduce_max_sync(0xffffffffu, m);
-    if ((threadIdx.x & 31) == 0 && m) atomicMax(o.most + 1, m);
-  }
+  if (SCALED && !AGAIN && o.sampled) block_largest(m, o.most + 1);
 }
 
 // joins the sums of a row's blocks: log2 of the whole sum
@@ -989,43 +1003,74 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       part[i] = (double)g[i] * (double)l;
     }
     const float gi = g[i] * to_range, at_target = gi * expm1f(-l), share = gi / v.sum;
+    // (four accesses of a thread under way)
+    constexpr int kAhead = 4;
     if (TERMS == 1) {
-      for (int c = threadIdx.x * 8; c < padded; c += 256 * 8) {
-        const float f = share * exp2_fast(mine[c / kSumColumns].x - v.k);
-        const uint4 raw = *reinterpret_cast<const uint4*>(at + c);
-        const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
-        uint32_t out[4];
+      for (int c0 = threadIdx.x * 8; c0 < padded; c0 += 256 * 8 * kAhead) {
+        uint4 raw[kAhead];
+        float f[kAhead];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float2 x = __half22float2(*reinterpret_cast<const __half2*>(&in[q]));
-          x.x = c + 2 * q == t ? at_target : x.x * f;
-          x.y = c + 2 * q + 1 == t ? at_target : x.y * f;
-          out[q] = half2_bits(x.x, x.y);
+        for (int j = 0; j < kAhead; ++j) {
+          const int c = c0 + j * 256 * 8;
+          if (c < padded) {
+            raw[j] = *reinterpret_cast<const uint4*>(at + c);
+            f[j] = mine[c / kSumColumns].x;
+          }
         }
-        *reinterpret_cast<uint4*>(at + c) = make_uint4(out[0], out[1], out[2], out[3]);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int c = c0 + j * 256 * 8;
+          if (c < padded) {
+            const float by = share * exp2_fast(f[j] - v.k);
+            const uint32_t in[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+            uint32_t out[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&in[q]));
+              out[q] = half2_bits(x.x * by, x.y * by);
+            }
+            if (t >= c && t < c + 8) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const uint32_t h = half2_bits(at_target, at_target);
+                if (t - c == 2 * q) out[q] = (out[q] & 0xffff0000u) | (h & 0xffffu);
+                if (t - c == 2 * q + 1) out[q] = (out[q] & 0xffffu) | (h & 0xffff0000u);
+              }
+            }
+            *reinterpret_cast<uint4*>(at + c) = make_uint4(out[0], out[1], out[2], out[3]);
+          }
+        }
       }
     } else {
       // a group of 64 floats becomes 64 leading terms and 64 remainders: sixteen lanes, four of them each
-      for (int c0 = warp * 128; c0 < padded; c0 += 8 * 128) {
-        const int c = c0 + lane * 4;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        if (c < padded) {
-          const float f = share * exp2_fast(mine[c / kSumColumns].x - v.k);
-          const float4 raw = *reinterpret_cast<const float4*>(at + 2 * c);
-          x[0] = raw.x * f; x[1] = raw.y * f; x[2] = raw.z * f; x[3] = raw.w * f;
+      for (int c0 = warp * 128 + lane * 4; c0 - lane * 4 < padded; c0 += 8 * 128 * kAhead) {          // (a warp together)
+        float4 raw[kAhead];
+        float f[kAhead];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) x[q] = c + q == t ? at_target : x[q];
+        for (int j = 0; j < kAhead; ++j) {
+          const int c = c0 + j * 8 * 128;
+          if (c < padded) {
+            raw[j] = *reinterpret_cast<const float4*>(at + 2 * c);
+            f[j] = mine[c / kSumColumns].x;
+          }
         }
         __syncwarp();
-        if (c < padded) {
-          unsigned short hi[4], lo[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) split_half(x[q], hi[q], lo[q]);
-          unsigned short* to = at + 2 * (c & ~63) + (c & 63);
-          *reinterpret_cast<uint2*>(to) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
-          *reinterpret_cast<uint2*>(to + 64) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+        for (int j = 0; j < kAhead; ++j) {
+          const int c = c0 + j * 8 * 128;
+          if (c < padded) {
+            const float by = share * exp2_fast(f[j] - v.k);
+            float x[4] = {raw[j].x * by, raw[j].y * by, raw[j].z * by, raw[j].w * by};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = c + q == t ? at_target : x[q];
+            unsigned short hi[4], lo[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) split_half(x[q], hi[q], lo[q]);
+            unsigned short* to = at + 2 * (c & ~63) + (c & 63);
+            *reinterpret_cast<uint2*>(to) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
+            *reinterpret_cast<uint2*>(to + 64) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+          }
         }
-        __syncwarp();
       }
     }
   }
