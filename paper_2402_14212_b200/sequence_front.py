@@ -1,6 +1,7 @@
 """A stack of recurrent blocks in front of a Moonwalk net, trained with the orthogonalised update.
 
-`python -m paper_2402_14212_b200.sequence_front` trains it on a synthetic sequence task and prints the loss.
+`python -m paper_2402_14212_b200.sequence_front` trains it on a synthetic sequence task and prints the loss; with
+`--inputs V` its inputs are tokens of a vocabulary of V, with `--tokens V` the stack alone learns to say the next token.
 
 Block (x: residual stream [batch * time, width], n: its normed copy):
 
@@ -13,6 +14,10 @@ cotangent of the stack's output: the blocks' backward calls carry it on from the
 sweep forms its own gradients.  Products, recurrence, norms, the net and the updates of its weights and of the projections
 run in the library; torch holds the memory, adds the fixed bias of f, puts dz beside dv and df, and takes the plain
 gradient steps of the per-channel weights.
+
+Tokens enter through rows of a table (embedding); a token model ends in the vocabulary's loss over the same table
+(token_loss_gradient), whose gradient takes that of the lookup on top.  clip bounds the norm of all gradients of a step
+together (clip_gradients).
 """
 from __future__ import annotations
 
@@ -93,11 +98,25 @@ class SequenceFront:
         return r.dx.view(B, T, D), grads
 
 
-class Trainer:
-    """The stack, a dense Moonwalk net behind it, and their updates."""
+def _table(vocab, width, seed):
+    import torch
+    g = torch.Generator(device="cpu").manual_seed(seed + 1000)
+    return (torch.randn(vocab, width, generator=g) / math.sqrt(width)).cuda()
 
-    def __init__(self, width=128, blocks=2, depth=3, batch=8, time=64, lr=2e-3, seed=0):
+
+def _flat(grads):
+    """All tensors of a dict of gradients, lists among them."""
+    return [t for g in grads.values() for t in (g if isinstance(g, list) else [g])]
+
+
+class Trainer:
+    """The stack, a dense Moonwalk net behind it, and their updates.  With `vocab` the inputs are tokens (of negative
+    ones a row is zero); with `clip` the gradients of a step are scaled together to that norm at most."""
+
+    def __init__(self, width=128, blocks=2, depth=3, batch=8, time=64, lr=2e-3, seed=0, vocab=None, clip=None):
         import torch
+        self.clip, self.norm = clip, None
+        self.table = None if vocab is None else _table(vocab, width, seed)
         self.front = SequenceFront(width, blocks, seed)
         problem = S.deep_mlp(seed=seed, depth=depth, n=width, batch=batch * time, reseed_every=2)
         self.net = mwb.net_for(problem, backend="tensor")
@@ -114,16 +133,24 @@ class Trainer:
         self.stepped = False
 
     def gradients(self, x, target):
-        """(gradients of the net's weights, of the stack's, dL/dx); the loss lands in self.loss."""
+        """(gradients of the net's weights, of the stack's, dL/dx); the loss lands in self.loss.  Of tokens x the
+        table's gradient is among the stack's, and dL/dx is that of their rows."""
+        tokens, scale = x, math.sqrt(self.front.width)
+        if self.table is not None:
+            x = mwb.embedding(tokens, self.table, scale=scale)
         x0, tape = self.front.forward(x)
         x0 = x0.contiguous()
         g0 = self.net.input_cotangent(self.params, x0, target, self.ws, loss_out=self.loss)
         dx, front = self.front.backward(g0, tape)
+        if self.table is not None:
+            front["table"] = mwb.embedding_backward(tokens, dx, self.table.shape[0], scale=scale)
         dW = self.net.forward_sweep(self.params, x0, g0, self.ws)
         return dW, front, dx
 
     def step(self, x, target):
         dW, front, _ = self.gradients(x, target)
+        if self.clip is not None:
+            self.norm = mwb.clip_gradients(list(dW) + _flat(front), self.clip)
         # orthogonalised updates move every direction of a weight alike, so the net's weights stay near a
         # multiple of an orthogonal matrix, where its inverse converges
         self.orth.step(self.params, dW, self.momentum, self.orth_ws, lr=self.lr)
@@ -133,6 +160,8 @@ class Trainer:
             for w, g in zip(getattr(self.front, name), front[name]):
                 w.sub_(g, alpha=self.lr)
         self.front.w_in.sub_(front["w_in"], alpha=self.lr)
+        if self.table is not None:
+            self.table.sub_(front["table"], alpha=self.lr)
         return self.loss
 
     def status(self) -> int:
@@ -141,6 +170,74 @@ class Trainer:
         if code == 0 and self.stepped:
             code = self.orth.status(self.orth_ws) or self.orth_proj.status(self.orth_proj_ws)
         return code
+
+
+class TokenTrainer:
+    """A token model of the stack alone: rows of a table, the blocks, a last norm, the vocabulary's loss by the same
+    table; each position says the token after it.  Negative tokens are padding: they are no input and no target."""
+
+    def __init__(self, vocab=1000, width=128, blocks=2, lr=2e-3, clip=1.0, seed=0):
+        import torch
+        self.front = SequenceFront(width, blocks, seed)
+        self.table = _table(vocab, width, seed)
+        self.w_out = torch.ones(width, device="cuda")
+        self.lr, self.clip, self.norm = lr, clip, None
+        self.orth_proj = mwb.Orth(3 * width, width, blocks, "f32")
+        self.orth_proj_ws = self.orth_proj.alloc_workspace()
+        self.proj_momentum = [torch.zeros_like(w) for w in self.front.proj]
+
+    def _states(self, tokens):
+        x = mwb.embedding(tokens, self.table, scale=math.sqrt(self.front.width))
+        s, tape = self.front.forward(x)
+        _, n, rms = mwb.residual_norm(s, w_pre=self.w_out, keep_rms=True)
+        return s, n, rms, tape
+
+    def losses(self, tokens):
+        """TokenLoss of tokens [batch, time + 1], a loss for each of the [batch * time] positions."""
+        _, n, _, _ = self._states(tokens[:, :-1])
+        return mwb.token_loss(n, self.table, tokens[:, 1:].reshape(-1))
+
+    def gradients(self, tokens):
+        """(TokenLoss, gradients by name) of tokens [batch, time + 1]."""
+        inputs, targets = tokens[:, :-1], tokens[:, 1:].reshape(-1)
+        s, n, rms, tape = self._states(inputs)
+        r = mwb.token_loss_gradient(n, self.table, targets)
+        g = mwb.residual_norm_backward(s, None, rms, w_pre=self.w_out, dn=r.dh)
+        dx, grads = self.front.backward(g.dx, tape)
+        grads["w_out"] = g.dw_pre
+        grads["table"] = mwb.embedding_backward(inputs, dx, self.table.shape[0], scale=math.sqrt(self.front.width),
+                                                dtable=r.dweight, accumulate=True)
+        return r, grads
+
+    def step(self, tokens):
+        """One update; returns the mean loss of the positions that have a target."""
+        r, grads = self.gradients(tokens)
+        if self.clip is not None:
+            self.norm = mwb.clip_gradients(_flat(grads), self.clip)
+        f = self.front
+        self.orth_proj.step(f.proj, grads["proj"], self.proj_momentum, self.orth_proj_ws, lr=4 * self.lr)
+        for name in ("w_post", "scale", "w_pre"):
+            for w, g in zip(getattr(f, name), grads[name]):
+                w.sub_(g, alpha=self.lr)
+        f.w_in.sub_(grads["w_in"], alpha=self.lr)
+        self.w_out.sub_(grads["w_out"], alpha=self.lr)
+        self.table.sub_(grads["table"], alpha=50 * self.lr)
+        return r.total
+
+
+def make_tokens(vocab, batch, time, seed):
+    """Token sequences [batch, time + 1] that a fixed table of successors drives, one step in eight at random; the last
+    sequence is padded from its middle on."""
+    import torch
+    g = torch.Generator(device="cpu").manual_seed(seed + 200)
+    after = torch.randperm(vocab, generator=g)
+    t = torch.empty(batch, time + 1, dtype=torch.int64)
+    t[:, 0] = torch.randint(0, vocab, (batch,), generator=g)
+    for i in range(1, time + 1):
+        any_, pick = torch.randint(0, vocab, (batch,), generator=g), torch.rand(batch, generator=g) < 0.125
+        t[:, i] = torch.where(pick, any_, after[t[:, i - 1]])
+    t[-1, time // 2:] = -1
+    return t.cuda()
 
 
 def make_task(width, batch, time, seed):
@@ -165,9 +262,22 @@ def main():
     ap.add_argument("--time", type=int, default=64)
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--lr", type=float, default=2e-3)
+    ap.add_argument("--inputs", type=int, default=0, metavar="V", help="inputs are tokens of a vocabulary of V")
+    ap.add_argument("--tokens", type=int, default=0, metavar="V", help="the stack alone says the next of V tokens")
+    ap.add_argument("--clip", type=float, default=None, help="bound of the gradients' norm")
     a = ap.parse_args()
-    t = Trainer(a.width, a.blocks, a.depth, a.batch, a.time, a.lr)
+    if a.tokens:
+        t = TokenTrainer(a.tokens, a.width, a.blocks, a.lr, a.clip)
+        tokens = make_tokens(a.tokens, a.batch, a.time, 0)
+        for i in range(a.steps):
+            loss = float(t.step(tokens))
+            if i % 10 == 0 or i == a.steps - 1:
+                print(f"step {i:4d}  loss {loss:.5f}" + (f"  norm {float(t.norm):.3f}" if a.clip is not None else ""))
+        return
+    t = Trainer(a.width, a.blocks, a.depth, a.batch, a.time, a.lr, vocab=a.inputs or None, clip=a.clip)
     x, target = make_task(a.width, a.batch, a.time, 0)
+    if a.inputs:
+        x = make_tokens(a.inputs, a.batch, a.time, 0)[:, :-1]
     for i in range(a.steps):
         loss = float(t.step(x, target).item())
         if i % 10 == 0 or i == a.steps - 1:
