@@ -1053,9 +1053,12 @@ def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=N
     of weight (a negative one, say), or whose row_weight is zero, are left out: their loss is zero and their h is
     not read into anything.  total = sum of row_weight * loss, the mean over the rows that are left without
     row_weight.  `stream` as in gated_scan."""
+    import torch
     if stream is not None:
         return _on_stream(stream, h, token_loss, h, weight, targets, scale, row_weight)
     h, weight = _own_memory(h, weight)
+    if weight.data_ptr() & 15:         # (read in place, by copies of 16 bytes)
+        weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(False, h, weight, targets, scale, row_weight, 0, None, None, None, (False, False))
 
 
@@ -1084,14 +1087,14 @@ def clip_gradients(grads, max_norm: float, out=None, stream=None):
     out = grads if out is None else list(out)
     if stream is not None:
         return _on_stream(stream, grads[0], clip_gradients, grads, max_norm, out)
-    n, device = len(grads), grads[0].device
+    n, device, place = len(grads), grads[0].device, {grads[0].get_device()}
     _need(grads[0].is_cuda and len(out) == n, "clip_gradients: CUDA tensors, and as many outputs")
     Tensor, in_place = torch.Tensor, all(map(operator.is_, grads, out))
     # (whole lists at a time: a step has hundreds of tensors, and the loop over them is the call's time)
     kinds, sizes = [g.dtype for g in grads], list(map(Tensor.numel, grads))
-    ok = all(map(Tensor.is_contiguous, grads)) and set(map(Tensor.get_device, grads)) == {device.index}
+    ok = all(map(Tensor.is_contiguous, grads)) and set(map(Tensor.get_device, grads)) == place
     if not in_place:
-        ok = ok and all(map(Tensor.is_contiguous, out)) and set(map(Tensor.get_device, out)) == {device.index}
+        ok = ok and all(map(Tensor.is_contiguous, out)) and set(map(Tensor.get_device, out)) == place
         ok = ok and kinds == [o.dtype for o in out] and sizes == list(map(Tensor.numel, out))
     codes = {torch.float32: 1, torch.bfloat16: 2}
     if not ok or not codes.keys() >= set(kinds):

@@ -1,0 +1,135 @@
+"""The lookup and the vocabulary's loss where their kernels change course: operands whose sample misleads, few rows taken
+as they lie, waves of tiles with a rest, pieces with gradients off the copy engine's boundaries, places beyond 2^31, two
+calls at once.  Formulas and tolerances are those of test_gpu_token_loss.py and test_gpu_embedding.py."""
+import pytest
+import torch
+
+from paper_2402_14212_b200 import binding as mwb
+from test_gpu_embedding import check_gradient
+from test_gpu_token_loss import ALL, BF16, F32, check, make, reference
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("how", ["as it is", "outlier", "zeros in the sample", "small sample", "large sample"])
+def test_operands_whose_sample_misleads(how, dtype):
+    """Operands of more than 32 MiB are written by what every sixteenth row holds, and again where that misses."""
+    V, D, N = (4300 if dtype == F32 else 8600), 2048, 200
+    h, W, t = make(N, V, D, dtype, lean=0.0)
+    sampled = torch.arange(V, device="cuda") % 16 == 0
+    if how == "outlier":
+        W[1, 5] = 3.0e4
+        h[:, 5] = 0
+    elif how == "zeros in the sample":
+        W[sampled] = 0
+    elif how == "small sample":
+        W[sampled] *= 2.0 ** -12
+    elif how == "large sample":
+        W[~sampled] *= 2.0 ** -12
+    check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("ids", [torch.int32, torch.int64])
+@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 33, 64, 65, 128, 129, 200, 256, 257])
+def test_few_rows_taken_as_they_lie(N, ids):
+    h, W, t = make(N, 3001, 264, BF16, seed=N, left_out=0.3)
+    w = torch.rand(N, device="cuda")
+    w[::5] = 0
+    h[::5] = float("nan")
+    for weight in (None, w):
+        on = h.clone() if weight is not None else torch.where(h.isnan(), 0.5, h.float()).to(BF16)
+        check(mwb.token_loss(on, W, t.to(ids), row_weight=weight), reference(on, W, t, weight=weight), ("loss", "total"))
+    # rows off the copy engine's boundaries
+    wide = torch.zeros(N, 300, device="cuda", dtype=BF16)
+    off = wide[:, 1:265]
+    off.copy_(on)
+    check(mwb.token_loss(off, W, t.to(ids), row_weight=w), reference(on, W, t, weight=w), ("loss", "total"))
+
+
+@pytest.mark.parametrize("V", [1, 31, 63, 64, 65, 4736, 4737, 18944, 18945, 20000])
+def test_vocabularies_of_few_rows(V):
+    h, W, t = make(20, V, 72, BF16, seed=V)
+    check(mwb.token_loss(h, W, t), reference(h, W, t), ("loss", "total"))
+
+
+def test_a_weight_that_starts_off_its_boundary():
+    h, W, t = make(300, 200, 64, BF16)
+    wide = torch.zeros(200, 72, device="cuda", dtype=BF16)
+    wide[:, 1:65] = W
+    check(mwb.token_loss(h, wide[:, 1:65], t), reference(h, W, t), ("loss", "total"))
+    check(mwb.token_loss_gradient(h, wide[:, 1:65], t), reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V,D", [(256, 520, 64), (256, 8200, 300), (1300, 4100, 260), (2600, 2100, 2050), (5000, 1100, 1024)])
+def test_waves_of_tiles_with_a_rest(N, V, D, dtype):
+    h, W, t = make(N, V, D, dtype, left_out=0.05)
+    check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("D", [65, 64, 130])
+def test_pieces_with_gradients_off_the_boundaries(D, kind, dtype):
+    h, W, t = make(900, 301, D, dtype, left_out=0.4)
+    wide = torch.full((301, D + 7), 5.0, device="cuda", dtype=kind)
+    r = mwb.token_loss_gradient(h, W, t, piece_rows=256, dweight=wide[:, 3:3 + D])
+    check(r, reference(h, W, t), ALL)
+    assert bool((wide[:, :3] == 5).all() and (wide[:, 3 + D:] == 5).all())
+    r = mwb.token_loss_gradient(h, W, t, piece_rows=256, grad_dtype=kind)
+    check(r, reference(h, W, t), ALL)
+
+
+def test_lookup_in_a_table_beyond_2_31_elements():
+    V, D = 2200000, 1024
+    table = torch.zeros(V, D, device="cuda", dtype=BF16)
+    t = torch.tensor([V - 1, 0, V - 1, V, V - 2, -1], device="cuda")
+    rows = torch.randn(6, D, device="cuda").to(BF16)
+    table[V - 1], table[V - 2], table[0] = rows[0], rows[1], rows[2]
+    out = mwb.embedding(t, table)
+    zero = torch.zeros_like(rows[0])
+    assert torch.equal(out, torch.stack([rows[0], rows[2], rows[0], zero, rows[1], zero]))
+    d = mwb.embedding_backward(t, rows, V)
+    near = torch.cat([d[:3], d[-3:]])
+    s = torch.tensor([0, -1, 2, -1, -1, 1], device="cuda")
+    check_gradient(near, torch.tensor([5, 0, 5, -1, 4, -1], device="cuda"), rows, 6, 1.0)
+    assert s.shape == (6,) and float(d[3:-3].abs().amax()) == 0.0
+
+
+def test_exponentials_beyond_2_31_elements():
+    N, V, D = 16384, 140000, 64
+    h, W, t = make(N, V, D, BF16, lean=4.0)
+    r = mwb.token_loss_gradient(h, W, t, piece_rows=N)
+    at = torch.tensor([0, 77777, V - 1], device="cuda")
+    lse = torch.cat([torch.logsumexp(p.double() @ W.double().T, 1) for p in h.split(1024)])
+    hd = h.double()
+    loss = lse - (hd * W[t].double()).sum(1)
+    assert float((r.loss.double() - loss).abs().max()) <= 1e-4          # (S < 100 here: 12 x 2^-23 x 100, twice, and 2^-20 x 20)
+    # dW of three rows of the vocabulary: relative errors of p of 2^-10, of its products of 2^-13 and less
+    dz = (torch.exp(hd @ W[at].double().T - lse[:, None]) - (t[:, None] == at).double()) / N
+    want, size = dz.T @ hd, dz.abs().T @ hd.abs()
+    off = (r.dweight[at].double() - want).abs()
+    assert bool((off <= 1.2e-3 * size + 2.0 ** -8 * want.abs() + 2.0 ** -38).all())
+    # dh of the last rows
+    p = torch.exp(hd[-64:] @ W.double().T - lse[-64:, None]) / N
+    p[torch.arange(64, device="cuda"), t[-64:]] -= 1 / N
+    want, size = p @ W.double(), p.abs() @ W.double().abs()
+    off = (r.dh[-64:].double() - want).abs()
+    assert bool((off <= 2.2e-3 * size + 2.0 ** -8 * want.abs() + 2.0 ** -38).all())          # (140000 / 16 cut-offs: 1e-3)
+
+
+def test_two_calls_at_once():
+    a, b = make(600, 5000, 256, BF16, seed=1), make(500, 4000, 320, F32, seed=2)
+    t = torch.randint(0, 300, (5000,), device="cuda")
+    d = torch.randn(5000, 256, device="cuda")
+    want = (mwb.token_loss_gradient(*a), mwb.token_loss_gradient(*b), mwb.embedding_backward(t, d, 300))
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(5):
+        got = (mwb.token_loss_gradient(*a, stream=s[0]), mwb.token_loss_gradient(*b, stream=s[1]),
+               mwb.embedding_backward(t, d, 300, stream=s[2]))
+        torch.cuda.synchronize()
+        for x, y in zip(got[:2], want[:2]):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
+        assert torch.equal(got[2], want[2])
