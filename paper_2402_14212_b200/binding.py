@@ -150,8 +150,7 @@ def lib() -> C.CDLL:
         L.mw_token_loss_gradient.argtypes = [tloss] + [vp] * 9 + [sz, vp]
         L.mw_token_loss_status.argtypes = [vp, vp]
         L.mw_clip_scratch_bytes.argtypes = [i32, C.POINTER(sz)]
-        L.mw_clip_gradients.argtypes = [i32, C.POINTER(vp), C.POINTER(vp), C.POINTER(C.c_int64), C.POINTER(i32),
-                                        C.c_double, vp, vp, sz, vp]
+        L.mw_clip_gradients.argtypes = [i32, vp, vp, vp, vp, C.c_double, vp, vp, sz, vp]     # (arrays by their addresses)
         L.mw_profile_begin.argtypes = []
         L.mw_profile_begin.restype = None
         L.mw_profile_end.argtypes = [C.POINTER(C.c_double), C.POINTER(C.c_int64),
@@ -1099,16 +1098,19 @@ def clip_gradients(grads, max_norm: float, out=None, stream=None):
     codes = {torch.float32: 1, torch.bfloat16: 2}
     if not ok or not codes.keys() >= set(kinds):
         raise ValueError("clip_gradients: contiguous float32 or bfloat16 tensors on one device, outputs like them")
-    need = C.c_size_t()
-    _check(lib().mw_clip_scratch_bytes(n, need), "mw_clip_scratch_bytes")
+    need = _passed.get(("clip", n))
+    if need is None:
+        size = C.c_size_t()
+        _check(lib().mw_clip_scratch_bytes(n, size), "mw_clip_scratch_bytes")
+        need = _remember(("clip", n), int(size.value))
     norm = torch.empty((), dtype=torch.float32, device=device)
-    scratch = torch.empty(need.value, dtype=torch.uint8, device=device)
-    ptrs = (C.c_void_p * n).from_buffer
-    src = ptrs(array.array("Q", map(Tensor.data_ptr, grads)))
-    dst = src if in_place else ptrs(array.array("Q", map(Tensor.data_ptr, out)))
-    _check(_call("mw_clip_gradients", device, n, src, dst, (C.c_int64 * n).from_buffer(array.array("q", sizes)),
-                 (C.c_int32 * n).from_buffer(array.array("i", map(codes.__getitem__, kinds))),
-                 float(max_norm), norm.data_ptr(), scratch.data_ptr(), need.value), "mw_clip_gradients")
+    scratch = torch.empty(need, dtype=torch.uint8, device=device)
+    src = array.array("Q", map(Tensor.data_ptr, grads))
+    dst = src if in_place else array.array("Q", map(Tensor.data_ptr, out))
+    sizes, kinds = array.array("q", sizes), array.array("i", map(codes.__getitem__, kinds))
+    at = [a.buffer_info()[0] for a in (src, dst, sizes, kinds)]
+    _check(_call("mw_clip_gradients", device, n, *at, float(max_norm), norm.data_ptr(), scratch.data_ptr(), need),
+           "mw_clip_gradients")
     return norm
 
 

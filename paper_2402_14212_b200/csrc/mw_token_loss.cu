@@ -201,6 +201,14 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live, c
   return w;
 }
 
+// K blocks of each of a tile's pieces: as even as they come, since a short one leaves the products waiting for the epilogue
+template <int TERMS, int KIND>
+__device__ __forceinline__ int piece_of(const Unit& w) {
+  constexpr int kMost = piece_blocks(TERMS, KIND);
+  const int n = w.kb1 - w.kb0, pieces = (n + kMost - 1) / kMost;
+  return pieces > 1 ? (n + pieces - 1) / pieces : kMost;
+}
+
 // byte offset of 16-byte piece c of row r in a block of 128-byte rows under the 128-byte swizzle
 __device__ __forceinline__ uint32_t piece_at(uint32_t r, uint32_t c) { return r * 128u + ((c ^ (r & 7u)) << 4); }
 __device__ __forceinline__ void bulk_store_2d(const CUtensorMap* tm, uint32_t src, int c0, int c1) {
@@ -243,6 +251,12 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// one lane of a warp whose lanes are all here: what it does may use the registers that the warp has in common
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -261,7 +275,7 @@ template <int TERMS, int KIND>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr int kBuffers = buffer_count(TERMS, KIND), kPiece = piece_blocks(TERMS, KIND);
+  constexpr int kBuffers = buffer_count(TERMS, KIND);
   constexpr uint32_t b_stage = TERMS * kPlaneBytes;
   __shared__ __align__(8) uint64_t full_bar[kStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
@@ -270,7 +284,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_cta_rank();
   const int stages = p.stages;
   const uint32_t a_stage = p.a_stage;
@@ -314,23 +328,25 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
   // (registers change hands inside the branches: where paths meet the compiler counts on the fewer)
   if (warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+  // The copies' and the products' loops are run by whole warps, and one lane is elected for the instructions themselves:
+  // addresses are then the warp's, in uniform registers, where a loop of one lane moves every operand there first (61
+  // cycles a product and 66 a commit; a K block's four and their waits came to 470 of the 512 that the products take).
   if (warp == 0 || warp == 2) {
     // ---------------- copies: A's by one warp, B's by another ----------------
-    // (A copy takes the lane that issues it 120 to 190 cycles; two a K block by one lane, with its waits, took 0.34 us,
-    // whatever the copies brought.)
-    if (lane == 0) {
-      const bool of_a = warp == 0;
-      uint32_t stage = 0, phase = 0;
-      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
-      const uint32_t full0_even = map_to_cta(full0, 0u);
-      const uint32_t tx = (p.a_even ? 1u : 2u) * a_stage + 2u * (KIND == P_SUMS ? b_stage / kHalf * (uint32_t)(p.tile_n / 2) : b_stage);
-      const bool idle = of_a && rank != 0 && p.a_even;
-      bool ok = true;
-      for (int u = pair; u < units && ok && !idle; u += pairs) {
-        const Unit w = unit_at<KIND>(p, u, live, plan);
-        const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * (KIND == P_SUMS ? p.tile_n / 2 : kHalf);
-        for (int kb = w.kb0; kb < w.kb1; ++kb) {
-          if (!mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u)) { ok = false; break; }
+    const bool of_a = warp == 0;
+    uint32_t stage = 0, phase = 0;
+    const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+    const uint32_t full0_even = map_to_cta(full0, 0u);
+    const uint32_t tx = (p.a_even ? 1u : 2u) * a_stage + 2u * (KIND == P_SUMS ? b_stage / kHalf * (uint32_t)(p.tile_n / 2) : b_stage);
+    const bool idle = of_a && rank != 0 && p.a_even;
+    bool ok = true;
+    for (int u = pair; u < units && ok && !idle; u += pairs) {
+      const Unit w = unit_at<KIND>(p, u, live, plan);
+      const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * (KIND == P_SUMS ? p.tile_n / 2 : kHalf);
+      for (int kb = w.kb0; kb < w.kb1; ++kb) {
+        ok = __all_sync(0xffffffffu, mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u));
+        if (!ok) break;
+        if (elect_one()) {
           if (of_a && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
           const uint32_t fb = full0_even + 8u * stage;
           const uint32_t to = of_a ? a_tiles + stage * a_stage : b_tiles + stage * b_stage;
@@ -344,13 +360,14 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             if (of_a) tma_load_4d<true>(to, &p.a, fb, 0, kb * kBK, am >> 6, 0);
             else tma_load_4d<true>(to, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
           }
-          if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
         }
+        __syncwarp();
+        if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
       }
     }
   } else if (warp == 1) {
     // ---------------- products (even CTA, for both) ----------------
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       uint32_t stage = 0, phase = 0;
       const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
       constexpr uint32_t a_base = (kTurnedA ? (8192u >> 4) : 1u) << 16, b_base = (kTurnedB ? (8192u >> 4) : 1u) << 16;
@@ -360,44 +377,34 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       bool ok = true;
       for (int u = pair; u < units && ok; u += pairs) {
         const Unit w = unit_at<KIND>(p, u, live, plan);
-        for (int kb0 = w.kb0; kb0 < w.kb1 && ok; kb0 += kPiece, ++j) {
+        const int piece = piece_of<TERMS, KIND>(w);
+        for (int kb0 = w.kb0; kb0 < w.kb1 && ok; kb0 += piece, ++j) {
           const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
-          if (!mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u)) { ok = false; break; }
+          ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u));
+          if (!ok) break;
           tc_fence_after();
           const uint32_t d = tmem_base + set * (uint32_t)kTile;
-          const int kb1 = kb0 + kPiece < w.kb1 ? kb0 + kPiece : w.kb1;
-          // Between the last instruction of a K block and the first of the next the pipe holds one of them: there stand
-          // only a test and a branch.  What frees the block's stage follows the next block's first instruction, and the
-          // next stage's barrier and addresses come before the other three.
-          bool ready = false;
-          uint32_t freed = 0;
-          uint32_t a0 = (a_tiles + stage * a_stage) >> 4 | a_base, b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
+          const int kb1 = kb0 + piece < w.kb1 ? kb0 + piece : w.kb1;
           for (int kb = kb0; kb < kb1; ++kb) {
-            if (!ready && !mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u)) { ok = false; break; }
-            umma_bf16<true>(d, a0, b0, p.idesc, kb > kb0);
-            if (TERMS == 2) {
-              umma_bf16<true>(d, a0, b0 + term, p.idesc, 1u);
-              umma_bf16<true>(d, a0 + term, b0, p.idesc, 1u);
-            }
-            if (freed) umma_commit<true>(freed);
-            freed = empty0 + 8u * stage;
-            if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
-            ready = kb + 1 < kb1 && mbar_test(full0 + 8u * stage, phase);
-            const uint32_t a1 = a0, b1 = b0;
-            a0 = (a_tiles + stage * a_stage) >> 4 | a_base;
-            b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
+            ok = __all_sync(0xffffffffu, mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u));
+            if (!ok) break;
+            const uint32_t a0 = (a_tiles + stage * a_stage) >> 4 | a_base, b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 1; k < kBK / 16; ++k) {
-              const uint32_t a = a1 + (uint32_t)k * a_adv, b = b1 + (uint32_t)k * b_adv;
-              umma_bf16<true>(d, a, b, p.idesc, 1u);
-              if (TERMS == 2) {
-                umma_bf16<true>(d, a, b + term, p.idesc, 1u);
-                umma_bf16<true>(d, a + term, b, p.idesc, 1u);
+              for (int k = 0; k < kBK / 16; ++k) {
+                const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
+                umma_bf16<true>(d, a, b, p.idesc, k > 0 || kb > kb0);
+                if (TERMS == 2) {
+                  umma_bf16<true>(d, a, b + term, p.idesc, 1u);
+                  umma_bf16<true>(d, a + term, b, p.idesc, 1u);
+                }
               }
+              umma_commit<true>(empty0 + 8u * stage);
+              if (kb + 1 == kb1) umma_commit<true>(smem_u32(&acc_full[set]));
             }
+            __syncwarp();
+            if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
           }
-          if (ok) umma_commit<true>(freed);
-          if (ok) umma_commit<true>(smem_u32(&acc_full[set]));
         }
       }
     }
@@ -439,8 +446,9 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const int cols = KIND == P_SUMS ? p.tile_n / 2 : kSumColumns;          // of this warp
       const int col0 = w.n0 + side * cols;
       float acc[kSumColumns];
+      const int piece = piece_of<TERMS, KIND>(w);
 #pragma unroll 1
-      for (int kb0 = w.kb0; kb0 < w.kb1; kb0 += kPiece) {
+      for (int kb0 = w.kb0; kb0 < w.kb1; kb0 += piece) {
         const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
         ++j;
         ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));

@@ -1,5 +1,7 @@
 """What the bindings of the lookup, the vocabulary's loss and the clipping hand to the library and what they refuse, seen
 without a GPU: CPU tensors stand in for CUDA ones, and a recorder stands in for the library."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -91,17 +93,21 @@ def test_loss_copies_a_weight_that_starts_off_its_boundary(recorder, allocations
     assert at % 16 == 0 and reach(V, d.ld_weight, D, 2) <= recorder.room[at]
 
 
-def test_clip_hands_over_what_it_is_given(recorder, allocations):
+def test_clip_hands_over_what_it_is_given(recorder, allocations, monkeypatch):
     g = [on_device(torch.randn(3, 5)), on_device(torch.randn(7).bfloat16()), on_device(torch.randn(0))]
     o = [torch.empty_like(t) for t in g]
+    seen = []
+
+    def clip(n, src, dst, sizes, kinds, most, norm, ws, size, stream):
+        at = lambda kind, address: list((kind * n).from_address(address))
+        seen.append((at(C.c_uint64, src), at(C.c_uint64, dst), at(C.c_int64, sizes), at(C.c_int32, kinds), most, norm))
+        return mwb.MW_OK
+
+    monkeypatch.setattr(recorder, "mw_clip_gradients", clip, raising=False)
     for out in (None, o):
-        recorder.calls.clear()
         norm = mwb.clip_gradients(g, 2.0, out=out)
-        name, (n, src, dst, sizes, kinds, most, at, ws, size, _) = recorder.calls[-1]
-        assert name == "mw_clip_gradients" and n == 3 and most == 2.0 and norm.shape == ()
-        null = lambda p: p or None
-        assert list(src) == [null(t.data_ptr()) for t in g] and list(dst) == [null(t.data_ptr()) for t in out or g]
-        assert list(sizes) == [15, 7, 0] and list(kinds) == [1, 2, 1] and at == norm.data_ptr()
+        assert norm.shape == () and seen.pop() == ([t.data_ptr() for t in g], [t.data_ptr() for t in out or g], [15, 7, 0],
+                                                   [1, 2, 1], 2.0, norm.data_ptr())
 
 
 def refuse(call, kind=ValueError):
