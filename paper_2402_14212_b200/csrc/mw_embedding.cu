@@ -93,12 +93,42 @@ __device__ __forceinline__ void store_vec(T* at, const float (&v)[VEC]) {
 template <typename I>
 __device__ __forceinline__ int row_of(I t, int vocab) { return t >= 0 && t < (I)vocab ? (int)t : vocab; }
 
-// A block takes `rows` whole rows, a thread four pieces of VEC columns at a time, whose loads are all under way
-// before the first store.
+// Rows of 64 accesses and more: a warp takes 256 accesses of a row, eight a lane, whose loads are all under way before
+// the first store.
+constexpr int kLookupAhead = 8;
+template <typename T, typename I, int VEC>
+__global__ void __launch_bounds__(256)
+lookup_kernel(EmbedArgs a, const I* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int segments) {
+  after_previous();
+  using Raw = typename RawOf<T, VEC>::type;
+  const int per = a.dim / VEC, lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = w / segments;
+  if (r >= a.n) return;
+  const int i0 = (int)(w - r * segments) * (32 * kLookupAhead) + lane;
+  const int v = row_of(tokens[r], a.vocab);
+  const T* from = table + v * a.ld_table;
+  T* to = out + r * a.ld_out;
+  Raw x[kLookupAhead];
+#pragma unroll
+  for (int k = 0; k < kLookupAhead; ++k)
+    if (v < a.vocab && i0 + 32 * k < per) x[k] = *reinterpret_cast<const Raw*>(from + (i0 + 32 * k) * VEC);
+#pragma unroll
+  for (int k = 0; k < kLookupAhead; ++k) {
+    float y[VEC];
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) y[q] = 0.f;
+    if (v < a.vocab && i0 + 32 * k < per) widen<T, VEC>(x[k], y);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) y[q] *= a.scale;
+    if (i0 + 32 * k < per) store_vec<T, VEC>(to + (i0 + 32 * k) * VEC, y);
+  }
+}
+
+// Shorter rows: a block takes `rows` of them, a thread four accesses at a time.
 constexpr int kLookupPieces = 4;
 template <typename T, typename I, int VEC>
 __global__ void __launch_bounds__(256)
-lookup_kernel(EmbedArgs a, const I* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int rows) {
+short_lookup_kernel(EmbedArgs a, const I* __restrict__ tokens, const T* __restrict__ table, T* __restrict__ out, int rows) {
   after_previous();
   using Raw = typename RawOf<T, VEC>::type;
   const int per = a.dim / VEC;
@@ -411,10 +441,11 @@ __device__ __forceinline__ void write_sum(G* at, float (&v)[VEC], float scale) {
   }
 }
 
-// A warp sums one piece of the sorted list over 32 VEC columns, eight rows under way at a time.  A run that lies
+// A warp sums one piece of the sorted list over 32 VEC MULT columns, MULT accesses a lane and row, eight rows under way at a
+// time.  A run that lies
 // whole in the piece goes to its row; what a piece holds of a run that came from the piece before goes to its
 // first partial sum, of one that starts here and goes on to its second, and the piece is listed for the join.
-template <typename T, typename G, int VEC, bool ADD, bool GWIDE>
+template <typename T, typename G, int VEC, int MULT, bool ADD, bool GWIDE>
 __global__ void __launch_bounds__(256)
 run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,
                 G* __restrict__ dtable, float* __restrict__ partial, int col_groups, uint32_t* joins) {
@@ -426,8 +457,7 @@ run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* _
   const uint32_t p = (uint32_t)(w / col_groups), i0 = p * kPiece;
   if (i0 >= n) return;
   const int group = (int)(w - (int64_t)p * col_groups);
-  const int c = (group * 32 + lane) * VEC;
-  const bool on = c < a.dim;
+  const int c = (group * MULT * 32 + lane) * VEC;            // and every 32 VEC columns on
   int count = (int)(n - i0 < kPiece ? n - i0 : kPiece);
   const uint32_t my_key = lane < count ? key[i0 + lane] : 0xffffffffu;
   const uint32_t my_pos = lane < count ? pos[i0 + lane] : 0;
@@ -435,18 +465,23 @@ run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* _
   const uint32_t after = i0 + kPiece < n ? key[i0 + kPiece] : 0xffffffffu;
   // tokens that name no row come last
   count = __popc(__ballot_sync(0xffffffffu, my_key < (uint32_t)a.vocab));
-  float acc[VEC];
+  float acc[MULT][VEC];
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
+  for (int m = 0; m < MULT; ++m)
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) acc[m][q] = 0.f;
   bool from_before = __shfl_sync(0xffffffffu, my_key, 0) == before;
   const int width = (a.dim + 3) / 4 * 4;
   for (int b = 0; b < count; b += kAhead) {
     using Raw = typename RawOf<T, VEC>::type;
-    Raw x[kAhead];
+    Raw x[kAhead][MULT];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const uint32_t r = __shfl_sync(0xffffffffu, my_pos, (b + k) & 31);
-      if (on && b + k < count) x[k] = *reinterpret_cast<const Raw*>(dout + r * a.ld_out + c);
+      const T* from = dout + r * a.ld_out + c;
+#pragma unroll
+      for (int m = 0; m < MULT; ++m)
+        if (c + m * 32 * VEC < a.dim && b + k < count) x[k][m] = *reinterpret_cast<const Raw*>(from + m * 32 * VEC);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
@@ -454,23 +489,30 @@ run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* _
       if (i < count) {
         const uint32_t v = __shfl_sync(0xffffffffu, my_key, i & 31);
         const uint32_t next = i == kPiece - 1 ? after : __shfl_sync(0xffffffffu, my_key, (i + 1) & 31);
-        if (on) {
-          float y[VEC];
-          widen<T, VEC>(x[k], y);
 #pragma unroll
-          for (int q = 0; q < VEC; ++q) acc[q] += y[q];
+        for (int m = 0; m < MULT; ++m) {
+          if (c + m * 32 * VEC < a.dim) {
+            float y[VEC];
+            widen<T, VEC>(x[k][m], y);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) acc[m][q] += y[q];
+          }
         }
         if (next != v || i == kPiece - 1) {
           const bool goes_on = next == v;
-          if (on) {
-            if (from_before || goes_on)
-              store_vec<float, VEC>(partial + ((size_t)p * 2 + (from_before ? 0 : 1)) * width + c, acc);
-            else
-              write_sum<G, VEC, ADD, GWIDE>(dtable + v * a.ld_dtable + c, acc, a.scale);
+#pragma unroll
+          for (int m = 0; m < MULT; ++m) {
+            const int at = c + m * 32 * VEC;
+            if (at < a.dim) {
+              if (from_before || goes_on)
+                store_vec<float, VEC>(partial + ((size_t)p * 2 + (from_before ? 0 : 1)) * width + at, acc[m]);
+              else
+                write_sum<G, VEC, ADD, GWIDE>(dtable + v * a.ld_dtable + at, acc[m], a.scale);
+            }
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) acc[m][q] = 0.f;
           }
           if (goes_on && !from_before && group == 0 && lane == 0) joins[1 + atomicAdd(joins, 1u)] = p;
-#pragma unroll
-          for (int q = 0; q < VEC; ++q) acc[q] = 0.f;
           from_before = false;
         }
       }
@@ -593,13 +635,16 @@ mw_status lookup(const mw_embedding_desc* d, const void* tokens, const void* tab
   constexpr int kVec = 16 / sizeof(T);
   const bool wide = wide_rows(table, a.ld_table, a.dim, sizeof(T)) && wide_rows(out, a.ld_out, a.dim, sizeof(T));
   const int per = wide ? a.dim / kVec : a.dim;
-  // 1024 pieces a block (4096 where rows do not come out even); fewer while that leaves multiprocessors idle (one row
-  // of 256 pieces is the least)
-  const int most = 1024 % per == 0 ? 1024 : 4096;
-  int rows = per >= most ? 1 : most / per;
-  while (rows > 1 && rows * per > 256 && ceil_div(a.n, rows) < 148 * 4) rows = (rows + 1) / 2;
-  const unsigned blocks = (unsigned)((a.n + rows - 1) / rows);
-  return launch_after(wide ? lookup_kernel<T, I, kVec> : lookup_kernel<T, I, 1>, blocks, 256, 0, s, a, (const I*)tokens, (const T*)table, (T*)out, rows);
+  const I* t = (const I*)tokens;
+  if (per >= 64) {
+    const int segments = ceil_div(per, 32 * kLookupAhead);
+    return launch_after(wide ? lookup_kernel<T, I, kVec> : lookup_kernel<T, I, 1>, (unsigned)((a.n * segments + 7) / 8), 256, 0, s, a, t,
+                        (const T*)table, (T*)out, segments);
+  }
+  // 1024 accesses a block
+  const int rows = 1024 / per;
+  return launch_after(wide ? short_lookup_kernel<T, I, kVec> : short_lookup_kernel<T, I, 1>, (unsigned)((a.n + rows - 1) / rows), 256, 0, s, a, t,
+                      (const T*)table, (T*)out, rows);
 }
 
 // Clusters of the sort that the device holds at once (asked for once a device; at least two).  Allows its
@@ -628,10 +673,11 @@ mw_status sort_clusters(K kernel, int* out) {
 template <typename T, typename G, int VEC, bool ADD, bool GWIDE>
 mw_status sum_runs(const EmbedArgs& a, const EmbedScratch& l, const uint32_t* key, const uint32_t* pos, const T* dout, G* dtable,
                    cudaStream_t s) {
-  const int groups = ceil_div(a.dim, 32 * VEC);
+  constexpr int kMult = VEC == 1 ? 4 : 1;
+  const int groups = ceil_div(a.dim, 32 * VEC * kMult);
   const int64_t warps = (int64_t)l.pieces * groups;
   if (warps > ((int64_t)1 << 34)) return MW_ERR_UNSUPPORTED;
-  MW_TRY(launch_after(run_sums_kernel<T, G, VEC, ADD, GWIDE>, (unsigned)((warps + 7) / 8), 256, 0, s, a, key, pos, dout, dtable, l.partial, groups, l.joins));
+  MW_TRY(launch_after(run_sums_kernel<T, G, VEC, kMult, ADD, GWIDE>, (unsigned)((warps + 7) / 8), 256, 0, s, a, key, pos, dout, dtable, l.partial, groups, l.joins));
   const int64_t joins = (int64_t)l.pieces * ceil_div(a.dim, kJoinColumns);
   return launch_after(join_runs_kernel<G, ADD>, (unsigned)(joins < 148 * 4 ? joins : 148 * 4), kJoinThreads, 0, s, a, key, l.partial, dtable, l.joins);
 }

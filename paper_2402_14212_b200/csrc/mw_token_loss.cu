@@ -598,7 +598,9 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
                 hand_over(&p.out, at, col0 + c, row0);
               } else {
                 __syncwarp();
-                for (int r = 0; r < 32 && row0 + r < p.vocab; ++r)
+                const int rows = p.vocab - row0 < 32 ? p.vocab - row0 : 32;
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r)
 #pragma unroll
                   for (int x = 0; x < 2; ++x) {
                     const int col = col0 + c + lane + 32 * x;
@@ -628,7 +630,9 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
                 hand_over(&p.out, at, col0 + c, row0);
               } else {
                 __syncwarp();
-                for (int r = 0; r < 32 && row0 + r < p.vocab; ++r) {
+                const int rows = p.vocab - row0 < 32 ? p.vocab - row0 : 32;
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r) {
                   uint32_t v;
                   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at + piece_at((uint32_t)r, (uint32_t)lane >> 2) + ((uint32_t)lane & 3u) * 4u) : "memory");
                   if (col0 + c + lane < p.dim) static_cast<uint32_t*>(p.dw)[(size_t)(row0 + r) * p.ld_dw + col0 + c + lane] = v;
