@@ -10,9 +10,9 @@ namespace mw {
 namespace {
 
 constexpr int kGroup = 256;             // tensors of one launch
-constexpr int kChunkBytes = 32768;      // of a tensor, a block at a time
-constexpr int kClipThreads = 512;
-constexpr int kClipBlocks = 592;        // four a multiprocessor
+constexpr int kChunkBytes = 65536;      // of a tensor, a block at a time
+constexpr int kClipThreads = 1024;
+constexpr int kClipBlocks = 296;        // two a multiprocessor
 constexpr int kAccesses = kChunkBytes / 16 / kClipThreads;      // of 16 bytes, a thread, all under way at once
 
 struct ClipGroup {
