@@ -52,11 +52,12 @@ constexpr int stages_for(int terms, int kind, uint32_t a_stage) {
   const int n = (int)(room / (a_stage + (uint32_t)terms * kPlaneBytes));
   return n < kStagesMax ? n : kStagesMax;
 }
-// K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place; of a sum of one sign 128
-// instructions (logits of bf16 operands), or 96 (two terms), take 2^-17.  dz of bf16 operands has 11 bits: its sums have
-// 512 instructions an accumulator, 2^-15, and are read out a quarter as often (3686 rows of 131072x4096: dh 3.05 ms with
-// 128 instructions).
-__host__ __device__ constexpr int piece_blocks(int terms, int kind) { return terms == 2 ? 8 : (kind == P_DH || kind == P_DW ? 128 : 32); }
+// K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
+// losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and 3.8e-7
+// with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
+// 8.7e-7 (1.10 and 1.12 ms).  dz of bf16 operands has 11 bits: its sums have 512 instructions, 2^-15 at the worst, and
+// are read out seldom.
+__host__ __device__ constexpr int piece_blocks(int terms, int kind) { return terms == 2 ? 4 : (kind == P_DH || kind == P_DW ? 128 : 16); }
 
 // what the kernels of one call share, behind the status block
 struct LossInfo {
@@ -217,15 +218,6 @@ __device__ __forceinline__ void bulk_store_2d(const CUtensorMap* tm, uint32_t sr
                "r"(src), "r"(c0), "r"(c1)
                : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
 }
 __device__ __forceinline__ void tmem_ld32_floats(uint32_t taddr, float* r) {
   asm volatile(
@@ -462,12 +454,12 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           tmem_ld_wait();
         } else {
 #pragma unroll
-          for (int c = 0; c < kSumColumns; c += 16) {
-            uint32_t r[16];
-            tmem_ld16_issue(t0 + (uint32_t)c, r);
+          for (int c = 0; c < kSumColumns; c += 32) {
+            uint32_t r[32];
+            tmem_ld32_issue(t0 + (uint32_t)c, r);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(r[i]);
+            for (int i = 0; i < 32; ++i) acc[c + i] += __uint_as_float(r[i]);
           }
         }
         tc_fence_before();
