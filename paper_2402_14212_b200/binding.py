@@ -1004,6 +1004,9 @@ def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, gra
     known = _passed.get(key)
     if known is None:
         _need(h.is_cuda, "token_loss: CUDA tensors")
+        if _repeats(h) or _repeats(weight):
+            h, weight = _own_memory(h, weight)
+            return _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want)
         _need(h.dim() == 2 and weight.dim() == 2 and h.shape[1] == weight.shape[1] and h.dtype == weight.dtype,
               "token_loss: h is [rows, columns], weight [vocabulary, columns] of the same type")
         _need(tuple(targets.shape) == (h.shape[0],) and targets.is_contiguous(), "token_loss: targets are contiguous, [rows]")
@@ -1027,23 +1030,22 @@ def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, gra
             _check(lib().mw_token_loss_workspace_bytes(d, int(gradient), need), "mw_token_loss_workspace_bytes")
         known = _remember(key, (d, int(need.value), kind))
     d, need, kind = known
-    R = h.shape[0]
-    # the total and the workspace are one allocation with the rows' losses behind the latter
-    loss = torch.empty(R + 1, dtype=torch.float32, device=h.device)
-    ws = torch.empty(need, dtype=torch.uint8, device=h.device)
+    device = h.device
+    loss = torch.empty(h.shape[0], dtype=torch.float32, device=device)
+    total = torch.empty((), dtype=torch.float32, device=device)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
     if not gradient:
-        _check(_call("mw_token_loss_forward", h.device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
-                     _ptr(row_weight), loss.data_ptr(), loss.data_ptr() + 4 * R, ws.data_ptr(), need),
-               "mw_token_loss_forward")
-        return TokenLoss(loss[:R], loss[R])
+        _check(_call("mw_token_loss_forward", device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
+                     _ptr(row_weight), loss.data_ptr(), total.data_ptr(), ws.data_ptr(), need), "mw_token_loss_forward")
+        return TokenLoss(loss, total)
     if dh is None and want[0]:
         dh = _dense_like(h)
     if dweight is None and want[1]:
-        dweight = torch.empty(weight.shape, dtype=kind, device=h.device)
-    _check(_call("mw_token_loss_gradient", h.device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
-                 _ptr(row_weight), loss.data_ptr(), loss.data_ptr() + 4 * R, _ptr(dh), _ptr(dweight), ws.data_ptr(),
-                 need), "mw_token_loss_gradient")
-    return TokenLoss(loss[:R], loss[R], dh, dweight)
+        dweight = torch.empty(weight.shape, dtype=kind, device=device)
+    _check(_call("mw_token_loss_gradient", device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
+                 _ptr(row_weight), loss.data_ptr(), total.data_ptr(), _ptr(dh), _ptr(dweight), ws.data_ptr(), need),
+           "mw_token_loss_gradient")
+    return TokenLoss(loss, total, dh, dweight)
 
 
 def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=None) -> TokenLoss:
@@ -1055,7 +1057,6 @@ def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=N
     import torch
     if stream is not None:
         return _on_stream(stream, h, token_loss, h, weight, targets, scale, row_weight)
-    h, weight = _own_memory(h, weight)
     if weight.data_ptr() & 15:         # (read in place, by copies of 16 bytes)
         weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(False, h, weight, targets, scale, row_weight, 0, None, None, None, (False, False))
@@ -1070,7 +1071,6 @@ def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None,
     if stream is not None:
         return _on_stream(stream, h, token_loss_gradient, h, weight, targets, scale, row_weight, dh, dweight, grad_dtype,
                           want, piece_rows)
-    h, weight = _own_memory(h, weight)
     return _token_loss(True, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight,
                        (bool(want[0]), bool(want[1])))
 

@@ -44,14 +44,21 @@ constexpr uint64_t kLossWaitNs = 2000000000ull;
 enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
 // Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
 // few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
-__host__ __device__ constexpr int buffer_count(int terms, int kind) { return kind == P_SUMS ? 0 : 1; }
 constexpr int kStagesMax = 12;
 constexpr size_t kSmemMost = 225 * 1024;
-constexpr int stages_for(int terms, int kind, uint32_t a_stage) {
-  const size_t room = kSmemMost - 1024 - (size_t)kEpi * buffer_count(terms, kind) * kBufferBytes;
+constexpr int stages_for(int terms, int buffers, uint32_t a_stage) {
+  const size_t room = kSmemMost - 1024 - (size_t)kEpi * buffers * kBufferBytes;
   const int n = (int)(room / (a_stage + (uint32_t)terms * kPlaneBytes));
   return n < kStagesMax ? n : kStagesMax;
 }
+// Buffers of an epilogue warp: one, which leaves the most stages, unless a tile has so few K blocks that its way out is
+// what takes the time.
+constexpr int buffers_for(int terms, int kind, int blocks_k) {
+  if (kind == P_SUMS) return 0;
+  if (kind == P_DH || blocks_k > 16) return 1;
+  return terms == 1 && blocks_k <= 8 ? 4 : 2;
+}
+
 // K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
 // losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and 3.8e-7
 // with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
@@ -65,9 +72,9 @@ struct LossInfo {
   unsigned pad[59];
   int live;                 // rows that are not left out
   unsigned g_max;           // bits of the largest |g|
-  unsigned h_max[2], w_max[2];    // bits of the largest finite |h|, |W|: of a sample of the rows, and of all
+  unsigned h_max, w_max;    // bits of the largest finite |h|, |W|
   unsigned done;            // blocks whose losses are in
-  unsigned pad2[57];
+  unsigned pad2[59];
 };
 
 // the power of two that brings numbers of at most this size to 2^13 .. 2^14
@@ -77,17 +84,16 @@ __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   const int x = 13 - e;
   return x < -100 ? -100 : (x > 100 ? 100 : x);
 }
-// ... of a large operand, whose size is known from a sample of its rows when it is written: room for numbers 16 times
-// as large as the sample's.  Where the largest of all turn out to lie elsewhere, too large or so small
-// that the lower terms would suffer, the operand is written again by what they are.
-constexpr int kSampleRoom = 4;
-__device__ __forceinline__ int sample_exponent(unsigned sample) { return range_exponent(sample) - (sample ? kSampleRoom : 0); }
-__device__ __forceinline__ bool sample_misses(const unsigned (&most)[2]) {
-  const int e = (int)(most[1] >> 23) - 127 + sample_exponent(most[0]);
-  return most[1] != 0 && (e > 14 || e < 13 - 2 * kSampleRoom);
+// ... of an operand whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up to 2^7, 2^-9),
+// which is written while it is looked at; where the largest lies elsewhere it is written again.  What is lost then
+// lies below 2^-30 for bf16, whose 8 bits fit (2^-33 for the second of two terms).
+__host__ __device__ constexpr int usual_exponent(int terms) { return terms == 1 ? 6 : 8; }
+__device__ __forceinline__ bool unusual(unsigned most, int terms) {
+  const int e = (int)(most >> 23) - 127 + usual_exponent(terms);
+  return most != 0 && (e > 14 || e < -2);
 }
-__device__ __forceinline__ int operand_exponent(const unsigned (&most)[2], bool sampled) {
-  return !sampled ? range_exponent(most[0]) : (sample_misses(most) ? range_exponent(most[1]) : sample_exponent(most[0]));
+__device__ __forceinline__ int operand_exponent(unsigned most, int terms) {
+  return unusual(most, terms) ? range_exponent(most) : usual_exponent(terms);
 }
 
 struct LossArgs {
@@ -96,7 +102,6 @@ struct LossArgs {
   int64_t ld_h, ld_w, ld_dh, ld_dw;
   float scale;
   int scaled;               // operands were multiplied by powers of two
-  int sampled_h, sampled_w;
 };
 
 struct alignas(64) ProductArgs {
@@ -110,7 +115,8 @@ struct alignas(64) ProductArgs {
   int pairs;                // CTA pairs that the device holds
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
-  int stages;
+  int stages, buffers;
+  int shares;               // P_DW: of K, where the tiles are few (their sums then lie in blocks, as dh's)
   int tile_n;               // columns of a tile: 256, fewer for few rows of the loss alone
   int direct;               // few rows of the loss alone: h as it is, rows that are left out among the others
   LossInfo* clear;          // ... and what the other kernels share is cleared here
@@ -119,7 +125,7 @@ struct alignas(64) ProductArgs {
   uint32_t a_stage;         // bytes of A in a stage of a CTA
   int a_even;               // A's copies are the even CTA's alone: its rows hold all there are
   float scale;
-  int scaled, sampled_h, sampled_w;
+  int scaled;
   float2* sums;             // [row][sum_blocks]: power, sum
   float* target_z;
   const int* target;
@@ -162,7 +168,7 @@ __device__ __forceinline__ int live_rows(const ProductArgs& p) {
 }
 template <int KIND>
 __device__ __forceinline__ int unit_count(const ProductArgs& p, int live, const DhPlan& plan) {
-  if (KIND == P_DW) return live > 0 || p.first == 0 ? p.tiles_m * p.tiles_n : 0;
+  if (KIND == P_DW) return live > 0 || p.first == 0 ? p.tiles_m * p.tiles_n * p.shares : 0;
   if (KIND == P_DH) return plan.whole + plan.rest * plan.shares;
   return (live + kTile - 1) / kTile * p.tiles_n;
 }
@@ -194,10 +200,13 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live, c
     w.kb0 = share * per;
     w.kb1 = w.kb0 + per < p.blocks_k ? w.kb0 + per : p.blocks_k;
   } else {
-    w.m0 = u / p.tiles_n * kTile;
-    w.n0 = u % p.tiles_n * kTile;
-    w.kb0 = 0;
-    w.kb1 = (live + kBK - 1) / kBK;
+    const int tiles = p.tiles_m * p.tiles_n, share = u / tiles, tile = u - share * tiles;
+    const int blocks = (live + kBK - 1) / kBK, per = (blocks + p.shares - 1) / p.shares;
+    if (p.shares > 1) w.share = tile * p.shares + share;
+    w.m0 = tile / p.tiles_n * kTile;
+    w.n0 = tile % p.tiles_n * kTile;
+    w.kb0 = share * per;
+    w.kb1 = w.kb0 + per < blocks ? w.kb0 + per : blocks;
   }
   return w;
 }
@@ -267,7 +276,6 @@ template <int TERMS, int KIND>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr int kBuffers = buffer_count(TERMS, KIND);
   constexpr uint32_t b_stage = TERMS * kPlaneBytes;
   __shared__ __align__(8) uint64_t full_bar[kStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
@@ -406,25 +414,30 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     // A lane has a row of 32 and a warp half the tile's columns, all of them in registers: an accumulator is handed
     // back as soon as it has been read.
     const int ew = warp - kFirstEpi, quarter = warp & 3, side = ew >> 2;
-    const uint32_t sbuf = b_tiles + (uint32_t)stages * b_stage + (uint32_t)ew * (kBuffers * kBufferBytes);
+    const int buffers = p.buffers;
+    const uint32_t sbuf = b_tiles + (uint32_t)stages * b_stage + (uint32_t)(ew * buffers) * kBufferBytes;
     uint32_t turn = 0;
     int j = 0;
     bool ok = true;
-    const int exps = p.scaled ? operand_exponent(p.info->h_max, p.sampled_h) : 0;
-    const int expw = p.scaled ? operand_exponent(p.info->w_max, p.sampled_w) : 0;
+    const int exps = p.scaled ? operand_exponent(p.info->h_max, TERMS) : 0;
+    const int expw = p.scaled ? operand_exponent(p.info->w_max, TERMS) : 0;
     const int expz = range_exponent(p.info->g_max);
-    const float factor = KIND == P_DH ? 1.f
-                         : KIND == P_DW ? (float)ldexp((double)p.scale, -(expz + exps))
-                                        : (float)ldexp((double)p.scale * 1.4426950408889634, -(exps + expw));
+    float factor = 1.f;
+    if (KIND == P_DW) factor = (float)ldexp((double)p.scale, -(expz + exps));
+    if (KIND == P_SUMS || KIND == P_EXP) {
+      factor = (float)ldexp((double)p.scale * 1.4426950408889634, -(exps + expw));
+      if (factor == 0.f) factor = 1e-30f;           // (a sign, for what takes a term out of the sum)
+    }
     // a block of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the next buffer
     auto next_buffer = [&]() -> uint32_t {
       if (lane == 0) {
-        if (kBuffers == 2) bulk_wait_read_but_one();
+        if (buffers == 4) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
+        else if (buffers == 2) bulk_wait_read_but_one();
         else bulk_wait_read_all();
       }
       __syncwarp();
-      const uint32_t at = sbuf + (kBuffers == 2 ? turn * kBufferBytes : 0u);
-      turn ^= 1u;
+      const uint32_t at = sbuf + turn * kBufferBytes;
+      if (++turn == (uint32_t)buffers) turn = 0;
       return at;
     };
     auto hand_over = [&](const CUtensorMap* map, uint32_t at, int col, int row) {
@@ -439,6 +452,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const int col0 = w.n0 + side * cols;
       float acc[kSumColumns];
       const int piece = piece_of<TERMS, KIND>(w);
+      // of few rows most warps have none: they only hand the accumulators back
+      const bool idle = KIND != P_DW && row0 >= live;
 #pragma unroll 1
       for (int kb0 = w.kb0; kb0 < w.kb1; kb0 += piece) {
         const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
@@ -449,10 +464,12 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kTile + (uint32_t)(side * cols);
         if (kb0 == w.kb0) {
           // the first piece goes where the sum is to be
+          if (!idle) {
 #pragma unroll
-          for (int c = 0; c < kSumColumns; c += 32) tmem_ld32_floats(t0 + (uint32_t)c, acc + c);
+            for (int c = 0; c < kSumColumns; c += 32) tmem_ld32_floats(t0 + (uint32_t)c, acc + c);
+          }
           tmem_ld_wait();
-        } else {
+        } else if (!idle) {
 #pragma unroll
           for (int c = 0; c < kSumColumns; c += 32) {
             uint32_t r[32];
@@ -470,6 +487,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         }
       }
       if (!ok) break;
+      if (idle) continue;
       if (w.kb0 >= w.kb1) {
 #pragma unroll
         for (int i = 0; i < kSumColumns; ++i) acc[i] = 0.f;
@@ -499,24 +517,32 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
               t = p.target[p.first + row] - col0;
             }
           }
-          if (__any_sync(0xffffffffu, t >= 0 && t < valid)) {
-            float zt = 0.f;
-#pragma unroll
-            for (int i = 0; i < kSumColumns; ++i) zt = i == t ? acc[i] : zt;
-            if (t >= 0 && t < valid) p.target_z[p.first + row] = zt * factor;
-          }
+          const bool here = t >= 0 && t < valid;
           // (a row of nothing but -inf here, or with an infinity, keeps its values as they are)
-          const float k = fabsf(m) < 1e30f ? ceilf(m) - 15.f : -15.f;
-          float sum = 0.f;
+          const float power = fabsf(m) < 1e30f ? ceilf(m) : 0.f;
+          // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row that is
+          // sure of it is what the others' terms add to one, with no difference of two logits in it
+          if (__any_sync(0xffffffffu, here)) {
+            float zt = 0.f;
+            const float gone = factor > 0.f ? -INFINITY : INFINITY;
 #pragma unroll
-          for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, -k));
+            for (int i = 0; i < kSumColumns; ++i) {
+              zt = i == t ? acc[i] : zt;
+              acc[i] = i == t ? gone : acc[i];
+            }
+            if (here) p.target_z[p.first + row] = fmaf(zt, factor, -power);
+          }
+          float sum = 0.f;
+          const float shift = 15.f - power;
+#pragma unroll
+          for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, shift));
           if (!whole) {
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) acc[i] = i < valid ? acc[i] : 0.f;
           }
 #pragma unroll
           for (int i = 0; i < kSumColumns; ++i) sum += acc[i];
-          if (on) p.sums[(size_t)row * p.sum_blocks + col0 / cols] = make_float2(k, sum);
+          if (on) p.sums[(size_t)row * p.sum_blocks + col0 / cols] = make_float2(power, sum);
           if (KIND == P_EXP) {
             constexpr int kCols = TERMS == 1 ? 64 : 32;
 #pragma unroll
@@ -541,7 +567,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             }
           }
         }
-      } else if (KIND == P_DH) {
+      } else if (KIND == P_DH || w.share >= 0) {
 #pragma unroll
         for (int c = 0; c < kSumColumns; c += 32) {
           if (col0 + c < p.dim) {
@@ -773,39 +799,11 @@ struct Operand {
   const int *row, *count;         // null: all rows
   int64_t rows, staged_rows;
   unsigned* most;                 // LossInfo::h_max or w_max
-  int sampled;                    // one row in kSampleRows was looked at
   unsigned short* out;
   T* dead;                        // rows of dh that get zeros
   int64_t ld_dead;
 };
-constexpr int kSampleRows = 16;
-// operands of more than this are sampled: looking at all of a smaller one costs less than the launch that writes
-// an operand again
-constexpr int64_t kSampledBytes = (int64_t)32 << 20;
-
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(256) largest_kernel(Operand<T> w, Operand<T> h, int dim, int64_t w_blocks) {
-  after_previous();
-  const bool of_w = blockIdx.x < w_blocks;
-  const Operand<T>& o = of_w ? w : h;
-  const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
-  const int64_t n = o.count ? *o.count : o.rows;
-  const uint32_t per = (uint32_t)(dim + 7) / 8, step = o.sampled ? kSampleRows : 1;
-  const int64_t items = (n + step - 1) / step * per;
-  const bool small = items < 0x7fffffff;           // (divisions in 32 bits)
-  unsigned m = 0;
-#pragma unroll 2
-  for (int64_t i = block * 256 + threadIdx.x; i < items; i += blocks * 256) {
-    const int64_t row = small ? (uint32_t)i / per : i / per, r = row * step;
-    float v[8];
-    load8<T, WIDE>(o.x + (o.row ? (int64_t)o.row[r] : r) * o.ld, (int)(i - row * per) * 8, dim, v);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) m = max(m, finite_bits(v[k]));
-  }
-  block_largest(m, o.most);
-}
-
-// AGAIN: only what the sample misjudged.  SCALED false: bf16 as it is.
+// AGAIN: only what is of an unusual size.  SCALED false: bf16 as it is.
 template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
 __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, int dim, int padded, int64_t w_blocks) {
   after_previous();
@@ -814,9 +812,12 @@ __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, 
   const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
   int e = 0;
   if (SCALED) {
-    const unsigned most[2] = {o.most[0], AGAIN ? o.most[1] : 0u};
-    if (AGAIN && (!o.sampled || !sample_misses(most))) return;
-    e = AGAIN ? range_exponent(most[1]) : (o.sampled ? sample_exponent(most[0]) : range_exponent(most[0]));
+    e = usual_exponent(TERMS);
+    if (AGAIN) {
+      const unsigned most = *o.most;
+      if (!unusual(most, TERMS)) return;
+      e = range_exponent(most);
+    }
   }
   const float f = __uint_as_float((unsigned)(127 + e) << 23);
   const int64_t n = o.count ? *o.count : o.rows;
@@ -866,7 +867,7 @@ __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, 
     if (!AGAIN && o.dead && r >= n && r < o.rows)
       for (int k = 0; k < 8 && c + k < dim; ++k) o.dead[at * o.ld_dead + c + k] = from_f64<T>(0.0);
   }
-  if (SCALED && !AGAIN && o.sampled) block_largest(m, o.most + 1);
+  if (SCALED && !AGAIN) block_largest(m, o.most);
 }
 
 // joins the sums of a row's blocks: log2 of the whole sum
@@ -886,10 +887,19 @@ __device__ __forceinline__ RowSum warp_join(RowSum v) {
 }
 // k of a block whose row is empty so far: small, and its difference to any k is finite
 constexpr float kNoPower = -3e38f;
-__device__ __forceinline__ float loss_of(RowSum v, float zt) {
-  // (the sum holds the target's own term, so what rounding leaves below zero is zero; NaN stays)
-  const float l = 0.69314718055994531f * ((v.k - zt) + log2f(v.sum));
-  return l < 0.f ? 0.f : l;
+// What a row's sums say: `v` of all terms but the target's (times 2^15, relative to 2^v.k), the target's logit relative
+// to its own block's power.  odds: log2 of the others' terms over the target's.
+struct RowEnd {
+  float loss, total, less;      // the loss, all terms as v.sum holds them, 1 - p of the target
+};
+__device__ __forceinline__ RowEnd row_end(RowSum v, float target_z, float target_power) {
+  RowEnd e;
+  const float odds = (v.k - target_power) + log2f(v.sum * 0x1p-15f) - target_z, r = exp2f(odds);
+  const bool far = odds > 24.f;
+  e.loss = far ? 0.69314718055994531f * odds : log1pf(r);
+  e.less = far ? 1.f : r / (1.f + r);
+  e.total = v.sum + exp2f((target_power - v.k) + 15.f + target_z);
+  return e;
 }
 
 // The last block of the launch that brings the last losses adds them up, in an order that the rows' number alone sets.
@@ -921,7 +931,7 @@ __device__ __forceinline__ void total_by_last(LossInfo* info, int n, const doubl
 
 // losses of all live rows, a warp each
 __global__ void __launch_bounds__(256)
-loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const int* row, const float* g,
+loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const int* row, const int* target, const float* g,
                  float* loss, double* part, float* total) {
   after_previous();
   const int lane = threadIdx.x & 31;
@@ -936,7 +946,7 @@ loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float
     }
     v = warp_join(v);
     if (lane == 0) {
-      const float l = loss_of(v, target_z[i]);
+      const float l = row_end(v, target_z[i], sums[i * sum_blocks + target[i] / kSumColumns].x).loss;
       loss[row[i]] = l;
       part[i] = (double)g[i] * (double)l;
     }
@@ -947,7 +957,7 @@ loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float
 // The same of at most 256 rows that were taken as they are: those left out are found here.
 template <typename I>
 __global__ void __launch_bounds__(256)
-direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float* target_z, const I* targets, const float* weight, int rows,
+direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, int columns, const float* target_z, const I* targets, const float* weight, int rows,
                    int vocab, float* loss, double* part, float* total) {
   after_previous();
   const int lane = threadIdx.x & 31, mine = threadIdx.x;
@@ -965,7 +975,7 @@ direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const flo
     }
     v = warp_join(v);
     if (lane == 0) {
-      const float l = on ? loss_of(v, target_z[i]) : 0.f;
+      const float l = on ? row_end(v, target_z[i], sums[(size_t)i * sum_blocks + (int)targets[i] / columns].x).loss : 0.f;
       loss[i] = l;
       part[i] = on ? (double)(weight ? weight[i] : 1.f / (float)live) * (double)l : 0.0;
     }
@@ -973,49 +983,52 @@ direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const flo
   total_by_last(info, rows, part, total);
 }
 
-// a row's exponentials -> dz times a power of two, in their place: a block a row
-template <int TERMS>
+// a row's exponentials -> dz times a power of two, in their place: WARPS warps of a block of eight a row
+template <int TERMS, int WARPS>
 __global__ void __launch_bounds__(256)
 dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
-          const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int vocab, int padded) {
+          const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int padded) {
   after_previous();
   __shared__ RowSum warp_v[8];
+  constexpr int kThreads = WARPS * 32, kRows = 8 / WARPS;
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
   const int upto = (live + kBK - 1) / kBK * kBK;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = WARPS == 1 ? 0 : (int)(threadIdx.x >> 5), lane = threadIdx.x & 31, thread = (int)threadIdx.x % kThreads;
   const float to_range = __uint_as_float((unsigned)(127 + range_exponent(info->g_max)) << 23);
-  for (int r = blockIdx.x; r < upto; r += gridDim.x) {
+  for (int r = (int)blockIdx.x * kRows + (WARPS == 1 ? (int)(threadIdx.x >> 5) : 0); r < upto; r += gridDim.x * kRows) {
     unsigned short* at = e + (size_t)r * padded * TERMS;
     if (r >= live) {                                  // rows that fill up the last block of K
-      for (int c = threadIdx.x; c < padded * TERMS / 8; c += 256) reinterpret_cast<uint4*>(at)[c] = make_uint4(0u, 0u, 0u, 0u);
+      for (int c = thread; c < padded * TERMS / 8; c += kThreads) reinterpret_cast<uint4*>(at)[c] = make_uint4(0u, 0u, 0u, 0u);
       continue;
     }
     const float2* mine = sums + (size_t)r * sum_blocks;
-    RowSum v = {kNoPower, 0.f};
-    for (int b = threadIdx.x; b < sum_blocks; b += 256) v = join(v, {mine[b].x, mine[b].y});
-    v = warp_join(v);
-    __syncthreads();
-    if (lane == 0) warp_v[warp] = v;
-    __syncthreads();
-    v = warp_v[0];
-    for (int w = 1; w < 8; ++w) v = join(v, warp_v[w]);
     const int i = first + r, t = target[i];
-    const float l = loss_of(v, target_z[i]);
-    if (threadIdx.x == 0) {
-      loss[row[i]] = l;
-      part[i] = (double)g[i] * (double)l;
+    RowSum v = {kNoPower, 0.f};
+    for (int b = thread; b < sum_blocks; b += kThreads) v = join(v, {mine[b].x, mine[b].y});
+    v = warp_join(v);
+    if (WARPS > 1) {
+      __syncthreads();
+      if (lane == 0) warp_v[warp] = v;
+      __syncthreads();
+      v = warp_v[0];
+      for (int w = 1; w < WARPS; ++w) v = join(v, warp_v[w]);
     }
-    const float gi = g[i] * to_range, at_target = gi * expm1f(-l), share = gi / v.sum;
+    const RowEnd end = row_end(v, target_z[i], mine[t / kSumColumns].x);
+    if (thread == 0) {
+      loss[row[i]] = end.loss;
+      part[i] = (double)g[i] * (double)end.loss;
+    }
+    const float gi = g[i] * to_range, at_target = -gi * end.less, share = gi / end.total;
     // (four accesses of a thread under way)
     constexpr int kAhead = 4;
     if (TERMS == 1) {
-      for (int c0 = threadIdx.x * 8; c0 < padded; c0 += 256 * 8 * kAhead) {
+      for (int c0 = thread * 8; c0 < padded; c0 += kThreads * 8 * kAhead) {
         uint4 raw[kAhead];
         float f[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          const int c = c0 + j * 256 * 8;
+          const int c = c0 + j * kThreads * 8;
           if (c < padded) {
             raw[j] = *reinterpret_cast<const uint4*>(at + c);
             f[j] = mine[c / kSumColumns].x;
@@ -1023,7 +1036,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          const int c = c0 + j * 256 * 8;
+          const int c = c0 + j * kThreads * 8;
           if (c < padded) {
             const float by = share * exp2_fast(f[j] - v.k);
             const uint32_t in[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
@@ -1047,12 +1060,12 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       }
     } else {
       // a group of 64 floats becomes 64 leading terms and 64 remainders: sixteen lanes, four of them each
-      for (int c0 = warp * 128 + lane * 4; c0 - lane * 4 < padded; c0 += 8 * 128 * kAhead) {          // (a warp together)
+      for (int c0 = warp * 128 + lane * 4; c0 - lane * 4 < padded; c0 += WARPS * 128 * kAhead) {          // (a warp together)
         float4 raw[kAhead];
         float f[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          const int c = c0 + j * 8 * 128;
+          const int c = c0 + j * WARPS * 128;
           if (c < padded) {
             raw[j] = *reinterpret_cast<const float4*>(at + 2 * c);
             f[j] = mine[c / kSumColumns].x;
@@ -1061,7 +1074,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          const int c = c0 + j * 8 * 128;
+          const int c = c0 + j * WARPS * 128;
           if (c < padded) {
             const float by = share * exp2_fast(f[j] - v.k);
             float x[4] = {raw[j].x * by, raw[j].y * by, raw[j].z * by, raw[j].w * by};
@@ -1092,7 +1105,7 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
   after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
-  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, a.sampled_w)));
+  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, terms)));
   const DhPlan plan = dh_plan(live, tiles_n, blocks_k, pairs, terms);
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)live * per;
@@ -1118,6 +1131,45 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (c + k < a.dim) put(to + k, x[k]);
+    }
+  }
+}
+
+// dW of few tiles: the sums over the shares of K, in order, and over the pieces before, four columns a thread
+template <typename G>
+__global__ void __launch_bounds__(256)
+dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int terms, int first, int piece, const LossInfo* info, float* partial,
+               int padded, G* dw) {
+  after_previous();
+  const int live = info->live;
+  if (first > 0 && live <= first) return;
+  const bool last = first + piece >= live;
+  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->h_max, terms)));
+  const uint32_t per = (uint32_t)(a.dim + 3) / 4;
+  const int64_t items = (int64_t)a.vocab * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
+    const int64_t v = i / per;
+    const int c = (int)(i - v * per) * 4;
+    const int tile = (int)(v / kTile) * tiles_n + c / kTile;
+    const float* from = blocks + ((size_t)tile * shares * kTile + v % kTile) * kTile + c % kTile;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < shares; ++s, from += kTile * kTile) {
+      const float4 y = *reinterpret_cast<const float4*>(from);
+      x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+    }
+    x.x *= f; x.y *= f; x.z *= f; x.w *= f;
+    float4* held = reinterpret_cast<float4*>(partial + (size_t)v * padded + c);
+    if (first > 0) {
+      const float4 y = *held;
+      x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+    }
+    if (!last) {
+      *held = x;
+    } else {
+      const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < a.dim) put(dw + v * a.ld_dw + c + k, y[k]);
     }
   }
 }
@@ -1240,7 +1292,8 @@ mw_status out_map(CUtensorMap* out, CUtensorMapDataType type, int size, const vo
 template <int TERMS, int KIND>
 mw_status run_product(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   if (KIND == P_DH || KIND == P_DW) p.a_stage = TERMS * kPlaneBytes;
-  p.stages = stages_for(TERMS, KIND, p.a_stage);
+  p.buffers = buffers_for(TERMS, KIND, p.blocks_k);
+  p.stages = stages_for(TERMS, p.buffers, p.a_stage);
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
   auto kernel = loss_products_kernel<TERMS, KIND>;
@@ -1288,8 +1341,6 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   // bf16 operands of the loss alone are taken as they are
   const bool scaled = TERMS == 2 || gradient;
   a.scaled = scaled;
-  a.sampled_h = scaled && a.rows * a.dim * (int64_t)sizeof(T) > kSampledBytes;
-  a.sampled_w = scaled && (int64_t)a.vocab * a.dim * (int64_t)sizeof(T) > kSampledBytes;
   const unsigned wide = 148 * 8;
   // few rows of the loss alone: no row is moved where the copy engine can read h as it lies
   const bool direct = l.in_place && a.rows > 0 && a.rows <= kTile && a.ld_h % 8 == 0 && ((uintptr_t)h & 15) == 0;
@@ -1298,8 +1349,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     int* counts = l.blocks > 1 ? l.counts : nullptr;
     if (counts) MW_TRY(launch_after(count_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts));
     MW_TRY(launch_after(index_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts, l.blocks, l.row, l.target, l.g, loss, l.info));
-    Operand<T> oh = {h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, l.info->h_max, a.sampled_h, l.h, dh, a.ld_dh};
-    Operand<T> ow = {w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, l.info->w_max, a.sampled_w, l.w, nullptr, 0};
+    Operand<T> oh = {h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, &l.info->h_max, l.h, dh, a.ld_dh};
+    Operand<T> ow = {w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, &l.info->w_max, l.w, nullptr, 0};
     if (l.in_place) ow.rows = ow.staged_rows = 0;
     auto aligned = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
     const bool rows16 = aligned(h, a.ld_h) && aligned(w, a.ld_w) && a.dim * (int64_t)sizeof(T) % 16 == 0;
@@ -1311,9 +1362,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     const int64_t bw = blocks_for(ow.rows), bh = blocks_for(a.rows + kTile);
     auto stage = [&](auto kernel) { return launch_after(kernel, (unsigned)(bw + bh), 256, 0, s, ow, oh, a.dim, l.padded, bw); };
     if (scaled) {
-      MW_TRY(launch_after(rows16 ? largest_kernel<T, true> : largest_kernel<T, false>, (unsigned)(bw + bh), 256, 0, s, ow, oh, a.dim, bw));
       MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, false> : stage_kernel<T, TERMS, true, false, false>));
-      if (a.sampled_h || a.sampled_w) MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>));
+      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>));
     } else {
       MW_TRY(stage(rows16 ? stage_kernel<T, 1, false, true, false> : stage_kernel<T, 1, false, false, false>));
     }
@@ -1326,11 +1376,12 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     p.info = l.info;
     p.st = &l.info->st;
     p.vocab = a.vocab; p.dim = a.dim;
-    p.scale = a.scale; p.scaled = scaled; p.sampled_h = a.sampled_h; p.sampled_w = a.sampled_w;
+    p.scale = a.scale; p.scaled = scaled;
     p.piece = l.piece;
     p.sum_blocks = l.sum_blocks;
     p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
     p.pairs = sm_count() / 2;
+    p.shares = 1;
     p.tile_n = kTile;
     ProductArgs logits = p, by_h = p, by_w = p;
     logits.direct = direct;
@@ -1366,15 +1417,23 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       // dW: K across the rows of both
       by_w.tiles_m = ceil_div(a.vocab, kTile);
       by_w.tiles_n = ceil_div(a.dim, kTile);
+      by_w.blocks_k = ceil_div(l.piece, kBK);
       by_w.idesc = instruction(false, true, true);
       MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, TERMS, kBK, 2));
       MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
+      // tiles for less than half of the pairs: each in shares of K, of eight blocks at least
+      const int tiles = by_w.tiles_m * by_w.tiles_n;
+      if (2 * tiles <= p.pairs && by_w.blocks_k >= 16) {
+        by_w.shares = p.pairs / tiles < by_w.blocks_k / 8 ? p.pairs / tiles : by_w.blocks_k / 8;
+        by_w.out = by_h.acc;
+        by_w.acc = by_h.acc;
+      }
       by_w.dw = dw; by_w.ld_dw = a.ld_dw; by_w.dw_bf16 = dw_bf16;
-      by_w.dw_engine = ((uintptr_t)dw & 15) == 0 && (a.ld_dw * dw_size) % 16 == 0;
+      by_w.dw_engine = by_w.shares == 1 && ((uintptr_t)dw & 15) == 0 && (a.ld_dw * dw_size) % 16 == 0;
       if (by_w.dw_engine && dw)
         MW_TRY(out_map(&by_w.out, dw_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, dw_size, dw, a.dim, a.vocab, a.ld_dw));
       by_w.partial = l.dw; by_w.ld_partial = l.padded;
-      if (l.piece < a.rows) MW_TRY(out_map(&by_w.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.dw, l.padded, a.vocab, l.padded));
+      if (l.piece < a.rows && by_w.shares == 1) MW_TRY(out_map(&by_w.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.dw, l.padded, a.vocab, l.padded));
     }
     const int64_t tm = ceil_div(l.piece, kTile);
     for (int64_t first = 0; first < (a.rows > 0 ? a.rows : 1); first += l.piece) {
@@ -1382,17 +1441,22 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       if (a.rows > 0) {
         if (gradient) {
           MW_TRY((run_product<TERMS, P_EXP>(logits, tm * logits.tiles_n, s)));
-          MW_TRY(launch_after(dz_kernel<TERMS>, (unsigned)(l.piece_rows < (int)wide ? l.piece_rows : wide), 256, 0, s, l.info, (int)first, l.piece,
-                              l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part, first + l.piece >= a.rows ? total : nullptr, l.e,
-                              a.vocab, l.vpadded));
+          // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of them waits of
+          // one row after another)
+          const bool short_rows = a.vocab <= 4096;
+          const int dz_blocks = short_rows ? ceil_div(l.piece_rows, 8) : l.piece_rows;
+          MW_TRY(launch_after(short_rows ? dz_kernel<TERMS, 1> : dz_kernel<TERMS, 8>, (unsigned)(dz_blocks < (int)wide ? dz_blocks : wide), 256, 0, s,
+                              l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part,
+                              first + l.piece >= a.rows ? total : nullptr, l.e, l.vpadded));
         } else {
           MW_TRY((run_product<TERMS, P_SUMS>(logits, tm * logits.tiles_n, s)));
           const unsigned blocks = (unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide);          // (a warp a row)
           if (direct)
-            MW_TRY(launch_after(direct_rows_kernel<I>, blocks, 256, 0, s, l.info, l.sums, logits.sum_blocks, l.target_z, targets, weight, (int)a.rows,
+            MW_TRY(launch_after(direct_rows_kernel<I>, blocks, 256, 0, s, l.info, l.sums, logits.sum_blocks, logits.tile_n / 2, l.target_z, targets, weight, (int)a.rows,
                                 a.vocab, loss, l.part, total));
           else
-            MW_TRY(launch_after(loss_rows_kernel, blocks, 256, 0, s, l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.g, loss, l.part, total));
+            MW_TRY(launch_after(loss_rows_kernel, blocks, 256, 0, s, l.info, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part,
+                                total));
         }
         if (dh) {
           MW_TRY((run_product<TERMS, P_DH>(by_h, p.pairs, s)));
@@ -1401,7 +1465,17 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
                               l.row, l.info, dh));
         }
       }
-      if (dw) MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n, s)));
+      if (dw) {
+        MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n * by_w.shares, s)));
+        if (by_w.shares > 1) {
+          if (dw_bf16)
+            MW_TRY(launch_after(dw_rows_kernel<__nv_bfloat16>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, TERMS, (int)first, l.piece,
+                                l.info, l.dw, l.padded, (__nv_bfloat16*)dw));
+          else
+            MW_TRY(launch_after(dw_rows_kernel<float>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, TERMS, (int)first, l.piece, l.info,
+                                l.dw, l.padded, (float*)dw));
+        }
+      }
     }
   }
   if (total && a.rows == 0) MW_CUDA_OK(cudaMemsetAsync(total, 0, 4, s));

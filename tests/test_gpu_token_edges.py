@@ -1,4 +1,4 @@
-"""The lookup and the vocabulary's loss where their kernels change course: operands whose sample misleads, few rows taken
+"""The lookup and the vocabulary's loss where their kernels change course: operands of unusual sizes, few rows taken
 as they lie, waves of tiles with a rest, pieces with gradients off the copy engine's boundaries, places beyond 2^31, two
 calls at once.  Formulas and tolerances are those of test_gpu_token_loss.py and test_gpu_embedding.py."""
 import pytest
@@ -12,22 +12,56 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("how", ["as it is", "outlier", "zeros in the sample", "small sample", "large sample"])
-def test_operands_whose_sample_misleads(how, dtype):
-    """Operands of more than 32 MiB are written by what every sixteenth row holds, and again where that misses."""
+@pytest.mark.parametrize("how", ["as it is", "outlier", "zeros", "small and large rows", "large and small rows"])
+def test_operands_of_unusual_sizes(how, dtype):
+    """Operands are written for numbers of the usual size, and again where their largest lies elsewhere."""
     V, D, N = (4300 if dtype == F32 else 8600), 2048, 200
     h, W, t = make(N, V, D, dtype, lean=0.0)
     sampled = torch.arange(V, device="cuda") % 16 == 0
     if how == "outlier":
         W[1, 5] = 3.0e4
         h[:, 5] = 0
-    elif how == "zeros in the sample":
+    elif how == "zeros":
         W[sampled] = 0
-    elif how == "small sample":
+    elif how == "small and large rows":
         W[sampled] *= 2.0 ** -12
-    elif how == "large sample":
+    elif how == "large and small rows":
         W[~sampled] *= 2.0 ** -12
     check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [-30, -12, -9, -8, -3, 4, 6, 7, 8, 9, 10, 14, 30])
+def test_operands_of_every_size(size, dtype):
+    h, W, t = make(150, 400, 192, dtype)
+    h, W = h * 2.0 ** size, W * 2.0 ** -size
+    check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lean", [0.0, 15.0, 40.0, 200.0])
+def test_losses_of_sure_rows(lean, dtype):
+    """The others' terms against the target's: a loss near zero keeps its digits.  Relative to e = exp(loss) - 1 it is
+    off by what the differences of logits are, each ((D / 16 + 8) 2^-23 and 2^-21) of S."""
+    h, W, t = make(300, 700, 128, dtype, lean=lean)
+    r = mwb.token_loss(h, W, t)
+    z, S = h.double() @ W.double().T, h.double().abs() @ W.double().abs().T
+    ez = 2 * ((128 / 16 + 8) * 2.0 ** -23 + 2.0 ** -21) * S.amax(1) + 2.0 ** -18
+    odds = torch.exp(z - z.gather(1, t[:, None]))
+    odds.scatter_(1, t[:, None], 0.0)
+    want = torch.log1p(odds.sum(1))
+    assert bool(((r.loss.double() - want).abs() <= torch.expm1(ez) * -torch.expm1(-want) + 2.0 ** -22 * want + 1e-36).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V,D,piece", [(2100, 200, 100, 0), (2100, 300, 64, 1024), (5000, 60, 520, 0), (1500, 2500, 128, 512), (1024, 256, 256, 0)])
+def test_few_tiles_of_the_weight_gradient(N, V, D, piece, dtype):
+    h, W, t = make(N, V, D, dtype, left_out=0.3)
+    for kind in (F32, BF16):
+        check(mwb.token_loss_gradient(h, W, t, piece_rows=piece, grad_dtype=kind), reference(h, W, t), ALL)
+    t[:] = -1
+    r = mwb.token_loss_gradient(h, W, t, piece_rows=piece)
+    assert bool((r.dweight == 0).all() and (r.dh == 0).all() and (r.loss == 0).all()) and float(r.total) == 0
 
 
 @pytest.mark.parametrize("ids", [torch.int32, torch.int64])
