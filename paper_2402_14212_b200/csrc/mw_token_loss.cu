@@ -272,6 +272,38 @@ __device__ __forceinline__ uint32_t bf162_bits(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// A buffer's 32 rows of 128 bytes to rows that do not lie on the copy engine's boundaries, E elements a lane and row.
+// (The loop is the time of a tile whose K is short: eight rows are read before the first is written, and addresses are
+// additions.)
+template <typename V, int E>
+__device__ __forceinline__ void store_rows(uint32_t at, V* to, int64_t ld, int rows, int cols, int lane) {
+  constexpr uint32_t kPer = 16 / sizeof(V);          // elements of a 16-byte piece
+  bool on[E];
+#pragma unroll
+  for (int x = 0; x < E; ++x) on[x] = lane + 32 * x < cols;
+  to += lane;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 32 && r0 < rows; r0 += 8) {
+    V v[8][E];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int x = 0; x < E; ++x) {
+        const uint32_t e = (uint32_t)(lane + 32 * x), from = at + (uint32_t)r0 * 128u + piece_at((uint32_t)r, e / kPer) + e % kPer * (uint32_t)sizeof(V);
+        if constexpr (sizeof(V) == 2) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v[r][x]) : "r"(from));
+        else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[r][x]) : "r"(from));
+      }
+#pragma unroll
+    for (int r = 0; r < 8; ++r, to += ld) {
+      if (r0 + r < rows) {
+#pragma unroll
+        for (int x = 0; x < E; ++x)
+          if (on[x]) to[32 * x] = v[r][x];
+      }
+    }
+  }
+}
+
 template <int TERMS, int KIND>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
@@ -616,17 +648,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
                 hand_over(&p.out, at, col0 + c, row0);
               } else {
                 __syncwarp();
-                const int rows = p.vocab - row0 < 32 ? p.vocab - row0 : 32;
-#pragma unroll 8
-                for (int r = 0; r < rows; ++r)
-#pragma unroll
-                  for (int x = 0; x < 2; ++x) {
-                    const int col = col0 + c + lane + 32 * x;
-                    const uint32_t e = (uint32_t)(lane + 32 * x);
-                    unsigned short v;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + piece_at((uint32_t)r, e >> 3) + (e & 7u) * 2u) : "memory");
-                    if (col < p.dim) static_cast<unsigned short*>(p.dw)[(size_t)(row0 + r) * p.ld_dw + col] = v;
-                  }
+                store_rows<unsigned short, 2>(at, static_cast<unsigned short*>(p.dw) + (size_t)row0 * p.ld_dw + col0 + c, p.ld_dw,
+                                              p.vocab - row0, p.dim - (col0 + c), lane);
                 __syncwarp();
               }
             }
@@ -648,13 +671,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
                 hand_over(&p.out, at, col0 + c, row0);
               } else {
                 __syncwarp();
-                const int rows = p.vocab - row0 < 32 ? p.vocab - row0 : 32;
-#pragma unroll 8
-                for (int r = 0; r < rows; ++r) {
-                  uint32_t v;
-                  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at + piece_at((uint32_t)r, (uint32_t)lane >> 2) + ((uint32_t)lane & 3u) * 4u) : "memory");
-                  if (col0 + c + lane < p.dim) static_cast<uint32_t*>(p.dw)[(size_t)(row0 + r) * p.ld_dw + col0 + c + lane] = v;
-                }
+                store_rows<uint32_t, 1>(at, static_cast<uint32_t*>(p.dw) + (size_t)row0 * p.ld_dw + col0 + c, p.ld_dw, p.vocab - row0,
+                                        p.dim - (col0 + c), lane);
                 __syncwarp();
               }
             }
