@@ -488,7 +488,8 @@ mw_status mw_token_loss_forward(const mw_token_loss_desc* desc, const void* h, c
 mw_status mw_token_loss_gradient(const mw_token_loss_desc* desc, const void* h, const void* weight,
                                  const void* targets, const float* row_weight, float* loss, float* total, void* dh,
                                  void* dweight, void* workspace, size_t workspace_bytes, void* stream);
-/* Synchronise `stream`, return the first device-side error recorded in the workspace by the last call. */
+/* Synchronise `stream`, return the first device-side error recorded in the workspace by the last call.  Where a bounded
+ * wait of the products ran out (2 s) the total is NaN, and what was formed after it. */
 mw_status mw_token_loss_status(const void* workspace, void* stream);
 
 /* Clipping by the norm of all gradients together:

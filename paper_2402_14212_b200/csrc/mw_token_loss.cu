@@ -108,6 +108,7 @@ struct alignas(64) ProductArgs {
   CUtensorMap a, b, out, acc;
   const LossInfo* info;
   DeviceStatus* st;
+  float* total;             // NaN where a wait ran out
   int first, piece;         // rows of this piece begin at `first` of the live ones
   int vocab, dim;
   int tiles_m, tiles_n;     // of the whole piece (P_DW: of the vocabulary and the columns)
@@ -688,6 +689,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     // a wait ran out: copies still in flight get a bounded time to land before the CTA retires
     for (int s = 0; s < stages; ++s)
       for (uint32_t i = 0; i < 4096u && !mbar_try_wait<true>(smem_u32(&full_bar[s]), 0u); ++i) __nanosleep(256);
+    if (p.total) *p.total = __int_as_float(0x7fffffff);       // (the kernels that follow see the status)
   }
   cluster_sync_all();
   tc_fence_after();
@@ -910,13 +912,14 @@ constexpr float kNoPower = -3e38f;
 struct RowEnd {
   float loss, total, less;      // the loss, all terms as v.sum holds them, 1 - p of the target
 };
-__device__ __forceinline__ RowEnd row_end(RowSum v, float target_z, float target_power) {
+__device__ __forceinline__ RowEnd row_end(const LossInfo* info, RowSum v, float target_z, float target_power) {
   RowEnd e;
   const float odds = (v.k - target_power) + log2f(v.sum * 0x1p-15f) - target_z, r = exp2f(odds);
   const bool far = odds > 24.f;
   e.loss = far ? 0.69314718055994531f * odds : log1pf(r);
   e.less = far ? 1.f : r / (1.f + r);
   e.total = v.sum + exp2f((target_power - v.k) + 15.f + target_z);
+  if (info->st.code != 0) e.loss = e.total = __int_as_float(0x7fffffff);          // a wait ran out: nothing here is right
   return e;
 }
 
@@ -964,7 +967,7 @@ loss_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, const float
     }
     v = warp_join(v);
     if (lane == 0) {
-      const float l = row_end(v, target_z[i], sums[i * sum_blocks + target[i] / kSumColumns].x).loss;
+      const float l = row_end(info, v, target_z[i], sums[i * sum_blocks + target[i] / kSumColumns].x).loss;
       loss[row[i]] = l;
       part[i] = (double)g[i] * (double)l;
     }
@@ -993,7 +996,7 @@ direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, int colum
     }
     v = warp_join(v);
     if (lane == 0) {
-      const float l = on ? row_end(v, target_z[i], sums[(size_t)i * sum_blocks + (int)targets[i] / columns].x).loss : 0.f;
+      const float l = on ? row_end(info, v, target_z[i], sums[(size_t)i * sum_blocks + (int)targets[i] / columns].x).loss : 0.f;
       loss[i] = l;
       part[i] = on ? (double)(weight ? weight[i] : 1.f / (float)live) * (double)l : 0.0;
     }
@@ -1032,7 +1035,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       v = warp_v[0];
       for (int w = 1; w < WARPS; ++w) v = join(v, warp_v[w]);
     }
-    const RowEnd end = row_end(v, target_z[i], mine[t / kSumColumns].x);
+    const RowEnd end = row_end(info, v, target_z[i], mine[t / kSumColumns].x);
     if (thread == 0) {
       loss[row[i]] = end.loss;
       part[i] = (double)g[i] * (double)end.loss;
@@ -1123,7 +1126,8 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
   after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
-  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, terms)));
+  float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, terms)));
+  if (info->st.code != 0) f = __int_as_float(0x7fffffff);
   const DhPlan plan = dh_plan(live, tiles_n, blocks_k, pairs, terms);
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)live * per;
@@ -1393,6 +1397,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     ProductArgs p = {};
     p.info = l.info;
     p.st = &l.info->st;
+    p.total = total;
     p.vocab = a.vocab; p.dim = a.dim;
     p.scale = a.scale; p.scaled = scaled;
     p.piece = l.piece;

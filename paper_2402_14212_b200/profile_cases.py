@@ -7,12 +7,14 @@
   python -m paper_2402_14212_b200.profile_cases sconv --images 16 --op 0 --terms 3
   python -m paper_2402_14212_b200.profile_cases step --workload sweep_mlp --depth 4 --no-coop
   python -m paper_2402_14212_b200.profile_cases sequence --no-coop --reps 1
+  python -m paper_2402_14212_b200.profile_cases tokens --reps 1
 
 Each case allocates its seeded inputs, runs the kernel `--reps` times and exits.
 """
 from __future__ import annotations
 
 import argparse
+import math
 
 import numpy as np
 
@@ -21,7 +23,7 @@ def main():
     import torch
     from . import binding as mwb
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "pack", "fragments", "vijp", "conv", "sconv", "step", "sequence"])
+    ap.add_argument("case", choices=["gemm", "pack", "fragments", "vijp", "conv", "sconv", "step", "sequence", "tokens"])
     ap.add_argument("--workload", default="sweep_mlp", help="step: a workload of paper_2402_14212_b200.synth")
     ap.add_argument("--depth", type=int, default=4)
     ap.add_argument("--no-coop", action="store_true",
@@ -61,6 +63,28 @@ def main():
             mwb.residual_norm_backward(x, b, rms, dx_out=dxo, dn=dn, **kw)
             for (p, _, _), m, ws in zip(plans, mats, wss):
                 p.project(m, ws)
+        torch.cuda.synchronize()
+        return
+    if a.case == "tokens":
+        # the vocabulary's loss and gradients of bf16 and fp32 operands and of few rows, the lookup and its gradient, clipping
+        for dt in (torch.bfloat16, torch.float32):
+            N, V, D = 4096, 18944, 2048 if dt == torch.bfloat16 else 1024
+            h = torch.randn(N, D, device="cuda", generator=g).to(dt)
+            w = (torch.randn(V, D, device="cuda", generator=g) / D ** 0.5).to(dt)
+            t = torch.randint(0, V, (N,), device="cuda", generator=g)
+            for _ in range(a.reps):
+                mwb.token_loss(h, w, t)
+                mwb.token_loss_gradient(h, w, t)
+                mwb.token_loss(h[:16], w, t[:16])
+        table = torch.randn(32768, 2048, device="cuda", generator=g).bfloat16()
+        rank = (torch.exp(torch.rand(16384, device="cuda", generator=g) * math.log(32768.0)) - 1).long().clamp_(0, 32767)
+        dout = torch.randn(16384, 2048, device="cuda", generator=g).bfloat16()
+        grads = [torch.randn(1024, 1024, device="cuda", generator=g) for _ in range(64)]
+        out = [torch.empty_like(x) for x in grads]
+        for _ in range(a.reps):
+            mwb.embedding(rank, table)
+            mwb.embedding_backward(rank, dout, 32768)
+            mwb.clip_gradients(grads, 1.0, out=out)
         torch.cuda.synchronize()
         return
     if a.case == "step":
