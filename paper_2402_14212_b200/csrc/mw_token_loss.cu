@@ -767,28 +767,6 @@ __device__ __forceinline__ unsigned finite_bits(float v) {
   return b < 0x7f800000u ? b : 0u;
 }
 
-// eight values of a row from column c on, zero from `dim` on (WIDE: rows and pieces lie on 16-byte boundaries)
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(const T* row, int c, int dim, float (&v)[8]) {
-  if (WIDE && sizeof(T) == 4) {
-    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 x = c < dim ? reinterpret_cast<const float4*>(row + c)[0] : zero;
-    const float4 y = c + 4 < dim ? reinterpret_cast<const float4*>(row + c)[1] : zero;
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-  } else if (WIDE) {
-    const uint4 x = c < dim ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < dim ? to_f32(row[c + i]) : 0.f;
-  }
-}
-
 // The terms of v times a power of two; beside an infinity or a NaN the second is zero.
 __device__ __forceinline__ void split_half(float v, unsigned short& hi, unsigned short& lo) {
   const __half h = __float2half_rn(v);
@@ -840,52 +818,90 @@ __global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, 
     }
   }
   const float f = __uint_as_float((unsigned)(127 + e) << 23);
-  const int64_t n = o.count ? *o.count : o.rows;
-  const int64_t whole = (n + kTile - 1) / kTile * kTile, upto = whole < o.staged_rows ? whole : o.staged_rows;
+  const int rows = (int)o.rows, n = o.count ? *o.count : rows;
+  const int whole = (n + kTile - 1) / kTile * kTile, upto = whole < (int)o.staged_rows ? whole : (int)o.staged_rows;
   const uint32_t per = (uint32_t)padded / 8;
-  const int64_t items = (o.dead && upto < o.rows ? o.rows : upto) * per;
+  const int64_t items = (int64_t)(o.dead && upto < rows ? rows : upto) * per;
   const bool small = items < 0x7fffffff;
   unsigned m = 0;
-#pragma unroll 2
-  for (int64_t i = block * 256 + threadIdx.x; i < items; i += blocks * 256) {
-    const int64_t r = small ? (uint32_t)i / per : i / per;
-    const int c = (int)(i - r * per) * 8;
-    const int64_t at = o.row && r < o.rows ? o.row[r] : r;
-    if (r < upto) {
-      unsigned short hi[8], lo[8];
-      if (SCALED) {
-        float v[8];
-        if (r < n) {
-          load8<T, WIDE>(o.x + at * o.ld, c, dim, v);
-        } else {
+  auto write = [&](int r, int c, const unsigned short (&hi)[8], const unsigned short (&lo)[8]) {
+    auto pack = [](const unsigned short (&x)[8]) {
+      return make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+    };
+    *reinterpret_cast<uint4*>(o.out + (int64_t)r * padded + c) = pack(hi);
+    if (TERMS == 2) *reinterpret_cast<uint4*>(o.out + (o.staged_rows + r) * padded + c) = pack(lo);
+  };
+  // a thread's pieces of eight columns: what several of them need is on its way before the first is used
+  constexpr int kAhead = WIDE ? (sizeof(T) == 2 ? 4 : 2) : 1, kLoads = sizeof(T) == 2 ? 1 : 2;
+  for (int64_t i0 = block * (256 * kAhead) + threadIdx.x; i0 < items; i0 += blocks * (256 * kAhead)) {
+    uint4 raw[kAhead][kLoads];
+    int rr[kAhead], at[kAhead], cc[kAhead];            // (rows are 2^24 at the most)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if (!AGAIN) m = max(m, finite_bits(v[k]));
-          split_half(v[k] * f, hi[k], lo[k]);
-        }
-      } else {
-        const unsigned short* from = reinterpret_cast<const unsigned short*>(o.x) + at * o.ld;
-        if (WIDE) {
-          const uint4 x = r < n && c < dim ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t b[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int k = 0; k < 8; ++k) hi[k] = (unsigned short)(b[k / 2] >> (k % 2 * 16));
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) hi[k] = r < n && c + k < dim ? from[c + k] : (unsigned short)0;
-        }
-      }
-      auto pack = [](const unsigned short (&x)[8]) {
-        return make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
-      };
-      *reinterpret_cast<uint4*>(o.out + r * padded + c) = pack(hi);
-      if (TERMS == 2) *reinterpret_cast<uint4*>(o.out + (o.staged_rows + r) * padded + c) = pack(lo);
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t i = i0 + a * 256;
+      rr[a] = i < items ? (int)(small ? (uint32_t)i / per : i / per) : INT32_MAX;
+      cc[a] = i < items ? (int)((uint32_t)i - (uint32_t)rr[a] * per) * 8 : 0;
+      at[a] = o.row && rr[a] < rows ? o.row[rr[a]] : rr[a];
     }
-    if (!AGAIN && o.dead && r >= n && r < o.rows)
-      for (int k = 0; k < 8 && c + k < dim; ++k) o.dead[at * o.ld_dead + c + k] = from_f64<T>(0.0);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q)
+        raw[a][q] = WIDE && rr[a] < n && cc[a] + q * 4 < dim ? reinterpret_cast<const uint4*>(o.x + (int64_t)at[a] * o.ld + cc[a])[q] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int r = rr[a], c = cc[a];
+      if (r == INT32_MAX) continue;
+      if (r < upto) {
+        const uint32_t b[4] = {raw[a][0].x, raw[a][0].y, raw[a][0].z, raw[a][0].w};
+        unsigned short hi[8], lo[8];
+        if (SCALED && WIDE && sizeof(T) == 2) {
+          // eight bf16 numbers: two conversions an instruction, and the largest of them two at a time (beside an infinity
+          // or a NaN one by one)
+          uint32_t pair = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t h = half2_bits(__uint_as_float(b[k] << 16) * f, __uint_as_float(b[k] & 0xffff0000u) * f);
+            hi[2 * k] = (unsigned short)h;
+            hi[2 * k + 1] = (unsigned short)(h >> 16);
+            if (!AGAIN) pair = __vmaxu2(pair, b[k] & 0x7fff7fffu);
+          }
+          if (!AGAIN) {
+            const unsigned top = max(pair & 0xffffu, pair >> 16);
+            if (top < 0x7f80u) {
+              m = max(m, top << 16);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) m = max(m, max(finite_bits(__uint_as_float(b[k] << 16)), finite_bits(__uint_as_float(b[k] & 0xffff0000u))));
+            }
+          }
+        } else if (SCALED) {
+          float v[8];
+          if (WIDE) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint4& w = raw[a][k / 4 % kLoads];
+              v[k] = __uint_as_float(k % 4 == 0 ? w.x : (k % 4 == 1 ? w.y : (k % 4 == 2 ? w.z : w.w)));
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = r < n && c + k < dim ? to_f32(o.x[(int64_t)at[a] * o.ld + c + k]) : 0.f;
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (!AGAIN) m = max(m, finite_bits(v[k]));
+            split_half(v[k] * f, hi[k], lo[k]);
+          }
+        } else {
+          const unsigned short* from = reinterpret_cast<const unsigned short*>(o.x) + (int64_t)at[a] * o.ld;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) hi[k] = WIDE ? (unsigned short)(b[k / 2] >> (k % 2 * 16)) : (r < n && c + k < dim ? from[c + k] : (unsigned short)0);
+        }
+        write(r, c, hi, lo);
+      }
+      if (!AGAIN && o.dead && r >= n && r < rows)
+        for (int k = 0; k < 8 && c + k < dim; ++k) o.dead[(int64_t)at[a] * o.ld_dead + c + k] = from_f64<T>(0.0);
+    }
   }
   if (SCALED && !AGAIN) block_largest(m, o.most);
 }
@@ -1382,12 +1398,14 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       return want < 8 * (int64_t)sm_count() ? want : 8 * (int64_t)sm_count();
     };
     const int64_t bw = blocks_for(ow.rows), bh = blocks_for(a.rows + kTile);
-    auto stage = [&](auto kernel) { return launch_after(kernel, (unsigned)(bw + bh), 256, 0, s, ow, oh, a.dim, l.padded, bw); };
+    auto stage = [&](auto kernel, int64_t nw, int64_t nh) { return launch_after(kernel, (unsigned)(nw + nh), 256, 0, s, ow, oh, a.dim, l.padded, nw); };
     if (scaled) {
-      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, false> : stage_kernel<T, TERMS, true, false, false>));
-      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>));
+      // (the second seldom has anything to do: two blocks a multiprocessor see to that sooner than eight)
+      const int64_t few = 2 * (int64_t)sm_count(), fw = bw < few ? bw : few, fh = bh < few ? bh : few;
+      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, false> : stage_kernel<T, TERMS, true, false, false>, bw, bh));
+      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>, fw, fh));
     } else {
-      MW_TRY(stage(rows16 ? stage_kernel<T, 1, false, true, false> : stage_kernel<T, 1, false, false, false>));
+      MW_TRY(stage(rows16 ? stage_kernel<T, 1, false, true, false> : stage_kernel<T, 1, false, false, false>, bw, bh));
     }
   }
   if (a.rows > 0 || dw) {
