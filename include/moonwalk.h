@@ -464,7 +464,7 @@ mw_status mw_embedding_backward(const mw_embedding_desc* desc, const void* token
  *   dz_ij = g_i (exp(z_ij) / sum_k exp(z_ik) - [j = targets_i])
  * A row whose target is not in 0..vocab-1 (or whose g_i is zero) is left out: its loss and dh are zero, and
  * nothing of its h is read into anything.  g_i = row_weight[i], or without row_weight 1 / (rows not left out).
- * A value that is not finite stays in the losses and dh of the rows it enters (and in dweight); an infinity may
+ * rows / 256 times vocab / 64 is at most 2^30.  A value that is not finite stays in the losses and dh of the rows it enters (and in dweight); an infinity may
  * come out as NaN.  The logits are never held whole: the loss alone keeps two numbers for 128 of them, the gradient a piece of
  * rows at a time, which is turned into dz in its place. */
 typedef struct {

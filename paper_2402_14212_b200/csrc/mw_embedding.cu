@@ -638,6 +638,7 @@ mw_status lookup(const mw_embedding_desc* d, const void* tokens, const void* tab
   const I* t = (const I*)tokens;
   if (per >= 64) {
     const int segments = ceil_div(per, 32 * kLookupAhead);
+    if (a.n * segments > ((int64_t)1 << 33)) return MW_ERR_UNSUPPORTED;
     return launch_after(wide ? lookup_kernel<T, I, kVec> : lookup_kernel<T, I, 1>, (unsigned)((a.n * segments + 7) / 8), 256, 0, s, a, t,
                         (const T*)table, (T*)out, segments);
   }
@@ -676,7 +677,7 @@ mw_status sum_runs(const EmbedArgs& a, const EmbedScratch& l, const uint32_t* ke
   constexpr int kMult = VEC == 1 ? 4 : 1;
   const int groups = ceil_div(a.dim, 32 * VEC * kMult);
   const int64_t warps = (int64_t)l.pieces * groups;
-  if (warps > ((int64_t)1 << 34)) return MW_ERR_UNSUPPORTED;
+  if (warps > ((int64_t)1 << 33)) return MW_ERR_UNSUPPORTED;
   MW_TRY(launch_after(run_sums_kernel<T, G, VEC, kMult, ADD, GWIDE>, (unsigned)((warps + 7) / 8), 256, 0, s, a, key, pos, dout, dtable, l.partial, groups, l.joins));
   const int64_t joins = (int64_t)l.pieces * ceil_div(a.dim, kJoinColumns);
   return launch_after(join_runs_kernel<G, ADD>, (unsigned)(joins < 148 * 4 ? joins : 148 * 4), kJoinThreads, 0, s, a, key, l.partial, dtable, l.joins);

@@ -142,7 +142,6 @@ struct alignas(64) ProductArgs {
 // wave is as short as the others leave it (4096 rows and 2048 columns are 128 tiles on 74 pairs: 1.75 waves with the last
 // 54 in four, 2 without).  The shares' sums, beyond the first, lie in blocks of their own and are added in order.
 struct DhPlan { int whole, rest, shares; };
-constexpr int kMostShares = 32;
 __host__ __device__ constexpr int share_blocks(int pairs) { return 4 * pairs; }      // most of them
 // (a warp calls it, a lane a number of shares)
 __device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, int pairs, int terms) {
@@ -1288,6 +1287,8 @@ mw_status check_loss(const mw_token_loss_desc* d) {
   if (d->grad_dtype != 0 && d->grad_dtype != MW_F32 && d->grad_dtype != MW_BF16_F32ACC) return MW_ERR_INVALID_ARG;
   for (int64_t ld : {d->ld_h, d->ld_weight, d->ld_dh, d->ld_dweight})
     if (ld != 0 && ld < d->dim) return MW_ERR_INVALID_ARG;
+  // (tiles are counted in 32 bits)
+  if ((d->rows / kTile + 1) * (d->vocab / 64 + 1) > (1 << 30)) return MW_ERR_UNSUPPORTED;
   return MW_OK;
 }
 

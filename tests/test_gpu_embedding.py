@@ -161,8 +161,9 @@ def test_gradient_against_differences():
     assert abs(float(rise - along)) <= 600 * 32 * 3.0 * 8 * 4 * U
 
 
-def test_another_stream_and_a_captured_call():
-    t, table, dout = make(500, 40, 128, torch.bfloat16, common=0.3)
+@pytest.mark.parametrize("n", [500, 70001])
+def test_another_stream_and_a_captured_call(n):
+    t, table, dout = make(n, 40, 128, torch.bfloat16, common=0.3)
     want, grad = mwb.embedding(t, table), mwb.embedding_backward(t, dout, 40)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
@@ -173,7 +174,7 @@ def test_another_stream_and_a_captured_call():
     with torch.cuda.graph(graph):
         c, d = mwb.embedding(t, table), mwb.embedding_backward(t, dout, 40)
     for seed in (5, 6):
-        t2, table2, dout2 = make(500, 40, 128, torch.bfloat16, seed=seed)
+        t2, table2, dout2 = make(n, 40, 128, torch.bfloat16, seed=seed)
         t.copy_(t2), table.copy_(table2), dout.copy_(dout2)
         graph.replay()
         assert torch.equal(c, mwb.embedding(t2, table2)) and torch.equal(d, mwb.embedding_backward(t2, dout2, 40))

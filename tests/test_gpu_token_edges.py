@@ -167,3 +167,23 @@ def test_two_calls_at_once():
         for x, y in zip(got[:2], want[:2]):
             assert all(torch.equal(p, q) for p, q in zip(x, y))
         assert torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V,piece", [(2500, 700, 0), (2500, 700, 512), (1030, 5000, 256)])
+def test_captured_calls_of_many_rows_and_pieces(N, V, piece, dtype):
+    h, W, t = make(N, V, 128, dtype)
+    call = lambda: mwb.token_loss_gradient(h, W, t, piece_rows=piece)
+    call(), mwb.token_loss(h, W, t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held, only = call(), mwb.token_loss(h, W, t)
+    for seed, out in ((3, 0.0), (4, 0.8), (5, 1.0)):
+        for a, b in zip((h, W, t), make(N, V, 128, dtype, seed=seed, left_out=out)):
+            a.copy_(b)
+        graph.replay()
+        got = [x.clone() for x in (*held, only.loss, only.total)]
+        fresh, loss = call(), mwb.token_loss(h, W, t)
+        assert all(torch.equal(a, b) for a, b in zip(got, (*fresh, loss.loss, loss.total)))
+        check(fresh, reference(h, W, t), ALL)

@@ -59,7 +59,7 @@ BAD_LOSS = [(dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(dim=0), IN
             (dict(dtype=3), INVALID), (dict(grad_dtype=-1), INVALID), (dict(index_bytes=1), INVALID),
             (dict(piece_rows=-1), INVALID), (dict(ld_h=63), INVALID), (dict(ld_weight=63), INVALID), (dict(ld_dh=63), INVALID),
             (dict(ld_dweight=63), INVALID), (dict(scale=float("nan")), INVALID), (dict(rows=(1 << 24) + 1), UNSUPPORTED),
-            (dict(vocab=(1 << 24) + 1), UNSUPPORTED), (dict(dim=(1 << 16) + 1), UNSUPPORTED)]
+            (dict(vocab=(1 << 24) + 1), UNSUPPORTED), (dict(rows=1 << 24, vocab=1 << 24), UNSUPPORTED), (dict(dim=(1 << 16) + 1), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_LOSS)
