@@ -62,9 +62,12 @@ constexpr int buffers_for(int terms, int kind, int blocks_k) {
 // K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
 // losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and 3.8e-7
 // with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
-// 8.7e-7 (1.10 and 1.12 ms).  dz of bf16 operands has 11 bits: its sums have 512 instructions, 2^-15 at the worst, and
-// are read out seldom.
-__host__ __device__ constexpr int piece_blocks(int terms, int kind) { return terms == 2 ? 4 : (kind == P_DH || kind == P_DW ? 128 : 16); }
+// 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many: 16 rows of 32768x2048
+// 3.4e-7 (7.5e-7) in 36.5 us (34.7), of fp32 operands 3.9e-7 in the same time.  dz of bf16 operands has 11 bits: its sums
+// have 512 instructions, 2^-15 at the worst, and are read out seldom.
+constexpr int piece_blocks(int terms, int kind, bool few) {
+  return terms == 2 ? (few ? 2 : 4) : (kind == P_DH || kind == P_DW ? 128 : (few ? 8 : 16));
+}
 
 // what the kernels of one call share, behind the status block
 struct LossInfo {
@@ -117,6 +120,7 @@ struct alignas(64) ProductArgs {
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
   int stages, buffers;
+  int most_blocks;          // K blocks of one accumulator
   int shares;               // P_DW: of K, where the tiles are few (their sums then lie in blocks, as dh's)
   int tile_n;               // columns of a tile: 256, fewer for few rows of the loss alone
   int direct;               // few rows of the loss alone: h as it is, rows that are left out among the others
@@ -212,11 +216,9 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live, c
 }
 
 // K blocks of each of a tile's pieces: as even as they come, since a short one leaves the products waiting for the epilogue
-template <int TERMS, int KIND>
-__device__ __forceinline__ int piece_of(const Unit& w) {
-  constexpr int kMost = piece_blocks(TERMS, KIND);
-  const int n = w.kb1 - w.kb0, pieces = (n + kMost - 1) / kMost;
-  return pieces > 1 ? (n + pieces - 1) / pieces : kMost;
+__device__ __forceinline__ int piece_of(const ProductArgs& p, const Unit& w) {
+  const int n = w.kb1 - w.kb0, pieces = (n + p.most_blocks - 1) / p.most_blocks;
+  return pieces > 1 ? (n + pieces - 1) / pieces : p.most_blocks;
 }
 
 // byte offset of 16-byte piece c of row r in a block of 128-byte rows under the 128-byte swizzle
@@ -409,7 +411,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       bool ok = true;
       for (int u = pair; u < units && ok; u += pairs) {
         const Unit w = unit_at<KIND>(p, u, live, plan);
-        const int piece = piece_of<TERMS, KIND>(w);
+        const int piece = piece_of(p, w);
         for (int kb0 = w.kb0; kb0 < w.kb1 && ok; kb0 += piece, ++j) {
           const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
           ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u));
@@ -483,7 +485,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const int cols = KIND == P_SUMS ? p.tile_n / 2 : kSumColumns;          // of this warp
       const int col0 = w.n0 + side * cols;
       float acc[kSumColumns];
-      const int piece = piece_of<TERMS, KIND>(w);
+      const int piece = piece_of(p, w);
       // of few rows most warps have none: they only hand the accumulators back
       const bool idle = KIND != P_DW && row0 >= live;
 #pragma unroll 1
@@ -1332,6 +1334,7 @@ template <int TERMS, int KIND>
 mw_status run_product(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   if (KIND == P_DH || KIND == P_DW) p.a_stage = TERMS * kPlaneBytes;
   p.buffers = buffers_for(TERMS, KIND, p.blocks_k);
+  p.most_blocks = piece_blocks(TERMS, KIND, p.piece <= kTile);
   p.stages = stages_for(TERMS, p.buffers, p.a_stage);
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
