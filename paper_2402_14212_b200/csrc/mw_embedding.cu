@@ -1,13 +1,15 @@
 // Embedding lookup with scaling, and its gradient (mw_embedding_*):
 //   out_i = s E[t_i],   dE_v = s sum_{t_i = v} dout_i
 // Both directions move rows and compute next to nothing: HBM bounds them (lookup 2 N rows, gradient N rows read
-// and V rows written).  The gradient sorts (token, position) by a stable radix sort, so that a token's positions
+// and V rows written).  Measured, bf16: lookup of 16384 in 32768x2048 20 us (6.7 TB/s, tokens met twice included), the
+// table's gradient 52 us (201 MB: 3.9 TB/s; zeros and sort 23, sums 22, joins 8, one after another), both of 5003 in
+// 10007x515 fp32 32 us (rows off 16-byte boundaries, half the tokens the same: four launches of 7 to 9 us).  The gradient sorts (token, position) by a stable radix sort, so that a token's positions
 // stand in a run, in order; runs are summed in float by warps that take 32 entries of the sorted list each,
 // whatever the runs' lengths, and what a run leaves in several warps' shares is joined in order afterwards.
 //
 // Up to 65536 tokens are sorted by one cluster of eight blocks, in their shared memory, while the other blocks of the
-// same launch fill the table's gradient with zeros: the sort's latency hides behind that.  More go through
-// three launches a digit.
+// same launch fill the table's gradient with zeros: the sort (9 us) hides behind that.  More go through
+// three launches a digit.  (By those launches, zeros first, 16384 tokens took 49 us before the first sum.)
 #include "mw_cluster.cuh"
 #include "mw_launch.cuh"
 
