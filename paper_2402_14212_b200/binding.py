@@ -1068,9 +1068,12 @@ def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None,
     (float32 or bfloat16 by grad_dtype, weight's type where None).  want: which of the two.  piece_rows: rows whose
     exponentials are held at a time (0: as many as take 1 GiB); fewer take less memory and more time.  `stream` as
     in gated_scan."""
+    import torch
     if stream is not None:
         return _on_stream(stream, h, token_loss_gradient, h, weight, targets, scale, row_weight, dh, dweight, grad_dtype,
                           want, piece_rows)
+    if weight.data_ptr() & 15:         # (of few rows read in place, by copies of 16 bytes)
+        weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(True, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight,
                        (bool(want[0]), bool(want[1])))
 

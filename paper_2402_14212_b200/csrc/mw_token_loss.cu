@@ -50,21 +50,32 @@ constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;       // one term of one opera
 constexpr uint32_t kBufferBytes = 32 * 128;             // 32 rows of 128 bytes of an epilogue warp
 constexpr uint64_t kLossWaitNs = 2000000000ull;
 enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
+// How operands are held.  M_ONE: one term (bf16 as it is in the loss alone, half precision times a power of two in the
+// gradient).  M_TWO: fp32 as two half-precision terms.  M_FEW: the gradient of few rows of bf16, whose time is the
+// vocabulary's way through memory: W is read in place, by both products that want it, exponentials are float and dz two
+// bf16 terms against one of W and h.  That saves writing and reading W once more and costs a product more of dz each: up to
+// 128 rows of 16-byte aligned W (1 row of 66235x2624: 238 us, 411 in half precision; the two meet at about 230 rows).
+enum { M_ONE = 1, M_TWO, M_FEW };
+constexpr bool of_logits(int kind) { return kind == P_SUMS || kind == P_EXP; }
+__host__ __device__ constexpr int terms_a(int mode, int kind) { return mode == M_TWO || (mode == M_FEW && kind >= P_DH) ? 2 : 1; }
+__host__ __device__ constexpr int terms_b(int mode) { return mode == M_TWO ? 2 : 1; }
+__host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ? 3 : (mode == M_FEW ? 2 : 1); }      // of dz
+constexpr int kFewRows = 128;
 // Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
 // few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
 constexpr int kStagesMax = 12;
 constexpr size_t kSmemMost = 225 * 1024;
-constexpr int stages_for(int terms, int buffers, uint32_t a_stage) {
+constexpr int stages_for(int buffers, uint32_t stage) {
   const size_t room = kSmemMost - 1024 - (size_t)kEpi * buffers * kBufferBytes;
-  const int n = (int)(room / (a_stage + (uint32_t)terms * kPlaneBytes));
+  const int n = (int)(room / stage);
   return n < kStagesMax ? n : kStagesMax;
 }
 // Buffers of an epilogue warp: one, which leaves the most stages, unless a tile has so few K blocks that its way out is
 // what takes the time.
-constexpr int buffers_for(int terms, int kind, int blocks_k) {
+constexpr int buffers_for(int mode, int kind, int blocks_k) {
   if (kind == P_SUMS) return 0;
   if (kind == P_DH || blocks_k > 16) return 1;
-  return terms == 1 && blocks_k <= 8 ? 4 : 2;
+  return mode != M_TWO && blocks_k <= 8 ? 4 : 2;
 }
 
 // K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
@@ -73,8 +84,8 @@ constexpr int buffers_for(int terms, int kind, int blocks_k) {
 // 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many: 16 rows of 32768x2048
 // 3.4e-7 (7.5e-7) in 36.5 us (34.7), of fp32 operands 3.9e-7 in the same time.  dz of bf16 operands has 11 bits: its sums
 // have 512 instructions, 2^-15 at the worst, and are read out seldom.
-constexpr int piece_blocks(int terms, int kind, bool few) {
-  return terms == 2 ? (few ? 2 : 4) : (kind == P_DH || kind == P_DW ? 128 : (few ? 8 : 16));
+constexpr int piece_blocks(int mode, int kind, bool few) {
+  return mode == M_TWO ? (few ? 2 : 4) : (of_logits(kind) ? (few ? 8 : 16) : 128 / products_of(mode));
 }
 
 // what the kernels of one call share, behind the status block
@@ -157,7 +168,7 @@ struct alignas(64) ProductArgs {
 struct DhPlan { int whole, rest, shares; };
 __host__ __device__ constexpr int share_blocks(int pairs) { return 4 * pairs; }      // most of them
 // (a warp calls it, a lane a number of shares)
-__device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, int pairs, int terms) {
+__device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, int pairs, int products) {
   const int tiles = (live + kTile - 1) / kTile * tiles_n;
   DhPlan d;
   d.whole = tiles / pairs * pairs;
@@ -165,7 +176,7 @@ __device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, i
   // cycles: a K block's products, what a tile costs beyond them, a sum's way through memory at 4.6 KB a cycle
   const int s = (int)(threadIdx.x & 31) + 1, per = (blocks_k + s - 1) / s;
   const bool can = s == 1 || (per >= 8 && d.rest * s <= share_blocks(pairs));
-  const unsigned cost = (unsigned)((d.rest * s + pairs - 1) / pairs) * (unsigned)(per * (terms == 1 ? 512 : 1536) + 3000) + (unsigned)(d.rest * s) * 114u;
+  const unsigned cost = (unsigned)((d.rest * s + pairs - 1) / pairs) * (unsigned)(per * products * 512 + 3000) + (unsigned)(d.rest * s) * 114u;
   const unsigned least = __reduce_min_sync(0xffffffffu, can ? cost : 0xffffffffu);
   d.shares = __ffs(__ballot_sync(0xffffffffu, can && cost == least));
   return d;
@@ -315,11 +326,13 @@ __device__ __forceinline__ void store_rows(uint32_t at, V* to, int64_t ld, int r
   }
 }
 
-template <int TERMS, int KIND>
+template <int MODE, int KIND>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr uint32_t b_stage = TERMS * kPlaneBytes;
+  constexpr int kTermsA = terms_a(MODE, KIND), kTermsB = terms_b(MODE);
+  constexpr bool kFloats = MODE != M_ONE;          // exponentials are float
+  constexpr uint32_t b_stage = kTermsB * kPlaneBytes;
   __shared__ __align__(8) uint64_t full_bar[kStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
   __shared__ __align__(8) uint64_t acc_full[2];
@@ -365,7 +378,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     reinterpret_cast<unsigned*>(p.clear)[threadIdx.x] = 0;
   const int live = live_rows<KIND>(p);
   DhPlan plan = {0, 0, 1};
-  if (KIND == P_DH) plan = dh_plan(live, p.tiles_n, p.blocks_k, p.pairs, TERMS);
+  if (KIND == P_DH) plan = dh_plan(live, p.tiles_n, p.blocks_k, p.pairs, products_of(MODE));
   const int units = unit_count<KIND>(p, live, plan);
 
   constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
@@ -437,10 +450,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
               for (int k = 0; k < kBK / 16; ++k) {
                 const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
                 umma_bf16<true>(d, a, b, p.idesc, k > 0 || kb > kb0);
-                if (TERMS == 2) {
-                  umma_bf16<true>(d, a, b + term, p.idesc, 1u);
-                  umma_bf16<true>(d, a + term, b, p.idesc, 1u);
-                }
+                if (kTermsB == 2) umma_bf16<true>(d, a, b + term, p.idesc, 1u);
+                if (kTermsA == 2) umma_bf16<true>(d, a + term, b, p.idesc, 1u);
               }
               umma_commit<true>(empty0 + 8u * stage);
               if (kb + 1 == kb1) umma_commit<true>(smem_u32(&acc_full[set]));
@@ -462,8 +473,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     uint32_t turn = 0;
     int j = 0;
     bool ok = true;
-    const int exps = p.scaled ? operand_exponent(p.info->h_max, TERMS) : 0;
-    const int expw = p.scaled ? operand_exponent(p.info->w_max, TERMS) : 0;
+    const int exps = p.scaled ? operand_exponent(p.info->h_max, kTermsB) : 0;
+    const int expw = p.scaled ? operand_exponent(p.info->w_max, kTermsB) : 0;
     const int expz = range_exponent(p.info->g_max);
     float factor = 1.f;
     if (KIND == P_DW) factor = (float)ldexp((double)p.scale, -(expz + exps));
@@ -587,14 +598,14 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           for (int i = 0; i < kSumColumns; ++i) sum += acc[i];
           if (on) p.sums[(size_t)row * p.sum_blocks + col0 / cols] = make_float2(power, sum);
           if (KIND == P_EXP) {
-            constexpr int kCols = TERMS == 1 ? 64 : 32;
+            constexpr int kCols = kFloats ? 32 : 64;
 #pragma unroll
             for (int c = 0; c < kSumColumns; c += kCols) {
               if (c >= (valid + kBK - 1) / kBK * kBK) continue;          // beyond the padded row
               const uint32_t at = next_buffer();
 #pragma unroll
               for (uint32_t q = 0; q < 8; ++q) {
-                if (TERMS == 1) {
+                if (!kFloats) {
                   const int i = c + 8 * (int)q;
                   st_shared_v4(at + piece_at((uint32_t)lane, q), half2_bits(acc[i % kSumColumns], acc[(i + 1) % kSumColumns]),
                                half2_bits(acc[(i + 2) % kSumColumns], acc[(i + 3) % kSumColumns]),
@@ -777,7 +788,7 @@ __device__ __forceinline__ unsigned finite_bits(float v) {
   return b < 0x7f800000u ? b : 0u;
 }
 
-// The terms of v times a power of two; beside an infinity or a NaN the second is zero.
+// The terms of v; beside an infinity or a NaN the second is zero.
 __device__ __forceinline__ void split_half(float v, unsigned short& hi, unsigned short& lo) {
   const __half h = __float2half_rn(v);
   const float back = __half2float(h);
@@ -796,6 +807,13 @@ __device__ __forceinline__ void block_largest(unsigned m, unsigned* most) {
     m = __reduce_max_sync(0xffffffffu, threadIdx.x < 8 ? warp_m[threadIdx.x] : 0u);
     if (threadIdx.x == 0 && m) atomicMax(most, m);
   }
+}
+
+__device__ __forceinline__ void split_bf16(float v, unsigned short& hi, unsigned short& lo) {
+  const __nv_bfloat16 h = __float2bfloat16_rn(v);
+  const float back = __bfloat162float(h);
+  hi = __bfloat16_as_ushort(h);
+  lo = __bfloat16_as_ushort(__float2bfloat16_rn(isfinite(back) ? v - back : 0.f));
 }
 
 // h (rows with a target, by their index) or W as operands: [terms][staged rows][padded columns], zero beyond a row's
@@ -1031,13 +1049,13 @@ direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, int colum
 }
 
 // a row's exponentials -> dz times a power of two, in their place: WARPS warps of a block of eight a row
-template <int TERMS, int WARPS>
+template <int MODE, int WARPS>
 __global__ void __launch_bounds__(256)
 dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
           const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int padded) {
   after_previous();
   __shared__ RowSum warp_v[8];
-  constexpr int kThreads = WARPS * 32, kRows = 8 / WARPS;
+  constexpr int kThreads = WARPS * 32, kRows = 8 / WARPS, TERMS = MODE == M_ONE ? 1 : 2;
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
   const int upto = (live + kBK - 1) / kBK * kBK;
@@ -1129,7 +1147,10 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
             for (int q = 0; q < 4; ++q) x[q] = c + q == t ? at_target : x[q];
             unsigned short hi[4], lo[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) split_half(x[q], hi[q], lo[q]);
+            for (int q = 0; q < 4; ++q) {
+              if (MODE == M_FEW) split_bf16(x[q], hi[q], lo[q]);
+              else split_half(x[q], hi[q], lo[q]);
+            }
             unsigned short* to = at + 2 * (c & ~63) + (c & 63);
             *reinterpret_cast<uint2*>(to) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
             *reinterpret_cast<uint2*>(to + 64) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
@@ -1147,14 +1168,14 @@ __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2
 // dh of the piece's rows: the sums over the shares of K, in order, to the rows they belong to, four columns a thread
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
-dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, int tiles_n, int blocks_k, int pairs, int terms, int first,
+dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, int tiles_n, int blocks_k, int pairs, int mode, int first,
                int piece, const int* row, const LossInfo* info, T* dh) {
   after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
-  float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->w_max, terms)));
+  float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? operand_exponent(info->w_max, terms_b(mode)) : 0)));
   if (info->st.code != 0) f = __int_as_float(0x7fffffff);
-  const DhPlan plan = dh_plan(live, tiles_n, blocks_k, pairs, terms);
+  const DhPlan plan = dh_plan(live, tiles_n, blocks_k, pairs, products_of(mode));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)live * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
@@ -1186,13 +1207,13 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
 // dW of few tiles: the sums over the shares of K, in order, and over the pieces before, four columns a thread
 template <typename G>
 __global__ void __launch_bounds__(256)
-dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int terms, int first, int piece, const LossInfo* info, float* partial,
+dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mode, int first, int piece, const LossInfo* info, float* partial,
                int padded, G* dw) {
   after_previous();
   const int live = info->live;
   if (first > 0 && live <= first) return;
   const bool last = first + piece >= live;
-  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + operand_exponent(info->h_max, terms)));
+  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? operand_exponent(info->h_max, terms_b(mode)) : 0)));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)a.vocab * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
@@ -1232,6 +1253,7 @@ struct LossWs {
   unsigned short *h, *w, *e;
   float *slab, *shares, *dw;
   int blocks, piece, padded, vpadded, sum_blocks, staged_rows, piece_rows;
+  bool few;               // M_FEW
   bool in_place;          // W is read where it lies
 };
 
@@ -1254,7 +1276,9 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   const int terms = d->dtype == MW_F32 ? 2 : 1;
   const size_t n = (size_t)d->rows, v = (size_t)d->vocab, dim = (size_t)d->dim;
   const int64_t ld_w = d->ld_weight ? d->ld_weight : d->dim;
-  l->in_place = !gradient && terms == 1 && ld_w % 8 == 0;
+  l->few = gradient && terms == 1 && d->rows > 0 && d->rows <= kFewRows && ld_w % 8 == 0 && d->dim % kBK == 0;
+  l->in_place = l->few || (!gradient && terms == 1 && ld_w % 8 == 0);
+  const int held = l->few ? 2 : terms;          // half-precision numbers that an exponential takes
   l->blocks = ceil_div(d->rows, kIndexRows);
   l->padded = (int)align_up(dim, kBK);
   l->vpadded = (int)align_up(v, kBK);
@@ -1264,7 +1288,7 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   if (gradient) {
     piece = d->piece_rows;
     if (!piece) {
-      piece = kPieceBytes / (2 * terms * (int64_t)l->vpadded);
+      piece = kPieceBytes / (2 * held * (int64_t)l->vpadded);
       if (piece < 1024) piece = 1024;
     }
     if (piece < d->rows) piece = (int64_t)align_up((size_t)piece, kTile);
@@ -1283,7 +1307,7 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->sums = (float2*)take((size_t)l->piece * (n <= kTile ? ceil_div(d->vocab, 32) : l->sum_blocks) * 8);
   l->h = (unsigned short*)take((size_t)l->staged_rows * l->padded * 2 * terms);
   l->w = (unsigned short*)take(l->in_place ? 0 : v * l->padded * 2 * terms);
-  l->e = (unsigned short*)take(gradient ? (size_t)l->piece_rows * l->vpadded * 2 * terms : 0);
+  l->e = (unsigned short*)take(gradient ? (size_t)l->piece_rows * l->vpadded * 2 * held : 0);
   l->slab = (float*)take(gradient ? (size_t)l->piece_rows * l->padded * 4 : 0);
   l->shares = (float*)take(gradient ? (size_t)share_blocks(sm_count() / 2) * kTile * kTile * 4 : 0);
   l->dw = (float*)take(gradient && l->piece < d->rows ? v * l->padded * 4 : 0);
@@ -1339,15 +1363,15 @@ mw_status out_map(CUtensorMap* out, CUtensorMapDataType type, int size, const vo
   return make_map(out, type, 2, base, dims, strides, box);
 }
 
-template <int TERMS, int KIND>
-mw_status run_product(ProductArgs& p, int64_t most_units, cudaStream_t s) {
-  if (KIND == P_DH || KIND == P_DW) p.a_stage = TERMS * kPlaneBytes;
-  p.buffers = buffers_for(TERMS, KIND, p.blocks_k);
-  p.most_blocks = piece_blocks(TERMS, KIND, p.piece <= kTile);
-  p.stages = stages_for(TERMS, p.buffers, p.a_stage);
+template <int MODE, int KIND>
+mw_status run_product_in(ProductArgs& p, int64_t most_units, cudaStream_t s) {
+  if (!of_logits(KIND)) p.a_stage = terms_a(MODE, KIND) * kPlaneBytes;
+  p.buffers = buffers_for(MODE, KIND, p.blocks_k);
+  p.most_blocks = piece_blocks(MODE, KIND, p.piece <= kTile);
+  p.stages = stages_for(p.buffers, p.a_stage + terms_b(MODE) * kPlaneBytes);
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
-  auto kernel = loss_products_kernel<TERMS, KIND>;
+  auto kernel = loss_products_kernel<MODE, KIND>;
   if (!ready[dev]) {
     MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost));
     ready[dev] = true;
@@ -1370,6 +1394,13 @@ mw_status run_product(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
 }
 
+template <int TERMS, int KIND>
+mw_status run_product(bool few, ProductArgs& p, int64_t most_units, cudaStream_t s) {
+  if constexpr (TERMS == 2) return run_product_in<M_TWO, KIND>(p, most_units, s);
+  else if constexpr (KIND == P_SUMS) return run_product_in<M_ONE, KIND>(p, most_units, s);
+  else return few ? run_product_in<M_FEW, KIND>(p, most_units, s) : run_product_in<M_ONE, KIND>(p, most_units, s);
+}
+
 // fp32 accumulator, the operands' type, K across the rows of A and of B, N / 8, M / 16
 uint32_t instruction(bool bf16, bool turned_a, bool turned_b, int n = kTile) {
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((turned_a ? 1u : 0u) << 15) | ((turned_b ? 1u : 0u) << 16) |
@@ -1389,12 +1420,13 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   a.scale = (float)d->scale;
   LossWs l;
   loss_layout(d, gradient, ws, &l);
-  // bf16 operands of the loss alone are taken as they are
-  const bool scaled = TERMS == 2 || gradient;
+  // bf16 operands of the loss alone, and of few rows, are taken as they are
+  const bool scaled = TERMS == 2 || (gradient && !l.few);
+  const int mode = TERMS == 2 ? M_TWO : (l.few ? M_FEW : M_ONE);
   a.scaled = scaled;
   const unsigned wide = 148 * 8;
   // few rows of the loss alone: no row is moved where the copy engine can read h as it lies
-  const bool direct = l.in_place && a.rows > 0 && a.rows <= kTile && a.ld_h % 8 == 0 && ((uintptr_t)h & 15) == 0;
+  const bool direct = l.in_place && !gradient && a.rows > 0 && a.rows <= kTile && a.ld_h % 8 == 0 && ((uintptr_t)h & 15) == 0;
   if (l.blocks != 1) MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
   if (a.rows > 0 && !direct) {
     int* counts = l.blocks > 1 ? l.counts : nullptr;
@@ -1459,23 +1491,25 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1, logits.tile_n / 2)
                       : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
     if (gradient) {
-      const int64_t row_bytes = (int64_t)l.vpadded * 2 * TERMS, group_bytes = 128 * TERMS;
-      const int64_t hw_bytes = (int64_t)l.padded * 2;
-      MW_TRY(out_map(&logits.out, TERMS == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2 * TERMS, l.e, l.vpadded, l.piece_rows, l.vpadded));
+      // an exponential's place, and that of dz's terms: groups of 64, one term after the other
+      const int held = l.few ? 2 : TERMS;
+      const int64_t row_bytes = (int64_t)l.vpadded * 2 * held, group_bytes = 128 * held, hw_bytes = (int64_t)l.padded * 2;
+      MW_TRY(out_map(&logits.out, held == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2 * held, l.e, l.vpadded, l.piece_rows, l.vpadded));
       // dh: K along the rows of dz and across those of W
       by_h.tiles_n = ceil_div(a.dim, kTile);
       by_h.blocks_k = l.vpadded / kBK;
-      by_h.idesc = instruction(false, false, true);
-      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, TERMS, kHalf, 1));
-      MW_TRY(group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, 2));
+      by_h.idesc = instruction(bf16, false, true);
+      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, kHalf, 1));
+      MW_TRY(l.few ? group_map(&by_h.b, w, a.dim, a.vocab, a.ld_w * 2, 128, 128, 1, kBK, 2)
+                   : group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, 2));
       MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece_rows, l.padded));
       MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)share_blocks(p.pairs) * kTile, kTile));
       // dW: K across the rows of both
       by_w.tiles_m = ceil_div(a.vocab, kTile);
       by_w.tiles_n = ceil_div(a.dim, kTile);
       by_w.blocks_k = ceil_div(l.piece, kBK);
-      by_w.idesc = instruction(false, true, true);
-      MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, TERMS, kBK, 2));
+      by_w.idesc = instruction(bf16, true, true);
+      MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, kBK, 2));
       MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
       // tiles for less than half of the pairs: each in shares of K, of eight blocks at least
       const int tiles = by_w.tiles_m * by_w.tiles_n;
@@ -1496,16 +1530,18 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       logits.first = by_h.first = by_w.first = (int)first;
       if (a.rows > 0) {
         if (gradient) {
-          MW_TRY((run_product<TERMS, P_EXP>(logits, tm * logits.tiles_n, s)));
+          MW_TRY((run_product<TERMS, P_EXP>(l.few, logits, tm * logits.tiles_n, s)));
           // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of them waits of
           // one row after another)
           const bool short_rows = a.vocab <= 4096;
           const int dz_blocks = short_rows ? ceil_div(l.piece_rows, 8) : l.piece_rows;
-          MW_TRY(launch_after(short_rows ? dz_kernel<TERMS, 1> : dz_kernel<TERMS, 8>, (unsigned)(dz_blocks < (int)wide ? dz_blocks : wide), 256, 0, s,
+          constexpr int kMode = TERMS == 2 ? M_TWO : M_ONE, kOther = TERMS == 2 ? M_TWO : M_FEW;
+          auto dz = l.few ? (short_rows ? dz_kernel<kOther, 1> : dz_kernel<kOther, 8>) : (short_rows ? dz_kernel<kMode, 1> : dz_kernel<kMode, 8>);
+          MW_TRY(launch_after(dz, (unsigned)(dz_blocks < (int)wide ? dz_blocks : wide), 256, 0, s,
                               l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part,
                               first + l.piece >= a.rows ? total : nullptr, l.e, l.vpadded));
         } else {
-          MW_TRY((run_product<TERMS, P_SUMS>(logits, tm * logits.tiles_n, s)));
+          MW_TRY((run_product<TERMS, P_SUMS>(false, logits, tm * logits.tiles_n, s)));
           const unsigned blocks = (unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide);          // (a warp a row)
           if (direct)
             MW_TRY(launch_after(direct_rows_kernel<I>, blocks, 256, 0, s, l.info, l.sums, logits.sum_blocks, logits.tile_n / 2, l.target_z, targets, weight, (int)a.rows,
@@ -1515,20 +1551,20 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
                                 total));
         }
         if (dh) {
-          MW_TRY((run_product<TERMS, P_DH>(by_h, p.pairs, s)));
+          MW_TRY((run_product<TERMS, P_DH>(l.few, by_h, p.pairs, s)));
           auto rows_kernel = ((uintptr_t)dh & 15) == 0 && a.ld_dh % 4 == 0 && a.dim % 4 == 0 ? dh_rows_kernel<T, true> : dh_rows_kernel<T, false>;
-          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.shares, l.padded, by_h.tiles_n, by_h.blocks_k, p.pairs, TERMS, (int)first, l.piece,
+          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.shares, l.padded, by_h.tiles_n, by_h.blocks_k, p.pairs, mode, (int)first, l.piece,
                               l.row, l.info, dh));
         }
       }
       if (dw) {
-        MW_TRY((run_product<TERMS, P_DW>(by_w, (int64_t)by_w.tiles_m * by_w.tiles_n * by_w.shares, s)));
+        MW_TRY((run_product<TERMS, P_DW>(l.few, by_w, (int64_t)by_w.tiles_m * by_w.tiles_n * by_w.shares, s)));
         if (by_w.shares > 1) {
           if (dw_bf16)
-            MW_TRY(launch_after(dw_rows_kernel<__nv_bfloat16>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, TERMS, (int)first, l.piece,
+            MW_TRY(launch_after(dw_rows_kernel<__nv_bfloat16>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, mode, (int)first, l.piece,
                                 l.info, l.dw, l.padded, (__nv_bfloat16*)dw));
           else
-            MW_TRY(launch_after(dw_rows_kernel<float>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, TERMS, (int)first, l.piece, l.info,
+            MW_TRY(launch_after(dw_rows_kernel<float>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, mode, (int)first, l.piece, l.info,
                                 l.dw, l.padded, (float*)dw));
         }
       }
@@ -1545,10 +1581,10 @@ mw_status loss_call(const mw_token_loss_desc* d, const void* h, const void* w, c
   const int64_t ld_h = d->ld_h ? d->ld_h : d->dim, ld_dh = d->ld_dh ? d->ld_dh : d->dim;
   if (dh == h && dh && ld_h != ld_dh) return MW_ERR_INVALID_ARG;
   // rows that the copy engine reads start on 16-byte boundaries
-  const int64_t ld_w = d->ld_weight ? d->ld_weight : d->dim;
-  if (!gradient && d->dtype == MW_BF16_F32ACC && ld_w % 8 == 0 && ((uintptr_t)w & 15)) return MW_ERR_INVALID_ARG;
   LossWs l;
-  if (!ws || ((uintptr_t)ws & 255u) || bytes < loss_layout(d, gradient, nullptr, &l)) return MW_ERR_WORKSPACE;
+  const size_t need = loss_layout(d, gradient, nullptr, &l);
+  if (l.in_place && ((uintptr_t)w & 15)) return MW_ERR_INVALID_ARG;
+  if (!ws || ((uintptr_t)ws & 255u) || bytes < need) return MW_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
   char* b = static_cast<char*>(ws);
   using bf = __nv_bfloat16;

@@ -187,3 +187,23 @@ def test_captured_calls_of_many_rows_and_pieces(N, V, piece, dtype):
         fresh, loss = call(), mwb.token_loss(h, W, t)
         assert all(torch.equal(a, b) for a, b in zip(got, (*fresh, loss.loss, loss.total)))
         check(fresh, reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("N,V,D", [(1, 1, 64), (1, 5000, 128), (3, 70, 64), (64, 333, 320), (65, 20000, 64), (128, 4097, 192), (129, 4097, 192)])
+def test_gradients_of_few_rows(N, V, D, kind):
+    h, W, t = make(N, V, D, BF16, seed=N, left_out=0.3 if N > 3 else 0.0)
+    check(mwb.token_loss_gradient(h, W, t, grad_dtype=kind, scale=1.3), reference(h, W, t, scale=1.3), ALL)
+    w = torch.randn(N, device="cuda") * 1e-4
+    w[::4] = 0
+    h[::4] = float("inf")
+    want = reference(h, W, t, weight=w)
+    r = mwb.token_loss_gradient(h, W, t, row_weight=w, grad_dtype=kind, piece_rows=1)
+    check(r, want, ALL)
+    full = mwb.token_loss_gradient(h, W, t, row_weight=w, grad_dtype=kind)
+    own, wide = h.clone(), torch.zeros(V, D + 8, device="cuda", dtype=BF16)
+    wide[:, 8:] = W
+    again = mwb.token_loss_gradient(own, wide[:, 8:], t, row_weight=w, grad_dtype=kind, dh=own)
+    assert all(torch.equal(a, b) for a, b in zip(full, again)) and again.dh is own
+    wide[:, 1:D + 1] = W.clone()                   # off the boundary: copied
+    check(mwb.token_loss_gradient(h, wide[:, 1:D + 1], t, row_weight=w, grad_dtype=kind), want, ALL)
