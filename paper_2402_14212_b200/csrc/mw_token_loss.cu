@@ -27,6 +27,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "mw_launch.cuh"
 #include "mw_tc_ptx.cuh"
 
@@ -147,7 +149,8 @@ struct alignas(64) ProductArgs {
   LossInfo* clear;          // ... and what the other kernels share is cleared here
   const void* targets;
   int index_bytes;
-  uint32_t a_stage;         // bytes of A in a stage of a CTA
+  uint32_t a_stage, a_term; // bytes of A in a stage of a CTA, and from a term to the next
+  int a_rows;               // rows of A that are copied into a CTA
   int a_even;               // A's copies are the even CTA's alone: its rows hold all there are
   float scale;
   int scaled;
@@ -332,6 +335,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
   constexpr int kTermsA = terms_a(MODE, KIND), kTermsB = terms_b(MODE);
   constexpr bool kFloats = MODE != M_ONE;          // exponentials are float
+  // two blocks a fence (not where that spills a tile's floats)
+  constexpr bool kPairs = (MODE == M_ONE && KIND == P_EXP) || (MODE != M_TWO && KIND == P_DW);
   constexpr uint32_t b_stage = kTermsB * kPlaneBytes;
   __shared__ __align__(8) uint64_t full_bar[kStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
@@ -428,7 +433,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
       constexpr uint32_t a_base = (kTurnedA ? (8192u >> 4) : 1u) << 16, b_base = (kTurnedB ? (8192u >> 4) : 1u) << 16;
       constexpr uint32_t a_adv = kTurnedA ? (2048u >> 4) : (32u >> 4), b_adv = kTurnedB ? (2048u >> 4) : (32u >> 4);
-      constexpr uint32_t term = kPlaneBytes >> 4;
+      constexpr uint32_t term_b = kPlaneBytes >> 4;
+      const uint32_t term_a = p.a_term >> 4;
       int j = 0;
       bool ok = true;
       for (int u = pair; u < units && ok; u += pairs) {
@@ -450,8 +456,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
               for (int k = 0; k < kBK / 16; ++k) {
                 const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
                 umma_bf16<true>(d, a, b, p.idesc, k > 0 || kb > kb0);
-                if (kTermsB == 2) umma_bf16<true>(d, a, b + term, p.idesc, 1u);
-                if (kTermsA == 2) umma_bf16<true>(d, a + term, b, p.idesc, 1u);
+                if (kTermsB == 2) umma_bf16<true>(d, a, b + term_b, p.idesc, 1u);
+                if (kTermsA == 2) umma_bf16<true>(d, a + term_a, b, p.idesc, 1u);
               }
               umma_commit<true>(empty0 + 8u * stage);
               if (kb + 1 == kb1) umma_commit<true>(smem_u32(&acc_full[set]));
@@ -482,23 +488,76 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       factor = (float)ldexp((double)p.scale * 1.4426950408889634, -(exps + expw));
       if (factor == 0.f) factor = 1e-30f;           // (a sign, for what takes a term out of the sum)
     }
-    // a block of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the next buffer
-    auto next_buffer = [&]() -> uint32_t {
+    // Blocks of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the warp's buffers in turn: `group` of
+    // them at a time, since the fence between their stores and the copy engine is what a short tile waits for.
+    auto free_buffers = [&](int group) {
       if (lane == 0) {
-        if (buffers == 4) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
-        else if (buffers == 2) bulk_wait_read_but_one();
+        const int busy = buffers - group;
+        if (busy == 3) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
+        else if (busy == 2) asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory");
+        else if (busy == 1) bulk_wait_read_but_one();
         else bulk_wait_read_all();
       }
       __syncwarp();
+    };
+    auto next_buffer = [&]() -> uint32_t {
       const uint32_t at = sbuf + turn * kBufferBytes;
       if (++turn == (uint32_t)buffers) turn = 0;
       return at;
     };
-    auto hand_over = [&](const CUtensorMap* map, uint32_t at, int col, int row) {
+    auto hand_over = [&]() {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) bulk_store_2d(map, at, col, row);
     };
+    // 32 floats, 64 halves or 64 bf16 numbers from acc + c on
+    auto lay_floats = [&](const float* v, uint32_t at) {
+#pragma unroll
+      for (uint32_t q = 0; q < 8; ++q)
+        st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
+                     __float_as_uint(v[4 * q + 3]));
+    };
+    auto lay_pairs = [&](const float* v, uint32_t at, auto pack) {
+#pragma unroll
+      for (uint32_t q = 0; q < 8; ++q)
+        st_shared_v4(at + piece_at((uint32_t)lane, q), pack(v[8 * q], v[8 * q + 1]), pack(v[8 * q + 2], v[8 * q + 3]), pack(v[8 * q + 4], v[8 * q + 5]),
+                     pack(v[8 * q + 6], v[8 * q + 7]));
+    };
+    // all of a lane's columns from `acc` to `map`, those before `most`, two blocks a fence where the warp has the buffers
+    auto store_all = [&](const float* acc, auto lay, auto columns, const CUtensorMap* map, int col, int row, int most) {
+      constexpr int kCols = decltype(columns)::value;
+      if (kPairs && buffers >= 2) {
+#pragma unroll
+        for (int c = 0; c < kSumColumns; c += 2 * kCols) {
+          if (c < most) {
+            free_buffers(2);
+            const uint32_t first = next_buffer(), second = next_buffer();
+            lay(acc + c, first);
+            lay(acc + c + kCols, second);
+            hand_over();
+            if (lane == 0) {
+              bulk_store_2d(map, first, col + c, row);
+              if (c + kCols < most) bulk_store_2d(map, second, col + c + kCols, row);
+              else asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < kSumColumns; c += kCols) {
+          if (c < most) {
+            free_buffers(1);
+            const uint32_t at = next_buffer();
+            lay(acc + c, at);
+            hand_over();
+            if (lane == 0) bulk_store_2d(map, at, col + c, row);
+          }
+        }
+      }
+    };
+    using Wide = std::integral_constant<int, 64>;
+    using Narrow = std::integral_constant<int, 32>;
+    auto halves = [](float a, float b) { return half2_bits(a, b); };
+    auto bf16s = [](float a, float b) { return bf162_bits(a, b); };
     for (int u = pair; u < units && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live, plan);
       const int row0 = w.m0 + (int)rank * kHalf + quarter * 32, row = row0 + lane;
@@ -598,44 +657,15 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           for (int i = 0; i < kSumColumns; ++i) sum += acc[i];
           if (on) p.sums[(size_t)row * p.sum_blocks + col0 / cols] = make_float2(power, sum);
           if (KIND == P_EXP) {
-            constexpr int kCols = kFloats ? 32 : 64;
-#pragma unroll
-            for (int c = 0; c < kSumColumns; c += kCols) {
-              if (c >= (valid + kBK - 1) / kBK * kBK) continue;          // beyond the padded row
-              const uint32_t at = next_buffer();
-#pragma unroll
-              for (uint32_t q = 0; q < 8; ++q) {
-                if (!kFloats) {
-                  const int i = c + 8 * (int)q;
-                  st_shared_v4(at + piece_at((uint32_t)lane, q), half2_bits(acc[i % kSumColumns], acc[(i + 1) % kSumColumns]),
-                               half2_bits(acc[(i + 2) % kSumColumns], acc[(i + 3) % kSumColumns]),
-                               half2_bits(acc[(i + 4) % kSumColumns], acc[(i + 5) % kSumColumns]),
-                               half2_bits(acc[(i + 6) % kSumColumns], acc[(i + 7) % kSumColumns]));
-                } else {
-                  const int i = c + 4 * (int)q;
-                  st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
-                               __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
-                }
-              }
-              hand_over(&p.out, at, col0 + c, row0);
-            }
+            // (up to the end of the padded row)
+            const int most = (valid + kBK - 1) / kBK * kBK;
+            if constexpr (kFloats) store_all(acc, lay_floats, Narrow{}, &p.out, col0, row0, most);
+            else store_all(acc, [&](const float* v, uint32_t at) { lay_pairs(v, at, halves); }, Wide{}, &p.out, col0, row0, most);
           }
         }
       } else if (KIND == P_DH || w.share >= 0) {
-#pragma unroll
-        for (int c = 0; c < kSumColumns; c += 32) {
-          if (col0 + c < p.dim) {
-            const uint32_t at = next_buffer();
-#pragma unroll
-            for (uint32_t q = 0; q < 8; ++q) {
-              const int i = c + 4 * (int)q;
-              st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
-                           __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
-            }
-            if (w.share < 0) hand_over(&p.out, at, col0 + c, row0);
-            else hand_over(&p.acc, at, col0 + c - w.n0, w.share * kTile + row0 - w.m0);
-          }
-        }
+        if (w.share < 0) store_all(acc, lay_floats, Narrow{}, &p.out, col0, row0, p.dim - col0);
+        else store_all(acc, lay_floats, Narrow{}, &p.acc, col0 - w.n0, w.share * kTile + row0 - w.m0, p.dim - col0);
       } else {
         // sums over earlier pieces come from, and unless this is the last go back to, a float array of their own
         const bool add = p.first > 0, last = p.first + p.piece >= p.info->live;
@@ -655,48 +685,30 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           }
         }
         if (row0 >= p.vocab) continue;
-        if (last && p.dw_bf16) {
+        const int left = p.dim - col0;
+        if (!last) {
+          store_all(acc, lay_floats, Narrow{}, &p.acc, col0, row0, left);
+        } else if (p.dw_engine) {
+          if (p.dw_bf16) store_all(acc, [&](const float* v, uint32_t at) { lay_pairs(v, at, bf16s); }, Wide{}, &p.out, col0, row0, left);
+          else store_all(acc, lay_floats, Narrow{}, &p.out, col0, row0, left);
+        } else if (p.dw_bf16) {
 #pragma unroll
           for (int c = 0; c < kSumColumns; c += 64) {
-            if (col0 + c < p.dim) {
-              const uint32_t at = next_buffer();
-#pragma unroll
-              for (uint32_t q = 0; q < 8; ++q) {
-                const int i = c + 8 * (int)q;
-                st_shared_v4(at + piece_at((uint32_t)lane, q), bf162_bits(acc[i], acc[i + 1]), bf162_bits(acc[i + 2], acc[i + 3]),
-                             bf162_bits(acc[i + 4], acc[i + 5]), bf162_bits(acc[i + 6], acc[i + 7]));
-              }
-              if (p.dw_engine) {
-                hand_over(&p.out, at, col0 + c, row0);
-              } else {
-                __syncwarp();
-                store_rows<unsigned short, 2>(at, static_cast<unsigned short*>(p.dw) + (size_t)row0 * p.ld_dw + col0 + c, p.ld_dw,
-                                              p.vocab - row0, p.dim - (col0 + c), lane);
-                __syncwarp();
-              }
+            if (c < left) {
+              __syncwarp();
+              lay_pairs(acc + c, sbuf, bf16s);
+              __syncwarp();
+              store_rows<unsigned short, 2>(sbuf, static_cast<unsigned short*>(p.dw) + (size_t)row0 * p.ld_dw + col0 + c, p.ld_dw, p.vocab - row0, left - c, lane);
             }
           }
         } else {
 #pragma unroll
           for (int c = 0; c < kSumColumns; c += 32) {
-            if (col0 + c < p.dim) {
-              const uint32_t at = next_buffer();
-#pragma unroll
-              for (uint32_t q = 0; q < 8; ++q) {
-                const int i = c + 4 * (int)q;
-                st_shared_v4(at + piece_at((uint32_t)lane, q), __float_as_uint(acc[i]), __float_as_uint(acc[i + 1]),
-                             __float_as_uint(acc[i + 2]), __float_as_uint(acc[i + 3]));
-              }
-              if (!last) {
-                hand_over(&p.acc, at, col0 + c, row0);
-              } else if (p.dw_engine) {
-                hand_over(&p.out, at, col0 + c, row0);
-              } else {
-                __syncwarp();
-                store_rows<uint32_t, 1>(at, static_cast<uint32_t*>(p.dw) + (size_t)row0 * p.ld_dw + col0 + c, p.ld_dw, p.vocab - row0,
-                                        p.dim - (col0 + c), lane);
-                __syncwarp();
-              }
+            if (c < left) {
+              __syncwarp();
+              lay_floats(acc + c, sbuf);
+              __syncwarp();
+              store_rows<uint32_t, 1>(sbuf, static_cast<uint32_t*>(p.dw) + (size_t)row0 * p.ld_dw + col0 + c, p.ld_dw, p.vocab - row0, left - c, lane);
             }
           }
         }
@@ -1365,7 +1377,9 @@ mw_status out_map(CUtensorMap* out, CUtensorMapDataType type, int size, const vo
 
 template <int MODE, int KIND>
 mw_status run_product_in(ProductArgs& p, int64_t most_units, cudaStream_t s) {
-  if (!of_logits(KIND)) p.a_stage = terms_a(MODE, KIND) * kPlaneBytes;
+  // (A of few rows is short; dW's rows are the vocabulary's)
+  p.a_term = KIND == P_DW ? kPlaneBytes : (uint32_t)p.a_rows * (kBK * 2);
+  p.a_stage = terms_a(MODE, KIND) * p.a_term;
   p.buffers = buffers_for(MODE, KIND, p.blocks_k);
   p.most_blocks = piece_blocks(MODE, KIND, p.piece <= kTile);
   p.stages = stages_for(p.buffers, p.a_stage + terms_b(MODE) * kPlaneBytes);
@@ -1481,13 +1495,13 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     const int64_t held = kHeldBytes / ((int64_t)kTile * l.padded * 2 * TERMS);
     logits.group_rows = held < 8 ? 8 : (int)held;
     logits.idesc = instruction(bf16, false, false, logits.tile_n);
-    // Few rows: only theirs are copied, the others' products come out as whatever they are and are not read.  (One term
-    // alone: the planes of two lie a whole share apart.)  The path from L2 is the limit there: 16 rows of 32768x2048
-    // bf16 40 us with all 256 rows copied, half of it with 16.
-    logits.a_even = TERMS == 1 && a.rows <= kHalf;
-    const int box_rows = !logits.a_even ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
-    logits.a_stage = TERMS * (uint32_t)box_rows * kBK * 2;
-    MW_TRY(direct ? row_map(&logits.a, bf16, h, a.dim, a.rows, a.ld_h, 1, box_rows) : row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, box_rows));
+    // Few rows: only theirs are copied, the others' products come out as whatever they are and are not read.  (16 rows of
+    // 32768x2048 fp32: 175 us with all 256 rows copied.)
+    p.a_even = a.rows <= kHalf;
+    p.a_rows = !p.a_even ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
+    logits.a_even = by_h.a_even = p.a_even;
+    logits.a_rows = by_h.a_rows = p.a_rows;
+    MW_TRY(direct ? row_map(&logits.a, bf16, h, a.dim, a.rows, a.ld_h, 1, p.a_rows) : row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, p.a_rows));
     MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1, logits.tile_n / 2)
                       : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
     if (gradient) {
@@ -1499,7 +1513,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       by_h.tiles_n = ceil_div(a.dim, kTile);
       by_h.blocks_k = l.vpadded / kBK;
       by_h.idesc = instruction(bf16, false, true);
-      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, kHalf, 1));
+      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, p.a_rows, 1));
       MW_TRY(l.few ? group_map(&by_h.b, w, a.dim, a.vocab, a.ld_w * 2, 128, 128, 1, kBK, 2)
                    : group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, 2));
       MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece_rows, l.padded));
