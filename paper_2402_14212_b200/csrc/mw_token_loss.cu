@@ -63,6 +63,9 @@ __host__ __device__ constexpr int terms_a(int mode, int kind) { return mode == M
 __host__ __device__ constexpr int terms_b(int mode) { return mode == M_TWO ? 2 : 1; }
 __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ? 3 : (mode == M_FEW ? 2 : 1); }      // of dz
 constexpr int kFewRows = 128;
+// Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long as
+// the vocabulary's way through memory (16 rows of 32768x2048 bf16: 36.5 us by pairs).
+__host__ __device__ constexpr uint32_t plane_b(bool pair) { return pair ? kPlaneBytes : 2 * kPlaneBytes; }     // a term of B in a CTA
 // Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
 // few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
 constexpr int kStagesMax = 12;
@@ -137,7 +140,8 @@ struct alignas(64) ProductArgs {
   int vocab, dim;
   int tiles_m, tiles_n;     // of the whole piece (P_DW: of the vocabulary and the columns)
   int blocks_k;
-  int pairs;                // CTA pairs that the device holds
+  int workers;              // CTA pairs that the device holds, or CTAs where each has tiles of its own
+  int share_room;           // blocks of 256 x 256 sums
   int sum_blocks;           // P_SUMS, P_EXP: blocks of 128 logits a row
   uint32_t idesc;
   int stages, buffers;
@@ -151,7 +155,6 @@ struct alignas(64) ProductArgs {
   int index_bytes;
   uint32_t a_stage, a_term; // bytes of A in a stage of a CTA, and from a term to the next
   int a_rows;               // rows of A that are copied into a CTA
-  int a_even;               // A's copies are the even CTA's alone: its rows hold all there are
   float scale;
   int scaled;
   float2* sums;             // [row][sum_blocks]: power, sum
@@ -165,21 +168,21 @@ struct alignas(64) ProductArgs {
   int64_t ld_partial;
 };
 
-// How dh's tiles are laid over the pairs: waves of whole tiles, then the rest of them with K in shares, so that the last
+// How dh's tiles are laid over the pairs (CTAs, of few rows): waves of whole tiles, then the rest of them with K in shares, so that the last
 // wave is as short as the others leave it (4096 rows and 2048 columns are 128 tiles on 74 pairs: 1.75 waves with the last
 // 54 in four, 2 without).  The shares' sums, beyond the first, lie in blocks of their own and are added in order.
 struct DhPlan { int whole, rest, shares; };
-__host__ __device__ constexpr int share_blocks(int pairs) { return 4 * pairs; }      // most of them
+constexpr int share_blocks(int pairs) { return 4 * pairs; }      // most of them
 // (a warp calls it, a lane a number of shares)
-__device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, int pairs, int products) {
+__device__ __forceinline__ DhPlan dh_plan(int live, int tiles_n, int blocks_k, int workers, int room, int products) {
   const int tiles = (live + kTile - 1) / kTile * tiles_n;
   DhPlan d;
-  d.whole = tiles / pairs * pairs;
+  d.whole = tiles / workers * workers;
   d.rest = tiles - d.whole;
   // cycles: a K block's products, what a tile costs beyond them, a sum's way through memory at 4.6 KB a cycle
   const int s = (int)(threadIdx.x & 31) + 1, per = (blocks_k + s - 1) / s;
-  const bool can = s == 1 || (per >= 8 && d.rest * s <= share_blocks(pairs));
-  const unsigned cost = (unsigned)((d.rest * s + pairs - 1) / pairs) * (unsigned)(per * products * 512 + 3000) + (unsigned)(d.rest * s) * 114u;
+  const bool can = s == 1 || (per >= 8 && d.rest * s <= room);
+  const unsigned cost = (unsigned)((d.rest * s + workers - 1) / workers) * (unsigned)(per * products * 512 + 3000) + (unsigned)(d.rest * s) * 114u;
   const unsigned least = __reduce_min_sync(0xffffffffu, can ? cost : 0xffffffffu);
   d.shares = __ffs(__ballot_sync(0xffffffffu, can && cost == least));
   return d;
@@ -329,7 +332,7 @@ __device__ __forceinline__ void store_rows(uint32_t at, V* to, int64_t ld, int r
   }
 }
 
-template <int MODE, int KIND>
+template <int MODE, int KIND, bool PAIR>
 __global__ void __launch_bounds__(kLossThreads, 1)
 loss_products_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
@@ -337,7 +340,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   constexpr bool kFloats = MODE != M_ONE;          // exponentials are float
   // two blocks a fence (not where that spills a tile's floats)
   constexpr bool kPairs = (MODE == M_ONE && KIND == P_EXP) || (MODE != M_TWO && KIND == P_DW);
-  constexpr uint32_t b_stage = kTermsB * kPlaneBytes;
+  constexpr uint32_t b_stage = kTermsB * plane_b(PAIR);
+  constexpr int kShareB = PAIR ? kHalf : kTile;          // of a tile's columns
   __shared__ __align__(8) uint64_t full_bar[kStagesMax];
   __shared__ __align__(8) uint64_t empty_bar[kStagesMax];
   __shared__ __align__(8) uint64_t acc_full[2];
@@ -346,11 +350,11 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   __shared__ int abort_flag;
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_cta_rank();
+  const uint32_t rank = PAIR ? cluster_cta_rank() : 0u;
   const int stages = p.stages;
   const uint32_t a_stage = p.a_stage;
   const uint32_t a_tiles = (smem_u32(smem_raw) + 1023u) & ~1023u, b_tiles = a_tiles + (uint32_t)stages * a_stage;
-  const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
+  const int pairs = (int)(PAIR ? gridDim.x >> 1 : gridDim.x), pair = (int)(PAIR ? blockIdx.x >> 1 : blockIdx.x);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
@@ -359,19 +363,24 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&acc_full[s]), 1);
-      mbar_init(smem_u32(&acc_empty[s]), kEpi * 2);
+      mbar_init(smem_u32(&acc_empty[s]), PAIR ? kEpi * 2 : kEpi);
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();
+  if (PAIR) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   WaitCtx wc;
@@ -383,7 +392,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     reinterpret_cast<unsigned*>(p.clear)[threadIdx.x] = 0;
   const int live = live_rows<KIND>(p);
   DhPlan plan = {0, 0, 1};
-  if (KIND == P_DH) plan = dh_plan(live, p.tiles_n, p.blocks_k, p.pairs, products_of(MODE));
+  if (KIND == P_DH) plan = dh_plan(live, p.tiles_n, p.blocks_k, p.workers, p.share_room, products_of(MODE));
   const int units = unit_count<KIND>(p, live, plan);
 
   constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
@@ -397,29 +406,29 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     const bool of_a = warp == 0;
     uint32_t stage = 0, phase = 0;
     const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
-    const uint32_t full0_even = map_to_cta(full0, 0u);
-    const uint32_t tx = (p.a_even ? 1u : 2u) * a_stage + 2u * (KIND == P_SUMS ? b_stage / kHalf * (uint32_t)(p.tile_n / 2) : b_stage);
-    const bool idle = of_a && rank != 0 && p.a_even;
+    const uint32_t full0_even = PAIR ? map_to_cta(full0, 0u) : full0;
+    const int share_n = KIND == P_SUMS ? (PAIR ? p.tile_n / 2 : p.tile_n) : kShareB;
+    const uint32_t tx = (PAIR ? 2u : 1u) * (a_stage + b_stage / kShareB * (uint32_t)share_n);
     bool ok = true;
-    for (int u = pair; u < units && ok && !idle; u += pairs) {
+    for (int u = pair; u < units && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live, plan);
-      const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * (KIND == P_SUMS ? p.tile_n / 2 : kHalf);
+      const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * share_n;
       for (int kb = w.kb0; kb < w.kb1; ++kb) {
-        ok = __all_sync(0xffffffffu, mbar_wait<true>(empty0 + 8u * stage, phase ^ 1u, wc, 1u));
+        ok = __all_sync(0xffffffffu, mbar_wait<PAIR>(empty0 + 8u * stage, phase ^ 1u, wc, 1u));
         if (!ok) break;
         if (elect_one()) {
           if (of_a && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
           const uint32_t fb = full0_even + 8u * stage;
           const uint32_t to = of_a ? a_tiles + stage * a_stage : b_tiles + stage * b_stage;
           if (KIND == P_SUMS || KIND == P_EXP) {
-            if (of_a) tma_load_3d<true>(to, &p.a, fb, kb * kBK, p.first + am, 0);
-            else tma_load_3d<true>(to, &p.b, fb, kb * kBK, bn, 0);
+            if (of_a) tma_load_3d<PAIR>(to, &p.a, fb, kb * kBK, p.first + am, 0);
+            else tma_load_3d<PAIR>(to, &p.b, fb, kb * kBK, bn, 0);
           } else if (KIND == P_DH) {
-            if (of_a) tma_load_4d<true>(to, &p.a, fb, 0, am, kb, 0);
-            else tma_load_4d<true>(to, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
+            if (of_a) tma_load_4d<PAIR>(to, &p.a, fb, 0, am, kb, 0);
+            else tma_load_4d<PAIR>(to, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
           } else {
-            if (of_a) tma_load_4d<true>(to, &p.a, fb, 0, kb * kBK, am >> 6, 0);
-            else tma_load_4d<true>(to, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
+            if (of_a) tma_load_4d<PAIR>(to, &p.a, fb, 0, kb * kBK, am >> 6, 0);
+            else tma_load_4d<PAIR>(to, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
           }
         }
         __syncwarp();
@@ -433,7 +442,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
       constexpr uint32_t a_base = (kTurnedA ? (8192u >> 4) : 1u) << 16, b_base = (kTurnedB ? (8192u >> 4) : 1u) << 16;
       constexpr uint32_t a_adv = kTurnedA ? (2048u >> 4) : (32u >> 4), b_adv = kTurnedB ? (2048u >> 4) : (32u >> 4);
-      constexpr uint32_t term_b = kPlaneBytes >> 4;
+      constexpr uint32_t term_b = plane_b(PAIR) >> 4;
       const uint32_t term_a = p.a_term >> 4;
       int j = 0;
       bool ok = true;
@@ -442,25 +451,25 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         const int piece = piece_of(p, w);
         for (int kb0 = w.kb0; kb0 < w.kb1 && ok; kb0 += piece, ++j) {
           const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
-          ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u));
+          ok = __all_sync(0xffffffffu, mbar_wait<PAIR>(smem_u32(&acc_empty[set]), aphase ^ 1u, wc, 2u));
           if (!ok) break;
           tc_fence_after();
           const uint32_t d = tmem_base + set * (uint32_t)kTile;
           const int kb1 = kb0 + piece < w.kb1 ? kb0 + piece : w.kb1;
           for (int kb = kb0; kb < kb1; ++kb) {
-            ok = __all_sync(0xffffffffu, mbar_wait<true>(full0 + 8u * stage, phase, wc, 3u));
+            ok = __all_sync(0xffffffffu, mbar_wait<PAIR>(full0 + 8u * stage, phase, wc, 3u));
             if (!ok) break;
             const uint32_t a0 = (a_tiles + stage * a_stage) >> 4 | a_base, b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < kBK / 16; ++k) {
                 const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
-                umma_bf16<true>(d, a, b, p.idesc, k > 0 || kb > kb0);
-                if (kTermsB == 2) umma_bf16<true>(d, a, b + term_b, p.idesc, 1u);
-                if (kTermsA == 2) umma_bf16<true>(d, a + term_a, b, p.idesc, 1u);
+                umma_bf16<PAIR>(d, a, b, p.idesc, k > 0 || kb > kb0);
+                if (kTermsB == 2) umma_bf16<PAIR>(d, a, b + term_b, p.idesc, 1u);
+                if (kTermsA == 2) umma_bf16<PAIR>(d, a + term_a, b, p.idesc, 1u);
               }
-              umma_commit<true>(empty0 + 8u * stage);
-              if (kb + 1 == kb1) umma_commit<true>(smem_u32(&acc_full[set]));
+              umma_commit<PAIR>(empty0 + 8u * stage);
+              if (kb + 1 == kb1) umma_commit<PAIR>(smem_u32(&acc_full[set]));
             }
             __syncwarp();
             if (++stage == (uint32_t)stages) { stage = 0; phase ^= 1u; }
@@ -571,7 +580,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
       for (int kb0 = w.kb0; kb0 < w.kb1; kb0 += piece) {
         const uint32_t set = (uint32_t)j & 1u, aphase = ((uint32_t)j >> 1) & 1u;
         ++j;
-        ok = __all_sync(0xffffffffu, mbar_wait<true>(smem_u32(&acc_full[set]), aphase, wc, 4u));
+        ok = __all_sync(0xffffffffu, mbar_wait<PAIR>(smem_u32(&acc_full[set]), aphase, wc, 4u));
         if (!ok) break;
         tc_fence_after();
         const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + set * (uint32_t)kTile + (uint32_t)(side * cols);
@@ -721,13 +730,15 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   if (warp == 0 && lane == 0 && abort_flag) {
     // a wait ran out: copies still in flight get a bounded time to land before the CTA retires
     for (int s = 0; s < stages; ++s)
-      for (uint32_t i = 0; i < 4096u && !mbar_try_wait<true>(smem_u32(&full_bar[s]), 0u); ++i) __nanosleep(256);
+      for (uint32_t i = 0; i < 4096u && !mbar_try_wait<PAIR>(smem_u32(&full_bar[s]), 0u); ++i) __nanosleep(256);
     if (p.total) *p.total = __int_as_float(0x7fffffff);       // (the kernels that follow see the status)
   }
-  cluster_sync_all();
+  if (PAIR) cluster_sync_all();
   tc_fence_after();
-  if (warp == 1)
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  if (warp == 1) {
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
 }
 
 // ---- rows -------------------------------------------------------------------------------------
@@ -1180,14 +1191,14 @@ __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2
 // dh of the piece's rows: the sums over the shares of K, in order, to the rows they belong to, four columns a thread
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
-dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, int tiles_n, int blocks_k, int pairs, int mode, int first,
+dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, int tiles_n, int blocks_k, int workers, int room, int mode, int first,
                int piece, const int* row, const LossInfo* info, T* dh) {
   after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
   float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? operand_exponent(info->w_max, terms_b(mode)) : 0)));
   if (info->st.code != 0) f = __int_as_float(0x7fffffff);
-  const DhPlan plan = dh_plan(live, tiles_n, blocks_k, pairs, products_of(mode));
+  const DhPlan plan = dh_plan(live, tiles_n, blocks_k, workers, room, products_of(mode));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)live * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
@@ -1270,11 +1281,10 @@ struct LossWs {
 };
 
 // Columns of a tile of few rows, whose time is the vocabulary's way through memory: as even a share for every pair as
-// the instructions allow, 64 at least (16 rows of 32768x2048: 147 tiles of 224 columns on 74 pairs, 128 of 256 leave 20
-// pairs idle for half the time).
-int logits_tile(int vocab) {
-  const int pairs = sm_count() / 2, waves = ceil_div(ceil_div(vocab, kTile), pairs);
-  const int n = (int)align_up((size_t)ceil_div(vocab, waves * pairs), 32);
+// the instructions allow, 64 at least (16 rows of 32768x2048: 147 tiles of 224 columns on 148 CTAs).
+int logits_tile(int vocab, int workers) {
+  const int waves = ceil_div(ceil_div(vocab, kTile), workers);
+  const int n = (int)align_up((size_t)ceil_div(vocab, waves * workers), 32);
   return n < 64 ? 64 : n;
 }
 
@@ -1356,7 +1366,7 @@ mw_status make_map(CUtensorMap* out, CUtensorMapDataType type, int rank, const v
              ? MW_OK : MW_ERR_CUDA;
 }
 // operand rows with K along them: boxes of 64 columns, 128 rows and all terms
-mw_status row_map(CUtensorMap* out, bool bf16, const void* base, int64_t cols, int64_t rows, int64_t ld, int terms, int box_rows = kHalf) {
+mw_status row_map(CUtensorMap* out, bool bf16, const void* base, int64_t cols, int64_t rows, int64_t ld, int terms, int box_rows) {
   const int64_t dims[3] = {cols, rows, terms}, strides[2] = {ld * 2, rows * ld * 2};
   const int box[3] = {kBK, box_rows, terms};
   return make_map(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dims, strides, box);
@@ -1375,50 +1385,57 @@ mw_status out_map(CUtensorMap* out, CUtensorMapDataType type, int size, const vo
   return make_map(out, type, 2, base, dims, strides, box);
 }
 
-template <int MODE, int KIND>
+template <int MODE, int KIND, bool PAIR>
 mw_status run_product_in(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   // (A of few rows is short; dW's rows are the vocabulary's)
   p.a_term = KIND == P_DW ? kPlaneBytes : (uint32_t)p.a_rows * (kBK * 2);
   p.a_stage = terms_a(MODE, KIND) * p.a_term;
   p.buffers = buffers_for(MODE, KIND, p.blocks_k);
   p.most_blocks = piece_blocks(MODE, KIND, p.piece <= kTile);
-  p.stages = stages_for(p.buffers, p.a_stage + terms_b(MODE) * kPlaneBytes);
+  p.stages = stages_for(p.buffers, p.a_stage + terms_b(MODE) * plane_b(PAIR));
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
-  auto kernel = loss_products_kernel<MODE, KIND>;
+  auto kernel = loss_products_kernel<MODE, KIND, PAIR>;
   if (!ready[dev]) {
     MW_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost));
     ready[dev] = true;
   }
-  const int64_t pairs = sm_count() / 2;
+  const int64_t each = PAIR ? 2 : 1, workers = sm_count() / each;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * (unsigned)(most_units < pairs ? (most_units < 1 ? 1 : most_units) : pairs));
+  cfg.gridDim = dim3((unsigned)(each * (most_units < workers ? (most_units < 1 ? 1 : most_units) : workers)));
   cfg.blockDim = dim3(kLossThreads);
   cfg.dynamicSmemBytes = kSmemMost;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = PAIR ? 2 : 1;
   ++g_launch_count;
   return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MW_OK : MW_ERR_CUDA;
 }
 
 template <int TERMS, int KIND>
-mw_status run_product(bool few, ProductArgs& p, int64_t most_units, cudaStream_t s) {
-  if constexpr (TERMS == 2) return run_product_in<M_TWO, KIND>(p, most_units, s);
-  else if constexpr (KIND == P_SUMS) return run_product_in<M_ONE, KIND>(p, most_units, s);
-  else return few ? run_product_in<M_FEW, KIND>(p, most_units, s) : run_product_in<M_ONE, KIND>(p, most_units, s);
+mw_status run_product(bool few, bool single, ProductArgs& p, int64_t most_units, cudaStream_t s) {
+  constexpr int kMode = TERMS == 2 ? M_TWO : M_ONE;
+  if constexpr (KIND == P_DW) {
+    if constexpr (TERMS == 1)
+      if (few) return run_product_in<M_FEW, KIND, true>(p, most_units, s);
+    return run_product_in<kMode, KIND, true>(p, most_units, s);
+  } else {
+    if constexpr (TERMS == 1 && KIND != P_SUMS)
+      if (few) return run_product_in<M_FEW, KIND, false>(p, most_units, s);
+    return single ? run_product_in<kMode, KIND, false>(p, most_units, s) : run_product_in<kMode, KIND, true>(p, most_units, s);
+  }
 }
 
 // fp32 accumulator, the operands' type, K across the rows of A and of B, N / 8, M / 16
-uint32_t instruction(bool bf16, bool turned_a, bool turned_b, int n = kTile) {
+uint32_t instruction(bool bf16, bool turned_a, bool turned_b, int m = kTile, int n = kTile) {
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((turned_a ? 1u : 0u) << 15) | ((turned_b ? 1u : 0u) << 16) |
-         ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+         ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
 template <typename T, typename I>
@@ -1480,7 +1497,11 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     p.piece = l.piece;
     p.sum_blocks = l.sum_blocks;
     p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
-    p.pairs = sm_count() / 2;
+    // (few rows: CTAs of their own)
+    const bool single = a.rows <= kHalf;
+    const int pairs = sm_count() / 2, tile_m = single ? kHalf : kTile;
+    p.workers = single ? sm_count() : pairs;
+    p.share_room = share_blocks(pairs);
     p.shares = 1;
     p.tile_n = kTile;
     ProductArgs logits = p, by_h = p, by_w = p;
@@ -1488,22 +1509,19 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     logits.clear = l.info;
     logits.targets = targets;
     logits.index_bytes = (int)sizeof(I);
-    if (direct) logits.tile_n = logits_tile(a.vocab);
+    if (direct) logits.tile_n = logits_tile(a.vocab, p.workers);
     logits.tiles_n = ceil_div(a.vocab, logits.tile_n);
     logits.sum_blocks = ceil_div(a.vocab, logits.tile_n / 2);
     logits.blocks_k = l.padded / kBK;
     const int64_t held = kHeldBytes / ((int64_t)kTile * l.padded * 2 * TERMS);
     logits.group_rows = held < 8 ? 8 : (int)held;
-    logits.idesc = instruction(bf16, false, false, logits.tile_n);
-    // Few rows: only theirs are copied, the others' products come out as whatever they are and are not read.  (16 rows of
-    // 32768x2048 fp32: 175 us with all 256 rows copied.)
-    p.a_even = a.rows <= kHalf;
-    p.a_rows = !p.a_even ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
-    logits.a_even = by_h.a_even = p.a_even;
-    logits.a_rows = by_h.a_rows = p.a_rows;
-    MW_TRY(direct ? row_map(&logits.a, bf16, h, a.dim, a.rows, a.ld_h, 1, p.a_rows) : row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, p.a_rows));
-    MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1, logits.tile_n / 2)
-                      : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS));
+    logits.idesc = instruction(bf16, false, false, tile_m, logits.tile_n);
+    // Few rows: only theirs are copied, the others' products come out as whatever they are and are not read.
+    logits.a_rows = by_h.a_rows = !single ? kHalf : (a.rows <= 16 ? 16 : (a.rows <= 32 ? 32 : (a.rows <= 64 ? 64 : kHalf)));
+    const int share_b = single ? kTile : kHalf;          // of a tile's columns in a CTA
+    MW_TRY(direct ? row_map(&logits.a, bf16, h, a.dim, a.rows, a.ld_h, 1, logits.a_rows) : row_map(&logits.a, bf16, l.h, l.padded, l.staged_rows, l.padded, TERMS, logits.a_rows));
+    MW_TRY(l.in_place ? row_map(&logits.b, bf16, w, a.dim, a.vocab, a.ld_w, 1, logits.tile_n * share_b / kTile)
+                      : row_map(&logits.b, bf16, l.w, l.padded, a.vocab, l.padded, TERMS, share_b));
     if (gradient) {
       // an exponential's place, and that of dz's terms: groups of 64, one term after the other
       const int held = l.few ? 2 : TERMS;
@@ -1512,12 +1530,12 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       // dh: K along the rows of dz and across those of W
       by_h.tiles_n = ceil_div(a.dim, kTile);
       by_h.blocks_k = l.vpadded / kBK;
-      by_h.idesc = instruction(bf16, false, true);
-      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, p.a_rows, 1));
-      MW_TRY(l.few ? group_map(&by_h.b, w, a.dim, a.vocab, a.ld_w * 2, 128, 128, 1, kBK, 2)
-                   : group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, 2));
+      by_h.idesc = instruction(bf16, false, true, tile_m);
+      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, by_h.a_rows, 1));
+      MW_TRY(l.few ? group_map(&by_h.b, w, a.dim, a.vocab, a.ld_w * 2, 128, 128, 1, kBK, share_b / 64)
+                   : group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, share_b / 64));
       MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece_rows, l.padded));
-      MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)share_blocks(p.pairs) * kTile, kTile));
+      MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)p.share_room * kTile, kTile));
       // dW: K across the rows of both
       by_w.tiles_m = ceil_div(a.vocab, kTile);
       by_w.tiles_n = ceil_div(a.dim, kTile);
@@ -1527,8 +1545,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
       // tiles for less than half of the pairs: each in shares of K, of eight blocks at least
       const int tiles = by_w.tiles_m * by_w.tiles_n;
-      if (2 * tiles <= p.pairs && by_w.blocks_k >= 16) {
-        by_w.shares = p.pairs / tiles < by_w.blocks_k / 8 ? p.pairs / tiles : by_w.blocks_k / 8;
+      if (2 * tiles <= pairs && by_w.blocks_k >= 16) {
+        by_w.shares = pairs / tiles < by_w.blocks_k / 8 ? pairs / tiles : by_w.blocks_k / 8;
         by_w.out = by_h.acc;
         by_w.acc = by_h.acc;
       }
@@ -1544,7 +1562,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       logits.first = by_h.first = by_w.first = (int)first;
       if (a.rows > 0) {
         if (gradient) {
-          MW_TRY((run_product<TERMS, P_EXP>(l.few, logits, tm * logits.tiles_n, s)));
+          MW_TRY((run_product<TERMS, P_EXP>(l.few, single, logits, tm * logits.tiles_n, s)));
           // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of them waits of
           // one row after another)
           const bool short_rows = a.vocab <= 4096;
@@ -1555,7 +1573,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
                               l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part,
                               first + l.piece >= a.rows ? total : nullptr, l.e, l.vpadded));
         } else {
-          MW_TRY((run_product<TERMS, P_SUMS>(false, logits, tm * logits.tiles_n, s)));
+          MW_TRY((run_product<TERMS, P_SUMS>(false, single, logits, tm * logits.tiles_n, s)));
           const unsigned blocks = (unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide);          // (a warp a row)
           if (direct)
             MW_TRY(launch_after(direct_rows_kernel<I>, blocks, 256, 0, s, l.info, l.sums, logits.sum_blocks, logits.tile_n / 2, l.target_z, targets, weight, (int)a.rows,
@@ -1565,14 +1583,14 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
                                 total));
         }
         if (dh) {
-          MW_TRY((run_product<TERMS, P_DH>(l.few, by_h, p.pairs, s)));
+          MW_TRY((run_product<TERMS, P_DH>(l.few, single, by_h, p.workers, s)));
           auto rows_kernel = ((uintptr_t)dh & 15) == 0 && a.ld_dh % 4 == 0 && a.dim % 4 == 0 ? dh_rows_kernel<T, true> : dh_rows_kernel<T, false>;
-          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.shares, l.padded, by_h.tiles_n, by_h.blocks_k, p.pairs, mode, (int)first, l.piece,
+          MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.shares, l.padded, by_h.tiles_n, by_h.blocks_k, p.workers, p.share_room, mode, (int)first, l.piece,
                               l.row, l.info, dh));
         }
       }
       if (dw) {
-        MW_TRY((run_product<TERMS, P_DW>(l.few, by_w, (int64_t)by_w.tiles_m * by_w.tiles_n * by_w.shares, s)));
+        MW_TRY((run_product<TERMS, P_DW>(l.few, false, by_w, (int64_t)by_w.tiles_m * by_w.tiles_n * by_w.shares, s)));
         if (by_w.shares > 1) {
           if (dw_bf16)
             MW_TRY(launch_after(dw_rows_kernel<__nv_bfloat16>, wide, 256, 0, s, a, l.shares, by_w.tiles_n, by_w.shares, mode, (int)first, l.piece,
