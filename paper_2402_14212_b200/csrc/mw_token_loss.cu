@@ -1071,23 +1071,27 @@ direct_rows_kernel(LossInfo* info, const float2* sums, int sum_blocks, int colum
   total_by_last(info, rows, part, total);
 }
 
-// a row's exponentials -> dz times a power of two, in their place: WARPS warps of a block of eight a row
+// a row's exponentials -> dz times a power of two, in their place: WARPS warps of a block of eight a row, or `slices`
+// blocks where rows are few and long (each joins the row's sums for itself)
 template <int MODE, int WARPS>
 __global__ void __launch_bounds__(256)
 dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_blocks, const float* target_z, const int* row,
-          const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int padded) {
+          const int* target, const float* g, float* loss, double* part, float* total, unsigned short* e, int padded, int slices) {
   after_previous();
   __shared__ RowSum warp_v[8];
   constexpr int kThreads = WARPS * 32, kRows = 8 / WARPS, TERMS = MODE == M_ONE ? 1 : 2;
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
-  const int upto = (live + kBK - 1) / kBK * kBK;
+  int upto = (live + kBK - 1) / kBK * kBK;            // (behind the piece's rows the copy engine brings zeros)
+  upto = upto < piece ? upto : piece;
   const int warp = WARPS == 1 ? 0 : (int)(threadIdx.x >> 5), lane = threadIdx.x & 31, thread = (int)threadIdx.x % kThreads;
   const float to_range = __uint_as_float((unsigned)(127 + range_exponent(info->g_max)) << 23);
-  for (int r = (int)blockIdx.x * kRows + (WARPS == 1 ? (int)(threadIdx.x >> 5) : 0); r < upto; r += gridDim.x * kRows) {
+  for (int b = (int)blockIdx.x; b * kRows < upto * slices; b += gridDim.x) {
+    const int slice = b % slices, r = b / slices * kRows + (WARPS == 1 ? (int)(threadIdx.x >> 5) : 0);
+    if (WARPS == 1 && r >= upto) break;
     unsigned short* at = e + (size_t)r * padded * TERMS;
     if (r >= live) {                                  // rows that fill up the last block of K
-      for (int c = thread; c < padded * TERMS / 8; c += kThreads) reinterpret_cast<uint4*>(at)[c] = make_uint4(0u, 0u, 0u, 0u);
+      for (int c = slice * kThreads + thread; c < padded * TERMS / 8; c += slices * kThreads) reinterpret_cast<uint4*>(at)[c] = make_uint4(0u, 0u, 0u, 0u);
       continue;
     }
     const float2* mine = sums + (size_t)r * sum_blocks;
@@ -1103,7 +1107,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       for (int w = 1; w < WARPS; ++w) v = join(v, warp_v[w]);
     }
     const RowEnd end = row_end(info, v, target_z[i], mine[t / kSumColumns].x);
-    if (thread == 0) {
+    if (thread == 0 && slice == 0) {
       loss[row[i]] = end.loss;
       part[i] = (double)g[i] * (double)end.loss;
     }
@@ -1111,7 +1115,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
     // (four accesses of a thread under way)
     constexpr int kAhead = 4;
     if (TERMS == 1) {
-      for (int c0 = thread * 8; c0 < padded; c0 += kThreads * 8 * kAhead) {
+      for (int c0 = (slice * kAhead * kThreads + thread) * 8; c0 < padded; c0 += slices * kThreads * 8 * kAhead) {
         uint4 raw[kAhead];
         float f[kAhead];
 #pragma unroll
@@ -1148,7 +1152,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       }
     } else {
       // a group of 64 floats becomes 64 leading terms and 64 remainders: sixteen lanes, four of them each
-      for (int c0 = warp * 128 + lane * 4; c0 - lane * 4 < padded; c0 += WARPS * 128 * kAhead) {          // (a warp together)
+      for (int c0 = (slice * kAhead * WARPS + warp) * 128 + lane * 4; c0 - lane * 4 < padded; c0 += slices * WARPS * 128 * kAhead) {          // (a warp together)
         float4 raw[kAhead];
         float f[kAhead];
 #pragma unroll
@@ -1275,7 +1279,7 @@ struct LossWs {
   float2* sums;
   unsigned short *h, *w, *e;
   float *slab, *shares, *dw;
-  int blocks, piece, padded, vpadded, sum_blocks, staged_rows, piece_rows;
+  int blocks, piece, padded, vpadded, sum_blocks, staged_rows;
   bool few;               // M_FEW
   bool in_place;          // W is read where it lies
 };
@@ -1317,7 +1321,6 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
     if (piece > d->rows) piece = d->rows ? d->rows : 1;
   }
   l->piece = (int)piece;
-  l->piece_rows = (int)align_up((size_t)piece, kTile);
   l->info = (LossInfo*)take(sizeof(LossInfo));
   l->counts = (int*)take((size_t)l->blocks * 4);
   l->row = (int*)take(n * 4);
@@ -1329,8 +1332,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->sums = (float2*)take((size_t)l->piece * (n <= kTile ? ceil_div(d->vocab, 32) : l->sum_blocks) * 8);
   l->h = (unsigned short*)take((size_t)l->staged_rows * l->padded * 2 * terms);
   l->w = (unsigned short*)take(l->in_place ? 0 : v * l->padded * 2 * terms);
-  l->e = (unsigned short*)take(gradient ? (size_t)l->piece_rows * l->vpadded * 2 * held : 0);
-  l->slab = (float*)take(gradient ? (size_t)l->piece_rows * l->padded * 4 : 0);
+  l->e = (unsigned short*)take(gradient ? (size_t)l->piece * l->vpadded * 2 * held : 0);
+  l->slab = (float*)take(gradient ? (size_t)l->piece * l->padded * 4 : 0);
   l->shares = (float*)take(gradient ? (size_t)share_blocks(sm_count() / 2) * kTile * kTile * 4 : 0);
   l->dw = (float*)take(gradient && l->piece < d->rows ? v * l->padded * 4 : 0);
   return at;
@@ -1526,22 +1529,22 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       // an exponential's place, and that of dz's terms: groups of 64, one term after the other
       const int held = l.few ? 2 : TERMS;
       const int64_t row_bytes = (int64_t)l.vpadded * 2 * held, group_bytes = 128 * held, hw_bytes = (int64_t)l.padded * 2;
-      MW_TRY(out_map(&logits.out, held == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2 * held, l.e, l.vpadded, l.piece_rows, l.vpadded));
+      MW_TRY(out_map(&logits.out, held == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2 * held, l.e, l.vpadded, l.piece, l.vpadded));
       // dh: K along the rows of dz and across those of W
       by_h.tiles_n = ceil_div(a.dim, kTile);
       by_h.blocks_k = l.vpadded / kBK;
       by_h.idesc = instruction(bf16, false, true, tile_m);
-      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, by_h.a_rows, 1));
+      MW_TRY(group_map(&by_h.a, l.e, l.vpadded, l.piece, row_bytes, group_bytes, 128, held, by_h.a_rows, 1));
       MW_TRY(l.few ? group_map(&by_h.b, w, a.dim, a.vocab, a.ld_w * 2, 128, 128, 1, kBK, share_b / 64)
                    : group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, share_b / 64));
-      MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece_rows, l.padded));
+      MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece, l.padded));
       MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)p.share_room * kTile, kTile));
       // dW: K across the rows of both
       by_w.tiles_m = ceil_div(a.vocab, kTile);
       by_w.tiles_n = ceil_div(a.dim, kTile);
       by_w.blocks_k = ceil_div(l.piece, kBK);
       by_w.idesc = instruction(bf16, true, true);
-      MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece_rows, row_bytes, group_bytes, 128, held, kBK, 2));
+      MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece, row_bytes, group_bytes, 128, held, kBK, 2));
       MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
       // tiles for less than half of the pairs: each in shares of K, of eight blocks at least
       const int tiles = by_w.tiles_m * by_w.tiles_n;
@@ -1566,12 +1569,14 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
           // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of them waits of
           // one row after another)
           const bool short_rows = a.vocab <= 4096;
-          const int dz_blocks = short_rows ? ceil_div(l.piece_rows, 8) : l.piece_rows;
+          const int most = 2 * sm_count() / l.piece, parts = ceil_div(l.vpadded, TERMS == 2 || l.few ? 4096 : 8192);
+          const int slices = short_rows || most < 2 ? 1 : (most < parts ? most : parts);
+          const int dz_blocks = short_rows ? ceil_div(l.piece, 8) : l.piece * slices;
           constexpr int kMode = TERMS == 2 ? M_TWO : M_ONE, kOther = TERMS == 2 ? M_TWO : M_FEW;
           auto dz = l.few ? (short_rows ? dz_kernel<kOther, 1> : dz_kernel<kOther, 8>) : (short_rows ? dz_kernel<kMode, 1> : dz_kernel<kMode, 8>);
           MW_TRY(launch_after(dz, (unsigned)(dz_blocks < (int)wide ? dz_blocks : wide), 256, 0, s,
                               l.info, (int)first, l.piece, l.sums, l.sum_blocks, l.target_z, l.row, l.target, l.g, loss, l.part,
-                              first + l.piece >= a.rows ? total : nullptr, l.e, l.vpadded));
+                              first + l.piece >= a.rows ? total : nullptr, l.e, l.vpadded, slices));
         } else {
           MW_TRY((run_product<TERMS, P_SUMS>(false, single, logits, tm * logits.tiles_n, s)));
           const unsigned blocks = (unsigned)(a.rows < wide * 8 ? ceil_div(a.rows, 8) : wide);          // (a warp a row)
