@@ -76,11 +76,11 @@ constexpr int stages_for(int buffers, uint32_t stage) {
   return n < kStagesMax ? n : kStagesMax;
 }
 // Buffers of an epilogue warp: one, which leaves the most stages, unless a tile has so few K blocks that its way out is
-// what takes the time.
+// what takes the time (dW of 66235x2048 bf16: 200 rows 97 us with one, 95 with two and four; 500 rows 112, 124, 144; the
+// exponentials of 2048 rows of 32768x768 91, 86, 96 and of 32768x1024 99, 103, 121; of fp32 x1024 282, 277, 444).
 constexpr int buffers_for(int mode, int kind, int blocks_k) {
   if (kind == P_SUMS) return 0;
-  if (kind == P_DH || blocks_k > 16) return 1;
-  return mode != M_TWO && blocks_k <= 8 ? 4 : 2;
+  return (kind == P_EXP && blocks_k <= (mode == M_TWO ? 24 : 12)) || (kind == P_DW && blocks_k <= 4) ? 2 : 1;
 }
 
 // K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
@@ -460,9 +460,12 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             ok = __all_sync(0xffffffffu, mbar_wait<PAIR>(full0 + 8u * stage, phase, wc, 3u));
             if (!ok) break;
             const uint32_t a0 = (a_tiles + stage * a_stage) >> 4 | a_base, b0 = (b_tiles + stage * b_stage) >> 4 | b_base;
+            // (sixteens of K behind the last row are zeros)
+            const int steps = KIND == P_DW && live - kb * kBK < kBK ? (live - kb * kBK + 15) / 16 : kBK / 16;
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < kBK / 16; ++k) {
+                if (KIND == P_DW && k >= steps) break;
                 const uint32_t a = a0 + (uint32_t)k * a_adv, b = b0 + (uint32_t)k * b_adv;
                 umma_bf16<PAIR>(d, a, b, p.idesc, k > 0 || kb > kb0);
                 if (kTermsB == 2) umma_bf16<PAIR>(d, a, b + term_b, p.idesc, 1u);
@@ -501,10 +504,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     // them at a time, since the fence between their stores and the copy engine is what a short tile waits for.
     auto free_buffers = [&](int group) {
       if (lane == 0) {
-        const int busy = buffers - group;
-        if (busy == 3) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
-        else if (busy == 2) asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory");
-        else if (busy == 1) bulk_wait_read_but_one();
+        if (buffers > group) bulk_wait_read_but_one();
         else bulk_wait_read_all();
       }
       __syncwarp();
