@@ -1072,7 +1072,7 @@ def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None,
     if stream is not None:
         return _on_stream(stream, h, token_loss_gradient, h, weight, targets, scale, row_weight, dh, dweight, grad_dtype,
                           want, piece_rows)
-    if weight.data_ptr() & 15:         # (of few rows read in place, by copies of 16 bytes)
+    if weight.data_ptr() & 15 and targets.numel() <= 128:         # (of few rows read in place, by copies of 16 bytes)
         weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(True, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight,
                        (bool(want[0]), bool(want[1])))

@@ -55,14 +55,17 @@ enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
 // How operands are held.  M_ONE: one term (bf16 as it is in the loss alone, half precision times a power of two in the
 // gradient).  M_TWO: fp32 as two half-precision terms.  M_FEW: the gradient of few rows of bf16, whose time is the
 // vocabulary's way through memory: W is read in place, by both products that want it, exponentials are float and dz two
-// bf16 terms against one of W and h.  That saves writing and reading W once more and costs a product more of dz each: up to
-// 128 rows of 16-byte aligned W (1 row of 66235x2624: 238 us, 411 in half precision; the two meet at about 230 rows).
+// bf16 terms against one of W and h.  That saves writing W once more and reading that, and costs wider exponentials and a
+// product more of dz each.  So it is for 16-byte aligned W of 24 MB and more, with eight columns to a row at least, and up to
+// 128 rows (half precision beside it: 1 row of 66235x2624 364 and 245 us, 128 rows 401 and 309; 128 rows of 16384x1024 77
+// and 73; but 16 rows of 33550x320 61 and 64 us, 128 rows 72 and 84, of 4096x512 44 and 49).
 enum { M_ONE = 1, M_TWO, M_FEW };
 constexpr bool of_logits(int kind) { return kind == P_SUMS || kind == P_EXP; }
 __host__ __device__ constexpr int terms_a(int mode, int kind) { return mode == M_TWO || (mode == M_FEW && kind >= P_DH) ? 2 : 1; }
 __host__ __device__ constexpr int terms_b(int mode) { return mode == M_TWO ? 2 : 1; }
 __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ? 3 : (mode == M_FEW ? 2 : 1); }      // of dz
 constexpr int kFewRows = 128;
+constexpr int64_t kFewNumbers = 12 << 20;
 // Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long as
 // the vocabulary's way through memory (16 rows of 32768x2048 bf16: 36.5 us by pairs).
 __host__ __device__ constexpr uint32_t plane_b(bool pair) { return pair ? kPlaneBytes : 2 * kPlaneBytes; }     // a term of B in a CTA
@@ -1302,7 +1305,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   const int terms = d->dtype == MW_F32 ? 2 : 1;
   const size_t n = (size_t)d->rows, v = (size_t)d->vocab, dim = (size_t)d->dim;
   const int64_t ld_w = d->ld_weight ? d->ld_weight : d->dim;
-  l->few = gradient && terms == 1 && d->rows > 0 && d->rows <= kFewRows && ld_w % 8 == 0 && d->dim % kBK == 0;
+  l->few = gradient && terms == 1 && d->rows > 0 && d->rows <= kFewRows && 8 * (int64_t)d->rows <= d->dim &&
+           (int64_t)d->vocab * d->dim >= kFewNumbers && ld_w % 8 == 0 && d->dim % kBK == 0;
   l->in_place = l->few || (!gradient && terms == 1 && ld_w % 8 == 0);
   const int held = l->few ? 2 : terms;          // half-precision numbers that an exponential takes
   l->blocks = ceil_div(d->rows, kIndexRows);
@@ -1567,8 +1571,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
         if (gradient) {
           MW_TRY((run_product<TERMS, P_EXP>(l.few, single, logits, tm * logits.tiles_n, s)));
           // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of them waits of
-          // one row after another)
-          const bool short_rows = a.vocab <= 4096;
+          // one row after another), several where rows are few (1 of 66235: 24 us, 10 in 17)
+          const bool short_rows = a.vocab <= 4096 && l.piece > 2 * sm_count();
           const int most = 2 * sm_count() / l.piece, parts = ceil_div(l.vpadded, TERMS == 2 || l.few ? 4096 : 8192);
           const int slices = short_rows || most < 2 ? 1 : (most < parts ? most : parts);
           const int dz_blocks = short_rows ? ceil_div(l.piece, 8) : l.piece * slices;

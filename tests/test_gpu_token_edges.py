@@ -207,3 +207,43 @@ def test_gradients_of_few_rows(N, V, D, kind):
     assert all(torch.equal(a, b) for a, b in zip(full, again)) and again.dh is own
     wide[:, 1:D + 1] = W.clone()                   # off the boundary: copied
     check(mwb.token_loss_gradient(h, wide[:, 1:D + 1], t, row_weight=w, grad_dtype=kind), want, ALL)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("N,V,D", [(1, 12353, 1088), (17, 13001, 1024), (64, 6151, 2112), (100, 12288, 1024), (128, 12353, 1088), (129, 12353, 1088), (8, 200000, 64)])
+def test_gradients_of_few_rows_and_a_large_weight(N, V, D, kind):
+    h, W, t = make(N, V, D, BF16, seed=N, left_out=0.3 if N > 1 else 0.0)
+    if N > 1:
+        t[N - 1] = V - 1
+        h[N - 1] = W[V - 1]
+    check(mwb.token_loss_gradient(h, W, t, grad_dtype=kind, scale=-1.3), reference(h, W, t, scale=-1.3), ALL)
+    w = torch.randn(N, device="cuda") * 1e-4 * (torch.arange(N, device="cuda") % 4 != 1)
+    h[1::4] = float("inf")                         # left out by their weight
+    want = reference(h * 2.0 ** 30, W * 2.0 ** -30, t, weight=w)
+    full = mwb.token_loss_gradient(h * 2.0 ** 30, W * 2.0 ** -30, t, row_weight=w, grad_dtype=kind)
+    check(full, want, ALL)
+    own, wide, out = h * 2.0 ** 30, torch.zeros(V, D + 8, device="cuda", dtype=BF16), torch.full((V, D + 7), 5.0, device="cuda", dtype=kind)
+    wide[:, 8:] = W * 2.0 ** -30
+    again = mwb.token_loss_gradient(own, wide[:, 8:], t, row_weight=w, grad_dtype=kind, dh=own, dweight=out[:, 3:D + 3])
+    assert all(torch.equal(a, b) for a, b in zip(full, again)) and again.dh is own
+    assert bool((out[:, :3] == 5).all() and (out[:, D + 3:] == 5).all())
+    part = mwb.token_loss_gradient(h * 2.0 ** 30, W * 2.0 ** -30, t, row_weight=w, grad_dtype=kind, piece_rows=1)
+    assert all(torch.equal(a, b) for a, b in zip(full, part))
+    if N > 2:
+        h, W, t = make(N, V, D, BF16, seed=N)
+        clean = mwb.token_loss_gradient(h, W, t)
+        h[2] = float("nan")
+        r = mwb.token_loss_gradient(h, W, t)
+        rest = torch.arange(N, device="cuda") != 2
+        assert bool(r.loss[2].isnan()) and bool(r.dh[2].isnan().all())
+        assert torch.equal(r.loss[rest], clean.loss[rest]) and torch.equal(r.dh[rest], clean.dh[rest])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V", [(1, 30000), (3, 20001), (70, 8300), (128, 8192), (129, 8193), (290, 700), (300, 700)])
+def test_rows_of_several_blocks(N, V, dtype):
+    h, W, t = make(N, V, 136, dtype, seed=V, left_out=0.2 if N > 1 else 0.0)
+    t[0] = V - 1
+    h[0] = W[V - 1]
+    check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
+    check(mwb.token_loss_gradient(h, W, t, piece_rows=256), reference(h, W, t), ALL)
