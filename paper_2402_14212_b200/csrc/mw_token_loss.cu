@@ -67,7 +67,8 @@ __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ?
 constexpr int kFewRows = 128;
 constexpr int64_t kFewNumbers = 12 << 20;
 // Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long as
-// the vocabulary's way through memory (16 rows of 32768x2048 bf16: 36.5 us by pairs).
+// the vocabulary's way through memory (loss of 16 rows of 32768x2048 bf16 36.5 us by pairs, 33.7 by CTAs, fp32 174 and 155;
+// gradients of 128 rows fp32 358 and 340; of 128 rows of 4096x512 fp32, whose 16 tiles leave most CTAs idle, 60 and 69).
 __host__ __device__ constexpr uint32_t plane_b(bool pair) { return pair ? kPlaneBytes : 2 * kPlaneBytes; }     // a term of B in a CTA
 // Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
 // few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
