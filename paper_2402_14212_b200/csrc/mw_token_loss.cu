@@ -90,9 +90,9 @@ constexpr int buffers_for(int mode, int kind, int blocks_k) {
 // K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
 // losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and 3.8e-7
 // with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
-// 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many: 16 rows of 32768x2048
-// 3.4e-7 (7.5e-7) in 36.5 us (34.7), of fp32 operands 3.9e-7 in the same time.  dz of bf16 operands has 11 bits: its sums
-// have 512 instructions, 2^-15 at the worst, and are read out seldom.
+// 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many at no cost (16 rows of
+// 32768x2048 33.7 us, fp32 153 us, either way): 3.4e-7 where twice as many leave 7.5e-7.  dz of bf16 operands has 11 bits:
+// its sums have 512 instructions, 2^-15 at the worst, and are read out seldom.
 constexpr int piece_blocks(int mode, int kind, bool few) {
   return mode == M_TWO ? (few ? 2 : 4) : (of_logits(kind) ? (few ? 8 : 16) : 128 / products_of(mode));
 }
