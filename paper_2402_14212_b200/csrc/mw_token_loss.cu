@@ -59,12 +59,15 @@ enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
 // product more of dz each.  So it is for 16-byte aligned W of 24 MB and more, with eight columns to a row at least, and up to
 // 128 rows (half precision beside it: 1 row of 66235x2624 364 and 245 us, 128 rows 401 and 309; 128 rows of 16384x1024 77
 // and 73; but 16 rows of 33550x320 61 and 64 us, 128 rows 72 and 84, of 4096x512 44 and 49).
-enum { M_ONE = 1, M_TWO, M_FEW };
+// M_THIN: very few rows, without the tensor cores (below).
+enum { M_ONE = 1, M_TWO, M_FEW, M_THIN };
 constexpr bool of_logits(int kind) { return kind == P_SUMS || kind == P_EXP; }
 __host__ __device__ constexpr int terms_a(int mode, int kind) { return mode == M_TWO || (mode == M_FEW && kind >= P_DH) ? 2 : 1; }
 __host__ __device__ constexpr int terms_b(int mode) { return mode == M_TWO ? 2 : 1; }
 __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ? 3 : (mode == M_FEW ? 2 : 1); }      // of dz
 constexpr int kFewRows = 128;
+constexpr int kThinRows = 8, kThinColumns = 64;
+constexpr int64_t kThinNumbers = 4 << 20, kThinDim = 512;
 constexpr int64_t kFewNumbers = 12 << 20;
 // Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long as
 // the vocabulary's way through memory (loss of 16 rows of 32768x2048 bf16 36.5 us by pairs, 33.7 by CTAs, fp32 174 and 155;
@@ -1084,12 +1087,13 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
   after_previous();
   __shared__ RowSum warp_v[8];
   constexpr int kThreads = WARPS * 32, kRows = 8 / WARPS, TERMS = MODE == M_ONE ? 1 : 2;
+  constexpr int kColumns = MODE == M_THIN ? kThinColumns : kSumColumns;
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
   int upto = (live + kBK - 1) / kBK * kBK;            // (behind the piece's rows the copy engine brings zeros)
-  upto = upto < piece ? upto : piece;
+  upto = MODE == M_THIN ? live : (upto < piece ? upto : piece);
   const int warp = WARPS == 1 ? 0 : (int)(threadIdx.x >> 5), lane = threadIdx.x & 31, thread = (int)threadIdx.x % kThreads;
-  const float to_range = __uint_as_float((unsigned)(127 + range_exponent(info->g_max)) << 23);
+  const float to_range = MODE == M_THIN ? 1.f : __uint_as_float((unsigned)(127 + range_exponent(info->g_max)) << 23);
   for (int b = (int)blockIdx.x; b * kRows < upto * slices; b += gridDim.x) {
     const int slice = b % slices, r = b / slices * kRows + (WARPS == 1 ? (int)(threadIdx.x >> 5) : 0);
     if (WARPS == 1 && r >= upto) break;
@@ -1110,7 +1114,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       v = warp_v[0];
       for (int w = 1; w < WARPS; ++w) v = join(v, warp_v[w]);
     }
-    const RowEnd end = row_end(info, v, target_z[i], mine[t / kSumColumns].x);
+    const RowEnd end = row_end(info, v, target_z[i], mine[t / kColumns].x);
     if (thread == 0 && slice == 0) {
       loss[row[i]] = end.loss;
       part[i] = (double)g[i] * (double)end.loss;
@@ -1127,7 +1131,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
           const int c = c0 + j * kThreads * 8;
           if (c < padded) {
             raw[j] = *reinterpret_cast<const uint4*>(at + c);
-            f[j] = mine[c / kSumColumns].x;
+            f[j] = mine[c / kColumns].x;
           }
         }
 #pragma unroll
@@ -1164,7 +1168,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
           const int c = c0 + j * WARPS * 128;
           if (c < padded) {
             raw[j] = *reinterpret_cast<const float4*>(at + 2 * c);
-            f[j] = mine[c / kSumColumns].x;
+            f[j] = mine[c / kColumns].x;
           }
         }
         __syncwarp();
@@ -1176,6 +1180,10 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
             float x[4] = {raw[j].x * by, raw[j].y * by, raw[j].z * by, raw[j].w * by};
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = c + q == t ? at_target : x[q];
+            if (MODE == M_THIN) {
+              *reinterpret_cast<float4*>(at + 2 * c) = make_float4(x[0], x[1], x[2], x[3]);
+              continue;
+            }
             unsigned short hi[4], lo[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -1274,6 +1282,306 @@ dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mod
   }
 }
 
+// ---- very few rows ----------------------------------------------------------------------------
+// Up to 8 rows of fp32 over a large W.  As operands W passes memory three times for the loss and five for the gradient; here
+// each kernel reads it once (or writes dW), in fp32 throughout, and the CUDA cores' multiplications stay below the time of
+// that.
+// A thread's four numbers of a group of 4 * STRIDE: together where rows allow 16 bytes at a time, else STRIDE apart.
+template <bool WIDE, int STRIDE>
+__device__ __forceinline__ int place(int i, int j) { return WIDE ? 4 * i + j : i + STRIDE * j; }
+__device__ __forceinline__ void load_wide(const float* from, float (&x)[4]) {
+  const float4 v = *reinterpret_cast<const float4*>(from);
+  x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+// zeros from `left` on (WIDE: a multiple of four)
+template <bool WIDE, int STRIDE>
+__device__ __forceinline__ void load_four(const float* from, int i, int left, float (&x)[4]) {
+  if (WIDE) {
+    if (4 * i < left) load_wide(from + 4 * i, x);
+    else x[0] = x[1] = x[2] = x[3] = 0.f;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = i + STRIDE * j < left ? from[i + STRIDE * j] : 0.f;
+  }
+}
+// Sums over a warp's lanes of N numbers each: afterwards a lane has number (lane * N + i) / 32 in v[i], i < N / 32 or one
+template <int N>
+__device__ __forceinline__ void sum_lanes(float (&v)[N], int lane) {
+  int m = N;
+#pragma unroll
+  for (int d = 16; d; d >>= 1) {
+    if (m > 1) {
+      m /= 2;
+      const bool upper = lane & d;
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        if (i < m) {
+          const float give = upper ? v[i] : v[i + m], keep = upper ? v[i + m] : v[i];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+        }
+      }
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+    }
+  }
+}
+
+// What P_SUMS (and, with `e`, P_EXP) leave, by blocks of 64 logits: a warp takes four rows of W at a time against all rows
+// of h, which lie in shared memory, whole or `chunk` columns of them.
+template <int R, bool WIDE>
+__global__ void __launch_bounds__(512, 1)
+thin_logits_kernel(const float* h, int64_t ld_h, const float* w, int64_t ld_w, int rows, int vocab, int dim, int chunk, float factor, LossInfo* info,
+                   const int* row, const int* target, const void* targets, int index_bytes, float2* sums, int sum_blocks, float* target_z,
+                   float* e, int padded) {
+  extern __shared__ __align__(16) float hs[];          // [R][chunk]
+  __shared__ float zs[2][R][kThinColumns];
+  after_previous();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (!row && blockIdx.x == 0 && threadIdx.x < sizeof(LossInfo) / 4) reinterpret_cast<unsigned*>(info)[threadIdx.x] = 0;
+  const int live = row ? info->live : rows;
+  if (live == 0) return;
+  int t = -1;
+  if (warp < live) {
+    if (row) {
+      t = target[warp];
+    } else {
+      const int64_t x = index_bytes == 4 ? (int64_t) static_cast<const int32_t*>(targets)[warp] : static_cast<const int64_t*>(targets)[warp];
+      t = x >= 0 && x < vocab ? (int)x : -1;
+    }
+  }
+  bool there = false;
+  int turn = 0;
+  for (int tile = blockIdx.x; (int64_t)tile * kThinColumns < vocab; tile += gridDim.x, turn ^= 1) {
+    const int v0 = tile * kThinColumns + warp * 4;
+    float acc[4 * R];
+#pragma unroll
+    for (int i = 0; i < 4 * R; ++i) acc[i] = 0.f;
+    const float* from[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) from[v] = w + (int64_t)(v0 + v < vocab ? v0 + v : vocab - 1) * ld_w;
+    for (int k0 = 0; k0 < dim; k0 += chunk) {
+      const int kc = dim - k0 < chunk ? dim - k0 : chunk;
+      // (two groups of 128 columns under way while two are multiplied)
+      float x[2][4][4], next[2][4][4];
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) load_four<WIDE, 32>(from[v] + k0 + 128 * g, lane, kc - 128 * g, x[g][v]);
+      if (!there || chunk < dim) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < R * chunk; i += 512) {
+          const int r = i / chunk, c = k0 + i - r * chunk;
+          hs[i] = r < live && c < dim ? h[(int64_t)(row ? row[r] : r) * ld_h + c] : 0.f;
+        }
+        there = true;
+        __syncthreads();
+      }
+      for (int k = 0; k < kc; k += 256) {
+        if (k + 256 < kc) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) load_four<WIDE, 32>(from[v] + k0 + k + 256 + 128 * g, lane, kc - k - 256 - 128 * g, next[g][v]);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (k + 128 * g < kc) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const float* at = hs + r * chunk + k + 128 * g;
+              float y[4];
+              if (WIDE) load_wide(at + 4 * lane, y);
+              else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = at[lane + 32 * j];
+              }
+#pragma unroll
+              for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[v * R + r] = fmaf(x[g][v][j], y[j], acc[v * R + r]);
+            }
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[g][v][j] = next[g][v][j];
+      }
+    }
+    sum_lanes<4 * R>(acc, lane);
+    constexpr int kEach = 4 * R / 32 > 1 ? 4 * R / 32 : 1;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int n = lane * (4 * R) / 32 + i;
+      zs[turn][n % R][warp * 4 + n / R] = acc[i] * factor;
+    }
+    __syncthreads();
+    if (warp < live && warp < R) {
+      const int col = tile * kThinColumns + lane;
+      float z[2];
+      float m = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        z[q] = col + 32 * q < vocab ? zs[turn][warp][lane + 32 * q] : -INFINITY;
+        m = fmaxf(m, z[q]);
+      }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      const float power = fabsf(m) < 1e30f ? ceilf(m) : 0.f;
+      float sum = 0.f;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        // (the target's term is kept apart)
+        if (col + 32 * q == t) {
+          target_z[warp] = z[q] - power;
+          z[q] = -INFINITY;
+        }
+        const float x = exp2_fast(z[q] + (15.f - power));
+        if (e) e[(int64_t)warp * padded + col + 32 * q] = x;
+        sum += x;
+      }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (lane == 0) sums[(int64_t)warp * sum_blocks + tile] = make_float2(power, sum);
+    }
+  }
+}
+
+// 64 rows of the vocabulary's dz, [row of W][row of h]
+template <int R>
+__device__ __forceinline__ void thin_rows(float (*d)[R], const float* e, int padded, int live, int v0, int v1) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * R; i += 256) {
+    const int r = i / 64, j = i - r * 64;
+    d[j][r] = r < live && v0 + j < v1 ? e[(int64_t)r * padded + v0 + j] : 0.f;
+  }
+  __syncthreads();
+}
+// dz W over `per` rows of W, 1024 columns a block, four a thread
+template <int R, bool WIDE>
+__global__ void __launch_bounds__(256)
+thin_dh_kernel(const float* w, int64_t ld_w, int vocab, int dim, const LossInfo* info, const float* e, int padded, float* parts, int tiles, int per) {
+  __shared__ __align__(16) float d[64][R];
+  after_previous();
+  const int live = info->live, tile = blockIdx.x % tiles, slice = blockIdx.x / tiles, left = dim - tile * 1024;
+  if (live == 0) return;
+  const int v0 = slice * per, v1 = v0 + per < vocab ? v0 + per : vocab;
+  float acc[R][4];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[r][j] = 0.f;
+  for (int vb = v0; vb < v1; vb += 64) {
+    thin_rows<R>(d, e, padded, live, vb, v1);
+    const int n = v1 - vb < 64 ? v1 - vb : 64;
+    const float* from = w + (int64_t)vb * ld_w + tile * 1024;
+    for (int v = 0; v < n; v += 8, from += 8 * ld_w) {
+      float x[8][4];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) load_four<WIDE, 256>(from + (v + u < n ? u : 0) * ld_w, threadIdx.x, left, x[u]);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (v + u < n) {
+#pragma unroll
+          for (int r = 0; r < R; r += 4) {
+            float y[4];
+            load_wide(&d[v + u][r], y);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) acc[r + q][j] = fmaf(y[q], x[u][j], acc[r + q][j]);
+          }
+        }
+      }
+    }
+  }
+  float* to = parts + ((int64_t)slice * R * tiles + tile) * 1024;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[(int64_t)r * tiles * 1024 + place<WIDE, 256>(threadIdx.x, j)] = acc[r][j];
+}
+// ... of all slices, in order, to the rows they belong to, and zeros to those left out: a block 32 columns of a row
+__global__ void __launch_bounds__(256)
+thin_dh_rows_kernel(LossArgs a, const float* parts, int tiles, int padded_rows, int slices, const int* row, const LossInfo* info, float* dh) {
+  __shared__ __align__(16) float4 some[32][8];
+  after_previous();
+  const int r = blockIdx.y, part = threadIdx.x >> 3, quad = threadIdx.x & 7, c = blockIdx.x * 32 + quad * 4;
+  const bool on = r < info->live;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (on && c < a.dim) {
+#pragma unroll 8
+    for (int s = part; s < slices; s += 32) {
+      const float4 x = *reinterpret_cast<const float4*>(parts + ((int64_t)s * padded_rows + r) * tiles * 1024 + c);
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+  }
+  some[part][quad] = v;
+  __syncthreads();
+  if (part == 0) {
+    for (int i = 1; i < 32; ++i) {
+      const float4 x = some[i][quad];
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    float* to = dh + (int64_t)row[r] * a.ld_dh + c;
+    const float out[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (c + q < a.dim) to[q] = on ? out[q] * a.scale : 0.f;
+  }
+}
+__device__ __forceinline__ void put_wide(float* to, const float (&x)[4]) { *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void put_wide(__nv_bfloat16* to, const float (&x)[4]) {
+  *reinterpret_cast<uint2*>(to) = make_uint2(bf162_bits(x[0], x[1]), bf162_bits(x[2], x[3]));
+}
+// dW of `per` rows, 1024 columns a block: a thread has its four columns of all rows of h
+template <typename U, int R, bool WIDE>
+__global__ void __launch_bounds__(256)
+thin_dw_kernel(const float* h, int64_t ld_h, const int* row, int vocab, int dim, float scale, const LossInfo* info, const float* e, int padded, U* dw,
+               int64_t ld_dw, int tiles, int per) {
+  __shared__ __align__(16) float d[64][R];
+  after_previous();
+  const int live = info->live, tile = blockIdx.x % tiles, slice = blockIdx.x / tiles, left = dim - tile * 1024;
+  const int v0 = slice * per, v1 = v0 + per < vocab ? v0 + per : vocab;
+  float y[R][4];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = place<WIDE, 256>(threadIdx.x, j);
+      y[r][j] = r < live && c < left ? h[(int64_t)row[r] * ld_h + tile * 1024 + c] : 0.f;
+    }
+  for (int vb = v0; vb < v1; vb += 64) {
+    thin_rows<R>(d, e, padded, live, vb, v1);
+    const int n = v1 - vb < 64 ? v1 - vb : 64;
+    U* to = dw + (int64_t)vb * ld_dw + tile * 1024;
+#pragma unroll 2
+    for (int v = 0; v < n; ++v, to += ld_dw) {
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < R; r += 4) {
+        float f[4];
+        load_wide(&d[v][r], f);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = fmaf(f[q], y[r + q][j], x[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] *= scale;
+      if (WIDE) {
+        if (4 * (int)threadIdx.x < left) put_wide(to + 4 * threadIdx.x, x);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((int)threadIdx.x + 256 * j < left) put(to + threadIdx.x + 256 * j, x[j]);
+      }
+    }
+  }
+}
+
 // ---- host -------------------------------------------------------------------------------------
 struct LossWs {
   LossInfo* info;
@@ -1285,6 +1593,7 @@ struct LossWs {
   float *slab, *shares, *dw;
   int blocks, piece, padded, vpadded, sum_blocks, staged_rows;
   bool few;               // M_FEW
+  bool thin;              // M_THIN
   bool in_place;          // W is read where it lies
 };
 
@@ -1309,7 +1618,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->few = gradient && terms == 1 && d->rows > 0 && d->rows <= kFewRows && 8 * (int64_t)d->rows <= d->dim &&
            (int64_t)d->vocab * d->dim >= kFewNumbers && ld_w % 8 == 0 && d->dim % kBK == 0;
   l->in_place = l->few || (!gradient && terms == 1 && ld_w % 8 == 0);
-  const int held = l->few ? 2 : terms;          // half-precision numbers that an exponential takes
+  l->thin = terms == 2 && d->rows > 0 && d->rows <= kThinRows && d->dim >= kThinDim && (int64_t)d->vocab * d->dim >= kThinNumbers;
+  const int held = l->few || l->thin ? 2 : terms;          // half-precision numbers that an exponential takes
   l->blocks = ceil_div(d->rows, kIndexRows);
   l->padded = (int)align_up(dim, kBK);
   l->vpadded = (int)align_up(v, kBK);
@@ -1335,8 +1645,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->part = (double*)take(n * 8);
   // (few rows have blocks of 32 columns and more)
   l->sums = (float2*)take((size_t)l->piece * (n <= kTile ? ceil_div(d->vocab, 32) : l->sum_blocks) * 8);
-  l->h = (unsigned short*)take((size_t)l->staged_rows * l->padded * 2 * terms);
-  l->w = (unsigned short*)take(l->in_place ? 0 : v * l->padded * 2 * terms);
+  l->h = (unsigned short*)take(l->thin ? 0 : (size_t)l->staged_rows * l->padded * 2 * terms);
+  l->w = (unsigned short*)take(l->in_place || l->thin ? 0 : v * l->padded * 2 * terms);
   l->e = (unsigned short*)take(gradient ? (size_t)l->piece * l->vpadded * 2 * held : 0);
   l->slab = (float*)take(gradient ? (size_t)l->piece * l->padded * 4 : 0);
   l->shares = (float*)take(gradient ? (size_t)share_blocks(sm_count() / 2) * kTile * kTile * 4 : 0);
@@ -1446,6 +1756,42 @@ uint32_t instruction(bool bf16, bool turned_a, bool turned_b, int m = kTile, int
          ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+// The calls of very few rows.  (dW before dh, which may take h's place.)
+template <int R>
+mw_status thin_run_of(const LossArgs& a, const LossWs& l, const float* h, const float* w, const void* targets, int index_bytes, float* loss, float* total, float* dh,
+                      void* dw, bool dw_bf16, bool gradient, cudaStream_t s) {
+  auto wide = [&](const void* p, int64_t ld, int size) { return ((uintptr_t)p & (uintptr_t)(4 * size - 1)) == 0 && ld % 4 == 0 && a.dim % 4 == 0; };
+  const bool wide_w = wide(w, a.ld_w, 4);
+  const int sums = ceil_div(a.vocab, kThinColumns), most = (int)(192 * 1024 / (4 * R)), chunk = std::min((int)align_up((size_t)a.dim, 128), most / 128 * 128);
+  auto logits = wide_w ? thin_logits_kernel<R, true> : thin_logits_kernel<R, false>;
+  const size_t smem = (size_t)R * chunk * 4;
+  MW_CUDA_OK(cudaFuncSetAttribute(logits, cudaFuncAttributeMaxDynamicSharedMemorySize, 192 * 1024));
+  MW_TRY(launch_after(logits, (unsigned)std::min(sums, sm_count()), 512, smem, s, h, a.ld_h, w, a.ld_w, (int)a.rows, a.vocab, a.dim, chunk,
+                      (float)((double)a.scale * 1.4426950408889634), l.info, gradient ? l.row : nullptr, l.target, targets, index_bytes, l.sums, sums,
+                      l.target_z, gradient ? (float*)l.e : nullptr, l.vpadded));
+  if (!gradient) return MW_OK;
+  const int slices = std::min(2 * sm_count() / (int)a.rows, ceil_div(l.vpadded, 4096));
+  MW_TRY(launch_after(dz_kernel<M_THIN, 8>, (unsigned)(a.rows * slices), 256, 0, s, l.info, 0, (int)a.rows, l.sums, sums, l.target_z, l.row, l.target, l.g,
+                      loss, l.part, total, l.e, l.vpadded, slices));
+  // slices of the vocabulary for as many blocks as the device holds a few times over
+  const int tiles = ceil_div(a.dim, 1024);
+  auto rows_of = [&](int blocks) { return ceil_div(a.vocab, std::max(1, std::min(blocks * sm_count() / tiles, ceil_div(a.vocab, 16)))); };
+  if (dw) {
+    const int per = rows_of(4), n = ceil_div(a.vocab, per) * tiles;
+    auto go = [&](auto kernel, auto* to) { return launch_after(kernel, (unsigned)n, 256, 0, s, h, a.ld_h, l.row, a.vocab, a.dim, a.scale, l.info, (const float*)l.e,
+                                                               l.vpadded, to, a.ld_dw, tiles, per); };
+    if (dw_bf16) MW_TRY(go(wide(dw, a.ld_dw, 2) ? thin_dw_kernel<__nv_bfloat16, R, true> : thin_dw_kernel<__nv_bfloat16, R, false>, (__nv_bfloat16*)dw));
+    else MW_TRY(go(wide(dw, a.ld_dw, 4) ? thin_dw_kernel<float, R, true> : thin_dw_kernel<float, R, false>, (float*)dw));
+  }
+  if (dh) {
+    const int per = rows_of(4), n = ceil_div(a.vocab, per);          // (their sums take 4 * 148 blocks of 8 x 1024 at the most)
+    MW_TRY(launch_after(wide_w ? thin_dh_kernel<R, true> : thin_dh_kernel<R, false>, (unsigned)(n * tiles), 256, 0, s, w, a.ld_w, a.vocab, a.dim, l.info,
+                        (const float*)l.e, l.vpadded, l.shares, tiles, per));
+    MW_TRY(launch_after(thin_dh_rows_kernel, dim3((unsigned)ceil_div(a.dim, 32), (unsigned)a.rows), 256, 0, s, a, l.shares, tiles, R, n, l.row, l.info, dh));
+  }
+  return MW_OK;
+}
+
 template <typename T, typename I>
 mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I* targets, const float* weight, float* loss, float* total,
                    T* dh, void* dw, bool gradient, char* ws, cudaStream_t s) {
@@ -1466,6 +1812,17 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   const unsigned wide = 148 * 8;
   // few rows of the loss alone: no row is moved where the copy engine can read h as it lies
   const bool direct = l.in_place && !gradient && a.rows > 0 && a.rows <= kTile && a.ld_h % 8 == 0 && ((uintptr_t)h & 15) == 0;
+  if constexpr (TERMS == 2) {
+    if (l.thin) {
+      if (gradient) MW_TRY(launch_after(index_live_kernel<I>, 1, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, (int*)nullptr, 1, l.row, l.target, l.g, loss, l.info));
+      auto run = a.rows <= 4 ? thin_run_of<4> : thin_run_of<8>;
+      const bool dw_bf16 = (d->grad_dtype ? d->grad_dtype : d->dtype) == MW_BF16_F32ACC;
+      MW_TRY(run(a, l, h, w, targets, (int)sizeof(I), loss, total, dh, dw, dw_bf16, gradient, s));
+      if (gradient) return MW_OK;
+      return launch_after(direct_rows_kernel<I>, 1, 256, 0, s, l.info, l.sums, ceil_div(a.vocab, kThinColumns), kThinColumns, l.target_z, targets, weight, (int)a.rows,
+                          a.vocab, loss, l.part, total);
+    }
+  }
   if (l.blocks != 1) MW_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(LossInfo), s));
   if (a.rows > 0 && !direct) {
     int* counts = l.blocks > 1 ? l.counts : nullptr;

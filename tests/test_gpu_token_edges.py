@@ -247,3 +247,60 @@ def test_rows_of_several_blocks(N, V, dtype):
     h[0] = W[V - 1]
     check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
     check(mwb.token_loss_gradient(h, W, t, piece_rows=256), reference(h, W, t), ALL)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,D", [(4103, 1030), (65601, 64), (1031, 4100), (1039, 4101), (70, 60000)])
+@pytest.mark.parametrize("N", [1, 3, 4, 5, 8, 9, 16, 17])
+def test_very_few_rows(N, V, D, dtype):
+    h, W, t = make(N, V, D, dtype, seed=N + V, left_out=0.3 if N > 1 else 0.0)
+    t[0], h[0] = V - 1, W[V - 1]
+    want = reference(h, W, t, scale=-0.7)
+    check(mwb.token_loss(h, W, t, scale=-0.7), want, ("loss", "total"))
+    kind = F32 if N % 2 else BF16
+    r = mwb.token_loss_gradient(h, W, t.to(torch.int32), scale=-0.7, grad_dtype=kind)
+    check(r, want, ALL)
+    out = (t < 0) | (t >= V)
+    assert bool((r.loss[out] == 0).all() and (r.dh[out] == 0).all())
+    w = torch.randn(N, device="cuda") * 1e3 * (torch.arange(N, device="cuda") % 4 != 1)
+    h[1::4] = float("nan")
+    want = reference(h, W, t, weight=w)
+    check(mwb.token_loss(h, W, t, row_weight=w), want, ("loss", "total"))
+    full = mwb.token_loss_gradient(h, W, t, row_weight=w, grad_dtype=kind)
+    check(full, want, ALL)
+    # windows of wider rows at odd places, h's own place for dh: other loads, the same numbers to rounding
+    wide, hw, grad = (torch.full((n, D + 9), 5.0, device="cuda", dtype=k) for n, k in ((V, dtype), (N, dtype), (V, kind)))
+    wide[:, 1:D + 1], hw[:, 5:D + 5] = W, h
+    again = mwb.token_loss_gradient(hw[:, 5:D + 5], wide[:, 1:D + 1], t, row_weight=w, dh=hw[:, 5:D + 5], dweight=grad[:, 3:D + 3], piece_rows=1)
+    check(again, want, ALL)
+    for x, at in ((hw, 5), (grad, 3)):
+        assert bool((x[:, :at] == 5).all() and (x[:, at + D:] == 5).all())
+    only = mwb.token_loss_gradient(h, W, t, row_weight=w, grad_dtype=kind, want=(False, True))
+    assert only.dh is None and torch.equal(only.dweight, full.dweight)
+    only = mwb.token_loss_gradient(h, W, t, row_weight=w, want=(True, False))
+    assert only.dweight is None and torch.equal(only.dh, full.dh)
+
+
+@pytest.mark.parametrize("left_out", [0.0, 1.0])
+def test_very_few_rows_captured_and_not_finite(left_out):
+    h, W, t = make(12, 9001, 520, F32, left_out=left_out)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        mwb.token_loss(h, W, t), mwb.token_loss_gradient(h, W, t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a, b = mwb.token_loss(h, W, t), mwb.token_loss_gradient(h, W, t)
+    for seed in (1, 2):
+        h2, W2, t2 = make(12, 9001, 520, F32, seed=seed, left_out=left_out)
+        h.copy_(h2), W.copy_(W2), t.copy_(t2)
+        graph.replay()
+        check(b, reference(h, W, t), ALL)
+        c, d = mwb.token_loss(h, W, t), mwb.token_loss_gradient(h, W, t)
+        assert torch.equal(a.loss, c.loss) and torch.equal(a.total, c.total) and all(torch.equal(x, y) for x, y in zip(b, d))
+    if left_out == 0.0:
+        h[5, 3] = float("nan")
+        r = mwb.token_loss_gradient(h, W, t)
+        rest = torch.arange(12, device="cuda") != 5
+        assert bool(r.loss[5].isnan()) and bool(r.dh[5].isnan().all())
+        assert torch.equal(r.loss[rest], d.loss[rest]) and torch.equal(r.dh[rest], d.dh[rest])
