@@ -67,7 +67,6 @@ __host__ __device__ constexpr int terms_b(int mode) { return mode == M_TWO ? 2 :
 __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ? 3 : (mode == M_FEW ? 2 : 1); }      // of dz
 constexpr int kFewRows = 128;
 constexpr int kThinRows = 8, kThinColumns = 64;
-constexpr int64_t kThinNumbers = 4 << 20, kThinDim = 512;
 constexpr int64_t kFewNumbers = 12 << 20;
 // Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long as
 // the vocabulary's way through memory (loss of 16 rows of 32768x2048 bf16 36.5 us by pairs, 33.7 by CTAs, fp32 174 and 155;
@@ -1283,9 +1282,13 @@ dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mod
 }
 
 // ---- very few rows ----------------------------------------------------------------------------
-// Up to 8 rows of fp32 over a large W.  As operands W passes memory three times for the loss and five for the gradient; here
-// each kernel reads it once (or writes dW), in fp32 throughout, and the CUDA cores' multiplications stay below the time of
-// that.
+// Up to 8 rows of fp32.  As operands W passes memory three times for the loss and five for the gradient; here each kernel
+// reads it once (or writes dW), in fp32 throughout, and the CUDA cores' multiplications stay below the time of that.  Beside
+// the products: loss of 32768x2048 59 us of 1 row, 81 of 8 (154), gradient 179 and 213 us (276); of 848x512 17 (33) and 32
+// (57); of 131072x100 gradient 108 and 165 (157).  16 rows took 155 and 325 us (154, 277), as bf16 rows off the copy engine's
+// boundaries did (8 rows of 33620x1615 gradient 272 us, 199 as operands).
+// Bound by memory: 8 rows' logits 3.4 TB/s (their h out of shared memory takes as long as the multiplications), 4 rows' 4.2;
+// dh 6.0 and 4.4 TB/s, eight rows of W under way a thread; dW 5.6.
 // A thread's four numbers of a group of 4 * STRIDE: together where rows allow 16 bytes at a time, else STRIDE apart.
 template <bool WIDE, int STRIDE>
 __device__ __forceinline__ int place(int i, int j) { return WIDE ? 4 * i + j : i + STRIDE * j; }
@@ -1618,7 +1621,7 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   l->few = gradient && terms == 1 && d->rows > 0 && d->rows <= kFewRows && 8 * (int64_t)d->rows <= d->dim &&
            (int64_t)d->vocab * d->dim >= kFewNumbers && ld_w % 8 == 0 && d->dim % kBK == 0;
   l->in_place = l->few || (!gradient && terms == 1 && ld_w % 8 == 0);
-  l->thin = terms == 2 && d->rows > 0 && d->rows <= kThinRows && d->dim >= kThinDim && (int64_t)d->vocab * d->dim >= kThinNumbers;
+  l->thin = terms == 2 && d->rows > 0 && d->rows <= kThinRows;
   const int held = l->few || l->thin ? 2 : terms;          // half-precision numbers that an exponential takes
   l->blocks = ceil_div(d->rows, kIndexRows);
   l->padded = (int)align_up(dim, kBK);

@@ -304,3 +304,22 @@ def test_very_few_rows_captured_and_not_finite(left_out):
         rest = torch.arange(12, device="cuda") != 5
         assert bool(r.loss[5].isnan()) and bool(r.dh[5].isnan().all())
         assert torch.equal(r.loss[rest], d.loss[rest]) and torch.equal(r.dh[rest], d.dh[rest])
+
+
+@pytest.mark.parametrize("N,V,D", [(1, 1, 1), (2, 63, 5), (8, 64, 128), (3, 65, 129), (8, 20011, 4), (5, 1000, 257), (8, 3, 2050), (7, 500, 8200)])
+def test_very_few_rows_of_small_sizes(N, V, D):
+    h, W, t = make(N, V, D, F32, seed=V, std=3.0)
+    t[0] = V - 1
+    want = reference(h, W, t, scale=2.0)
+    check(mwb.token_loss(h, W, t, scale=2.0), want, ("loss", "total"))
+    check(mwb.token_loss_gradient(h, W, t, scale=2.0), want, ALL)
+    check(mwb.token_loss_gradient(h, W, t, scale=0.0), reference(h, W, t, scale=0.0), ALL)
+    big = 2.0 ** 60
+    check(mwb.token_loss_gradient(h * big, W / big, t, scale=2.0), reference(h * big, W / big, t, scale=2.0), ALL)
+    h, W, t = make(N, V, D, F32, seed=V, lean=200.0 if V > 1 and D > 4 else 0.0)
+    check(mwb.token_loss_gradient(h, W, t), reference(h, W, t), ALL)
+    if V > 1:
+        # a row of the vocabulary that is never chosen
+        h, t = h.abs() + 0.5, t.clamp(min=1)
+        W[0] = float("-inf")
+        check(mwb.token_loss(h, W, t), reference(h, W[1:], t - 1), ("loss", "total"))
