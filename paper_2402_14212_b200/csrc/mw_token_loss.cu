@@ -11,8 +11,8 @@
 //
 // Loss alone: a tile's epilogue leaves, for each row and 128 columns, a power of two k and the sum of 2^(z' - k)
 // (z' = z log2 e) of all logits but the target's; a last kernel joins them.  Nothing else of the logits is written.  Up to
-// 256 rows of bf16 are read as they lie, without being put together: two launches, 37 us for 16 rows of 32768x2048 (the
-// vocabulary's way through memory is 20 us).
+// 256 rows of bf16 are read as they lie, without being put together: two launches, 34 us for 16 rows of 32768x2048 (the
+// vocabulary's way through memory is 20 us).  Up to 8 rows of fp32 stay off the tensor cores ("very few rows" below).
 //
 // Gradient: the logits are not computed twice.  A piece of rows at a time, the epilogue also writes 2^(z' - k) in
 // half precision (float for float operands); once the row's sum is known those become dz in their place, by
@@ -27,6 +27,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "mw_launch.cuh"
@@ -92,11 +93,13 @@ constexpr int buffers_for(int mode, int kind, int blocks_k) {
 // K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
 // losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and 3.8e-7
 // with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
-// 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many at no cost (16 rows of
-// 32768x2048 33.7 us, fp32 153 us, either way): 3.4e-7 where twice as many leave 7.5e-7.  dz of bf16 operands has 11 bits:
-// its sums have 512 instructions, 2^-15 at the worst, and are read out seldom.
-constexpr int piece_blocks(int mode, int kind, bool few) {
-  return mode == M_TWO ? (few ? 2 : 4) : (of_logits(kind) ? (few ? 8 : 16) : 128 / products_of(mode));
+// 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many, and a quarter where a CTA has
+// them all and it costs nothing: 16 rows of 32768x2048 1.6e-7 (3.4e-7 with half, 7.5e-7 with all) in 33.8 us, 200 rows 3.7e-7
+// (1.8e-7 in 49 us of 43).  dz of bf16 operands has 11 bits: its sums have 512 instructions, 2^-15 at the worst, and are
+// read out seldom.
+constexpr int piece_blocks(int mode, int kind, int rows) {
+  const bool few = rows <= kTile;
+  return mode == M_TWO ? (few ? 2 : 4) : (of_logits(kind) ? (rows <= kHalf ? 4 : (few ? 8 : 16)) : 128 / products_of(mode));
 }
 
 // what the kernels of one call share, behind the status block
@@ -1288,7 +1291,8 @@ dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mod
 // (57); of 131072x100 gradient 108 and 165 (157).  16 rows took 155 and 325 us (154, 277), as bf16 rows off the copy engine's
 // boundaries did (8 rows of 33620x1615 gradient 272 us, 199 as operands).
 // Bound by memory: 8 rows' logits 3.4 TB/s (their h out of shared memory takes as long as the multiplications), 4 rows' 4.2;
-// dh 6.0 and 4.4 TB/s, eight rows of W under way a thread; dW 5.6.
+// dh 6.0 and 4.4 TB/s, eight rows of W under way a thread; dW 5.6.  (Tiles of 32 logits, which divide evenly among the blocks,
+// were no faster: 62 us of 1 row.)
 // A thread's four numbers of a group of 4 * STRIDE: together where rows allow 16 bytes at a time, else STRIDE apart.
 template <bool WIDE, int STRIDE>
 __device__ __forceinline__ int place(int i, int j) { return WIDE ? 4 * i + j : i + STRIDE * j; }
@@ -1712,7 +1716,7 @@ mw_status run_product_in(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   p.a_term = KIND == P_DW ? kPlaneBytes : (uint32_t)p.a_rows * (kBK * 2);
   p.a_stage = terms_a(MODE, KIND) * p.a_term;
   p.buffers = buffers_for(MODE, KIND, p.blocks_k);
-  p.most_blocks = piece_blocks(MODE, KIND, p.piece <= kTile);
+  p.most_blocks = piece_blocks(MODE, KIND, p.piece);
   p.stages = stages_for(p.buffers, p.a_stage + terms_b(MODE) * plane_b(PAIR));
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
