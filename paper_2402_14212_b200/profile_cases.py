@@ -77,6 +77,7 @@ def main():
                 mwb.token_loss_gradient(h, w, t)
                 mwb.token_loss(h[:16], w, t[:16])
                 mwb.token_loss_gradient(h[:16], w, t[:16])
+                mwb.token_loss_gradient(h[:8], w, t[:8])
         table = torch.randn(32768, 2048, device="cuda", generator=g).bfloat16()
         rank = (torch.exp(torch.rand(16384, device="cuda", generator=g) * math.log(32768.0)) - 1).long().clamp_(0, 32767)
         dout = torch.randn(16384, 2048, device="cuda", generator=g).bfloat16()
