@@ -37,6 +37,11 @@ namespace mw {
 namespace {
 
 constexpr int kIndexRows = 1024;          // rows of one block that looks for targets
+// The power of two of a block of logits whose largest is m (in powers of two): what its exponentials are relative to.  Of
+// nothing but -inf it is small, so that the empty block sets no row's scale, and differences to any power are finite; beside
+// an infinity or a NaN alone the values stay as they are.
+constexpr float kNoPower = -3e38f;
+__device__ __forceinline__ float power_of(float m) { return m == -INFINITY ? kNoPower : (m < INFINITY ? ceilf(m) : 0.f); }
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 constexpr int64_t kHeldBytes = (int64_t)40 << 20;          // of rows that stay in L2 (126 MB) while the vocabulary passes
 
@@ -649,8 +654,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             }
           }
           const bool here = t >= 0 && t < valid;
-          // (a row of nothing but -inf here, or with an infinity, keeps its values as they are)
-          const float power = fabsf(m) < 1e30f ? ceilf(m) : 0.f;
+          const float power = power_of(m);
           // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row that is
           // sure of it is what the others' terms add to one, with no difference of two logits in it
           if (__any_sync(0xffffffffu, here)) {
@@ -981,8 +985,6 @@ __device__ __forceinline__ RowSum warp_join(RowSum v) {
   }
   return v;
 }
-// k of a block whose row is empty so far: small, and its difference to any k is finite
-constexpr float kNoPower = -3e38f;
 // What a row's sums say: `v` of all terms but the target's (times 2^15, relative to 2^v.k), the target's logit relative
 // to its own block's power.  odds: log2 of the others' terms over the target's.
 struct RowEnd {
@@ -1436,7 +1438,7 @@ thin_logits_kernel(const float* h, int64_t ld_h, const float* w, int64_t ld_w, i
       }
 #pragma unroll
       for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      const float power = fabsf(m) < 1e30f ? ceilf(m) : 0.f;
+      const float power = power_of(m);
       float sum = 0.f;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
