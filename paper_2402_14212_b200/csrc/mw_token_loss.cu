@@ -997,7 +997,8 @@ __device__ __forceinline__ RowEnd row_end(const LossInfo* info, RowSum v, float 
   e.loss = far ? 0.69314718055994531f * odds : log1pf(r);
   e.less = far ? 1.f : r / (1.f + r);
   e.total = v.sum + exp2f((target_power - v.k) + 15.f + target_z);
-  if (info->st.code != 0) e.loss = e.total = __int_as_float(0x7fffffff);          // a wait ran out: nothing here is right
+  // a wait ran out: nothing here is right; or the target's logit is infinite, and inf - inf no difference
+  if (info->st.code != 0 || target_z == INFINITY) e.loss = e.total = e.less = __int_as_float(0x7fffffff);
   return e;
 }
 

@@ -1,4 +1,5 @@
-"""The vocabulary's loss where logits are infinite: a block of the vocabulary that no row can choose.  Formulas and tolerances are those of test_gpu_token_loss.py."""
+"""The vocabulary's loss where logits are infinite: a block of the vocabulary that no row can choose, and a target whose
+own logit is infinite.  Formulas and tolerances are those of test_gpu_token_loss.py."""
 import pytest
 import torch
 
@@ -32,3 +33,27 @@ def test_blocks_that_no_row_can_choose_of_a_large_weight():
     W[V:] = float("-inf")
     W, h, t = W.to(BF16), torch.ones(N, D, device="cuda", dtype=BF16), torch.arange(N, device="cuda") * 600
     check(mwb.token_loss_gradient(h, W, t), reference(h, W[:V].contiguous(), t), ("loss", "total"))
+
+
+@pytest.mark.parametrize("N,dtype", [(1, F32), (4, F32), (8, F32), (1, BF16), (20, BF16), (200, BF16), (300, BF16)])
+def test_an_infinite_logit_of_the_target(N, dtype):
+    """inf - inf is no loss of zero: a row of the weight that holds infinities is not a sure prediction of its own token."""
+    h, W, t = make(N, 300, 64, dtype, lean=0.0)
+    h, t = h.abs() + 0.5, torch.full((N,), 170, device="cuda")
+    W[170] = float("inf")
+    for r in (mwb.token_loss(h, W, t), mwb.token_loss_gradient(h, W, t)):
+        assert bool(r.loss.isnan().all()) and bool(r.total.isnan())
+    assert not bool(torch.isfinite(r.dh).any())
+
+
+@pytest.mark.parametrize("N,dtype", [(3, F32), (8, F32), (9, F32), (200, F32), (3, BF16), (300, BF16)])
+def test_a_target_whose_logit_overflows(N, dtype):
+    """Finite operands whose product is beyond 32 bits: loss and dh of that row alone are not finite."""
+    h, W, t = make(N, 300, 64, dtype, lean=0.0)
+    h[:, 0], W[:, 0], t[0] = 0.0, 0.0, 170
+    t[1:][t[1:] == 170] = 171
+    h[0, 0] = 2.0 ** 70
+    W[170, 0] = 2.0 ** 70
+    for r in (mwb.token_loss(h, W, t), mwb.token_loss_gradient(h, W, t)):
+        assert bool(r.loss[0].isnan()) and bool(torch.isfinite(r.loss[1:]).all())
+    assert not bool(torch.isfinite(r.dh[0]).any()) and bool(torch.isfinite(r.dh[1:]).all())
