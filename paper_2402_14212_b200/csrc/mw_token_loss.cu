@@ -655,6 +655,10 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           }
           const bool here = t >= 0 && t < valid;
           const float power = power_of(m);
+          // Exponentials reach 2^15, near the end of half precision.  Logits beyond 2^22 are rounded by half of one and more, as
+          // their power was: a lane that has some takes the difference of the rounded ones.
+          const bool far = fabsf(power) >= 4194304.f, any_far = __any_sync(0xffffffffu, far);
+          auto relative = [&](float v, float plus) { return far ? __fadd_rn(__fmul_rn(v, factor), -power) : fmaf(v, factor, plus - power); };
           // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row that is
           // sure of it is what the others' terms add to one, with no difference of two logits in it
           if (__any_sync(0xffffffffu, here)) {
@@ -665,12 +669,17 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
               zt = i == t ? acc[i] : zt;
               acc[i] = i == t ? gone : acc[i];
             }
-            if (here) p.target_z[p.first + row] = fmaf(zt, factor, -power);
+            if (here) p.target_z[p.first + row] = relative(zt, 0.f);
           }
           float sum = 0.f;
-          const float shift = 15.f - power;
+          if (!any_far) {
+            const float shift = 15.f - power;
 #pragma unroll
-          for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, shift));
+            for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, shift));
+          } else {
+#pragma unroll
+            for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(relative(acc[i], 15.f)) * (far ? 32768.f : 1.f);
+          }
           if (!whole) {
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) acc[i] = i < valid ? acc[i] : 0.f;

@@ -1,10 +1,10 @@
-"""The vocabulary's loss where logits are infinite: a block of the vocabulary that no row can choose, and a target whose
-own logit is infinite.  Formulas and tolerances are those of test_gpu_token_loss.py."""
+"""The vocabulary's loss where logits are infinite or very large: a block of the vocabulary that no row can choose, a target
+whose own logit is infinite, powers of two that 32 bits round.  Formulas and tolerances are those of test_gpu_token_loss.py."""
 import pytest
 import torch
 
 from paper_2402_14212_b200 import binding as mwb
-from test_gpu_token_loss import BF16, F32, check, make, reference
+from test_gpu_token_loss import ALL, BF16, F32, check, make, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,14 @@ def test_a_target_whose_logit_overflows(N, dtype):
     for r in (mwb.token_loss(h, W, t), mwb.token_loss_gradient(h, W, t)):
         assert bool(r.loss[0].isnan()) and bool(torch.isfinite(r.loss[1:]).all())
     assert not bool(torch.isfinite(r.dh[0]).any()) and bool(torch.isfinite(r.dh[1:]).all())
+
+
+@pytest.mark.parametrize("N,dtype", [(8, F32), (9, F32), (300, F32), (20, BF16), (300, BF16)])
+@pytest.mark.parametrize("size", [10, 18, 20, 22, 24, 30, 44, 100])
+def test_logits_far_from_one(size, N, dtype):
+    """Logits of 2^size: everything is finite, and rows that are sure of their target have a loss of zero."""
+    h, W, t = make(N, 700, 128, dtype, seed=N, lean=8.0)
+    h, W = h * 2.0 ** (size // 2), W * 2.0 ** (size - size // 2)
+    want = reference(h, W, t)
+    check(mwb.token_loss(h, W, t), want, ("loss", "total"))
+    check(mwb.token_loss_gradient(h, W, t), want, ALL)
