@@ -19,7 +19,7 @@
 // a factor per 128 columns, and two products take them in.  That costs 4 bytes of traffic an element (0.175 ms of the
 // 2.8 above), less than the 2 D flops of computing it again (0.75 ms) from D of about 400 up.
 //
-// Numbers.  bf16 operands are taken as half-precision numbers times one power of two a tensor: their 8 bits
+// Numbers.  bf16 operands are taken as half-precision numbers times a power of two (one a row of h, one for W): their 8 bits
 // fit, and dz keeps 11 bits where bf16 would leave 8 (dh and dW of bf16 are as far from 64 bits as the last rounding leaves
 // any result: 1.7e-3).  Float operands are split in two such terms (22 bits), three products of four.  Sums are float; the
 // tensor core cuts its accumulator off at every step, so a sum goes to registers, rounded to nearest, a piece of K at a
@@ -67,7 +67,7 @@ enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
 // and 73; but 16 rows of 33550x320 61 and 64 us, 128 rows 72 and 84, of 4096x512 44 and 49).
 // M_THIN: very few rows, without the tensor cores (below).
 enum { M_ONE = 1, M_TWO, M_FEW, M_THIN };
-constexpr bool of_logits(int kind) { return kind == P_SUMS || kind == P_EXP; }
+__host__ __device__ constexpr bool of_logits(int kind) { return kind == P_SUMS || kind == P_EXP; }
 __host__ __device__ constexpr int terms_a(int mode, int kind) { return mode == M_TWO || (mode == M_FEW && kind >= P_DH) ? 2 : 1; }
 __host__ __device__ constexpr int terms_b(int mode) { return mode == M_TWO ? 2 : 1; }
 __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ? 3 : (mode == M_FEW ? 2 : 1); }      // of dz
@@ -113,11 +113,19 @@ struct LossInfo {
   unsigned pad[59];
   int live;                 // rows that are not left out
   unsigned g_max;           // bits of the largest |g|
-  unsigned h_max, w_max;    // bits of the largest finite |h|, |W|
+  unsigned w_max;           // bits of the largest finite |W|
+  unsigned reach;           // 1024 + the largest power of two in the rows of h (0: zeros alone)
+  unsigned uneven;          // some row of h is of an unusual size
   unsigned done;            // blocks whose losses are in
-  unsigned pad2[59];
+  unsigned pad2[58];
 };
 
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }      // of -126..127
+// v 2^e, whose factor may lie beyond a float's range
+__device__ __forceinline__ float scaled_by(float v, int e) {
+  e = e < -250 ? -250 : (e > 250 ? 250 : e);
+  return v * power_of_two(e / 2) * power_of_two(e - e / 2);
+}
 // the power of two that brings numbers of at most this size to 2^13 .. 2^14
 __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   const int e = (int)(max_bits >> 23) - 127;         // 2^e <= max < 2^(e + 1)
@@ -125,8 +133,8 @@ __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   const int x = 13 - e;
   return x < -100 ? -100 : (x > 100 ? 100 : x);
 }
-// ... of an operand whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up to 2^7, 2^-9),
-// which is written while it is looked at; where the largest lies elsewhere it is written again.  What is lost then
+// ... of a row of h, or of W whole, whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up to 2^7,
+// 2^-9), which is written while it is looked at; where the largest lies elsewhere it is written again.  What is lost then
 // lies below 2^-30 for bf16, whose 8 bits fit (2^-33 for the second of two terms).
 __host__ __device__ constexpr int usual_exponent(int terms) { return terms == 1 ? 6 : 8; }
 __device__ __forceinline__ bool unusual(unsigned most, int terms) {
@@ -135,6 +143,12 @@ __device__ __forceinline__ bool unusual(unsigned most, int terms) {
 }
 __device__ __forceinline__ int operand_exponent(unsigned most, int terms) {
   return unusual(most, terms) ? range_exponent(most) : usual_exponent(terms);
+}
+// Rows of h have a power of two each for the logits, which an epilogue's lane takes out of its row.  The sums of dW run over
+// the rows, which want one for all of them: where they have the usual one alike, the same operand serves; else dW has an
+// operand of its own, whose largest number is brought to 2^13 .. 2^14.
+__device__ __forceinline__ int common_exponent(const LossInfo* info, int terms) {
+  return info->uneven == 0 ? usual_exponent(terms) : (info->reach ? 13 + 1024 - (int)info->reach : 0);
 }
 
 struct LossArgs {
@@ -147,6 +161,7 @@ struct LossArgs {
 
 struct alignas(64) ProductArgs {
   CUtensorMap a, b, out, acc;
+  CUtensorMap b_common;     // P_DW: h where its rows are not of one size
   const LossInfo* info;
   DeviceStatus* st;
   float* total;             // NaN where a wait ran out
@@ -174,6 +189,7 @@ struct alignas(64) ProductArgs {
   float2* sums;             // [row][sum_blocks]: power, sum
   float* target_z;
   const int* target;
+  const int* row_exponent;  // of h as an operand, by row; null: 0
   // P_DW: the gradient itself where the copy engine cannot write it, and the sums over pieces
   void* dw;
   int64_t ld_dw;
@@ -423,6 +439,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     const uint32_t full0_even = PAIR ? map_to_cta(full0, 0u) : full0;
     const int share_n = KIND == P_SUMS ? (PAIR ? p.tile_n / 2 : p.tile_n) : kShareB;
     const uint32_t tx = (PAIR ? 2u : 1u) * (a_stage + b_stage / kShareB * (uint32_t)share_n);
+    const CUtensorMap* by_rows = KIND == P_DW && p.scaled && p.info->uneven ? &p.b_common : &p.b;
     bool ok = true;
     for (int u = pair; u < units && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live, plan);
@@ -442,7 +459,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
             else tma_load_4d<PAIR>(to, &p.b, fb, 0, kb * kBK, bn >> 6, 0);
           } else {
             if (of_a) tma_load_4d<PAIR>(to, &p.a, fb, 0, kb * kBK, am >> 6, 0);
-            else tma_load_4d<PAIR>(to, &p.b, fb, 0, p.first + kb * kBK, bn >> 6, 0);
+            else tma_load_4d<PAIR>(to, by_rows, fb, 0, p.first + kb * kBK, bn >> 6, 0);
           }
         }
         __syncwarp();
@@ -505,15 +522,18 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     uint32_t turn = 0;
     int j = 0;
     bool ok = true;
-    const int exps = p.scaled ? operand_exponent(p.info->h_max, kTermsB) : 0;
-    const int expw = p.scaled ? operand_exponent(p.info->w_max, kTermsB) : 0;
-    const int expz = range_exponent(p.info->g_max);
     float factor = 1.f;
-    if (KIND == P_DW) factor = (float)ldexp((double)p.scale, -(expz + exps));
-    if (KIND == P_SUMS || KIND == P_EXP) {
-      factor = (float)ldexp((double)p.scale * 1.4426950408889634, -(exps + expw));
-      if (factor == 0.f) factor = 1e-30f;           // (a sign, for what takes a term out of the sum)
+    int exponent = 0;                               // factor's, but for a row's own (logits)
+    if (KIND == P_DW) {
+      const int exps = p.scaled ? common_exponent(p.info, kTermsB) : 0;
+      factor = (float)ldexp((double)p.scale, -(range_exponent(p.info->g_max) + exps));
     }
+    if (of_logits(KIND)) {
+      factor = (float)frexp((double)p.scale * 1.4426950408889634, &exponent);
+      if (p.scaled) exponent -= operand_exponent(p.info->w_max, kTermsB);
+    }
+    const float mantissa = factor;
+    const bool rises = mantissa >= 0.f;             // (the same of all rows, whose logits then go the same way)
     // Blocks of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the warp's buffers in turn: `group` of
     // them at a time, since the fence between their stores and the copy engine is what a short tile waits for.
     auto free_buffers = [&](int group) {
@@ -584,6 +604,17 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     for (int u = pair; u < units && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live, plan);
       const int row0 = w.m0 + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+      // what a tile of logits wants to know of its rows, on its way while the accumulator is waited for
+      int own = 0, target = -1;
+      if (of_logits(KIND) && row < live) {
+        if (p.row_exponent) own = p.row_exponent[p.first + row];
+        if (KIND == P_SUMS && p.direct) {
+          const int64_t x = p.index_bytes == 4 ? (int64_t) static_cast<const int32_t*>(p.targets)[row] : static_cast<const int64_t*>(p.targets)[row];
+          target = x >= 0 && x < p.vocab ? (int)x : -1;
+        } else {
+          target = p.target[p.first + row];
+        }
+      }
       const int cols = KIND == P_SUMS ? p.tile_n / 2 : kSumColumns;          // of this warp
       const int col0 = w.n0 + side * cols;
       float acc[kSumColumns];
@@ -629,6 +660,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         for (int i = 0; i < kSumColumns; ++i) acc[i] = 0.f;
       }
       if (KIND == P_SUMS || KIND == P_EXP) {
+        factor = scaled_by(mantissa, exponent - own);
+        if (factor == 0.f) factor = rises ? 1e-30f : -1e-30f;           // (a sign, for what takes a term out of the sum)
         // columns of the vocabulary among them (the registers beyond hold another warp's, or nothing)
         const int left = p.vocab - col0, valid = left < cols ? left : cols;
         const bool on = row < live;
@@ -636,7 +669,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           // the largest logit: of a negative factor the least sum's
           const bool whole = valid == kSumColumns;
           float m = -INFINITY;
-          if (whole && factor > 0.f) {
+          if (whole && rises) {
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) m = fmaxf(m, acc[i]);
             m *= factor;
@@ -644,42 +677,35 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) m = fmaxf(m, i < valid ? acc[i] * factor : -INFINITY);
           }
-          int t = -1;
-          if (on) {
-            if (KIND == P_SUMS && p.direct) {
-              const int64_t x = p.index_bytes == 4 ? (int64_t) static_cast<const int32_t*>(p.targets)[row] : static_cast<const int64_t*>(p.targets)[row];
-              t = x >= col0 && x < col0 + valid ? (int)(x - col0) : -1;
-            } else {
-              t = p.target[p.first + row] - col0;
-            }
-          }
-          const bool here = t >= 0 && t < valid;
+          const int t = target - col0;
+          const bool here = on && t >= 0 && t < valid;
           const float power = power_of(m);
-          // Exponentials reach 2^15, near the end of half precision.  Logits beyond 2^22 are rounded by half of one and more, as
-          // their power was: a lane that has some takes the difference of the rounded ones.
-          const bool far = fabsf(power) >= 4194304.f, any_far = __any_sync(0xffffffffu, far);
-          auto relative = [&](float v, float plus) { return far ? __fadd_rn(__fmul_rn(v, factor), -power) : fmaf(v, factor, plus - power); };
-          // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row that is
-          // sure of it is what the others' terms add to one, with no difference of two logits in it
-          if (__any_sync(0xffffffffu, here)) {
+          const bool far = fabsf(power) >= 4194304.f;
+          float shift = 15.f - power;
+          if (__any_sync(0xffffffffu, here || far)) {
+            float below = -power;
+            // Exponentials reach 2^15, near the end of half precision.  Logits beyond 2^22 are rounded by half of one and more, as
+            // their power was: a lane that has some goes on with the rounded ones' differences to it.
+            if (__any_sync(0xffffffffu, far)) {
+              const float way = rises ? 1.f : -1.f;
+#pragma unroll
+              for (int i = 0; i < kSumColumns; ++i) acc[i] = far ? __fadd_rn(__fmul_rn(acc[i], factor), -power) * way : acc[i];
+              if (far) { factor = way; shift = 15.f; below = 0.f; }
+            }
+            // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row that is
+            // sure of it is what the others' terms add to one, with no difference of two logits in it
             float zt = 0.f;
-            const float gone = factor > 0.f ? -INFINITY : INFINITY;
+            const float gone = rises ? -INFINITY : INFINITY;
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) {
               zt = i == t ? acc[i] : zt;
               acc[i] = i == t ? gone : acc[i];
             }
-            if (here) p.target_z[p.first + row] = relative(zt, 0.f);
+            if (here) p.target_z[p.first + row] = fmaf(zt, factor, below);
           }
           float sum = 0.f;
-          if (!any_far) {
-            const float shift = 15.f - power;
 #pragma unroll
-            for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, shift));
-          } else {
-#pragma unroll
-            for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(relative(acc[i], 15.f)) * (far ? 32768.f : 1.f);
-          }
+          for (int i = 0; i < kSumColumns; ++i) acc[i] = exp2_fast(fmaf(acc[i], factor, shift));
           if (!whole) {
 #pragma unroll
             for (int i = 0; i < kSumColumns; ++i) acc[i] = i < valid ? acc[i] : 0.f;
@@ -861,122 +887,212 @@ __device__ __forceinline__ void split_bf16(float v, unsigned short& hi, unsigned
   lo = __bfloat16_as_ushort(__float2bfloat16_rn(isfinite(back) ? v - back : 0.f));
 }
 
-// h (rows with a target, by their index) or W as operands: [terms][staged rows][padded columns], zero beyond a row's
-// end and beyond the last row to a multiple of a tile
+// h (rows with a target, by their index) and W as operands: [terms][staged rows][padded columns], zero beyond a row's
+// end, and of h beyond the last row to a multiple of a tile
 template <typename T>
-struct Operand {
-  const T* x;
-  int64_t ld;
-  const int *row, *count;         // null: all rows
-  int64_t rows, staged_rows;
-  unsigned* most;                 // LossInfo::h_max or w_max
-  unsigned short* out;
+struct Operands {
+  const T *w, *h;
+  int64_t ld_w, ld_h;
+  unsigned short *w_out, *h_out;
+  unsigned short* common_out;     // h under one power of two (null: not wanted)
+  const int* row;
+  int* row_exponent;
+  int vocab, dim, padded;
+  int rows, staged_rows;          // of h
   T* dead;                        // rows of dh that get zeros
   int64_t ld_dead;
+  LossInfo* info;
+  int row_threads;                // of a row of h
+  int64_t w_blocks;               // the first blocks are W's
 };
-// AGAIN: only what is of an unusual size.  SCALED false: bf16 as it is.
+
+// What a thread has of a row at a time: eight columns, on their way (WIDE) before the first is used
+template <typename T, bool WIDE>
+struct Eights {
+  static constexpr int kAhead = WIDE ? (sizeof(T) == 2 ? 4 : 2) : 1, kLoads = sizeof(T) == 2 ? 1 : 2;
+  uint4 raw[kAhead][kLoads];
+  // from: a row's start, or null
+  __device__ __forceinline__ void load(int a, const T* from, int c, int dim) {
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q)
+      raw[a][q] = WIDE && from && c + q * 4 < dim ? reinterpret_cast<const uint4*>(from + c)[q] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  // their terms under f1 f2, and the largest finite of them (bits; not where it is not LARGEST)
+  template <int TERMS, bool SCALED, bool LARGEST>
+  __device__ __forceinline__ unsigned write(int a, const T* from, int c, int dim, float f1, float f2, unsigned short* out, int64_t next_term) const {
+    const uint32_t b[4] = {raw[a][0].x, raw[a][0].y, raw[a][0].z, raw[a][0].w};
+    unsigned short hi[8], lo[8];
+    unsigned m = 0;
+    if (SCALED && WIDE && sizeof(T) == 2) {
+      // eight bf16 numbers: two conversions an instruction, and the largest of them two at a time (beside an infinity
+      // or a NaN one by one)
+      uint32_t pair = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t h = half2_bits(__uint_as_float(b[k] << 16) * f1 * f2, __uint_as_float(b[k] & 0xffff0000u) * f1 * f2);
+        hi[2 * k] = (unsigned short)h;
+        hi[2 * k + 1] = (unsigned short)(h >> 16);
+        if (LARGEST) pair = __vmaxu2(pair, b[k] & 0x7fff7fffu);
+      }
+      if (LARGEST) {
+        const unsigned top = max(pair & 0xffffu, pair >> 16);
+        if (top < 0x7f80u) {
+          m = top << 16;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) m = max(m, max(finite_bits(__uint_as_float(b[k] << 16)), finite_bits(__uint_as_float(b[k] & 0xffff0000u))));
+        }
+      }
+    } else if (SCALED) {
+      float v[8];
+      if (WIDE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint4& w = raw[a][k / 4 % kLoads];
+          v[k] = __uint_as_float(k % 4 == 0 ? w.x : (k % 4 == 1 ? w.y : (k % 4 == 2 ? w.z : w.w)));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = from && c + k < dim ? to_f32(from[c + k]) : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (LARGEST) m = max(m, finite_bits(v[k]));
+        split_half(v[k] * f1 * f2, hi[k], lo[k]);
+      }
+    } else {
+      const unsigned short* x = reinterpret_cast<const unsigned short*>(from);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) hi[k] = WIDE ? (unsigned short)(b[k / 2] >> (k % 2 * 16)) : (from && c + k < dim ? x[c + k] : (unsigned short)0);
+    }
+    auto pack = [](const unsigned short (&x)[8]) {
+      return make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+    };
+    *reinterpret_cast<uint4*>(out + c) = pack(hi);
+    if (TERMS == 2) *reinterpret_cast<uint4*>(out + c + next_term) = pack(lo);
+    return m;
+  }
+};
+
+// W under one power of two, in pieces of eight columns whatever the rows.  AGAIN: only where it is of an unusual size.
 template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
-__global__ void __launch_bounds__(256) stage_kernel(Operand<T> w, Operand<T> h, int dim, int padded, int64_t w_blocks) {
-  after_previous();
-  const bool of_w = blockIdx.x < w_blocks;
-  const Operand<T>& o = of_w ? w : h;
-  const int64_t blocks = of_w ? w_blocks : gridDim.x - w_blocks, block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
+__device__ __forceinline__ void stage_weight(const Operands<T>& o) {
   int e = 0;
   if (SCALED) {
     e = usual_exponent(TERMS);
     if (AGAIN) {
-      const unsigned most = *o.most;
-      if (!unusual(most, TERMS)) return;
-      e = range_exponent(most);
+      if (!unusual(o.info->w_max, TERMS)) return;
+      e = range_exponent(o.info->w_max);
     }
   }
-  const float f = __uint_as_float((unsigned)(127 + e) << 23);
-  const int rows = (int)o.rows, n = o.count ? *o.count : rows;
-  const int whole = (n + kTile - 1) / kTile * kTile, upto = whole < (int)o.staged_rows ? whole : (int)o.staged_rows;
-  const uint32_t per = (uint32_t)padded / 8;
-  const int64_t items = (int64_t)(o.dead && upto < rows ? rows : upto) * per;
+  const float f = power_of_two(e);
+  const uint32_t per = (uint32_t)o.padded / 8;
+  const int64_t items = (int64_t)o.vocab * per;
   const bool small = items < 0x7fffffff;
   unsigned m = 0;
-  auto write = [&](int r, int c, const unsigned short (&hi)[8], const unsigned short (&lo)[8]) {
-    auto pack = [](const unsigned short (&x)[8]) {
-      return make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
-    };
-    *reinterpret_cast<uint4*>(o.out + (int64_t)r * padded + c) = pack(hi);
-    if (TERMS == 2) *reinterpret_cast<uint4*>(o.out + (o.staged_rows + r) * padded + c) = pack(lo);
-  };
-  // a thread's pieces of eight columns: what several of them need is on its way before the first is used
-  constexpr int kAhead = WIDE ? (sizeof(T) == 2 ? 4 : 2) : 1, kLoads = sizeof(T) == 2 ? 1 : 2;
-  for (int64_t i0 = block * (256 * kAhead) + threadIdx.x; i0 < items; i0 += blocks * (256 * kAhead)) {
-    uint4 raw[kAhead][kLoads];
-    int rr[kAhead], at[kAhead], cc[kAhead];            // (rows are 2^24 at the most)
+  using Pieces = Eights<T, WIDE>;
+  constexpr int kAhead = Pieces::kAhead;
+  for (int64_t i0 = (int64_t)blockIdx.x * (256 * kAhead) + threadIdx.x; i0 < items; i0 += o.w_blocks * (256 * kAhead)) {
+    Pieces x;
+    int rr[kAhead], cc[kAhead];            // (rows are 2^24 at the most)
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
       const int64_t i = i0 + a * 256;
-      rr[a] = i < items ? (int)(small ? (uint32_t)i / per : i / per) : INT32_MAX;
+      rr[a] = i < items ? (int)(small ? (uint32_t)i / per : i / per) : -1;
       cc[a] = i < items ? (int)((uint32_t)i - (uint32_t)rr[a] * per) * 8 : 0;
-      at[a] = o.row && rr[a] < rows ? o.row[rr[a]] : rr[a];
+      x.load(a, rr[a] >= 0 ? o.w + (int64_t)rr[a] * o.ld_w : nullptr, cc[a], o.dim);
     }
 #pragma unroll
     for (int a = 0; a < kAhead; ++a)
-#pragma unroll
-      for (int q = 0; q < kLoads; ++q)
-        raw[a][q] = WIDE && rr[a] < n && cc[a] + q * 4 < dim ? reinterpret_cast<const uint4*>(o.x + (int64_t)at[a] * o.ld + cc[a])[q] : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const int r = rr[a], c = cc[a];
-      if (r == INT32_MAX) continue;
-      if (r < upto) {
-        const uint32_t b[4] = {raw[a][0].x, raw[a][0].y, raw[a][0].z, raw[a][0].w};
-        unsigned short hi[8], lo[8];
-        if (SCALED && WIDE && sizeof(T) == 2) {
-          // eight bf16 numbers: two conversions an instruction, and the largest of them two at a time (beside an infinity
-          // or a NaN one by one)
-          uint32_t pair = 0;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t h = half2_bits(__uint_as_float(b[k] << 16) * f, __uint_as_float(b[k] & 0xffff0000u) * f);
-            hi[2 * k] = (unsigned short)h;
-            hi[2 * k + 1] = (unsigned short)(h >> 16);
-            if (!AGAIN) pair = __vmaxu2(pair, b[k] & 0x7fff7fffu);
-          }
-          if (!AGAIN) {
-            const unsigned top = max(pair & 0xffffu, pair >> 16);
-            if (top < 0x7f80u) {
-              m = max(m, top << 16);
-            } else {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) m = max(m, max(finite_bits(__uint_as_float(b[k] << 16)), finite_bits(__uint_as_float(b[k] & 0xffff0000u))));
-            }
-          }
-        } else if (SCALED) {
-          float v[8];
-          if (WIDE) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint4& w = raw[a][k / 4 % kLoads];
-              v[k] = __uint_as_float(k % 4 == 0 ? w.x : (k % 4 == 1 ? w.y : (k % 4 == 2 ? w.z : w.w)));
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = r < n && c + k < dim ? to_f32(o.x[(int64_t)at[a] * o.ld + c + k]) : 0.f;
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            if (!AGAIN) m = max(m, finite_bits(v[k]));
-            split_half(v[k] * f, hi[k], lo[k]);
-          }
-        } else {
-          const unsigned short* from = reinterpret_cast<const unsigned short*>(o.x) + (int64_t)at[a] * o.ld;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) hi[k] = WIDE ? (unsigned short)(b[k / 2] >> (k % 2 * 16)) : (r < n && c + k < dim ? from[c + k] : (unsigned short)0);
+      if (rr[a] >= 0)
+        m = max(m, x.template write<TERMS, SCALED, !AGAIN>(a, o.w + (int64_t)rr[a] * o.ld_w, cc[a], o.dim, f, 1.f, o.w_out + (int64_t)rr[a] * o.padded,
+                                                            (int64_t)o.vocab * o.padded));
+  }
+  if (SCALED && !AGAIN) block_largest(m, &o.info->w_max);
+}
+
+// The rows of h, `row_threads` each (8, 32 or 256), under a power of two each.  AGAIN: under one for all, where
+// they are not of one size and dW is wanted.
+template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
+__device__ __forceinline__ void stage_rows(const Operands<T>& o) {
+  __shared__ unsigned warp_m[2][8];
+  if (AGAIN && (!o.common_out || o.info->uneven == 0)) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, threads = o.row_threads, thread = (int)threadIdx.x % threads, at_once = 256 / threads;
+  const int64_t blocks = gridDim.x - o.w_blocks, block = blockIdx.x - o.w_blocks;
+  const int n = o.info->live, whole = (n + kTile - 1) / kTile * kTile, upto = whole < o.staged_rows ? whole : o.staged_rows;
+  const int last = o.dead && upto < o.rows ? o.rows : upto;
+  const int64_t next_term = (int64_t)o.staged_rows * o.padded;
+  unsigned short* to = AGAIN ? o.common_out : o.h_out;
+  using Pieces = Eights<T, WIDE>;
+  constexpr int kStep = 8 * Pieces::kAhead;
+  unsigned reach = 0, uneven = 0;
+  int turn = 0;
+  // (the lanes of a warp together, whatever rows they have)
+  for (int64_t r0 = block * at_once; r0 < last; r0 += blocks * at_once, turn ^= 1) {
+    const int64_t r = r0 + threadIdx.x / threads;
+    unsigned short* out = to + r * o.padded;
+    if (r >= n && r < last) {
+      if (r < upto)
+        for (int c = thread * 8; c < o.padded; c += threads * 8) {
+          *reinterpret_cast<uint4*>(out + c) = make_uint4(0u, 0u, 0u, 0u);
+          if (TERMS == 2) *reinterpret_cast<uint4*>(out + c + next_term) = make_uint4(0u, 0u, 0u, 0u);
         }
-        write(r, c, hi, lo);
+      if (!AGAIN && o.dead && r < o.rows)
+        for (int c = thread; c < o.dim; c += threads) o.dead[(int64_t)o.row[r] * o.ld_dead + c] = from_f64<T>(0.0);
+    }
+    if (r0 >= n) continue;
+    const bool on = r < n;
+    const T* from = on ? o.h + (int64_t)o.row[r] * o.ld_h : nullptr;
+    auto pass = [&](auto largest, int e) {
+      constexpr bool kLargest = decltype(largest)::value;
+      unsigned m = 0;
+      const float f1 = power_of_two(e / 2), f2 = power_of_two(e - e / 2);
+      for (int c0 = thread * 8; on && c0 < o.padded; c0 += threads * kStep) {
+        Pieces x;
+#pragma unroll
+        for (int a = 0; a < Pieces::kAhead; ++a) x.load(a, from, c0 + a * threads * 8, o.dim);
+#pragma unroll
+        for (int a = 0; a < Pieces::kAhead; ++a)
+          if (c0 + a * threads * 8 < o.padded)
+            m = max(m, x.template write<TERMS, SCALED, kLargest>(a, from, c0 + a * threads * 8, o.dim, f1, f2, out, next_term));
       }
-      if (!AGAIN && o.dead && r >= n && r < rows)
-        for (int k = 0; k < 8 && c + k < dim; ++k) o.dead[(int64_t)at[a] * o.ld_dead + c + k] = from_f64<T>(0.0);
+      return m;
+    };
+    if (AGAIN) {
+      pass(std::false_type{}, common_exponent(o.info, TERMS));
+    } else if (!SCALED) {
+      pass(std::false_type{}, 0);
+    } else {
+      unsigned m = pass(std::true_type{}, usual_exponent(TERMS));
+      if (threads < 32) {
+#pragma unroll
+        for (int d = 4; d; d >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+      } else {
+        m = __reduce_max_sync(0xffffffffu, m);
+      }
+      if (threads > 32) {
+        if (lane == 0) warp_m[turn][warp] = m;
+        __syncthreads();
+        m = __reduce_max_sync(0xffffffffu, warp_m[turn][lane & 7]);
+      }
+      const bool other = unusual(m, TERMS);
+      if (other) pass(std::false_type{}, range_exponent(m));
+      if (on && thread == 0) o.row_exponent[r] = operand_exponent(m, TERMS);
+      if (m) reach = max(reach, 1024u + (m >> 23) - 127u);
+      uneven |= other;
     }
   }
-  if (SCALED && !AGAIN) block_largest(m, o.most);
+  if (SCALED && !AGAIN) {
+    block_largest(reach, &o.info->reach);
+    if (uneven && thread == 0) o.info->uneven = 1;
+  }
+}
+
+template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
+__global__ void __launch_bounds__(256, WIDE ? 4 : 6) stage_kernel(const Operands<T> o) {
+  after_previous();
+  if (blockIdx.x < o.w_blocks) stage_weight<T, TERMS, SCALED, WIDE, AGAIN>(o);
+  else stage_rows<T, TERMS, SCALED, WIDE, AGAIN>(o);
 }
 
 // joins the sums of a row's blocks: log2 of the whole sum
@@ -1266,7 +1382,7 @@ dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mod
   const int live = info->live;
   if (first > 0 && live <= first) return;
   const bool last = first + piece >= live;
-  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? operand_exponent(info->h_max, terms_b(mode)) : 0)));
+  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? common_exponent(info, terms_b(mode)) : 0)));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)a.vocab * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
@@ -1605,10 +1721,11 @@ thin_dw_kernel(const float* h, int64_t ld_h, const int* row, int vocab, int dim,
 struct LossWs {
   LossInfo* info;
   int *counts, *row, *target;
+  int* row_exponent;
   float *g, *target_z;
   double* part;
   float2* sums;
-  unsigned short *h, *w, *e;
+  unsigned short *h, *h_common, *w, *e;
   float *slab, *shares, *dw;
   int blocks, piece, padded, vpadded, sum_blocks, staged_rows;
   bool few;               // M_FEW
@@ -1665,6 +1782,8 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   // (few rows have blocks of 32 columns and more)
   l->sums = (float2*)take((size_t)l->piece * (n <= kTile ? ceil_div(d->vocab, 32) : l->sum_blocks) * 8);
   l->h = (unsigned short*)take(l->thin ? 0 : (size_t)l->staged_rows * l->padded * 2 * terms);
+  l->h_common = (unsigned short*)take(gradient && !l->thin && !l->few ? (size_t)l->staged_rows * l->padded * 2 * terms : 0);
+  l->row_exponent = (int*)take(n * 4);
   l->w = (unsigned short*)take(l->in_place || l->thin ? 0 : v * l->padded * 2 * terms);
   l->e = (unsigned short*)take(gradient ? (size_t)l->piece * l->vpadded * 2 * held : 0);
   l->slab = (float*)take(gradient ? (size_t)l->piece * l->padded * 4 : 0);
@@ -1847,23 +1966,25 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     int* counts = l.blocks > 1 ? l.counts : nullptr;
     if (counts) MW_TRY(launch_after(count_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts));
     MW_TRY(launch_after(index_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts, l.blocks, l.row, l.target, l.g, loss, l.info));
-    Operand<T> oh = {h, a.ld_h, l.row, &l.info->live, a.rows, l.staged_rows, &l.info->h_max, l.h, dh, a.ld_dh};
-    Operand<T> ow = {w, a.ld_w, nullptr, nullptr, a.vocab, a.vocab, &l.info->w_max, l.w, nullptr, 0};
-    if (l.in_place) ow.rows = ow.staged_rows = 0;
+    Operands<T> o = {w, h, a.ld_w, a.ld_h, l.w, l.h, scaled && dw ? l.h_common : nullptr, l.row, l.row_exponent, l.in_place ? 0 : a.vocab, a.dim, l.padded,
+                     (int)a.rows, l.staged_rows, dh, a.ld_dh, l.info, 0, 0};
     auto aligned = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
     const bool rows16 = aligned(h, a.ld_h) && aligned(w, a.ld_w) && a.dim * (int64_t)sizeof(T) % 16 == 0;
-    // blocks by the operands' shares of the work, eight a multiprocessor at the most
-    auto blocks_for = [&](int64_t rows) {
-      const int64_t want = (rows * (l.padded / 8) + 511) / 512;
-      return want < 8 * (int64_t)sm_count() ? want : 8 * (int64_t)sm_count();
+    // a warp a row of h, a quarter of one a short row (16384 rows of 64: 5.2 us, by warps 12.4), a block a long one (1003 rows of 515
+    // fp32 are no faster by blocks: 10.9 us, by warps 9.3)
+    o.row_threads = l.padded <= (rows16 ? 256 : 64) ? 8 : (l.padded <= 2048 ? 32 : 256);
+    // blocks by the operands' shares of the work, eight a multiprocessor at the most of either
+    const int64_t most = 8 * (int64_t)sm_count(), want_w = ((int64_t)o.vocab * (l.padded / 8) + 511) / 512, want_h = ceil_div(a.rows + kTile, 256 / o.row_threads);
+    const int64_t bw = std::min(want_w, most), bh = std::min(want_h, most);
+    auto stage = [&](auto kernel, int64_t nw, int64_t nh) {
+      o.w_blocks = nw;
+      return launch_after(kernel, (unsigned)(nw + nh), 256, 0, s, o);
     };
-    const int64_t bw = blocks_for(ow.rows), bh = blocks_for(a.rows + kTile);
-    auto stage = [&](auto kernel, int64_t nw, int64_t nh) { return launch_after(kernel, (unsigned)(nw + nh), 256, 0, s, ow, oh, a.dim, l.padded, nw); };
     if (scaled) {
       // (the second seldom has anything to do: two blocks a multiprocessor see to that sooner than eight)
-      const int64_t few = 2 * (int64_t)sm_count(), fw = bw < few ? bw : few, fh = bh < few ? bh : few;
+      const int64_t few = 2 * (int64_t)sm_count();
       MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, false> : stage_kernel<T, TERMS, true, false, false>, bw, bh));
-      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>, fw, fh));
+      MW_TRY(stage(rows16 ? stage_kernel<T, TERMS, true, true, true> : stage_kernel<T, TERMS, true, false, true>, std::min(bw, few), std::min(bh, few)));
     } else {
       MW_TRY(stage(rows16 ? stage_kernel<T, 1, false, true, false> : stage_kernel<T, 1, false, false, false>, bw, bh));
     }
@@ -1881,6 +2002,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     p.piece = l.piece;
     p.sum_blocks = l.sum_blocks;
     p.sums = l.sums; p.target_z = l.target_z; p.target = l.target;
+    p.row_exponent = scaled ? l.row_exponent : nullptr;
     // (few rows: CTAs of their own)
     const bool single = a.rows <= kHalf;
     const int pairs = sm_count() / 2, tile_m = single ? kHalf : kTile;
@@ -1927,6 +2049,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       by_w.idesc = instruction(bf16, true, true);
       MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece, row_bytes, group_bytes, 128, held, kBK, 2));
       MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
+      if (scaled) MW_TRY(group_map(&by_w.b_common, l.h_common, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
       // tiles for less than half of the pairs: each in shares of K, of eight blocks at least
       const int tiles = by_w.tiles_m * by_w.tiles_n;
       if (2 * tiles <= pairs && by_w.blocks_k >= 16) {

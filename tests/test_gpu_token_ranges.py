@@ -1,0 +1,78 @@
+"""The vocabulary's loss of rows that differ by many powers of two: a row's loss and dh keep their digits whatever stands
+beside it, in h or among the row weights.
+
+Tolerances are those of test_gpu_token_loss.py, without what they allow a row for the weights of others: dh_i = g_i times the
+dh_i of weight one, so its bound is |g_i| times the bound there.  In dweight the rows meet: h_i times 2^x, x by its weight,
+is held in half precision (two terms of float operands) with the largest number at 2^13 and more, so each is off by 2^-25 of
+that scale, and its dz, relative to its weight at most |p - [j = t]|, times 2^14: 2^-37 max_i(|g_i| max |h_i|) sum_i |p_ij - [j = t_i]|."""
+import pytest
+import torch
+
+from paper_2402_14212_b200 import binding as mwb
+from test_gpu_token_loss import ALL, BF16, F32, check, make, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def by_weight(want, w):
+    """Values and bounds of dh of weight one, turned into those of the weights w."""
+    value, bound = want["dh"]
+    return dict(want, dh=(value * w.double()[:, None], bound * w.double().abs()[:, None]))
+
+
+def meeting(want, h, W, t, w, scale=1.0):
+    """dweight's bound with what rows of different sizes lose there."""
+    p = torch.softmax(scale * h.double() @ W.double().T, 1)
+    d = p.scatter_add(1, t[:, None], -torch.ones(len(t), 1, device="cuda", dtype=torch.float64)).abs().sum(0)
+    value, bound = want["dweight"]
+    most = float((w.double().abs() * h.double().abs().amax(1)).max())
+    return dict(want, dweight=(value, bound + 2.0 ** -37 * most * abs(scale) * d[:, None]))
+
+
+@pytest.mark.parametrize("N,dtype", [(5, F32), (9, F32), (100, F32), (300, F32), (9, BF16), (129, BF16), (300, BF16)])
+@pytest.mark.parametrize("size", [-40, -20, 12, 20, 32, 60])
+def test_one_row_far_larger_or_smaller_than_the_others(size, N, dtype):
+    h, W, t = make(N, 700, 128, dtype, seed=N, lean=4.0)
+    h[3] *= 2.0 ** size
+    want = meeting(reference(h, W, t), h, W, t, torch.full((N,), 1 / N, device="cuda"))
+    check(mwb.token_loss(h, W, t), want, ("loss", "total"))
+    check(mwb.token_loss_gradient(h, W, t), want, ALL)
+    check(mwb.token_loss_gradient(h, W, t, piece_rows=256), want, ALL)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [40, 300, 1500])
+def test_rows_of_every_size(N, dtype):
+    """Rows from 2^-30 to 2^30 beside one another, targets left out among them."""
+    h, W, t = make(N, 333, 200, dtype, seed=N, lean=2.0)
+    h *= torch.exp2((torch.arange(N, device="cuda") % 61 - 30.0))[:, None]
+    t[::7] = -1
+    h[::7] = float("nan")
+    on = (t >= 0).float()
+    want = reference(h, W, t)
+    hc, tc = torch.where(on[:, None] > 0, h, torch.zeros_like(h)), t.clamp(min=0)
+    want = meeting(want, hc, W, tc, on / on.sum())
+    check(mwb.token_loss(h, W, t), want, ("loss", "total"))
+    for piece in (0, 256):
+        check(mwb.token_loss_gradient(h, W, t, piece_rows=piece), want, ALL)
+
+
+def test_captured_calls_of_even_and_uneven_rows():
+    """One graph, replayed on rows of one size and of many, with weights alike and not."""
+    N, V, D = 300, 500, 128
+    h, W, t = make(N, V, D, BF16)
+    w = torch.full((N,), 1 / N, device="cuda")
+    call = lambda: mwb.token_loss_gradient(h, W, t, row_weight=w)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for size, weight in ((0, 0), (24, 0), (24, 24), (0, 0)):
+        for a, b in zip((h, W, t), make(N, V, D, BF16, seed=size + weight)):
+            a.copy_(b)
+        h[5] *= 2.0 ** size
+        w[6] = 2.0 ** weight / N
+        graph.replay()
+        got = [x.clone() for x in held]
+        assert all(torch.equal(a, b) for a, b in zip(got, call()))
