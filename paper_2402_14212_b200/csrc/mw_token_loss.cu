@@ -112,12 +112,12 @@ struct LossInfo {
   DeviceStatus st;
   unsigned pad[59];
   int live;                 // rows that are not left out
-  unsigned g_max;           // bits of the largest |g|
+  unsigned g_max, g_far;    // bits of the largest finite |g|, and how far those of the smallest lie below 2^31
   unsigned w_max;           // bits of the largest finite |W|
-  unsigned reach;           // 1024 + the largest power of two in the rows of h (0: zeros alone)
+  unsigned reach;           // 1024 + the largest power of two of |g| |h|, a row's largest (0: zeros alone)
   unsigned uneven;          // some row of h is of an unusual size
   unsigned done;            // blocks whose losses are in
-  unsigned pad2[58];
+  unsigned pad2[57];
 };
 
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }      // of -126..127
@@ -144,11 +144,26 @@ __device__ __forceinline__ bool unusual(unsigned most, int terms) {
 __device__ __forceinline__ int operand_exponent(unsigned most, int terms) {
   return unusual(most, terms) ? range_exponent(most) : usual_exponent(terms);
 }
-// Rows of h have a power of two each for the logits, which an epilogue's lane takes out of its row.  The sums of dW run over
-// the rows, which want one for all of them: where they have the usual one alike, the same operand serves; else dW has an
-// operand of its own, whose largest number is brought to 2^13 .. 2^14.
-__device__ __forceinline__ int common_exponent(const LossInfo* info, int terms) {
-  return info->uneven == 0 ? usual_exponent(terms) : (info->reach ? 13 + 1024 - (int)info->reach : 0);
+// ... of a row's dz, by its weight (any finite one above 2^-113 to 2^13 .. 2^14); dz of float exponentials that are bf16 numbers
+// or floats has that type's range, and no power
+__device__ __forceinline__ int weight_exponent(unsigned bits) {
+  const int e = (int)(bits >> 23) - 127;
+  return e > 127 ? 0 : (13 - e > 126 ? 126 : 13 - e);
+}
+__device__ __forceinline__ int weight_exponent(float g) { return weight_exponent(__float_as_uint(fabsf(g))); }
+// Rows of h and of dz have powers of two of their own: the logits' epilogue and the last kernel of dh, whose lanes have a row,
+// take them out.  dW's sums run over the rows.  Where these are of one size, dz and h have one power each in truth; else dW
+// takes h from an operand of its own, in which each row lies as far down as its dz was taken up, under one power for all: the
+// rows whose |g| |h| is largest are brought to 2^13 .. 2^14, and what others lose there is small beside those.
+__device__ __forceinline__ bool of_one_size(const LossInfo* info) {
+  return info->uneven == 0 && weight_exponent(info->g_max) == weight_exponent(0x7fffffffu - info->g_far);
+}
+__device__ __forceinline__ int common_exponent(const LossInfo* info) { return info->reach ? 13 + 1024 - (int)info->reach : 0; }
+// what dW's sums are too large by
+__device__ __forceinline__ float dweight_factor(const LossInfo* info, double scale, bool scaled, int terms) {
+  if (!scaled) return (float)scale;
+  const int e = of_one_size(info) ? usual_exponent(terms) + weight_exponent(info->g_max) : common_exponent(info);
+  return fminf(fmaxf((float)ldexp(scale, -e), -3e38f), 3e38f);
 }
 
 struct LossArgs {
@@ -439,7 +454,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     const uint32_t full0_even = PAIR ? map_to_cta(full0, 0u) : full0;
     const int share_n = KIND == P_SUMS ? (PAIR ? p.tile_n / 2 : p.tile_n) : kShareB;
     const uint32_t tx = (PAIR ? 2u : 1u) * (a_stage + b_stage / kShareB * (uint32_t)share_n);
-    const CUtensorMap* by_rows = KIND == P_DW && p.scaled && p.info->uneven ? &p.b_common : &p.b;
+    const CUtensorMap* by_rows = KIND == P_DW && p.scaled && !of_one_size(p.info) ? &p.b_common : &p.b;
     bool ok = true;
     for (int u = pair; u < units && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live, plan);
@@ -524,10 +539,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     bool ok = true;
     float factor = 1.f;
     int exponent = 0;                               // factor's, but for a row's own (logits)
-    if (KIND == P_DW) {
-      const int exps = p.scaled ? common_exponent(p.info, kTermsB) : 0;
-      factor = (float)ldexp((double)p.scale, -(range_exponent(p.info->g_max) + exps));
-    }
+    if (KIND == P_DW) factor = dweight_factor(p.info, p.scale, p.scaled, kTermsB);
     if (of_logits(KIND)) {
       factor = (float)frexp((double)p.scale * 1.4426950408889634, &exponent);
       if (p.scaled) exponent -= operand_exponent(p.info->w_max, kTermsB);
@@ -838,14 +850,21 @@ index_live_kernel(const I* targets, const float* weight, int64_t rows, int vocab
   for (int w = 0; w < warp; ++w) at += warp_sum[w];
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     info->live = live;
-    if (!weight && live > 0) info->g_max = __float_as_uint(1.f / (float)live);
+    if (!weight && live > 0) {
+      info->g_max = __float_as_uint(1.f / (float)live);
+      info->g_far = 0x7fffffffu - info->g_max;
+    }
   }
   if (i >= rows) return;
   if (t >= 0) {
     row[at] = (int)i;
     target[at] = t;
     g[at] = weight ? weight[i] : 1.f / (float)live;
-    if (weight) atomicMax(&info->g_max, __float_as_uint(fabsf(weight[i])));
+    const unsigned bits = __float_as_uint(fabsf(g[at]));
+    if (weight && bits < 0x7f800000u) {
+      atomicMax(&info->g_max, bits);
+      atomicMax(&info->g_far, 0x7fffffffu - bits);
+    }
   } else {
     row[rows - 1 - (i - at)] = (int)i;
     loss[i] = 0.f;
@@ -894,8 +913,9 @@ struct Operands {
   const T *w, *h;
   int64_t ld_w, ld_h;
   unsigned short *w_out, *h_out;
-  unsigned short* common_out;     // h under one power of two (null: not wanted)
+  unsigned short* common_out;     // h as dW wants it where the rows are not of one size (null: not wanted)
   const int* row;
+  const float* g;
   int* row_exponent;
   int vocab, dim, padded;
   int rows, staged_rows;          // of h
@@ -1011,12 +1031,11 @@ __device__ __forceinline__ void stage_weight(const Operands<T>& o) {
   if (SCALED && !AGAIN) block_largest(m, &o.info->w_max);
 }
 
-// The rows of h, `row_threads` each (8, 32 or 256), under a power of two each.  AGAIN: under one for all, where
-// they are not of one size and dW is wanted.
+// The rows of h, `row_threads` each (8, 32 or 256), under a power of two each.  AGAIN: for dW, where they are not of one size.
 template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
 __device__ __forceinline__ void stage_rows(const Operands<T>& o) {
   __shared__ unsigned warp_m[2][8];
-  if (AGAIN && (!o.common_out || o.info->uneven == 0)) return;
+  if (AGAIN && (!o.common_out || of_one_size(o.info))) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, threads = o.row_threads, thread = (int)threadIdx.x % threads, at_once = 256 / threads;
   const int64_t blocks = gridDim.x - o.w_blocks, block = blockIdx.x - o.w_blocks;
   const int n = o.info->live, whole = (n + kTile - 1) / kTile * kTile, upto = whole < o.staged_rows ? whole : o.staged_rows;
@@ -1059,7 +1078,8 @@ __device__ __forceinline__ void stage_rows(const Operands<T>& o) {
       return m;
     };
     if (AGAIN) {
-      pass(std::false_type{}, common_exponent(o.info, TERMS));
+      const int e = common_exponent(o.info) - (on ? weight_exponent(o.g[r]) : 0);
+      pass(std::false_type{}, e < -250 ? -250 : (e > 250 ? 250 : e));
     } else if (!SCALED) {
       pass(std::false_type{}, 0);
     } else {
@@ -1078,7 +1098,7 @@ __device__ __forceinline__ void stage_rows(const Operands<T>& o) {
       const bool other = unusual(m, TERMS);
       if (other) pass(std::false_type{}, range_exponent(m));
       if (on && thread == 0) o.row_exponent[r] = operand_exponent(m, TERMS);
-      if (m) reach = max(reach, 1024u + (m >> 23) - 127u);
+      if (m && fabsf(o.g[r]) < INFINITY) reach = max(reach, (unsigned)(1024 + (int)(m >> 23) - 127 - weight_exponent(o.g[r])));
       uneven |= other;
     }
   }
@@ -1223,7 +1243,6 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
   int upto = (live + kBK - 1) / kBK * kBK;            // (behind the piece's rows the copy engine brings zeros)
   upto = MODE == M_THIN ? live : (upto < piece ? upto : piece);
   const int warp = WARPS == 1 ? 0 : (int)(threadIdx.x >> 5), lane = threadIdx.x & 31, thread = (int)threadIdx.x % kThreads;
-  const float to_range = MODE == M_THIN ? 1.f : __uint_as_float((unsigned)(127 + range_exponent(info->g_max)) << 23);
   for (int b = (int)blockIdx.x; b * kRows < upto * slices; b += gridDim.x) {
     const int slice = b % slices, r = b / slices * kRows + (WARPS == 1 ? (int)(threadIdx.x >> 5) : 0);
     if (WARPS == 1 && r >= upto) break;
@@ -1249,7 +1268,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       loss[row[i]] = end.loss;
       part[i] = (double)g[i] * (double)end.loss;
     }
-    const float gi = g[i] * to_range, at_target = -gi * end.less, share = gi / end.total;
+    const float gi = g[i] * (MODE == M_ONE || MODE == M_TWO ? power_of_two(weight_exponent(g[i])) : 1.f), at_target = -gi * end.less, share = gi / end.total;
     // (four accesses of a thread under way)
     constexpr int kAhead = 4;
     if (TERMS == 1) {
@@ -1338,12 +1357,14 @@ __device__ __forceinline__ void put(__nv_bfloat16* at, float v) { *at = __float2
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
 dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, int tiles_n, int blocks_k, int workers, int room, int mode, int first,
-               int piece, const int* row, const LossInfo* info, T* dh) {
+               int piece, const int* row, const float* g, const LossInfo* info, T* dh) {
   after_previous();
   int live = info->live - first;
   live = live < 0 ? 0 : (live < piece ? live : piece);
-  float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? operand_exponent(info->w_max, terms_b(mode)) : 0)));
-  if (info->st.code != 0) f = __int_as_float(0x7fffffff);
+  int exponent = 0;
+  float mantissa = (float)frexp((double)a.scale, &exponent);
+  if (a.scaled) exponent -= operand_exponent(info->w_max, terms_b(mode));
+  if (info->st.code != 0) mantissa = __int_as_float(0x7fffffff);
   const DhPlan plan = dh_plan(live, tiles_n, blocks_k, workers, room, products_of(mode));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)live * per;
@@ -1359,7 +1380,11 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
         v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
       }
     }
-    v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+    // (two factors: their product may lie below a float's range where dh does not)
+    int x = exponent - (a.scaled ? weight_exponent(g[first + r]) : 0);
+    x = x < -250 ? -250 : (x > 250 ? 250 : x);
+    const float f1 = mantissa * power_of_two(x / 2), f2 = power_of_two(x - x / 2);
+    v.x = v.x * f1 * f2; v.y = v.y * f1 * f2; v.z = v.z * f1 * f2; v.w = v.w * f1 * f2;
     T* to = dh + (int64_t)row[first + r] * a.ld_dh + c;
     if (WIDE) {
       if (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = v;
@@ -1382,7 +1407,7 @@ dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mod
   const int live = info->live;
   if (first > 0 && live <= first) return;
   const bool last = first + piece >= live;
-  const float f = (float)ldexp((double)a.scale, -(range_exponent(info->g_max) + (a.scaled ? common_exponent(info, terms_b(mode)) : 0)));
+  const float f = dweight_factor(info, a.scale, a.scaled, terms_b(mode));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;
   const int64_t items = (int64_t)a.vocab * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
@@ -1966,7 +1991,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     int* counts = l.blocks > 1 ? l.counts : nullptr;
     if (counts) MW_TRY(launch_after(count_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts));
     MW_TRY(launch_after(index_live_kernel<I>, l.blocks, kIndexRows, 0, s, targets, weight, a.rows, a.vocab, counts, l.blocks, l.row, l.target, l.g, loss, l.info));
-    Operands<T> o = {w, h, a.ld_w, a.ld_h, l.w, l.h, scaled && dw ? l.h_common : nullptr, l.row, l.row_exponent, l.in_place ? 0 : a.vocab, a.dim, l.padded,
+    Operands<T> o = {w, h, a.ld_w, a.ld_h, l.w, l.h, scaled && dw ? l.h_common : nullptr, l.row, l.g, l.row_exponent, l.in_place ? 0 : a.vocab, a.dim, l.padded,
                      (int)a.rows, l.staged_rows, dh, a.ld_dh, l.info, 0, 0};
     auto aligned = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
     const bool rows16 = aligned(h, a.ld_h) && aligned(w, a.ld_w) && a.dim * (int64_t)sizeof(T) % 16 == 0;
@@ -2095,7 +2120,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
           MW_TRY((run_product<TERMS, P_DH>(l.few, single, by_h, p.workers, s)));
           auto rows_kernel = ((uintptr_t)dh & 15) == 0 && a.ld_dh % 4 == 0 && a.dim % 4 == 0 ? dh_rows_kernel<T, true> : dh_rows_kernel<T, false>;
           MW_TRY(launch_after(rows_kernel, wide, 256, 0, s, a, l.slab, l.shares, l.padded, by_h.tiles_n, by_h.blocks_k, p.workers, p.share_room, mode, (int)first, l.piece,
-                              l.row, l.info, dh));
+                              l.row, l.g, l.info, dh));
         }
       }
       if (dw) {

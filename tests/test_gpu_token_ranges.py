@@ -57,6 +57,50 @@ def test_rows_of_every_size(N, dtype):
         check(mwb.token_loss_gradient(h, W, t, piece_rows=piece), want, ALL)
 
 
+@pytest.mark.parametrize("N,dtype", [(8, F32), (9, F32), (100, F32), (300, F32), (9, BF16), (129, BF16), (300, BF16)])
+@pytest.mark.parametrize("light", [1e-3, 1e-6, 1e-8, 2.0 ** -40, 2.0 ** -80])
+def test_light_rows_keep_their_digits(light, N, dtype):
+    h, W, t = make(N, 700, 128, dtype, seed=N, lean=4.0)
+    w = torch.rand(N, device="cuda") + 0.5
+    w[1::2] *= light
+    w[::5] *= -1
+    one = reference(h, W, t, weight=torch.ones(N, device="cuda"))
+    want = dict(reference(h, W, t, weight=w), dh=by_weight(one, w)["dh"])
+    want = meeting(want, h, W, t, w)
+    for piece in (0, 256):
+        check(mwb.token_loss_gradient(h, W, t, row_weight=w, piece_rows=piece), want, ALL)
+
+
+@pytest.mark.parametrize("N,dtype", [(8, F32), (9, F32), (300, F32), (129, BF16), (300, BF16), (1500, BF16)])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_weight_that_is_not_finite_stays_in_its_row(bad, N, dtype):
+    h, W, t = make(N, 700, 128, dtype, seed=N, lean=4.0)
+    w = torch.full((N,), 2.0 ** -13, device="cuda")
+    w[4] = bad
+    one = reference(h, W, t, weight=torch.ones(N, device="cuda"))
+    r = mwb.token_loss_gradient(h, W, t, row_weight=w)
+    assert not bool(torch.isfinite(r.dh[4]).any()) and not bool(torch.isfinite(r.total))
+    rest = torch.arange(N, device="cuda") != 4
+    w[4] = 1.0
+    want = by_weight(one, w)
+    value, bound = (x[rest] for x in want["dh"])
+    check(mwb.TokenLoss(r.loss, None, r.dh[rest]), dict(want, dh=(value, bound)), ("loss", "dh"))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_weights_and_rows_of_every_size(dtype):
+    """Weights and rows of h go against one another, so that g_i h_i is of one size and every row counts in dweight."""
+    N = 700
+    h, W, t = make(N, 333, 136, dtype, lean=2.0)
+    x = torch.exp2(torch.arange(N, device="cuda") % 41 - 20.0)
+    h, w = h * x[:, None].to(dtype), (torch.rand(N, device="cuda") + 0.5) / x
+    one = reference(h, W, t, weight=torch.ones(N, device="cuda"))
+    want = dict(reference(h, W, t, weight=w), dh=by_weight(one, w)["dh"])
+    want = meeting(want, h, W, t, w)
+    for piece in (0, 256):
+        check(mwb.token_loss_gradient(h, W, t, row_weight=w, piece_rows=piece), want, ALL)
+
+
 def test_captured_calls_of_even_and_uneven_rows():
     """One graph, replayed on rows of one size and of many, with weights alike and not."""
     N, V, D = 300, 500, 128
@@ -68,7 +112,7 @@ def test_captured_calls_of_even_and_uneven_rows():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         held = call()
-    for size, weight in ((0, 0), (24, 0), (24, 24), (0, 0)):
+    for size, weight in ((0, 0), (24, 0), (0, 24), (24, 24), (0, 0)):
         for a, b in zip((h, W, t), make(N, V, D, BF16, seed=size + weight)):
             a.copy_(b)
         h[5] *= 2.0 ** size
