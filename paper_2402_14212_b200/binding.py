@@ -997,7 +997,29 @@ class TokenLoss(NamedTuple):
     dweight: object = None
 
 
-def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want):
+def token_loss_workspace(h, weight, gradient: bool = False, piece_rows: int = 0):
+    """Memory for token_loss (or token_loss_gradient) calls with this h and weight, for their `workspace`."""
+    import torch
+    _need(h.is_cuda and h.dim() == 2 and weight.dim() == 2, "token_loss_workspace: CUDA tensors [rows, columns]")
+    d = TokenLossDesc(h.shape[0], weight.shape[0], h.shape[1], _operand_dtype(h, "token_loss_workspace"), 0, 8, int(piece_rows), 0, 0,
+                      0, 0, 1.0)
+    need, most = C.c_size_t(), 0
+    rows_apart = weight.shape[1] if _repeats(weight) else _table_rows(weight, "token_loss_workspace: weight")
+    with torch.cuda.device(h.device):
+        for d.ld_weight in {rows_apart, weight.shape[1]}:          # (as it is, or copied)
+            _check(lib().mw_token_loss_workspace_bytes(d, int(bool(gradient)), need), "mw_token_loss_workspace_bytes")
+            most = max(most, int(need.value))
+    return torch.empty(most + 256, dtype=torch.uint8, device=h.device)
+
+
+def token_loss_status(workspace, stream=None) -> int:
+    """Waits for the stream; the first device-side error of the last token_loss or token_loss_gradient call on this
+    workspace (0: none)."""
+    wp, _ = Net._ws(workspace)
+    return int(_call("mw_token_loss_status", workspace.device, wp, stream=stream))
+
+
+def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want, workspace=None):
     import torch
     key = ("token loss", gradient, scale, piece_rows, grad_dtype, want, _layout(h), _layout(weight), _layout(targets),
            _layout(row_weight), _layout(dh), _layout(dweight))
@@ -1006,7 +1028,7 @@ def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, gra
         _need(h.is_cuda, "token_loss: CUDA tensors")
         if _repeats(h) or _repeats(weight):
             h, weight = _own_memory(h, weight)
-            return _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want)
+            return _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want, workspace)
         _need(h.dim() == 2 and weight.dim() == 2 and h.shape[1] == weight.shape[1] and h.dtype == weight.dtype,
               "token_loss: h is [rows, columns], weight [vocabulary, columns] of the same type")
         _need(tuple(targets.shape) == (h.shape[0],) and targets.is_contiguous(), "token_loss: targets are contiguous, [rows]")
@@ -1033,49 +1055,57 @@ def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, gra
     device = h.device
     loss = torch.empty(h.shape[0], dtype=torch.float32, device=device)
     total = torch.empty((), dtype=torch.float32, device=device)
-    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        at = ws.data_ptr()
+    else:
+        _need(workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.device == device,
+              f"token_loss: workspace is of bytes (uint8) on {device}")
+        at, room = Net._ws(workspace)
+        _need(room >= need, f"token_loss: workspace of {need} bytes from a multiple of 256 on")
     if not gradient:
         _check(_call("mw_token_loss_forward", device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
-                     _ptr(row_weight), loss.data_ptr(), total.data_ptr(), ws.data_ptr(), need), "mw_token_loss_forward")
+                     _ptr(row_weight), loss.data_ptr(), total.data_ptr(), at, need), "mw_token_loss_forward")
         return TokenLoss(loss, total)
     if dh is None and want[0]:
         dh = _dense_like(h)
     if dweight is None and want[1]:
         dweight = torch.empty(weight.shape, dtype=kind, device=device)
     _check(_call("mw_token_loss_gradient", device, d, h.data_ptr(), weight.data_ptr(), targets.data_ptr(),
-                 _ptr(row_weight), loss.data_ptr(), total.data_ptr(), _ptr(dh), _ptr(dweight), ws.data_ptr(), need),
+                 _ptr(row_weight), loss.data_ptr(), total.data_ptr(), _ptr(dh), _ptr(dweight), at, need),
            "mw_token_loss_gradient")
     return TokenLoss(loss, total, dh, dweight)
 
 
-def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=None) -> TokenLoss:
+def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=None, workspace=None) -> TokenLoss:
     """Softmax cross entropy of z = scale * h weight^T over a vocabulary, the logits never held: h [rows, columns]
     and weight [vocabulary, columns] float32 or bfloat16, targets int32 or int64 [rows].  Rows whose target is no row
     of weight (a negative one, say), or whose row_weight is zero, are left out: their loss is zero and their h is
     not read into anything.  total = sum of row_weight * loss, the mean over the rows that are left without
-    row_weight.  `stream` as in gated_scan."""
+    row_weight.  workspace: memory of token_loss_workspace, which no other call in flight uses and from which
+    token_loss_status reads whether all went well; a call's own otherwise.  `stream` as in gated_scan."""
     import torch
     if stream is not None:
-        return _on_stream(stream, h, token_loss, h, weight, targets, scale, row_weight)
+        return _on_stream(stream, h, token_loss, h, weight, targets, scale, row_weight, None, workspace)
     if weight.data_ptr() & 15:         # (read in place, by copies of 16 bytes)
         weight = weight.clone(memory_format=torch.contiguous_format)
-    return _token_loss(False, h, weight, targets, scale, row_weight, 0, None, None, None, (False, False))
+    return _token_loss(False, h, weight, targets, scale, row_weight, 0, None, None, None, (False, False), workspace)
 
 
 def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None, dh=None, dweight=None,
-                        grad_dtype=None, want=(True, True), piece_rows: int = 0, stream=None) -> TokenLoss:
+                        grad_dtype=None, want=(True, True), piece_rows: int = 0, stream=None, workspace=None) -> TokenLoss:
     """token_loss, and the gradients of its total: dh (zero in rows left out; may be h itself) and dweight
     (float32 or bfloat16 by grad_dtype, weight's type where None).  want: which of the two.  piece_rows: rows whose
-    exponentials are held at a time (0: as many as take 1 GiB); fewer take less memory and more time.  `stream` as
-    in gated_scan."""
+    exponentials are held at a time (0: as many as take 1 GiB); fewer take less memory and more time.  dz of bf16
+    operands has 11 bits, which a float32 dweight shows.  `workspace` as in token_loss, `stream` as in gated_scan."""
     import torch
     if stream is not None:
         return _on_stream(stream, h, token_loss_gradient, h, weight, targets, scale, row_weight, dh, dweight, grad_dtype,
-                          want, piece_rows)
+                          want, piece_rows, None, workspace)
     if weight.data_ptr() & 15 and targets.numel() <= 128:         # (of few rows read in place, by copies of 16 bytes)
         weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(True, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight,
-                       (bool(want[0]), bool(want[1])))
+                       (bool(want[0]), bool(want[1])), workspace)
 
 
 def clip_gradients(grads, max_norm: float, out=None, stream=None):
