@@ -495,8 +495,11 @@ mw_status mw_token_loss_gradient(const mw_token_loss_desc* desc, const void* h, 
                                  const void* targets, const float* row_weight, float* loss, float* total, void* dh,
                                  void* dweight, void* workspace, size_t workspace_bytes, void* stream);
 /* Synchronise `stream`, return the first device-side error recorded in the workspace by the last call.  Where a bounded
- * wait of the products ran out (2 s) the total is NaN, and what was formed after it. */
+ * wait of the products ran out (2 s) the total is NaN, and so is of losses, dh and dweight what was formed after it. */
 mw_status mw_token_loss_status(const void* workspace, void* stream);
+/* Self-test: this thread's next calls hold a wait that nothing meets and that runs out after limit_ms (1..1000; 0 ends it),
+ * in the product of the logits (0), of dh (1) or of dweight (2).  Calls of up to 8 rows of float operands have none. */
+mw_status mw_token_loss_selftest_unmet_wait(uint32_t limit_ms, int32_t product);
 
 /* Clipping by the norm of all gradients together:
  *   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)

@@ -149,6 +149,7 @@ def lib() -> C.CDLL:
         L.mw_token_loss_forward.argtypes = [tloss] + [vp] * 7 + [sz, vp]
         L.mw_token_loss_gradient.argtypes = [tloss] + [vp] * 9 + [sz, vp]
         L.mw_token_loss_status.argtypes = [vp, vp]
+        L.mw_token_loss_selftest_unmet_wait.argtypes = [C.c_uint32, i32]
         L.mw_clip_scratch_bytes.argtypes = [i32, C.POINTER(sz)]
         L.mw_clip_gradients.argtypes = [i32, vp, vp, vp, vp, C.c_double, vp, vp, sz, vp]     # (arrays by their addresses)
         L.mw_profile_begin.argtypes = []
@@ -1017,6 +1018,12 @@ def token_loss_status(workspace, stream=None) -> int:
     workspace (0: none)."""
     wp, _ = Net._ws(workspace)
     return int(_call("mw_token_loss_status", workspace.device, wp, stream=stream))
+
+
+def token_loss_selftest_unmet_wait(limit_ms: int, product: int = 0):
+    """The calls of this thread hold a wait that nothing meets and that runs out after limit_ms (0 ends it): in the
+    product of the logits (0), of dh (1) or of dweight (2)."""
+    _check(lib().mw_token_loss_selftest_unmet_wait(int(limit_ms), int(product)), "mw_token_loss_selftest_unmet_wait")
 
 
 def _token_loss(gradient, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight, want, workspace=None):

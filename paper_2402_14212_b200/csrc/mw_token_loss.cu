@@ -57,6 +57,9 @@ constexpr int kFewRegisters = 104, kManyRegisters = 200;
 constexpr uint32_t kPlaneBytes = kHalf * kBK * 2;       // one term of one operand of one stage and CTA
 constexpr uint32_t kBufferBytes = 32 * 128;             // 32 rows of 128 bytes of an epilogue warp
 constexpr uint64_t kLossWaitNs = 2000000000ull;
+// self-test of this thread's calls: the product of which a CTA's rows are not copied, and how long they are waited for
+thread_local uint32_t unmet_ms = 0;
+thread_local int unmet_product = 0;
 enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
 // How operands are held.  M_ONE: one term (bf16 as it is in the loss alone, half precision times a power of two in the
 // gradient).  M_TWO: fp32 as two half-precision terms.  M_FEW: the gradient of few rows of bf16, whose time is the
@@ -159,8 +162,9 @@ __device__ __forceinline__ bool of_one_size(const LossInfo* info) {
   return info->uneven == 0 && weight_exponent(info->g_max) == weight_exponent(0x7fffffffu - info->g_far);
 }
 __device__ __forceinline__ int common_exponent(const LossInfo* info) { return info->reach ? 13 + 1024 - (int)info->reach : 0; }
-// what dW's sums are too large by
+// what dW's sums are too large by (NaN where a wait ran out before)
 __device__ __forceinline__ float dweight_factor(const LossInfo* info, double scale, bool scaled, int terms) {
+  if (info->st.code != 0) return __int_as_float(0x7fffffff);
   if (!scaled) return (float)scale;
   const int e = of_one_size(info) ? usual_exponent(terms) + weight_exponent(info->g_max) : common_exponent(info);
   return fminf(fmaxf((float)ldexp(scale, -e), -3e38f), 3e38f);
@@ -180,6 +184,8 @@ struct alignas(64) ProductArgs {
   const LossInfo* info;
   DeviceStatus* st;
   float* total;             // NaN where a wait ran out
+  uint64_t wait_ns;
+  int unmet;                // self-test: A of the first CTA is not copied
   int first, piece;         // rows of this piece begin at `first` of the live ones
   int vocab, dim;
   int tiles_m, tiles_n;     // of the whole piece (P_DW: of the vocabulary and the columns)
@@ -431,7 +437,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   WaitCtx wc;
   wc.st = p.st;
   wc.abort_flag = &abort_flag;
-  wc.limit_ns = kLossWaitNs;
+  wc.limit_ns = p.wait_ns;
   after_previous();
   if (KIND == P_SUMS && p.direct && blockIdx.x == 0 && threadIdx.x < sizeof(LossInfo) / 4)
     reinterpret_cast<unsigned*>(p.clear)[threadIdx.x] = 0;
@@ -454,9 +460,10 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     const uint32_t full0_even = PAIR ? map_to_cta(full0, 0u) : full0;
     const int share_n = KIND == P_SUMS ? (PAIR ? p.tile_n / 2 : p.tile_n) : kShareB;
     const uint32_t tx = (PAIR ? 2u : 1u) * (a_stage + b_stage / kShareB * (uint32_t)share_n);
+    const int some = p.unmet && of_a && blockIdx.x == 0 ? 0 : units;
     const CUtensorMap* by_rows = KIND == P_DW && p.scaled && !of_one_size(p.info) ? &p.b_common : &p.b;
     bool ok = true;
-    for (int u = pair; u < units && ok; u += pairs) {
+    for (int u = pair; u < some && ok; u += pairs) {
       const Unit w = unit_at<KIND>(p, u, live, plan);
       const int am = w.m0 + (int)rank * kHalf, bn = w.n0 + (int)rank * share_n;
       for (int kb = w.kb0; kb < w.kb1; ++kb) {
@@ -788,10 +795,21 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   tc_fence_before();
   __syncthreads();
   if (warp == 0 && lane == 0 && abort_flag) {
-    // a wait ran out: copies still in flight get a bounded time to land before the CTA retires
-    for (int s = 0; s < stages; ++s)
-      for (uint32_t i = 0; i < 4096u && !mbar_try_wait<PAIR>(smem_u32(&full_bar[s]), 0u); ++i) __nanosleep(256);
+    // a wait ran out: copies still in flight get 4 ms to land before the CTA retires
+    for (const uint64_t t0 = global_timer_ns(); global_timer_ns() - t0 < 4000000ull;) __nanosleep(1000);
     if (p.total) *p.total = __int_as_float(0x7fffffff);       // (the kernels that follow see the status)
+  }
+  if (KIND == P_DW && abort_flag && p.shares == 1 && p.first + p.piece >= p.info->live) {
+    // no kernel follows that could: what this CTA has not written of dW, and what it has
+    for (int u = pair; u < units; u += pairs) {
+      const Unit w = unit_at<KIND>(p, u, live, plan);
+      for (int i = threadIdx.x; i < kHalf * kTile; i += kLossThreads) {
+        const int v = w.m0 + (int)rank * kHalf + i / kTile, c = w.n0 + i % kTile;
+        if (v >= p.vocab || c >= p.dim) continue;
+        if (p.dw_bf16) static_cast<__nv_bfloat16*>(p.dw)[(int64_t)v * p.ld_dw + c] = __float2bfloat16_rn(__int_as_float(0x7fffffff));
+        else static_cast<float*>(p.dw)[(int64_t)v * p.ld_dw + c] = __int_as_float(0x7fffffff);
+      }
+    }
   }
   if (PAIR) cluster_sync_all();
   tc_fence_after();
@@ -1170,7 +1188,8 @@ __device__ __forceinline__ void total_by_last(LossInfo* info, int n, const doubl
   if (threadIdx.x == 0) {
     t = 0.0;
     for (int i = 0; i < 8; ++i) t += sums[i];
-    *total = (float)t;
+    // (a wait that ran out where gradients of earlier rows are formed leaves these losses right, and the call wrong)
+    *total = info->st.code != 0 ? __int_as_float(0x7fffffff) : (float)t;
   }
 }
 
@@ -1874,6 +1893,8 @@ mw_status run_product_in(ProductArgs& p, int64_t most_units, cudaStream_t s) {
   p.buffers = buffers_for(MODE, KIND, p.blocks_k);
   p.most_blocks = piece_blocks(MODE, KIND, p.piece);
   p.stages = stages_for(p.buffers, p.a_stage + terms_b(MODE) * plane_b(PAIR));
+  p.wait_ns = unmet_ms ? unmet_ms * 1000000ull : kLossWaitNs;
+  p.unmet = unmet_ms != 0 && unmet_product == (of_logits(KIND) ? 0 : (KIND == P_DH ? 1 : 2));
   static bool ready[kMaxDevices] = {};
   const int dev = current_device();
   auto kernel = loss_products_kernel<MODE, KIND, PAIR>;
@@ -2193,4 +2214,11 @@ extern "C" mw_status mw_token_loss_status(const void* workspace, void* stream) {
   MW_CUDA_OK(cudaMemcpyAsync(&host, workspace, sizeof(host), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
   MW_CUDA_OK(cudaStreamSynchronize((cudaStream_t)stream));
   return (mw_status)host.code;
+}
+
+extern "C" mw_status mw_token_loss_selftest_unmet_wait(uint32_t limit_ms, int32_t product) {
+  if (limit_ms > 1000 || product < 0 || product > 2) return MW_ERR_INVALID_ARG;
+  mw::unmet_ms = limit_ms;
+  mw::unmet_product = product;
+  return MW_OK;
 }
