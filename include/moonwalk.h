@@ -504,7 +504,7 @@ mw_status mw_token_loss_selftest_unmet_wait(uint32_t limit_ms, int32_t product);
 /* Clipping by the norm of all gradients together:
  *   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)
  * Where norm is not finite, out = g and norm says so.  Host arrays of `count`: device pointers (dense tensors;
- * out[k] may be in[k]), element counts, dtypes.  norm: float [1], device.  max_norm > 0; infinity: the norm alone
+ * out[k] may be in[k], and shares memory with no other in or out), element counts, dtypes.  norm: float [1], device.  max_norm > 0; infinity: the norm alone
  * (out may then be NULL).  scratch: 256-byte aligned device memory. */
 mw_status mw_clip_scratch_bytes(int32_t count, size_t* bytes);
 mw_status mw_clip_gradients(int32_t count, const void* const* in, void* const* out, const int64_t* sizes,

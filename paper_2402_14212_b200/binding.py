@@ -1117,9 +1117,10 @@ def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None,
 
 def clip_gradients(grads, max_norm: float, out=None, stream=None):
     """Scales the tensors together so that their common norm is at most max_norm; in place unless `out` gives a
-    tensor for each.  Dense float32 or bfloat16 tensors of any shapes on one device.  Returns the norm before, a
-    float32 tensor of no dimensions; where it is not finite the gradients stay as they are.  max_norm infinite: the
-    norm alone.  `stream` as in gated_scan."""
+    tensor for each.  Contiguous float32 or bfloat16 tensors of any shapes on one device, none of which shares memory
+    with another (a weight used twice has one gradient).  Returns the norm before, a float32 tensor of no dimensions;
+    where it is not finite the gradients stay as they are, and a step that looks at it leaves its weights alone.
+    max_norm infinite: the norm alone.  `stream` as in gated_scan."""
     import torch
     grads = list(grads)
     _need(len(grads) > 0, "clip_gradients: at least one tensor")

@@ -7,6 +7,10 @@
 // is where it begins.
 #include <math.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "mw_launch.cuh"
 
 namespace mw {
@@ -152,6 +156,30 @@ scale_kernel(const __grid_constant__ ClipGroup g, const double* __restrict__ par
   }
 }
 
+// Whether what a call writes is apart from what its other blocks read and write: a tensor that stands in the list twice would be
+// scaled twice, or half of it.
+struct Span { uintptr_t from, to; };
+bool overlaps(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
+mw_status check_apart(int count, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, bool norm_alone) {
+  std::unique_ptr<Span[]> written(new (std::nothrow) Span[count]);
+  if (!written) return MW_ERR_WORKSPACE;
+  int n = 0;
+  auto span = [&](const void* p, int k) { return Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)sizes[k] * (dtypes[k] == MW_BF16_F32ACC ? 2 : 4)}; };
+  for (int k = 0; k < count; ++k)
+    if (sizes[k] > 0 && !(norm_alone && in[k] == out[k])) written[n++] = span(out[k], k);
+  auto before = [](const Span& a, const Span& b) { return a.from < b.from; };
+  if (!std::is_sorted(&written[0], &written[0] + n, before)) std::sort(&written[0], &written[0] + n, before);
+  for (int i = 1; i < n; ++i)
+    if (overlaps(written[i - 1], written[i])) return MW_ERR_INVALID_ARG;
+  for (int k = 0; k < count && n; ++k) {
+    if (sizes[k] == 0 || in[k] == out[k]) continue;
+    const Span x = span(in[k], k);
+    const Span* next = std::lower_bound(&written[0], &written[0] + n, x, before);          // the first that starts there or later
+    if ((next < &written[0] + n && overlaps(*next, x)) || (next > &written[0] && overlaps(next[-1], x))) return MW_ERR_INVALID_ARG;
+  }
+  return MW_OK;
+}
+
 }  // namespace
 }  // namespace mw
 
@@ -172,6 +200,7 @@ extern "C" mw_status mw_clip_gradients(int32_t count, const void* const* in, voi
     if (sizes[k] < 0 || (dtypes[k] != MW_F32 && dtypes[k] != MW_BF16_F32ACC)) return MW_ERR_INVALID_ARG;
     if (sizes[k] > 0 && (!in[k] || (out && !out[k]))) return MW_ERR_INVALID_ARG;
   }
+  if (out && count > 0) MW_TRY(check_apart(count, in, out, sizes, dtypes, isinf(max_norm)));
   size_t need = 0;
   MW_TRY(mw_clip_scratch_bytes(count, &need));
   if (!scratch || ((uintptr_t)scratch & 255u) || scratch_bytes < need) return MW_ERR_WORKSPACE;
