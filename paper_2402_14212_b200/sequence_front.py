@@ -17,7 +17,7 @@ gradient steps of the per-channel weights.
 
 Tokens enter through rows of a table (embedding); a token model ends in the vocabulary's loss over the same table
 (token_loss_gradient), whose gradient takes that of the lookup on top.  clip bounds the norm of all gradients of a step
-together (clip_gradients).
+together (clip_gradients); where that is not finite there is no step.
 """
 from __future__ import annotations
 
@@ -109,13 +109,32 @@ def _flat(grads):
     return [t for g in grads.values() for t in (g if isinstance(g, list) else [g])]
 
 
-class Trainer:
+class Clipping:
+    """The bound of a step's gradients: `clip` (None: none), the last step's `norm`, how many steps were `skipped`."""
+
+    def __init__(self, clip):
+        self.clip, self.norm, self.skipped = clip, None, 0
+
+    def _clipped(self, grads):
+        """Clips them; whether they are to be applied.  A norm that is not finite bounds nothing: such a step, which the
+        host waits for, changes no weight and no momentum."""
+        if self.clip is None:
+            return True
+        self.norm = mwb.clip_gradients(grads, self.clip)
+        if math.isfinite(float(self.norm)):
+            return True
+        self.skipped += 1
+        return False
+
+
+class Trainer(Clipping):
     """The stack, a dense Moonwalk net behind it, and their updates.  With `vocab` the inputs are tokens (of negative
-    ones a row is zero); with `clip` the gradients of a step are scaled together to that norm at most."""
+    ones a row is zero); with `clip` the gradients of a step are scaled together to that norm at most, and steps whose
+    norm is not finite are skipped."""
 
     def __init__(self, width=128, blocks=2, depth=3, batch=8, time=64, lr=2e-3, seed=0, vocab=None, clip=None):
         import torch
-        self.clip, self.norm = clip, None
+        super().__init__(clip)
         self.table = None if vocab is None else _table(vocab, width, seed)
         self.front = SequenceFront(width, blocks, seed)
         problem = S.deep_mlp(seed=seed, depth=depth, n=width, batch=batch * time, reseed_every=2)
@@ -149,8 +168,8 @@ class Trainer:
 
     def step(self, x, target):
         dW, front, _ = self.gradients(x, target)
-        if self.clip is not None:
-            self.norm = mwb.clip_gradients(list(dW) + _flat(front), self.clip)
+        if not self._clipped(list(dW) + _flat(front)):
+            return self.loss
         # orthogonalised updates move every direction of a weight alike, so the net's weights stay near a
         # multiple of an orthogonal matrix, where its inverse converges
         self.orth.step(self.params, dW, self.momentum, self.orth_ws, lr=self.lr)
@@ -172,7 +191,7 @@ class Trainer:
         return code
 
 
-class TokenTrainer:
+class TokenTrainer(Clipping):
     """A token model of the stack alone: rows of a table, the blocks, a last norm, the vocabulary's loss by the same
     table; each position says the token after it.  Negative tokens are padding: they are no input and no target."""
 
@@ -181,7 +200,8 @@ class TokenTrainer:
         self.front = SequenceFront(width, blocks, seed)
         self.table = _table(vocab, width, seed)
         self.w_out = torch.ones(width, device="cuda")
-        self.lr, self.clip, self.norm = lr, clip, None
+        super().__init__(clip)
+        self.lr = lr
         self.orth_proj = mwb.Orth(3 * width, width, blocks, "f32")
         self.orth_proj_ws = self.orth_proj.alloc_workspace()
         self.proj_momentum = [torch.zeros_like(w) for w in self.front.proj]
@@ -210,10 +230,10 @@ class TokenTrainer:
         return r, grads
 
     def step(self, tokens):
-        """One update; returns the mean loss of the positions that have a target."""
+        """One update, unless the gradients' norm is not finite; returns the mean loss of the positions that have a target."""
         r, grads = self.gradients(tokens)
-        if self.clip is not None:
-            self.norm = mwb.clip_gradients(_flat(grads), self.clip)
+        if not self._clipped(_flat(grads)):
+            return r.total
         f = self.front
         self.orth_proj.step(f.proj, grads["proj"], self.proj_momentum, self.orth_proj_ws, lr=4 * self.lr)
         for name in ("w_post", "scale", "w_pre"):
