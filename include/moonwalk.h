@@ -484,9 +484,9 @@ typedef struct {
 } mw_token_loss_desc;
 mw_status mw_token_loss_workspace_bytes(const mw_token_loss_desc* desc, int32_t gradient, size_t* bytes);
 /* loss: float [rows]; total: float [1] or NULL; row_weight: float [rows] or NULL.  workspace: 256-byte aligned
- * device memory, which no other call in flight uses.  A bf16 weight starts on a 16-byte boundary where it is read in
- * place: where ld_weight is a multiple of 8, for the loss alone, and for gradients of up to 128 rows where dim is a
- * multiple of 64 and eight times the rows or more, and the weight has 12 * 2^20 numbers or more. */
+ * device memory, which no other call in flight uses.  A bf16 weight whose ld_weight is a multiple of 8 starts on a 16-byte
+ * boundary here, where it is read in place; the gradient takes any (of up to 128 rows an aligned one of 12 * 2^20 numbers
+ * and more is read in place there, too: dim a multiple of 64, and eight times the rows or more). */
 mw_status mw_token_loss_forward(const mw_token_loss_desc* desc, const void* h, const void* weight,
                                 const void* targets, const float* row_weight, float* loss, float* total,
                                 void* workspace, size_t workspace_bytes, void* stream);

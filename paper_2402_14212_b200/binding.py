@@ -1094,7 +1094,7 @@ def token_loss(h, weight, targets, scale: float = 1.0, row_weight=None, stream=N
     import torch
     if stream is not None:
         return _on_stream(stream, h, token_loss, h, weight, targets, scale, row_weight, None, workspace)
-    if weight.data_ptr() & 15:         # (read in place, by copies of 16 bytes)
+    if weight.dtype == torch.bfloat16 and weight.data_ptr() & 15:         # (read in place, by copies of 16 bytes)
         weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(False, h, weight, targets, scale, row_weight, 0, None, None, None, (False, False), workspace)
 
@@ -1109,7 +1109,8 @@ def token_loss_gradient(h, weight, targets, scale: float = 1.0, row_weight=None,
     if stream is not None:
         return _on_stream(stream, h, token_loss_gradient, h, weight, targets, scale, row_weight, dh, dweight, grad_dtype,
                           want, piece_rows, None, workspace)
-    if weight.data_ptr() & 15 and targets.numel() <= 128:         # (of few rows read in place, by copies of 16 bytes)
+    # (of few rows read in place, by copies of 16 bytes)
+    if weight.dtype == torch.bfloat16 and weight.data_ptr() & 15 and targets.numel() <= 128:
         weight = weight.clone(memory_format=torch.contiguous_format)
     return _token_loss(True, h, weight, targets, scale, row_weight, piece_rows, grad_dtype, dh, dweight,
                        (bool(want[0]), bool(want[1])), workspace)

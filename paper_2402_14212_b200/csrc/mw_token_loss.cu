@@ -1785,7 +1785,8 @@ int logits_tile(int vocab, int workers) {
   return n < 64 ? 64 : n;
 }
 
-size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossWs* l) {
+// aligned: the weight starts on a 16-byte boundary
+size_t loss_layout(const mw_token_loss_desc* d, bool gradient, bool aligned, char* base, LossWs* l) {
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* p = base + at;
@@ -1795,7 +1796,7 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, char* base, LossW
   const int terms = d->dtype == MW_F32 ? 2 : 1;
   const size_t n = (size_t)d->rows, v = (size_t)d->vocab, dim = (size_t)d->dim;
   const int64_t ld_w = d->ld_weight ? d->ld_weight : d->dim;
-  l->few = gradient && terms == 1 && d->rows > 0 && d->rows <= kFewRows && 8 * (int64_t)d->rows <= d->dim &&
+  l->few = gradient && aligned && terms == 1 && d->rows > 0 && d->rows <= kFewRows && 8 * (int64_t)d->rows <= d->dim &&
            (int64_t)d->vocab * d->dim >= kFewNumbers && ld_w % 8 == 0 && d->dim % kBK == 0;
   l->in_place = l->few || (!gradient && terms == 1 && ld_w % 8 == 0);
   l->thin = terms == 2 && d->rows > 0 && d->rows <= kThinRows;
@@ -1988,7 +1989,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
   a.ld_dw = d->ld_dweight ? d->ld_dweight : d->dim;
   a.scale = (float)d->scale;
   LossWs l;
-  loss_layout(d, gradient, ws, &l);
+  loss_layout(d, gradient, ((uintptr_t)w & 15) == 0, ws, &l);
   // bf16 operands of the loss alone, and of few rows, are taken as they are
   const bool scaled = TERMS == 2 || (gradient && !l.few);
   const int mode = TERMS == 2 ? M_TWO : (l.few ? M_FEW : M_ONE);
@@ -2167,10 +2168,11 @@ mw_status loss_call(const mw_token_loss_desc* d, const void* h, const void* w, c
   if (!w || (d->rows > 0 && (!h || !targets || !loss))) return MW_ERR_INVALID_ARG;
   const int64_t ld_h = d->ld_h ? d->ld_h : d->dim, ld_dh = d->ld_dh ? d->ld_dh : d->dim;
   if (dh == h && dh && ld_h != ld_dh) return MW_ERR_INVALID_ARG;
-  // rows that the copy engine reads start on 16-byte boundaries
+  // rows that the copy engine reads start on 16-byte boundaries (the gradient copies a weight that does not)
+  const bool aligned = ((uintptr_t)w & 15) == 0;
   LossWs l;
-  const size_t need = loss_layout(d, gradient, nullptr, &l);
-  if (l.in_place && ((uintptr_t)w & 15)) return MW_ERR_INVALID_ARG;
+  const size_t need = loss_layout(d, gradient, aligned, nullptr, &l);
+  if (l.in_place && !aligned) return MW_ERR_INVALID_ARG;
   if (!ws || ((uintptr_t)ws & 255u) || bytes < need) return MW_ERR_WORKSPACE;
   cudaStream_t s = (cudaStream_t)stream;
   char* b = static_cast<char*>(ws);
@@ -2191,7 +2193,7 @@ extern "C" mw_status mw_token_loss_workspace_bytes(const mw_token_loss_desc* des
   if (!bytes || (gradient != 0 && gradient != 1)) return MW_ERR_INVALID_ARG;
   MW_TRY(check_loss(desc));
   LossWs l;
-  *bytes = loss_layout(desc, gradient != 0, nullptr, &l);
+  *bytes = std::max(loss_layout(desc, gradient != 0, true, nullptr, &l), loss_layout(desc, gradient != 0, false, nullptr, &l));
   return MW_OK;
 }
 
