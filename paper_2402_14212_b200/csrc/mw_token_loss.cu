@@ -1772,6 +1772,7 @@ struct LossWs {
   unsigned short *h, *h_common, *w, *e;
   float *slab, *shares, *dw;
   int blocks, piece, padded, vpadded, sum_blocks, staged_rows;
+  int dh_room, share_blocks;        // blocks of 256 x 256 sums: that dh's plan may use, and of all
   bool few;               // M_FEW
   bool thin;              // M_THIN
   bool in_place;          // W is read where it lies
@@ -1784,6 +1785,16 @@ int logits_tile(int vocab, int workers) {
   const int n = (int)align_up((size_t)ceil_div(vocab, waves * workers), 32);
   return n < 64 ? 64 : n;
 }
+
+// K shares of dW's tiles where these are for less than half of the pairs, of eight blocks at least
+int dw_shares(int tiles, int blocks_k, int pairs) {
+  return 2 * tiles <= pairs && blocks_k >= 16 ? std::min(pairs / tiles, blocks_k / 8) : 1;
+}
+// Slices of the vocabulary, for `blocks` blocks a multiprocessor, of very few rows: rows of each
+int thin_slice(int vocab, int tiles, int blocks) {
+  return ceil_div(vocab, std::max(1, std::min(blocks * sm_count() / tiles, ceil_div(vocab, 16))));
+}
+constexpr int kThinBlocks = 4;
 
 // aligned: the weight starts on a 16-byte boundary
 size_t loss_layout(const mw_token_loss_desc* d, bool gradient, bool aligned, char* base, LossWs* l) {
@@ -1832,7 +1843,21 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, bool aligned, cha
   l->w = (unsigned short*)take(l->in_place || l->thin ? 0 : v * l->padded * 2 * terms);
   l->e = (unsigned short*)take(gradient ? (size_t)l->piece * l->vpadded * 2 * held : 0);
   l->slab = (float*)take(gradient ? (size_t)l->piece * l->padded * 4 : 0);
-  l->shares = (float*)take(gradient ? (size_t)share_blocks(sm_count() / 2) * kTile * kTile * 4 : 0);
+  l->dh_room = l->share_blocks = 0;
+  if (l->thin) {
+    const int tiles = ceil_div(d->dim, 1024), slices = ceil_div(d->vocab, thin_slice(d->vocab, tiles, kThinBlocks));
+    l->share_blocks = ceil_div((int64_t)slices * tiles * 1024 * (d->rows <= 4 ? 4 : kThinRows), kTile * kTile);
+  } else if (gradient) {
+    // the most that the plan of dh may want: tiles beside the whole waves, times shares of eight blocks of K and more
+    const int pairs = sm_count() / 2, workers = d->rows <= kHalf ? sm_count() : pairs, across = ceil_div(d->dim, kTile);
+    const int64_t rest = std::min((int64_t)ceil_div(l->piece, kTile) * across, (int64_t)workers - 1);
+    const int most_shares = std::min(32, std::max(1, (l->vpadded / kBK - 1) / 7));
+    l->dh_room = (int)std::min((int64_t)share_blocks(pairs), rest * most_shares);
+    const int tiles = ceil_div(d->vocab, kTile) * across, shares = dw_shares(tiles, ceil_div(l->piece, kBK), pairs);
+    const int held = (int)std::min((int64_t)l->dh_room, rest * (most_shares - 1));          // (a tile's first share has its own place)
+    l->share_blocks = std::max(std::max(1, held), shares > 1 ? tiles * shares : 0);
+  }
+  l->shares = (float*)take(gradient ? (size_t)l->share_blocks * kTile * kTile * 4 : 0);
   l->dw = (float*)take(gradient && l->piece < d->rows ? v * l->padded * 4 : 0);
   return at;
 }
@@ -1960,16 +1985,15 @@ mw_status thin_run_of(const LossArgs& a, const LossWs& l, const float* h, const 
                       loss, l.part, total, l.e, l.vpadded, slices));
   // slices of the vocabulary for as many blocks as the device holds a few times over
   const int tiles = ceil_div(a.dim, 1024);
-  auto rows_of = [&](int blocks) { return ceil_div(a.vocab, std::max(1, std::min(blocks * sm_count() / tiles, ceil_div(a.vocab, 16)))); };
   if (dw) {
-    const int per = rows_of(4), n = ceil_div(a.vocab, per) * tiles;
+    const int per = thin_slice(a.vocab, tiles, kThinBlocks), n = ceil_div(a.vocab, per) * tiles;
     auto go = [&](auto kernel, auto* to) { return launch_after(kernel, (unsigned)n, 256, 0, s, h, a.ld_h, l.row, a.vocab, a.dim, a.scale, l.info, (const float*)l.e,
                                                                l.vpadded, to, a.ld_dw, tiles, per); };
     if (dw_bf16) MW_TRY(go(wide(dw, a.ld_dw, 2) ? thin_dw_kernel<__nv_bfloat16, R, true> : thin_dw_kernel<__nv_bfloat16, R, false>, (__nv_bfloat16*)dw));
     else MW_TRY(go(wide(dw, a.ld_dw, 4) ? thin_dw_kernel<float, R, true> : thin_dw_kernel<float, R, false>, (float*)dw));
   }
   if (dh) {
-    const int per = rows_of(4), n = ceil_div(a.vocab, per);          // (their sums take 4 * 148 blocks of 8 x 1024 at the most)
+    const int per = thin_slice(a.vocab, tiles, kThinBlocks), n = ceil_div(a.vocab, per);
     MW_TRY(launch_after(wide_w ? thin_dh_kernel<R, true> : thin_dh_kernel<R, false>, (unsigned)(n * tiles), 256, 0, s, w, a.ld_w, a.vocab, a.dim, l.info,
                         (const float*)l.e, l.vpadded, l.shares, tiles, per));
     MW_TRY(launch_after(thin_dh_rows_kernel, dim3((unsigned)ceil_div(a.dim, 32), (unsigned)a.rows), 256, 0, s, a, l.shares, tiles, R, n, l.row, l.info, dh));
@@ -2054,7 +2078,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
     const bool single = a.rows <= kHalf;
     const int pairs = sm_count() / 2, tile_m = single ? kHalf : kTile;
     p.workers = single ? sm_count() : pairs;
-    p.share_room = share_blocks(pairs);
+    p.share_room = l.dh_room;
     p.shares = 1;
     p.tile_n = kTile;
     ProductArgs logits = p, by_h = p, by_w = p;
@@ -2088,7 +2112,7 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       MW_TRY(l.few ? group_map(&by_h.b, w, a.dim, a.vocab, a.ld_w * 2, 128, 128, 1, kBK, share_b / 64)
                    : group_map(&by_h.b, l.w, l.padded, a.vocab, hw_bytes, 128, hw_bytes * a.vocab, TERMS, kBK, share_b / 64));
       MW_TRY(out_map(&by_h.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.slab, l.padded, l.piece, l.padded));
-      MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)p.share_room * kTile, kTile));
+      MW_TRY(out_map(&by_h.acc, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, l.shares, kTile, (int64_t)l.share_blocks * kTile, kTile));
       // dW: K across the rows of both
       by_w.tiles_m = ceil_div(a.vocab, kTile);
       by_w.tiles_n = ceil_div(a.dim, kTile);
@@ -2097,13 +2121,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       MW_TRY(group_map(&by_w.a, l.e, l.vpadded, l.piece, row_bytes, group_bytes, 128, held, kBK, 2));
       MW_TRY(group_map(&by_w.b, l.h, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
       if (scaled) MW_TRY(group_map(&by_w.b_common, l.h_common, l.padded, l.staged_rows, hw_bytes, 128, hw_bytes * l.staged_rows, TERMS, kBK, 2));
-      // tiles for less than half of the pairs: each in shares of K, of eight blocks at least
-      const int tiles = by_w.tiles_m * by_w.tiles_n;
-      if (2 * tiles <= pairs && by_w.blocks_k >= 16) {
-        by_w.shares = pairs / tiles < by_w.blocks_k / 8 ? pairs / tiles : by_w.blocks_k / 8;
-        by_w.out = by_h.acc;
-        by_w.acc = by_h.acc;
-      }
+      by_w.shares = dw_shares(by_w.tiles_m * by_w.tiles_n, by_w.blocks_k, pairs);
+      if (by_w.shares > 1) by_w.out = by_w.acc = by_h.acc;
       by_w.dw = dw; by_w.ld_dw = a.ld_dw; by_w.dw_bf16 = dw_bf16;
       by_w.dw_engine = by_w.shares == 1 && ((uintptr_t)dw & 15) == 0 && (a.ld_dw * dw_size) % 16 == 0;
       if (by_w.dw_engine && dw)

@@ -51,3 +51,17 @@ def test_calls_in_kept_memory(rows, dtype):
     side.wait_stream(torch.cuda.current_stream())
     got = mwb.token_loss_gradient(h, w, t, piece_rows=256, stream=side, workspace=room)
     assert mwb.token_loss_status(room, stream=side) == 0 and all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_a_small_gradient_takes_little_memory():
+    """Operands, exponentials and sums of 10 rows of 50x16 are a few hundred KB; a large call has room for shares."""
+    import ctypes as C
+
+    def need(rows, vocab, dim, dtype=2):
+        n = C.c_size_t()
+        assert mwb.lib().mw_token_loss_workspace_bytes(mwb.TokenLossDesc(rows, vocab, dim, dtype, 0, 8, 0, 0, 0, 0, 0, 1.0), 1, n) == 0
+        return n.value
+
+    assert need(10, 50, 16) < 1 << 20 and need(10, 50, 16, 1) < 1 << 20
+    assert need(4, 50, 16, 1) < 1 << 20 and need(300, 1000, 64) < 16 << 20
+    assert need(4096, 32768, 2048) > 4096 * 32768 * 2 + (4096 + 32768) * 2048 * 2 + 54 * 3 * 65536 * 4
