@@ -447,7 +447,7 @@ typedef struct {
   int32_t index_bytes;        /* tokens are int32 (4) or int64 (8) */
   int32_t reserved;           /* 0 */
   int64_t ld_table, ld_out, ld_dtable; /* elements between rows (0 = dim); ld_out: of out and of dout */
-  double scale;
+  double scale;               /* finite as a float */
 } mw_embedding_desc;
 mw_status mw_embedding_forward(const mw_embedding_desc* desc, const void* tokens, const void* table, void* out,
                                void* stream);
@@ -480,7 +480,7 @@ typedef struct {
   int32_t index_bytes;        /* targets are int32 (4) or int64 (8) */
   int32_t piece_rows;         /* rows of a piece of the gradient; 0 = as many as take 1 GiB, 1024 at least */
   int64_t ld_h, ld_weight, ld_dh, ld_dweight; /* elements between rows (0 = dim) */
-  double scale;
+  double scale;               /* finite as a float */
 } mw_token_loss_desc;
 mw_status mw_token_loss_workspace_bytes(const mw_token_loss_desc* desc, int32_t gradient, size_t* bytes);
 /* loss: float [rows]; total: float [1] or NULL; row_weight: float [rows] or NULL.  workspace: 256-byte aligned

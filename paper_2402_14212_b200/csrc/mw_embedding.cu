@@ -606,7 +606,7 @@ size_t embed_layout(const mw_embedding_desc* d, char* base, EmbedScratch* l) {
 }
 
 mw_status check_embed(const mw_embedding_desc* d) {
-  if (!d || d->tokens < 0 || d->vocab < 1 || d->dim < 1 || d->reserved != 0 || !isfinite(d->scale)) return MW_ERR_INVALID_ARG;
+  if (!d || d->tokens < 0 || d->vocab < 1 || d->dim < 1 || d->reserved != 0 || !isfinite((float)d->scale)) return MW_ERR_INVALID_ARG;
   if (d->index_bytes != 4 && d->index_bytes != 8) return MW_ERR_INVALID_ARG;
   if (d->tokens > (1 << 30) || d->dtype == MW_F64 || d->vocab == INT32_MAX) return MW_ERR_UNSUPPORTED;
   if (d->dtype != MW_F32 && d->dtype != MW_BF16_F32ACC) return MW_ERR_INVALID_ARG;

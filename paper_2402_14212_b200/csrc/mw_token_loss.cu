@@ -1863,7 +1863,7 @@ size_t loss_layout(const mw_token_loss_desc* d, bool gradient, bool aligned, cha
 }
 
 mw_status check_loss(const mw_token_loss_desc* d) {
-  if (!d || d->rows < 0 || d->vocab < 1 || d->dim < 1 || d->piece_rows < 0 || !isfinite(d->scale)) return MW_ERR_INVALID_ARG;
+  if (!d || d->rows < 0 || d->vocab < 1 || d->dim < 1 || d->piece_rows < 0 || !isfinite((float)d->scale)) return MW_ERR_INVALID_ARG;
   if (d->index_bytes != 4 && d->index_bytes != 8) return MW_ERR_INVALID_ARG;
   if (d->rows > (1 << 24) || d->vocab > (1 << 24) || d->dim > (1 << 16) || d->dtype == MW_F64) return MW_ERR_UNSUPPORTED;
   if (d->dtype != MW_F32 && d->dtype != MW_BF16_F32ACC) return MW_ERR_INVALID_ARG;
