@@ -490,7 +490,8 @@ mw_status mw_token_loss_workspace_bytes(const mw_token_loss_desc* desc, int32_t 
 mw_status mw_token_loss_forward(const mw_token_loss_desc* desc, const void* h, const void* weight,
                                 const void* targets, const float* row_weight, float* loss, float* total,
                                 void* workspace, size_t workspace_bytes, void* stream);
-/* dh or dweight may be NULL (not wanted); dh may be h itself where ld_dh = ld_h. */
+/* dh or dweight may be NULL (not wanted); dh may be h itself where ld_dh = ld_h.  Other results share no memory with
+ * one another or with what is read. */
 mw_status mw_token_loss_gradient(const mw_token_loss_desc* desc, const void* h, const void* weight,
                                  const void* targets, const float* row_weight, float* loss, float* total, void* dh,
                                  void* dweight, void* workspace, size_t workspace_bytes, void* stream);

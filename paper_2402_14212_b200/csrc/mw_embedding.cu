@@ -758,7 +758,7 @@ extern "C" mw_status mw_embedding_forward(const mw_embedding_desc* desc, const v
   using namespace mw;
   MW_TRY(check_embed(desc));
   if (desc->tokens == 0) return MW_OK;
-  if (!tokens || !table || !out) return MW_ERR_INVALID_ARG;
+  if (!tokens || !table || !out || out == table) return MW_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   if (desc->dtype == MW_F32)
     return desc->index_bytes == 4 ? lookup<float, int32_t>(desc, tokens, table, out, s)
@@ -783,6 +783,7 @@ extern "C" mw_status mw_embedding_backward(const mw_embedding_desc* desc, const 
   if ((accumulate != 0 && accumulate != 1) || !dtable || (desc->tokens > 0 && (!tokens || !dout))) return MW_ERR_INVALID_ARG;
   EmbedScratch l;
   if (!scratch || ((uintptr_t)scratch & 255u) || scratch_bytes < embed_layout(desc, nullptr, &l)) return MW_ERR_WORKSPACE;
+  if (dtable == dout) return MW_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   char* ws = static_cast<char*>(scratch);
   const bool add = accumulate != 0;

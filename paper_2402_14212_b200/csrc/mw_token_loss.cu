@@ -2193,6 +2193,8 @@ mw_status loss_call(const mw_token_loss_desc* d, const void* h, const void* w, c
   const size_t need = loss_layout(d, gradient, aligned, nullptr, &l);
   if (l.in_place && !aligned) return MW_ERR_INVALID_ARG;
   if (!ws || ((uintptr_t)ws & 255u) || bytes < need) return MW_ERR_WORKSPACE;
+  // (dh is formed when h has been read, and either gradient may come first)
+  if ((dw && (dw == w || dw == h || dw == dh)) || (dh && dh == w)) return MW_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   char* b = static_cast<char*>(ws);
   using bf = __nv_bfloat16;
