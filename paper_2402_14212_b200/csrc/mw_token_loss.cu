@@ -129,12 +129,11 @@ __device__ __forceinline__ float scaled_by(float v, int e) {
   e = e < -250 ? -250 : (e > 250 ? 250 : e);
   return v * power_of_two(e / 2) * power_of_two(e - e / 2);
 }
-// the power of two that brings numbers of at most this size to 2^13 .. 2^14
+// the power of two that brings numbers of at most this size to 2^13 .. 2^14 (the smallest, 2^-113 and less, below that)
 __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   const int e = (int)(max_bits >> 23) - 127;         // 2^e <= max < 2^(e + 1)
   if (max_bits == 0 || e > 127) return 0;
-  const int x = 13 - e;
-  return x < -100 ? -100 : (x > 100 ? 100 : x);
+  return 13 - e > 126 ? 126 : 13 - e;
 }
 // ... of a row of h, or of W whole, whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up to 2^7,
 // 2^-9), which is written while it is looked at; where the largest lies elsewhere it is written again.  What is lost then

@@ -120,3 +120,16 @@ def test_captured_calls_of_even_and_uneven_rows():
         graph.replay()
         got = [x.clone() for x in held]
         assert all(torch.equal(a, b) for a, b in zip(got, call()))
+
+
+@pytest.mark.parametrize("N,dtype", [(8, F32), (9, F32), (300, F32), (9, BF16), (300, BF16)])
+@pytest.mark.parametrize("size", [-118, -105, 105, 118])
+def test_operands_near_the_ends_of_the_range(size, N, dtype):
+    h, W, t = make(N, 700, 128, dtype, seed=N, lean=4.0)
+    h, W = h * 2.0 ** size, W * 2.0 ** -size
+    want = reference(h, W, t)
+    check(mwb.token_loss(h, W, t), want, ("loss", "total"))
+    check(mwb.token_loss_gradient(h, W, t), want, ALL)
+    h[3] *= 2.0 ** (-size // 2)
+    want = meeting(reference(h, W, t), h, W, t, torch.full((N,), 1 / N, device="cuda"))
+    check(mwb.token_loss_gradient(h, W, t), want, ALL)
