@@ -1,10 +1,10 @@
 // Clipping by the norm of all gradients together (mw_clip_gradients):
 //   norm = sqrt(sum g^2),   out = g min(1, max_norm / norm)
-// HBM bounds it: every element is read for the norm, read again and written for the product.  Tensors are cut into
-// chunks that the blocks take in turn, so one launch serves many tensors of any sizes; squares are summed in 64 bits, which
-// costs nothing (64 of 1024x1024 fp32, 268 MB: squares 46 to 55 us with sums in 64 bits and in 32).  Measured, the same case:
-// 136 us for both launches, 5.9 TB/s of the 805 MB that pass; of the second read L2 holds what the first ended with, which
-// is where it begins.
+// HBM bounds it: every element is read for the norm, read again and written for the product. Tensors are cut into
+// chunks that the blocks take in turn, so one launch serves many tensors of any sizes; squares are summed in 64 bits,
+// which costs nothing (64 of 1024x1024 fp32, 268 MB: squares 46 to 55 us with sums in 64 bits and in 32). Measured, the
+// same case: 136 us for both launches, 5.9 TB/s of the 805 MB that pass; of the second read L2 holds what the first
+// ended with, which is where it begins.
 #include <math.h>
 
 #include <algorithm>
@@ -156,8 +156,8 @@ scale_kernel(const __grid_constant__ ClipGroup g, const double* __restrict__ par
   }
 }
 
-// Whether what a call writes is apart from what its other blocks read and write: a tensor that stands in the list twice would be
-// scaled twice, or half of it.
+// Whether what a call writes is apart from what its other blocks read and write: a tensor that stands in the list twice
+// would be scaled twice, or half of it.
 struct Span { uintptr_t from, to; };
 bool overlaps(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
 mw_status check_apart(int count, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, bool norm_alone) {

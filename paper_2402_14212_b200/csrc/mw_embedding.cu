@@ -1,15 +1,16 @@
 // Embedding lookup with scaling, and its gradient (mw_embedding_*):
 //   out_i = s E[t_i],   dE_v = s sum_{t_i = v} dout_i
-// Both directions move rows and compute next to nothing: HBM bounds them (lookup 2 N rows, gradient N rows read
-// and V rows written).  Measured, bf16: lookup of 16384 in 32768x2048 20 us (6.7 TB/s, tokens met twice included), the
-// table's gradient 52 us (201 MB: 3.9 TB/s; zeros and sort 23, sums 22, joins 8, one after another), both of 5003 in
-// 10007x515 fp32 32 us (rows off 16-byte boundaries, half the tokens the same: four launches of 7 to 9 us).  The gradient sorts (token, position) by a stable radix sort, so that a token's positions
-// stand in a run, in order; runs are summed in float by warps that take 32 entries of the sorted list each,
-// whatever the runs' lengths, and what a run leaves in several warps' shares is joined in order afterwards.
+// Both directions move rows and compute next to nothing: HBM bounds them (lookup 2 N rows, gradient N rows read and V
+// rows written). Measured, bf16: lookup of 16384 in 32768x2048 20 us (6.7 TB/s, tokens met twice included), the table's
+// gradient 52 us (201 MB: 3.9 TB/s; zeros and sort 23, sums 22, joins 8, one after another), both of 5003 in 10007x515
+// fp32 32 us (rows off 16-byte boundaries, half the tokens the same: four launches of 7 to 9 us). The gradient sorts
+// (token, position) by a stable radix sort, so that a token's positions stand in a run, in order; runs are summed in
+// float by warps that take 32 entries of the sorted list each, whatever the runs' lengths, and what a run leaves in
+// several warps' shares is joined in order afterwards.
 //
 // Up to 65536 tokens are sorted by one cluster of eight blocks, in their shared memory, while the other blocks of the
-// same launch fill the table's gradient with zeros: the sort (9 us) hides behind that.  More go through
-// three launches a digit.  (By those launches, zeros first, 16384 tokens took 49 us before the first sum.)
+// same launch fill the table's gradient with zeros: the sort (9 us) hides behind that. More go through three launches a
+// digit. (By those launches, zeros first, 16384 tokens took 49 us before the first sum.)
 #include "mw_cluster.cuh"
 #include "mw_launch.cuh"
 
@@ -443,10 +444,10 @@ __device__ __forceinline__ void write_sum(G* at, float (&v)[VEC], float scale) {
   }
 }
 
-// A warp sums one piece of the sorted list over 32 VEC MULT columns, MULT accesses a lane and row, eight rows under way at a
-// time.  A run that lies
-// whole in the piece goes to its row; what a piece holds of a run that came from the piece before goes to its
-// first partial sum, of one that starts here and goes on to its second, and the piece is listed for the join.
+// A warp sums one piece of the sorted list over 32 VEC MULT columns, MULT accesses a lane and row, eight rows under way
+// at a time. A run that lies whole in the piece goes to its row; what a piece holds of a run that came from the piece
+// before goes to its first partial sum, of one that starts here and goes on to its second, and the piece is listed for
+// the join.
 template <typename T, typename G, int VEC, int MULT, bool ADD, bool GWIDE>
 __global__ void __launch_bounds__(256)
 run_sums_kernel(EmbedArgs a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,

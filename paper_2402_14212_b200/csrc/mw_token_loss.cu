@@ -1,29 +1,33 @@
 // Softmax cross entropy over a vocabulary, and its gradient (mw_token_loss_*):
 //   z = s h W^T,  loss_i = log sum_j exp z_ij - z_{i,t_i},  dz_ij = g_i (p_ij - [j = t_i]),  dh = s dz W,  dW = s dz^T h
 //
-// Rows that have a target are put together first, so that the others cost nothing and nothing of them is read.
-// The products run on the tensor cores (CTA pairs, 256 x 256 tiles, one persistent launch a product) and bound the time:
-// 2 N V D flops for the loss, three times that with both gradients.  Measured (1374 TFLOP/s is what a library product of
-// 8192^3 bf16 reaches under the power cap, 1658 in a burst): loss of 8192 rows of 32768x2048 bf16 0.80 ms,
-// 1.37 PFLOP/s, where the library's product of the logits alone takes 0.83 ms; with both gradients 2.8 ms, 1.15 PFLOP/s;
-// 3700 rows of 131072x4096 10.4 ms, 1.13 PFLOP/s; 2048 rows of 32768x1024 fp32 1.13 ms, 1.09 PFLOP/s of the three products a
-// product.  The tensor pipe is busy for 86 to 93% of the cycles.
+// Rows that have a target are put together first, so that the others cost nothing and nothing of them is read. The
+// products run on the tensor cores (CTA pairs, 256 x 256 tiles, one persistent launch a product) and bound the time: 2
+// N V D flops for the loss, three times that with both gradients. Measured (1374 TFLOP/s is what a library product of
+// 8192^3 bf16 reaches under the power cap, 1658 in a burst): loss of 8192 rows of 32768x2048 bf16 0.80 ms, 1.37
+// PFLOP/s, where the library's product of the logits alone takes 0.83 ms; with both gradients 2.8 ms, 1.15 PFLOP/s;
+// 3700 rows of 131072x4096 10.4 ms, 1.13 PFLOP/s; 2048 rows of 32768x1024 fp32 1.13 ms, 1.09 PFLOP/s of the three
+// products a product. The tensor pipe is busy for 86 to 93% of the cycles.
 //
-// Loss alone: a tile's epilogue leaves, for each row and 128 columns, a power of two k and the sum of 2^(z' - k)
-// (z' = z log2 e) of all logits but the target's; a last kernel joins them.  Nothing else of the logits is written.  Up to
-// 256 rows of bf16 are read as they lie, without being put together: two launches, 34 us for 16 rows of 32768x2048 (the
-// vocabulary's way through memory is 20 us).  Up to 8 rows of fp32 stay off the tensor cores ("very few rows" below).
+// Loss alone: a tile's epilogue leaves, for each row and 128 columns, a power of two k and the sum of 2^(z' - k) (z' =
+// z log2 e) of all logits but the target's; a last kernel joins them. Nothing else of the logits is written. Up to 256
+// rows of bf16 are read as they lie, without being put together: two launches, 34 us for 16 rows of 32768x2048 (the
+// vocabulary's way through memory is 20 us). Up to 8 rows of fp32 stay off the tensor cores ("very few rows" below).
 //
-// Gradient: the logits are not computed twice.  A piece of rows at a time, the epilogue also writes 2^(z' - k) in
-// half precision (float for float operands); once the row's sum is known those become dz in their place, by
-// a factor per 128 columns, and two products take them in.  That costs 4 bytes of traffic an element (0.175 ms of the
-// 2.8 above), less than the 2 D flops of computing it again (0.75 ms) from D of about 400 up.
+// Gradient: the logits are not computed twice. A piece of rows at a time, the epilogue also writes 2^(z' - k) in half
+// precision (float for float operands); once the row's sum is known those become dz in their place, by a factor per 128
+// columns, and two products take them in. That costs 4 bytes of traffic an element (0.175 ms of the 2.8 above), less
+// than the 2 D flops of computing it again (0.75 ms) from D of about 400 up.
 //
-// Numbers.  bf16 operands are taken as half-precision numbers times a power of two (one a row of h, one for W): their 8 bits
-// fit, and dz keeps 11 bits where bf16 would leave 8 (dh and dW of bf16 are as far from 64 bits as the last rounding leaves
-// any result: 1.7e-3).  Float operands are split in two such terms (22 bits), three products of four.  Sums are float; the
-// tensor core cuts its accumulator off at every step, so a sum goes to registers, rounded to nearest, a piece of K at a
-// time.  The loss is log1p of the other terms' sum over the target's, so that rows sure of their target keep its digits.
+// Numbers. bf16 operands are taken as half-precision numbers times a power of two (one a row of h, one for W): their 8
+// bits fit, and dz keeps 11 bits where bf16 would leave 8 (dh and dW of bf16 are as far from 64 bits as the last
+// rounding leaves any result: 1.7e-3). Float operands are split in two such terms (22 bits), three products of four.
+// Sums are float; the tensor core cuts its accumulator off at every step, so a sum goes to registers, rounded to
+// nearest, a piece of K at a time. The loss is log1p of the other terms' sum over the target's, so that rows sure of
+// their target keep its digits. Rows do not share their powers of two: a large row of h, or a heavy or infinite weight
+// among the rows', takes no digits from the others' losses and dh (where dW's sums run over such rows, h goes into them
+// as an operand of its own). An epilogue's lane has a row and takes its power out: 3% of a call whose tiles are one K
+// block long (16384 rows of 5000x64, 285 and 294 us), nothing of 2048 columns.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -37,9 +41,9 @@ namespace mw {
 namespace {
 
 constexpr int kIndexRows = 1024;          // rows of one block that looks for targets
-// The power of two of a block of logits whose largest is m (in powers of two): what its exponentials are relative to.  Of
-// nothing but -inf it is small, so that the empty block sets no row's scale, and differences to any power are finite; beside
-// an infinity or a NaN alone the values stay as they are.
+// The power of two of a block of logits whose largest is m (in powers of two): what its exponentials are relative to.
+// Of nothing but -inf it is small, so that the empty block sets no row's scale, and differences to any power are
+// finite; beside an infinity or a NaN alone the values stay as they are.
 constexpr float kNoPower = -3e38f;
 __device__ __forceinline__ float power_of(float m) { return m == -INFINITY ? kNoPower : (m < INFINITY ? ceilf(m) : 0.f); }
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
@@ -61,14 +65,14 @@ constexpr uint64_t kLossWaitNs = 2000000000ull;
 thread_local uint32_t unmet_ms = 0;
 thread_local int unmet_product = 0;
 enum { P_SUMS = 0, P_EXP, P_DH, P_DW };
-// How operands are held.  M_ONE: one term (bf16 as it is in the loss alone, half precision times a power of two in the
-// gradient).  M_TWO: fp32 as two half-precision terms.  M_FEW: the gradient of few rows of bf16, whose time is the
+// How operands are held. M_ONE: one term (bf16 as it is in the loss alone, half precision times a power of two in the
+// gradient). M_TWO: fp32 as two half-precision terms. M_FEW: the gradient of few rows of bf16, whose time is the
 // vocabulary's way through memory: W is read in place, by both products that want it, exponentials are float and dz two
-// bf16 terms against one of W and h.  That saves writing W once more and reading that, and costs wider exponentials and a
-// product more of dz each.  So it is for 16-byte aligned W of 24 MB and more, with eight columns to a row at least, and up to
-// 128 rows (half precision beside it: 1 row of 66235x2624 364 and 245 us, 128 rows 401 and 309; 128 rows of 16384x1024 77
-// and 73; but 16 rows of 33550x320 61 and 64 us, 128 rows 72 and 84, of 4096x512 44 and 49).
-// M_THIN: very few rows, without the tensor cores (below).
+// bf16 terms against one of W and h. That saves writing W once more and reading that, and costs wider exponentials and
+// a product more of dz each. So it is for 16-byte aligned W of 24 MB and more, with eight columns to a row at least,
+// and up to 128 rows (half precision beside it: 1 row of 66235x2624 364 and 245 us, 128 rows 401 and 309; 128 rows of
+// 16384x1024 77 and 73; but 16 rows of 33550x320 61 and 64 us, 128 rows 72 and 84, of 4096x512 44 and 49). M_THIN: very
+// few rows, without the tensor cores (below).
 enum { M_ONE = 1, M_TWO, M_FEW, M_THIN };
 __host__ __device__ constexpr bool of_logits(int kind) { return kind == P_SUMS || kind == P_EXP; }
 __host__ __device__ constexpr int terms_a(int mode, int kind) { return mode == M_TWO || (mode == M_FEW && kind >= P_DH) ? 2 : 1; }
@@ -77,11 +81,12 @@ __host__ __device__ constexpr int products_of(int mode) { return mode == M_TWO ?
 constexpr int kFewRows = 128;
 constexpr int kThinRows = 8, kThinColumns = 64;
 constexpr int64_t kFewNumbers = 12 << 20;
-// Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long as
-// the vocabulary's way through memory (loss of 16 rows of 32768x2048 bf16 36.5 us by pairs, 33.7 by CTAs, fp32 174 and 155;
-// gradients of 128 rows fp32 358 and 340; of 128 rows of 4096x512 fp32, whose 16 tiles leave most CTAs idle, 60 and 69).
+// Up to 128 rows are one CTA's: the other of a pair would multiply nothing, and the products of 256 rows take as long
+// as the vocabulary's way through memory (loss of 16 rows of 32768x2048 bf16 36.5 us by pairs, 33.7 by CTAs, fp32 174
+// and 155; gradients of 128 rows fp32 358 and 340; of 128 rows of 4096x512 fp32, whose 16 tiles leave most CTAs idle,
+// 60 and 69).
 __host__ __device__ constexpr uint32_t plane_b(bool pair) { return pair ? kPlaneBytes : 2 * kPlaneBytes; }     // a term of B in a CTA
-// Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none).  A of
+// Shared memory: the stages' shares of A, theirs of B, the epilogue's buffers (of which the sums alone need none). A of
 // few rows is short: its instructions read on into what follows, and nobody reads what comes of that.
 constexpr int kStagesMax = 12;
 constexpr size_t kSmemMost = 225 * 1024;
@@ -91,20 +96,20 @@ constexpr int stages_for(int buffers, uint32_t stage) {
   return n < kStagesMax ? n : kStagesMax;
 }
 // Buffers of an epilogue warp: one, which leaves the most stages, unless a tile has so few K blocks that its way out is
-// what takes the time (dW of 66235x2048 bf16: 200 rows 97 us with one, 95 with two and four; 500 rows 112, 124, 144; the
-// exponentials of 2048 rows of 32768x768 91, 86, 96 and of 32768x1024 99, 103, 121; of fp32 x1024 282, 277, 444).
+// what takes the time (dW of 66235x2048 bf16: 200 rows 97 us with one, 95 with two and four; 500 rows 112, 124, 144;
+// the exponentials of 2048 rows of 32768x768 91, 86, 96 and of 32768x1024 99, 103, 121; of fp32 x1024 282, 277, 444).
 constexpr int buffers_for(int mode, int kind, int blocks_k) {
   if (kind == P_SUMS) return 0;
   return (kind == P_EXP && blocks_k <= (mode == M_TWO ? 24 : 12)) || (kind == P_DW && blocks_k <= 4) ? 2 : 1;
 }
 
-// K blocks that one accumulator takes.  Each instruction cuts the sum off at its last place, always towards zero: the
-// losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and 3.8e-7
-// with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
-// 8.7e-7 (1.10 and 1.12 ms).  Few rows, whose losses no others average out, take half as many, and a quarter where a CTA has
-// them all and it costs nothing: 16 rows of 32768x2048 1.6e-7 (3.4e-7 with half, 7.5e-7 with all) in 33.8 us, 200 rows 3.7e-7
-// (1.8e-7 in 49 us of 43).  dz of bf16 operands has 11 bits: its sums have 512 instructions, 2^-15 at the worst, and are
-// read out seldom.
+// K blocks that one accumulator takes. Each instruction cuts the sum off at its last place, always towards zero: the
+// losses of 8192x32768x2048 bf16 are 1.6e-6 from 64 bits with 128 instructions an accumulator, 7.8e-7 with 64 and
+// 3.8e-7 with 32, at 811, 810 and 837 us; two terms with 96 instructions leave 1.8e-6 in dW of 2048x32768x1024, with 48
+// 8.7e-7 (1.10 and 1.12 ms). Few rows, whose losses no others average out, take half as many, and a quarter where a CTA
+// has them all and it costs nothing: 16 rows of 32768x2048 1.6e-7 (3.4e-7 with half, 7.5e-7 with all) in 33.8 us, 200
+// rows 3.7e-7 (1.8e-7 in 49 us of 43). dz of bf16 operands has 11 bits: its sums have 512 instructions, 2^-15 at the
+// worst, and are read out seldom.
 constexpr int piece_blocks(int mode, int kind, int rows) {
   const bool few = rows <= kTile;
   return mode == M_TWO ? (few ? 2 : 4) : (of_logits(kind) ? (rows <= kHalf ? 4 : (few ? 8 : 16)) : 128 / products_of(mode));
@@ -135,9 +140,9 @@ __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   if (max_bits == 0 || e > 127) return 0;
   return 13 - e > 126 ? 126 : 13 - e;
 }
-// ... of a row of h, or of W whole, whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up to 2^7,
-// 2^-9), which is written while it is looked at; where the largest lies elsewhere it is written again.  What is lost then
-// lies below 2^-30 for bf16, whose 8 bits fit (2^-33 for the second of two terms).
+// ... of a row of h, or of W whole, whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up
+// to 2^7, 2^-9), which is written while it is looked at; where the largest lies elsewhere it is written again. What is
+// lost then lies below 2^-30 for bf16, whose 8 bits fit (2^-33 for the second of two terms).
 __host__ __device__ constexpr int usual_exponent(int terms) { return terms == 1 ? 6 : 8; }
 __device__ __forceinline__ bool unusual(unsigned most, int terms) {
   const int e = (int)(most >> 23) - 127 + usual_exponent(terms);
@@ -146,17 +151,18 @@ __device__ __forceinline__ bool unusual(unsigned most, int terms) {
 __device__ __forceinline__ int operand_exponent(unsigned most, int terms) {
   return unusual(most, terms) ? range_exponent(most) : usual_exponent(terms);
 }
-// ... of a row's dz, by its weight (any finite one above 2^-113 to 2^13 .. 2^14); dz of float exponentials that are bf16 numbers
-// or floats has that type's range, and no power
+// ... of a row's dz, by its weight (any finite one above 2^-113 to 2^13 .. 2^14); dz of float exponentials that are
+// bf16 numbers or floats has that type's range, and no power
 __device__ __forceinline__ int weight_exponent(unsigned bits) {
   const int e = (int)(bits >> 23) - 127;
   return e > 127 ? 0 : (13 - e > 126 ? 126 : 13 - e);
 }
 __device__ __forceinline__ int weight_exponent(float g) { return weight_exponent(__float_as_uint(fabsf(g))); }
-// Rows of h and of dz have powers of two of their own: the logits' epilogue and the last kernel of dh, whose lanes have a row,
-// take them out.  dW's sums run over the rows.  Where these are of one size, dz and h have one power each in truth; else dW
-// takes h from an operand of its own, in which each row lies as far down as its dz was taken up, under one power for all: the
-// rows whose |g| |h| is largest are brought to 2^13 .. 2^14, and what others lose there is small beside those.
+// Rows of h and of dz have powers of two of their own: the logits' epilogue and the last kernel of dh, whose lanes have
+// a row, take them out. dW's sums run over the rows. Where these are of one size, dz and h have one power each in
+// truth; else dW takes h from an operand of its own, in which each row lies as far down as its dz was taken up, under
+// one power for all: the rows whose |g| |h| is largest are brought to 2^13 .. 2^14, and what others lose there is small
+// beside those.
 __device__ __forceinline__ bool of_one_size(const LossInfo* info) {
   return info->uneven == 0 && weight_exponent(info->g_max) == weight_exponent(0x7fffffffu - info->g_far);
 }
@@ -218,9 +224,10 @@ struct alignas(64) ProductArgs {
   int64_t ld_partial;
 };
 
-// How dh's tiles are laid over the pairs (CTAs, of few rows): waves of whole tiles, then the rest of them with K in shares, so that the last
-// wave is as short as the others leave it (4096 rows and 2048 columns are 128 tiles on 74 pairs: 1.75 waves with the last
-// 54 in four, 2 without).  The shares' sums, beyond the first, lie in blocks of their own and are added in order.
+// How dh's tiles are laid over the pairs (CTAs, of few rows): waves of whole tiles, then the rest of them with K in
+// shares, so that the last wave is as short as the others leave it (4096 rows and 2048 columns are 128 tiles on 74
+// pairs: 1.75 waves with the last 54 in four, 2 without). The shares' sums, beyond the first, lie in blocks of their
+// own and are added in order.
 struct DhPlan { int whole, rest, shares; };
 constexpr int share_blocks(int pairs) { return 4 * pairs; }      // most of them
 // (a warp calls it, a lane a number of shares)
@@ -252,9 +259,10 @@ __device__ __forceinline__ int unit_count(const ProductArgs& p, int live, const 
   if (KIND == P_DH) return plan.whole + plan.rest * plan.shares;
   return (live + kTile - 1) / kTile * p.tiles_n;
 }
-// Tiles that run at the same time share operands in L2.  Logits: as many tiles of rows as L2 holds go through the
+// Tiles that run at the same time share operands in L2. Logits: as many tiles of rows as L2 holds go through the
 // vocabulary together, which is read once for them (8192x32768x2048 bf16: 33 MB of rows at once 771 us, 8 tiles of rows
-// 807 us).  dh: tiles of the same rows of dz, or of the same share of K.  dW: a tile of the vocabulary with all its columns.
+// 807 us). dh: tiles of the same rows of dz, or of the same share of K. dW: a tile of the vocabulary with all its
+// columns.
 template <int KIND>
 __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live, const DhPlan& plan) {
   Unit w;
@@ -291,7 +299,8 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& p, int u, int live, c
   return w;
 }
 
-// K blocks of each of a tile's pieces: as even as they come, since a short one leaves the products waiting for the epilogue
+// K blocks of each of a tile's pieces: as even as they come, since a short one leaves the products waiting for the
+// epilogue
 __device__ __forceinline__ int piece_of(const ProductArgs& p, const Unit& w) {
   const int n = w.kb1 - w.kb0, pieces = (n + p.most_blocks - 1) / p.most_blocks;
   return pieces > 1 ? (n + pieces - 1) / pieces : p.most_blocks;
@@ -448,9 +457,10 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
   constexpr bool kTurnedA = KIND == P_DW, kTurnedB = KIND == P_DH || KIND == P_DW;      // K across the rows in memory
   // (registers change hands inside the branches: where paths meet the compiler counts on the fewer)
   if (warp < kFirstEpi) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
-  // The copies' and the products' loops are run by whole warps, and one lane is elected for the instructions themselves:
-  // addresses are then the warp's, in uniform registers, where a loop of one lane moves every operand there first (61
-  // cycles a product and 66 a commit; a K block's four and their waits came to 470 of the 512 that the products take).
+  // The copies' and the products' loops are run by whole warps, and one lane is elected for the instructions
+  // themselves: addresses are then the warp's, in uniform registers, where a loop of one lane moves every operand there
+  // first (61 cycles a product and 66 a commit; a K block's four and their waits came to 470 of the 512 that the
+  // products take).
   if (warp == 0 || warp == 2) {
     // ---------------- copies: A's by one warp, B's by another ----------------
     const bool of_a = warp == 0;
@@ -552,8 +562,9 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     }
     const float mantissa = factor;
     const bool rises = mantissa >= 0.f;             // (the same of all rows, whose logits then go the same way)
-    // Blocks of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the warp's buffers in turn: `group` of
-    // them at a time, since the fence between their stores and the copy engine is what a short tile waits for.
+    // Blocks of 32 rows of 128 bytes, this lane's row in eight pieces of 16 bytes, into the warp's buffers in turn:
+    // `group` of them at a time, since the fence between their stores and the copy engine is what a short tile waits
+    // for.
     auto free_buffers = [&](int group) {
       if (lane == 0) {
         if (buffers > group) bulk_wait_read_but_one();
@@ -583,7 +594,8 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
         st_shared_v4(at + piece_at((uint32_t)lane, q), pack(v[8 * q], v[8 * q + 1]), pack(v[8 * q + 2], v[8 * q + 3]), pack(v[8 * q + 4], v[8 * q + 5]),
                      pack(v[8 * q + 6], v[8 * q + 7]));
     };
-    // all of a lane's columns from `acc` to `map`, those before `most`, two blocks a fence where the warp has the buffers
+    // all of a lane's columns from `acc` to `map`, those before `most`, two blocks a fence where the warp has the
+    // buffers
     auto store_all = [&](const float* acc, auto lay, auto columns, const CUtensorMap* map, int col, int row, int most) {
       constexpr int kCols = decltype(columns)::value;
       if (kPairs && buffers >= 2) {
@@ -702,16 +714,16 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           float shift = 15.f - power;
           if (__any_sync(0xffffffffu, here || far)) {
             float below = -power;
-            // Exponentials reach 2^15, near the end of half precision.  Logits beyond 2^22 are rounded by half of one and more, as
-            // their power was: a lane that has some goes on with the rounded ones' differences to it.
+            // Exponentials reach 2^15, near the end of half precision. Logits beyond 2^22 are rounded by half of one
+            // and more, as their power was: a lane that has some goes on with the rounded ones' differences to it.
             if (__any_sync(0xffffffffu, far)) {
               const float way = rises ? 1.f : -1.f;
 #pragma unroll
               for (int i = 0; i < kSumColumns; ++i) acc[i] = far ? __fadd_rn(__fmul_rn(acc[i], factor), -power) * way : acc[i];
               if (far) { factor = way; shift = 15.f; below = 0.f; }
             }
-            // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row that is
-            // sure of it is what the others' terms add to one, with no difference of two logits in it
+            // the target's term stays out of the sum, and its logit is kept relative to the power: the loss of a row
+            // that is sure of it is what the others' terms add to one, with no difference of two logits in it
             float zt = 0.f;
             const float gone = rises ? -INFINITY : INFINITY;
 #pragma unroll
@@ -1048,7 +1060,8 @@ __device__ __forceinline__ void stage_weight(const Operands<T>& o) {
   if (SCALED && !AGAIN) block_largest(m, &o.info->w_max);
 }
 
-// The rows of h, `row_threads` each (8, 32 or 256), under a power of two each.  AGAIN: for dW, where they are not of one size.
+// The rows of h, `row_threads` each (8, 32 or 256), under a power of two each. AGAIN: for dW, where they are not of one
+// size.
 template <typename T, int TERMS, bool SCALED, bool WIDE, bool AGAIN>
 __device__ __forceinline__ void stage_rows(const Operands<T>& o) {
   __shared__ unsigned warp_m[2][8];
@@ -1456,15 +1469,15 @@ dw_rows_kernel(LossArgs a, const float* blocks, int tiles_n, int shares, int mod
 }
 
 // ---- very few rows ----------------------------------------------------------------------------
-// Up to 8 rows of fp32.  As operands W passes memory three times for the loss and five for the gradient; here each kernel
-// reads it once (or writes dW), in fp32 throughout, and the CUDA cores' multiplications stay below the time of that.  Beside
-// the products: loss of 32768x2048 59 us of 1 row, 81 of 8 (154), gradient 179 and 213 us (276); of 848x512 17 (33) and 32
-// (57); of 131072x100 gradient 108 and 165 (157).  16 rows took 155 and 325 us (154, 277), as bf16 rows off the copy engine's
-// boundaries did (8 rows of 33620x1615 gradient 272 us, 199 as operands).
-// Bound by memory: 8 rows' logits 3.4 TB/s (their h out of shared memory takes as long as the multiplications), 4 rows' 4.2;
-// dh 6.0 and 4.4 TB/s, eight rows of W under way a thread; dW 5.6.  (Tiles of 32 logits, which divide evenly among the blocks,
-// were no faster: 62 us of 1 row.)
-// A thread's four numbers of a group of 4 * STRIDE: together where rows allow 16 bytes at a time, else STRIDE apart.
+// Up to 8 rows of fp32. As operands W passes memory three times for the loss and five for the gradient; here each
+// kernel reads it once (or writes dW), in fp32 throughout, and the CUDA cores' multiplications stay below the time of
+// that. Beside the products: loss of 32768x2048 59 us of 1 row, 81 of 8 (154), gradient 179 and 213 us (276); of
+// 848x512 17 (33) and 32 (57); of 131072x100 gradient 108 and 165 (157). 16 rows took 155 and 325 us (154, 277), as
+// bf16 rows off the copy engine's boundaries did (8 rows of 33620x1615 gradient 272 us, 199 as operands). Bound by
+// memory: 8 rows' logits 3.4 TB/s (their h out of shared memory takes as long as the multiplications), 4 rows' 4.2; dh
+// 6.0 and 4.4 TB/s, eight rows of W under way a thread; dW 5.6. (Tiles of 32 logits, which divide evenly among the
+// blocks, were no faster: 62 us of 1 row.) A thread's four numbers of a group of 4 * STRIDE: together where rows allow
+// 16 bytes at a time, else STRIDE apart.
 template <bool WIDE, int STRIDE>
 __device__ __forceinline__ int place(int i, int j) { return WIDE ? 4 * i + j : i + STRIDE * j; }
 __device__ __forceinline__ void load_wide(const float* from, float (&x)[4]) {
@@ -1482,7 +1495,8 @@ __device__ __forceinline__ void load_four(const float* from, int i, int left, fl
     for (int j = 0; j < 4; ++j) x[j] = i + STRIDE * j < left ? from[i + STRIDE * j] : 0.f;
   }
 }
-// Sums over a warp's lanes of N numbers each: afterwards a lane has number (lane * N + i) / 32 in v[i], i < N / 32 or one
+// Sums over a warp's lanes of N numbers each: afterwards a lane has number (lane * N + i) / 32 in v[i], i < N / 32 or
+// one
 template <int N>
 __device__ __forceinline__ void sum_lanes(float (&v)[N], int lane) {
   int m = N;
@@ -1504,8 +1518,8 @@ __device__ __forceinline__ void sum_lanes(float (&v)[N], int lane) {
   }
 }
 
-// What P_SUMS (and, with `e`, P_EXP) leave, by blocks of 64 logits: a warp takes four rows of W at a time against all rows
-// of h, which lie in shared memory, whole or `chunk` columns of them.
+// What P_SUMS (and, with `e`, P_EXP) leave, by blocks of 64 logits: a warp takes four rows of W at a time against all
+// rows of h, which lie in shared memory, whole or `chunk` columns of them.
 template <int R, bool WIDE>
 __global__ void __launch_bounds__(512, 1)
 thin_logits_kernel(const float* h, int64_t ld_h, const float* w, int64_t ld_w, int rows, int vocab, int dim, int chunk, float factor, LossInfo* info,
@@ -2040,8 +2054,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
                      (int)a.rows, l.staged_rows, dh, a.ld_dh, l.info, 0, 0};
     auto aligned = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0; };
     const bool rows16 = aligned(h, a.ld_h) && aligned(w, a.ld_w) && a.dim * (int64_t)sizeof(T) % 16 == 0;
-    // a warp a row of h, a quarter of one a short row (16384 rows of 64: 5.2 us, by warps 12.4), a block a long one (1003 rows of 515
-    // fp32 are no faster by blocks: 10.9 us, by warps 9.3)
+    // a warp a row of h, a quarter of one a short row (16384 rows of 64: 5.2 us, by warps 12.4), a block a long one
+    // (1003 rows of 515 fp32 are no faster by blocks: 10.9 us, by warps 9.3)
     o.row_threads = l.padded <= (rows16 ? 256 : 64) ? 8 : (l.padded <= 2048 ? 32 : 256);
     // blocks by the operands' shares of the work, eight a multiprocessor at the most of either
     const int64_t most = 8 * (int64_t)sm_count(), want_w = ((int64_t)o.vocab * (l.padded / 8) + 511) / 512, want_h = ceil_div(a.rows + kTile, 256 / o.row_threads);
@@ -2135,8 +2149,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       if (a.rows > 0) {
         if (gradient) {
           MW_TRY((run_product<TERMS, P_EXP>(l.few, single, logits, tm * logits.tiles_n, s)));
-          // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of them waits of
-          // one row after another), several where rows are few (1 of 66235: 24 us, 10 in 17)
+          // A warp a row of up to 4096 logits, a block a longer one (9234 rows of 2882, a block each: 51 us, most of
+          // them waits of one row after another), several where rows are few (1 of 66235: 24 us, 10 in 17)
           const bool short_rows = a.vocab <= 4096 && l.piece > 2 * sm_count();
           const int most = 2 * sm_count() / l.piece, parts = ceil_div(l.vpadded, TERMS == 2 || l.few ? 4096 : 8192);
           const int slices = short_rows || most < 2 ? 1 : (most < parts ? most : parts);
