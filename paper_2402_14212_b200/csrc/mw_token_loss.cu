@@ -151,8 +151,8 @@ __device__ __forceinline__ bool unusual(unsigned most, int terms) {
 __device__ __forceinline__ int operand_exponent(unsigned most, int terms) {
   return unusual(most, terms) ? range_exponent(most) : usual_exponent(terms);
 }
-// ... of a row's dz, by its weight (any finite one above 2^-113 to 2^13 .. 2^14); dz of float exponentials that are
-// bf16 numbers or floats has that type's range, and no power
+// ... of a row's dz, by its weight (any finite one above 2^-113 to 2^13 .. 2^14). dz of few rows, bf16 numbers with their
+// range, has one power by the largest weight, and of very few rows, floats, none.
 __device__ __forceinline__ int weight_exponent(unsigned bits) {
   const int e = (int)(bits >> 23) - 127;
   return e > 127 ? 0 : (13 - e > 126 ? 126 : 13 - e);
@@ -170,8 +170,8 @@ __device__ __forceinline__ int common_exponent(const LossInfo* info) { return in
 // what dW's sums are too large by (NaN where a wait ran out before)
 __device__ __forceinline__ float dweight_factor(const LossInfo* info, double scale, bool scaled, int terms) {
   if (info->st.code != 0) return __int_as_float(0x7fffffff);
-  if (!scaled) return (float)scale;
-  const int e = of_one_size(info) ? usual_exponent(terms) + weight_exponent(info->g_max) : common_exponent(info);
+  const int same = weight_exponent(info->g_max);
+  const int e = !scaled ? same : (of_one_size(info) ? usual_exponent(terms) + same : common_exponent(info));
   return fminf(fmaxf((float)ldexp(scale, -e), -3e38f), 3e38f);
 }
 
@@ -710,7 +710,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
           const int t = target - col0;
           const bool here = on && t >= 0 && t < valid;
           const float power = power_of(m);
-          const bool far = fabsf(power) >= 4194304.f;
+          const bool far = on && fabsf(power) >= 4194304.f;
           float shift = 15.f - power;
           if (__any_sync(0xffffffffu, here || far)) {
             float below = -power;
@@ -1299,7 +1299,7 @@ dz_kernel(LossInfo* info, int first, int piece, const float2* sums, int sum_bloc
       loss[row[i]] = end.loss;
       part[i] = (double)g[i] * (double)end.loss;
     }
-    const float gi = g[i] * (MODE == M_ONE || MODE == M_TWO ? power_of_two(weight_exponent(g[i])) : 1.f), at_target = -gi * end.less, share = gi / end.total;
+    const float gi = g[i] * (MODE == M_THIN ? 1.f : power_of_two(MODE == M_FEW ? weight_exponent(info->g_max) : weight_exponent(g[i]))), at_target = -gi * end.less, share = gi / end.total;
     // (four accesses of a thread under way)
     constexpr int kAhead = 4;
     if (TERMS == 1) {
@@ -1412,7 +1412,7 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
       }
     }
     // (two factors: their product may lie below a float's range where dh does not)
-    int x = exponent - (a.scaled ? weight_exponent(g[first + r]) : 0);
+    int x = exponent - (a.scaled ? weight_exponent(g[first + r]) : weight_exponent(info->g_max));
     x = x < -250 ? -250 : (x > 250 ? 250 : x);
     const float f1 = mantissa * power_of_two(x / 2), f2 = power_of_two(x - x / 2);
     v.x = v.x * f1 * f2; v.y = v.y * f1 * f2; v.z = v.z * f1 * f2; v.w = v.w * f1 * f2;

@@ -133,3 +133,17 @@ def test_operands_near_the_ends_of_the_range(size, N, dtype):
     h[3] *= 2.0 ** (-size // 2)
     want = meeting(reference(h, W, t), h, W, t, torch.full((N,), 1 / N, device="cuda"))
     check(mwb.token_loss_gradient(h, W, t), want, ALL)
+
+
+SIZED = [(8, F32, 700, 128), (100, F32, 700, 128), (300, BF16, 700, 128), (20, BF16, 12353, 1088)]
+
+
+@pytest.mark.parametrize("size,N,dtype,V,D", [(2.0 ** x, *s) for x in (-108, 100) for s in SIZED] + [(2.0 ** -114, *s) for s in SIZED[1:]])
+def test_weights_near_the_ends_of_the_range(size, N, dtype, V, D):
+    """W lies so that dh of weight one is of the size of 1 / size: what is formed of them does not end where they do."""
+    h, W, t = make(N, V, D, dtype, seed=N, lean=4.0)
+    h, W = h * size, W * (1 / size)
+    w = (torch.rand(N, device="cuda") + 0.5) * size
+    one = reference(h, W, t, weight=torch.ones(N, device="cuda"))
+    r = mwb.token_loss_gradient(h, W, t, row_weight=w, want=(True, False))
+    check(r, by_weight(one, w), ("loss", "dh"))
