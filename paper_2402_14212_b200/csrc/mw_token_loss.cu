@@ -2137,7 +2137,8 @@ mw_status loss_run(const mw_token_loss_desc* d, const T* h, const T* w, const I*
       by_w.shares = dw_shares(by_w.tiles_m * by_w.tiles_n, by_w.blocks_k, pairs);
       if (by_w.shares > 1) by_w.out = by_w.acc = by_h.acc;
       by_w.dw = dw; by_w.ld_dw = a.ld_dw; by_w.dw_bf16 = dw_bf16;
-      by_w.dw_engine = by_w.shares == 1 && ((uintptr_t)dw & 15) == 0 && (a.ld_dw * dw_size) % 16 == 0;
+      // (the copy engine ends a row at 16 bytes, which may lie beyond its last column)
+      by_w.dw_engine = by_w.shares == 1 && ((uintptr_t)dw & 15) == 0 && (a.ld_dw * dw_size) % 16 == 0 && (int64_t)a.dim * dw_size % 16 == 0;
       if (by_w.dw_engine && dw)
         MW_TRY(out_map(&by_w.out, dw_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, dw_size, dw, a.dim, a.vocab, a.ld_dw));
       by_w.partial = l.dw; by_w.ld_partial = l.padded;
