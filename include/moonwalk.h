@@ -467,11 +467,12 @@ mw_status mw_embedding_backward(const mw_embedding_desc* desc, const void* token
  * rows / 256 times vocab / 64 is at most 2^30.  A value that is not finite stays in the losses and dh of the rows it enters
  * (and in dweight); an infinity may come out as NaN.  The logits are never held whole: the loss alone keeps two numbers for 128
  * of them, the gradient a piece of rows at a time, which is turned into dz in its place.
- * Digits: float operands are held to 22 bits (bf16 ones as they are), or to 2^-23 of the largest number of their row of h, or
- * of all of weight, where that is more; in dweight rows of h, times their weights, to 2^-23 of the largest of all.  dz is held
- * to 22 bits, of bf16 operands to 11 (dh and dweight are then 1.5e-4 from 64 bits before their last rounding, and so is a
- * float dweight); sums are float.  A row's loss and dh keep these whatever the size of the other rows and their weights.  Up to 8
- * rows of float operands have 32 bits throughout, up to 128 of bf16 over a large weight 16 bits of dz. */
+ * Digits: float operands are held to 22 bits (bf16 ones as they are), or to 2^-29 of the largest number of their row of h
+ * and 2^-23 of the largest of all of weight, where that is more; in dweight a row of h, times its weight, also to 2^-37 of
+ * the largest of all.  dz is held to 22 bits, of bf16 operands to 11 (dh and dweight are then 1.5e-4 from 64 bits before their
+ * last rounding, and so is a float dweight); sums are float.  A row's loss and dh keep these whatever the size of the other
+ * rows and their weights.  Up to 8 rows of float operands have 32 bits throughout, up to 128 of bf16 over a large weight 16
+ * bits of dz. */
 typedef struct {
   int64_t rows;               /* 0..2^24 */
   int32_t vocab, dim;         /* 1..2^24, 1..2^16 */

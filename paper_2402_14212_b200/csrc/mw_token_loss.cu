@@ -140,16 +140,19 @@ __device__ __forceinline__ int range_exponent(unsigned max_bits) {
   if (max_bits == 0 || e > 127) return 0;
   return 13 - e > 126 ? 126 : 13 - e;
 }
-// ... of a row of h, or of W whole, whose numbers have the usual size (bf16: up to 2^9 and down to 2^-7; two terms: up
-// to 2^7, 2^-9), which is written while it is looked at; where the largest lies elsewhere it is written again. What is
-// lost then lies below 2^-30 for bf16, whose 8 bits fit (2^-33 for the second of two terms).
+// ... of a row of h, or of W whole, whose numbers have the usual size, which is written while it is looked at; where the
+// largest lies elsewhere it is written again. What is lost lies below 2^-25 of what is written, so the least that is left
+// as it is sets the digits of small numbers: 2^-29 of the largest of its row for h, whose rows are written again at once
+// (two terms: largest numbers of 2^-4 to 2^7, bf16 2^-2 to 2^9); 2^-23 of the largest for W, which takes a pass more (2^-10
+// and 2^-8 on).
 __host__ __device__ constexpr int usual_exponent(int terms) { return terms == 1 ? 6 : 8; }
-__device__ __forceinline__ bool unusual(unsigned most, int terms) {
+constexpr int kLeastOfRow = 4, kLeastOfWeight = -2;
+__device__ __forceinline__ bool unusual(unsigned most, int terms, int least) {
   const int e = (int)(most >> 23) - 127 + usual_exponent(terms);
-  return most != 0 && (e > 14 || e < -2);
+  return most != 0 && (e > 14 || e < least);
 }
-__device__ __forceinline__ int operand_exponent(unsigned most, int terms) {
-  return unusual(most, terms) ? range_exponent(most) : usual_exponent(terms);
+__device__ __forceinline__ int operand_exponent(unsigned most, int terms, int least) {
+  return unusual(most, terms, least) ? range_exponent(most) : usual_exponent(terms);
 }
 // ... of a row's dz, by its weight (any finite one above 2^-113 to 2^13 .. 2^14). dz of few rows, bf16 numbers with their
 // range, has one power by the largest weight, and of very few rows, floats, none.
@@ -558,7 +561,7 @@ loss_products_kernel(const __grid_constant__ ProductArgs p) {
     if (KIND == P_DW) factor = dweight_factor(p.info, p.scale, p.scaled, kTermsB);
     if (of_logits(KIND)) {
       factor = (float)frexp((double)p.scale * 1.4426950408889634, &exponent);
-      if (p.scaled) exponent -= operand_exponent(p.info->w_max, kTermsB);
+      if (p.scaled) exponent -= operand_exponent(p.info->w_max, kTermsB, kLeastOfWeight);
     }
     const float mantissa = factor;
     const bool rises = mantissa >= 0.f;             // (the same of all rows, whose logits then go the same way)
@@ -1030,7 +1033,7 @@ __device__ __forceinline__ void stage_weight(const Operands<T>& o) {
   if (SCALED) {
     e = usual_exponent(TERMS);
     if (AGAIN) {
-      if (!unusual(o.info->w_max, TERMS)) return;
+      if (!unusual(o.info->w_max, TERMS, kLeastOfWeight)) return;
       e = range_exponent(o.info->w_max);
     }
   }
@@ -1125,9 +1128,9 @@ __device__ __forceinline__ void stage_rows(const Operands<T>& o) {
         __syncthreads();
         m = __reduce_max_sync(0xffffffffu, warp_m[turn][lane & 7]);
       }
-      const bool other = unusual(m, TERMS);
+      const bool other = unusual(m, TERMS, kLeastOfRow);
       if (other) pass(std::false_type{}, range_exponent(m));
-      if (on && thread == 0) o.row_exponent[r] = operand_exponent(m, TERMS);
+      if (on && thread == 0) o.row_exponent[r] = operand_exponent(m, TERMS, kLeastOfRow);
       if (m && fabsf(o.g[r]) < INFINITY) reach = max(reach, (unsigned)(1024 + (int)(m >> 23) - 127 - weight_exponent(o.g[r])));
       uneven |= other;
     }
@@ -1394,7 +1397,7 @@ dh_rows_kernel(LossArgs a, const float* slab, const float* shares, int padded, i
   live = live < 0 ? 0 : (live < piece ? live : piece);
   int exponent = 0;
   float mantissa = (float)frexp((double)a.scale, &exponent);
-  if (a.scaled) exponent -= operand_exponent(info->w_max, terms_b(mode));
+  if (a.scaled) exponent -= operand_exponent(info->w_max, terms_b(mode), kLeastOfWeight);
   if (info->st.code != 0) mantissa = __int_as_float(0x7fffffff);
   const DhPlan plan = dh_plan(live, tiles_n, blocks_k, workers, room, products_of(mode));
   const uint32_t per = (uint32_t)(a.dim + 3) / 4;

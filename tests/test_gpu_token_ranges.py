@@ -4,7 +4,9 @@ beside it, in h or among the row weights.
 Tolerances are those of test_gpu_token_loss.py, without what they allow a row for the weights of others: dh_i = g_i times the
 dh_i of weight one, so its bound is |g_i| times the bound there.  In dweight the rows meet: h_i times 2^x, x by its weight,
 is held in half precision (two terms of float operands) with the largest number at 2^13 and more, so each is off by 2^-25 of
-that scale, and its dz, relative to its weight at most |p - [j = t]|, times 2^14: 2^-37 max_i(|g_i| max |h_i|) sum_i |p_ij - [j = t_i]|."""
+that scale, and its dz, relative to its weight at most |p - [j = t]|, times 2^14: 2^-37 max_i(|g_i| max |h_i|) sum_i |p_ij - [j = t_i]|.
+Where all rows are of the usual size that operand is the logits', whose rows have their largest number at 2^4 and more: each
+is off by 2^-25 of that scale, 2^-29 of its row's largest: 2^-29 sum_i |g_i| max |h_i| |p_ij - [j = t_i]|."""
 import pytest
 import torch
 
@@ -23,10 +25,10 @@ def by_weight(want, w):
 def meeting(want, h, W, t, w, scale=1.0):
     """dweight's bound with what rows of different sizes lose there."""
     p = torch.softmax(scale * h.double() @ W.double().T, 1)
-    d = p.scatter_add(1, t[:, None], -torch.ones(len(t), 1, device="cuda", dtype=torch.float64)).abs().sum(0)
+    d = p.scatter_add(1, t[:, None], -torch.ones(len(t), 1, device="cuda", dtype=torch.float64)).abs()
     value, bound = want["dweight"]
-    most = float((w.double().abs() * h.double().abs().amax(1)).max())
-    return dict(want, dweight=(value, bound + 2.0 ** -37 * most * abs(scale) * d[:, None]))
+    size = w.double().abs() * h.double().abs().amax(1)
+    return dict(want, dweight=(value, bound + abs(scale) * (2.0 ** -37 * size.max() * d.sum(0) + 2.0 ** -29 * size @ d)[:, None]))
 
 
 @pytest.mark.parametrize("N,dtype", [(5, F32), (9, F32), (100, F32), (300, F32), (9, BF16), (129, BF16), (300, BF16)])
@@ -147,3 +149,17 @@ def test_weights_near_the_ends_of_the_range(size, N, dtype, V, D):
     one = reference(h, W, t, weight=torch.ones(N, device="cuda"))
     r = mwb.token_loss_gradient(h, W, t, row_weight=w, want=(True, False))
     check(r, by_weight(one, w), ("loss", "dh"))
+
+
+@pytest.mark.parametrize("N,dtype", [(8, F32), (9, F32), (300, F32), (9, BF16), (300, BF16)])
+@pytest.mark.parametrize("size", [-16, -9, -6, -3, 0, 5])
+def test_small_columns_of_rows_of_any_size(size, N, dtype):
+    """Columns of h 2^-14 below the others, which no sum hides in dweight: what they lose goes by their row's largest."""
+    h, W, t = make(N, 333, 128, dtype, seed=N, lean=0.0)
+    h *= 2.0 ** size
+    h[:, :16] *= 2.0 ** -14
+    want = meeting(reference(h, W, t), h, W, t, torch.full((N,), 1 / N, device="cuda"))
+    check(mwb.token_loss_gradient(h, W, t), want, ALL)
+    g = torch.rand(N, device="cuda") + 0.5
+    want = meeting(reference(h, W, t, weight=g), h, W, t, g)
+    check(mwb.token_loss_gradient(h, W, t, row_weight=g), want, ALL)
